@@ -273,6 +273,115 @@ ff_status ff_attention_core_backward(const ff_core_desc* desc, const void* q, co
                                      void* dq, void* dk, void* dv, void* dg, float* dbias,
                                      void* ws, size_t ws_bytes, void* hip_stream);
 
+/* Layer norm in training: the forward pass with the residual sum in front of it and the statistics kept, and the
+ * gradient of both (Section 5.2 names LayerNorm's batch reduction and "bias + dropout + add" as the kernels around
+ * every module; Table 6 counts forward and backward).  Per row of c channels, with s = x (+ residual), rounded to
+ * the tensor dtype:
+ *   mean = sum(s) / c;  rstd = 1 / sqrt(sum((s - mean)^2) / c + ln_eps);  y = (s - mean) rstd gamma + beta
+ * and, for gradients dy = dLoss/dy and dsum = what reaches s by other ways (the residual path around the module):
+ *   u = (s - mean) rstd;  h = dy gamma;  dx = rstd (h - mean(h) - u mean(h u)) (+ dsum)
+ *   dgamma = sum over the rows of dy u;  dbeta = sum over the rows of dy
+ * dx is the gradient of x and of residual alike.  Statistics, sums over channels and over rows are float32; the sums
+ * over rows are formed in an order that depends on rows and c alone, so equal calls give equal bits. */
+typedef struct {
+    int32_t dtype;      /* ff_dtype of x, residual, sum, y, gamma, beta, dy, dsum and dx */
+    int32_t c;          /* 1 .. 8192 */
+    int64_t rows;       /* >= 0 */
+    float   ln_eps;
+} ff_norm_desc;
+
+/*   x, residual  [rows, c]; residual may be NULL
+ *   sum          [rows, c] receives s; given exactly when residual is; may be x itself or residual itself
+ *   y            [rows, c]; must not overlap x, residual or sum
+ *   mean, rstd   float32 [rows], both or neither
+ * Partial overlaps are refused.  FF_EINVAL for bad sizes or NULL pointers, FF_EHIP if the launch fails. */
+ff_status ff_layernorm_forward(const ff_norm_desc* desc, const void* x, const void* residual, const void* gamma,
+                               const void* beta, void* sum, void* y, float* mean, float* rstd, void* hip_stream);
+
+/* Bytes of device workspace ff_layernorm_backward needs (partial sums of dgamma and dbeta); 0 if desc is invalid. */
+size_t ff_layernorm_backward_workspace_bytes(const ff_norm_desc* desc);
+
+/*   s            [rows, c] what the forward pass normalised: its x, or its sum
+ *   mean, rstd   float32 [rows] as the forward pass left them, or both NULL: formed again from s (the fused modules
+ *                of this library keep none)
+ *   dsum         [rows, c] or NULL
+ *   dx           [rows, c]; may be dy itself or dsum itself, must not overlap s
+ *   dgamma, dbeta  float32 [c]; accumulate = 1 adds to what they hold, 0 overwrites it
+ *   ws, ws_bytes   device scratch, 256-byte aligned, at least the size above
+ * rows = 0 gives zero dgamma and dbeta.  Errors as for the other entry points. */
+ff_status ff_layernorm_backward(const ff_norm_desc* desc, const void* s, const void* gamma, const float* mean,
+                                const float* rstd, const void* dy, const void* dsum, void* dx, float* dgamma,
+                                float* dbeta, int32_t accumulate, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The optimiser: AdamW over all tensors of a model at once, with gradients clipped by their common norm.  Evoformer
+ * blocks have some 70 small tensors each; one launch serves all of them.  The tensors are laid out once into a plan
+ * (host memory, which the caller copies to the device and keeps as long as the addresses hold).  Per value, with k = 1 or, if a norm is
+ * given, k = min(1, max_norm / (norm + 1e-6)):
+ *   g' = k g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in float32, each operation rounded by itself.  w is the float32 parameter; or the float32 master copy of a
+ * bfloat16 parameter, which receives its rounding; or the bfloat16 parameter itself.
+ *
+ * state_bits = 32: m and v are float32.  state_bits = 8: a byte for each, and for each 256 values of a tensor (from
+ * its first value on, the last group may be short) a byte of exponent E, the exponent field of the group's largest
+ * magnitude as a float32.  A value x is held as the upper bits of the float32 |x| 2^(14 - E) (m: sign, four bits of
+ * exponent, three of mantissa) or x 2^(30 - E) (v: five of exponent, three of mantissa), subnormals included.  The
+ * step computes with m and v as they are before this rounding.  Which of its two neighbours a value goes to is drawn with
+ * probabilities that keep its mean (16 bits of a hash of the value's index and the step's seed): with beta near 1 a
+ * step changes m and v by less than the nearest code would ever show.  A positive v is never held as 0, so that no
+ * step divides by eps alone.  A group with a value that is not finite is held as NaN.  All bytes 0 are m = v = 0. */
+typedef struct {
+    int32_t param_dtype;   /* ff_dtype of the parameters */
+    int32_t grad_dtype;    /* ff_dtype of the gradients */
+    int32_t state_bits;    /* 32, 8, or 0: gradients alone (a plan for ff_grad_norm) */
+    int32_t n_tensors;     /* >= 0 */
+} ff_adamw_desc;
+
+/* One tensor: dense device memory, each pointer aligned to its own type.  With state_bits = 0 only g and numel count. */
+typedef struct {
+    void*       p;             /* [numel] param_dtype */
+    const void* g;             /* [numel] grad_dtype */
+    float*      master;        /* [numel], FF_BF16 parameters only; NULL = none */
+    void*       m;             /* [numel] float32 or codes */
+    void*       v;
+    uint8_t*    m_exp;         /* [ceil(numel / 256)] with 8-bit states, else NULL */
+    uint8_t*    v_exp;
+    int64_t     numel;         /* >= 0 */
+    float       weight_decay;  /* >= 0 */
+} ff_adamw_tensor;
+
+typedef struct {
+    double   lr, beta1, beta2, eps;   /* lr >= 0; 0 <= beta < 1; eps >= 0 */
+    double   max_norm;                /* > 0; read only if a norm is given */
+    int64_t  step;                    /* 1 for the first step */
+    uint32_t seed;                    /* of the rounding of 8-bit states: another one for each step */
+} ff_adamw_hyper;
+
+/* Bytes of the plan for these tensors (host array of desc->n_tensors entries); 0 if an argument is invalid. */
+size_t ff_adamw_plan_bytes(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors);
+
+/* Writes the plan into host memory (plan_bytes as reported above).  Tensors of one plan must not overlap. */
+ff_status ff_adamw_plan(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors, void* plan, size_t plan_bytes);
+
+/* Bytes of device workspace ff_grad_norm needs. */
+size_t ff_grad_norm_workspace_bytes(void);
+
+/* norm[0] (float32, device) = square root of the sum of the squares of all gradients of the plan, summed in float64 in a fixed order.
+ * plan: device copy, 16-byte aligned, of a plan made with this desc; ws 256-byte aligned. */
+ff_status ff_grad_norm(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* norm, void* ws,
+                       size_t ws_bytes, void* hip_stream);
+
+/* One step over all tensors of the plan.  norm: device, or NULL for gradients as they are; a norm that is not finite
+ * leaves parameters and states as they were.  hyper is read before the call returns, so a captured call repeats its values.  The plan is the
+ * device copy of one made with this desc: under another desc its tensors are left alone. */
+ff_status ff_adamw_step(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, const ff_adamw_hyper* hyper,
+                        const float* norm, void* hip_stream);
+
+/* m and v of all tensors as float32, one tensor after another (for checkpoints and inspection): m_out, v_out hold
+ * the sum of all numel; either may be NULL. */
+ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* m_out, float* v_out,
+                           void* hip_stream);
+
 /* For callers that cannot allocate: code under HIP graph capture, tight serving loops and
  * harnesses that forbid hipMalloc, which therefore have no workspace to hand over.
  * The same module as ff_attention_chunked, with the workspace taken from a device array that is

@@ -59,6 +59,25 @@ class CoreDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("heads", C.c_int32), ("length", C.c_int32), ("head_dim", C.c_int32)]
 
 
+class NormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("c", C.c_int32), ("rows", C.c_int64), ("ln_eps", C.c_float)]
+
+
+class AdamWDesc(C.Structure):
+    _fields_ = [("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("n_tensors", C.c_int32)]
+
+
+ADAMW_POINTERS = ("p", "g", "master", "m", "v", "m_exp", "v_exp")
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ADAMW_POINTERS] + [("numel", C.c_int64), ("weight_decay", C.c_float)]
+
+
+class AdamWHyper(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "max_norm")] + [("step", C.c_int64), ("seed", C.c_uint32)]
+
+
 class FFError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"libff status {status}: {message}")
@@ -109,6 +128,24 @@ def lib() -> C.CDLL:
         L.ff_attention_core_backward_workspace_bytes.argtypes = [C.POINTER(CoreDesc)]
         L.ff_attention_core_backward.restype = C.c_int
         L.ff_attention_core_backward.argtypes = [C.POINTER(CoreDesc)] + [C.c_void_p] * 13 + [C.c_size_t, C.c_void_p]
+        L.ff_layernorm_forward.restype = C.c_int
+        L.ff_layernorm_forward.argtypes = [C.POINTER(NormDesc)] + [C.c_void_p] * 9
+        L.ff_layernorm_backward_workspace_bytes.restype = C.c_size_t
+        L.ff_layernorm_backward_workspace_bytes.argtypes = [C.POINTER(NormDesc)]
+        L.ff_layernorm_backward.restype = C.c_int
+        L.ff_layernorm_backward.argtypes = [C.POINTER(NormDesc)] + [C.c_void_p] * 9 + [C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ff_adamw_plan_bytes.restype = C.c_size_t
+        L.ff_adamw_plan_bytes.argtypes = [C.POINTER(AdamWDesc), C.c_void_p]
+        L.ff_adamw_plan.restype = C.c_int
+        L.ff_adamw_plan.argtypes = [C.POINTER(AdamWDesc), C.c_void_p, C.c_void_p, C.c_size_t]
+        L.ff_grad_norm_workspace_bytes.restype = C.c_size_t
+        L.ff_grad_norm_workspace_bytes.argtypes = []
+        L.ff_grad_norm.restype = C.c_int
+        L.ff_grad_norm.argtypes = [C.POINTER(AdamWDesc), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ff_adamw_step.restype = C.c_int
+        L.ff_adamw_step.argtypes = [C.POINTER(AdamWDesc), C.c_void_p, C.c_size_t, C.POINTER(AdamWHyper), C.c_void_p, C.c_void_p]
+        L.ff_adamw_moments.restype = C.c_int
+        L.ff_adamw_moments.argtypes = [C.POINTER(AdamWDesc), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
         L.ff_attention_path.restype = C.c_char_p
         L.ff_attention_path.argtypes = [C.POINTER(AttnDesc)]
         L.ff_attention_last_path.restype = C.c_char_p
@@ -348,6 +385,197 @@ def ff_gated_attention_residual(desc: AttnDesc, w: Dict[str, "object"], x, z=Non
     _check(lib().ff_gated_attention_residual(C.byref(desc), C.byref(wts), _ptr(x), _ptr(z), _ptr(mask), _ptr(out),
                                              _ptr(ws), ws.numel(), _stream(), chunk_rows))
     return out
+
+
+# ------------------------------------------------------------------------- training: layer norm, clipping, AdamW
+def _want(t, name, dtype=None, shape=None, numel=None, device=None):
+    """The tensor, if a kernel may take it as `name`; otherwise TypeError or ValueError."""
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} is on {t.device}" + (f", not on {device}" if device is not None else ", not on a GPU"))
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} values, not {numel}")
+    return t
+
+
+def _norm_desc(x, gamma, eps):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"no channels in shape {tuple(x.shape)}")
+    c = x.shape[-1]
+    desc = NormDesc(_dtype_code(x), c, x.numel() // c, eps)
+    _want(x, "x")
+    _want(gamma, "gamma", x.dtype, (c,), device=x.device)
+    return desc
+
+
+def ff_layernorm_forward(x, gamma, beta, residual=None, eps: float = 1e-5, stats: bool = True, out=None, sum_out=None):
+    """Layer norm over the last axis of x, or of x + residual; returns (y, sum, mean, rstd).  sum (the rounded x + residual,
+    None without one) is what ff_layernorm_backward takes as s; sum_out may be x or residual itself.  stats=False keeps no mean and rstd."""
+    import torch
+    desc = _norm_desc(x, gamma, eps)
+    _want(beta, "beta", x.dtype, gamma.shape, device=x.device)
+    out = torch.empty_like(x) if out is None else _want(out, "out", x.dtype, x.shape, device=x.device)
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("sum_out needs a residual")
+    else:
+        _want(residual, "residual", x.dtype, x.shape, device=x.device)
+        sum_out = torch.empty_like(x) if sum_out is None else _want(sum_out, "sum_out", x.dtype, x.shape, device=x.device)
+    mean = rstd = None
+    if stats:
+        mean, rstd = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device).unbind(0)
+    _check(lib().ff_layernorm_forward(C.byref(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(sum_out), _ptr(out), _ptr(mean),
+                                      _ptr(rstd), _stream()))
+    return out, sum_out, mean, rstd
+
+
+def ff_layernorm_backward(s, gamma, dy, mean=None, rstd=None, dsum=None, eps: float = 1e-5, dx=None, dgamma=None, dbeta=None,
+                          accumulate: bool = False, ws=None):
+    """Gradients of ff_layernorm_forward; returns (dx, dgamma, dbeta), the last two float32.  s: what was normalised (x, or
+    sum).  Without mean and rstd they are formed again from s.  dsum: the gradient that reaches s by other ways, added to dx.
+    dx may be dy or dsum itself; accumulate adds to the given dgamma and dbeta."""
+    import torch
+    desc = _norm_desc(s, gamma, eps)
+    _want(dy, "dy", s.dtype, s.shape, device=s.device)
+    if dsum is not None:
+        _want(dsum, "dsum", s.dtype, s.shape, device=s.device)
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is not None:
+            _want(t, name, torch.float32, numel=desc.rows, device=s.device)
+    if accumulate and (dgamma is None or dbeta is None):
+        raise ValueError("accumulate needs dgamma and dbeta")
+    dx = torch.empty_like(s) if dx is None else _want(dx, "dx", s.dtype, s.shape, device=s.device)
+    if dgamma is None and dbeta is None:
+        dgamma, dbeta = torch.empty(2, desc.c, dtype=torch.float32, device=s.device).unbind(0)
+    dgamma = torch.empty(desc.c, dtype=torch.float32, device=s.device) if dgamma is None else _want(dgamma, "dgamma", torch.float32, gamma.shape, device=s.device)
+    dbeta = torch.empty(desc.c, dtype=torch.float32, device=s.device) if dbeta is None else _want(dbeta, "dbeta", torch.float32, gamma.shape, device=s.device)
+    if ws is None:
+        ws = _alloc_ws(ff_layernorm_backward_workspace_bytes(desc), s.device)
+    _check(lib().ff_layernorm_backward(C.byref(desc), _ptr(s), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dgamma),
+                                       _ptr(dbeta), 1 if accumulate else 0, _ptr(ws), ws.numel(), _stream()))
+    return dx, dgamma, dbeta
+
+
+def ff_layernorm_backward_workspace_bytes(desc: NormDesc) -> int:
+    n = lib().ff_layernorm_backward_workspace_bytes(C.byref(desc))
+    if n == 0:
+        raise FFError(FF_EINVAL, last_error())
+    return n
+
+
+class AdamWPlan:
+    """The tensors of a model laid out for ff_grad_norm, ff_adamw_step and ff_adamw_moments.  It holds their addresses (and
+    the tensors): a gradient that is allocated anew needs a new plan, one that is written in place does not."""
+
+    def __init__(self, desc, table, tensors, values, device):
+        import numpy as np
+        import torch
+        self.desc, self.tensors, self.values, self.device = desc, tensors, values, device
+        n = lib().ff_adamw_plan_bytes(C.byref(desc), table)
+        if n == 0:
+            raise FFError(FF_EINVAL, last_error())
+        host = np.empty(n, np.uint8)
+        _check(lib().ff_adamw_plan(C.byref(desc), table, host.ctypes.data, n))
+        self.plan = torch.from_numpy(host).to(device)
+        self.norm_ws = _alloc_ws(lib().ff_grad_norm_workspace_bytes(), device)
+
+
+def _make_plan(state_bits, columns, weight_decay):
+    """columns: {pointer name: list of tensors or None}."""
+    import numpy as np
+    grads = columns["g"]
+    count = len(grads)
+    if count == 0:
+        raise ValueError("a plan needs a tensor")
+    device = grads[0].device
+    numels = [t.numel() for t in grads]
+    row = np.dtype(AdamWTensor)
+    table = np.zeros(count, row)
+    for name, ts in columns.items():
+        if ts is None:
+            continue
+        if len(ts) != count:
+            raise ValueError(f"{len(ts)} tensors of {name} for {count} gradients")
+        for t, n in zip(ts, numels):
+            _want(t, name, ts[0].dtype, numel=-(-n // 256) if name.endswith("_exp") else n, device=device)
+        table[name] = [t.data_ptr() for t in ts]
+    table["numel"] = numels
+    table["weight_decay"] = weight_decay
+    p = columns.get("p")
+    desc = AdamWDesc(FF_F32 if p is None else _dtype_code(p[0]), _dtype_code(grads[0]), state_bits, count)
+    return AdamWPlan(desc, table.ctypes.data, (table, columns), sum(numels), device)
+
+
+def make_grad_plan(grads) -> AdamWPlan:
+    """A plan of gradients alone, for ff_grad_norm."""
+    return _make_plan(0, {"g": list(grads)}, 0.0)
+
+
+def make_adamw_plan(params, grads, m, v, master=None, m_exp=None, v_exp=None, weight_decay=0.0) -> AdamWPlan:
+    """A plan for ff_adamw_step.  m, v: float32 of the parameters' sizes, or uint8 with m_exp, v_exp (uint8, one for each 256
+    values of a tensor; adamw_states allocates either).  master: float32 copies of bfloat16 parameters.  weight_decay: a number, or
+    one for each tensor."""
+    import torch
+    columns = {"p": list(params), "g": list(grads), "m": list(m), "v": list(v), "master": None if master is None else list(master),
+               "m_exp": None if m_exp is None else list(m_exp), "v_exp": None if v_exp is None else list(v_exp)}
+    if (columns["m_exp"] is None) != (columns["v_exp"] is None):
+        raise ValueError("m_exp and v_exp are given together")
+    bits = 32 if columns["m_exp"] is None else 8
+    kinds = {"m": torch.uint8 if bits == 8 else torch.float32, "master": torch.float32, "m_exp": torch.uint8}
+    kinds["v"], kinds["v_exp"] = kinds["m"], kinds["m_exp"]
+    for name, dtype in kinds.items():
+        for t in columns[name] or ():
+            if t.dtype != dtype:
+                raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    return _make_plan(bits, columns, weight_decay)
+
+
+def adamw_states(params, bits: int = 32):
+    """Zero states for make_adamw_plan: {"m", "v"} and, in 8 bits, {"m_exp", "v_exp"}."""
+    import torch
+    if bits not in (8, 32):
+        raise ValueError(f"states have 8 or 32 bits, not {bits}")
+    new = lambda t, n, dtype: torch.zeros(n, dtype=dtype, device=t.device)  # noqa: E731
+    kind = torch.float32 if bits == 32 else torch.uint8
+    states = {k: [new(t, t.numel(), kind) for t in params] for k in ("m", "v")}
+    if bits == 8:
+        states.update({k: [new(t, -(-t.numel() // 256), torch.uint8) for t in params] for k in ("m_exp", "v_exp")})
+    return states
+
+
+def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
+    """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another."""
+    import torch
+    out = torch.empty(1, dtype=torch.float32, device=plan.device) if out is None else _want(out, "out", torch.float32, numel=1, device=plan.device)
+    ws = plan.norm_ws if ws is None else ws
+    _check(lib().ff_grad_norm(C.byref(plan.desc), _ptr(plan.plan), plan.plan.numel(), _ptr(out), _ptr(ws), ws.numel(), _stream()))
+    return out
+
+
+def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: int = 0):
+    """One AdamW step over the plan's tensors, in place.  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm
+    that is not finite leaves everything as it was.  seed: of the rounding of 8-bit states, another for each step."""
+    import torch
+    if (norm is None) != (max_norm is None):
+        raise ValueError("norm and max_norm are given together")
+    if norm is not None:
+        _want(norm, "norm", torch.float32, numel=1, device=plan.device)
+    hyper = AdamWHyper(lr, betas[0], betas[1], eps, 0.0 if max_norm is None else max_norm, step, seed & 0xFFFFFFFF)
+    _check(lib().ff_adamw_step(C.byref(plan.desc), _ptr(plan.plan), plan.plan.numel(), C.byref(hyper), _ptr(norm), _stream()))
+
+
+def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
+    """(m, v) of all tensors of the plan, one after another, as float32."""
+    import torch
+    m = torch.empty(plan.values, dtype=torch.float32, device=plan.device) if m is None else _want(m, "m", torch.float32, numel=plan.values, device=plan.device)
+    v = torch.empty(plan.values, dtype=torch.float32, device=plan.device) if v is None else _want(v, "v", torch.float32, numel=plan.values, device=plan.device)
+    _check(lib().ff_adamw_moments(C.byref(plan.desc), _ptr(plan.plan), plan.plan.numel(), _ptr(m), _ptr(v), _stream()))
+    return m, v
 
 
 def ff_profile_enable(on: bool):

@@ -33,11 +33,14 @@ FLAGS = [
     "-mllvm", "-amdgpu-mfma-vgpr-form=1",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
+# the optimiser's states are the same to the last bit as its formulas evaluated one rounded operation at a time
+# (8-bit codes would show a difference as a whole step), so none of its products is fused with a sum
+SOURCE_FLAGS = {"ff_adamw.hip": ["-ffp-contract=off"]}
 
 
 def _compile(src: str) -> str:
     obj = os.path.join(OBJ, os.path.basename(src) + ".o")
-    cmd = [HIPCC, *FLAGS, "-c", src, "-o", obj]
+    cmd = [HIPCC, *FLAGS, *SOURCE_FLAGS.get(os.path.basename(src), []), "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
     err = "\n".join(l for l in r.stderr.splitlines() if noise not in l and l.strip())

@@ -22,7 +22,8 @@ static const char* kKindNames[KK_COUNT] = {"k_prep", "pair bias pass", "k_gemm<P
                                            "probe: copy", "k_tm_prep", "k_tm_proj", "k_tm_mul", "k_tm_out",
                                            "k_gca_kv", "k_gca_softmax", "k_gca_out",
                                            "k_bwd_stats", "k_bwd_dq", "k_bwd_dkv", "k_bwd_dbias", "probe: vector loop",
-                                           "k_proj_attn", "k_bwd_rows", "k_bwd_prepare", "k_bwd_dbias_reduce"};
+                                           "k_proj_attn", "k_bwd_rows", "k_bwd_prepare", "k_bwd_dbias_reduce", "k_ln_forward",
+                                           "k_ln_backward", "k_ln_join", "k_grad_norm", "k_adamw", "k_moments"};
 
 static hipEvent_t prof_event() {
     if (!g_prof_pool.empty()) {
@@ -371,6 +372,163 @@ ff_status ff_attention_core_backward(const ff_core_desc* desc, const void* q, co
     if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
     if (ws_bytes < need) return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);
     return core_backward_run(*desc, q, k, v, g, bias, mask, dout, dq, dk, dv, dg, dbias, ws, (hipStream_t)hip_stream);
+}
+
+// ---- layer norm in training
+static ff_status check_norm(const ff_norm_desc* d) {
+    if (!d) return fail(FF_EINVAL, "desc is NULL");
+    if (d->dtype != FF_F32 && d->dtype != FF_BF16) return fail(FF_EINVAL, "bad dtype %d", d->dtype);
+    if (d->rows < 0 || d->c < 1 || d->c > 8192 || d->rows > (int64_t)1 << 40)
+        return fail(FF_EINVAL, "bad size rows=%lld c=%d", (long long)d->rows, d->c);
+    if (!(d->ln_eps >= 0.f)) return fail(FF_EINVAL, "ln_eps must be >= 0");
+    return FF_OK;
+}
+static bool aligned_to(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
+
+ff_status ff_layernorm_forward(const ff_norm_desc* desc, const void* x, const void* residual, const void* gamma, const void* beta,
+                               void* sum, void* y, float* mean, float* rstd, void* hip_stream) {
+    ff_status st = check_norm(desc);
+    if (st != FF_OK) return st;
+    if ((residual == nullptr) != (sum == nullptr)) return fail(FF_EINVAL, "sum must be given exactly when residual is");
+    if ((mean == nullptr) != (rstd == nullptr)) return fail(FF_EINVAL, "mean and rstd must be given together");
+    if (desc->rows == 0) return FF_OK;
+    if (!x || !gamma || !beta || !y) return fail(FF_EINVAL, "NULL pointer");
+    const size_t esz = desc->dtype == FF_F32 ? 4 : 2, n = (size_t)desc->rows * desc->c * esz;
+    const void* ptrs[] = {x, residual, gamma, beta, sum, y};
+    for (const void* p : ptrs)
+        if (!aligned_to(p, esz)) return fail(FF_EINVAL, "a pointer is not aligned to its type");
+    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4)) return fail(FF_EINVAL, "mean and rstd must be 4-byte aligned");
+    if (overlaps(y, n, x, n) || (residual && (overlaps(y, n, residual, n) || overlaps(y, n, sum, n))))
+        return fail(FF_EINVAL, "y must not overlap x, residual or sum");
+    if (sum && ((sum != x && overlaps(sum, n, x, n)) || (sum != residual && overlaps(sum, n, residual, n))))
+        return fail(FF_EINVAL, "sum must be x itself, residual itself, or overlap neither");
+    return layernorm_forward_run(*desc, x, residual, gamma, beta, sum, y, mean, rstd, (hipStream_t)hip_stream);
+}
+
+size_t ff_layernorm_backward_workspace_bytes(const ff_norm_desc* desc) {
+    if (check_norm(desc) != FF_OK) return 0;
+    return layernorm_backward_workspace(*desc);
+}
+
+ff_status ff_layernorm_backward(const ff_norm_desc* desc, const void* s, const void* gamma, const float* mean, const float* rstd,
+                                const void* dy, const void* dsum, void* dx, float* dgamma, float* dbeta, int32_t accumulate,
+                                void* ws, size_t ws_bytes, void* hip_stream) {
+    ff_status st = check_norm(desc);
+    if (st != FF_OK) return st;
+    if ((mean == nullptr) != (rstd == nullptr)) return fail(FF_EINVAL, "mean and rstd must be given together");
+    if (accumulate != 0 && accumulate != 1) return fail(FF_EINVAL, "accumulate must be 0 or 1 (got %d)", accumulate);
+    if (!gamma || !dgamma || !dbeta || (desc->rows > 0 && (!s || !dy || !dx))) return fail(FF_EINVAL, "NULL pointer");
+    const size_t esz = desc->dtype == FF_F32 ? 4 : 2, n = (size_t)desc->rows * desc->c * esz;
+    const void* ptrs[] = {s, gamma, dy, dsum, dx};
+    for (const void* p : ptrs)
+        if (!aligned_to(p, esz)) return fail(FF_EINVAL, "a pointer is not aligned to its type");
+    const float* floats[] = {mean, rstd, dgamma, dbeta};
+    for (const float* p : floats)
+        if (!aligned_to(p, 4)) return fail(FF_EINVAL, "mean, rstd, dgamma and dbeta must be 4-byte aligned");
+    if (overlaps(dx, n, s, n)) return fail(FF_EINVAL, "dx must not overlap s");
+    if ((dx != dy && overlaps(dx, n, dy, n)) || (dsum && dx != dsum && overlaps(dx, n, dsum, n)))
+        return fail(FF_EINVAL, "dx must be dy itself, dsum itself, or overlap neither");
+    const size_t need = layernorm_backward_workspace(*desc), cb = (size_t)desc->c * 4;
+    if (overlaps(dgamma, cb, dbeta, cb)) return fail(FF_EINVAL, "dgamma and dbeta overlap");
+    if (!ws) return fail(FF_EINVAL, "workspace is NULL (%zu bytes needed)", need);
+    if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
+    if (ws_bytes < need) return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);
+    return layernorm_backward_run(*desc, s, gamma, mean, rstd, dy, dsum, dx, dgamma, dbeta, accumulate != 0, ws, (hipStream_t)hip_stream);
+}
+
+// ---- the optimiser
+static ff_status check_adamw(const ff_adamw_desc* d) {
+    if (!d) return fail(FF_EINVAL, "desc is NULL");
+    if (d->param_dtype != FF_F32 && d->param_dtype != FF_BF16) return fail(FF_EINVAL, "bad param_dtype %d", d->param_dtype);
+    if (d->grad_dtype != FF_F32 && d->grad_dtype != FF_BF16) return fail(FF_EINVAL, "bad grad_dtype %d", d->grad_dtype);
+    if (d->state_bits != 0 && d->state_bits != 8 && d->state_bits != 32) return fail(FF_EINVAL, "state_bits must be 0, 8 or 32 (got %d)", d->state_bits);
+    if (d->n_tensors < 0) return fail(FF_EINVAL, "n_tensors must be >= 0 (got %d)", d->n_tensors);
+    return FF_OK;
+}
+
+static ff_status check_tensors(const ff_adamw_desc* d, const ff_adamw_tensor* ts) {
+    ff_status st = check_adamw(d);
+    if (st != FF_OK) return st;
+    if (d->n_tensors > 0 && !ts) return fail(FF_EINVAL, "tensors is NULL");
+    int64_t total = 0;
+    for (int i = 0; i < d->n_tensors; ++i) {
+        const ff_adamw_tensor& t = ts[i];
+        if (t.numel < 0 || t.numel > (int64_t)1 << 40 || (total += t.numel) > (int64_t)1 << 40)
+            return fail(FF_EINVAL, "tensor %d: bad numel %lld", i, (long long)t.numel);
+        if (t.numel == 0) continue;
+        if (!t.g || !aligned_to(t.g, d->grad_dtype == FF_F32 ? 4 : 2)) return fail(FF_EINVAL, "tensor %d: g is NULL or misaligned", i);
+        if (d->state_bits == 0) continue;
+        if (!t.p || !t.m || !t.v) return fail(FF_EINVAL, "tensor %d: p, m or v is NULL", i);
+        if (!aligned_to(t.p, d->param_dtype == FF_F32 ? 4 : 2)) return fail(FF_EINVAL, "tensor %d: p is misaligned", i);
+        if (t.master && (d->param_dtype != FF_BF16 || !aligned_to(t.master, 4)))
+            return fail(FF_EINVAL, "tensor %d: master belongs to bfloat16 parameters and is 4-byte aligned", i);
+        if (d->state_bits == 32 && (!aligned_to(t.m, 4) || !aligned_to(t.v, 4))) return fail(FF_EINVAL, "tensor %d: m or v is misaligned", i);
+        if ((d->state_bits == 8) != (t.m_exp != nullptr) || (d->state_bits == 8) != (t.v_exp != nullptr))
+            return fail(FF_EINVAL, "tensor %d: m_exp and v_exp belong to 8-bit states", i);
+        if (!(t.weight_decay >= 0.f) || t.weight_decay > 1e30f) return fail(FF_EINVAL, "tensor %d: weight_decay must be finite and >= 0", i);
+    }
+    return FF_OK;
+}
+
+static ff_status check_plan(const ff_adamw_desc* d, const void* plan, size_t bytes) {
+    ff_status st = check_adamw(d);
+    if (st != FF_OK) return st;
+    if (!plan) return fail(FF_EINVAL, "plan is NULL");
+    if (!aligned16(plan)) return fail(FF_EINVAL, "plan must be 16-byte aligned");
+    if (!adamw_plan_whole(bytes)) return fail(FF_EINVAL, "no plan has %zu bytes", bytes);
+    return FF_OK;
+}
+
+size_t ff_adamw_plan_bytes(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors) {
+    if (check_tensors(desc, tensors) != FF_OK) return 0;
+    return adamw_plan_size(*desc, tensors);
+}
+
+ff_status ff_adamw_plan(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors, void* plan, size_t plan_bytes) {
+    ff_status st = check_tensors(desc, tensors);
+    if (st != FF_OK) return st;
+    const size_t need = adamw_plan_size(*desc, tensors);
+    if (!plan || !aligned_to(plan, 8)) return fail(FF_EINVAL, "plan is NULL or misaligned");
+    if (plan_bytes != need) return fail(FF_EWORKSPACE, "the plan has %zu bytes, %zu given", need, plan_bytes);
+    adamw_plan_fill(*desc, tensors, plan);
+    return FF_OK;
+}
+
+size_t ff_grad_norm_workspace_bytes(void) { return grad_norm_workspace(); }
+
+ff_status ff_grad_norm(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* norm, void* ws, size_t ws_bytes,
+                       void* hip_stream) {
+    ff_status st = check_plan(desc, plan, plan_bytes);
+    if (st != FF_OK) return st;
+    if (!norm || !aligned_to(norm, 4)) return fail(FF_EINVAL, "norm is NULL or misaligned");
+    if (!ws) return fail(FF_EINVAL, "workspace is NULL (%zu bytes needed)", grad_norm_workspace());
+    if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
+    if (ws_bytes < grad_norm_workspace())
+        return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", ws_bytes, grad_norm_workspace());
+    return grad_norm_run(*desc, plan, plan_bytes, norm, ws, (hipStream_t)hip_stream);
+}
+
+ff_status ff_adamw_step(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, const ff_adamw_hyper* h, const float* norm,
+                        void* hip_stream) {
+    ff_status st = check_plan(desc, plan, plan_bytes);
+    if (st != FF_OK) return st;
+    if (desc->state_bits == 0) return fail(FF_EINVAL, "a plan of gradients alone has nothing to step");
+    if (!h) return fail(FF_EINVAL, "hyper is NULL");
+    if (!(h->lr >= 0.) || h->lr > 1e30 || !(h->eps >= 0.) || h->eps > 1e30) return fail(FF_EINVAL, "lr and eps must be finite and >= 0");
+    if (!(h->beta1 >= 0.) || !(h->beta1 < 1.) || !(h->beta2 >= 0.) || !(h->beta2 < 1.)) return fail(FF_EINVAL, "beta1 and beta2 must be in [0, 1)");
+    if (h->step < 1) return fail(FF_EINVAL, "step must be >= 1 (got %lld)", (long long)h->step);
+    if (norm && (!(h->max_norm > 0.) || h->max_norm > 1e30)) return fail(FF_EINVAL, "max_norm must be finite and > 0");
+    if (!aligned_to(norm, 4)) return fail(FF_EINVAL, "norm is misaligned");
+    return adamw_step_run(*desc, plan, plan_bytes, *h, norm, (hipStream_t)hip_stream);
+}
+
+ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* m_out, float* v_out, void* hip_stream) {
+    ff_status st = check_plan(desc, plan, plan_bytes);
+    if (st != FF_OK) return st;
+    if (desc->state_bits == 0) return fail(FF_EINVAL, "a plan of gradients alone has no moments");
+    if (!aligned_to(m_out, 4) || !aligned_to(v_out, 4)) return fail(FF_EINVAL, "m_out or v_out is misaligned");
+    if (!m_out && !v_out) return FF_OK;
+    return adamw_moments_run(*desc, plan, plan_bytes, m_out, v_out, (hipStream_t)hip_stream);
 }
 
 size_t ff_attention_workspace_bytes(const ff_attn_desc* desc, int32_t chunk_rows) {

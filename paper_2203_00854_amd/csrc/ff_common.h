@@ -102,7 +102,8 @@ struct Workspace {
 enum KernelKind { KK_PREP = 0, KK_BIAS, KK_PROJ, KK_ATTN, KK_OUT, KK_LAYERNORM, KK_GENERIC, KK_PROBE_MFMA, KK_PROBE_COPY,
                   KK_TM_PREP, KK_TM_PROJ, KK_TM_MUL, KK_TM_OUT, KK_GCA_KV, KK_GCA_SOFTMAX, KK_GCA_OUT,
                   KK_BWD_STATS, KK_BWD_DQ, KK_BWD_DKV, KK_BWD_DBIAS, KK_PROBE_VALU, KK_PROJ_ATTN, KK_BWD_ROWS,
-                  KK_BWD_PREPARE, KK_BWD_DBIAS_REDUCE, KK_COUNT };
+                  KK_BWD_PREPARE, KK_BWD_DBIAS_REDUCE, KK_LN_FORWARD, KK_LN_BACKWARD, KK_LN_JOIN, KK_GRAD_NORM, KK_ADAMW,
+                  KK_MOMENTS, KK_COUNT };
 void prof_begin(int kind, hipStream_t st);
 void prof_end(int kind, hipStream_t st);
 // brackets the launches issued in its scope with HIP events when the timer is on
@@ -164,5 +165,23 @@ ff_status core_backward_run(const ff_core_desc& d, const void* q, const void* k,
 // LayerNorm (ff_layernorm.hip)
 ff_status layernorm_launch(const void* x, const void* g, const void* b, void* y, int64_t rows, int c,
                            float eps, int dt, hipStream_t stream);
+
+// layer norm in training (ff_layernorm_train.hip)
+size_t layernorm_backward_workspace(const ff_norm_desc& d);
+ff_status layernorm_forward_run(const ff_norm_desc& d, const void* x, const void* residual, const void* gamma, const void* beta,
+                                void* sum, void* y, float* mean, float* rstd, hipStream_t stream);
+ff_status layernorm_backward_run(const ff_norm_desc& d, const void* s, const void* gamma, const float* mean, const float* rstd,
+                                 const void* dy, const void* dsum, void* dx, float* dgamma, float* dbeta, bool accumulate, void* ws,
+                                 hipStream_t stream);
+
+// AdamW over many tensors (ff_adamw.hip); plan: device memory
+size_t adamw_plan_size(const ff_adamw_desc& d, const ff_adamw_tensor* tensors);
+void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* tensors, void* plan);
+// whether a plan can have this many bytes
+bool adamw_plan_whole(size_t bytes);
+size_t grad_norm_workspace();
+ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, float* norm, void* ws, hipStream_t stream);
+ff_status adamw_step_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, const ff_adamw_hyper& h, const float* norm, hipStream_t stream);
+ff_status adamw_moments_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, float* m_out, float* v_out, hipStream_t stream);
 
 }  // namespace ff

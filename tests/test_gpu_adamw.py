@@ -1,0 +1,312 @@
+"""GPU parity of ff_grad_norm, ff_adamw_step and ff_adamw_moments.
+
+Against the float64 oracle the tolerances count roundings, u = 2^-24: g' is two operations from g (and the norm's and the factor's
+own, six in all), m and v three more, the change of w some twenty.  The 8-bit states are the float32 formulas' to the bit
+(the same operations in the same order, each rounded by itself), so codes and exponents are compared as whole numbers.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_00854_amd as P
+from oracle import adamw as A
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+HYPER = dict(lr=1e-2, betas=(0.9, 0.999), eps=1e-8)
+
+
+class Model:
+    """Tensors of the given sizes, each `gap` values behind the one before in a buffer of its kind."""
+
+    def __init__(self, sizes, param, grad, bits, seed, gap=0, scale=1.0):
+        gen = torch.Generator(DEV).manual_seed(seed)
+        self.sizes, self.bits, self.gap = sizes, bits, gap
+        room = sum(n + gap for n in sizes) + gap
+        randn = lambda: torch.randn(room, generator=gen, device=DEV)  # noqa: E731
+        self.flat = {"p": randn().to(torch.float32 if param == "f32" else torch.bfloat16), "g": (randn() * scale).to({"f32": torch.float32, "bf16": torch.bfloat16}[grad])}
+        self.flat["master"] = self.flat["p"].float() + randn() * 1e-4 if param == "master" else None
+        self.lists = {k: None if v is None else self.cut(v) for k, v in self.flat.items()}
+        if bits == 32:
+            self.flat["m"], self.flat["v"] = randn() * 0.1 * scale, randn().square() * scale ** 2
+            self.lists["m"], self.lists["v"] = self.cut(self.flat["m"]), self.cut(self.flat["v"])
+            self.lists["m_exp"] = self.lists["v_exp"] = None
+        else:
+            rng = np.random.default_rng(seed)
+            self.lists.update(P.adamw_states(self.lists["p"], 8))
+            for i, n in enumerate(sizes):
+                for k, top, x in (("m", A.TOP_M, rng.normal(size=n) * 0.1 * scale), ("v", A.TOP_V, rng.normal(size=n) ** 2 * scale ** 2)):
+                    code, exp = A.encode(x.astype(np.float32), top, rng.integers(0, 1 << 16, n))
+                    self.lists[k][i].copy_(torch.from_numpy(code))
+                    self.lists[k + "_exp"][i].copy_(torch.from_numpy(exp))
+        self.decay = [0.1 * (i % 3) for i in range(len(sizes))]
+        self.plan = P.make_adamw_plan(self.lists["p"], self.lists["g"], self.lists["m"], self.lists["v"], master=self.lists["master"], m_exp=self.lists["m_exp"],
+                                      v_exp=self.lists["v_exp"], weight_decay=self.decay)
+
+    def cut(self, flat):
+        out, at = [], self.gap
+        for n in self.sizes:
+            out.append(flat[at:at + n])
+            at += n + self.gap
+        return out
+
+    def host(self):
+        """Every tensor as a numpy array, and the moments as float32."""
+        get = lambda t: t.float().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()  # noqa: E731
+        h = {k: None if ts is None else [get(t) for t in ts] for k, ts in self.lists.items()}
+        if self.bits == 8:
+            h["m32"] = [A.decode(c, e, A.TOP_M) for c, e in zip(h["m"], h["m_exp"])]
+            h["v32"] = [A.decode(c, e, A.TOP_V) for c, e in zip(h["v"], h["v_exp"])]
+        else:
+            h["m32"], h["v32"] = h["m"], h["v"]
+        return h
+
+
+def check_step(model, before, step, k=1.0, seed=0, hyper=HYPER):
+    after = model.host()
+    b1, b2 = hyper["betas"]
+    first = 0
+    for i, n in enumerate(model.sizes):
+        g, m0, v0 = before["g"][i], before["m32"][i], before["v32"][i]
+        w0 = before["p"][i] if before["master"] is None else before["master"][i]
+        decay = float(np.float32(model.decay[i]))
+        w, m, v = A.step(w0, g, m0, v0, hyper["lr"], b1, b2, hyper["eps"], decay, step, k)
+        e_m = 10 * U * (np.abs(b1 * m0) + np.abs((1 - b1) * g * k)) + 1e-44
+        e_v = 16 * U * v + 1e-44
+        root = np.sqrt(v) / np.sqrt(1 - b2 ** step) + hyper["eps"]
+        size = hyper["lr"] / (1 - b1 ** step)
+        e_w = size * (e_m + 28 * U * np.abs(m)) / root + 4 * U * (np.abs(w0) + np.abs(w))
+        name = f"tensor {i} of {n}"
+        if before["master"] is not None:
+            assert np.all(np.abs(after["master"][i] - w) <= e_w), name
+            assert torch.equal(model.lists["p"][i], model.lists["master"][i].to(torch.bfloat16)), name
+        else:
+            half = 0.0 if model.lists["p"][i].dtype == torch.float32 else torch.finfo(torch.bfloat16).eps / 2
+            assert np.all(np.abs(after["p"][i] - w) <= e_w + half * (np.abs(w) + e_w)), name
+        if model.bits == 32:
+            assert np.all(np.abs(after["m"][i] - m) <= e_m), name
+            assert np.all(np.abs(after["v"][i] - v) <= e_v), name
+        else:
+            m32, v32 = A.moments_f32(g, m0, v0, b1, b2, np.float32(k))
+            bits = A.dither(np.arange(n) + first * 256, seed)
+            for which, top, x, b in (("m", A.TOP_M, m32, bits & 0xFFFF), ("v", A.TOP_V, v32, bits >> 16)):
+                code, exp = A.encode(x, top, b)
+                assert np.array_equal(after[which + "_exp"][i], exp), (name, which)
+                assert np.array_equal(after[which][i], code), (name, which)
+        first += -(-n // 256)
+    return after
+
+
+SIZES = [[1], [255, 256, 257], [5, 4096, 1, 4097, 2048, 31], [12345, 70000, 8, 0, 3], [64, 128, 512, 1024] * 6]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param", ["f32", "master", "bf16"])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_steps(param, grad, bits):
+    for j, sizes in enumerate(SIZES):
+        for gap in (0, 1, 16):
+            print(f"{param} {grad} {bits} bits, sizes {sizes[:6]}, gap {gap}", flush=True)
+            model = Model(sizes, param, grad, bits, seed=j * 10 + gap, gap=gap)
+            around = {k: v.clone() for k, v in model.flat.items() if v is not None}
+            for step in (1, 2, 1000):
+                before = model.host()
+                P.ff_adamw_step(model.plan, step, seed=step * 77, **HYPER)
+                torch.cuda.synchronize()
+                check_step(model, before, step, seed=step * 77)
+            if gap:                                     # what lies between the tensors stays
+                for k, v in around.items():
+                    at = 0
+                    for n in sizes + [0]:
+                        assert torch.equal(model.flat[k][at:at + gap], v[at:at + gap]), k
+                        at += gap + n
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("max_norm", [0.1, 1e6])
+def test_clipped_steps(bits, max_norm):
+    model = Model([300, 5000, 17], "f32", "f32", bits, seed=2, gap=3)
+    for step in (1, 2):
+        before = model.host()
+        norm = P.ff_grad_norm(model.plan)
+        P.ff_adamw_step(model.plan, step, norm=norm, max_norm=max_norm, seed=step, **HYPER)
+        want = np.sqrt(sum((g.astype(np.float64) ** 2).sum() for g in before["g"]))
+        assert abs(norm.item() - want) <= U * want * (1 + 1e-6)
+        n32 = np.float32(want)
+        k = min(np.float32(1), np.float32(max_norm) / (n32 + np.float32(1e-6)))
+        check_step(model, before, step, k=float(k), seed=step)
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[1], [5, 4096, 1, 4097], [70000] * 40, [1_000_003], list(range(1, 600))])
+def test_norm(sizes, grad):
+    dtype = torch.float32 if grad == "f32" else torch.bfloat16
+    gen = torch.Generator(DEV).manual_seed(len(sizes))
+    flat = torch.randn(sum(sizes) + len(sizes), generator=gen, device=DEV).to(dtype)
+    parts, at = [], 1
+    for n in sizes:
+        parts.append(flat[at:at + n])
+        at += n + 1
+    plan = P.make_grad_plan(parts)
+    got = P.ff_grad_norm(plan)
+    want = torch.cat(parts).double().square().sum().sqrt().item()
+    # float64 sums: the float32 result is the correctly rounded one up to 2^-20 of its last place
+    assert abs(got.item() - want) <= U * want * (1 + 1e-6)
+    assert torch.equal(got, P.ff_grad_norm(plan))
+    for scale in (1e-30, 1e30):                          # squares that no float32 holds
+        for p in parts:
+            p.mul_(scale)
+        want = torch.cat(parts).double().square().sum().sqrt().item()
+        got = P.ff_grad_norm(plan).item()
+        assert abs(got - want) <= U * want * (1 + 1e-6) + 2.0 ** -149
+        for p in parts:
+            p.div_(scale)
+    parts[-1][-1] = float("nan")
+    assert P.ff_grad_norm(plan).isnan().all()
+    parts[-1][-1] = float("-inf")
+    assert P.ff_grad_norm(plan).item() == float("inf")
+
+
+def test_no_values():
+    empty = torch.empty(0, device=DEV)
+    plan = P.make_adamw_plan([empty], [empty], [empty], [empty])
+    assert P.ff_grad_norm(plan).item() == 0
+    P.ff_adamw_step(plan, 1, **HYPER)
+    m, v = P.ff_adamw_moments(plan)
+    assert m.numel() == 0 and v.numel() == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_norm_that_is_not_finite_changes_nothing(bits, bad):
+    model = Model([300, 5000], "master", "bf16", bits, seed=4)
+    model.lists["g"][1][77] = bad
+    before = model.host()
+    norm = P.ff_grad_norm(model.plan)
+    assert not norm.isfinite().any()
+    P.ff_adamw_step(model.plan, 3, norm=norm, max_norm=1.0, **HYPER)
+    after = model.host()
+    for k in ("p", "master", "m", "v"):
+        assert all(np.array_equal(a, b) for a, b in zip(before[k], after[k])), k
+
+
+def test_gradients_that_are_not_finite_show():
+    """Without a norm they reach their own values in 32 bits, and their group of 256 in 8."""
+    for bits in (32, 8):
+        model = Model([600], "f32", "f32", bits, seed=5)
+        model.lists["g"][0][300] = float("nan")
+        P.ff_adamw_step(model.plan, 1, **HYPER)
+        bad = model.lists["p"][0].isnan().nonzero().flatten().tolist()
+        assert bad == [300]
+        m, v = P.ff_adamw_moments(model.plan)
+        for x in (m, v):
+            assert x.isnan().nonzero().flatten().tolist() == ([300] if bits == 32 else list(range(256, 512)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_extreme_gradients(bits):
+    """Zero gradients, subnormal ones and large ones beside each other."""
+    model = Model([2000], "f32", "f32", bits, seed=6)
+    g = model.lists["g"][0]
+    g[::7] = 0
+    g[1::7] *= 1e-22
+    g[2::7] *= 1e12
+    g[3::7] *= 1e-40
+    g[512:768] = 0
+    for step in (1, 2, 3):
+        before = model.host()
+        P.ff_adamw_step(model.plan, step, seed=step, **HYPER)
+        after = check_step(model, before, step, seed=step)
+        assert np.isfinite(after["p"][0]).all()
+
+
+def test_zero_states_and_first_step():
+    """From nothing, the first step moves every weight by lr against its gradient's sign, in 8 bits as in 32."""
+    for bits in (32, 8):
+        p, g = torch.zeros(1000, device=DEV), torch.randn(1000, generator=torch.Generator(DEV).manual_seed(1), device=DEV)
+        states = P.adamw_states([p], bits)
+        plan = P.make_adamw_plan([p], [g], weight_decay=0.0, **states)
+        P.ff_adamw_step(plan, 1, lr=1e-2, eps=1e-12)
+        assert torch.allclose(p, -1e-2 * g.sign(), rtol=1e-5)
+
+
+def test_moments_are_what_the_states_hold():
+    for bits in (32, 8):
+        model = Model([255, 1, 4097, 300], "f32", "bf16", bits, seed=7, gap=5)
+        m, v = P.ff_adamw_moments(model.plan)
+        h = model.host()
+        assert np.array_equal(m.cpu().numpy(), np.concatenate(h["m32"])) and np.array_equal(v.cpu().numpy(), np.concatenate(h["v32"]))
+
+
+def test_a_plan_under_another_descriptor_is_left_alone():
+    model = Model([3000], "f32", "f32", 32, seed=8)
+    before = model.host()
+    real = model.plan.desc
+    model.plan.desc = P.AdamWDesc(real.param_dtype, real.grad_dtype, 8, real.n_tensors)
+    P.ff_adamw_step(model.plan, 1, **HYPER)
+    P.ff_adamw_moments(model.plan)
+    torch.cuda.synchronize()
+    after = model.host()
+    for k in ("p", "m", "v"):
+        assert np.array_equal(before[k][0], after[k][0]), k
+
+
+def test_eight_bits_follow_thirty_two():
+    """A quadratic bowl with noise: after 300 steps both are at its bottom.  32 bits leave the noise of the last steps, about lr; 8
+    bits double it at most (a code's step is an eighth of a moment, drawn to either side)."""
+    gen = torch.Generator(DEV).manual_seed(3)
+    target = torch.randn(20_000, generator=gen, device=DEV)
+    left = {}
+    for bits in (32, 8):
+        p, g = torch.zeros(20_000, device=DEV), torch.zeros(20_000, device=DEV)
+        plan = P.make_adamw_plan([p], [g], weight_decay=0.0, **P.adamw_states([p], bits))
+        for step in range(1, 301):
+            torch.add(p - target, torch.randn(20_000, generator=gen, device=DEV), alpha=0.1, out=g)
+            P.ff_adamw_step(plan, step, lr=2e-2, betas=(0.9, 0.99), seed=step)
+        left[bits] = (p - target).square().mean().sqrt().item()
+    print(left)
+    assert left[32] < 0.1 and left[8] < 2 * left[32] + 0.02
+
+
+def test_captured_into_a_graph():
+    model = Model([300, 5000, 17], "master", "bf16", 8, seed=9)
+    other = Model([300, 5000, 17], "master", "bf16", 8, seed=9)
+    norm = torch.empty(1, device=DEV)
+
+    def work(m):
+        P.ff_grad_norm(m.plan, out=norm)
+        P.ff_adamw_step(m.plan, 10, norm=norm, max_norm=0.5, seed=3, **HYPER)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work(model)
+    for _ in range(4):
+        for m in (model, other):
+            m.flat["g"].mul_(0.75)
+        work(other)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = model.host(), other.host()
+        for k in ("p", "master", "m", "v", "m_exp", "v_exp"):
+            assert all(np.array_equal(x, y) for x, y in zip(a[k], b[k])), k
+
+
+def test_more_values_than_32_bit_offsets():
+    """A tensor whose values pass 2^32 bytes (bfloat16 parameter without a master copy): the last ones step as in a small call."""
+    n = (1 << 31) + 300
+    g = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    p = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    tail = torch.randn(300, generator=torch.Generator(DEV).manual_seed(2), device=DEV).to(torch.bfloat16)
+    g[-300:] = tail
+    states = P.adamw_states([p], 8)
+    plan = P.make_adamw_plan([p], [g], **states)
+    norm = P.ff_grad_norm(plan)
+    want = tail.double().square().sum().sqrt().item()
+    assert abs(norm.item() - want) <= U * want * (1 + 1e-6)
+    P.ff_adamw_step(plan, 1, lr=1e-2, eps=1e-12)
+    assert torch.equal(p[-300:].float().sign(), -tail.float().sign()) and (p[:-300:1_000_003] == 0).all()
+    small = [torch.zeros(300, dtype=torch.bfloat16, device=DEV), tail.clone()]
+    P.ff_adamw_step(P.make_adamw_plan([small[0]], [small[1]], **P.adamw_states([small[0]], 8)), 1, lr=1e-2, eps=1e-12)
+    assert torch.equal(p[-300:], small[0])

@@ -1,0 +1,182 @@
+"""The training entry points: struct layouts, plans and refusals, without a launch (CPU)."""
+import ctypes as C
+import os
+import re
+
+import numpy as np
+import pytest
+
+import paper_2203_00854_amd as P
+from paper_2203_00854_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+X, Y, S, R, G, BETA, MEAN, RSTD, WS = (0x1000000 * (i + 1) for i in range(9))
+
+
+def test_struct_layouts_match_the_header():
+    assert C.sizeof(B.NormDesc) == 24 and C.sizeof(B.AdamWDesc) == 16 and C.sizeof(B.AdamWTensor) == 72 and C.sizeof(B.AdamWHyper) == 56
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "ff.h")).read(), flags=re.S)
+    for struct, name in ((B.NormDesc, "ff_norm_desc"), (B.AdamWDesc, "ff_adamw_desc"), (B.AdamWTensor, "ff_adamw_tensor"),
+                         (B.AdamWHyper, "ff_adamw_hyper")):
+        body = [b for b, n in re.findall(r"typedef struct\s*\{([^{}]*)\}\s*(\w+)", text) if n == name][0]
+        declared = re.findall(r"([a-z_0-9]+)\s*(?=[,;])", body)
+        assert declared == [f[0] for f in struct._fields_], name
+
+
+def norm_desc(**kw):
+    return B.NormDesc(**{**dict(dtype=P.FF_BF16, c=64, rows=10, ln_eps=1e-5), **kw})
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(c=0), dict(c=8193), dict(rows=-1), dict(rows=1 << 41), dict(ln_eps=-1.0), dict(ln_eps=float("nan"))])
+def test_layernorm_descriptors(kw):
+    d = norm_desc(**kw)
+    assert P.lib().ff_layernorm_backward_workspace_bytes(C.byref(d)) == 0
+    assert P.last_error() != ""
+    assert P.lib().ff_layernorm_forward(C.byref(d), X, None, G, BETA, None, Y, None, None, None) == B.FF_EINVAL
+    assert P.lib().ff_layernorm_backward(C.byref(d), X, G, None, None, Y, None, S, MEAN, RSTD, 0, WS, 1 << 40, None) == B.FF_EINVAL
+
+
+def test_layernorm_forward_refusals():
+    d, f = norm_desc(), P.lib().ff_layernorm_forward
+    bad = [(None, None, G, BETA, None, Y, None, None), (X, None, None, BETA, None, Y, None, None), (X, None, G, None, None, Y, None, None),
+           (X, None, G, BETA, None, None, None, None), (X, R, G, BETA, None, Y, None, None), (X, None, G, BETA, S, Y, None, None),
+           (X, None, G, BETA, None, Y, MEAN, None), (X, None, G, BETA, None, Y, None, RSTD), (X, None, G, BETA, None, X, None, None),
+           (X, None, G, BETA, None, X + 1278, None, None), (X, R, G, BETA, S, R, None, None), (X, R, G, BETA, S, S, None, None),
+           (X, R, G, BETA, X + 2, Y, None, None), (X, R, G, BETA, R + 2, Y, None, None), (X + 1, None, G, BETA, None, Y, None, None),
+           (X, None, G, BETA, None, Y, MEAN + 2, RSTD)]
+    for args in bad:
+        assert f(C.byref(d), *args, None) == B.FF_EINVAL, args
+    assert f(None, X, None, G, BETA, None, Y, None, None, None) == B.FF_EINVAL
+    assert f(C.byref(norm_desc(rows=0)), None, None, None, None, None, None, None, None, None) == B.FF_OK
+
+
+def test_layernorm_backward_refusals():
+    d, f = norm_desc(), P.lib().ff_layernorm_backward
+    need = P.ff_layernorm_backward_workspace_bytes(d)
+    good = dict(s=X, gamma=G, mean=MEAN, rstd=RSTD, dy=Y, dsum=None, dx=S, dgamma=R, dbeta=BETA, accumulate=0, ws=WS, n=need)
+    assert need % 256 == 0
+    for kw in (dict(s=None), dict(gamma=None), dict(dy=None), dict(dx=None), dict(dgamma=None), dict(dbeta=None), dict(mean=None), dict(rstd=None),
+               dict(accumulate=2), dict(dx=X), dict(dx=X + 2), dict(dx=Y + 2), dict(dsum=S + 2), dict(dbeta=R + 4), dict(dgamma=R + 2),
+               dict(ws=None), dict(ws=WS + 8), dict(dy=Y + 1)):
+        assert f(C.byref(d), *{**good, **kw}.values(), None) == B.FF_EINVAL, kw
+        assert P.last_error() != ""
+    assert f(C.byref(d), *{**good, "n": need - 1}.values(), None) == B.FF_EWORKSPACE
+    assert "workspace too small" in P.last_error()
+
+
+def test_backward_workspace_is_a_fraction_of_the_input():
+    for rows, c in ((2048 * 2048, 128), (5120 * 384, 64), (100_000, 1024)):
+        assert P.ff_layernorm_backward_workspace_bytes(norm_desc(rows=rows, c=c)) <= rows * c * 2 / 8
+    assert P.ff_layernorm_backward_workspace_bytes(norm_desc(rows=0)) >= 1
+
+
+def tensors(*rows):
+    t = np.zeros(len(rows), np.dtype(B.AdamWTensor))
+    for i, r in enumerate(rows):
+        for k, v in r.items():
+            t[k][i] = v
+    return t
+
+
+GOOD = dict(p=0x10000, g=0x20000, m=0x30000, v=0x40000, numel=5000, weight_decay=0.1)
+
+
+def plan_bytes(desc, t):
+    return P.lib().ff_adamw_plan_bytes(C.byref(desc), t.ctypes.data)
+
+
+def test_plan_covers_every_value_once():
+    d = B.AdamWDesc(P.FF_F32, P.FF_BF16, 8, 4)
+    sizes = [5000, 0, 1, 8192]
+    t = tensors(*({**GOOD, "p": 0x100000 * (i + 1), "g": 0x10000000 + 0x100000 * i, "m": 0x20000000 + 0x100000 * i, "v": 0x30000000 + 0x100000 * i,
+                   "m_exp": 0x40000000 + 0x100000 * i, "v_exp": 0x50000000 + 0x100000 * i, "numel": n} for i, n in enumerate(sizes)))
+    n = plan_bytes(d, t)
+    host = np.zeros(n, np.uint8)
+    assert P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, host.ctypes.data, n) == B.FF_OK
+    rec = host.view(np.dtype({"names": ["p", "g", "master", "m", "v", "m_exp", "v_exp", "value", "group", "n", "decay", "tag"],
+                              "formats": ["<u8"] * 7 + ["<i8", "<u4", "<i4", "<f4", "<u4"]}))[1:]
+    assert rec["n"].sum() == sum(sizes) and (rec["n"] > 0).all()
+    assert np.array_equal(rec["value"], np.concatenate([[0], np.cumsum(rec["n"])[:-1]]))
+    groups = np.cumsum([0] + [-(-s // 256) for s in sizes])
+    for r in rec:
+        i = int(r["p"] // 0x100000) - 1
+        at = (int(r["p"]) - 0x100000 * (i + 1)) // 4
+        assert at % 256 == 0 and at + r["n"] <= sizes[i]
+        assert r["g"] == t["g"][i] + 2 * at and r["m"] == t["m"][i] + at and r["v"] == t["v"][i] + at
+        assert r["m_exp"] == t["m_exp"][i] + at // 256 and r["v_exp"] == t["v_exp"][i] + at // 256
+        assert r["group"] == groups[i] + at // 256 and r["decay"] == np.float32(0.1) and r["master"] == 0
+
+
+@pytest.mark.parametrize("desc", [(2, 0, 32, 1), (0, 5, 32, 1), (0, 0, 16, 1), (0, 0, 32, -1)])
+def test_plan_descriptors(desc):
+    d = B.AdamWDesc(*desc)
+    assert plan_bytes(d, tensors(GOOD)) == 0
+    assert P.last_error() != ""
+
+
+@pytest.mark.parametrize("bits,kw", [
+    (32, dict(numel=-1)), (32, dict(g=0)), (32, dict(p=0)), (32, dict(m=0)), (32, dict(v=0)), (32, dict(p=0x10002)), (32, dict(g=0x20001)),
+    (32, dict(m=0x30002)), (32, dict(v=0x40001)), (32, dict(m_exp=0x50000, v_exp=0x60000)), (8, dict(m_exp=0x50000)), (8, dict(v_exp=0x50000)),
+    (8, dict()), (32, dict(master=0x70000)), (32, dict(weight_decay=-0.1)), (32, dict(weight_decay=np.nan)), (32, dict(weight_decay=np.inf)),
+    (32, dict(numel=1 << 41)), (0, dict(g=0)),
+])
+def test_plan_refusals(bits, kw):
+    d = B.AdamWDesc(P.FF_F32, P.FF_F32, bits, 2)
+    more = dict(m_exp=0x50000, v_exp=0x60000) if bits == 8 and not kw.keys() & {"m_exp", "v_exp"} and kw else {}
+    t = tensors({**GOOD, **({"m_exp": 0x50000, "v_exp": 0x60000} if bits == 8 else {})}, {**GOOD, **more, **kw})
+    assert plan_bytes(d, t) == 0, kw
+    assert P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, 0x1000, 240) == B.FF_EINVAL
+
+
+def test_plan_needs_its_own_size():
+    d, t = B.AdamWDesc(P.FF_F32, P.FF_F32, 32, 1), tensors(GOOD)
+    n = plan_bytes(d, t)
+    host = np.zeros(n + 8, np.uint8)
+    assert P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, host.ctypes.data, n - 1) == B.FF_EWORKSPACE
+    assert P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, None, n) == B.FF_EINVAL
+    assert P.lib().ff_adamw_plan_bytes(C.byref(d), None) == 0
+    assert P.lib().ff_adamw_plan_bytes(None, t.ctypes.data) == 0
+
+
+def test_step_and_norm_refusals():
+    lib = P.lib()
+    d = B.AdamWDesc(P.FF_F32, P.FF_F32, 32, 1)
+    n = plan_bytes(d, tensors(GOOD))
+    hyper = lambda **kw: C.byref(B.AdamWHyper(**{**dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=1.0, step=1, seed=0), **kw}))  # noqa: E731
+    nan = float("nan")
+    step = lambda desc=d, plan=X, size=n, h=hyper(), norm=None: lib.ff_adamw_step(C.byref(desc), plan, size, h, norm, None)  # noqa: E731
+    for kw in (dict(lr=-1.0), dict(lr=nan), dict(lr=float("inf")), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=nan), dict(eps=-1e-8),
+               dict(step=0)):
+        assert step(h=hyper(**kw)) == B.FF_EINVAL, kw
+    for kw in (dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=nan)):
+        assert step(h=hyper(**kw), norm=Y) == B.FF_EINVAL, kw
+    assert step(plan=None) == B.FF_EINVAL and step(plan=X + 8) == B.FF_EINVAL
+    assert step(size=n - 1) == B.FF_EINVAL and step(size=0) == B.FF_EINVAL
+    assert step(h=None) == B.FF_EINVAL and step(norm=Y + 2) == B.FF_EINVAL
+    assert step(desc=B.AdamWDesc(P.FF_F32, P.FF_F32, 0, 1)) == B.FF_EINVAL and "gradients alone" in P.last_error()
+    need = lib.ff_grad_norm_workspace_bytes()
+    norm = lambda plan=X, size=n, out=Y, ws=WS, wn=need: lib.ff_grad_norm(C.byref(d), plan, size, out, ws, wn, None)  # noqa: E731
+    assert norm(plan=None) == B.FF_EINVAL and norm(out=None) == B.FF_EINVAL and norm(ws=None) == B.FF_EINVAL and norm(ws=WS + 8) == B.FF_EINVAL
+    assert norm(size=n + 1) == B.FF_EINVAL and norm(wn=need - 1) == B.FF_EWORKSPACE
+    assert lib.ff_adamw_moments(C.byref(d), X, n, Y + 1, None, None) == B.FF_EINVAL
+    assert lib.ff_adamw_moments(C.byref(d), None, n, Y, None, None) == B.FF_EINVAL
+    assert lib.ff_adamw_moments(C.byref(B.AdamWDesc(0, 0, 0, 1)), X, n, Y, None, None) == B.FF_EINVAL
+
+
+def test_binding_refuses_tensors_that_a_kernel_must_not_see():
+    import torch
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        P.ff_layernorm_forward(x, torch.ones(8), torch.ones(8))                 # not on a GPU
+    with pytest.raises(ValueError):
+        P.ff_layernorm_backward(x, torch.ones(8), x)
+    with pytest.raises(ValueError):
+        P.make_grad_plan([])
+    with pytest.raises(ValueError):
+        P.make_grad_plan([x])
+    with pytest.raises(TypeError):
+        P.make_adamw_plan([x], [x], [x.to(torch.uint8)], [x.to(torch.uint8)])    # codes without exponents
+    with pytest.raises(ValueError):
+        P.make_adamw_plan([x], [x], [x], [x], m_exp=[x])
+    with pytest.raises(ValueError):
+        P.adamw_states([x], 16)
