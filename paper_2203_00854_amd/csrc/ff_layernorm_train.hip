@@ -182,7 +182,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kBackwardThreads) void k_ln_b
     const T* __restrict__ s, const T* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in, const T* dy,
     const T* dsum, T* dx, float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta, bool accumulate, int64_t rows,
     int c, int lanes, float eps) {
-    extern __shared__ float joined[];                  // 2 c floats; WIDE: the wavefronts' sums
+    extern __shared__ float joined[];                  // every wavefront's sums of dgamma and dbeta; WIDE: what Team needs
     typedef Pack<T, V> Pc;
     Team<WIDE> team{lanes, WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), joined};
     const Held<V, ITERS, RAGGED> held(team.place, team.lanes, c);
@@ -298,23 +298,32 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kBackwardThreads) void k_ln_b
                 dg[it][i] = across_teams(dg[it][i], lanes);
                 db[it][i] = across_teams(db[it][i], lanes);
             }
-        const int wave = threadIdx.x >> 6;
-        for (int w = 0; w < kBackwardThreads / 64; ++w) {
-            if (wave == w && (threadIdx.x & 63) < (unsigned)lanes) {
+        // each wavefront's sums by (kind, piece, value, lane), then a thread adds up a channel's over the wavefronts
+        const int wave = threadIdx.x >> 6, slots = ITERS * V * lanes;
+        if ((int)(threadIdx.x & 63) < lanes) {
+            float* to = joined + wave * 2 * slots + team.place;
 #pragma unroll
-                for (int it = 0; it < ITERS; ++it)
-                    if (held.has[it])
+            for (int it = 0; it < ITERS; ++it)
 #pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            if (held.counts(it, i)) {
-                                const int at = held.at[it] + i;
-                                joined[at] = w ? joined[at] + dg[it][i] : dg[it][i];
-                                joined[c + at] = w ? joined[c + at] + db[it][i] : db[it][i];
-                            }
-            }
-            __syncthreads();
+                for (int i = 0; i < V; ++i) {
+                    to[(it * V + i) * lanes] = dg[it][i];
+                    to[slots + (it * V + i) * lanes] = db[it][i];
+                }
         }
-        for (int i = threadIdx.x; i < 2 * c; i += kBackwardThreads) leave(i, joined[i]);
+        __syncthreads();
+        const int last = (c + V - 1) / V - 1;
+        for (int ch = threadIdx.x; ch < c; ch += kBackwardThreads) {
+            const int p = ch / V, i = RAGGED && p == last ? ch - (c - V) : ch % V;
+            const float* from = joined + (p / lanes * V + i) * lanes + (p & (lanes - 1));
+            float g = 0.f, b = 0.f;
+#pragma unroll
+            for (int w = 0; w < kBackwardThreads / 64; ++w) {
+                g += from[w * 2 * slots];
+                b += from[w * 2 * slots + slots];
+            }
+            leave(ch, g);
+            leave(c + ch, b);
+        }
     }
 }
 
@@ -441,7 +450,7 @@ static void backward_t(const ff_norm_desc& d, const Shape& s, int blocks, const 
         constexpr int V = decltype(v)::value, I = decltype(iters)::value;
         constexpr bool R = decltype(ragged)::value, W = decltype(wide)::value;
         if constexpr (V != (sizeof(T) == 4 ? 8 : 4)) {
-            const size_t lds = W ? 2 * kWideThreads / 64 * sizeof(float) : 2 * d.c * sizeof(float);
+            const size_t lds = W ? 2 * kWideThreads / 64 * sizeof(float) : (size_t)kBackwardThreads / 64 * 2 * I * V * s.lanes * sizeof(float);     // at most 64 KiB
             hipLaunchKernelGGL((k_ln_backward<T, V, I, R, W>), dim3(blocks), dim3(W ? s.lanes : kBackwardThreads), lds, stream, (const T*)src,
                                (const T*)gamma, mean, rstd, (const T*)dy, (const T*)dsum, (T*)dx, partial, dgamma, dbeta, accumulate, d.rows, d.c,
                                s.lanes, d.ln_eps);
