@@ -3,7 +3,7 @@
 // Both passes are bound by HBM (a dozen to two dozen vector instructions per value, where 45 lane-instructions fit into the time that six bytes
 // take), so a row is read once, stays in registers, and is written once.  A team of 8 to 64 lanes of one wavefront holds a row, each
 // lane up to four pieces of 16 bytes; rows of more than 256 pieces are held by a whole block.  Rows that are no whole number of pieces, and tensors at any
-// offset, take the same path: pieces are loaded at the alignment of their type, and a last piece that
+// offset, take the same path: pieces are loaded at the alignment of their type, and a piece that
 // would pass the row's end is moved back to end with it - its first values, which the piece before holds too, count in no sum.
 #include <type_traits>
 
@@ -51,111 +51,152 @@ __device__ __forceinline__ float team_sum(float v, int lanes) {
     if (lanes > 32) v = half_sum(v);
     return v;
 }
+__device__ __forceinline__ void team_sum(float& v, float& w, int lanes) {
+    v = sum8(v);
+    w = sum8(w);
+    if (lanes > 8) {
+        v += dpp<kDppRor8>(v);
+        w += dpp<kDppRor8>(w);
+    }
+    if (lanes > 16) {
+        v = swap16_sum(v);
+        w = swap16_sum(w);
+    }
+    if (lanes > 32) {
+        v = half_sum(v);
+        w = half_sum(w);
+    }
+}
 // over the lanes at the same place of the wavefront's teams
-__device__ __forceinline__ float across_teams(float v, int lanes) {
-    if (lanes <= 8) v += dpp<kDppRor8>(v);
-    if (lanes <= 16) v = swap16_sum(v);
-    if (lanes <= 32) v = half_sum(v);
-    return v;
+template <int N> __device__ __forceinline__ void across_teams(float (&v)[N], int lanes) {
+    if (lanes <= 8) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += dpp<kDppRor8>(v[i]);
+    }
+    if (lanes <= 16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = swap16_sum(v[i]);
+    }
+    if (lanes <= 32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = half_sum(v[i]);
+    }
 }
 
-constexpr int kForwardThreads = 256, kBackwardThreads = 512, kWideThreads = 512;
+constexpr int kForwardThreads = 256, kWideThreads = 512;
+// Threads of a backward block whose rows are held by lanes: as many as leave a lane the registers for its values (eight take 82, sixteen 150).
+constexpr int backward_threads(int values) { return values <= 8 ? 1024 : 512; }
 
 // Who works on a row: lanes of a wavefront, or (WIDE) a whole block, whose sums pass through LDS.
 template <bool WIDE> struct Team {
     int lanes, place;              // members, own number among them
-    float* part;                   // WIDE: a word for each wavefront, twice (sums of two successive calls do not meet)
+    float* part;                   // WIDE: two words for each wavefront, twice (sums of two successive calls do not meet)
     int turn = 0;
     __device__ __forceinline__ float sum(float v) {
         if constexpr (!WIDE) {
             return team_sum(v, lanes);
         } else {
-            v = wave_sum(v);
+            float none = 0.f;
+            sum(v, none);
+            return v;
+        }
+    }
+    // of two at once
+    __device__ __forceinline__ void sum(float& v, float& w) {
+        if constexpr (!WIDE) {
+            team_sum(v, w, lanes);
+        } else {
+            constexpr int W = kWideThreads / 64;
             float* p = part + turn;
-            turn ^= kWideThreads / 64;
-            if ((threadIdx.x & 63) == 0) p[threadIdx.x >> 6] = v;
+            turn ^= 2 * W;
+            v = wave_sum(v);
+            w = wave_sum(w);
+            if ((threadIdx.x & 63) == 0) {
+                p[threadIdx.x >> 6] = v;
+                p[W + (threadIdx.x >> 6)] = w;
+            }
             __syncthreads();
-            float s = (p[0] + p[1]) + (p[2] + p[3]);
-            if (lanes > 256) s += (p[4] + p[5]) + (p[6] + p[7]);
-            return s;
+            v = (p[0] + p[1]) + (p[2] + p[3]);
+            w = (p[W] + p[W + 1]) + (p[W + 2] + p[W + 3]);
+            if (lanes > 256) {
+                v += (p[4] + p[5]) + (p[6] + p[7]);
+                w += (p[W + 4] + p[W + 5]) + (p[W + 6] + p[W + 7]);
+            }
         }
     }
 };
 
-// The pieces of a row that a lane holds: ITERS of them, `lanes` pieces apart.
-template <int V, int ITERS, bool RAGGED> struct Held {
+// The pieces of a row that a lane holds: ITERS of them, `lanes` pieces apart.  Where the team's places are more than the row
+// (MASKED), a piece past the end is moved back to end with the row: all lanes load and compute alike, without branches, and only
+// values that no other place holds count in sums over the row.
+template <int V, int ITERS, bool MASKED> struct Held {
     int at[ITERS];                 // first channel
-    int skip[ITERS];               // values at its front that another piece holds
-    bool has[ITERS];
+    int skip[ITERS];               // values at its front that another place holds; V or more: all of them
     __device__ __forceinline__ Held(int place, int lanes, int c) {
-        const int pieces = (c + V - 1) / V;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int p = place + it * lanes;
-            has[it] = p < pieces;
-            const int from = p * V;
-            at[it] = RAGGED && has[it] && from > c - V ? c - V : from;
-            skip[it] = RAGGED ? from - at[it] : 0;
+            const int from = (place + it * lanes) * V;
+            at[it] = MASKED && from > c - V ? c - V : from;
+            skip[it] = MASKED ? from - at[it] : 0;
         }
     }
-    __device__ __forceinline__ bool counts(int it, int i) const { return !RAGGED || i >= skip[it]; }
+    __device__ __forceinline__ float counted(int it, int i, float v) const { return !MASKED || i >= skip[it] ? v : 0.f; }
+    __device__ __forceinline__ bool stores(int it) const { return !MASKED || skip[it] < V; }
 };
 
-template <typename T, int V, int ITERS, bool RAGGED, bool WIDE>
+template <typename T, int V, int ITERS, bool MASKED, bool WIDE>
 __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_forward(
     const T* x, const T* residual, const T* __restrict__ gamma, const T* __restrict__ beta, T* sum, T* __restrict__ y,
-    float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int c, int lanes, float eps) {
-    __shared__ float part[WIDE ? 2 * kWideThreads / 64 : 1];
+    float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int c, int lanes, int turns, float eps) {
+    __shared__ float part[WIDE ? 4 * kWideThreads / 64 : 1];
     typedef Pack<T, V> Pc;
     Team<WIDE> team{lanes, WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), part};
-    const Held<V, ITERS, RAGGED> held(team.place, team.lanes, c);
-    float gm[ITERS][V] = {}, bt[ITERS][V] = {};
+    const Held<V, ITERS, MASKED> held(team.place, team.lanes, c);
+    Pc gm[ITERS], bt[ITERS];
 #pragma unroll
-    for (int it = 0; it < ITERS; ++it)
-        if (held.has[it]) {
-            widen<T, V>(*(const Pc*)(gamma + held.at[it]), gm[it]);
-            widen<T, V>(*(const Pc*)(beta + held.at[it]), bt[it]);
-        }
+    for (int it = 0; it < ITERS; ++it) {
+        gm[it] = *(const Pc*)(gamma + held.at[it]);
+        bt[it] = *(const Pc*)(beta + held.at[it]);
+    }
     const float inv_c = 1.f / (float)c;
     const int per_block = WIDE ? 1 : (int)blockDim.x / lanes;
-    const int64_t stride = (int64_t)gridDim.x * per_block;
-    for (int64_t row = (int64_t)blockIdx.x * per_block + (WIDE ? 0 : threadIdx.x / lanes); row < rows; row += stride) {
+    const int64_t first = (int64_t)blockIdx.x * per_block * turns;
+    const int64_t end = first + (int64_t)per_block * turns < rows ? first + (int64_t)per_block * turns : rows;
+    for (int64_t row = first + (WIDE ? 0 : threadIdx.x / lanes); row < end; row += per_block) {
         const int64_t base = row * c;
         float v[ITERS][V];
         Pc kept[ITERS];
         float s = 0.f;
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) kept[it] = *(const Pc*)(x + base + held.at[it]);
+        for (int it = 0; it < ITERS; ++it) kept[it] = *(const Pc*)(x + base + held.at[it]);
         if (residual) {
+            Pc more[ITERS];
 #pragma unroll
-            for (int it = 0; it < ITERS; ++it)
-                if (held.has[it]) {
-                    float r[V];
-                    widen<T, V>(*(const Pc*)(residual + base + held.at[it]), r);
-                    widen<T, V>(kept[it], v[it]);
+            for (int it = 0; it < ITERS; ++it) more[it] = *(const Pc*)(residual + base + held.at[it]);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[i] += v[it][i];
-                    kept[it] = narrow<T, V>(r);
-                }
-        }
-#pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
+            for (int it = 0; it < ITERS; ++it) {
+                float r[V];
+                widen<T, V>(more[it], r);
                 widen<T, V>(kept[it], v[it]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) s += held.counts(it, i) ? v[it][i] : 0.f;
+                for (int i = 0; i < V; ++i) r[i] += v[it][i];
+                kept[it] = narrow<T, V>(r);
             }
+        }
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            widen<T, V>(kept[it], v[it]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s += held.counted(it, i, v[it][i]);
+        }
         const float mean = team.sum(s) * inv_c;
         float q = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    v[it][i] -= mean;
-                    q += held.counts(it, i) ? v[it][i] * v[it][i] : 0.f;
-                }
+            for (int i = 0; i < V; ++i) {
+                v[it][i] -= mean;
+                q += held.counted(it, i, v[it][i] * v[it][i]);
             }
         const float rstd = 1.f / sqrtf(team.sum(q) * inv_c + eps);
         if (mean_out && team.place == 0) {
@@ -164,111 +205,104 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
         }
         // (the sum may lie where x or the residual was: every value of the row has been read when its statistics are known)
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
-                if (residual) *(Pc*)(sum + base + held.at[it]) = kept[it];
-                float o[V];
+        for (int it = 0; it < ITERS; ++it) {
+            float o[V], g[V], b[V];
+            widen<T, V>(gm[it], g);
+            widen<T, V>(bt[it], b);
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = v[it][i] * rstd * gm[it][i] + bt[it][i];
+            for (int i = 0; i < V; ++i) o[i] = v[it][i] * rstd * g[i] + b[i];
+            if (held.stores(it)) {
+                if (residual) *(Pc*)(sum + base + held.at[it]) = kept[it];
                 *(Pc*)(y + base + held.at[it]) = narrow<T, V>(o);
             }
+        }
     }
 }
 
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
 // over its teams and wavefronts in a fixed order and leaves 2 c partial sums; with one block in all these are the result.
-template <typename T, int V, int ITERS, bool RAGGED, bool WIDE>
-__global__ __launch_bounds__(WIDE ? kWideThreads : kBackwardThreads) void k_ln_backward(
+template <typename T, int V, int ITERS, bool MASKED, bool WIDE>
+__global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) void k_ln_backward(
     const T* __restrict__ s, const T* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in, const T* dy,
     const T* dsum, T* dx, float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta, bool accumulate, int64_t rows,
     int c, int lanes, float eps) {
+    constexpr int THREADS = backward_threads(V * ITERS);
     extern __shared__ float joined[];                  // every wavefront's sums of dgamma and dbeta; WIDE: what Team needs
     typedef Pack<T, V> Pc;
     Team<WIDE> team{lanes, WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), joined};
-    const Held<V, ITERS, RAGGED> held(team.place, team.lanes, c);
-    float gm[ITERS][V] = {}, dg[ITERS][V] = {}, db[ITERS][V] = {};
+    const Held<V, ITERS, MASKED> held(team.place, team.lanes, c);
+    float dg[ITERS][V] = {}, db[ITERS][V] = {};
+    Pc gm[ITERS];
 #pragma unroll
-    for (int it = 0; it < ITERS; ++it)
-        if (held.has[it]) widen<T, V>(*(const Pc*)(gamma + held.at[it]), gm[it]);
+    for (int it = 0; it < ITERS; ++it) gm[it] = *(const Pc*)(gamma + held.at[it]);
     const float inv_c = 1.f / (float)c;
     const int per_block = WIDE ? 1 : (int)blockDim.x / lanes;
     const int64_t stride = (int64_t)gridDim.x * per_block;
     for (int64_t row = (int64_t)blockIdx.x * per_block + (WIDE ? 0 : threadIdx.x / lanes); row < rows; row += stride) {
         const int64_t base = row * c;
-        float u[ITERS][V] = {}, d[ITERS][V] = {};
+        float u[ITERS][V], d[ITERS][V];
         Pc pu[ITERS], pd[ITERS], ps[ITERS];
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
-                pu[it] = *(const Pc*)(s + base + held.at[it]);
-                pd[it] = *(const Pc*)(dy + base + held.at[it]);
-            }
+        for (int it = 0; it < ITERS; ++it) {
+            pu[it] = *(const Pc*)(s + base + held.at[it]);
+            pd[it] = *(const Pc*)(dy + base + held.at[it]);
+        }
         if (dsum) {
 #pragma unroll
-            for (int it = 0; it < ITERS; ++it)
-                if (held.has[it]) ps[it] = *(const Pc*)(dsum + base + held.at[it]);
+            for (int it = 0; it < ITERS; ++it) ps[it] = *(const Pc*)(dsum + base + held.at[it]);
         }
-        float t = 0.f;
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
-                widen<T, V>(pu[it], u[it]);
-                widen<T, V>(pd[it], d[it]);
-            }
+        for (int it = 0; it < ITERS; ++it) widen<T, V>(pu[it], u[it]);
         float mean, rstd;
         if (mean_in) {
             mean = mean_in[row];
             rstd = rstd_in[row];
         } else {
+            float t = 0.f, q = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it)
-                if (held.has[it]) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) t += held.counts(it, i) ? u[it][i] : 0.f;
-                }
+                for (int i = 0; i < V; ++i) t += held.counted(it, i, u[it][i]);
             mean = team.sum(t) * inv_c;
-            float q = 0.f;
 #pragma unroll
             for (int it = 0; it < ITERS; ++it)
-                if (held.has[it]) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) q += held.counts(it, i) ? (u[it][i] - mean) * (u[it][i] - mean) : 0.f;
-                }
+                for (int i = 0; i < V; ++i) q += held.counted(it, i, (u[it][i] - mean) * (u[it][i] - mean));
             rstd = 1.f / sqrtf(team.sum(q) * inv_c + eps);
         }
         float a = 0.f, b = 0.f;
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
+        for (int it = 0; it < ITERS; ++it) {
+            float g[V];
+            widen<T, V>(gm[it], g);
+            widen<T, V>(pd[it], d[it]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    u[it][i] = (u[it][i] - mean) * rstd;
-                    const float e = d[it][i];
-                    d[it][i] *= gm[it][i];
-                    if (held.counts(it, i)) {
-                        dg[it][i] += e * u[it][i];
-                        db[it][i] += e;
-                        a += d[it][i];
-                        b += d[it][i] * u[it][i];
-                    }
-                }
+            for (int i = 0; i < V; ++i) {
+                u[it][i] = (u[it][i] - mean) * rstd;
+                dg[it][i] += d[it][i] * u[it][i];              // (another place's values too, which leave() never takes)
+                db[it][i] += d[it][i];
+                d[it][i] *= g[i];
+                const float h = held.counted(it, i, d[it][i]);
+                a += h;
+                b += h * u[it][i];
             }
-        a = team.sum(a) * inv_c;
-        b = team.sum(b) * inv_c;
+        }
+        team.sum(a, b);
+        a *= inv_c;
+        b *= inv_c;
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-            if (held.has[it]) {
-                float o[V];
+        for (int it = 0; it < ITERS; ++it) {
+            float o[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = rstd * (d[it][i] - a - u[it][i] * b);
-                if (dsum) {
-                    float r[V];
-                    widen<T, V>(ps[it], r);
+            for (int i = 0; i < V; ++i) o[i] = rstd * (d[it][i] - a - u[it][i] * b);
+            if (dsum) {
+                float r[V];
+                widen<T, V>(ps[it], r);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) o[i] += r[i];
-                }
-                *(Pc*)(dx + base + held.at[it]) = narrow<T, V>(o);
+                for (int i = 0; i < V; ++i) o[i] += r[i];
             }
+            if (held.stores(it)) *(Pc*)(dx + base + held.at[it]) = narrow<T, V>(o);
+        }
     }
     const bool alone = gridDim.x == 1;
     float* out = partial + (size_t)blockIdx.x * 2 * c;
@@ -283,21 +317,18 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kBackwardThreads) void k_ln_b
     if constexpr (WIDE) {
 #pragma unroll
         for (int it = 0; it < ITERS; ++it)
-            if (held.has[it])
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (held.counts(it, i)) {
-                        leave(held.at[it] + i, dg[it][i]);
-                        leave(c + held.at[it] + i, db[it][i]);
-                    }
+            for (int i = 0; i < V; ++i)
+                if (!MASKED || i >= held.skip[it]) {
+                    leave(held.at[it] + i, dg[it][i]);
+                    leave(c + held.at[it] + i, db[it][i]);
+                }
     } else {
 #pragma unroll
-        for (int it = 0; it < ITERS; ++it)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                dg[it][i] = across_teams(dg[it][i], lanes);
-                db[it][i] = across_teams(db[it][i], lanes);
-            }
+        for (int it = 0; it < ITERS; ++it) {
+            across_teams<V>(dg[it], lanes);
+            across_teams<V>(db[it], lanes);
+        }
         // each wavefront's sums by (kind, piece, value, lane), then a thread adds up a channel's over the wavefronts
         const int wave = threadIdx.x >> 6, slots = ITERS * V * lanes;
         if ((int)(threadIdx.x & 63) < lanes) {
@@ -312,12 +343,12 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kBackwardThreads) void k_ln_b
         }
         __syncthreads();
         const int last = (c + V - 1) / V - 1;
-        for (int ch = threadIdx.x; ch < c; ch += kBackwardThreads) {
-            const int p = ch / V, i = RAGGED && p == last ? ch - (c - V) : ch % V;
+        for (int ch = threadIdx.x; ch < c; ch += THREADS) {
+            const int p = ch / V, i = MASKED && p == last ? ch - (c - V) : ch % V;
             const float* from = joined + (p / lanes * V + i) * lanes + (p & (lanes - 1));
             float g = 0.f, b = 0.f;
 #pragma unroll
-            for (int w = 0; w < kBackwardThreads / 64; ++w) {
+            for (int w = 0; w < THREADS / 64; ++w) {
                 g += from[w * 2 * slots];
                 b += from[w * 2 * slots + slots];
             }
@@ -350,21 +381,21 @@ __global__ __launch_bounds__(1024) void k_ln_join(const float* __restrict__ part
 // ---- which kernel takes a shape ------------------------------------------------------------
 // Pieces are 16 bytes (one value where the row is shorter).  A lane holds at most sixteen values: with the sums of dgamma and dbeta beside them
 // more would leave two wavefronts per SIMD, or spill.  Of the ways to cover a row by lanes times pieces the one with the
-// fewest idle places is taken, of equals the one with the most lanes; rows of more than 64 such lanes are a block's, of 256 threads or, beyond 512 pieces, of 512.
+// fewest idle places is taken, of equals the one with the most lanes; rows of more than 64 such lanes are a block's, of 256 threads or, beyond 256 pieces, of 512.
 struct Shape {
     int v, iters, lanes;
-    bool ragged, wide;
+    bool masked, wide;
 };
 static Shape shape_of(int dtype, int c) {
     Shape s{dtype == FF_F32 ? 4 : 8, 1, 8, false, false};
     if (c < s.v) s.v = 1;
     const int pieces = (c + s.v - 1) / s.v;
-    s.ragged = c % s.v != 0;
     const int most = s.v == 8 ? 2 : 4;
     if (pieces > 64 * most) {
         s.wide = true;
-        s.lanes = pieces > 512 ? kWideThreads : 256;
+        s.lanes = pieces > 256 ? kWideThreads : 256;
         s.iters = (pieces + s.lanes - 1) / s.lanes;
+        s.masked = c != s.lanes * s.iters * s.v;
         return s;
     }
     int best = 1 << 30;
@@ -375,13 +406,14 @@ static Shape shape_of(int dtype, int c) {
         s.iters = iters;
         s.lanes = lanes;
     }
+    s.masked = c != s.lanes * s.iters * s.v;
     return s;
 }
 
 template <typename F> static void with_shape(const Shape& s, F go) {
-    auto it = [&](auto v, auto ragged) {
+    auto it = [&](auto v, auto masked) {
         constexpr int V = decltype(v)::value;
-        constexpr bool R = decltype(ragged)::value;
+        constexpr bool R = decltype(masked)::value;
         auto at = [&](auto wide) {
             if (s.iters == 1) go(v, std::integral_constant<int, 1>{}, std::bool_constant<R>{}, wide);
             else if (s.iters == 2) go(v, std::integral_constant<int, 2>{}, std::bool_constant<R>{}, wide);
@@ -394,30 +426,44 @@ template <typename F> static void with_shape(const Shape& s, F go) {
         else at(std::false_type{});
     };
     auto full = [&](auto v) {
-        if (s.ragged) it(v, std::true_type{});
+        if (s.masked) it(v, std::true_type{});
         else it(v, std::false_type{});
     };
     if (s.v == 8) full(std::integral_constant<int, 8>{});
     else if (s.v == 4) full(std::integral_constant<int, 4>{});
-    else go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::false_type{}, std::false_type{});
+    else go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::true_type{}, std::false_type{});
 }
 
 static int64_t turns_of(int64_t rows, int per_block) { return (rows + per_block - 1) / per_block; }
+
+// How often a block of the forward pass loads rows, `bytes` at a time.  The rows of a block follow each other and blocks start in
+// order, so that what the card works on at one time lies together: 2048 x 2048 x 128 took 505 us with as many blocks as fit on
+// the card, each striding over the whole tensor, 428 with a turn each, 377 with two.  Blocks of less than 8 KiB come faster than
+// the card starts them (196608 x 384: 77 us with one turn of 3 KiB, 59 with four), more turns gain nothing (16: 411).
+static int forward_turns(int64_t all, int64_t bytes) {
+    const int64_t most_blocks = 1 << 22;               // the grid's threads stay below 2^32
+    int64_t turns = 10240 / bytes, spread = all / (16 * compute_units());
+    if (turns > spread) turns = spread;
+    if (turns < 1) turns = 1;
+    if (all / turns >= most_blocks) turns = (all + most_blocks - 1) / most_blocks;
+    return (int)turns;
+}
 
 template <typename T>
 static void forward_t(const ff_norm_desc& d, const void* x, const void* residual, const void* gamma, const void* beta, void* sum, void* y,
                       float* mean, float* rstd, hipStream_t stream) {
     const Shape s = shape_of(d.dtype, d.c);
-    with_shape(s, [&](auto v, auto iters, auto ragged, auto wide) {
+    with_shape(s, [&](auto v, auto iters, auto masked, auto wide) {
         constexpr int V = decltype(v)::value, I = decltype(iters)::value;
-        constexpr bool R = decltype(ragged)::value, W = decltype(wide)::value;
+        constexpr bool R = decltype(masked)::value, W = decltype(wide)::value;
         if constexpr (V != (sizeof(T) == 4 ? 8 : 4)) {
             const int threads = W ? s.lanes : kForwardThreads;
-            int64_t blocks = turns_of(d.rows, W ? 1 : threads / s.lanes);
-            const int64_t cap = (int64_t)compute_units() * (W ? 4 : 16);
-            if (blocks > cap) blocks = cap;
+            const int per_block = W ? 1 : threads / s.lanes;
+            const int64_t all = turns_of(d.rows, per_block);
+            const int turns = forward_turns(all, (int64_t)per_block * d.c * sizeof(T) * (residual ? 2 : 1));
+            const int64_t blocks = (all + turns - 1) / turns;
             hipLaunchKernelGGL((k_ln_forward<T, V, I, R, W>), dim3((unsigned)blocks), dim3(threads), 0, stream, (const T*)x, (const T*)residual,
-                               (const T*)gamma, (const T*)beta, (T*)sum, (T*)y, mean, rstd, d.rows, d.c, s.lanes, d.ln_eps);
+                               (const T*)gamma, (const T*)beta, (T*)sum, (T*)y, mean, rstd, d.rows, d.c, s.lanes, turns, d.ln_eps);
         }
     });
 }
@@ -430,12 +476,13 @@ ff_status layernorm_forward_run(const ff_norm_desc& d, const void* x, const void
     return check_launch("ff_layernorm_forward");
 }
 
-// Blocks of the backward pass.  A number of its own, not the device's, so that the order of the sums does not depend on the machine.
-constexpr int kBackwardBlocks = 512;
+// Blocks of the backward pass.  Numbers of its own, not the device's, so that the order of the sums does not depend on the machine.
+constexpr int kBackwardBlocks = 256, kBackwardBlocksWide = 512;
 static int backward_blocks(const ff_norm_desc& d, const Shape& s) {
-    const int64_t turns = turns_of(d.rows, s.wide ? 1 : kBackwardThreads / s.lanes);
+    const int64_t turns = turns_of(d.rows, s.wide ? 1 : backward_threads(s.v * s.iters) / s.lanes);
     if (turns <= 4) return turns > 0;                  // one block: no partial sums, no second launch
-    return (int)(turns < kBackwardBlocks ? turns : kBackwardBlocks);
+    const int most = s.wide && s.v * s.iters <= 8 ? kBackwardBlocksWide : kBackwardBlocks;
+    return (int)(turns < most ? turns : most);
 }
 
 size_t layernorm_backward_workspace(const ff_norm_desc& d) {
@@ -446,12 +493,12 @@ size_t layernorm_backward_workspace(const ff_norm_desc& d) {
 template <typename T>
 static void backward_t(const ff_norm_desc& d, const Shape& s, int blocks, const void* src, const void* gamma, const float* mean, const float* rstd, const void* dy,
                        const void* dsum, void* dx, float* dgamma, float* dbeta, bool accumulate, float* partial, hipStream_t stream) {
-    with_shape(s, [&](auto v, auto iters, auto ragged, auto wide) {
+    with_shape(s, [&](auto v, auto iters, auto masked, auto wide) {
         constexpr int V = decltype(v)::value, I = decltype(iters)::value;
-        constexpr bool R = decltype(ragged)::value, W = decltype(wide)::value;
+        constexpr bool R = decltype(masked)::value, W = decltype(wide)::value;
         if constexpr (V != (sizeof(T) == 4 ? 8 : 4)) {
-            const size_t lds = W ? 2 * kWideThreads / 64 * sizeof(float) : (size_t)kBackwardThreads / 64 * 2 * I * V * s.lanes * sizeof(float);     // at most 64 KiB
-            hipLaunchKernelGGL((k_ln_backward<T, V, I, R, W>), dim3(blocks), dim3(W ? s.lanes : kBackwardThreads), lds, stream, (const T*)src,
+            const size_t lds = W ? 4 * kWideThreads / 64 * sizeof(float) : (size_t)backward_threads(I * V) / 64 * 2 * I * V * s.lanes * sizeof(float);     // at most 64 KiB
+            hipLaunchKernelGGL((k_ln_backward<T, V, I, R, W>), dim3(blocks), dim3(W ? s.lanes : backward_threads(I * V)), lds, stream, (const T*)src,
                                (const T*)gamma, mean, rstd, (const T*)dy, (const T*)dsum, (T*)dx, partial, dgamma, dbeta, accumulate, d.rows, d.c,
                                s.lanes, d.ln_eps);
         }
