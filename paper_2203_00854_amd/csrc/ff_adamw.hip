@@ -9,11 +9,10 @@
 
 namespace ff {
 
-constexpr int kGroup = 256;              // values that share an exponent in 8-bit states; half a wavefront holds them, eight a lane
-constexpr int kPer = 8;
+constexpr int kGroup = 256;              // values that share an exponent in 8-bit states
 constexpr int kTurn = 8 * kGroup;        // values that a block of 256 threads holds at one time
 constexpr int kPiece = 2 * kTurn;
-constexpr int kNormBlocks = 1024;        // partial sums of the norm
+constexpr int kNormBlocks = 2048;        // partial sums of the norm
 constexpr int kTopM = 14, kTopV = 30;    // exponent field of a group's largest magnitude among the codes: the highest that rounding up cannot leave
 
 struct Piece {
@@ -88,6 +87,64 @@ void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* ts, void* pl
     head->values = value;
 }
 
+// ---- four neighbours ---------------------------------------------------------------------
+// A record's pointers are read from memory, where the compiler cannot see that they lead to global memory: it is told, or it would use loads
+// that look for LDS behind every address.
+template <typename T> struct At {
+    typedef __attribute__((address_space(1))) T One;
+    typedef T Vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));        // at the alignment of one value
+    typedef __attribute__((address_space(1))) Vec Four;
+};
+template <typename T> __device__ __forceinline__ typename At<T>::One* global(void* p) { return (typename At<T>::One*)p; }
+template <typename T> __device__ __forceinline__ const typename At<T>::One* global(const void* p) { return (const typename At<T>::One*)p; }
+
+template <typename T> __device__ __forceinline__ void load4(const void* base, int at, int n, float (&v)[4]) {       // n: values that are there
+    const auto p = global<T>(base) + at;
+    if (n >= 4) {
+        const typename At<T>::Vec f = *(const typename At<T>::Four*)p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = to_f32<T>(f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32<T>(p[i]) : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store4(void* base, int at, int n, const float (&v)[4]) {
+    const auto p = global<T>(base) + at;
+    typename At<T>::Vec f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = from_f32<T>(v[i]);
+    if (n >= 4) {
+        *(typename At<T>::Four*)p = f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) p[i] = f[i];
+    }
+}
+__device__ __forceinline__ uint32_t load4(const void* base, int at, int n) {                                       // four codes
+    const auto p = global<uint8_t>(base) + at;
+    uint32_t w = 0;
+    if (n >= 4) {
+        w = __builtin_bit_cast(uint32_t, (At<uint8_t>::Vec)(*(const At<uint8_t>::Four*)p));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) w |= (uint32_t)p[i] << 8 * i;
+    }
+    return w;
+}
+__device__ __forceinline__ void store4(void* base, int at, int n, uint32_t w) {
+    const auto p = global<uint8_t>(base) + at;
+    if (n >= 4) {
+        *(At<uint8_t>::Four*)p = __builtin_bit_cast(At<uint8_t>::Vec, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) p[i] = (uint8_t)(w >> 8 * i);
+    }
+}
+
 // ---- 8-bit states ------------------------------------------------------------------------
 // over the 32 lanes of half a wavefront
 __device__ __forceinline__ uint32_t max32(uint32_t x) {
@@ -110,18 +167,21 @@ __device__ __forceinline__ uint32_t dither_bits(uint32_t index, uint32_t seed) {
     return h ^ (h >> 16);
 }
 
-// code of |x| in a group whose largest magnitude has exponent field e; r: 16 random bits below the code's last place
-template <int TOP> __device__ __forceinline__ uint32_t encode(float mag, uint32_t e, uint32_t r) {
-    return (__float_as_uint(__builtin_ldexpf(mag, TOP - (int)e)) + (r << 4)) >> 20;
-}
-template <int TOP> __device__ __forceinline__ float decode(uint32_t code, uint32_t e) {
-    const float x = __builtin_ldexpf(__uint_as_float(code << 20), (int)e - TOP);
-    return e == 255u ? __uint_as_float(0x7fc00000u) : x;
-}
-__device__ __forceinline__ float decode_m(uint8_t code, uint32_t e) {
-    const float x = decode<kTopM>(code & 0x7fu, e);
-    return code & 0x80u ? -x : x;
-}
+// A group's exponent field e turns codes into values by a shift of the exponent, e - TOP, and into NaN where a member was not finite.
+template <int TOP> struct Scale {
+    int shift;
+    uint32_t nan;
+    __device__ __forceinline__ explicit Scale(uint32_t e) : shift((int)e - TOP), nan(e == 255u ? 0x7fc00000u : 0u) {}
+    // code i of four; TOP 14 has a sign in the upper bit
+    __device__ __forceinline__ float value(uint32_t four, int i) const {
+        const uint32_t w = four >> 8 * i;
+        uint32_t bits = (w & (TOP == kTopM ? 0x7fu : 0xffu)) << 20 | nan;
+        if constexpr (TOP == kTopM) bits |= w << 24 & 0x80000000u;
+        return __builtin_ldexpf(__uint_as_float(bits), shift);
+    }
+    // code of |x|; r: 16 random bits at places 4 to 19, below the code's last
+    __device__ __forceinline__ uint32_t code(float mag, uint32_t r) const { return (__float_as_uint(__builtin_ldexpf(mag, -shift)) + r) >> 20; }
+};
 
 // ---- norm of all gradients ---------------------------------------------------------------
 // squares and sums in float64: no square leaves its range, and the order of the sums does not show in the float32 result
@@ -138,12 +198,17 @@ __global__ __launch_bounds__(256) void k_grad_norm(const Piece* __restrict__ pie
     double sum = 0.;
     for (int i = blockIdx.x; i < n_pieces; i += gridDim.x) {
         const Piece& pc = pieces[i];
-        if (pc.tag != tag) continue;
-        const G* g = (const G*)pc.g;
-        for (int j = threadIdx.x; j < pc.n; j += 256) {
-            const double x = to_f32<G>(g[j]);
-            sum += x * x;
+        const int n = pc.tag == tag ? pc.n : 0;
+        float v[kPiece / 1024][4];
+#pragma unroll
+        for (int t = 0; t < kPiece / 1024; ++t) {
+            const int at = (threadIdx.x + 256 * t) * 4;
+            load4<G>(pc.g, at, n - at, v[t]);
         }
+#pragma unroll
+        for (int t = 0; t < kPiece / 1024; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += (double)v[t][j] * (double)v[t][j];
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
@@ -173,6 +238,14 @@ ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_by
 }
 
 // ---- the step ----------------------------------------------------------------------------
+// The square root and the reciprocal are the machine's, good to a unit in their last place: they reach the weight alone, where
+// they are 2^-23 of the step.  (It takes no subnormal numbers: those are brought into its range.)
+__device__ __forceinline__ float root_of(float v) {
+    const bool small = v < 0x1p-100f;
+    const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p60f : v);
+    return small ? r * 0x1p-30f : r;
+}
+
 template <typename P, typename G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces, uint32_t tag, StepArgs a, const float* __restrict__ norm) {
     const Piece& pc = pieces[blockIdx.x];
@@ -186,65 +259,89 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
     if (pc.tag != tag) return;
     const int lane = threadIdx.x & 31;
     const float keep = 1.f - a.lr * pc.decay;
-    const G* g_ = (const G*)pc.g;
-    P* p_ = (P*)pc.p;
     for (int base = (threadIdx.x >> 5) * kGroup; base < pc.n; base += kTurn) {
-        float m[kPer], v[kPer], w[kPer];
-        uint32_t em = 0, ev = 0;
+        float m[2][4], v[2][4], w[2][4], g[2][4];
+        [[maybe_unused]] uint32_t fm[2], fv[2], em, ev;
         if constexpr (BITS == 8) {
-            em = pc.m_exp[base / kGroup];
-            ev = pc.v_exp[base / kGroup];
+            em = global<uint8_t>((const void*)pc.m_exp)[base / kGroup];
+            ev = global<uint8_t>((const void*)pc.v_exp)[base / kGroup];
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int at = base + lane + 32 * i;
-            m[i] = v[i] = w[i] = 0.f;
-            if (at < pc.n) {
-                const float g = to_f32<G>(g_[at]) * k;
-                if constexpr (BITS == 8) {
-                    m[i] = decode_m(((const uint8_t*)pc.m)[at], em);
-                    v[i] = decode<kTopV>(((const uint8_t*)pc.v)[at], ev);
-                } else {
-                    m[i] = ((const float*)pc.m)[at];
-                    v[i] = ((const float*)pc.v)[at];
-                }
-                w[i] = pc.master ? pc.master[at] : to_f32<P>(p_[at]);
-                m[i] = a.beta1 * m[i] + a.rest1 * g;
-                v[i] = a.beta2 * v[i] + a.rest2 * (g * g);
-                w[i] = w[i] * keep - a.step_size * (m[i] / (sqrtf(v[i]) * a.inv_root + a.eps));
+        for (int h = 0; h < 2; ++h) {
+            const int at = base + h * 128 + lane * 4, there = pc.n - at;
+            load4<G>(pc.g, at, there, g[h]);
+            if (pc.master) load4<float>(pc.master, at, there, w[h]);
+            else load4<P>(pc.p, at, there, w[h]);
+            if constexpr (BITS == 8) {
+                fm[h] = load4(pc.m, at, there);
+                fv[h] = load4(pc.v, at, there);
+            } else {
+                load4<float>(pc.m, at, there, m[h]);
+                load4<float>(pc.v, at, there, v[h]);
             }
         }
         if constexpr (BITS == 8) {
+            const Scale<kTopM> sm(em);
+            const Scale<kTopV> sv(ev);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    m[h][i] = sm.value(fm[h], i);
+                    v[h][i] = sv.value(fv[h], i);
+                }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = g[h][i] * k;
+                m[h][i] = a.beta1 * m[h][i] + a.rest1 * x;
+                v[h][i] = a.beta2 * v[h][i] + a.rest2 * (x * x);
+                const float root = root_of(v[h][i]) * a.inv_root + a.eps;
+                w[h][i] = w[h][i] * keep - a.step_size * (m[h][i] * __builtin_amdgcn_rcpf(root));
+            }
+            const int at = base + h * 128 + lane * 4, there = pc.n - at;
+            if (pc.master) store4<float>(pc.master, at, there, w[h]);
+            store4<P>(pc.p, at, there, w[h]);
+            if constexpr (BITS == 32) {
+                store4<float>(pc.m, at, there, m[h]);
+                store4<float>(pc.v, at, there, v[h]);
+            }
+        }
+        if constexpr (BITS == 8) {
+            // places past the tensor's end have loaded zeros, but for NaN in a group that holds it: they stay out of the maximum
             uint32_t mm = 0, mv = 0;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const uint32_t bm = __float_as_uint(m[i]) & 0x7fffffffu, bv = __float_as_uint(v[i]) & 0x7fffffffu;
-                mm = mm > bm ? mm : bm;
-                mv = mv > bv ? mv : bv;
-            }
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (base + h * 128 + lane * 4 + i < pc.n) {
+                        const uint32_t bm = __float_as_uint(m[h][i]) & 0x7fffffffu, bv = __float_as_uint(v[h][i]) & 0x7fffffffu;
+                        mm = mm > bm ? mm : bm;
+                        mv = mv > bv ? mv : bv;
+                    }
             em = max32(mm) >> 23;
             ev = max32(mv) >> 23;
             if (lane == 0) {
-                pc.m_exp[base / kGroup] = (uint8_t)em;
-                pc.v_exp[base / kGroup] = (uint8_t)ev;
+                global<uint8_t>(pc.m_exp)[base / kGroup] = (uint8_t)em;
+                global<uint8_t>(pc.v_exp)[base / kGroup] = (uint8_t)ev;
             }
-        }
+            const Scale<kTopM> sm(em);
+            const Scale<kTopV> sv(ev);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int at = base + lane + 32 * i;
-            if (at >= pc.n) continue;
-            if (pc.master) pc.master[at] = w[i];
-            p_[at] = from_f32<P>(w[i]);
-            if constexpr (BITS == 8) {
-                const uint32_t r = dither_bits(pc.first_group * kGroup + (uint32_t)at, a.seed);
-                uint32_t cm = encode<kTopM>(fabsf(m[i]), em, r & 0xffffu) | (__float_as_uint(m[i]) >> 31 << 7);
-                uint32_t cv = encode<kTopV>(v[i], ev, r >> 16);
-                cv = cv == 0 && v[i] > 0.f ? 1u : cv;
-                ((uint8_t*)pc.m)[at] = (uint8_t)(em == 255u ? 0u : cm);
-                ((uint8_t*)pc.v)[at] = (uint8_t)(ev == 255u ? 0u : cv);
-            } else {
-                ((float*)pc.m)[at] = m[i];
-                ((float*)pc.v)[at] = v[i];
+            for (int h = 0; h < 2; ++h) {
+                const int at = base + h * 128 + lane * 4, there = pc.n - at;
+                uint32_t cm = 0, cv = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t r = dither_bits(pc.first_group * kGroup + (uint32_t)(at + i), a.seed);
+                    cm |= (sm.code(fabsf(m[h][i]), r << 4 & 0xffff0u) | (__float_as_uint(m[h][i]) >> 31 << 7)) << 8 * i;
+                    const uint32_t c = sv.code(v[h][i], r >> 12 & 0xffff0u);
+                    cv |= (c == 0 && v[h][i] > 0.f ? 1u : c) << 8 * i;
+                }
+                store4(pc.m, at, there, em == 255u ? 0u : cm);
+                store4(pc.v, at, there, ev == 255u ? 0u : cv);
             }
         }
     }
@@ -281,9 +378,28 @@ template <int BITS>
 __global__ __launch_bounds__(256) void k_moments(const Piece* __restrict__ pieces, uint32_t tag, float* __restrict__ m_out, float* __restrict__ v_out) {
     const Piece& pc = pieces[blockIdx.x];
     if (pc.tag != tag) return;
-    for (int at = threadIdx.x; at < pc.n; at += 256) {
-        if (m_out) m_out[pc.first_value + at] = BITS == 8 ? decode_m(((const uint8_t*)pc.m)[at], pc.m_exp[at / kGroup]) : ((const float*)pc.m)[at];
-        if (v_out) v_out[pc.first_value + at] = BITS == 8 ? decode<kTopV>(((const uint8_t*)pc.v)[at], pc.v_exp[at / kGroup]) : ((const float*)pc.v)[at];
+    const int lane = threadIdx.x & 31;
+    for (int base = (threadIdx.x >> 5) * kGroup; base < pc.n; base += kTurn) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = base + h * 128 + lane * 4, there = pc.n - at;
+            float m[4], v[4];
+            if constexpr (BITS == 8) {
+                const Scale<kTopM> sm(global<uint8_t>((const void*)pc.m_exp)[base / kGroup]);
+                const Scale<kTopV> sv(global<uint8_t>((const void*)pc.v_exp)[base / kGroup]);
+                const uint32_t fm = load4(pc.m, at, there), fv = load4(pc.v, at, there);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    m[i] = sm.value(fm, i);
+                    v[i] = sv.value(fv, i);
+                }
+            } else {
+                load4<float>(pc.m, at, there, m);
+                load4<float>(pc.v, at, there, v);
+            }
+            if (m_out) store4<float>(m_out + pc.first_value, at, there, m);
+            if (v_out) store4<float>(v_out + pc.first_value, at, there, v);
+        }
     }
 }
 
