@@ -5,6 +5,8 @@
 // that small tensors cost a block and large ones as many as they have pieces.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ff_common.h"
 
 namespace ff {
@@ -98,50 +100,62 @@ template <typename T> struct At {
 template <typename T> __device__ __forceinline__ typename At<T>::One* global(void* p) { return (typename At<T>::One*)p; }
 template <typename T> __device__ __forceinline__ const typename At<T>::One* global(const void* p) { return (const typename At<T>::One*)p; }
 
-template <typename T> __device__ __forceinline__ void load4(const void* base, int at, int n, float (&v)[4]) {       // n: values that are there
+// Values at, .. at + 3 of a piece of n; WHOLE: all of them are there.
+template <bool WHOLE, typename T> __device__ __forceinline__ void load4(const void* base, int at, int n, float (&v)[4]) {
     const auto p = global<T>(base) + at;
-    if (n >= 4) {
+    if constexpr (WHOLE) {
         const typename At<T>::Vec f = *(const typename At<T>::Four*)p;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = to_f32<T>(f[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32<T>(p[i]) : 0.f;
+        for (int i = 0; i < 4; ++i) v[i] = at + i < n ? to_f32<T>(p[i]) : 0.f;
     }
 }
-template <typename T> __device__ __forceinline__ void store4(void* base, int at, int n, const float (&v)[4]) {
+template <bool WHOLE, typename T> __device__ __forceinline__ void store4(void* base, int at, int n, const float (&v)[4]) {
     const auto p = global<T>(base) + at;
     typename At<T>::Vec f;
+    if constexpr (sizeof(T) == 2) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        f = __builtin_bit_cast(typename At<T>::Vec, __builtin_convertvector((f32x4{v[0], v[1], v[2], v[3]}), bf16x4));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = from_f32<T>(v[i]);
-    if (n >= 4) {
+        for (int i = 0; i < 4; ++i) f[i] = v[i];
+    }
+    if constexpr (WHOLE) {
         *(typename At<T>::Four*)p = f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < n) p[i] = f[i];
+        for (int i = 0; i < 4; ++i)
+            if (at + i < n) p[i] = f[i];
     }
 }
-__device__ __forceinline__ uint32_t load4(const void* base, int at, int n) {                                       // four codes
+template <bool WHOLE> __device__ __forceinline__ uint32_t load4(const void* base, int at, int n) {                   // four codes
     const auto p = global<uint8_t>(base) + at;
+    if constexpr (WHOLE) return __builtin_bit_cast(uint32_t, (At<uint8_t>::Vec)(*(const At<uint8_t>::Four*)p));
     uint32_t w = 0;
-    if (n >= 4) {
-        w = __builtin_bit_cast(uint32_t, (At<uint8_t>::Vec)(*(const At<uint8_t>::Four*)p));
-    } else {
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < n) w |= (uint32_t)p[i] << 8 * i;
-    }
+    for (int i = 0; i < 4; ++i) w |= at + i < n ? (uint32_t)p[i] << 8 * i : 0u;
     return w;
 }
-__device__ __forceinline__ void store4(void* base, int at, int n, uint32_t w) {
+template <bool WHOLE> __device__ __forceinline__ void store4(void* base, int at, int n, uint32_t w) {
     const auto p = global<uint8_t>(base) + at;
-    if (n >= 4) {
+    if constexpr (WHOLE) {
         *(At<uint8_t>::Four*)p = __builtin_bit_cast(At<uint8_t>::Vec, w);
     } else {
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < n) p[i] = (uint8_t)(w >> 8 * i);
+        for (int i = 0; i < 4; ++i)
+            if (at + i < n) p[i] = (uint8_t)(w >> 8 * i);
+    }
+}
+
+// The turns of a piece, 512 values to a wavefront: whole ones without a check of any lane, then the one at its end.
+template <typename F> __device__ __forceinline__ void turns(int n, F go) {
+    for (int first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 2 * kGroup; first < n; first += kTurn) {
+        const int base = first + (threadIdx.x & 32) * (kGroup / 32);
+        if (first + 2 * kGroup <= n) go(std::true_type{}, base);
+        else go(std::false_type{}, base);
     }
 }
 
@@ -160,8 +174,8 @@ __device__ __forceinline__ uint32_t max32(uint32_t x) {
 // 32 bits from the index of a value and the step's seed, each round xor with the upper half and a product with an odd factor
 // (2^32 / golden ratio, and the leading digits of pi and of e - 2): enough for the bits of neighbours and of successive
 // steps to be unrelated.
-__device__ __forceinline__ uint32_t dither_bits(uint32_t index, uint32_t seed) {
-    uint32_t h = index + seed * 0x9E3779B1u;
+constexpr uint32_t kDitherSeed = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t dither_bits(uint32_t h) {                  // h: index + seed kDitherSeed
     h = (h ^ (h >> 16)) * 0x243F6A89u;
     h = (h ^ (h >> 15)) * 0xB7E15163u;
     return h ^ (h >> 16);
@@ -179,8 +193,8 @@ template <int TOP> struct Scale {
         if constexpr (TOP == kTopM) bits |= w << 24 & 0x80000000u;
         return __builtin_ldexpf(__uint_as_float(bits), shift);
     }
-    // code of |x|; r: 16 random bits at places 4 to 19, below the code's last
-    __device__ __forceinline__ uint32_t code(float mag, uint32_t r) const { return (__float_as_uint(__builtin_ldexpf(mag, -shift)) + r) >> 20; }
+    // code of a magnitude; r: 16 random bits, which stand below the code's last place
+    __device__ __forceinline__ uint32_t code(float mag, uint32_t r) const { return (__float_as_uint(__builtin_ldexpf(mag, -shift)) + (r << 4)) >> 20; }
 };
 
 // ---- norm of all gradients ---------------------------------------------------------------
@@ -196,19 +210,27 @@ __device__ __forceinline__ double block_sum(double x) {
 template <typename G>
 __global__ __launch_bounds__(256) void k_grad_norm(const Piece* __restrict__ pieces, int n_pieces, uint32_t tag, double* __restrict__ partial) {
     double sum = 0.;
+    const void* g = pieces[blockIdx.x].g;
+    int n = pieces[blockIdx.x].tag == tag ? pieces[blockIdx.x].n : 0;
     for (int i = blockIdx.x; i < n_pieces; i += gridDim.x) {
-        const Piece& pc = pieces[i];
-        const int n = pc.tag == tag ? pc.n : 0;
+        // the next piece's record is on its way while this one's values are
+        const Piece& next = pieces[i + (int)gridDim.x < n_pieces ? i + (int)gridDim.x : i];
+        const void* g_next = next.g;
+        const int n_next = next.tag == tag ? next.n : 0;
         float v[kPiece / 1024][4];
+        if (n == kPiece) {
 #pragma unroll
-        for (int t = 0; t < kPiece / 1024; ++t) {
-            const int at = (threadIdx.x + 256 * t) * 4;
-            load4<G>(pc.g, at, n - at, v[t]);
+            for (int t = 0; t < kPiece / 1024; ++t) load4<true, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < kPiece / 1024; ++t) load4<false, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
         }
 #pragma unroll
         for (int t = 0; t < kPiece / 1024; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum += (double)v[t][j] * (double)v[t][j];
+        g = g_next;
+        n = n_next;
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
@@ -239,13 +261,14 @@ ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_by
 
 // ---- the step ----------------------------------------------------------------------------
 // The square root and the reciprocal are the machine's, good to a unit in their last place: they reach the weight alone, where
-// they are 2^-23 of the step.  (It takes no subnormal numbers: those are brought into its range.)
+// they are 2^-23 of the step.  The root takes no subnormal numbers: a v below 2^-126 counts as that (as whole numbers, so that NaN stays the larger).
 __device__ __forceinline__ float root_of(float v) {
-    const bool small = v < 0x1p-100f;
-    const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p60f : v);
-    return small ? r * 0x1p-30f : r;
+    const uint32_t b = __float_as_uint(v);
+    return __builtin_amdgcn_sqrtf(__uint_as_float(b > 0x00800000u ? b : 0x00800000u));
 }
 
+// 32-bit states: 28 bytes a value for float32 tensors, bound by HBM (48 Evoformer blocks, 49.1 M values: 255 us, 5.4 TB/s).
+// 8-bit states: some 70 vector instructions a value for 10 to 16 bytes; where the tensors are bfloat16 these, not HBM, bound it.
 template <typename P, typename G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces, uint32_t tag, StepArgs a, const float* __restrict__ norm) {
     const Piece& pc = pieces[blockIdx.x];
@@ -259,25 +282,30 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
     if (pc.tag != tag) return;
     const int lane = threadIdx.x & 31;
     const float keep = 1.f - a.lr * pc.decay;
-    for (int base = (threadIdx.x >> 5) * kGroup; base < pc.n; base += kTurn) {
+    const bool master = pc.master != nullptr;
+    turns(pc.n, [&](auto whole, int base) {
+        constexpr bool W = decltype(whole)::value;
         float m[2][4], v[2][4], w[2][4], g[2][4];
-        [[maybe_unused]] uint32_t fm[2], fv[2], em, ev;
+        [[maybe_unused]] uint32_t fm[2], fv[2], em = 0, ev = 0;
+        const bool group = W || base < pc.n;                   // (at the end of a piece half a wavefront may have none)
         if constexpr (BITS == 8) {
-            em = global<uint8_t>((const void*)pc.m_exp)[base / kGroup];
-            ev = global<uint8_t>((const void*)pc.v_exp)[base / kGroup];
+            if (group) {
+                em = global<uint8_t>((const void*)pc.m_exp)[base / kGroup];
+                ev = global<uint8_t>((const void*)pc.v_exp)[base / kGroup];
+            }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int at = base + h * 128 + lane * 4, there = pc.n - at;
-            load4<G>(pc.g, at, there, g[h]);
-            if (pc.master) load4<float>(pc.master, at, there, w[h]);
-            else load4<P>(pc.p, at, there, w[h]);
+            const int at = base + h * 128 + lane * 4;
+            load4<W, G>(pc.g, at, pc.n, g[h]);
+            if (master) load4<W, float>(pc.master, at, pc.n, w[h]);
+            else load4<W, P>(pc.p, at, pc.n, w[h]);
             if constexpr (BITS == 8) {
-                fm[h] = load4(pc.m, at, there);
-                fv[h] = load4(pc.v, at, there);
+                fm[h] = load4<W>(pc.m, at, pc.n);
+                fv[h] = load4<W>(pc.v, at, pc.n);
             } else {
-                load4<float>(pc.m, at, there, m[h]);
-                load4<float>(pc.v, at, there, v[h]);
+                load4<W, float>(pc.m, at, pc.n, m[h]);
+                load4<W, float>(pc.v, at, pc.n, v[h]);
             }
         }
         if constexpr (BITS == 8) {
@@ -301,12 +329,12 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
                 const float root = root_of(v[h][i]) * a.inv_root + a.eps;
                 w[h][i] = w[h][i] * keep - a.step_size * (m[h][i] * __builtin_amdgcn_rcpf(root));
             }
-            const int at = base + h * 128 + lane * 4, there = pc.n - at;
-            if (pc.master) store4<float>(pc.master, at, there, w[h]);
-            store4<P>(pc.p, at, there, w[h]);
+            const int at = base + h * 128 + lane * 4;
+            if (master) store4<W, float>(pc.master, at, pc.n, w[h]);
+            store4<W, P>(pc.p, at, pc.n, w[h]);
             if constexpr (BITS == 32) {
-                store4<float>(pc.m, at, there, m[h]);
-                store4<float>(pc.v, at, there, v[h]);
+                store4<W, float>(pc.m, at, pc.n, m[h]);
+                store4<W, float>(pc.v, at, pc.n, v[h]);
             }
         }
         if constexpr (BITS == 8) {
@@ -316,14 +344,14 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (base + h * 128 + lane * 4 + i < pc.n) {
+                    if (W || base + h * 128 + lane * 4 + i < pc.n) {
                         const uint32_t bm = __float_as_uint(m[h][i]) & 0x7fffffffu, bv = __float_as_uint(v[h][i]) & 0x7fffffffu;
                         mm = mm > bm ? mm : bm;
                         mv = mv > bv ? mv : bv;
                     }
             em = max32(mm) >> 23;
             ev = max32(mv) >> 23;
-            if (lane == 0) {
+            if (lane == 0 && group) {
                 global<uint8_t>(pc.m_exp)[base / kGroup] = (uint8_t)em;
                 global<uint8_t>(pc.v_exp)[base / kGroup] = (uint8_t)ev;
             }
@@ -331,20 +359,21 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
             const Scale<kTopV> sv(ev);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int at = base + h * 128 + lane * 4, there = pc.n - at;
+                const int at = base + h * 128 + lane * 4;
+                const uint32_t index = pc.first_group * kGroup + a.seed + (uint32_t)at;
                 uint32_t cm = 0, cv = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t r = dither_bits(pc.first_group * kGroup + (uint32_t)(at + i), a.seed);
-                    cm |= (sm.code(fabsf(m[h][i]), r << 4 & 0xffff0u) | (__float_as_uint(m[h][i]) >> 31 << 7)) << 8 * i;
-                    const uint32_t c = sv.code(v[h][i], r >> 12 & 0xffff0u);
-                    cv |= (c == 0 && v[h][i] > 0.f ? 1u : c) << 8 * i;
+                    const uint32_t r = dither_bits(index + i), bm = __float_as_uint(m[h][i]), bv = __float_as_uint(v[h][i]);
+                    cm |= (sm.code(fabsf(m[h][i]), r & 0xffffu) | (bm >> 24 & 0x80u)) << 8 * i;
+                    const uint32_t c = sv.code(v[h][i], r >> 16), least = bv < 1u ? bv : 1u;      // a positive v is not held as 0
+                    cv |= (c > least ? c : least) << 8 * i;
                 }
-                store4(pc.m, at, there, em == 255u ? 0u : cm);
-                store4(pc.v, at, there, ev == 255u ? 0u : cv);
+                store4<W>(pc.m, at, pc.n, em == 255u ? 0u : cm);
+                store4<W>(pc.v, at, pc.n, ev == 255u ? 0u : cv);
             }
         }
-    }
+    });
 }
 
 template <typename P, typename G>
@@ -360,7 +389,7 @@ ff_status adamw_step_run(const ff_adamw_desc& d, const void* plan, size_t plan_b
     if (n == 0) return FF_OK;
     const double c1 = 1. - pow(h.beta1, (double)h.step), c2 = 1. - pow(h.beta2, (double)h.step);
     StepArgs a{(float)h.lr, (float)(h.lr / c1), (float)h.beta1, (float)(1. - h.beta1), (float)h.beta2, (float)(1. - h.beta2),
-               (float)(1. / sqrt(c2)), (float)h.eps, norm ? (float)h.max_norm : 0.f, h.seed};
+               (float)(1. / sqrt(c2)), (float)h.eps, norm ? (float)h.max_norm : 0.f, h.seed * kDitherSeed};
     const uint32_t tag = tag_of(d);
     Timed t(KK_ADAMW, stream);
     if (d.param_dtype == FF_F32) {
@@ -379,28 +408,39 @@ __global__ __launch_bounds__(256) void k_moments(const Piece* __restrict__ piece
     const Piece& pc = pieces[blockIdx.x];
     if (pc.tag != tag) return;
     const int lane = threadIdx.x & 31;
-    for (int base = (threadIdx.x >> 5) * kGroup; base < pc.n; base += kTurn) {
+    turns(pc.n, [&](auto whole, int base) {
+        constexpr bool W = decltype(whole)::value;
+        float m[2][4], v[2][4];
+        if constexpr (BITS == 8) {
+            const bool group = W || base < pc.n;
+            const Scale<kTopM> sm(group ? global<uint8_t>((const void*)pc.m_exp)[base / kGroup] : 0u);
+            const Scale<kTopV> sv(group ? global<uint8_t>((const void*)pc.v_exp)[base / kGroup] : 0u);
+            uint32_t fm[2], fv[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int at = base + h * 128 + lane * 4, there = pc.n - at;
-            float m[4], v[4];
-            if constexpr (BITS == 8) {
-                const Scale<kTopM> sm(global<uint8_t>((const void*)pc.m_exp)[base / kGroup]);
-                const Scale<kTopV> sv(global<uint8_t>((const void*)pc.v_exp)[base / kGroup]);
-                const uint32_t fm = load4(pc.m, at, there), fv = load4(pc.v, at, there);
+            for (int h = 0; h < 2; ++h) {
+                fm[h] = load4<W>(pc.m, base + h * 128 + lane * 4, pc.n);
+                fv[h] = load4<W>(pc.v, base + h * 128 + lane * 4, pc.n);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    m[i] = sm.value(fm, i);
-                    v[i] = sv.value(fv, i);
+                    m[h][i] = sm.value(fm[h], i);
+                    v[h][i] = sv.value(fv[h], i);
                 }
-            } else {
-                load4<float>(pc.m, at, there, m);
-                load4<float>(pc.v, at, there, v);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                load4<W, float>(pc.m, base + h * 128 + lane * 4, pc.n, m[h]);
+                load4<W, float>(pc.v, base + h * 128 + lane * 4, pc.n, v[h]);
             }
-            if (m_out) store4<float>(m_out + pc.first_value, at, there, m);
-            if (v_out) store4<float>(v_out + pc.first_value, at, there, v);
         }
-    }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (m_out) store4<W, float>(m_out + pc.first_value, base + h * 128 + lane * 4, pc.n, m[h]);
+            if (v_out) store4<W, float>(v_out + pc.first_value, base + h * 128 + lane * 4, pc.n, v[h]);
+        }
+    });
 }
 
 ff_status adamw_moments_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, float* m_out, float* v_out, hipStream_t stream) {
