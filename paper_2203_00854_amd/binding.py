@@ -388,49 +388,56 @@ def ff_gated_attention_residual(desc: AttnDesc, w: Dict[str, "object"], x, z=Non
 
 
 # ------------------------------------------------------------------------- training: layer norm, clipping, AdamW
-def _want(t, name, dtype=None, shape=None, numel=None, device=None):
-    """The tensor, if a kernel may take it as `name`; otherwise TypeError or ValueError."""
-    if dtype is not None and t.dtype != dtype:
+def _refuse(t, name, dtype, shape, device):
+    if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
-    if not t.is_cuda or (device is not None and t.device != device):
-        raise ValueError(f"{name} is on {t.device}" + (f", not on {device}" if device is not None else ", not on a GPU"))
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device if device.type == 'cuda' else 'a GPU'}")
     if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if numel is not None and t.numel() != numel:
-        raise ValueError(f"{name} has {t.numel()} values, not {numel}")
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+
+
+def _fit(t, name, dtype, shape, device):
+    """The tensor, if a kernel may take it as `name`; otherwise TypeError or ValueError."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not (t.is_cuda and t.is_contiguous()):
+        _refuse(t, name, dtype, shape, device)
     return t
+
+
+def _stream_of(device) -> int:
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (a stream object costs as much as a launch)
+    return torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device.index)
 
 
 def _norm_desc(x, gamma, eps):
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"no channels in shape {tuple(x.shape)}")
-    c = x.shape[-1]
-    desc = NormDesc(_dtype_code(x), c, x.numel() // c, eps)
-    _want(x, "x")
-    _want(gamma, "gamma", x.dtype, (c,), device=x.device)
-    return desc
+    c, dtype, device = x.shape[-1], x.dtype, x.device
+    _fit(x, "x", dtype, x.shape, device)
+    _fit(gamma, "gamma", dtype, (c,), device)
+    return NormDesc(_dtype_code(x), c, x.numel() // c, eps), dtype, device
 
 
 def ff_layernorm_forward(x, gamma, beta, residual=None, eps: float = 1e-5, stats: bool = True, out=None, sum_out=None):
     """Layer norm over the last axis of x, or of x + residual; returns (y, sum, mean, rstd).  sum (the rounded x + residual,
     None without one) is what ff_layernorm_backward takes as s; sum_out may be x or residual itself.  stats=False keeps no mean and rstd."""
     import torch
-    desc = _norm_desc(x, gamma, eps)
-    _want(beta, "beta", x.dtype, gamma.shape, device=x.device)
-    out = torch.empty_like(x) if out is None else _want(out, "out", x.dtype, x.shape, device=x.device)
-    if residual is None:
-        if sum_out is not None:
-            raise ValueError("sum_out needs a residual")
-    else:
-        _want(residual, "residual", x.dtype, x.shape, device=x.device)
-        sum_out = torch.empty_like(x) if sum_out is None else _want(sum_out, "sum_out", x.dtype, x.shape, device=x.device)
+    desc, dtype, device = _norm_desc(x, gamma, eps)
+    shape = x.shape
+    _fit(beta, "beta", dtype, gamma.shape, device)
+    out = torch.empty_like(x) if out is None else _fit(out, "out", dtype, shape, device)
+    if residual is not None:
+        _fit(residual, "residual", dtype, shape, device)
+        sum_out = torch.empty_like(x) if sum_out is None else _fit(sum_out, "sum_out", dtype, shape, device)
+    elif sum_out is not None:
+        raise ValueError("sum_out needs a residual")
     mean = rstd = None
     if stats:
-        mean, rstd = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device).unbind(0)
-    _check(lib().ff_layernorm_forward(C.byref(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(sum_out), _ptr(out), _ptr(mean),
-                                      _ptr(rstd), _stream()))
+        mean, rstd = (torch.empty(shape[:-1], dtype=torch.float32, device=device) for _ in range(2))
+    _check(lib().ff_layernorm_forward(C.byref(desc), x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), _ptr(sum_out), out.data_ptr(),
+                                      _ptr(mean), _ptr(rstd), _stream_of(device)))
     return out, sum_out, mean, rstd
 
 
@@ -440,24 +447,25 @@ def ff_layernorm_backward(s, gamma, dy, mean=None, rstd=None, dsum=None, eps: fl
     sum).  Without mean and rstd they are formed again from s.  dsum: the gradient that reaches s by other ways, added to dx.
     dx may be dy or dsum itself; accumulate adds to the given dgamma and dbeta."""
     import torch
-    desc = _norm_desc(s, gamma, eps)
-    _want(dy, "dy", s.dtype, s.shape, device=s.device)
+    desc, dtype, device = _norm_desc(s, gamma, eps)
+    shape = s.shape
+    _fit(dy, "dy", dtype, shape, device)
     if dsum is not None:
-        _want(dsum, "dsum", s.dtype, s.shape, device=s.device)
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        if t is not None:
-            _want(t, name, torch.float32, numel=desc.rows, device=s.device)
+        _fit(dsum, "dsum", dtype, shape, device)
+    if mean is not None:
+        _fit(mean, "mean", torch.float32, shape[:-1], device)
+    if rstd is not None:
+        _fit(rstd, "rstd", torch.float32, shape[:-1], device)
     if accumulate and (dgamma is None or dbeta is None):
         raise ValueError("accumulate needs dgamma and dbeta")
-    dx = torch.empty_like(s) if dx is None else _want(dx, "dx", s.dtype, s.shape, device=s.device)
-    if dgamma is None and dbeta is None:
-        dgamma, dbeta = torch.empty(2, desc.c, dtype=torch.float32, device=s.device).unbind(0)
-    dgamma = torch.empty(desc.c, dtype=torch.float32, device=s.device) if dgamma is None else _want(dgamma, "dgamma", torch.float32, gamma.shape, device=s.device)
-    dbeta = torch.empty(desc.c, dtype=torch.float32, device=s.device) if dbeta is None else _want(dbeta, "dbeta", torch.float32, gamma.shape, device=s.device)
+    dx = torch.empty_like(s) if dx is None else _fit(dx, "dx", dtype, shape, device)
+    sums = gamma.shape
+    dgamma = torch.empty(sums, dtype=torch.float32, device=device) if dgamma is None else _fit(dgamma, "dgamma", torch.float32, sums, device)
+    dbeta = torch.empty(sums, dtype=torch.float32, device=device) if dbeta is None else _fit(dbeta, "dbeta", torch.float32, sums, device)
     if ws is None:
-        ws = _alloc_ws(ff_layernorm_backward_workspace_bytes(desc), s.device)
-    _check(lib().ff_layernorm_backward(C.byref(desc), _ptr(s), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dgamma),
-                                       _ptr(dbeta), 1 if accumulate else 0, _ptr(ws), ws.numel(), _stream()))
+        ws = _alloc_ws(ff_layernorm_backward_workspace_bytes(desc), device)
+    _check(lib().ff_layernorm_backward(C.byref(desc), s.data_ptr(), gamma.data_ptr(), _ptr(mean), _ptr(rstd), dy.data_ptr(), _ptr(dsum), dx.data_ptr(),
+                                       dgamma.data_ptr(), dbeta.data_ptr(), 1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream_of(device)))
     return dx, dgamma, dbeta
 
 
@@ -483,37 +491,51 @@ class AdamWPlan:
         _check(lib().ff_adamw_plan(C.byref(desc), table, host.ctypes.data, n))
         self.plan = torch.from_numpy(host).to(device)
         self.norm_ws = _alloc_ws(lib().ff_grad_norm_workspace_bytes(), device)
+        self.address, self.bytes = self.plan.data_ptr(), n
+
+    @property
+    def ref(self):
+        return C.byref(self.desc)
 
 
 def _make_plan(state_bits, columns, weight_decay):
-    """columns: {pointer name: list of tensors or None}."""
+    """columns: {pointer name: (list of tensors, their dtype) or None}."""
     import numpy as np
-    grads = columns["g"]
+    import torch
+    grads = columns["g"][0]
     count = len(grads)
     if count == 0:
         raise ValueError("a plan needs a tensor")
     device = grads[0].device
-    numels = [t.numel() for t in grads]
-    row = np.dtype(AdamWTensor)
-    table = np.zeros(count, row)
-    for name, ts in columns.items():
-        if ts is None:
-            continue
+    numels = list(map(torch.Tensor.numel, grads))
+    table = np.zeros(count, np.dtype(AdamWTensor))
+    columns = {name: column for name, column in columns.items() if column is not None}
+    for name, (ts, dtype) in columns.items():
+        other = {t.dtype for t in ts} - {dtype}
+        if other:
+            raise TypeError(f"{name} is {other.pop()}, not {dtype}")
+    for name, (ts, dtype) in columns.items():
         if len(ts) != count:
             raise ValueError(f"{len(ts)} tensors of {name} for {count} gradients")
-        for t, n in zip(ts, numels):
-            _want(t, name, ts[0].dtype, numel=-(-n // 256) if name.endswith("_exp") else n, device=device)
-        table[name] = [t.data_ptr() for t in ts]
+        want = [-(-n // 256) for n in numels] if name.endswith("_exp") else numels
+        got = list(map(torch.Tensor.numel, ts))
+        # (all at once: a model has thousands of tensors)
+        if {t.device for t in ts} != {device} or device.type != "cuda" or not all(map(torch.Tensor.is_contiguous, ts)) or got != want:
+            for t, n, w in zip(ts, got, want):
+                if n != w:
+                    raise ValueError(f"{name} has {n} values, not {w}")
+                _fit(t, name, dtype, t.shape, device)
+        table[name] = list(map(torch.Tensor.data_ptr, ts))
     table["numel"] = numels
     table["weight_decay"] = weight_decay
-    p = columns.get("p")
-    desc = AdamWDesc(FF_F32 if p is None else _dtype_code(p[0]), _dtype_code(grads[0]), state_bits, count)
+    desc = AdamWDesc(_dtype_code(columns["p"][0][0]) if "p" in columns else FF_F32, _dtype_code(grads[0]), state_bits, count)
     return AdamWPlan(desc, table.ctypes.data, (table, columns), sum(numels), device)
 
 
 def make_grad_plan(grads) -> AdamWPlan:
     """A plan of gradients alone, for ff_grad_norm."""
-    return _make_plan(0, {"g": list(grads)}, 0.0)
+    grads = list(grads)
+    return _make_plan(0, {"g": (grads, grads[0].dtype if grads else None)}, 0.0)
 
 
 def make_adamw_plan(params, grads, m, v, master=None, m_exp=None, v_exp=None, weight_decay=0.0) -> AdamWPlan:
@@ -521,18 +543,16 @@ def make_adamw_plan(params, grads, m, v, master=None, m_exp=None, v_exp=None, we
     values of a tensor; adamw_states allocates either).  master: float32 copies of bfloat16 parameters.  weight_decay: a number, or
     one for each tensor."""
     import torch
-    columns = {"p": list(params), "g": list(grads), "m": list(m), "v": list(v), "master": None if master is None else list(master),
-               "m_exp": None if m_exp is None else list(m_exp), "v_exp": None if v_exp is None else list(v_exp)}
-    if (columns["m_exp"] is None) != (columns["v_exp"] is None):
+    params, grads = list(params), list(grads)
+    if not params or not grads:
+        raise ValueError("a plan needs a tensor")
+    if (m_exp is None) != (v_exp is None):
         raise ValueError("m_exp and v_exp are given together")
-    bits = 32 if columns["m_exp"] is None else 8
-    kinds = {"m": torch.uint8 if bits == 8 else torch.float32, "master": torch.float32, "m_exp": torch.uint8}
-    kinds["v"], kinds["v_exp"] = kinds["m"], kinds["m_exp"]
-    for name, dtype in kinds.items():
-        for t in columns[name] or ():
-            if t.dtype != dtype:
-                raise TypeError(f"{name} is {t.dtype}, not {dtype}")
-    return _make_plan(bits, columns, weight_decay)
+    bits = 32 if m_exp is None else 8
+    state = torch.uint8 if bits == 8 else torch.float32
+    column = lambda ts, dtype: None if ts is None else (list(ts), dtype)  # noqa: E731
+    return _make_plan(bits, {"p": (params, params[0].dtype), "g": (grads, grads[0].dtype), "m": column(m, state), "v": column(v, state),
+                             "master": column(master, torch.float32), "m_exp": column(m_exp, torch.uint8), "v_exp": column(v_exp, torch.uint8)}, weight_decay)
 
 
 def adamw_states(params, bits: int = 32):
@@ -551,9 +571,10 @@ def adamw_states(params, bits: int = 32):
 def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
     """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another."""
     import torch
-    out = torch.empty(1, dtype=torch.float32, device=plan.device) if out is None else _want(out, "out", torch.float32, numel=1, device=plan.device)
+    device = plan.device
+    out = torch.empty(1, dtype=torch.float32, device=device) if out is None else _fit(out, "out", torch.float32, (1,), device)
     ws = plan.norm_ws if ws is None else ws
-    _check(lib().ff_grad_norm(C.byref(plan.desc), _ptr(plan.plan), plan.plan.numel(), _ptr(out), _ptr(ws), ws.numel(), _stream()))
+    _check(lib().ff_grad_norm(plan.ref, plan.address, plan.bytes, out.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(device)))
     return out
 
 
@@ -564,17 +585,18 @@ def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps
     if (norm is None) != (max_norm is None):
         raise ValueError("norm and max_norm are given together")
     if norm is not None:
-        _want(norm, "norm", torch.float32, numel=1, device=plan.device)
+        _fit(norm, "norm", torch.float32, (1,), plan.device)
     hyper = AdamWHyper(lr, betas[0], betas[1], eps, 0.0 if max_norm is None else max_norm, step, seed & 0xFFFFFFFF)
-    _check(lib().ff_adamw_step(C.byref(plan.desc), _ptr(plan.plan), plan.plan.numel(), C.byref(hyper), _ptr(norm), _stream()))
+    _check(lib().ff_adamw_step(plan.ref, plan.address, plan.bytes, C.byref(hyper), _ptr(norm), _stream_of(plan.device)))
 
 
 def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
     """(m, v) of all tensors of the plan, one after another, as float32."""
     import torch
-    m = torch.empty(plan.values, dtype=torch.float32, device=plan.device) if m is None else _want(m, "m", torch.float32, numel=plan.values, device=plan.device)
-    v = torch.empty(plan.values, dtype=torch.float32, device=plan.device) if v is None else _want(v, "v", torch.float32, numel=plan.values, device=plan.device)
-    _check(lib().ff_adamw_moments(C.byref(plan.desc), _ptr(plan.plan), plan.plan.numel(), _ptr(m), _ptr(v), _stream()))
+    device, shape = plan.device, (plan.values,)
+    m = torch.empty(shape, dtype=torch.float32, device=device) if m is None else _fit(m, "m", torch.float32, shape, device)
+    v = torch.empty(shape, dtype=torch.float32, device=device) if v is None else _fit(v, "v", torch.float32, shape, device)
+    _check(lib().ff_adamw_moments(plan.ref, plan.address, plan.bytes, m.data_ptr(), v.data_ptr(), _stream_of(device)))
     return m, v
 
 
