@@ -294,7 +294,7 @@ typedef struct {
  *   sum          [rows, c] receives s; given exactly when residual is; may be x itself or residual itself
  *   y            [rows, c]; must not overlap x, residual or sum
  *   mean, rstd   float32 [rows], both or neither
- * Partial overlaps are refused.  FF_EINVAL for bad sizes or NULL pointers, FF_EHIP if the launch fails. */
+ * Other overlaps of outputs are refused.  FF_EINVAL for bad sizes or NULL pointers, FF_EHIP if the launch fails. */
 ff_status ff_layernorm_forward(const ff_norm_desc* desc, const void* x, const void* residual, const void* gamma,
                                const void* beta, void* sum, void* y, float* mean, float* rstd, void* hip_stream);
 
@@ -319,7 +319,7 @@ ff_status ff_layernorm_backward(const ff_norm_desc* desc, const void* s, const v
  * given, k = min(1, max_norm / (norm + 1e-6)):
  *   g' = k g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in float32, each operation rounded by itself.  w is the float32 parameter; or the float32 master copy of a
+ * in float32, each operation of m and v rounded by itself (in w a v below 2^-126 counts as 2^-126).  w is the float32 parameter; or the float32 master copy of a
  * bfloat16 parameter, which receives its rounding; or the bfloat16 parameter itself.
  *
  * state_bits = 32: m and v are float32.  state_bits = 8: a byte for each, and for each 256 values of a tensor (from
@@ -357,7 +357,8 @@ typedef struct {
     uint32_t seed;                    /* of the rounding of 8-bit states: another one for each step */
 } ff_adamw_hyper;
 
-/* Bytes of the plan for these tensors (host array of desc->n_tensors entries); 0 if an argument is invalid. */
+/* Bytes of the plan for these tensors (host array of desc->n_tensors entries); 0 if an argument is invalid, or if the
+ * tensors come to 2^24 pieces or more (FF_EUNSUPPORTED in ff_adamw_plan): one for each 4096 values of a tensor, at least one. */
 size_t ff_adamw_plan_bytes(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors);
 
 /* Writes the plan into host memory (plan_bytes as reported above).  Tensors of one plan must not overlap. */

@@ -52,7 +52,7 @@ size_t adamw_plan_size(const ff_adamw_desc& d, const ff_adamw_tensor* ts) {
     return sizeof(PlanHead) + pieces * sizeof(Piece);
 }
 bool adamw_plan_whole(size_t bytes) {
-    return bytes >= sizeof(PlanHead) && bytes % sizeof(Piece) == 0 && bytes / sizeof(Piece) - 1 <= 0x7fffffffu;
+    return bytes >= sizeof(PlanHead) && bytes % sizeof(Piece) == 0 && bytes / sizeof(Piece) - 1 < (1u << 24);     // 2^32 threads in blocks of 256
 }
 static int pieces_of(size_t bytes) { return (int)(bytes / sizeof(Piece) - 1); }
 

@@ -4,6 +4,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -402,6 +403,15 @@ ff_status ff_layernorm_forward(const ff_norm_desc* desc, const void* x, const vo
         return fail(FF_EINVAL, "y must not overlap x, residual or sum");
     if (sum && ((sum != x && overlaps(sum, n, x, n)) || (sum != residual && overlaps(sum, n, residual, n))))
         return fail(FF_EINVAL, "sum must be x itself, residual itself, or overlap neither");
+    const size_t cb = desc->c * esz, rb = (size_t)desc->rows * 4;
+    for (const void* w : {gamma, beta})
+        if (overlaps(y, n, w, cb) || (sum && overlaps(sum, n, w, cb)) || (mean && (overlaps(mean, rb, w, cb) || overlaps(rstd, rb, w, cb))))
+            return fail(FF_EINVAL, "an output overlaps gamma or beta");
+    if (mean) {
+        if (overlaps(mean, rb, rstd, rb)) return fail(FF_EINVAL, "mean and rstd overlap");
+        for (const void* t : {x, residual, (const void*)sum, (const void*)y})
+            if (t && (overlaps(mean, rb, t, n) || overlaps(rstd, rb, t, n))) return fail(FF_EINVAL, "mean or rstd overlaps a tensor");
+    }
     return layernorm_forward_run(*desc, x, residual, gamma, beta, sum, y, mean, rstd, (hipStream_t)hip_stream);
 }
 
@@ -430,6 +440,17 @@ ff_status ff_layernorm_backward(const ff_norm_desc* desc, const void* s, const v
         return fail(FF_EINVAL, "dx must be dy itself, dsum itself, or overlap neither");
     const size_t need = layernorm_backward_workspace(*desc), cb = (size_t)desc->c * 4;
     if (overlaps(dgamma, cb, dbeta, cb)) return fail(FF_EINVAL, "dgamma and dbeta overlap");
+    const size_t wb = desc->c * esz, rb = (size_t)desc->rows * 4;
+    for (const void* o : {(const void*)dgamma, (const void*)dbeta}) {
+        for (const void* t : {s, dy, dsum, (const void*)dx})
+            if (t && overlaps(o, cb, t, n)) return fail(FF_EINVAL, "dgamma or dbeta overlaps a tensor");
+        if (overlaps(o, cb, gamma, wb) || (mean && (overlaps(o, cb, mean, rb) || overlaps(o, cb, rstd, rb))) || (ws && overlaps(o, cb, ws, need)))
+            return fail(FF_EINVAL, "dgamma or dbeta overlaps an input or the workspace");
+    }
+    if (overlaps(dx, n, gamma, wb) || (mean && (overlaps(dx, n, mean, rb) || overlaps(dx, n, rstd, rb))))
+        return fail(FF_EINVAL, "dx overlaps gamma, mean or rstd");
+    for (const void* t : {s, dy, dsum, (const void*)dx})
+        if (t && ws && overlaps(ws, need, t, n)) return fail(FF_EINVAL, "the workspace overlaps a tensor");
     if (!ws) return fail(FF_EINVAL, "workspace is NULL (%zu bytes needed)", need);
     if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
     if (ws_bytes < need) return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);
@@ -481,13 +502,19 @@ static ff_status check_plan(const ff_adamw_desc* d, const void* plan, size_t byt
 
 size_t ff_adamw_plan_bytes(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors) {
     if (check_tensors(desc, tensors) != FF_OK) return 0;
-    return adamw_plan_size(*desc, tensors);
+    const size_t bytes = adamw_plan_size(*desc, tensors);
+    if (!adamw_plan_whole(bytes)) {
+        fail(FF_EUNSUPPORTED, "the tensors need more pieces than one launch has blocks");
+        return 0;
+    }
+    return bytes;
 }
 
 ff_status ff_adamw_plan(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors, void* plan, size_t plan_bytes) {
     ff_status st = check_tensors(desc, tensors);
     if (st != FF_OK) return st;
     const size_t need = adamw_plan_size(*desc, tensors);
+    if (!adamw_plan_whole(need)) return fail(FF_EUNSUPPORTED, "the tensors need more pieces than one launch has blocks");
     if (!plan || !aligned_to(plan, 8)) return fail(FF_EINVAL, "plan is NULL or misaligned");
     if (plan_bytes != need) return fail(FF_EWORKSPACE, "the plan has %zu bytes, %zu given", need, plan_bytes);
     adamw_plan_fill(*desc, tensors, plan);

@@ -180,3 +180,26 @@ def test_binding_refuses_tensors_that_a_kernel_must_not_see():
         P.make_adamw_plan([x], [x], [x], [x], m_exp=[x])
     with pytest.raises(ValueError):
         P.adamw_states([x], 16)
+
+
+def test_layernorm_overlaps():
+    d, lib = norm_desc(), P.lib()
+    fwd = lambda x=X, res=None, g=G, b=BETA, s=None, y=Y, m=MEAN, r=RSTD: lib.ff_layernorm_forward(C.byref(d), x, res, g, b, s, y, m, r, None)  # noqa: E731
+    for kw in (dict(y=G), dict(y=BETA - 64), dict(y=MEAN), dict(m=RSTD + 4), dict(m=X + 8), dict(r=Y), dict(m=G), dict(r=BETA), dict(res=R, s=S, m=S), dict(res=R, s=G)):
+        assert fwd(**kw) == B.FF_EINVAL, kw
+        assert "overlap" in P.last_error()
+    need = P.ff_layernorm_backward_workspace_bytes(d)
+    bwd = lambda s=X, g=G, m=MEAN, r=RSTD, dy=Y, ds=None, dx=S, dg=R, db=BETA, ws=WS: lib.ff_layernorm_backward(C.byref(d), s, g, m, r, dy, ds, dx, dg, db, 0, ws, need, None)  # noqa: E731
+    for kw in (dict(dg=X), dict(db=Y + 4), dict(dg=S), dict(dg=G), dict(db=MEAN), dict(dg=WS), dict(dx=G), dict(dx=MEAN), dict(ws=X), dict(ws=S), dict(ds=S + 2), dict(ds=WS)):
+        assert bwd(**kw) == B.FF_EINVAL, kw
+        assert "overlap" in P.last_error() or "itself" in P.last_error()
+
+
+def test_more_pieces_than_blocks_are_refused():
+    d = B.AdamWDesc(P.FF_F32, P.FF_F32, 0, 1)
+    t = tensors({"g": 0x10000, "numel": 4096 * ((1 << 24) - 1)})
+    n = plan_bytes(d, t)
+    assert n > 0
+    t["numel"] += 1
+    assert plan_bytes(d, t) == 0 and "pieces" in P.last_error()
+    assert P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, 0x1000, n + 80) == B.FF_EUNSUPPORTED
