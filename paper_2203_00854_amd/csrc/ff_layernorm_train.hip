@@ -1,8 +1,8 @@
 // Layer norm in training: forward pass with residual sum and statistics, backward pass with the gradients of gamma and beta.
 //
 // Both passes are bound by HBM (a dozen to two dozen vector instructions per value, where 45 lane-instructions fit into the time that six bytes
-// take), so a row is read once, stays in registers, and is written once.  A team of 8 to 64 lanes of one wavefront holds a row, each
-// lane up to four pieces of 16 bytes; rows of more than 256 pieces are held by a whole block.  Rows that are no whole number of pieces, and tensors at any
+// take), so a row is read once, stays in registers, and is written once.  A team of 1 to 64 lanes of one wavefront holds a row, each
+// lane up to sixteen values in pieces of 16 bytes; rows of more than 1024 channels are held by a whole block.  Rows that are no whole number of pieces, and tensors at any
 // offset, take the same path: pieces are loaded at the alignment of their type, and a piece that
 // would pass the row's end is moved back to end with it - its first values, which the piece before holds too, count in no sum.
 #include <type_traits>
@@ -43,44 +43,31 @@ __device__ __forceinline__ float swap16_sum(float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-// over the lane's team of 8, 16, 32 or 64 lanes
-__device__ __forceinline__ float team_sum(float v, int lanes) {
-    v = sum8(v);
-    if (lanes > 8) v += dpp<kDppRor8>(v);
-    if (lanes > 16) v = swap16_sum(v);
-    if (lanes > 32) v = half_sum(v);
-    return v;
-}
-__device__ __forceinline__ void team_sum(float& v, float& w, int lanes) {
-    v = sum8(v);
-    w = sum8(w);
-    if (lanes > 8) {
-        v += dpp<kDppRor8>(v);
-        w += dpp<kDppRor8>(w);
-    }
-    if (lanes > 16) {
-        v = swap16_sum(v);
-        w = swap16_sum(w);
-    }
-    if (lanes > 32) {
-        v = half_sum(v);
-        w = half_sum(w);
+// over the lane's team of 1, 2, 4, .. 64 lanes, of several values at once
+template <typename... F> __device__ __forceinline__ void team_sum(int lanes, F&... v) {
+    if (lanes > 4) {
+        ((v = sum8(v)), ...);
+        if (lanes > 8) ((v += dpp<kDppRor8>(v)), ...);
+        if (lanes > 16) ((v = swap16_sum(v)), ...);
+        if (lanes > 32) ((v = half_sum(v)), ...);
+    } else {
+        if (lanes > 1) ((v += dpp<kDppXor1>(v)), ...);
+        if (lanes > 2) ((v += dpp<kDppXor2>(v)), ...);
     }
 }
-// over the lanes at the same place of the wavefront's teams
+// over the lanes at the same place of the wavefront's teams (rotations of sixteen lanes: together they visit all of a row's teams)
 template <int N> __device__ __forceinline__ void across_teams(float (&v)[N], int lanes) {
-    if (lanes <= 8) {
+    constexpr int kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;
+    auto each = [&](auto f) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += dpp<kDppRor8>(v[i]);
-    }
-    if (lanes <= 16) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = swap16_sum(v[i]);
-    }
-    if (lanes <= 32) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = half_sum(v[i]);
-    }
+        for (int i = 0; i < N; ++i) v[i] = f(v[i]);
+    };
+    if (lanes <= 8) each([](float x) { return x + dpp<kDppRor8>(x); });
+    if (lanes <= 4) each([](float x) { return x + dpp<kRor4>(x); });
+    if (lanes <= 2) each([](float x) { return x + dpp<kRor2>(x); });
+    if (lanes <= 1) each([](float x) { return x + dpp<kRor1>(x); });
+    if (lanes <= 16) each([](float x) { return swap16_sum(x); });
+    if (lanes <= 32) each([](float x) { return half_sum(x); });
 }
 
 constexpr int kForwardThreads = 256, kWideThreads = 512;
@@ -90,21 +77,27 @@ constexpr int backward_threads(int values) { return values <= 8 ? 1024 : 512; }
 // Who works on a row: lanes of a wavefront, or (WIDE) a whole block, whose sums pass through LDS.
 template <bool WIDE> struct Team {
     int lanes, place;              // members, own number among them
-    float* part;                   // WIDE: two words for each wavefront, twice (sums of two successive calls do not meet)
+    float* part;                   // WIDE: two words for each of kWideThreads / 64 wavefronts, twice (sums of two successive calls do not meet)
     int turn = 0;
+    __device__ __forceinline__ Team(int lanes_, float* part_) : lanes(lanes_), place(WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes_ - 1)), part(part_) {
+        if constexpr (WIDE) {
+            if (threadIdx.x < 4 * kWideThreads / 64) part[threadIdx.x] = 0.f;
+            __syncthreads();
+        }
+    }
     __device__ __forceinline__ float sum(float v) {
-        if constexpr (!WIDE) {
-            return team_sum(v, lanes);
-        } else {
+        if constexpr (WIDE) {
             float none = 0.f;
             sum(v, none);
-            return v;
+        } else {
+            team_sum(lanes, v);
         }
+        return v;
     }
     // of two at once
     __device__ __forceinline__ void sum(float& v, float& w) {
         if constexpr (!WIDE) {
-            team_sum(v, w, lanes);
+            team_sum(lanes, v, w);
         } else {
             constexpr int W = kWideThreads / 64;
             float* p = part + turn;
@@ -116,11 +109,11 @@ template <bool WIDE> struct Team {
                 p[W + (threadIdx.x >> 6)] = w;
             }
             __syncthreads();
-            v = (p[0] + p[1]) + (p[2] + p[3]);
-            w = (p[W] + p[W + 1]) + (p[W + 2] + p[W + 3]);
-            if (lanes > 256) {
-                v += (p[4] + p[5]) + (p[6] + p[7]);
-                w += (p[W + 4] + p[W + 5]) + (p[W + 6] + p[W + 7]);
+            v = w = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {              // (the words of wavefronts that a smaller block lacks are zero)
+                v += p[i];
+                w += p[W + i];
             }
         }
     }
@@ -150,7 +143,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
     float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int c, int lanes, int turns, float eps) {
     __shared__ float part[WIDE ? 4 * kWideThreads / 64 : 1];
     typedef Pack<T, V> Pc;
-    Team<WIDE> team{lanes, WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), part};
+    Team<WIDE> team(lanes, part);
     const Held<V, ITERS, MASKED> held(team.place, team.lanes, c);
     Pc gm[ITERS], bt[ITERS];
 #pragma unroll
@@ -219,6 +212,9 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
     }
 }
 
+// Bytes bound it: 2048 x 2048 x 128 bfloat16 in 577 us (5.6 TB/s), 612 where the statistics are formed again (four sums over a team one after
+// the other, not two); 5120 x 384 x 64 in 141 (5.4 TB/s).  Sixteen wavefronts on a compute unit carry that: twice as many,
+// in registers or blocks, took longer (662), and each block more makes the second launch longer.
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
 // over its teams and wavefronts in a fixed order and leaves 2 c partial sums; with one block in all these are the result.
 template <typename T, int V, int ITERS, bool MASKED, bool WIDE>
@@ -229,7 +225,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
     constexpr int THREADS = backward_threads(V * ITERS);
     extern __shared__ float joined[];                  // every wavefront's sums of dgamma and dbeta; WIDE: what Team needs
     typedef Pack<T, V> Pc;
-    Team<WIDE> team{lanes, WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), joined};
+    Team<WIDE> team(lanes, joined);
     const Held<V, ITERS, MASKED> held(team.place, team.lanes, c);
     float dg[ITERS][V] = {}, db[ITERS][V] = {};
     Pc gm[ITERS];
@@ -381,30 +377,35 @@ __global__ __launch_bounds__(1024) void k_ln_join(const float* __restrict__ part
 // ---- which kernel takes a shape ------------------------------------------------------------
 // Pieces are 16 bytes (one value where the row is shorter).  A lane holds at most sixteen values: with the sums of dgamma and dbeta beside them
 // more would leave two wavefronts per SIMD, or spill.  Of the ways to cover a row by lanes times pieces the one with the
-// fewest idle places is taken, of equals the one with the most lanes; rows of more than 64 such lanes are a block's, of 256 threads or, beyond 256 pieces, of 512.
+// fewest idle places is taken, of equals the one with the fewest pieces a lane; short rows have teams of fewer than eight lanes with a
+// piece each (2 M rows of 32 bfloat16 backward, eight lanes: 105 us, four: 77).  Rows of more than 64 such lanes are a block's,
+// of as many wavefronts as they need (50000 x 1100 bfloat16 backward, 256 threads: 123 us, 192: 76).
 struct Shape {
     int v, iters, lanes;
     bool masked, wide;
 };
 static Shape shape_of(int dtype, int c) {
-    Shape s{dtype == FF_F32 ? 4 : 8, 1, 8, false, false};
+    Shape s{dtype == FF_F32 ? 4 : 8, 1, 1, false, false};
     if (c < s.v) s.v = 1;
-    const int pieces = (c + s.v - 1) / s.v;
-    const int most = s.v == 8 ? 2 : 4;
-    if (pieces > 64 * most) {
-        s.wide = true;
-        s.lanes = pieces > 256 ? kWideThreads : 256;
-        s.iters = (pieces + s.lanes - 1) / s.lanes;
-        s.masked = c != s.lanes * s.iters * s.v;
-        return s;
-    }
+    const int pieces = (c + s.v - 1) / s.v, most = s.v == 8 ? 2 : 4;
+    s.wide = pieces > 64 * most;
     int best = 1 << 30;
-    for (int lanes = 64; lanes >= 8; lanes >>= 1) {
-        const int iters = (pieces + lanes - 1) / lanes;
-        if (iters > most || iters * lanes >= best) continue;
+    auto take = [&](int iters, int lanes) {
+        if (iters * lanes >= best) return;
         best = iters * lanes;
         s.iters = iters;
         s.lanes = lanes;
+    };
+    for (int iters = 1; iters <= most; ++iters) {
+        const int need = (pieces + iters - 1) / iters;
+        if (s.wide) {
+            const int lanes = (need + 63) & ~63;
+            if (lanes <= kWideThreads) take(iters, lanes);
+        } else {
+            int lanes = iters == 1 ? 1 : 8;
+            while (lanes < need) lanes <<= 1;
+            if (lanes <= 64) take(iters, lanes);
+        }
     }
     s.masked = c != s.lanes * s.iters * s.v;
     return s;
@@ -476,12 +477,15 @@ ff_status layernorm_forward_run(const ff_norm_desc& d, const void* x, const void
     return check_launch("ff_layernorm_forward");
 }
 
-// Blocks of the backward pass.  Numbers of its own, not the device's, so that the order of the sums does not depend on the machine.
-constexpr int kBackwardBlocks = 256, kBackwardBlocksWide = 512;
+// Blocks of the backward pass.  Numbers of its own, not the device's, so that the order of the sums does not depend on the machine:
+// about sixteen wavefronts on each of 256 compute units, eight where a lane holds more than eight values, and equally many blocks on
+// each (20000 x 3000 float32 in 512 blocks of 384 threads 139 us, in 682 171).
+constexpr int kBackwardBlocks = 256;
 static int backward_blocks(const ff_norm_desc& d, const Shape& s) {
+    const bool many = s.v * s.iters > 8;
     const int64_t turns = turns_of(d.rows, s.wide ? 1 : backward_threads(s.v * s.iters) / s.lanes);
     if (turns <= 4) return turns > 0;                  // one block: no partial sums, no second launch
-    const int most = s.wide && s.v * s.iters <= 8 ? kBackwardBlocksWide : kBackwardBlocks;
+    const int per_unit = s.wide ? (many ? 512 + s.lanes / 2 : 1024) / s.lanes : 1, most = per_unit * kBackwardBlocks;
     return (int)(turns < most ? turns : most);
 }
 

@@ -134,6 +134,20 @@ def test_many_rows(rows, c, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(70_001, 1), (70_001, 3), (40_000, 8), (30_011, 12), (30_011, 16), (20_000, 24), (20_000, 31)])
+def test_short_rows(rows, c, dtype):
+    """Teams of one to four lanes, in one block and in many."""
+    for n in (rows, 1023):
+        t = make(n, c, dtype, seed=c)
+        d = {k: up(v) for k, v in t.items()}
+        out = P.ff_layernorm_forward(d["x"], d["gamma"], d["beta"], residual=d["residual"], eps=EPS)
+        check_forward(t, dtype, out, True)
+        for saved in (True, False):
+            grads = P.ff_layernorm_backward(out[1], d["gamma"], d["dy"], mean=out[2] if saved else None, rstd=out[3] if saved else None, dsum=d["dsum"], eps=EPS)
+            check_backward(out[1].cpu(), t, dtype, grads, True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("c", [24, 128, 173, 1000, 3000])
 @pytest.mark.parametrize("shift", [1, 3, 4])
 def test_tensors_at_any_offset(c, dtype, shift):
@@ -192,13 +206,14 @@ def test_accumulation_and_no_rows():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_values_that_are_not_finite_stay_in_their_row(dtype):
-    t = make(64, 128, dtype, seed=9)
+@pytest.mark.parametrize("c", [16, 128, 173, 1100])
+def test_values_that_are_not_finite_stay_in_their_row(c, dtype):
+    t = make(64, c, dtype, seed=9)
     d = {k: up(v) for k, v in t.items()}
     clean = P.ff_layernorm_forward(d["x"], d["gamma"], d["beta"], eps=EPS)
     dirty = d["x"].clone()
     dirty[5, 3] = float("nan")
-    dirty[9, 100] = float("inf")
+    dirty[9, c - 1] = float("inf")
     y = P.ff_layernorm_forward(dirty, d["gamma"], d["beta"], eps=EPS)[0]
     dx = P.ff_layernorm_backward(dirty, d["gamma"], d["dy"], eps=EPS)[0]
     want_dx = P.ff_layernorm_backward(d["x"], d["gamma"], d["dy"], eps=EPS)[0]
