@@ -55,12 +55,17 @@ template <typename... F> __device__ __forceinline__ void team_sum(int lanes, F&.
         if (lanes > 2) ((v += dpp<kDppXor2>(v)), ...);
     }
 }
-// over the lanes at the same place of the wavefront's teams (rotations of sixteen lanes: together they visit all of a row's teams)
-template <int N> __device__ __forceinline__ void across_teams(float (&v)[N], int lanes) {
+// over the lanes at the same place of the wavefront's teams (rotations of sixteen lanes: together they visit all of a row's teams), of two tables at once
+template <int N, int M> __device__ __forceinline__ void across_teams(int lanes, float (&v)[N][M], float (&w)[N][M]) {
     constexpr int kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;
     auto each = [&](auto f) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = f(v[i]);
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                v[n][m] = f(v[n][m]);
+                w[n][m] = f(w[n][m]);
+            }
     };
     if (lanes <= 8) each([](float x) { return x + dpp<kDppRor8>(x); });
     if (lanes <= 4) each([](float x) { return x + dpp<kRor4>(x); });
@@ -320,11 +325,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
                     leave(c + held.at[it] + i, db[it][i]);
                 }
     } else {
-#pragma unroll
-        for (int it = 0; it < ITERS; ++it) {
-            across_teams<V>(dg[it], lanes);
-            across_teams<V>(db[it], lanes);
-        }
+        across_teams(lanes, dg, db);
         // each wavefront's sums by (kind, piece, value, lane), then a thread adds up a channel's over the wavefronts
         const int wave = threadIdx.x >> 6, slots = ITERS * V * lanes;
         if ((int)(threadIdx.x & 63) < lanes) {
