@@ -310,3 +310,51 @@ def test_more_values_than_32_bit_offsets():
     small = [torch.zeros(300, dtype=torch.bfloat16, device=DEV), tail.clone()]
     P.ff_adamw_step(P.make_adamw_plan([small[0]], [small[1]], **P.adamw_states([small[0]], 8)), 1, lr=1e-2, eps=1e-12)
     assert torch.equal(p[-300:], small[0])
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3, 5])
+def test_codes_at_any_byte(shift):
+    """8-bit states that lie back to back in one buffer, at every alignment, step like ones with allocations of their own."""
+    sizes = [1001, 257, 4099, 3]
+    model, other = (Model(sizes, "f32", "bf16", 8, seed=11) for _ in range(2))
+    packed = {}
+    for k in ("m", "v", "m_exp", "v_exp"):
+        room = torch.full((sum(t.numel() for t in model.lists[k]) + 16,), 77, dtype=torch.uint8, device=DEV)
+        at, views = shift, []
+        for t in model.lists[k]:
+            view = room[at:at + t.numel()]
+            view.copy_(t)
+            views.append(view)
+            at += t.numel()
+        packed[k], model.lists[k] = (room, at), views
+    model.plan = P.make_adamw_plan(model.lists["p"], model.lists["g"], model.lists["m"], model.lists["v"], m_exp=model.lists["m_exp"], v_exp=model.lists["v_exp"],
+                                   weight_decay=model.decay)
+    for step in (1, 2):
+        for m in (model, other):
+            P.ff_adamw_step(m.plan, step, seed=step, **HYPER)
+    a, b = model.host(), other.host()
+    for k in ("p", "m", "v", "m_exp", "v_exp"):
+        assert all(np.array_equal(x, y) for x, y in zip(a[k], b[k])), k
+    assert all(torch.equal(x, y) for x, y in zip(P.ff_adamw_moments(model.plan), P.ff_adamw_moments(other.plan)))
+    for room, end in packed.values():
+        assert (room[:shift] == 77).all() and (room[end:] == 77).all()
+
+
+def test_refused_tensors():
+    x, half = torch.zeros(300, device=DEV), torch.zeros(300, device=DEV, dtype=torch.bfloat16)
+    codes, exps = torch.zeros(300, dtype=torch.uint8, device=DEV), torch.zeros(2, dtype=torch.uint8, device=DEV)
+    ok = dict(params=[x], grads=[half], m=[codes], v=[codes.clone()], m_exp=[exps], v_exp=[exps.clone()])
+    P.make_adamw_plan(**ok)
+    for kw, error in ((dict(params=[x.double()]), TypeError), (dict(grads=[half.half()]), TypeError), (dict(m=[x]), TypeError), (dict(m_exp=[exps[:1]]), ValueError),
+                      (dict(v=[codes[:299]]), ValueError), (dict(params=[x, x]), ValueError), (dict(params=[torch.zeros(600, device=DEV)[::2]]), ValueError),
+                      (dict(v_exp=None), ValueError), (dict(params=[x.cpu()]), ValueError), (dict(master=[x.clone()]), P.FFError), (dict(params=[]), ValueError)):
+        with pytest.raises(error):
+            P.make_adamw_plan(**{**ok, **kw})
+    plan = P.make_adamw_plan(**ok)
+    norm = P.ff_grad_norm(plan)
+    for kw, error in ((dict(norm=norm), ValueError), (dict(max_norm=1.0), ValueError), (dict(norm=norm.double(), max_norm=1.0), TypeError),
+                      (dict(norm=norm.cpu(), max_norm=1.0), ValueError), (dict(step=0), P.FFError), (dict(lr=float("nan")), P.FFError), (dict(norm=norm, max_norm=-1.0), P.FFError)):
+        with pytest.raises(error):
+            P.ff_adamw_step(plan, **{**dict(step=1, lr=1e-3), **kw})
+    with pytest.raises(P.FFError):
+        P.ff_adamw_step(P.make_grad_plan([half]), 1, lr=1e-3)

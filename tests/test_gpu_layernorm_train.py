@@ -310,3 +310,32 @@ def test_rows_beyond_32_bit_offsets():
     want = P.ff_layernorm_backward(tail, gamma, tail, eps=EPS)
     assert torch.equal(dx[-64:], want[0]) and (dx[:-64:1_000_003] == 0).all()
     assert torch.allclose(dgamma, want[1], rtol=1e-5, atol=1e-4) and torch.allclose(dbeta, want[2], rtol=1e-5, atol=1e-4)
+
+
+def test_refused_tensors():
+    x, g = torch.randn(20, 64, device=DEV), torch.ones(64, device=DEV)
+    cases = [(dict(x=x.t().contiguous().t()), ValueError), (dict(x=x.half()), TypeError), (dict(gamma=g[:32]), ValueError), (dict(beta=g.bfloat16()), TypeError),
+             (dict(residual=x[:10]), ValueError), (dict(out=x), P.FFError), (dict(sum_out=x), ValueError), (dict(residual=x.bfloat16()), TypeError),
+             (dict(eps=-1.0), P.FFError), (dict(gamma=g.cpu()), ValueError), (dict(out=torch.empty(20, 65, device=DEV)), ValueError)]
+    for kw, error in cases:
+        with pytest.raises(error):
+            P.ff_layernorm_forward(**{**dict(x=x, gamma=g, beta=g), **kw})
+    _, _, mean, rstd = P.ff_layernorm_forward(x, g, g)
+    cases = [(dict(dy=x[:, :32]), ValueError), (dict(mean=mean), P.FFError), (dict(mean=mean[:5], rstd=rstd[:5]), ValueError), (dict(dsum=x.bfloat16()), TypeError),
+             (dict(accumulate=True), ValueError), (dict(dx=x), P.FFError), (dict(ws=torch.empty(8, dtype=torch.uint8, device=DEV)), P.FFError),
+             (dict(dgamma=g.bfloat16(), dbeta=g.clone()), TypeError), (dict(dgamma=g, dbeta=g.clone()), P.FFError)]
+    for kw, error in cases:
+        with pytest.raises(error):
+            P.ff_layernorm_backward(**{**dict(s=x, gamma=g, dy=x.clone()), **kw})
+
+
+def test_leading_axes():
+    """[n_a, n_b, c] as the modules have it: statistics of that shape without the channels."""
+    x = torch.randn(6, 10, 64, device=DEV)
+    g, b = torch.rand(64, device=DEV), torch.rand(64, device=DEV)
+    y, _, mean, rstd = P.ff_layernorm_forward(x, g, b)
+    flat = P.ff_layernorm_forward(x.view(60, 64), g, b)
+    assert mean.shape == (6, 10) and torch.equal(y.view(60, 64), flat[0]) and torch.equal(rstd.view(60), flat[3])
+    dx, dgamma, _ = P.ff_layernorm_backward(x, g, y, mean=mean, rstd=rstd)
+    want = P.ff_layernorm_backward(x.view(60, 64), g, y.view(60, 64), mean=flat[2], rstd=flat[3])
+    assert torch.equal(dx.view(60, 64), want[0]) and torch.equal(dgamma, want[1])
