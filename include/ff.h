@@ -358,7 +358,7 @@ typedef struct {
 } ff_adamw_hyper;
 
 /* Bytes of the plan for these tensors (host array of desc->n_tensors entries); 0 if an argument is invalid, or if the
- * tensors come to 2^24 pieces or more (FF_EUNSUPPORTED in ff_adamw_plan): one for each 4096 values of a tensor, at least one. */
+ * tensors come to 2^24 pieces or more (FF_EUNSUPPORTED in ff_adamw_plan): one for each 2048 values of a tensor, at least one. */
 size_t ff_adamw_plan_bytes(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors);
 
 /* Writes the plan into host memory (plan_bytes as reported above).  Tensors of one plan must not overlap. */

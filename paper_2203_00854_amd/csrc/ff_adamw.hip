@@ -13,7 +13,7 @@ namespace ff {
 
 constexpr int kGroup = 256;              // values that share an exponent in 8-bit states
 constexpr int kTurn = 8 * kGroup;        // values that a block of 256 threads holds at one time
-constexpr int kPiece = 2 * kTurn;
+constexpr int kPiece = kTurn;            // (two turns to a piece: 264 us where one takes 245, by the blocks that end together)
 constexpr int kNormBlocks = 2048;        // partial sums of the norm
 constexpr int kTopM = 14, kTopV = 30;    // exponent field of a group's largest magnitude among the codes: the highest that rounding up cannot leave
 
@@ -100,11 +100,22 @@ template <typename T> struct At {
 template <typename T> __device__ __forceinline__ typename At<T>::One* global(void* p) { return (typename At<T>::One*)p; }
 template <typename T> __device__ __forceinline__ const typename At<T>::One* global(const void* p) { return (const typename At<T>::One*)p; }
 
-// Values at, .. at + 3 of a piece of n; WHOLE: all of them are there.
-template <bool WHOLE, typename T> __device__ __forceinline__ void load4(const void* base, int at, int n, float (&v)[4]) {
+// How values at, .. at + 3 of a piece of n are reached: each checked, all known to be there, or that and past the caches.
+enum How { kChecked, kWhole, kStreamed };
+template <How HOW, typename T> __device__ __forceinline__ typename At<T>::Vec fetch(const typename At<T>::One* p) {
+    const typename At<T>::Four* four = (const typename At<T>::Four*)p;
+    if constexpr (HOW == kStreamed) return __builtin_nontemporal_load(four);
+    else return *four;
+}
+template <How HOW, typename T> __device__ __forceinline__ void put(typename At<T>::One* p, typename At<T>::Vec v) {
+    typename At<T>::Four* four = (typename At<T>::Four*)p;
+    if constexpr (HOW == kStreamed) __builtin_nontemporal_store(v, four);
+    else *four = v;
+}
+template <How HOW, typename T> __device__ __forceinline__ void load4(const void* base, int at, int n, float (&v)[4]) {
     const auto p = global<T>(base) + at;
-    if constexpr (WHOLE) {
-        const typename At<T>::Vec f = *(const typename At<T>::Four*)p;
+    if constexpr (HOW != kChecked) {
+        const typename At<T>::Vec f = fetch<HOW, T>(p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = to_f32<T>(f[i]);
     } else {
@@ -112,7 +123,7 @@ template <bool WHOLE, typename T> __device__ __forceinline__ void load4(const vo
         for (int i = 0; i < 4; ++i) v[i] = at + i < n ? to_f32<T>(p[i]) : 0.f;
     }
 }
-template <bool WHOLE, typename T> __device__ __forceinline__ void store4(void* base, int at, int n, const float (&v)[4]) {
+template <How HOW, typename T> __device__ __forceinline__ void store4(void* base, int at, int n, const float (&v)[4]) {
     const auto p = global<T>(base) + at;
     typename At<T>::Vec f;
     if constexpr (sizeof(T) == 2) {
@@ -123,26 +134,26 @@ template <bool WHOLE, typename T> __device__ __forceinline__ void store4(void* b
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = v[i];
     }
-    if constexpr (WHOLE) {
-        *(typename At<T>::Four*)p = f;
+    if constexpr (HOW != kChecked) {
+        put<HOW, T>(p, f);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (at + i < n) p[i] = f[i];
     }
 }
-template <bool WHOLE> __device__ __forceinline__ uint32_t load4(const void* base, int at, int n) {                   // four codes
+template <How HOW> __device__ __forceinline__ uint32_t load4(const void* base, int at, int n) {                     // four codes
     const auto p = global<uint8_t>(base) + at;
-    if constexpr (WHOLE) return __builtin_bit_cast(uint32_t, (At<uint8_t>::Vec)(*(const At<uint8_t>::Four*)p));
+    if constexpr (HOW != kChecked) return __builtin_bit_cast(uint32_t, (At<uint8_t>::Vec)fetch<HOW, uint8_t>(p));
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w |= at + i < n ? (uint32_t)p[i] << 8 * i : 0u;
     return w;
 }
-template <bool WHOLE> __device__ __forceinline__ void store4(void* base, int at, int n, uint32_t w) {
+template <How HOW> __device__ __forceinline__ void store4(void* base, int at, int n, uint32_t w) {
     const auto p = global<uint8_t>(base) + at;
-    if constexpr (WHOLE) {
-        *(At<uint8_t>::Four*)p = __builtin_bit_cast(At<uint8_t>::Vec, w);
+    if constexpr (HOW != kChecked) {
+        put<HOW, uint8_t>(p, __builtin_bit_cast(At<uint8_t>::Vec, w));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -150,13 +161,21 @@ template <bool WHOLE> __device__ __forceinline__ void store4(void* base, int at,
     }
 }
 
-// The turns of a piece, 512 values to a wavefront: whole ones without a check of any lane, then the one at its end.
-template <typename F> __device__ __forceinline__ void turns(int n, F go) {
+// The turn of a piece, 512 values to a wavefront: without a check of any lane where all of them are there.
+template <How HOW, typename F> __device__ __forceinline__ void turns_as(int n, F go) {
     for (int first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 2 * kGroup; first < n; first += kTurn) {
         const int base = first + (threadIdx.x & 32) * (kGroup / 32);
-        if (first + 2 * kGroup <= n) go(std::true_type{}, base);
-        else go(std::false_type{}, base);
+        if (first + 2 * kGroup <= n) go(std::integral_constant<How, HOW>{}, base);
+        else go(std::integral_constant<How, kChecked>{}, base);
     }
+}
+// What passes once per step goes past the caches, which keeps them for the gradients between their norm and the step: 48 blocks with a
+// master copy 300 -> 245 us for both, float32 alone 316 -> 244, 8 bits 139 -> 120.  Not where a tensor lies across the
+// lines, whose parts would reach memory one by one (400 ragged tensors 64 -> 71).  (A loop of its own for each: of two branches inside
+// one loop the compiler would join the loads, and lose their hint.)
+template <typename F> __device__ __forceinline__ void turns(int n, bool streamed, F go) {
+    if (streamed) turns_as<kStreamed>(n, go);
+    else turns_as<kWhole>(n, go);
 }
 
 // ---- 8-bit states ------------------------------------------------------------------------
@@ -220,10 +239,10 @@ __global__ __launch_bounds__(256) void k_grad_norm(const Piece* __restrict__ pie
         float v[kPiece / 1024][4];
         if (n == kPiece) {
 #pragma unroll
-            for (int t = 0; t < kPiece / 1024; ++t) load4<true, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
+            for (int t = 0; t < kPiece / 1024; ++t) load4<kWhole, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
         } else {
 #pragma unroll
-            for (int t = 0; t < kPiece / 1024; ++t) load4<false, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
+            for (int t = 0; t < kPiece / 1024; ++t) load4<kChecked, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
         }
 #pragma unroll
         for (int t = 0; t < kPiece / 1024; ++t)
@@ -283,8 +302,11 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
     const int lane = threadIdx.x & 31;
     const float keep = 1.f - a.lr * pc.decay;
     const bool master = pc.master != nullptr;
-    turns(pc.n, [&](auto whole, int base) {
-        constexpr bool W = decltype(whole)::value;
+    const uintptr_t states = BITS == 32 ? (uintptr_t)pc.m | (uintptr_t)pc.v : 0;
+    const bool streamed = (((uintptr_t)pc.p | (uintptr_t)pc.g | (uintptr_t)pc.master | states) & 15u) == 0;
+    turns(pc.n, streamed, [&](auto how, int base) {
+        constexpr How H = decltype(how)::value;
+        constexpr bool W = H != kChecked;
         float m[2][4], v[2][4], w[2][4], g[2][4];
         [[maybe_unused]] uint32_t fm[2], fv[2], em = 0, ev = 0;
         const bool group = W || base < pc.n;                   // (at the end of a piece half a wavefront may have none)
@@ -297,15 +319,15 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = base + h * 128 + lane * 4;
-            load4<W, G>(pc.g, at, pc.n, g[h]);
-            if (master) load4<W, float>(pc.master, at, pc.n, w[h]);
-            else load4<W, P>(pc.p, at, pc.n, w[h]);
+            load4<H, G>(pc.g, at, pc.n, g[h]);
+            if (master) load4<H, float>(pc.master, at, pc.n, w[h]);
+            else load4<H, P>(pc.p, at, pc.n, w[h]);
             if constexpr (BITS == 8) {
-                fm[h] = load4<W>(pc.m, at, pc.n);
-                fv[h] = load4<W>(pc.v, at, pc.n);
+                fm[h] = load4<H>(pc.m, at, pc.n);
+                fv[h] = load4<H>(pc.v, at, pc.n);
             } else {
-                load4<W, float>(pc.m, at, pc.n, m[h]);
-                load4<W, float>(pc.v, at, pc.n, v[h]);
+                load4<H, float>(pc.m, at, pc.n, m[h]);
+                load4<H, float>(pc.v, at, pc.n, v[h]);
             }
         }
         if constexpr (BITS == 8) {
@@ -330,11 +352,11 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
                 w[h][i] = w[h][i] * keep - a.step_size * (m[h][i] * __builtin_amdgcn_rcpf(root));
             }
             const int at = base + h * 128 + lane * 4;
-            if (master) store4<W, float>(pc.master, at, pc.n, w[h]);
-            store4<W, P>(pc.p, at, pc.n, w[h]);
+            if (master) store4<H, float>(pc.master, at, pc.n, w[h]);
+            store4<H, P>(pc.p, at, pc.n, w[h]);
             if constexpr (BITS == 32) {
-                store4<W, float>(pc.m, at, pc.n, m[h]);
-                store4<W, float>(pc.v, at, pc.n, v[h]);
+                store4<H, float>(pc.m, at, pc.n, m[h]);
+                store4<H, float>(pc.v, at, pc.n, v[h]);
             }
         }
         if constexpr (BITS == 8) {
@@ -369,8 +391,8 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
                     const uint32_t c = sv.code(v[h][i], r >> 16), least = bv < 1u ? bv : 1u;      // a positive v is not held as 0
                     cv |= (c > least ? c : least) << 8 * i;
                 }
-                store4<W>(pc.m, at, pc.n, em == 255u ? 0u : cm);
-                store4<W>(pc.v, at, pc.n, ev == 255u ? 0u : cv);
+                store4<H>(pc.m, at, pc.n, em == 255u ? 0u : cm);
+                store4<H>(pc.v, at, pc.n, ev == 255u ? 0u : cv);
             }
         }
     });
@@ -408,8 +430,11 @@ __global__ __launch_bounds__(256) void k_moments(const Piece* __restrict__ piece
     const Piece& pc = pieces[blockIdx.x];
     if (pc.tag != tag) return;
     const int lane = threadIdx.x & 31;
-    turns(pc.n, [&](auto whole, int base) {
-        constexpr bool W = decltype(whole)::value;
+    const uintptr_t states = BITS == 32 ? (uintptr_t)pc.m | (uintptr_t)pc.v : 0;
+    const bool streamed = (((uintptr_t)m_out | (uintptr_t)v_out | (uintptr_t)pc.first_value * 4 | states) & 15u) == 0;
+    turns(pc.n, streamed, [&](auto how, int base) {
+        constexpr How H = decltype(how)::value;
+        constexpr bool W = H != kChecked;
         float m[2][4], v[2][4];
         if constexpr (BITS == 8) {
             const bool group = W || base < pc.n;
@@ -418,8 +443,8 @@ __global__ __launch_bounds__(256) void k_moments(const Piece* __restrict__ piece
             uint32_t fm[2], fv[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                fm[h] = load4<W>(pc.m, base + h * 128 + lane * 4, pc.n);
-                fv[h] = load4<W>(pc.v, base + h * 128 + lane * 4, pc.n);
+                fm[h] = load4<H>(pc.m, base + h * 128 + lane * 4, pc.n);
+                fv[h] = load4<H>(pc.v, base + h * 128 + lane * 4, pc.n);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -431,14 +456,14 @@ __global__ __launch_bounds__(256) void k_moments(const Piece* __restrict__ piece
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                load4<W, float>(pc.m, base + h * 128 + lane * 4, pc.n, m[h]);
-                load4<W, float>(pc.v, base + h * 128 + lane * 4, pc.n, v[h]);
+                load4<H, float>(pc.m, base + h * 128 + lane * 4, pc.n, m[h]);
+                load4<H, float>(pc.v, base + h * 128 + lane * 4, pc.n, v[h]);
             }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (m_out) store4<W, float>(m_out + pc.first_value, base + h * 128 + lane * 4, pc.n, m[h]);
-            if (v_out) store4<W, float>(v_out + pc.first_value, base + h * 128 + lane * 4, pc.n, v[h]);
+            if (m_out) store4<H, float>(m_out + pc.first_value, base + h * 128 + lane * 4, pc.n, m[h]);
+            if (v_out) store4<H, float>(v_out + pc.first_value, base + h * 128 + lane * 4, pc.n, v[h]);
         }
     });
 }

@@ -197,7 +197,7 @@ def test_layernorm_overlaps():
 
 def test_more_pieces_than_blocks_are_refused():
     d = B.AdamWDesc(P.FF_F32, P.FF_F32, 0, 1)
-    t = tensors({"g": 0x10000, "numel": 4096 * ((1 << 24) - 1)})
+    t = tensors({"g": 0x10000, "numel": 2048 * ((1 << 24) - 1)})
     n = plan_bytes(d, t)
     assert n > 0
     t["numel"] += 1
