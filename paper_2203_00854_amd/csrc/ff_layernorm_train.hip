@@ -252,18 +252,36 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
     const float inv_c = 1.f / (float)c;
     const int per_block = WIDE ? 1 : (int)blockDim.x / lanes;
     const int64_t stride = (int64_t)gridDim.x * per_block;
-    for (int64_t row = (int64_t)blockIdx.x * per_block + (WIDE ? 0 : threadIdx.x / lanes); row < rows; row += stride) {
-        const int64_t base = row * c;
-        float u[ITERS][V], d[ITERS][V];
-        Pc pu[ITERS], pd[ITERS], ps[ITERS];
+    // the next row on its way while this one is worked on: 196608 x 256 56 -> 53 us, with dsum 66 -> 61, but 2048 x 2048 x 128 574 -> 611
+    constexpr bool AHEAD = STREAMED && !WIDE && V * ITERS <= 8;
+    int64_t row = (int64_t)blockIdx.x * per_block + (WIDE ? 0 : threadIdx.x / lanes);
+    Pc pu[ITERS], pd[ITERS], ps[ITERS];
+    [[maybe_unused]] Pc nu[ITERS], nd[ITERS], ns[ITERS];
+    auto load = [&](Pc(&x)[ITERS], Pc(&y)[ITERS], Pc(&z)[ITERS], int64_t base) {
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            pu[it] = fetch<STREAMED, T, V>(s + base + held.at[it]);
-            pd[it] = fetch<STREAMED, T, V>(dy + base + held.at[it]);
+            x[it] = fetch<STREAMED, T, V>(s + base + held.at[it]);
+            y[it] = fetch<STREAMED, T, V>(dy + base + held.at[it]);
         }
         if (dsum) {
 #pragma unroll
-            for (int it = 0; it < ITERS; ++it) ps[it] = fetch<STREAMED, T, V>(dsum + base + held.at[it]);
+            for (int it = 0; it < ITERS; ++it) z[it] = fetch<STREAMED, T, V>(dsum + base + held.at[it]);
+        }
+    };
+    if (AHEAD && row < rows) load(nu, nd, ns, row * c);
+    for (; row < rows; row += stride) {
+        const int64_t base = row * c;
+        float u[ITERS][V], d[ITERS][V];
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) {
+                pu[it] = nu[it];
+                pd[it] = nd[it];
+                ps[it] = ns[it];
+            }
+            if (row + stride < rows) load(nu, nd, ns, base + stride * c);
+        } else {
+            load(pu, pd, ps, base);
         }
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) widen<T, V>(pu[it], u[it]);
@@ -426,7 +444,7 @@ static Shape shape_of(int dtype, int c) {
 }
 
 // Inputs of 160 MB to 1 GB are loaded past the caches, which hold 256 MB and then keep more of what is written for its reader: 5120 x 384 x 64
-// forward 90 -> 80 us, backward 140 -> 128, 196608 x 256 with the residual sum 73 -> 62.  Smaller ones may lie in the caches (65536 x 128 float32, 34 MB,
+// forward 90 -> 80 us, backward 140 -> 125, 196608 x 256 with the residual sum 73 -> 62.  Smaller ones may lie in the caches (65536 x 128 float32, 34 MB,
 // 13.6 -> 15.9), larger ones pass through them whole either way (2048 x 2048 x 128 forward 379 -> 386).
 static bool streams(int64_t input_bytes) { return input_bytes > 160000000 && input_bytes < 1000000000; }
 

@@ -339,3 +339,35 @@ def test_leading_axes():
     dx, dgamma, _ = P.ff_layernorm_backward(x, g, y, mean=mean, rstd=rstd)
     want = P.ff_layernorm_backward(x.view(60, 64), g, y.view(60, 64), mean=flat[2], rstd=flat[3])
     assert torch.equal(dx.view(60, 64), want[0]) and torch.equal(dgamma, want[1])
+
+
+@pytest.mark.parametrize("dtype,rows,c", [("bf16", 500_000, 128), ("bf16", 500_000, 100), ("f32", 150_000, 173), ("bf16", 90_000, 1100), ("f32", 30_000, 2000)])
+def test_inputs_beyond_the_caches(dtype, rows, c):
+    """Sizes whose inputs are loaded past the caches: rows from all over the tensor against the oracle, sums over all rows in float64,
+    results in place as well."""
+    gen = torch.Generator(DEV).manual_seed(c)
+    randn = lambda *s: torch.randn(*s, generator=gen, device=DEV).to(DT[dtype])  # noqa: E731
+    d = {"x": randn(rows, c), "residual": randn(rows, c), "dy": randn(rows, c), "dsum": randn(rows, c), "gamma": randn(c), "beta": randn(c)}
+    assert 160e6 < 2 * d["x"].numel() * d["x"].element_size() < 1e9
+    some = torch.cat([torch.arange(40), torch.arange(0, rows, 9973), torch.arange(rows - 40, rows)]).to(DEV)
+    part = {k: (v[some] if v.dim() == 2 else v).cpu() for k, v in d.items()}
+    y, s, mean, rstd = P.ff_layernorm_forward(d["x"], d["gamma"], d["beta"], residual=d["residual"], eps=EPS)
+    check_forward(part, dtype, (y[some], s[some], mean[some], rstd[some]), True)
+    del y
+    for saved in (True, False):
+        kw = dict(mean=mean, rstd=rstd) if saved else {}
+        dx, dgamma, dbeta = P.ff_layernorm_backward(s, d["gamma"], d["dy"], dsum=d["dsum"], eps=EPS, **kw)
+        u = (s.double() - mean.double()[:, None]) * rstd.double()[:, None]
+        terms = d["dy"].double() * u
+        # at most 1200 additions, and the terms' own error: what mean and rstd are off by (test's head) and two operations
+        size = terms.abs().sum(0)
+        off = (1200 + 80) * U * size + (d["dy"].double().abs() * (45 * U * s.double().abs().mean(1) * rstd.double())[:, None]).sum(0)
+        assert ((dgamma.double() - terms.sum(0)).abs() <= off).all()
+        assert ((dbeta.double() - d["dy"].double().sum(0)).abs() <= 1200 * U * d["dy"].double().abs().sum(0)).all()
+        del u, terms
+        small = P.ff_layernorm_backward(s[some], d["gamma"], d["dy"][some], dsum=d["dsum"][some], eps=EPS, **{k: v[some] for k, v in kw.items()})
+        check_backward(s[some].cpu(), part, dtype, (dx[some], small[1], small[2]), True)
+        over = d["dy"].clone() if saved else d["dsum"].clone()
+        args = dict(dy=over, dsum=d["dsum"]) if saved else dict(dy=d["dy"], dsum=over)
+        again = P.ff_layernorm_backward(s, d["gamma"], eps=EPS, dx=over, **args, **kw)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dgamma) and torch.equal(again[2], dbeta)
