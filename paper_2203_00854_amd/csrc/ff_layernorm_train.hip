@@ -231,7 +231,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
 }
 
 // Bytes bound it: 2048 x 2048 x 128 bfloat16 in 574 us (5.6 TB/s), 612 where the statistics are formed again (four sums over a team one after
-// the other, not two); 5120 x 384 x 64 in 125 (6.0 TB/s).  Sixteen wavefronts on a compute unit carry that: twice as many,
+// the other, not two); 5120 x 384 x 64 in 125 to 133 (5.7 to 6.0 TB/s).  Sixteen wavefronts on a compute unit carry that: twice as many,
 // in registers or blocks, took longer (662), and each block more makes the second launch longer.
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
 // over its teams and wavefronts in a fixed order and leaves 2 c partial sums; with one block in all these are the result.
@@ -252,7 +252,8 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
     const float inv_c = 1.f / (float)c;
     const int per_block = WIDE ? 1 : (int)blockDim.x / lanes;
     const int64_t stride = (int64_t)gridDim.x * per_block;
-    // the next row on its way while this one is worked on: 196608 x 256 56 -> 53 us, with dsum 66 -> 61, but 2048 x 2048 x 128 574 -> 611
+    // the next row on its way while this one is worked on: 5120 x 384 x 64 with saved statistics 145 -> 140 us, 196608 x 256 with dsum 71 -> 68,
+    // but 2048 x 2048 x 128 574 -> 611
     constexpr bool AHEAD = STREAMED && !WIDE && V * ITERS <= 8;
     int64_t row = (int64_t)blockIdx.x * per_block + (WIDE ? 0 : threadIdx.x / lanes);
     Pc pu[ITERS], pd[ITERS], ps[ITERS];
@@ -444,7 +445,7 @@ static Shape shape_of(int dtype, int c) {
 }
 
 // Inputs of 160 MB to 1 GB are loaded past the caches, which hold 256 MB and then keep more of what is written for its reader: 5120 x 384 x 64
-// forward 90 -> 80 us, backward 140 -> 125, 196608 x 256 with the residual sum 73 -> 62.  Smaller ones may lie in the caches (65536 x 128 float32, 34 MB,
+// backward 144 -> 140 us, 196608 x 256 61 -> 55, with the gradient that passes by 77 -> 71.  Smaller ones may lie in the caches (65536 x 128 float32, 34 MB,
 // 13.6 -> 15.9), larger ones pass through them whole either way (2048 x 2048 x 128 forward 379 -> 386).
 static bool streams(int64_t input_bytes) { return input_bytes > 160000000 && input_bytes < 1000000000; }
 
