@@ -412,20 +412,21 @@ def _stream_of(device) -> int:
 
 
 def _norm_desc(x, gamma, eps):
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError(f"no channels in shape {tuple(x.shape)}")
-    c, dtype, device = x.shape[-1], x.dtype, x.device
-    _fit(x, "x", dtype, x.shape, device)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    if not shape or shape[-1] < 1:
+        raise ValueError(f"no channels in shape {tuple(shape)}")
+    if not (x.is_cuda and x.is_contiguous()):
+        _refuse(x, "x", dtype, shape, device)
+    c = shape[-1]
     _fit(gamma, "gamma", dtype, (c,), device)
-    return NormDesc(_dtype_code(x), c, x.numel() // c, eps), dtype, device
+    return NormDesc(_dtype_code(x), c, x.numel() // c, eps), shape, dtype, device
 
 
 def ff_layernorm_forward(x, gamma, beta, residual=None, eps: float = 1e-5, stats: bool = True, out=None, sum_out=None):
     """Layer norm over the last axis of x, or of x + residual; returns (y, sum, mean, rstd).  sum (the rounded x + residual,
     None without one) is what ff_layernorm_backward takes as s; sum_out may be x or residual itself.  stats=False keeps no mean and rstd."""
     import torch
-    desc, dtype, device = _norm_desc(x, gamma, eps)
-    shape = x.shape
+    desc, shape, dtype, device = _norm_desc(x, gamma, eps)
     _fit(beta, "beta", dtype, gamma.shape, device)
     out = torch.empty_like(x) if out is None else _fit(out, "out", dtype, shape, device)
     if residual is not None:
@@ -435,7 +436,9 @@ def ff_layernorm_forward(x, gamma, beta, residual=None, eps: float = 1e-5, stats
         raise ValueError("sum_out needs a residual")
     mean = rstd = None
     if stats:
-        mean, rstd = (torch.empty(shape[:-1], dtype=torch.float32, device=device) for _ in range(2))
+        rows = shape[:-1]
+        mean = torch.empty(rows, dtype=torch.float32, device=device)
+        rstd = torch.empty(rows, dtype=torch.float32, device=device)
     _check(lib().ff_layernorm_forward(C.byref(desc), x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), _ptr(sum_out), out.data_ptr(),
                                       _ptr(mean), _ptr(rstd), _stream_of(device)))
     return out, sum_out, mean, rstd
@@ -447,8 +450,7 @@ def ff_layernorm_backward(s, gamma, dy, mean=None, rstd=None, dsum=None, eps: fl
     sum).  Without mean and rstd they are formed again from s.  dsum: the gradient that reaches s by other ways, added to dx.
     dx may be dy or dsum itself; accumulate adds to the given dgamma and dbeta."""
     import torch
-    desc, dtype, device = _norm_desc(s, gamma, eps)
-    shape = s.shape
+    desc, shape, dtype, device = _norm_desc(s, gamma, eps)
     _fit(dy, "dy", dtype, shape, device)
     if dsum is not None:
         _fit(dsum, "dsum", dtype, shape, device)
