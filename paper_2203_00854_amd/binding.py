@@ -1,4 +1,5 @@
-"""Thin Python binding of libff's C ABI (include/ff.h): argument marshalling only.
+"""Thin Python binding of libff's C ABI (include/ff.h): argument marshalling only, by ctypes, or in C++
+(csrc/ff_calls.cpp) where a call's kernels take less time than ctypes does.
 
 Every step of the attention path runs inside the HIP library; torch is used here for
 device memory and the current stream.  If the library has not been built the import of
@@ -178,6 +179,30 @@ def last_error() -> str:
 def _check(status: int):
     if status != FF_OK:
         raise FFError(status, last_error())
+
+
+_calls = None
+
+
+def calls():
+    """The module of csrc/ff_calls.cpp: checks, allocations and C call of a training operator in one step; raises if it has not been built."""
+    global _calls
+    if _calls is None:
+        lib()
+        if not os.path.exists(os.path.join(PKG, "_calls.so")):
+            raise FileNotFoundError(f"{PKG}/_calls.so is missing: build it with `python -m paper_2203_00854_amd.build` (there is no fallback path)")
+        import torch  # noqa: F401    (its libraries are what the module's names are looked up in)
+
+        from . import _calls as module
+        _calls = module
+    return _calls
+
+
+def _done(result):
+    """The results of a call, which are a status if the library refused it."""
+    if result.__class__ is int:
+        _check(result)
+    return result
 
 
 def _dtype_code(t) -> int:
@@ -411,37 +436,10 @@ def _stream_of(device) -> int:
     return torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device.index)
 
 
-def _norm_desc(x, gamma, eps):
-    shape, dtype, device = x.shape, x.dtype, x.device
-    if not shape or shape[-1] < 1:
-        raise ValueError(f"no channels in shape {tuple(shape)}")
-    if not (x.is_cuda and x.is_contiguous()):
-        _refuse(x, "x", dtype, shape, device)
-    c = shape[-1]
-    _fit(gamma, "gamma", dtype, (c,), device)
-    return NormDesc(_dtype_code(x), c, x.numel() // c, eps), shape, dtype, device
-
-
 def ff_layernorm_forward(x, gamma, beta, residual=None, eps: float = 1e-5, stats: bool = True, out=None, sum_out=None):
     """Layer norm over the last axis of x, or of x + residual; returns (y, sum, mean, rstd).  sum (the rounded x + residual,
     None without one) is what ff_layernorm_backward takes as s; sum_out may be x or residual itself.  stats=False keeps no mean and rstd."""
-    import torch
-    desc, shape, dtype, device = _norm_desc(x, gamma, eps)
-    _fit(beta, "beta", dtype, gamma.shape, device)
-    out = torch.empty_like(x) if out is None else _fit(out, "out", dtype, shape, device)
-    if residual is not None:
-        _fit(residual, "residual", dtype, shape, device)
-        sum_out = torch.empty_like(x) if sum_out is None else _fit(sum_out, "sum_out", dtype, shape, device)
-    elif sum_out is not None:
-        raise ValueError("sum_out needs a residual")
-    mean = rstd = None
-    if stats:
-        rows = shape[:-1]
-        mean = torch.empty(rows, dtype=torch.float32, device=device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=device)
-    _check(lib().ff_layernorm_forward(C.byref(desc), x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), _ptr(sum_out), out.data_ptr(),
-                                      _ptr(mean), _ptr(rstd), _stream_of(device)))
-    return out, sum_out, mean, rstd
+    return _done(calls().layernorm_forward(x, gamma, beta, residual, eps, stats, out, sum_out))
 
 
 def ff_layernorm_backward(s, gamma, dy, mean=None, rstd=None, dsum=None, eps: float = 1e-5, dx=None, dgamma=None, dbeta=None,
@@ -449,26 +447,7 @@ def ff_layernorm_backward(s, gamma, dy, mean=None, rstd=None, dsum=None, eps: fl
     """Gradients of ff_layernorm_forward; returns (dx, dgamma, dbeta), the last two float32.  s: what was normalised (x, or
     sum).  Without mean and rstd they are formed again from s.  dsum: the gradient that reaches s by other ways, added to dx.
     dx may be dy or dsum itself; accumulate adds to the given dgamma and dbeta."""
-    import torch
-    desc, shape, dtype, device = _norm_desc(s, gamma, eps)
-    _fit(dy, "dy", dtype, shape, device)
-    if dsum is not None:
-        _fit(dsum, "dsum", dtype, shape, device)
-    if mean is not None:
-        _fit(mean, "mean", torch.float32, shape[:-1], device)
-    if rstd is not None:
-        _fit(rstd, "rstd", torch.float32, shape[:-1], device)
-    if accumulate and (dgamma is None or dbeta is None):
-        raise ValueError("accumulate needs dgamma and dbeta")
-    dx = torch.empty_like(s) if dx is None else _fit(dx, "dx", dtype, shape, device)
-    sums = gamma.shape
-    dgamma = torch.empty(sums, dtype=torch.float32, device=device) if dgamma is None else _fit(dgamma, "dgamma", torch.float32, sums, device)
-    dbeta = torch.empty(sums, dtype=torch.float32, device=device) if dbeta is None else _fit(dbeta, "dbeta", torch.float32, sums, device)
-    if ws is None:
-        ws = _alloc_ws(ff_layernorm_backward_workspace_bytes(desc), device)
-    _check(lib().ff_layernorm_backward(C.byref(desc), s.data_ptr(), gamma.data_ptr(), _ptr(mean), _ptr(rstd), dy.data_ptr(), _ptr(dsum), dx.data_ptr(),
-                                       dgamma.data_ptr(), dbeta.data_ptr(), 1 if accumulate else 0, ws.data_ptr(), ws.numel(), _stream_of(device)))
-    return dx, dgamma, dbeta
+    return _done(calls().layernorm_backward(s, gamma, dy, mean, rstd, dsum, eps, dx, dgamma, dbeta, accumulate, ws))
 
 
 def ff_layernorm_backward_workspace_bytes(desc: NormDesc) -> int:
@@ -493,7 +472,7 @@ class AdamWPlan:
         _check(lib().ff_adamw_plan(C.byref(desc), table, host.ctypes.data, n))
         self.plan = torch.from_numpy(host).to(device)
         self.norm_ws = _alloc_ws(lib().ff_grad_norm_workspace_bytes(), device)
-        self.address, self.bytes = self.plan.data_ptr(), n
+        self.address, self.bytes, self.desc_address = self.plan.data_ptr(), n, C.addressof(desc)
 
     @property
     def ref(self):
@@ -572,12 +551,7 @@ def adamw_states(params, bits: int = 32):
 
 def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
     """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another."""
-    import torch
-    device = plan.device
-    out = torch.empty(1, dtype=torch.float32, device=device) if out is None else _fit(out, "out", torch.float32, (1,), device)
-    ws = plan.norm_ws if ws is None else ws
-    _check(lib().ff_grad_norm(plan.ref, plan.address, plan.bytes, out.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(device)))
-    return out
+    return _done(calls().grad_norm(plan.desc_address, plan.plan, out, plan.norm_ws if ws is None else ws))
 
 
 def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: int = 0):

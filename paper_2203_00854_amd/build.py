@@ -1,9 +1,9 @@
-"""Build libff.so (HIP, gfx950) in-tree, and the C parts of the test oracle if any.
+"""Build libff.so (HIP, gfx950) and _calls.so (the binding's part in C++) in-tree.
 
     python -m paper_2203_00854_amd.build
 
 hipcc cross-compiles for gfx950 without a GPU.  Objects go to _build/, the library to
-paper_2203_00854_amd/libff.so (git-ignored; it travels with the source tree to the GPU machine).
+paper_2203_00854_amd/libff.so and paper_2203_00854_amd/_calls.so (git-ignored; they travel with the source tree to the GPU machine).
 """
 from __future__ import annotations
 
@@ -11,6 +11,7 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +19,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libff.so")
+CALLS = os.path.join(PKG, "_calls.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -51,6 +53,22 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_calls() -> None:
+    """ff_calls.cpp, host code: a CPython module on libff.so and torch's libraries."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(home, "include"),
+           "-isystem", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"), os.path.join(CSRC, "ff_calls.cpp"), "-o", CALLS,
+           "-L", PKG, "-l:libff.so", "-L", os.path.join(home, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for ff_calls.cpp:\n" + r.stderr)
+    if r.stderr.strip():
+        sys.stderr.write(r.stderr)
+
+
 def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
@@ -60,8 +78,9 @@ def build(verbose: bool = True) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
+    _build_calls()
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources")
+        print(f"built {LIB} from {len(srcs)} sources, {CALLS}")
     return LIB
 
 
