@@ -413,29 +413,6 @@ def ff_gated_attention_residual(desc: AttnDesc, w: Dict[str, "object"], x, z=Non
 
 
 # ------------------------------------------------------------------------- training: layer norm, clipping, AdamW
-def _refuse(t, name, dtype, shape, device):
-    if t.dtype != dtype:
-        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device if device.type == 'cuda' else 'a GPU'}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
-    raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-
-
-def _fit(t, name, dtype, shape, device):
-    """The tensor, if a kernel may take it as `name`; otherwise TypeError or ValueError."""
-    if t.dtype != dtype or t.shape != shape or t.device != device or not (t.is_cuda and t.is_contiguous()):
-        _refuse(t, name, dtype, shape, device)
-    return t
-
-
-def _stream_of(device) -> int:
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (a stream object costs as much as a launch)
-    return torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device.index)
-
-
 def ff_layernorm_forward(x, gamma, beta, residual=None, eps: float = 1e-5, stats: bool = True, out=None, sum_out=None):
     """Layer norm over the last axis of x, or of x + residual; returns (y, sum, mean, rstd).  sum (the rounded x + residual,
     None without one) is what ff_layernorm_backward takes as s; sum_out may be x or residual itself.  stats=False keeps no mean and rstd."""
@@ -472,11 +449,6 @@ class AdamWPlan:
         _check(lib().ff_adamw_plan(C.byref(desc), table, host.ctypes.data, n))
         self.plan = torch.from_numpy(host).to(device)
         self.norm_ws = _alloc_ws(lib().ff_grad_norm_workspace_bytes(), device)
-        self.address, self.bytes, self.desc_address = self.plan.data_ptr(), n, C.addressof(desc)
-
-    @property
-    def ref(self):
-        return C.byref(self.desc)
 
 
 def _make_plan(state_bits, columns, weight_decay):
@@ -505,7 +477,10 @@ def _make_plan(state_bits, columns, weight_decay):
             for t, n, w in zip(ts, got, want):
                 if n != w:
                     raise ValueError(f"{name} has {n} values, not {w}")
-                _fit(t, name, dtype, t.shape, device)
+                if not t.is_cuda or t.device != device:
+                    raise ValueError(f"{name} is on {t.device}, not on {device if device.type == 'cuda' else 'a GPU'}")
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} is not contiguous")
         table[name] = list(map(torch.Tensor.data_ptr, ts))
     table["numel"] = numels
     table["weight_decay"] = weight_decay
@@ -551,29 +526,18 @@ def adamw_states(params, bits: int = 32):
 
 def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
     """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another."""
-    return _done(calls().grad_norm(plan.desc_address, plan.plan, out, plan.norm_ws if ws is None else ws))
+    return _done(calls().grad_norm(C.addressof(plan.desc), plan.plan, out, plan.norm_ws if ws is None else ws))
 
 
 def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: int = 0):
     """One AdamW step over the plan's tensors, in place.  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm
     that is not finite leaves everything as it was.  seed: of the rounding of 8-bit states, another for each step."""
-    import torch
-    if (norm is None) != (max_norm is None):
-        raise ValueError("norm and max_norm are given together")
-    if norm is not None:
-        _fit(norm, "norm", torch.float32, (1,), plan.device)
-    hyper = AdamWHyper(lr, betas[0], betas[1], eps, 0.0 if max_norm is None else max_norm, step, seed & 0xFFFFFFFF)
-    _check(lib().ff_adamw_step(plan.ref, plan.address, plan.bytes, C.byref(hyper), _ptr(norm), _stream_of(plan.device)))
+    _done(calls().adamw_step(C.addressof(plan.desc), plan.plan, step, lr, betas[0], betas[1], eps, norm, max_norm, seed))
 
 
 def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
     """(m, v) of all tensors of the plan, one after another, as float32."""
-    import torch
-    device, shape = plan.device, (plan.values,)
-    m = torch.empty(shape, dtype=torch.float32, device=device) if m is None else _fit(m, "m", torch.float32, shape, device)
-    v = torch.empty(shape, dtype=torch.float32, device=device) if v is None else _fit(v, "v", torch.float32, shape, device)
-    _check(lib().ff_adamw_moments(plan.ref, plan.address, plan.bytes, m.data_ptr(), v.data_ptr(), _stream_of(device)))
-    return m, v
+    return _done(calls().adamw_moments(C.addressof(plan.desc), plan.plan, plan.values, m, v))
 
 
 def ff_profile_enable(on: bool):

@@ -1,4 +1,4 @@
-// _calls: the entry points of the layer norm and of the gradient norm for torch tensors, as a CPython module beside libff.so.
+// _calls: the training operators' entry points for torch tensors, as a CPython module beside libff.so.
 //
 // The kernels of a small call take 3 us, a ctypes call that allocates its results from Python 12 to 15.  Here the checks, the allocations and the C call
 // are one step, which takes 6 to 8, with the interpreter lock let go.  The functions take every argument by place (binding.py holds the
@@ -175,9 +175,61 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// address of the plan's ff_adamw_desc, the plan, step, lr, beta1, beta2, eps, norm, max_norm, seed -> status
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("adamw_step", 10, n, [&]() -> PyObject* {
+        const auto* desc = (const ff_adamw_desc*)PyLong_AsVoidPtr(a[0]);
+        if (PyErr_Occurred()) return nullptr;
+        const at::Tensor plan = tensor(a[1], "plan"), norm = optional(a[7], "norm");
+        if (norm.defined() != (a[8] != Py_None)) value_error("norm and max_norm are given together");
+        const at::Device device = plan.device();
+        fit_optional(norm, "norm", at::kFloat, {1}, device);
+        ff_adamw_hyper h;
+        h.step = PyLong_AsLongLong(a[2]);
+        h.lr = PyFloat_AsDouble(a[3]);
+        h.beta1 = PyFloat_AsDouble(a[4]);
+        h.beta2 = PyFloat_AsDouble(a[5]);
+        h.eps = PyFloat_AsDouble(a[6]);
+        h.max_norm = norm.defined() ? PyFloat_AsDouble(a[8]) : 0.;
+        h.seed = (uint32_t)PyLong_AsUnsignedLongLongMask(a[9]);
+        if (PyErr_Occurred()) return nullptr;
+        ff_status status;
+        {
+            Unlocked unlocked;
+            const c10::DeviceGuard guard(device);
+            status = ff_adamw_step(desc, in(plan), plan.nbytes(), &h, (const float*)in(norm), c10::hip::getCurrentHIPStream(device.index()).stream());
+        }
+        return PyLong_FromLong(status);
+    });
+}
+
+// address of the plan's ff_adamw_desc, the plan, its values, m, v -> (m, v)
+PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("adamw_moments", 5, n, [&]() -> PyObject* {
+        const auto* desc = (const ff_adamw_desc*)PyLong_AsVoidPtr(a[0]);
+        if (PyErr_Occurred()) return nullptr;
+        const int64_t values = PyLong_AsLongLong(a[2]);
+        if (PyErr_Occurred()) return nullptr;
+        const at::Tensor plan = tensor(a[1], "plan");
+        at::Tensor m = optional(a[3], "m"), v = optional(a[4], "v");
+        const at::Device device = plan.device();
+        ff_status status;
+        {
+            Unlocked unlocked;
+            const c10::DeviceGuard guard(device);
+            result(m, "m", at::kFloat, {values}, device);
+            result(v, "v", at::kFloat, {values}, device);
+            status = ff_adamw_moments(desc, in(plan), plan.nbytes(), out<float>(m), out<float>(v), c10::hip::getCurrentHIPStream(device.index()).stream());
+        }
+        return status == FF_OK ? tuple_of(m, v) : PyLong_FromLong(status);
+    });
+}
+
 PyMethodDef kMethods[] = {{"layernorm_forward", (PyCFunction)(void (*)(void))layernorm_forward, METH_FASTCALL, nullptr},
                           {"layernorm_backward", (PyCFunction)(void (*)(void))layernorm_backward, METH_FASTCALL, nullptr},
                           {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
+                          {"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, nullptr},
+                          {"adamw_moments", (PyCFunction)(void (*)(void))adamw_moments, METH_FASTCALL, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, kMethods};
 

@@ -203,3 +203,19 @@ def test_more_pieces_than_blocks_are_refused():
     t["numel"] += 1
     assert plan_bytes(d, t) == 0 and "pieces" in P.last_error()
     assert P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, 0x1000, n + 80) == B.FF_EUNSUPPORTED
+
+
+def test_calls_refuse_what_is_no_tensor_or_number():
+    import torch
+    x, g = torch.zeros(4, 8), torch.ones(8)
+    for args in ((1, g, g), (x, None, g), (x, g, "beta"), (x, g, g, 3)):
+        with pytest.raises(TypeError):
+            P.ff_layernorm_forward(*args)
+    with pytest.raises(TypeError):
+        P.ff_layernorm_forward(x, g, g, eps="small")
+    with pytest.raises(ValueError):
+        P.ff_layernorm_forward(torch.zeros(()), g, g)
+    with pytest.raises(ValueError):
+        P.ff_layernorm_backward(x.to("meta"), g, x)
+    with pytest.raises(TypeError):
+        P.calls().grad_norm(0)
