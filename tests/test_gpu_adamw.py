@@ -124,6 +124,25 @@ def test_steps(param, grad, bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad", [("f32", "bf16"), ("bf16", "f32"), ("master", "bf16")])
+def test_every_kind_of_end(param, grad, bits):
+    """A wavefront takes 512 values, a lane four: tensors that end anywhere among them, a value apart from each other."""
+    sizes = [*range(1, 14), *range(253, 262), *range(507, 519), *range(765, 772), *range(2043, 2054), 2560, 2561]
+    model = Model(sizes, param, grad, bits, seed=5, gap=1)
+    around = {k: v.clone() for k, v in model.flat.items() if v is not None}
+    before = model.host()
+    P.ff_adamw_step(model.plan, 3, seed=9, **HYPER)
+    after = check_step(model, before, 3, seed=9)
+    m, v = P.ff_adamw_moments(model.plan)
+    assert np.array_equal(m.cpu().numpy(), np.concatenate(after["m32"])) and np.array_equal(v.cpu().numpy(), np.concatenate(after["v32"]))
+    for k, was in around.items():
+        at = 0
+        for n in sizes + [0]:
+            assert torch.equal(model.flat[k][at], was[at]), k
+            at += 1 + n
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("max_norm", [0.1, 1e6])
 def test_clipped_steps(bits, max_norm):
     model = Model([300, 5000, 17], "f32", "f32", bits, seed=2, gap=3)
@@ -136,6 +155,24 @@ def test_clipped_steps(bits, max_norm):
         n32 = np.float32(want)
         k = min(np.float32(1), np.float32(max_norm) / (n32 + np.float32(1e-6)))
         check_step(model, before, step, k=float(k), seed=step)
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("pieces", [1, 15, 16, 17, 32, 33])
+@pytest.mark.parametrize("longest", [7, 300, 2048])
+def test_norm_of_few_pieces(longest, pieces, grad):
+    """One block up to 32 pieces, several above; the values between the tensors are too large to be missed."""
+    gen = torch.Generator(DEV).manual_seed(longest + pieces)
+    sizes = [longest - i % 7 for i in range(pieces)]
+    flat = torch.randn(sum(sizes) + pieces + 1, generator=gen, device=DEV).to(torch.float32 if grad == "f32" else torch.bfloat16)
+    parts, at = [], 0
+    for n in sizes:
+        flat[at] = 1e30
+        parts.append(flat[at + 1:at + 1 + n])
+        at += n + 1
+    flat[at] = 1e30
+    want = torch.cat(parts).double().square().sum().sqrt().item()
+    assert abs(P.ff_grad_norm(P.make_grad_plan(parts)).item() - want) <= U * want * (1 + 1e-6)
 
 
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
