@@ -361,7 +361,8 @@ typedef struct {
  * tensors come to 2^24 pieces or more (FF_EUNSUPPORTED in ff_adamw_plan): one for each 2048 values of a tensor, at least one. */
 size_t ff_adamw_plan_bytes(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors);
 
-/* Writes the plan into host memory (plan_bytes as reported above).  Tensors of one plan must not overlap. */
+/* Writes the plan into host memory (plan_bytes as reported above).  Gradients may share memory; a tensor that the step writes
+ * and that overlaps another one is refused (FF_EINVAL). */
 ff_status ff_adamw_plan(const ff_adamw_desc* desc, const ff_adamw_tensor* tensors, void* plan, size_t plan_bytes);
 
 /* Bytes of device workspace ff_grad_norm needs. */

@@ -483,6 +483,8 @@ def _make_plan(state_bits, columns, weight_decay):
                     raise ValueError(f"{name} is not contiguous")
         table[name] = list(map(torch.Tensor.data_ptr, ts))
     table["numel"] = numels
+    if np.ndim(weight_decay) and len(weight_decay) != count:
+        raise ValueError(f"{len(weight_decay)} values of weight_decay for {count} gradients")
     table["weight_decay"] = weight_decay
     desc = AdamWDesc(_dtype_code(columns["p"][0][0]) if "p" in columns else FF_F32, _dtype_code(grads[0]), state_bits, count)
     return AdamWPlan(desc, table.ctypes.data, (table, columns), sum(numels), device)

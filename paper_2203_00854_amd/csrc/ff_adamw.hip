@@ -4,7 +4,9 @@
 // one record each with everything a block needs (addresses, length, decay): a block reads one record and works on one piece, so
 // that small tensors cost a block and large ones as many as they have pieces.
 #include <math.h>
+#include <stdlib.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "ff_common.h"
@@ -87,6 +89,48 @@ void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* ts, void* pl
     }
     head->pieces = out - ((Piece*)plan + 1);
     head->values = value;
+}
+
+// Whether a tensor that the step writes shares memory with another one (tied weights listed twice, say): their blocks would race.
+// -1 if there is no host memory to find out.
+int adamw_overlaps(const ff_adamw_desc& d, const ff_adamw_tensor* ts) {
+    struct Span {
+        uintptr_t from, to;
+        bool written;
+    };
+    if (d.state_bits == 0 || d.n_tensors == 0) return 0;
+    Span* spans = (Span*)malloc(sizeof(Span) * 7 * (size_t)d.n_tensors);
+    if (!spans) return -1;
+    const int64_t ps = d.param_dtype == FF_F32 ? 4 : 2, gs = d.grad_dtype == FF_F32 ? 4 : 2, ss = d.state_bits == 32 ? 4 : 1;
+    size_t n = 0;
+    const auto before = [](const Span& a, const Span& b) { return a.from < b.from; };
+    // one kind of tensor after the other: each is mostly in order already (3504 tensors 0.2 ms)
+    auto take = [&](bool written, auto from, auto bytes) {
+        Span* first = spans + n;
+        for (int i = 0; i < d.n_tensors; ++i)
+            if (from(ts[i]) && ts[i].numel) spans[n++] = Span{(uintptr_t)from(ts[i]), (uintptr_t)from(ts[i]) + (uintptr_t)bytes(ts[i]), written};
+        if (!std::is_sorted(first, spans + n, before)) std::sort(first, spans + n, before);
+        std::inplace_merge(spans, first, spans + n, before);
+    };
+    typedef const ff_adamw_tensor& Tensor;
+    const auto groups = [](Tensor t) { return (t.numel + kGroup - 1) / kGroup; };
+    const auto states = [=](Tensor t) { return t.numel * ss; };
+    take(true, [](Tensor t) { return t.p; }, [=](Tensor t) { return t.numel * ps; });
+    take(true, [](Tensor t) { return t.master; }, [](Tensor t) { return t.numel * 4; });
+    take(true, [](Tensor t) { return t.m; }, states);
+    take(true, [](Tensor t) { return t.v; }, states);
+    take(true, [](Tensor t) { return t.m_exp; }, groups);
+    take(true, [](Tensor t) { return t.v_exp; }, groups);
+    take(false, [](Tensor t) { return t.g; }, [=](Tensor t) { return t.numel * gs; });
+    uintptr_t end = 0, end_written = 0;
+    int found = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (spans[i].from < (spans[i].written ? end : end_written)) found = 1;
+        if (spans[i].to > end) end = spans[i].to;
+        if (spans[i].written && spans[i].to > end_written) end_written = spans[i].to;
+    }
+    free(spans);
+    return found;
 }
 
 // ---- four neighbours ---------------------------------------------------------------------

@@ -517,6 +517,9 @@ ff_status ff_adamw_plan(const ff_adamw_desc* desc, const ff_adamw_tensor* tensor
     if (!adamw_plan_whole(need)) return fail(FF_EUNSUPPORTED, "the tensors need more pieces than one launch has blocks");
     if (!plan || !aligned_to(plan, 8)) return fail(FF_EINVAL, "plan is NULL or misaligned");
     if (plan_bytes != need) return fail(FF_EWORKSPACE, "the plan has %zu bytes, %zu given", need, plan_bytes);
+    const int overlaps = adamw_overlaps(*desc, tensors);
+    if (overlaps < 0) return fail(FF_EINVAL, "no host memory for %d tensors", desc->n_tensors);
+    if (overlaps) return fail(FF_EINVAL, "a tensor that the step writes overlaps another one of the plan");
     adamw_plan_fill(*desc, tensors, plan);
     return FF_OK;
 }

@@ -177,6 +177,7 @@ ff_status layernorm_backward_run(const ff_norm_desc& d, const void* s, const voi
 // AdamW over many tensors (ff_adamw.hip); plan: device memory
 size_t adamw_plan_size(const ff_adamw_desc& d, const ff_adamw_tensor* tensors);
 void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* tensors, void* plan);
+int adamw_overlaps(const ff_adamw_desc& d, const ff_adamw_tensor* tensors);
 // whether a plan can have this many bytes
 bool adamw_plan_whole(size_t bytes);
 size_t grad_norm_workspace();

@@ -219,3 +219,33 @@ def test_calls_refuse_what_is_no_tensor_or_number():
         P.ff_layernorm_backward(x.to("meta"), g, x)
     with pytest.raises(TypeError):
         P.calls().grad_norm(0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_plan_refuses_tensors_that_overlap(bits):
+    """A weight listed twice would be stepped by two blocks at a time; gradients are only read."""
+    d = B.AdamWDesc(P.FF_BF16, P.FF_F32, bits, 3)
+    size = dict(p=2, master=4, m=bits // 8, v=bits // 8, g=4)
+    kinds = [*size] + (["m_exp", "v_exp"] if bits == 8 else [])
+    space = {k: 0x1000000 * (j + 1) for j, k in enumerate(kinds)}
+    clean = lambda: [{**GOOD, **{k: at + 0x40000 * i for k, at in space.items()}} for i in range(3)]  # noqa: E731
+
+    def status(rows):
+        t = tensors(*rows)
+        n = plan_bytes(d, t)
+        return P.lib().ff_adamw_plan(C.byref(d), t.ctypes.data, np.zeros(n, np.uint8).ctypes.data, n)
+
+    assert status(clean()) == B.FF_OK
+    rows = clean()
+    rows[2]["g"] = rows[0]["g"] + 8
+    assert status(rows) == B.FF_OK
+    for a in kinds:
+        for b in kinds:
+            if a == b == "g":
+                continue
+            length = {k: 5000 * s for k, s in size.items()}.get(b, 20)
+            rows = clean()
+            rows[2][a] = rows[1][b] + length - 4             # the last four bytes of another
+            assert status(rows) == B.FF_EINVAL, (a, b)
+            rows[2][a] = rows[1][b] + length                 # right behind it
+            assert status(rows) == B.FF_OK, (a, b)
