@@ -235,7 +235,8 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
 // in registers or blocks, took longer (662), and each block more makes the second launch longer.
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
 // over its teams and wavefronts in a fixed order and leaves 2 c partial sums; with one block in all these are the result.
-template <typename T, int V, int ITERS, bool MASKED, bool WIDE, bool STREAMED>
+// AHEAD: the next row is on its way while this one is worked on.
+template <typename T, int V, int ITERS, bool MASKED, bool WIDE, bool STREAMED, bool AHEAD>
 __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) void k_ln_backward(
     const T* __restrict__ s, const T* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in, const T* dy,
     const T* dsum, T* dx, float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta, bool accumulate, int64_t rows,
@@ -252,9 +253,6 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
     const float inv_c = 1.f / (float)c;
     const int per_block = WIDE ? 1 : (int)blockDim.x / lanes;
     const int64_t stride = (int64_t)gridDim.x * per_block;
-    // the next row on its way while this one is worked on: 5120 x 384 x 64 with saved statistics 145 -> 140 us, 196608 x 256 with dsum 71 -> 68,
-    // but 2048 x 2048 x 128 574 -> 611
-    constexpr bool AHEAD = STREAMED && !WIDE && V * ITERS <= 8;
     int64_t row = (int64_t)blockIdx.x * per_block + (WIDE ? 0 : threadIdx.x / lanes);
     Pc pu[ITERS], pd[ITERS], ps[ITERS];
     [[maybe_unused]] Pc nu[ITERS], nd[ITERS], ns[ITERS];
@@ -534,17 +532,32 @@ size_t layernorm_backward_workspace(const ff_norm_desc& d) {
     return n < 256 ? 256 : (n + 255) & ~(size_t)255;
 }
 
+// Whether a lane of the backward pass asks for its next row ahead.  Streamed inputs always (up to eight values a lane: 5120 x 384 x 64 with saved
+// statistics 145 -> 140 us, 196608 x 256 with dsum 71 -> 68).  Of those that may lie in the caches the bfloat16 ones with saved statistics, whose turns
+// are the shortest (128 x 256 x 256 14.6 -> 13.7, with dsum 17.2 -> 15.8, 65536 x 384 32.6 -> 29.4; formed again 14.4 -> 15.0 and 33.8 -> 36.1, float32 65536 x 384
+// 51.6 -> 52.5).  Of the largest the float32 ones (2^20 x 128 300 -> 289, 2048 x 2048 x 128 1230 -> 1186; bfloat16 571 -> 611).
+static bool asks_ahead(const Shape& s, int size, bool saved, int64_t input_bytes) {
+    return size == 2 ? saved && input_bytes < 1000000000 : s.iters * s.v <= 8 && input_bytes >= 1000000000;
+}
+
 template <typename T>
 static void backward_t(const ff_norm_desc& d, const Shape& s, int blocks, const void* src, const void* gamma, const float* mean, const float* rstd, const void* dy,
                        const void* dsum, void* dx, float* dgamma, float* dbeta, bool accumulate, float* partial, hipStream_t stream) {
-    with_shape(s, d.rows * d.c * (int64_t)sizeof(T) * (dsum ? 3 : 2), [&](auto v, auto iters, auto masked, auto wide, auto streamed) {
+    const int64_t input_bytes = d.rows * d.c * (int64_t)sizeof(T) * (dsum ? 3 : 2);
+    with_shape(s, input_bytes, [&](auto v, auto iters, auto masked, auto wide, auto streamed) {
         constexpr int V = decltype(v)::value, I = decltype(iters)::value;
         constexpr bool R = decltype(masked)::value, W = decltype(wide)::value, S = decltype(streamed)::value;
         if constexpr (V != (sizeof(T) == 4 ? 8 : 4)) {
             const size_t lds = W ? 4 * kWideThreads / 64 * sizeof(float) : (size_t)backward_threads(I * V) / 64 * 2 * I * V * s.lanes * sizeof(float);     // at most 64 KiB
-            hipLaunchKernelGGL((k_ln_backward<T, V, I, R, W, S>), dim3(blocks), dim3(W ? s.lanes : backward_threads(I * V)), lds, stream, (const T*)src,
-                               (const T*)gamma, mean, rstd, (const T*)dy, (const T*)dsum, (T*)dx, partial, dgamma, dbeta, accumulate, d.rows, d.c,
-                               s.lanes, d.ln_eps);
+            auto launch = [&](auto ahead) {
+                constexpr bool A = decltype(ahead)::value;
+                hipLaunchKernelGGL((k_ln_backward<T, V, I, R, W, S, A>), dim3(blocks), dim3(W ? s.lanes : backward_threads(I * V)), lds, stream, (const T*)src,
+                                   (const T*)gamma, mean, rstd, (const T*)dy, (const T*)dsum, (T*)dx, partial, dgamma, dbeta, accumulate, d.rows, d.c,
+                                   s.lanes, d.ln_eps);
+            };
+            if constexpr (W || S) launch(std::integral_constant<bool, !W && I * V <= 8>{});
+            else if (asks_ahead(s, sizeof(T), mean, input_bytes)) launch(std::true_type{});
+            else launch(std::false_type{});
         }
     });
 }

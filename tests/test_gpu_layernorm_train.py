@@ -371,3 +371,33 @@ def test_inputs_beyond_the_caches(dtype, rows, c):
         args = dict(dy=over, dsum=d["dsum"]) if saved else dict(dy=d["dy"], dsum=over)
         again = P.ff_layernorm_backward(s, d["gamma"], eps=EPS, dx=over, **args, **kw)
         assert torch.equal(again[0], dx) and torch.equal(again[1], dgamma) and torch.equal(again[2], dbeta)
+
+
+@pytest.mark.parametrize("dtype,rows,c", [("bf16", 60_001, 128), ("bf16", 40_000, 173), ("bf16", 90_011, 24), ("bf16", 12_003, 1000), ("bf16", 70_001, 3),
+                                          ("f32", 1_050_001, 128), ("f32", 1_050_001, 125)])
+def test_backward_with_the_next_row_on_its_way(dtype, rows, c):
+    """Many turns of rows a block with saved statistics: rows from all over the tensor against the oracle, sums over all rows in float64, in place as well."""
+    gen = torch.Generator(DEV).manual_seed(c + 1)
+    randn = lambda *s: torch.randn(*s, generator=gen, device=DEV).to(DT[dtype])  # noqa: E731
+    d = {"x": randn(rows, c), "dy": randn(rows, c), "dsum": randn(rows, c), "gamma": randn(c), "beta": randn(c)}
+    size = 2 * d["x"].numel() * d["x"].element_size()
+    assert size < 160e6 if dtype == "bf16" else size > 1e9
+    some = torch.cat([torch.arange(40), torch.arange(0, rows, 997), torch.arange(rows - 40, rows)]).to(DEV)
+    part = {k: (v[some] if v.dim() == 2 else v).cpu() for k, v in d.items()}
+    x, gamma, dy = d["x"], d["gamma"], d["dy"]
+    _, _, mean, rstd = P.ff_layernorm_forward(x, gamma, d["beta"], eps=EPS)
+    terms = dy.double() * ((x.double() - mean.double()[:, None]) * rstd.double()[:, None])
+    # at most 1200 additions, and the terms' own error: what mean and rstd are off by (test's head) and two operations
+    off = (1200 + 80) * U * terms.abs().sum(0) + (dy.double().abs() * (45 * U * x.double().abs().mean(1) * rstd.double())[:, None]).sum(0)
+    want, off_b = terms.sum(0), 1200 * U * dy.double().abs().sum(0)
+    del terms
+    for dsum in (None, d["dsum"]):
+        kw = dict(mean=mean, rstd=rstd, dsum=dsum, eps=EPS)
+        dx, dgamma, dbeta = P.ff_layernorm_backward(x, gamma, dy, **kw)
+        assert ((dgamma.double() - want).abs() <= off).all()
+        assert ((dbeta.double() - dy.double().sum(0)).abs() <= off_b).all()
+        small = P.ff_layernorm_backward(x[some], gamma, dy[some], mean=mean[some], rstd=rstd[some], dsum=None if dsum is None else dsum[some], eps=EPS)
+        check_backward(part["x"], part, dtype, (dx[some], small[1], small[2]), dsum is not None)
+        over = dy.clone()
+        again = P.ff_layernorm_backward(x, gamma, over, dx=over, **kw)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dgamma) and torch.equal(again[2], dbeta)
