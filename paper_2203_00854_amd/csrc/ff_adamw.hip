@@ -286,12 +286,15 @@ template <int TOP> struct Scale {
 // Squares and sums in float64: no square leaves its range, and the order of the sums does not show in the float32 result.  Bound by HBM and two
 // dependent launches: 49.1 M bfloat16 values 21 us (4.7 TB/s) and 4 for the join.  As many blocks as the card holds, each
 // with the next record on its way: blocks of neighbouring pieces, two or four pieces at a time, took 27 to 32 for both.
-__device__ __forceinline__ double block_sum(double x) {
-    __shared__ double part[4];
+template <int WAVES> __device__ __forceinline__ double block_sum(double x) {
+    __shared__ double part[WAVES];
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    return part[0] + part[1] + part[2] + part[3];
+    x = part[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) x += part[w];
+    return x;
 }
 
 template <typename G>
@@ -322,14 +325,16 @@ __global__ __launch_bounds__(256) void k_grad_norm(const Piece* __restrict__ pie
         g = g_next;
         n = n_next;
     }
-    sum = block_sum(sum);
+    sum = block_sum<4>(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(256) void k_norm_join(const double* __restrict__ partial, int n, float* __restrict__ norm) {
+__global__ __launch_bounds__(1024) void k_norm_join(const double* __restrict__ partial, int n, float* __restrict__ norm) {
     double sum = 0.;
-    for (int i = threadIdx.x; i < n; i += 256) sum += partial[i];
-    sum = block_sum(sum);
+#pragma unroll
+    for (int i = 0; i < kNormBlocks; i += 1024)
+        if (i + (int)threadIdx.x < n) sum += partial[i + threadIdx.x];
+    sum = block_sum<16>(sum);
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
@@ -338,7 +343,6 @@ __global__ __launch_bounds__(256) void k_norm_join(const double* __restrict__ pa
 constexpr int kFewPieces = 32;
 template <typename G>
 __global__ __launch_bounds__(1024) void k_norm_few(const Piece* __restrict__ pieces, int n_pieces, uint32_t tag, float* __restrict__ norm) {
-    __shared__ double part[16];
     const int lane = threadIdx.x & 63;
     double sum = 0.;
     for (int i = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < n_pieces; i += 16) {
@@ -360,14 +364,8 @@ __global__ __launch_bounds__(1024) void k_norm_few(const Piece* __restrict__ pie
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum += (double)v[t][j] * (double)v[t][j];
     }
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (lane == 0) part[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    sum = 0.;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) sum += part[w];
-    *norm = (float)sqrt(sum);
+    sum = block_sum<16>(sum);
+    if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
 size_t grad_norm_workspace() { return kNormBlocks * sizeof(double); }
@@ -387,7 +385,7 @@ ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_by
         if (d.grad_dtype == FF_F32) hipLaunchKernelGGL((k_grad_norm<float>), dim3(blocks), dim3(256), 0, stream, pieces, n, tag_of(d), partial);
         else hipLaunchKernelGGL((k_grad_norm<bf16_t>), dim3(blocks), dim3(256), 0, stream, pieces, n, tag_of(d), partial);
     }
-    hipLaunchKernelGGL(k_norm_join, dim3(1), dim3(256), 0, stream, partial, blocks, norm);
+    hipLaunchKernelGGL(k_norm_join, dim3(1), dim3(1024), 0, stream, partial, blocks, norm);
     return check_launch("ff_grad_norm");
 }
 
