@@ -284,7 +284,7 @@ template <int TOP> struct Scale {
 
 // ---- norm of all gradients ---------------------------------------------------------------
 // Squares and sums in float64: no square leaves its range, and the order of the sums does not show in the float32 result.  Bound by HBM and two
-// dependent launches: 49.1 M bfloat16 values 21 us (4.7 TB/s) and 4 for the join.  As many blocks as the card holds, each
+// dependent launches: 49.1 M bfloat16 values 19 us (5.2 TB/s) and 4 for the join, whose loads are all under way at once.  As many blocks as the card holds, each
 // with the next record on its way: blocks of neighbouring pieces, two or four pieces at a time, took 27 to 32 for both.
 template <int WAVES> __device__ __forceinline__ double block_sum(double x) {
     __shared__ double part[WAVES];
@@ -398,8 +398,8 @@ __device__ __forceinline__ float root_of(float v) {
 }
 
 // Bound by HBM: with 32-bit states 28 bytes a value, with 8 bits 10 to 16 and 63 vector instructions a value, which take about as long where
-// the tensors are bfloat16.  48 Evoformer blocks (49.1 M values): 221 us with master copies (6.2 TB/s), 114 with float32 weights
-// and 8-bit states (6.0 TB/s).
+// the tensors are bfloat16.  48 Evoformer blocks (49.1 M values): 215 us with master copies (6.4 TB/s), 110 with float32 weights
+// and 8-bit states (6.2 TB/s).
 template <typename P, typename G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces, uint32_t tag, StepArgs a, const float* __restrict__ norm) {
     const Piece& pc = pieces[blockIdx.x];

@@ -154,7 +154,7 @@ template <int V, int ITERS, bool MASKED> struct Held {
 };
 
 // Two sums over a team, the second of squared distances from the mean that the first gives (in registers: no second reading, no cancellation).
-// 128 x 256 x 256 bfloat16 with the residual sum 12.7 us, 2048 x 2048 x 128 371 us (5.8 TB/s).
+// 128 x 256 x 256 bfloat16 with the residual sum 12.4 us, 2048 x 2048 x 128 373 us (5.8 TB/s).
 template <typename T, int V, int ITERS, bool MASKED, bool WIDE, bool STREAMED>
 __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_forward(
     const T* x, const T* residual, const T* __restrict__ gamma, const T* __restrict__ beta, T* sum, T* __restrict__ y,
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
 }
 
 // Bytes bound it: 2048 x 2048 x 128 bfloat16 in 574 us (5.6 TB/s), 612 where the statistics are formed again (four sums over a team one after
-// the other, not two); 5120 x 384 x 64 in 125 to 133 (5.7 to 6.0 TB/s).  Sixteen wavefronts on a compute unit carry that: twice as many,
+// the other, not two); 5120 x 384 x 64 in 128 to 135 (5.6 to 5.9 TB/s), 128 x 256 x 256 with dsum in 14.6.  Sixteen wavefronts on a compute unit carry that: twice as many,
 // in registers or blocks, took longer (662), and each block more makes the second launch longer.
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
 // over its teams and wavefronts in a fixed order and leaves 2 c partial sums; with one block in all these are the result.
