@@ -531,10 +531,11 @@ def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
     return _done(calls().grad_norm(C.addressof(plan.desc), plan.plan, out, plan.norm_ws if ws is None else ws))
 
 
-def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: int = 0):
+def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: Optional[int] = None):
     """One AdamW step over the plan's tensors, in place.  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm
-    that is not finite leaves everything as it was.  seed: of the rounding of 8-bit states, another for each step."""
-    _done(calls().adamw_step(C.addressof(plan.desc), plan.plan, step, lr, betas[0], betas[1], eps, norm, max_norm, seed))
+    that is not finite leaves everything as it was.  seed: of the rounding of 8-bit states, another for each step (None: the step's number).  With
+    one seed for all steps a value would be rounded the same way every time, and its moments would drift."""
+    _done(calls().adamw_step(C.addressof(plan.desc), plan.plan, step, lr, betas[0], betas[1], eps, norm, max_norm, step if seed is None else seed))
 
 
 def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
