@@ -319,7 +319,8 @@ ff_status ff_layernorm_backward(const ff_norm_desc* desc, const void* s, const v
  * given, k = min(1, max_norm / (norm + 1e-6)):
  *   g' = k g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in float32, each operation of m and v rounded by itself (in w a v below 2^-126 counts as 2^-126).  w is the float32 parameter; or the float32 master copy of a
+ * in float32, each operation of m and v rounded by itself (in w a v below 2^-126 counts as 2^-126, and the decay lr weight_decay w joins the
+ * step before either meets w, so that small decays count too).  w is the float32 parameter; or the float32 master copy of a
  * bfloat16 parameter, which receives its rounding; or the bfloat16 parameter itself.
  *
  * state_bits = 32: m and v are float32.  state_bits = 8: a byte for each, and for each 256 values of a tensor (from

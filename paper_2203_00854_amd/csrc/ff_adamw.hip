@@ -412,7 +412,7 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
     }
     if (pc.tag != tag) return;
     const int lane = threadIdx.x & 31;
-    const float keep = 1.f - a.lr * pc.decay;
+    const float decay = a.lr * pc.decay;
     const bool master = pc.master != nullptr;
     const uintptr_t states = BITS == 32 ? (uintptr_t)pc.m | (uintptr_t)pc.v : 0;
     const bool streamed = (((uintptr_t)pc.p | (uintptr_t)pc.g | (uintptr_t)pc.master | states) & 15u) == 0;
@@ -461,7 +461,8 @@ __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces,
                 m[h][i] = a.beta1 * m[h][i] + a.rest1 * x;
                 v[h][i] = a.beta2 * v[h][i] + a.rest2 * (x * x);
                 const float root = root_of(v[h][i]) * a.inv_root + a.eps;
-                w[h][i] = w[h][i] * keep - a.step_size * (m[h][i] * __builtin_amdgcn_rcpf(root));
+                // (the decay's share and the step's meet before the one rounding against the weight: 1 - decay next to 1 loses a fifth of a decay of 1e-7)
+                w[h][i] -= decay * w[h][i] + a.step_size * (m[h][i] * __builtin_amdgcn_rcpf(root));
             }
             const int at = base + h * 128 + lane * 4;
             if (master) store4<H, float>(pc.master, at, pc.n, w[h]);

@@ -395,3 +395,35 @@ def test_refused_tensors():
             P.ff_adamw_step(plan, **{**dict(step=1, lr=1e-3), **kw})
     with pytest.raises(P.FFError):
         P.ff_adamw_step(P.make_grad_plan([half]), 1, lr=1e-3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param", ["f32", "master"])
+@pytest.mark.parametrize("lr", [1e-5, 1e-6])
+def test_small_decays_count_in_the_mean(lr, param, bits):
+    """lr times decay of 1e-7 and 1e-8, whose distance from 1 a float32 hardly holds.  A weight is rounded once, by at most half a step 2^-24 either way as the
+    updates of tens of steps happen to fall, so the mean over 2^18 weights between 1 and 2 is off by six of its deviations at most, beside the relative
+    roundings of the decay and of the update."""
+    n, decay, betas, eps, step = 1 << 18, 0.01, (0.9, 0.999), 1e-8, 1000
+    gen = torch.Generator(DEV).manual_seed(13)
+    w = 1.1 + 0.8 * torch.rand(n, generator=gen, device=DEV)
+    master, p = ([w.clone()], [w.to(torch.bfloat16)]) if param == "master" else (None, [w.clone()])
+    rng = np.random.default_rng(13)
+    m, v = rng.normal(size=n).astype(np.float32), np.ones(n, np.float32)
+    if bits == 32:
+        states = {"m": [torch.from_numpy(m).to(DEV)], "v": [torch.from_numpy(v).to(DEV)]}
+    else:
+        states = {}
+        for k, x, top in (("m", m, A.TOP_M), ("v", v, A.TOP_V)):
+            code, exp = A.encode(x, top, rng.integers(0, 1 << 16, n))
+            states[k], states[k + "_exp"] = [torch.from_numpy(code).to(DEV)], [torch.from_numpy(exp).to(DEV)]
+    plan = P.make_adamw_plan(p, [torch.zeros(n, device=DEV)], master=master, weight_decay=decay, **states)
+    m, v = (x.cpu().numpy() for x in P.ff_adamw_moments(plan))
+    P.ff_adamw_step(plan, step, lr=lr, betas=betas, eps=eps)
+    w0 = w.double().cpu().numpy()
+    want = A.step(w0, np.zeros(n), m, v, lr, *betas, eps, float(np.float32(decay)), step)[0]
+    off = (master or p)[0].double().cpu().numpy() - want
+    share = lr * decay * w0
+    bound = 6 * U / np.sqrt(n) + 40 * U * (share.mean() + np.abs(want - w0 + share).mean())
+    print(f"mean off by {off.mean():.2e}, bound {bound:.2e}, decay {share.mean():.2e}", flush=True)
+    assert abs(off.mean()) <= bound
