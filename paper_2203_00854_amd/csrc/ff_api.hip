@@ -451,6 +451,8 @@ ff_status ff_layernorm_backward(const ff_norm_desc* desc, const void* s, const v
         return fail(FF_EINVAL, "dx overlaps gamma, mean or rstd");
     for (const void* t : {s, dy, dsum, (const void*)dx})
         if (t && ws && overlaps(ws, need, t, n)) return fail(FF_EINVAL, "the workspace overlaps a tensor");
+    if (ws && (overlaps(ws, need, gamma, wb) || (mean && (overlaps(ws, need, mean, rb) || overlaps(ws, need, rstd, rb)))))
+        return fail(FF_EINVAL, "the workspace overlaps gamma, mean or rstd");
     if (!ws) return fail(FF_EINVAL, "workspace is NULL (%zu bytes needed)", need);
     if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
     if (ws_bytes < need) return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", ws_bytes, need);

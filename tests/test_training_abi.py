@@ -249,3 +249,13 @@ def test_plan_refuses_tensors_that_overlap(bits):
             assert status(rows) == B.FF_EINVAL, (a, b)
             rows[2][a] = rows[1][b] + length                 # right behind it
             assert status(rows) == B.FF_OK, (a, b)
+
+
+def test_layernorm_workspace_apart_from_every_input():
+    """A block that ends early writes its partial sums while others still read gamma and the statistics."""
+    d, lib = norm_desc(rows=1000), P.lib()
+    need = P.ff_layernorm_backward_workspace_bytes(d)
+    bwd = lambda ws, g=G, m=MEAN, r=RSTD: lib.ff_layernorm_backward(C.byref(d), X, g, m, r, Y, None, S, R, BETA, 0, ws, need, None)  # noqa: E731
+    for kw in (dict(ws=G), dict(ws=MEAN), dict(ws=RSTD), dict(ws=WS, g=WS + need - 2), dict(ws=WS, m=WS + need - 4), dict(ws=WS, r=WS - 3996), dict(ws=WS, g=WS - 126)):
+        assert bwd(**kw) == B.FF_EINVAL, kw
+        assert "the workspace overlaps" in P.last_error()
