@@ -7,6 +7,7 @@ any entry point fails loudly - there is no CPU or PyTorch fallback.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes as C
 import os
 from typing import Dict, Optional
@@ -441,7 +442,7 @@ class AdamWPlan:
     def __init__(self, desc, table, tensors, values, device):
         import numpy as np
         import torch
-        self.desc, self.tensors, self.values, self.device = desc, tensors, values, device
+        self.desc, self.tensors, self.values, self.device, self.spans = desc, tensors, values, device, {}
         n = lib().ff_adamw_plan_bytes(C.byref(desc), table)
         if n == 0:
             raise FFError(FF_EINVAL, last_error())
@@ -449,6 +450,24 @@ class AdamWPlan:
         _check(lib().ff_adamw_plan(C.byref(desc), table, host.ctypes.data, n))
         self.plan = torch.from_numpy(host).to(device)
         self.norm_ws = _alloc_ws(lib().ff_grad_norm_workspace_bytes(), device)
+
+    def meets(self, kinds, t) -> bool:
+        """Whether t shares memory with one of the plan's tensors of these kinds (pointer names); what is no tensor does not."""
+        import numpy as np
+        import torch
+        if not isinstance(t, torch.Tensor):
+            return False
+        if kinds not in self.spans:
+            table, columns = self.tensors
+            numel = table["numel"]
+            # starts in order, and how far the tensors up to each of them reach
+            ends = [(table[k].astype(np.int64), (-(-numel // 256) if k.endswith("_exp") else numel) * columns[k][1].itemsize) for k in kinds if k in columns]
+            start, size = (np.concatenate([e[i][numel > 0] for e in ends] or [np.zeros(0, np.int64)]) for i in (0, 1))
+            order = np.argsort(start)
+            self.spans[kinds] = start[order].tolist(), np.maximum.accumulate((start + size)[order]).tolist()
+        start, reach = self.spans[kinds]
+        i = bisect.bisect_left(start, t.data_ptr() + t.nbytes)
+        return t.nbytes > 0 and i > 0 and reach[i - 1] > t.data_ptr()
 
 
 def _make_plan(state_bits, columns, weight_decay):
@@ -527,7 +546,11 @@ def adamw_states(params, bits: int = 32):
 
 
 def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
-    """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another."""
+    """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another.
+    out and ws must not share memory with a gradient."""
+    for name, t in (("out", out), ("ws", ws)):
+        if t is not None and plan.meets(("g",), t):
+            raise ValueError(f"{name} shares memory with a gradient of the plan")
     return _done(calls().grad_norm(C.addressof(plan.desc), plan.plan, out, plan.norm_ws if ws is None else ws))
 
 

@@ -537,6 +537,9 @@ ff_status ff_grad_norm(const ff_adamw_desc* desc, const void* plan, size_t plan_
     if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
     if (ws_bytes < grad_norm_workspace())
         return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", ws_bytes, grad_norm_workspace());
+    if (overlaps(norm, 4, ws, grad_norm_workspace())) return fail(FF_EINVAL, "norm overlaps the workspace");
+    if (overlaps(norm, 4, plan, plan_bytes) || overlaps(ws, grad_norm_workspace(), plan, plan_bytes))
+        return fail(FF_EINVAL, "norm or the workspace overlaps the plan");
     return grad_norm_run(*desc, plan, plan_bytes, norm, ws, (hipStream_t)hip_stream);
 }
 

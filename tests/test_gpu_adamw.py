@@ -427,3 +427,19 @@ def test_small_decays_count_in_the_mean(lr, param, bits):
     bound = 6 * U / np.sqrt(n) + 40 * U * (share.mean() + np.abs(want - w0 + share).mean())
     print(f"mean off by {off.mean():.2e}, bound {bound:.2e}, decay {share.mean():.2e}", flush=True)
     assert abs(off.mean()) <= bound
+
+
+def test_norm_refuses_memory_of_the_gradients():
+    flat, ws = torch.randn(9000, device=DEV), torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+    plan = P.make_grad_plan([flat[:4000], flat[5000:8000]])
+    want = P.ff_grad_norm(plan).item()
+    kept = flat.clone()
+    for kw in (dict(out=flat[3999:4000]), dict(out=flat[5000:5001]), dict(ws=flat), dict(ws=flat[64:])):
+        with pytest.raises(ValueError):
+            P.ff_grad_norm(plan, **kw)
+    assert torch.equal(flat, kept)
+    assert P.ff_grad_norm(plan, out=flat[4000:4001], ws=ws).item() == want and flat[4000].item() == want
+    with pytest.raises(P.FFError):
+        P.ff_grad_norm(plan, out=ws[:4].view(torch.float32), ws=ws)
+    with pytest.raises(P.FFError):
+        P.ff_grad_norm(plan, out=plan.plan[:4].view(torch.float32))

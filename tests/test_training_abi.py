@@ -259,3 +259,46 @@ def test_layernorm_workspace_apart_from_every_input():
     for kw in (dict(ws=G), dict(ws=MEAN), dict(ws=RSTD), dict(ws=WS, g=WS + need - 2), dict(ws=WS, m=WS + need - 4), dict(ws=WS, r=WS - 3996), dict(ws=WS, g=WS - 126)):
         assert bwd(**kw) == B.FF_EINVAL, kw
         assert "the workspace overlaps" in P.last_error()
+
+
+def test_norm_and_workspace_overlaps():
+    """Blocks write their partial sums while others still read the plan's addresses."""
+    lib, d = P.lib(), B.AdamWDesc(P.FF_F32, P.FF_F32, 32, 1)
+    n, need = plan_bytes(d, tensors(GOOD)), P.lib().ff_grad_norm_workspace_bytes()
+    norm = lambda out=Y, ws=WS: lib.ff_grad_norm(C.byref(d), X, n, out, ws, need, None)  # noqa: E731
+    for kw in (dict(out=X), dict(out=X + n - 4), dict(ws=X), dict(ws=X + 256), dict(ws=X - need + 256), dict(out=WS), dict(out=WS + need - 4)):
+        assert norm(**kw) == B.FF_EINVAL, kw
+        assert "overlap" in P.last_error()
+
+
+def plan_of(columns):
+    """A plan's record of its tensors, on the CPU."""
+    import torch
+    plan = B.AdamWPlan.__new__(B.AdamWPlan)
+    numel = [t.numel() for t in columns["g"]]
+    table = np.zeros(len(numel), np.dtype(B.AdamWTensor))
+    table["numel"] = numel
+    for k, ts in columns.items():
+        table[k] = [t.data_ptr() for t in ts]
+    plan.tensors, plan.spans = (table, {k: (ts, ts[0].dtype) for k, ts in columns.items()}), {}
+    assert torch.is_tensor(columns["g"][0])
+    return plan
+
+
+def test_what_shares_memory_with_a_plan():
+    import torch
+    room = torch.zeros(4000)
+    codes = torch.zeros(3000, dtype=torch.uint8)
+    exps = torch.zeros(20, dtype=torch.uint8)
+    g = [room[2000:2600], room[100:100], room[100:400]]
+    plan = plan_of({"g": g, "m": [codes[1000:1600], codes[7:7], codes[300:600]], "m_exp": [exps[10:13], exps[0:0], exps[4:6]]})
+    for lo, hi, meets in ((0, 100, False), (99, 101, True), (100, 400, True), (399, 401, True), (400, 2000, False), (1999, 2001, True), (2599, 2601, True), (2600, 4000, False),
+                          (0, 4000, True), (250, 250, False)):
+        assert plan.meets(("g",), room[lo:hi]) == meets, (lo, hi)
+        assert not plan.meets(("m", "m_exp"), room[lo:hi])
+    for lo, hi, meets in ((0, 300, False), (299, 301, True), (599, 600, True), (600, 1000, False), (1599, 1601, True), (1600, 3000, False)):
+        assert plan.meets(("m", "m_exp"), codes[lo:hi]) == meets, (lo, hi)
+    for lo, hi, meets in ((0, 4, False), (5, 6, True), (6, 10, False), (12, 13, True), (13, 20, False)):
+        assert plan.meets(("m", "m_exp"), exps[lo:hi]) == meets, (lo, hi)
+        assert not plan.meets(("v", "g"), exps[lo:hi])
+    assert not plan.meets(("g",), 3)
