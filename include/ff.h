@@ -382,7 +382,7 @@ ff_status ff_adamw_step(const ff_adamw_desc* desc, const void* plan, size_t plan
                         const float* norm, void* hip_stream);
 
 /* m and v of all tensors as float32, one tensor after another (for checkpoints and inspection): m_out, v_out hold
- * the sum of all numel; either may be NULL. */
+ * the sum of all numel; either may be NULL.  They must not overlap each other or the plan (FF_EINVAL as far as desc and plan_bytes show it), nor a state. */
 ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* m_out, float* v_out,
                            void* hip_stream);
 

@@ -562,7 +562,10 @@ def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps
 
 
 def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
-    """(m, v) of all tensors of the plan, one after another, as float32."""
+    """(m, v) of all tensors of the plan, one after another, as float32, in memory that none of the plan's states holds."""
+    for name, t in (("m", m), ("v", v)):
+        if t is not None and plan.meets(("m", "v", "m_exp", "v_exp"), t):
+            raise ValueError(f"{name} shares memory with a state of the plan")
     return _done(calls().adamw_moments(C.addressof(plan.desc), plan.plan, plan.values, m, v))
 
 

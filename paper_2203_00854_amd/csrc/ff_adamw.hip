@@ -57,6 +57,10 @@ bool adamw_plan_whole(size_t bytes) {
     return bytes >= sizeof(PlanHead) && bytes % sizeof(Piece) == 0 && bytes / sizeof(Piece) - 1 < (1u << 24);     // 2^32 threads in blocks of 256
 }
 static int pieces_of(size_t bytes) { return (int)(bytes / sizeof(Piece) - 1); }
+size_t adamw_least_values(const ff_adamw_desc& d, size_t plan_bytes) {         // all pieces but each tensor's last are full
+    const size_t pieces = pieces_of(plan_bytes), last = pieces < (size_t)d.n_tensors ? pieces : (size_t)d.n_tensors;
+    return (pieces - last) * kPiece + last;
+}
 
 void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* ts, void* plan) {
     PlanHead* head = (PlanHead*)plan;

@@ -563,6 +563,10 @@ ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t p
     if (desc->state_bits == 0) return fail(FF_EINVAL, "a plan of gradients alone has no moments");
     if (!aligned_to(m_out, 4) || !aligned_to(v_out, 4)) return fail(FF_EINVAL, "m_out or v_out is misaligned");
     if (!m_out && !v_out) return FF_OK;
+    const size_t least = adamw_least_values(*desc, plan_bytes) * 4;
+    if (m_out && v_out && overlaps(m_out, least, v_out, least)) return fail(FF_EINVAL, "m_out and v_out overlap");
+    if ((m_out && overlaps(m_out, least, plan, plan_bytes)) || (v_out && overlaps(v_out, least, plan, plan_bytes)))
+        return fail(FF_EINVAL, "m_out or v_out overlaps the plan");
     return adamw_moments_run(*desc, plan, plan_bytes, m_out, v_out, (hipStream_t)hip_stream);
 }
 

@@ -219,6 +219,8 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const c10::DeviceGuard guard(device);
             result(m, "m", at::kFloat, {values}, device);
             result(v, "v", at::kFloat, {values}, device);
+            const char *from_m = (const char*)in(m), *from_v = (const char*)in(v);
+            if (from_m < from_v + v.nbytes() && from_v < from_m + m.nbytes()) value_error("m and v share memory");
             status = ff_adamw_moments(desc, in(plan), plan.nbytes(), out<float>(m), out<float>(v), c10::hip::getCurrentHIPStream(device.index()).stream());
         }
         return status == FF_OK ? tuple_of(m, v) : PyLong_FromLong(status);

@@ -180,6 +180,8 @@ void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* tensors, voi
 int adamw_overlaps(const ff_adamw_desc& d, const ff_adamw_tensor* tensors);
 // whether a plan can have this many bytes
 bool adamw_plan_whole(size_t bytes);
+// how many values the tensors of a plan of this many bytes have at least
+size_t adamw_least_values(const ff_adamw_desc& d, size_t plan_bytes);
 size_t grad_norm_workspace();
 ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, float* norm, void* ws, hipStream_t stream);
 ff_status adamw_step_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, const ff_adamw_hyper& h, const float* norm, hipStream_t stream);

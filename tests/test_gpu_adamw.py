@@ -443,3 +443,31 @@ def test_norm_refuses_memory_of_the_gradients():
         P.ff_grad_norm(plan, out=ws[:4].view(torch.float32), ws=ws)
     with pytest.raises(P.FFError):
         P.ff_grad_norm(plan, out=plan.plan[:4].view(torch.float32))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_refuse_memory_in_use(bits):
+    model = Model([3000, 700], "f32", "f32", bits, seed=12, gap=2)
+    want = P.ff_adamw_moments(model.plan)
+    room = torch.full((3 * 3700,), 7.0, device=DEV)
+    for kw in (dict(m=room[:3700], v=room[:3700]), dict(m=room[:3700], v=room[3699:7399]), dict(m=room[3699:7399], v=room[:3700])):
+        with pytest.raises((ValueError, P.FFError)):
+            P.ff_adamw_moments(model.plan, **kw)
+    assert (room == 7).all()
+    if bits == 32:
+        for k in ("m", "v"):
+            for out in ("m", "v"):
+                with pytest.raises(ValueError):
+                    P.ff_adamw_moments(model.plan, **{out: model.flat[k][1:3701]})
+    else:
+        codes = torch.zeros(4 * 3700, dtype=torch.uint8, device=DEV)
+        states = P.adamw_states(model.lists["p"], 8)
+        states["m"] = [codes[:3000], codes[3000:3700]]
+        plan = P.make_adamw_plan(model.lists["p"], model.lists["g"], **states)
+        with pytest.raises(ValueError):
+            P.ff_adamw_moments(plan, v=codes.view(torch.float32))
+        assert not codes.any()
+    got = P.ff_adamw_moments(model.plan, m=room[:3700], v=room[3700:7400])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and (room[7400:] == 7).all()
+    got = P.ff_adamw_moments(model.plan, m=model.flat["g"][1:3701])          # the gradients' memory, which the call does not read
+    assert torch.equal(got[0], want[0])

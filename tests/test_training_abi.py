@@ -302,3 +302,14 @@ def test_what_shares_memory_with_a_plan():
         assert plan.meets(("m", "m_exp"), exps[lo:hi]) == meets, (lo, hi)
         assert not plan.meets(("v", "g"), exps[lo:hi])
     assert not plan.meets(("g",), 3)
+
+
+def test_moments_overlaps():
+    """Two tensors of 5000 and 3 values are four pieces, which hold 2 x 2048 + 2 values at least."""
+    lib, d = P.lib(), B.AdamWDesc(P.FF_F32, P.FF_F32, 32, 2)
+    second = {k: GOOD[k] + 0x1000000 for k in ("p", "g", "m", "v")}
+    n, least = plan_bytes(d, tensors(GOOD, {**GOOD, **second, "numel": 3})), 4 * (2 * 2048 + 2)
+    assert n == 5 * 80
+    for m, v in ((Y, Y), (Y, Y + least - 4), (Y + least - 4, Y), (X, None), (None, X + n - 4), (X - least + 4, Y), (Y, X + 16)):
+        assert lib.ff_adamw_moments(C.byref(d), X, n, m, v, None) == B.FF_EINVAL, (m, v)
+        assert "overlap" in P.last_error()
