@@ -371,7 +371,7 @@ size_t ff_grad_norm_workspace_bytes(void);
 
 /* norm[0] (float32, device) = square root of the sum of the squares of all gradients of the plan, summed in float64 in a fixed order.
  * plan: device copy, 16-byte aligned, of a plan made with this desc; ws 256-byte aligned.  norm and ws must not overlap each other or the plan (FF_EINVAL), nor
- * a gradient (whose addresses are on the device, so that this call does not see them). */
+ * a gradient (whose addresses are on the device, so that this call does not see them).  Under another desc than the plan's the norm is NaN. */
 ff_status ff_grad_norm(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* norm, void* ws,
                        size_t ws_bytes, void* hip_stream);
 

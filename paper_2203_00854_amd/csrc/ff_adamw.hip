@@ -290,6 +290,8 @@ template <int TOP> struct Scale {
 // Squares and sums in float64: no square leaves its range, and the order of the sums does not show in the float32 result.  Bound by HBM and two
 // dependent launches: 49.1 M bfloat16 values 19 us (5.2 TB/s) and 4 for the join, whose loads are all under way at once.  As many blocks as the card holds, each
 // with the next record on its way: blocks of neighbouring pieces, two or four pieces at a time, took 27 to 32 for both.
+// (A piece of another plan has no values here, and makes the norm one that no step is taken with.)
+constexpr double kNoNorm = __builtin_nan("");
 template <int WAVES> __device__ __forceinline__ double block_sum(double x) {
     __shared__ double part[WAVES];
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
@@ -321,6 +323,8 @@ __global__ __launch_bounds__(256) void k_grad_norm(const Piece* __restrict__ pie
         } else if (n > 0) {
 #pragma unroll
             for (int t = 0; t < kPiece / 1024; ++t) load4<kTiny, G>(g, (threadIdx.x + 256 * t) * 4, n, v[t]);
+        } else {
+            sum = kNoNorm;
         }
 #pragma unroll
         for (int t = 0; t < kPiece / 1024; ++t)
@@ -362,6 +366,8 @@ __global__ __launch_bounds__(1024) void k_norm_few(const Piece* __restrict__ pie
         } else if (n > 0) {
 #pragma unroll
             for (int t = 0; t < kPiece / 256; ++t) load4<kTiny, G>(pc.g, (lane + 64 * t) * 4, n, v[t]);
+        } else {
+            sum = kNoNorm;
         }
 #pragma unroll
         for (int t = 0; t < kPiece / 256; ++t)

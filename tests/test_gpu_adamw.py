@@ -471,3 +471,21 @@ def test_moments_refuse_memory_in_use(bits):
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and (room[7400:] == 7).all()
     got = P.ff_adamw_moments(model.plan, m=model.flat["g"][1:3701])          # the gradients' memory, which the call does not read
     assert torch.equal(got[0], want[0])
+
+
+@pytest.mark.parametrize("sizes", [[3000], [100] * 40])
+def test_a_norm_under_another_descriptor_clips_nothing_away(sizes):
+    """It is NaN, which a step leaves everything alone for, and not the 0 of gradients that need no clipping."""
+    model = Model(sizes, "f32", "f32", 32, seed=8)
+    real = model.plan.desc
+    for other in (P.AdamWDesc(real.param_dtype, P.FF_BF16, 32, real.n_tensors), P.AdamWDesc(real.param_dtype, real.grad_dtype, 0, real.n_tensors)):
+        model.plan.desc = other
+        norm = P.ff_grad_norm(model.plan)
+        assert norm.isnan().all()
+        model.plan.desc = real
+        before = model.host()
+        P.ff_adamw_step(model.plan, 1, norm=norm, max_norm=1.0, **HYPER)
+        after = model.host()
+        for k in ("p", "m", "v"):
+            assert all(np.array_equal(a, b) for a, b in zip(before[k], after[k])), k
+    assert P.ff_grad_norm(model.plan).isfinite().all()
