@@ -489,3 +489,15 @@ def test_a_norm_under_another_descriptor_clips_nothing_away(sizes):
         for k in ("p", "m", "v"):
             assert all(np.array_equal(a, b) for a, b in zip(before[k], after[k])), k
     assert P.ff_grad_norm(model.plan).isfinite().all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_step_left_out_keeps_shared_exponents(bad):
+    model = Model([300, 5000], "f32", "f32", 8, seed=14)
+    model.lists["g"][0][5] = bad
+    model.lists["g"][1].mul_(1e6)                       # exponents that a step would change
+    before = model.host()
+    P.ff_adamw_step(model.plan, 3, norm=P.ff_grad_norm(model.plan), max_norm=1e30, **HYPER)
+    after = model.host()
+    for k in ("p", "m", "v", "m_exp", "v_exp"):
+        assert all(np.array_equal(a, b) for a, b in zip(before[k], after[k])), k
