@@ -7,6 +7,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -49,6 +50,9 @@ void result(at::Tensor& t, const char* name, at::ScalarType dtype, at::IntArrayR
 }
 const void* in(const at::Tensor& t) { return t.defined() ? t.const_data_ptr() : nullptr; }
 template <typename T = void> T* out(const at::Tensor& t) { return t.defined() ? (T*)t.mutable_data_ptr() : nullptr; }
+
+// Memory that the binding has allocated and this stream still reads: the allocator, which knows it as another stream's, does not hand it out before.
+void in_use(const at::Tensor& t, const c10::hip::HIPStream& stream) { c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), stream); }
 
 struct Unlocked {                      // without the interpreter lock
     PyThreadState* state = PyEval_SaveThread();
@@ -169,7 +173,10 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
             Unlocked unlocked;
             const c10::DeviceGuard guard(device);
             result(norm, "out", at::kFloat, {1}, device);
-            status = ff_grad_norm(desc, in(plan), plan.nbytes(), out<float>(norm), out(ws), ws.nbytes(), c10::hip::getCurrentHIPStream(device.index()).stream());
+            const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
+            status = ff_grad_norm(desc, in(plan), plan.nbytes(), out<float>(norm), out(ws), ws.nbytes(), stream.stream());
+            in_use(plan, stream);
+            in_use(ws, stream);
         }
         return status == FF_OK ? THPVariable_Wrap(norm) : PyLong_FromLong(status);
     });
@@ -197,7 +204,9 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
         {
             Unlocked unlocked;
             const c10::DeviceGuard guard(device);
-            status = ff_adamw_step(desc, in(plan), plan.nbytes(), &h, (const float*)in(norm), c10::hip::getCurrentHIPStream(device.index()).stream());
+            const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
+            status = ff_adamw_step(desc, in(plan), plan.nbytes(), &h, (const float*)in(norm), stream.stream());
+            in_use(plan, stream);
         }
         return PyLong_FromLong(status);
     });
@@ -221,7 +230,9 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t n) {
             result(v, "v", at::kFloat, {values}, device);
             const char *from_m = (const char*)in(m), *from_v = (const char*)in(v);
             if (from_m < from_v + v.nbytes() && from_v < from_m + m.nbytes()) value_error("m and v share memory");
-            status = ff_adamw_moments(desc, in(plan), plan.nbytes(), out<float>(m), out<float>(v), c10::hip::getCurrentHIPStream(device.index()).stream());
+            const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
+            status = ff_adamw_moments(desc, in(plan), plan.nbytes(), out<float>(m), out<float>(v), stream.stream());
+            in_use(plan, stream);
         }
         return status == FF_OK ? tuple_of(m, v) : PyLong_FromLong(status);
     });

@@ -501,3 +501,28 @@ def test_a_step_left_out_keeps_shared_exponents(bad):
     after = model.host()
     for k in ("p", "m", "v", "m_exp", "v_exp"):
         assert all(np.array_equal(a, b) for a, b in zip(before[k], after[k])), k
+
+
+@pytest.mark.parametrize("what", ["norm", "step", "moments"])
+def test_a_plan_used_on_another_stream_keeps_its_memory(what):
+    """A plan that is dropped while another stream than its own still has to read it: its memory is not handed out again before."""
+    model = Model([3000] * 40, "f32", "f32", 32, seed=15)
+    a = torch.randn(8192, 8192, device=DEV).to(torch.bfloat16)
+    product, side = a @ a, torch.cuda.Stream()
+    norm, out = torch.empty(1, device=DEV), torch.empty(2, 120_000, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(200):                            # a fifth of a second that the call has to wait for
+            torch.mm(a, a, out=product)
+        if what == "norm":
+            P.ff_grad_norm(model.plan, out=norm)
+        elif what == "step":
+            P.ff_adamw_step(model.plan, 1, **HYPER)
+        else:
+            P.ff_adamw_moments(model.plan, m=out[0], v=out[1])
+    plan = {t.data_ptr(): t.numel() for t in ((model.plan.plan, model.plan.norm_ws) if what == "norm" else (model.plan.plan,))}
+    model.plan = None
+    again = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in plan.values() for _ in range(50)]
+    assert not side.query()
+    assert not plan.keys() & {t.data_ptr() for t in again}
+    torch.cuda.synchronize()
