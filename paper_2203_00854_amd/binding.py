@@ -453,11 +453,11 @@ class AdamWPlan:
 
     def meets(self, kinds, t) -> bool:
         """Whether t shares memory with one of the plan's tensors of these kinds (pointer names); what is no tensor does not."""
-        import numpy as np
         import torch
         if not isinstance(t, torch.Tensor):
             return False
         if kinds not in self.spans:
+            import numpy as np
             table, columns = self.tensors
             numel = table["numel"]
             # starts in order, and how far the tensors up to each of them reach
