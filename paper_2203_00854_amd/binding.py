@@ -10,10 +10,12 @@ from __future__ import annotations
 import bisect
 import ctypes as C
 import os
+import sysconfig
 from typing import Dict, Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libff.so")
+CALLS_PATH = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 FF_OK, FF_EINVAL, FF_EUNSUPPORTED, FF_EWORKSPACE, FF_EHIP = range(5)
 FF_F32, FF_BF16 = 0, 1
@@ -190,8 +192,8 @@ def calls():
     global _calls
     if _calls is None:
         lib()
-        if not os.path.exists(os.path.join(PKG, "_calls.so")):
-            raise FileNotFoundError(f"{PKG}/_calls.so is missing: build it with `python -m paper_2203_00854_amd.build` (there is no fallback path)")
+        if not os.path.exists(CALLS_PATH):
+            raise FileNotFoundError(f"{CALLS_PATH} is missing: build it with `python -m paper_2203_00854_amd.build` (there is no fallback path)")
         import torch  # noqa: F401    (its libraries are what the module's names are looked up in)
 
         from . import _calls as module

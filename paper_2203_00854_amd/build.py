@@ -1,14 +1,16 @@
-"""Build libff.so (HIP, gfx950) and _calls.so (the binding's part in C++) in-tree.
+"""Build libff.so (HIP, gfx950) and the module _calls (the binding's part in C++) in-tree.
 
     python -m paper_2203_00854_amd.build
 
 hipcc cross-compiles for gfx950 without a GPU.  Objects go to _build/, the library to
-paper_2203_00854_amd/libff.so and paper_2203_00854_amd/_calls.so (git-ignored; they travel with the source tree to the GPU machine).
+paper_2203_00854_amd/libff.so, the module, of one interpreter's version, beside it (git-ignored; they travel with the source tree to the GPU machine).
+The library needs hipcc alone.  Where g++, torch or the interpreter's headers are missing the module is left out, and with it the Python entry points of the training operators.
 """
 from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -19,7 +21,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libff.so")
-CALLS = os.path.join(PKG, "_calls.so")
+CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -53,11 +55,23 @@ def _compile(src: str) -> str:
     return obj
 
 
-def _build_calls() -> None:
-    """ff_calls.cpp, host code: a CPython module on libff.so and torch's libraries."""
-    import torch
+def _build_calls() -> str:
+    """ff_calls.cpp, host code: a CPython module on libff.so and torch's libraries.  What is missing for it, or ""."""
+    for old in (CALLS, os.path.join(PKG, "_calls.so")):          # (the latter: without an interpreter's version, as it was once named)
+        if os.path.exists(old):
+            os.remove(old)
+    compiler = shutil.which("g++")
+    if not compiler:
+        return "g++"
+    try:
+        import torch
+    except ImportError:
+        return "torch"
     home = os.path.dirname(torch.__file__)
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+    for header in (os.path.join(sysconfig.get_paths()["include"], "Python.h"), os.path.join(home, "include", "ATen", "ATen.h")):
+        if not os.path.exists(header):
+            return header
+    cmd = [compiler, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
            "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(home, "include"),
            "-isystem", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"), os.path.join(CSRC, "ff_calls.cpp"), "-o", CALLS,
@@ -67,6 +81,7 @@ def _build_calls() -> None:
         raise RuntimeError("g++ failed for ff_calls.cpp:\n" + r.stderr)
     if r.stderr.strip():
         sys.stderr.write(r.stderr)
+    return ""
 
 
 def build(verbose: bool = True) -> str:
@@ -78,9 +93,11 @@ def build(verbose: bool = True) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
-    _build_calls()
+    missing = _build_calls()
+    if missing:
+        print(f"without {missing}: {os.path.basename(CALLS)} is left out, and with it the Python entry points of the training operators")
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources, {CALLS}")
+        print(f"built {LIB} from {len(srcs)} sources" + ("" if missing else f", {CALLS}"))
     return LIB
 
 
