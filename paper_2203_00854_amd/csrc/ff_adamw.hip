@@ -34,12 +34,7 @@ struct Piece {
     uint32_t tag;                        // the plan's types: a piece of another plan is left alone
 };
 static_assert(sizeof(Piece) == 80, "the plan's records");
-
-struct PlanHead {
-    int64_t pieces, values;
-    char rest[80 - 16];
-};
-static_assert(sizeof(PlanHead) == sizeof(Piece), "a head as long as a record");
+// (A plan is an empty record, so that one without values has an address too, and one record a piece.)
 
 struct StepArgs {
     float lr, step_size, beta1, rest1, beta2, rest2, inv_root, eps, max_norm;
@@ -51,10 +46,10 @@ static uint32_t tag_of(const ff_adamw_desc& d) { return 0x46000000u | (d.param_d
 size_t adamw_plan_size(const ff_adamw_desc& d, const ff_adamw_tensor* ts) {
     size_t pieces = 0;
     for (int i = 0; i < d.n_tensors; ++i) pieces += (size_t)((ts[i].numel + kPiece - 1) / kPiece);
-    return sizeof(PlanHead) + pieces * sizeof(Piece);
+    return (1 + pieces) * sizeof(Piece);
 }
 bool adamw_plan_whole(size_t bytes) {
-    return bytes >= sizeof(PlanHead) && bytes % sizeof(Piece) == 0 && bytes / sizeof(Piece) - 1 < (1u << 24);     // 2^32 threads in blocks of 256
+    return bytes >= sizeof(Piece) && bytes % sizeof(Piece) == 0 && bytes / sizeof(Piece) - 1 < (1u << 24);     // 2^32 threads in blocks of 256
 }
 static int pieces_of(size_t bytes) { return (int)(bytes / sizeof(Piece) - 1); }
 size_t adamw_least_values(const ff_adamw_desc& d, size_t plan_bytes) {         // all pieces but each tensor's last are full
@@ -63,9 +58,8 @@ size_t adamw_least_values(const ff_adamw_desc& d, size_t plan_bytes) {         /
 }
 
 void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* ts, void* plan) {
-    PlanHead* head = (PlanHead*)plan;
-    *head = PlanHead{};
-    Piece* out = (Piece*)plan + 1;
+    Piece* out = (Piece*)plan;
+    *out++ = Piece{};
     const size_t ps = d.param_dtype == FF_F32 ? 4 : 2, gs = d.grad_dtype == FF_F32 ? 4 : 2, ss = d.state_bits == 32 ? 4 : 1;
     int64_t value = 0, group = 0;
     for (int i = 0; i < d.n_tensors; ++i) {
@@ -91,8 +85,6 @@ void adamw_plan_fill(const ff_adamw_desc& d, const ff_adamw_tensor* ts, void* pl
         value += t.numel;
         group += (t.numel + kGroup - 1) / kGroup;
     }
-    head->pieces = out - ((Piece*)plan + 1);
-    head->values = value;
 }
 
 // Whether a tensor that the step writes shares memory with another one (tied weights listed twice, say): their blocks would race.
@@ -391,10 +383,8 @@ ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_by
         else hipLaunchKernelGGL((k_norm_few<bf16_t>), dim3(1), dim3(1024), 0, stream, pieces, n, tag_of(d), norm);
         return check_launch("ff_grad_norm");
     }
-    if (blocks > 0) {
-        if (d.grad_dtype == FF_F32) hipLaunchKernelGGL((k_grad_norm<float>), dim3(blocks), dim3(256), 0, stream, pieces, n, tag_of(d), partial);
-        else hipLaunchKernelGGL((k_grad_norm<bf16_t>), dim3(blocks), dim3(256), 0, stream, pieces, n, tag_of(d), partial);
-    }
+    if (d.grad_dtype == FF_F32) hipLaunchKernelGGL((k_grad_norm<float>), dim3(blocks), dim3(256), 0, stream, pieces, n, tag_of(d), partial);
+    else hipLaunchKernelGGL((k_grad_norm<bf16_t>), dim3(blocks), dim3(256), 0, stream, pieces, n, tag_of(d), partial);
     hipLaunchKernelGGL(k_norm_join, dim3(1), dim3(1024), 0, stream, partial, blocks, norm);
     return check_launch("ff_grad_norm");
 }
