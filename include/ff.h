@@ -281,8 +281,8 @@ ff_status ff_attention_core_backward(const ff_core_desc* desc, const void* q, co
  * and, for gradients dy = dLoss/dy and dsum = what reaches s by other ways (the residual path around the module):
  *   u = (s - mean) rstd;  h = dy gamma;  dx = rstd (h - mean(h) - u mean(h u)) (+ dsum)
  *   dgamma = sum over the rows of dy u;  dbeta = sum over the rows of dy
- * dx is the gradient of x and of residual alike.  Statistics, sums over channels and over rows are float32; the sums
- * over rows are formed in an order that depends on rows and c alone, so equal calls give equal bits. */
+ * dx is the gradient of x and of residual alike.  Statistics and sums over channels are float32; sums over rows are float32 within a
+ * wavefront (a block, for long rows) and float64 beyond, in an order that depends on dtype, rows and c alone, so equal calls give equal bits. */
 typedef struct {
     int32_t dtype;      /* ff_dtype of x, residual, sum, y, gamma, beta, dy, dsum and dx */
     int32_t c;          /* 1 .. 8192 */

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
 // the other, not two); 5120 x 384 x 64 in 128 to 135 (5.6 to 5.9 TB/s), 128 x 256 x 256 with dsum in 14.6.  Sixteen wavefronts on a compute unit carry that: twice as many,
 // in registers or blocks, took longer (662), and each block more makes the second launch longer.
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
-// over its teams and wavefronts in a fixed order and leaves 2 c partial sums; with one block in all these are the result.
+// over its teams and, in float64, its wavefronts in a fixed order and leaves 2 c float32 partial sums; with one block in all these are the result.
 // AHEAD: the next row is on its way while this one is worked on.
 template <typename T, int V, int ITERS, bool MASKED, bool WIDE, bool STREAMED, bool AHEAD>
 __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) void k_ln_backward(
@@ -337,12 +337,12 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
     }
     const bool alone = gridDim.x == 1;
     float* out = partial + (size_t)blockIdx.x * 2 * c;
-    auto leave = [&](int i, float v) {                 // partial sum number i of 2 c
+    auto leave = [&](int i, double v) {                // partial sum number i of 2 c
         if (alone) {
             float* to = i < c ? dgamma + i : dbeta + i - c;
-            *to = accumulate ? *to + v : v;
+            *to = (float)(accumulate ? *to + v : v);
         } else {
-            out[i] = v;
+            out[i] = (float)v;
         }
     };
     if constexpr (WIDE) {
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
         for (int ch = threadIdx.x; ch < c; ch += THREADS) {
             const int p = ch / V, i = MASKED && p == last ? ch - (c - V) : ch % V;
             const float* from = joined + (p / lanes * V + i) * lanes + (p & (lanes - 1));
-            float g = 0.f, b = 0.f;
+            double g = 0., b = 0.;
 #pragma unroll
             for (int w = 0; w < THREADS / 64; ++w) {
                 g += from[w * 2 * slots];
@@ -385,12 +385,12 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : backward_threads(V * ITERS)) 
     }
 }
 
-// dgamma and dbeta from the blocks' partial sums: a block takes 64 of the 2 c columns, its sixteen wavefronts every sixteenth of the partial sums each
+// dgamma and dbeta from the blocks' partial sums, in float64 (the loads take the time): a block takes 64 of the 2 c columns, its sixteen wavefronts every sixteenth of the partial sums each
 __global__ __launch_bounds__(1024) void k_ln_join(const float* __restrict__ partial, int blocks, int c, bool accumulate,
                                                   float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ float part[16][64];
+    __shared__ double part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
-    float sum = 0.f;
+    double sum = 0.;
     if (i < 2 * c) {
 #pragma unroll 8
         for (int b = wave; b < blocks; b += 16) sum += partial[(size_t)b * 2 * c + i];
@@ -398,11 +398,11 @@ __global__ __launch_bounds__(1024) void k_ln_join(const float* __restrict__ part
     part[wave][lane] = sum;
     __syncthreads();
     if (wave != 0 || i >= 2 * c) return;
-    sum = 0.f;
+    sum = 0.;
 #pragma unroll
     for (int w = 0; w < 16; ++w) sum += part[w][lane];
     float* to = i < c ? dgamma + i : dbeta + i - c;
-    *to = accumulate ? *to + sum : sum;
+    *to = (float)(accumulate ? *to + sum : sum);
 }
 
 // ---- which kernel takes a shape ------------------------------------------------------------

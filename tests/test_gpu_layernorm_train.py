@@ -401,3 +401,21 @@ def test_backward_with_the_next_row_on_its_way(dtype, rows, c):
         over = dy.clone()
         again = P.ff_layernorm_backward(x, gamma, over, dx=over, **kw)
         assert torch.equal(again[0], dx) and torch.equal(again[1], dgamma) and torch.equal(again[2], dbeta)
+
+
+@pytest.mark.parametrize("dtype,rows,c,own", [("f32", 16, 256, 1), ("bf16", 16, 512, 1), ("f32", 61, 200, 4), ("f32", 300, 2048, 1), ("f32", 1000, 1100, 2),
+                                              ("bf16", 700, 1500, 1), ("f32", 4096, 256, 1), ("bf16", 8000, 300, 2)])
+def test_sums_over_rows_lose_nothing_between_wavefronts_and_blocks(dtype, rows, c, own):
+    """A row of 2^24 beside rows of 1, which a float32 sum that has reached 2^24 does not take in.  Only a wavefront's (or, of long rows, a block's) own rows,
+    here `own` of them at most, are added up in float32, so that no more than the ones beside the large row can be lost; a block's sum and
+    the result are rounded once each."""
+    x, dy = torch.randn(rows, c, device=DEV).to(DT[dtype]), torch.ones(rows, c, device=DEV, dtype=DT[dtype])
+    dy[rows // 2] = 2.0 ** 24
+    want = 2.0 ** 24 + rows - 1
+    gamma = torch.ones(c, device=DEV, dtype=DT[dtype])
+    _, _, dbeta = P.ff_layernorm_backward(x, gamma, dy, eps=EPS)
+    off = (dbeta.double() - want).abs().max().item()
+    print(f"off by {off}", flush=True)
+    assert off <= own - 1 + 2 * U * want
+    _, _, dbeta = P.ff_layernorm_backward(x, gamma, dy, eps=EPS, dgamma=torch.zeros(c, device=DEV), dbeta=torch.full((c,), 5.0, device=DEV), accumulate=True)
+    assert (dbeta.double() - (want + 5)).abs().max().item() <= own - 1 + 2 * U * (want + 5)
