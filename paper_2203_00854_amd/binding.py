@@ -539,6 +539,7 @@ def adamw_states(params, bits: int = 32):
     import torch
     if bits not in (8, 32):
         raise ValueError(f"states have 8 or 32 bits, not {bits}")
+    params = list(params)
     new = lambda t, n, dtype: torch.zeros(n, dtype=dtype, device=t.device)  # noqa: E731
     kind = torch.float32 if bits == 32 else torch.uint8
     states = {k: [new(t, t.numel(), kind) for t in params] for k in ("m", "v")}

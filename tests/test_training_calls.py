@@ -56,3 +56,13 @@ def test_a_seed_that_is_given_is_passed(calls):
     for seed in (0, 7, 1 << 31):
         P.ff_adamw_step(PLAN, 3, lr=1e-3, seed=seed)
     assert [args[9] for args in calls.seen] == [0, 7, 1 << 31]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_of_tensors_that_are_given_once(bits):
+    """What a module's parameters() gives can be gone through once only."""
+    import torch
+    params = [torch.zeros(n) for n in (300, 1, 0)]
+    states, want = P.adamw_states((p for p in params), bits), P.adamw_states(params, bits)
+    assert {k: [(t.numel(), t.dtype) for t in ts] for k, ts in states.items()} == {k: [(t.numel(), t.dtype) for t in ts] for k, ts in want.items()}
+    assert [t.numel() for t in states["v"]] == [300, 1, 0] and all(not t.any() for ts in states.values() for t in ts)
