@@ -452,6 +452,7 @@ class AdamWPlan:
         _check(lib().ff_adamw_plan(C.byref(desc), table, host.ctypes.data, n))
         self.plan = torch.from_numpy(host).to(device)
         self.norm_ws = _alloc_ws(lib().ff_grad_norm_workspace_bytes(), device)
+        self.stream = torch.cuda.current_stream(device).cuda_stream          # the one that the two belong to
 
     def meets(self, kinds, t) -> bool:
         """Whether t shares memory with one of the plan's tensors of these kinds (pointer names); what is no tensor does not."""
@@ -551,25 +552,27 @@ def adamw_states(params, bits: int = 32):
 def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
     """The norm of all gradients of the plan, float32 [1] on the device.  The plan's own workspace serves one stream at a time; give ws for another.
     out and ws must not share memory with a gradient."""
-    for name, t in (("out", out), ("ws", ws)):
-        if t is not None and plan.meets(("g",), t):
-            raise ValueError(f"{name} shares memory with a gradient of the plan")
-    return _done(calls().grad_norm(C.addressof(plan.desc), plan.plan, out, plan.norm_ws if ws is None else ws))
+    if out is not None and plan.meets(("g",), out):
+        raise ValueError("out shares memory with a gradient of the plan")
+    if ws is not None and plan.meets(("g",), ws):
+        raise ValueError("ws shares memory with a gradient of the plan")
+    return _done(calls().grad_norm(C.addressof(plan.desc), plan.plan, out, plan.norm_ws if ws is None else ws, plan.stream))
 
 
 def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: Optional[int] = None):
     """One AdamW step over the plan's tensors, in place.  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm
     that is not finite leaves everything as it was.  seed: of the rounding of 8-bit states, another for each step (None: the step's number).  With
     one seed for all steps a value would be rounded the same way every time, and its moments would drift."""
-    _done(calls().adamw_step(C.addressof(plan.desc), plan.plan, step, lr, betas[0], betas[1], eps, norm, max_norm, step if seed is None else seed))
+    _done(calls().adamw_step(C.addressof(plan.desc), plan.plan, step, lr, betas[0], betas[1], eps, norm, max_norm, step if seed is None else seed, plan.stream))
 
 
 def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
     """(m, v) of all tensors of the plan, one after another, as float32, in memory that none of the plan's states holds."""
-    for name, t in (("m", m), ("v", v)):
-        if t is not None and plan.meets(("m", "v", "m_exp", "v_exp"), t):
-            raise ValueError(f"{name} shares memory with a state of the plan")
-    return _done(calls().adamw_moments(C.addressof(plan.desc), plan.plan, plan.values, m, v))
+    if m is not None and plan.meets(("m", "v", "m_exp", "v_exp"), m):
+        raise ValueError("m shares memory with a state of the plan")
+    if v is not None and plan.meets(("m", "v", "m_exp", "v_exp"), v):
+        raise ValueError("v shares memory with a state of the plan")
+    return _done(calls().adamw_moments(C.addressof(plan.desc), plan.plan, plan.values, m, v, plan.stream))
 
 
 def ff_profile_enable(on: bool):

@@ -51,8 +51,10 @@ void result(at::Tensor& t, const char* name, at::ScalarType dtype, at::IntArrayR
 const void* in(const at::Tensor& t) { return t.defined() ? t.const_data_ptr() : nullptr; }
 template <typename T = void> T* out(const at::Tensor& t) { return t.defined() ? (T*)t.mutable_data_ptr() : nullptr; }
 
-// Memory that the binding has allocated and this stream still reads: the allocator, which knows it as another stream's, does not hand it out before.
-void in_use(const at::Tensor& t, const c10::hip::HIPStream& stream) { c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), stream); }
+// Memory that the binding has allocated for one stream (`own`) and another one still reads: the allocator is told, and does not hand it out before.
+void in_use(const at::Tensor& t, const c10::hip::HIPStream& stream, void* own) {
+    if (stream.stream() != own) c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), stream);
+}
 
 struct Unlocked {                      // without the interpreter lock
     PyThreadState* state = PyEval_SaveThread();
@@ -159,10 +161,11 @@ PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// address of the plan's ff_adamw_desc, the plan, out, ws -> norm
+// address of the plan's ff_adamw_desc, the plan, out, ws, the plan's stream -> norm
 PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded("grad_norm", 4, n, [&]() -> PyObject* {
+    return guarded("grad_norm", 5, n, [&]() -> PyObject* {
         const auto* desc = (const ff_adamw_desc*)PyLong_AsVoidPtr(a[0]);
+        void* const own = PyLong_AsVoidPtr(a[4]);
         if (PyErr_Occurred()) return nullptr;
         const at::Tensor plan = tensor(a[1], "plan"), ws = tensor(a[3], "ws");
         at::Tensor norm = optional(a[2], "out");
@@ -175,17 +178,18 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
             result(norm, "out", at::kFloat, {1}, device);
             const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
             status = ff_grad_norm(desc, in(plan), plan.nbytes(), out<float>(norm), out(ws), ws.nbytes(), stream.stream());
-            in_use(plan, stream);
-            in_use(ws, stream);
+            in_use(plan, stream, own);
+            in_use(ws, stream, own);
         }
         return status == FF_OK ? THPVariable_Wrap(norm) : PyLong_FromLong(status);
     });
 }
 
-// address of the plan's ff_adamw_desc, the plan, step, lr, beta1, beta2, eps, norm, max_norm, seed -> status
+// address of the plan's ff_adamw_desc, the plan, step, lr, beta1, beta2, eps, norm, max_norm, seed, the plan's stream -> status
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded("adamw_step", 10, n, [&]() -> PyObject* {
+    return guarded("adamw_step", 11, n, [&]() -> PyObject* {
         const auto* desc = (const ff_adamw_desc*)PyLong_AsVoidPtr(a[0]);
+        void* const own = PyLong_AsVoidPtr(a[10]);
         if (PyErr_Occurred()) return nullptr;
         const at::Tensor plan = tensor(a[1], "plan"), norm = optional(a[7], "norm");
         if (norm.defined() != (a[8] != Py_None)) value_error("norm and max_norm are given together");
@@ -206,16 +210,17 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const c10::DeviceGuard guard(device);
             const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
             status = ff_adamw_step(desc, in(plan), plan.nbytes(), &h, (const float*)in(norm), stream.stream());
-            in_use(plan, stream);
+            in_use(plan, stream, own);
         }
         return PyLong_FromLong(status);
     });
 }
 
-// address of the plan's ff_adamw_desc, the plan, its values, m, v -> (m, v)
+// address of the plan's ff_adamw_desc, the plan, its values, m, v, the plan's stream -> (m, v)
 PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded("adamw_moments", 5, n, [&]() -> PyObject* {
+    return guarded("adamw_moments", 6, n, [&]() -> PyObject* {
         const auto* desc = (const ff_adamw_desc*)PyLong_AsVoidPtr(a[0]);
+        void* const own = PyLong_AsVoidPtr(a[5]);
         if (PyErr_Occurred()) return nullptr;
         const int64_t values = PyLong_AsLongLong(a[2]);
         if (PyErr_Occurred()) return nullptr;
@@ -232,7 +237,7 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (from_m < from_v + v.nbytes() && from_v < from_m + m.nbytes()) value_error("m and v share memory");
             const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
             status = ff_adamw_moments(desc, in(plan), plan.nbytes(), out<float>(m), out<float>(v), stream.stream());
-            in_use(plan, stream);
+            in_use(plan, stream, own);
         }
         return status == FF_OK ? tuple_of(m, v) : PyLong_FromLong(status);
     });

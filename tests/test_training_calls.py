@@ -27,7 +27,7 @@ def calls(monkeypatch):
     return stand_in
 
 
-PLAN = types.SimpleNamespace(desc=B.AdamWDesc(P.FF_F32, P.FF_F32, 8, 1), plan=None)
+PLAN = types.SimpleNamespace(desc=B.AdamWDesc(P.FF_F32, P.FF_F32, 8, 1), plan=None, stream=0)
 
 
 def test_steps_without_a_seed_keep_the_mean(calls):
