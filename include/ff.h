@@ -376,13 +376,15 @@ ff_status ff_grad_norm(const ff_adamw_desc* desc, const void* plan, size_t plan_
                        size_t ws_bytes, void* hip_stream);
 
 /* One step over all tensors of the plan.  norm: device, or NULL for gradients as they are; a norm that is not finite
- * leaves parameters and states as they were.  hyper is read before the call returns, so a captured call repeats its values.  The plan is the
+ * leaves parameters and states as they were; it must not lie in a tensor that the step writes.  hyper is read before the call returns: a captured call repeats its step
+ * number, learning rate and seed at every replay, which is the same step again and not the next one of a training run.  The plan is the
  * device copy of one made with this desc: under another desc its tensors are left alone. */
 ff_status ff_adamw_step(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, const ff_adamw_hyper* hyper,
                         const float* norm, void* hip_stream);
 
 /* m and v of all tensors as float32, one tensor after another (for checkpoints and inspection): m_out, v_out hold
- * the sum of all numel; either may be NULL.  They must not overlap each other or the plan (FF_EINVAL as far as desc and plan_bytes show it), nor a state. */
+ * the sum of all numel; either may be NULL.  They must not overlap each other or the plan (FF_EINVAL as far as desc and plan_bytes show it), nor a state.
+ * Under another desc than the plan's nothing is written. */
 ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* m_out, float* v_out,
                            void* hip_stream);
 

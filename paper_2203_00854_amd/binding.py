@@ -562,7 +562,8 @@ def ff_grad_norm(plan: AdamWPlan, out=None, ws=None):
 def ff_adamw_step(plan: AdamWPlan, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, norm=None, max_norm=None, seed: Optional[int] = None):
     """One AdamW step over the plan's tensors, in place.  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm
     that is not finite leaves everything as it was.  seed: of the rounding of 8-bit states, another for each step (None: the step's number).  With
-    one seed for all steps a value would be rounded the same way every time, and its moments would drift."""
+    one seed for all steps a value would be rounded the same way every time, and its moments would drift.  Captured into a graph the call keeps step, lr and seed as they are:
+    a replay is not the next step of a training run."""
     _done(calls().adamw_step(C.addressof(plan.desc), plan.plan, step, lr, betas[0], betas[1], eps, norm, max_norm, step if seed is None else seed, plan.stream))
 
 

@@ -280,7 +280,7 @@ template <int TOP> struct Scale {
 
 // ---- norm of all gradients ---------------------------------------------------------------
 // Squares and sums in float64: no square leaves its range, and the order of the sums does not show in the float32 result.  Bound by HBM and two
-// dependent launches: 49.1 M bfloat16 values 19 us (5.2 TB/s) and 4 for the join, whose loads are all under way at once.  As many blocks as the card holds, each
+// dependent launches: 49.1 M bfloat16 values 19 us (5.2 TB/s) and 5 for the join, whose loads are all under way at once.  As many blocks as the card holds, each
 // with the next record on its way: blocks of neighbouring pieces, two or four pieces at a time, took 27 to 32 for both.
 // (A piece of another plan has no values here, and makes the norm one that no step is taken with.)
 constexpr double kNoNorm = __builtin_nan("");
@@ -397,9 +397,9 @@ __device__ __forceinline__ float root_of(float v) {
     return __builtin_amdgcn_sqrtf(__uint_as_float(b > 0x00800000u ? b : 0x00800000u));
 }
 
-// Bound by HBM: with 32-bit states 28 bytes a value, with 8 bits 10 to 16 and 63 vector instructions a value, which take about as long where
-// the tensors are bfloat16.  48 Evoformer blocks (49.1 M values): 215 us with master copies (6.4 TB/s), 110 with float32 weights
-// and 8-bit states (6.2 TB/s).
+// Bound by HBM: with 32-bit states 22 to 30 bytes a value, with 8 bits 10 to 18 and 66 vector instructions a value, which take about as long where
+// the tensors are bfloat16.  48 Evoformer blocks (49.1 M values): 215 us with master copies (6.4 TB/s), 107 with float32 weights
+// and 8-bit states (6.4 TB/s).
 template <typename P, typename G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(const Piece* __restrict__ pieces, uint32_t tag, StepArgs a, const float* __restrict__ norm) {
     const Piece& pc = pieces[blockIdx.x];
@@ -538,7 +538,7 @@ ff_status adamw_step_run(const ff_adamw_desc& d, const void* plan, size_t plan_b
 }
 
 // ---- moments as float32 ------------------------------------------------------------------
-// 2 bytes read, 8 written a value: 49.1 M values 87 us, 5.6 TB/s.
+// 2 bytes read, 8 written a value: 49.1 M values 86 us, 5.7 TB/s.
 template <int BITS>
 __global__ __launch_bounds__(256) void k_moments(const Piece* __restrict__ pieces, uint32_t tag, float* __restrict__ m_out, float* __restrict__ v_out) {
     const Piece& pc = pieces[blockIdx.x];

@@ -154,7 +154,7 @@ template <int V, int ITERS, bool MASKED> struct Held {
 };
 
 // Two sums over a team, the second of squared distances from the mean that the first gives (in registers: no second reading, no cancellation).
-// 128 x 256 x 256 bfloat16 with the residual sum 12.4 us, 2048 x 2048 x 128 373 us (5.8 TB/s).
+// 128 x 256 x 256 bfloat16 with the residual sum 12.2 us, 2048 x 2048 x 128 368 us (5.9 TB/s).
 template <typename T, int V, int ITERS, bool MASKED, bool WIDE, bool STREAMED>
 __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_forward(
     const T* x, const T* residual, const T* __restrict__ gamma, const T* __restrict__ beta, T* sum, T* __restrict__ y,
@@ -230,8 +230,8 @@ __global__ __launch_bounds__(WIDE ? kWideThreads : kForwardThreads) void k_ln_fo
     }
 }
 
-// Bytes bound it: 2048 x 2048 x 128 bfloat16 in 574 us (5.6 TB/s), 612 where the statistics are formed again (four sums over a team one after
-// the other, not two); 5120 x 384 x 64 in 128 to 135 (5.6 to 5.9 TB/s), 128 x 256 x 256 with dsum in 14.6.  Sixteen wavefronts on a compute unit carry that: twice as many,
+// Bytes bound it: 2048 x 2048 x 128 bfloat16 in 572 us (5.6 TB/s), 610 where the statistics are formed again (four sums over a team one after
+// the other, not two); 5120 x 384 x 64 in 130 (5.8 TB/s), 128 x 256 x 256 with dsum in 14.7.  Sixteen wavefronts on a compute unit carry that: twice as many,
 // in registers or blocks, took longer (662), and each block more makes the second launch longer.
 // A block goes through its rows with the sums of dgamma and dbeta in registers (a lane's channels are the same in every row), joins them
 // over its teams and, in float64, its wavefronts in a fixed order and leaves 2 c float32 partial sums; with one block in all these are the result.
@@ -444,7 +444,8 @@ static Shape shape_of(int dtype, int c) {
 
 // Inputs of 160 MB to 1 GB are loaded past the caches, which hold 256 MB and then keep more of what is written for its reader: 5120 x 384 x 64
 // backward 144 -> 140 us, 196608 x 256 61 -> 55, with the gradient that passes by 77 -> 71.  Smaller ones may lie in the caches (65536 x 128 float32, 34 MB,
-// 13.6 -> 15.9), larger ones pass through them whole either way (2048 x 2048 x 128 forward 379 -> 386).
+// 13.6 -> 15.9), larger ones pass through them whole either way (2048 x 2048 x 128 forward 379 -> 386, the one
+// shape measured above 1 GB; 0.5 GB is the largest measured that gains, and where between them the rule should turn is not known).
 static bool streams(int64_t input_bytes) { return input_bytes > 160000000 && input_bytes < 1000000000; }
 
 template <typename F> static void with_shape(const Shape& s, int64_t input_bytes, F go) {
