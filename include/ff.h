@@ -388,6 +388,116 @@ ff_status ff_adamw_step(const ff_adamw_desc* desc, const void* plan, size_t plan
 ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t plan_bytes, float* m_out, float* v_out,
                            void* hip_stream);
 
+/* The gated transition, the feed-forward block behind the attention modules, with its gradients:
+ *   a = x Wa^T;  b = x Wb^T;  h = act(a) b;  y = h Wo^T (+ residual)
+ *   dh = dy Wo;  da = dh b act'(a);  db = dh act(a);  dx = da Wa + db Wb;  dWa = da^T x;  dWb = db^T x;  dWo = dy^T h
+ * act(a) is a sigmoid(a) (FF_SILU), a (1 + erf(a / sqrt 2)) / 2 (FF_GELU) or sigmoid(a) (FF_SIGMOID).  A row whose mask is 0 takes no part, whatever
+ * x and dy hold there: its y is the residual or 0, its dx 0, and it reaches no gradient of a weight.  The backward pass forms a, b and h again.
+ * All sums are float32.  Of bfloat16 tensors h, da and db are rounded to bfloat16 as operands of the following products.  Sums over rows
+ * are taken in an order that depends on the descriptor alone: equal calls give equal bits. */
+typedef enum { FF_SILU = 0, FF_GELU = 1, FF_SIGMOID = 2 } ff_act;
+
+typedef struct {
+    int32_t dtype;      /* ff_dtype of all tensors but the mask and, if asked for, the weights' gradients */
+    int32_t act;        /* ff_act */
+    int32_t c;          /* channels, 1 .. 8192 */
+    int32_t f;          /* hidden channels, 1 .. 32768 */
+    int64_t rows;       /* >= 0 */
+} ff_transition_desc;
+
+/* Bytes of device workspace (padded copies of weights and tokens, hidden tensors of some thousand rows, partial sums); 0 if desc is invalid. */
+size_t ff_gated_transition_forward_workspace_bytes(const ff_transition_desc* desc);
+size_t ff_gated_transition_backward_workspace_bytes(const ff_transition_desc* desc);
+
+/*   x            [rows, c];  w_a, w_b [f, c];  w_o [c, f]: aligned to their type (fastest 16-byte aligned, c and f multiples of 16)
+ *   residual     [rows, c] or NULL;  mask float32 [rows], 0 = masked, or NULL
+ *   y            [rows, c]; may be residual itself, must not overlap x, a weight or the mask
+ *   ws, ws_bytes device scratch, 256-byte aligned, at least the size above, that overlaps none of them
+ * Errors as for the other entry points. */
+ff_status ff_gated_transition_forward(const ff_transition_desc* desc, const void* x, const void* w_a, const void* w_b, const void* w_o,
+                                      const void* residual, const float* mask, void* y, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*   dy           [rows, c]
+ *   dx           [rows, c]; must not overlap an input
+ *   dw_a, dw_b [f, c], dw_o [c, f] of grad_dtype (ff_dtype); accumulate = 1 adds to what they hold, 0 overwrites it; overlap nothing
+ * rows = 0 gives zero gradients of the weights. */
+ff_status ff_gated_transition_backward(const ff_transition_desc* desc, const void* x, const void* w_a, const void* w_b, const void* w_o,
+                                       const void* dy, const float* mask, void* dx, void* dw_a, void* dw_b, void* dw_o, int32_t grad_dtype,
+                                       int32_t accumulate, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Orthogonalising a matrix by Newton-Schulz products: X = G / (|G| + eps) with the root of the sum of squares as norm, then `steps` times, with n the
+ * shorter side and A = X X^T [n, n] (X^T X for a matrix with more rows than columns):
+ *   X = a X + (b A + c A^2) X      (X (b A + c A^2))
+ * which brings all singular values near 1.  Norms are float64, sums float32; X, A and the polynomial are held as pairs of float16 values, 24
+ * significant bits together, with places for magnitudes below 255 (the usual coefficients 3.4445, -4.7750, 2.0315 keep singular values below 1.3; coefficients that let them
+ * grow past that give infinities). */
+typedef struct {
+    int32_t dtype;              /* ff_dtype of x and out */
+    int32_t count;              /* matrices, one after another, >= 0 */
+    int32_t rows, cols;         /* 1 .. 32768 */
+    int32_t steps;              /* 1 .. 64 */
+    double  a, b, c;            /* finite */
+    double  eps;                /* >= 0 */
+} ff_orthogonalise_desc;
+
+/* Bytes of device workspace; 0 if desc is invalid. */
+size_t ff_orthogonalise_workspace_bytes(const ff_orthogonalise_desc* desc);
+
+/*   x, out [count, rows, cols], aligned to their type; out may be x itself.  ws as for the other entry points. */
+ff_status ff_orthogonalise(const ff_orthogonalise_desc* desc, const void* x, void* out, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* The optimiser of a model's matrices (Muon): momentum whose matrices are orthogonalised.  Per matrix [rows, cols], with k = 1 or, if a norm is given,
+ * k = min(1, max_norm / (norm + 1e-6)):
+ *   m = beta m + (1 - beta) k g;   u = m, or beta m + (1 - beta) k g with the new m (nesterov)
+ *   w = w - lr (weight_decay w + s O),   O = u orthogonalised as above
+ *   s = sqrt(max(1, rows / cols)) (FF_MUON_SPECTRAL) or 0.2 sqrt(max(rows, cols)) (FF_MUON_RMS)
+ * w is the float32 parameter; or the float32 master copy of a bfloat16 parameter, which receives its rounding; or the bfloat16 parameter itself.
+ * All matrices are served by the same few launches, from a plan laid out once in host memory, of which the caller keeps a copy on the device as
+ * long as the addresses hold.  Tensors with other than two dimensions belong to ff_adamw_step. */
+typedef enum { FF_MUON_SPECTRAL = 0, FF_MUON_RMS = 1 } ff_muon_scale;
+
+typedef struct {
+    int32_t param_dtype;   /* ff_dtype of the parameters */
+    int32_t grad_dtype;    /* ff_dtype of the gradients */
+    int32_t n_tensors;     /* >= 0 */
+} ff_muon_desc;
+
+/* One matrix: dense device memory, each pointer aligned to its own type. */
+typedef struct {
+    void*       p;             /* [rows, cols] param_dtype */
+    const void* g;             /* [rows, cols] grad_dtype */
+    float*      master;        /* [rows, cols], FF_BF16 parameters only; NULL = none */
+    float*      m;             /* [rows, cols] */
+    int32_t     rows, cols;    /* 0 .. 32768; a matrix without values is left out */
+    float       weight_decay;  /* >= 0 */
+} ff_muon_tensor;
+
+typedef struct {
+    double  lr, beta;          /* lr >= 0; 0 <= beta < 1 */
+    double  max_norm;          /* > 0; read only if a norm is given */
+    double  a, b, c, eps;      /* as in ff_orthogonalise_desc */
+    int32_t steps;
+    int32_t nesterov;          /* 0 or 1 */
+    int32_t scale;             /* ff_muon_scale */
+} ff_muon_hyper;
+
+/* Bytes of the plan for these matrices (host array of desc->n_tensors entries); 0 if an argument is invalid. */
+size_t ff_muon_plan_bytes(const ff_muon_desc* desc, const ff_muon_tensor* tensors);
+
+/* Writes the plan into host memory (plan_bytes as reported above, 8-byte aligned).  Gradients may share memory; a tensor that the step writes and that overlaps
+ * another one is refused (FF_EINVAL). */
+ff_status ff_muon_plan(const ff_muon_desc* desc, const ff_muon_tensor* tensors, void* plan, size_t plan_bytes);
+
+/* Bytes of device workspace a step over this plan (host memory) needs; 0 if it is none of this descriptor. */
+size_t ff_muon_workspace_bytes(const ff_muon_desc* desc, const void* plan_host, size_t plan_bytes);
+
+/* One step over all matrices of the plan.  plan_host: the plan as ff_muon_plan wrote it; plan: its copy on the device, 16-byte aligned.  norm: device, or NULL
+ * for gradients as they are (ff_grad_norm gives one; it may be that of more tensors than these); a norm that is not finite leaves weights and momentum as
+ * they were.  plan_host and hyper are read before the call returns; a captured call repeats its hyper at every replay.  ws, 256-byte aligned, must overlap neither the
+ * plan nor the norm (FF_EINVAL), nor a tensor (whose addresses are not looked through here). */
+ff_status ff_muon_step(const ff_muon_desc* desc, const void* plan_host, const void* plan, size_t plan_bytes, const ff_muon_hyper* hyper,
+                       const float* norm, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* For callers that cannot allocate: code under HIP graph capture, tight serving loops and
  * harnesses that forbid hipMalloc, which therefore have no workspace to hand over.
  * The same module as ff_attention_chunked, with the workspace taken from a device array that is

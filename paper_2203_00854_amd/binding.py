@@ -82,6 +82,34 @@ class AdamWHyper(C.Structure):
     _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "max_norm")] + [("step", C.c_int64), ("seed", C.c_uint32)]
 
 
+FF_SILU, FF_GELU, FF_SIGMOID = range(3)
+FF_MUON_SPECTRAL, FF_MUON_RMS = range(2)
+ACTS = {"silu": FF_SILU, "gelu": FF_GELU, "sigmoid": FF_SIGMOID}
+SCALES = {"spectral": FF_MUON_SPECTRAL, "rms": FF_MUON_RMS}
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)       # of the polynomial a X + b X X^T X + c (X X^T)^2 X
+
+
+class TransitionDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("c", C.c_int32), ("f", C.c_int32), ("rows", C.c_int64)]
+
+
+class OrthogonaliseDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("count", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("steps", C.c_int32), ("a", C.c_double), ("b", C.c_double),
+                ("c", C.c_double), ("eps", C.c_double)]
+
+
+class MuonDesc(C.Structure):
+    _fields_ = [("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("n_tensors", C.c_int32)]
+
+
+class MuonTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("p", "g", "master", "m")] + [("rows", C.c_int32), ("cols", C.c_int32), ("weight_decay", C.c_float)]
+
+
+class MuonHyper(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta", "max_norm", "a", "b", "c", "eps")] + [(n, C.c_int32) for n in ("steps", "nesterov", "scale")]
+
+
 class FFError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"libff status {status}: {message}")
@@ -150,6 +178,26 @@ def lib() -> C.CDLL:
         L.ff_adamw_step.argtypes = [C.POINTER(AdamWDesc), C.c_void_p, C.c_size_t, C.POINTER(AdamWHyper), C.c_void_p, C.c_void_p]
         L.ff_adamw_moments.restype = C.c_int
         L.ff_adamw_moments.argtypes = [C.POINTER(AdamWDesc), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.ff_gated_transition_forward_workspace_bytes.restype = C.c_size_t
+        L.ff_gated_transition_forward_workspace_bytes.argtypes = [C.POINTER(TransitionDesc)]
+        L.ff_gated_transition_backward_workspace_bytes.restype = C.c_size_t
+        L.ff_gated_transition_backward_workspace_bytes.argtypes = [C.POINTER(TransitionDesc)]
+        L.ff_gated_transition_forward.restype = C.c_int
+        L.ff_gated_transition_forward.argtypes = [C.POINTER(TransitionDesc)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        L.ff_gated_transition_backward.restype = C.c_int
+        L.ff_gated_transition_backward.argtypes = [C.POINTER(TransitionDesc)] + [C.c_void_p] * 10 + [C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ff_orthogonalise_workspace_bytes.restype = C.c_size_t
+        L.ff_orthogonalise_workspace_bytes.argtypes = [C.POINTER(OrthogonaliseDesc)]
+        L.ff_orthogonalise.restype = C.c_int
+        L.ff_orthogonalise.argtypes = [C.POINTER(OrthogonaliseDesc)] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+        L.ff_muon_plan_bytes.restype = C.c_size_t
+        L.ff_muon_plan_bytes.argtypes = [C.POINTER(MuonDesc), C.c_void_p]
+        L.ff_muon_plan.restype = C.c_int
+        L.ff_muon_plan.argtypes = [C.POINTER(MuonDesc), C.c_void_p, C.c_void_p, C.c_size_t]
+        L.ff_muon_workspace_bytes.restype = C.c_size_t
+        L.ff_muon_workspace_bytes.argtypes = [C.POINTER(MuonDesc), C.c_void_p, C.c_size_t]
+        L.ff_muon_step.restype = C.c_int
+        L.ff_muon_step.argtypes = [C.POINTER(MuonDesc), C.c_void_p, C.c_void_p, C.c_size_t, C.POINTER(MuonHyper), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.ff_attention_path.restype = C.c_char_p
         L.ff_attention_path.argtypes = [C.POINTER(AttnDesc)]
         L.ff_attention_last_path.restype = C.c_char_p
@@ -574,6 +622,134 @@ def ff_adamw_moments(plan: AdamWPlan, m=None, v=None):
     if v is not None and plan.meets(("m", "v", "m_exp", "v_exp"), v):
         raise ValueError("v shares memory with a state of the plan")
     return _done(calls().adamw_moments(C.addressof(plan.desc), plan.plan, plan.values, m, v, plan.stream))
+
+
+# ------------------------------------------------------------------------- the gated transition
+def _named(table, name, what):
+    if name not in table:
+        raise ValueError(f"{what} is one of {', '.join(table)}, not {name!r}")
+    return table[name]
+
+
+def ff_gated_transition_forward(x, w_a, w_b, w_o, act: str = "silu", residual=None, mask=None, out=None, ws=None):
+    """y = (act(x w_a^T) * (x w_b^T)) w_o^T (+ residual) over the last axis of x; w_a, w_b [f, c], w_o [c, f]; act: "silu", "gelu" or "sigmoid".
+    mask: float32 of x's leading shape; a row whose mask is 0 gives the residual or 0, whatever it holds.  out may be residual itself."""
+    return _done(calls().transition_forward(x, w_a, w_b, w_o, _named(ACTS, act, "act"), residual, mask, out, ws))
+
+
+def ff_gated_transition_backward(x, w_a, w_b, w_o, dy, act: str = "silu", mask=None, dx=None, dw_a=None, dw_b=None, dw_o=None, grad_dtype=None,
+                                 accumulate: bool = False, ws=None):
+    """Gradients of ff_gated_transition_forward (without the residual, whose gradient is dy); returns (dx, dw_a, dw_b, dw_o).  The hidden layer is
+    formed again from x.  grad_dtype: of the weights' gradients, float32 or bfloat16 (None: the given dw_a's, or the weights').
+    accumulate adds to the given dw_a, dw_b and dw_o."""
+    import torch
+    wide = -1 if grad_dtype is None else {torch.bfloat16: 0, torch.float32: 1}.get(grad_dtype)
+    if wide is None:
+        raise TypeError(f"unsupported grad_dtype {grad_dtype}")
+    return _done(calls().transition_backward(x, w_a, w_b, w_o, dy, _named(ACTS, act, "act"), mask, dx, dw_a, dw_b, dw_o, wide, accumulate, ws))
+
+
+def ff_gated_transition_forward_workspace_bytes(desc: TransitionDesc) -> int:
+    n = lib().ff_gated_transition_forward_workspace_bytes(C.byref(desc))
+    if n == 0:
+        raise FFError(FF_EINVAL, last_error())
+    return n
+
+
+def ff_gated_transition_backward_workspace_bytes(desc: TransitionDesc) -> int:
+    n = lib().ff_gated_transition_backward_workspace_bytes(C.byref(desc))
+    if n == 0:
+        raise FFError(FF_EINVAL, last_error())
+    return n
+
+
+# ------------------------------------------------------------------------- orthogonalising, Muon
+def ff_orthogonalise(x, steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7, out=None, ws=None):
+    """The matrices x [..., rows, cols] with their singular values brought near 1 by Newton-Schulz products: X = x / (|x| + eps), then `steps` times
+    a X + (b A + c A^2) X with A = X X^T (on the shorter side).  out may be x itself."""
+    a, b, c = coefficients
+    return _done(calls().orthogonalise(x, steps, a, b, c, eps, out, ws))
+
+
+def ff_orthogonalise_workspace_bytes(desc: OrthogonaliseDesc) -> int:
+    n = lib().ff_orthogonalise_workspace_bytes(C.byref(desc))
+    if n == 0:
+        raise FFError(FF_EINVAL, last_error())
+    return n
+
+
+class MuonPlan:
+    """The matrices of a model laid out for ff_muon_step, with its workspace.  It holds their addresses (and the tensors): a gradient that is allocated anew
+    needs a new plan, one that is written in place does not."""
+
+    def __init__(self, desc, table, tensors, device):
+        import numpy as np
+        import torch
+        self.desc, self.tensors, self.device = desc, tensors, device
+        n = lib().ff_muon_plan_bytes(C.byref(desc), table)
+        if n == 0:
+            raise FFError(FF_EINVAL, last_error())
+        self.host = np.empty(n, np.uint8)
+        _check(lib().ff_muon_plan(C.byref(desc), table, self.host.ctypes.data, n))
+        self.plan = torch.from_numpy(self.host).to(device)
+        self.ws = _alloc_ws(lib().ff_muon_workspace_bytes(C.byref(desc), self.host.ctypes.data, n), device)
+        self.stream = torch.cuda.current_stream(device).cuda_stream          # the one that the two belong to
+
+
+def make_muon_plan(params, grads, m, master=None, weight_decay=0.0) -> MuonPlan:
+    """A plan for ff_muon_step.  params, grads: matrices; m: float32 of the parameters' sizes (muon_states allocates it).  master: float32
+    copies of bfloat16 parameters.  weight_decay: a number, or one for each matrix."""
+    import numpy as np
+    import torch
+    lists = {"p": list(params), "g": list(grads), "m": list(m)}
+    if master is not None:
+        lists["master"] = list(master)
+    params, grads = lists["p"], lists["g"]
+    if not params or not grads:
+        raise ValueError("a plan needs a tensor")
+    count, device = len(params), params[0].device
+    dtypes = {"p": params[0].dtype, "g": grads[0].dtype, "m": torch.float32, "master": torch.float32}
+    shapes = [tuple(t.shape) for t in params]
+    for i, s in enumerate(shapes):
+        if len(s) != 2:
+            raise ValueError(f"tensor {i} has shape {list(s)}: it is no matrix")
+        if max(s) > 32768:
+            raise ValueError(f"tensor {i} has shape {list(s)}: rows and columns go up to 32768")
+    table = np.zeros(count, np.dtype(MuonTensor))
+    for name, ts in lists.items():
+        if len(ts) != count:
+            raise ValueError(f"{len(ts)} tensors of {name} for {count} parameters")
+        for t, s in zip(ts, shapes):
+            if t.dtype != dtypes[name]:
+                raise TypeError(f"{name} is {t.dtype}, not {dtypes[name]}")
+            if tuple(t.shape) != s:
+                raise ValueError(f"{name} has shape {list(t.shape)}, not {list(s)}")
+            if not t.is_cuda or t.device != device:
+                raise ValueError(f"{name} is on {t.device}, not on {device if device.type == 'cuda' else 'a GPU'}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} is not contiguous")
+        table[name] = [t.data_ptr() for t in ts]
+    table["rows"], table["cols"] = [s[0] for s in shapes], [s[1] for s in shapes]
+    if np.ndim(weight_decay) and len(weight_decay) != count:
+        raise ValueError(f"{len(weight_decay)} values of weight_decay for {count} parameters")
+    table["weight_decay"] = weight_decay
+    return MuonPlan(MuonDesc(_dtype_code(params[0]), _dtype_code(grads[0]), count), table.ctypes.data, (table, lists), device)
+
+
+def muon_states(params):
+    """Zero momenta for make_muon_plan: {"m"}."""
+    import torch
+    return {"m": [torch.zeros(t.shape, dtype=torch.float32, device=t.device) for t in params]}
+
+
+def ff_muon_step(plan: MuonPlan, lr: float, beta: float = 0.95, nesterov: bool = True, steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7,
+                 scale: str = "spectral", norm=None, max_norm=None, ws=None):
+    """One Muon step over the plan's matrices, in place.  scale of the orthogonalised update: "spectral", sqrt(max(1, rows / cols)), or "rms", 0.2
+    sqrt(max(rows, cols)).  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm that is not finite leaves everything as it
+    was.  The plan's own workspace serves one stream at a time; give ws for another.  Captured into a graph the call keeps its numbers as they are."""
+    a, b, c = coefficients
+    hyper = MuonHyper(lr, beta, 0.0 if max_norm is None else max_norm, a, b, c, eps, steps, 1 if nesterov else 0, _named(SCALES, scale, "scale"))
+    _done(calls().muon_step(C.addressof(plan.desc), plan.host.ctypes.data, plan.plan, C.addressof(hyper), norm, max_norm, plan.ws if ws is None else ws, plan.stream))
 
 
 def ff_profile_enable(on: bool):

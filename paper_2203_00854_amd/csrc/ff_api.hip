@@ -24,7 +24,8 @@ static const char* kKindNames[KK_COUNT] = {"k_prep", "pair bias pass", "k_gemm<P
                                            "k_gca_kv", "k_gca_softmax", "k_gca_out",
                                            "k_bwd_stats", "k_bwd_dq", "k_bwd_dkv", "k_bwd_dbias", "probe: vector loop",
                                            "k_proj_attn", "k_bwd_rows", "k_bwd_prepare", "k_bwd_dbias_reduce", "k_ln_forward",
-                                           "k_ln_backward", "k_ln_join", "k_grad_norm", "k_adamw", "k_moments"};
+                                           "k_ln_backward", "k_ln_join", "k_grad_norm", "k_adamw", "k_moments", "k_tr_pack", "k_tr_hidden", "k_tr_out",
+                                           "k_tr_grad", "k_tr_weights", "k_tr_join", "k_muon_momentum", "k_ns_start", "k_ns_gram", "k_ns_poly", "k_ns_apply"};
 
 static hipEvent_t prof_event() {
     if (!g_prof_pool.empty()) {
@@ -568,6 +569,197 @@ ff_status ff_adamw_moments(const ff_adamw_desc* desc, const void* plan, size_t p
     if ((m_out && overlaps(m_out, least, plan, plan_bytes)) || (v_out && overlaps(v_out, least, plan, plan_bytes)))
         return fail(FF_EINVAL, "m_out or v_out overlaps the plan");
     return adamw_moments_run(*desc, plan, plan_bytes, m_out, v_out, (hipStream_t)hip_stream);
+}
+
+// ---- the gated transition
+static ff_status check_transition(const ff_transition_desc* d) {
+    if (!d) return fail(FF_EINVAL, "desc is NULL");
+    if (d->dtype != FF_F32 && d->dtype != FF_BF16) return fail(FF_EINVAL, "bad dtype %d", d->dtype);
+    if (d->act != FF_SILU && d->act != FF_GELU && d->act != FF_SIGMOID) return fail(FF_EINVAL, "bad act %d", d->act);
+    if (d->c < 1 || d->c > 8192) return fail(FF_EINVAL, "c must be in 1 .. 8192 (got %d)", d->c);
+    if (d->f < 1 || d->f > 32768) return fail(FF_EINVAL, "f must be in 1 .. 32768 (got %d)", d->f);
+    if (d->rows < 0 || d->rows > (int64_t)1 << 40 || d->rows * d->c > (int64_t)1 << 40) return fail(FF_EINVAL, "bad number of rows %lld", (long long)d->rows);
+    return FF_OK;
+}
+static ff_status check_ws(const void* ws, size_t given, size_t need) {
+    if (!ws) return fail(FF_EINVAL, "workspace is NULL (%zu bytes needed)", need);
+    if (((uintptr_t)ws & 255u) != 0) return fail(FF_EINVAL, "workspace must be 256-byte aligned");
+    if (given < need) return fail(FF_EWORKSPACE, "workspace too small: %zu bytes given, %zu needed", given, need);
+    return FF_OK;
+}
+namespace {
+struct Span {
+    const void* p;
+    size_t n;
+    const char* name;
+};
+}  // namespace
+// outputs overlap neither each other nor an input, but for the one that may be that input itself
+static ff_status check_spans(const Span* out, int n_out, const Span* in, int n_in, const void* same_out = nullptr, const void* same_in = nullptr) {
+    for (int i = 0; i < n_out; ++i) {
+        if (!out[i].p || !out[i].n) continue;
+        for (int j = 0; j < i; ++j)
+            if (out[j].p && overlaps(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(FF_EINVAL, "%s overlaps %s", out[i].name, out[j].name);
+        for (int j = 0; j < n_in; ++j)
+            if (in[j].p && in[j].n && !(out[i].p == same_out && in[j].p == same_in && same_out == same_in) && overlaps(out[i].p, out[i].n, in[j].p, in[j].n))
+                return fail(FF_EINVAL, "%s overlaps %s", out[i].name, in[j].name);
+    }
+    return FF_OK;
+}
+
+size_t ff_gated_transition_forward_workspace_bytes(const ff_transition_desc* desc) {
+    return check_transition(desc) == FF_OK ? transition_forward_workspace(*desc) : 0;
+}
+size_t ff_gated_transition_backward_workspace_bytes(const ff_transition_desc* desc) {
+    return check_transition(desc) == FF_OK ? transition_backward_workspace(*desc) : 0;
+}
+
+ff_status ff_gated_transition_forward(const ff_transition_desc* desc, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
+                                      const float* mask, void* y, void* ws, size_t ws_bytes, void* hip_stream) {
+    ff_status st = check_transition(desc);
+    if (st != FF_OK) return st;
+    if (desc->rows == 0) return FF_OK;
+    if (!x || !w_a || !w_b || !w_o || !y) return fail(FF_EINVAL, "NULL pointer");
+    const size_t esz = desc->dtype == FF_F32 ? 4 : 2, n = (size_t)desc->rows * desc->c * esz, wn = (size_t)desc->c * desc->f * esz;
+    for (const void* p : {x, w_a, w_b, w_o, residual, (const void*)y})
+        if (!aligned_to(p, esz)) return fail(FF_EINVAL, "a pointer is not aligned to its type");
+    if (!aligned_to(mask, 4)) return fail(FF_EINVAL, "mask must be 4-byte aligned");
+    const size_t need = transition_forward_workspace(*desc);
+    if ((st = check_ws(ws, ws_bytes, need)) != FF_OK) return st;
+    const Span in[] = {{x, n, "x"}, {w_a, wn, "w_a"}, {w_b, wn, "w_b"}, {w_o, wn, "w_o"}, {mask, (size_t)desc->rows * 4, "mask"}};
+    const Span out[] = {{y, n, "y"}, {ws, need, "the workspace"}}, kept[] = {{residual, n, "residual"}};
+    if ((st = check_spans(out, 2, in, 5)) != FF_OK) return st;
+    if ((st = check_spans(out, 2, kept, 1, y, residual)) != FF_OK) return st;
+    return transition_forward_run(*desc, x, w_a, w_b, w_o, residual, mask, y, ws, (hipStream_t)hip_stream);
+}
+
+ff_status ff_gated_transition_backward(const ff_transition_desc* desc, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
+                                       const float* mask, void* dx, void* dw_a, void* dw_b, void* dw_o, int32_t grad_dtype, int32_t accumulate, void* ws,
+                                       size_t ws_bytes, void* hip_stream) {
+    ff_status st = check_transition(desc);
+    if (st != FF_OK) return st;
+    if (grad_dtype != FF_F32 && grad_dtype != FF_BF16) return fail(FF_EINVAL, "bad grad_dtype %d", grad_dtype);
+    if (accumulate != 0 && accumulate != 1) return fail(FF_EINVAL, "accumulate must be 0 or 1 (got %d)", accumulate);
+    if (!w_a || !w_b || !w_o || !dw_a || !dw_b || !dw_o || (desc->rows > 0 && (!x || !dy || !dx))) return fail(FF_EINVAL, "NULL pointer");
+    const size_t esz = desc->dtype == FF_F32 ? 4 : 2, gsz = grad_dtype == FF_F32 ? 4 : 2, n = (size_t)desc->rows * desc->c * esz,
+                 wn = (size_t)desc->c * desc->f * esz, gn = (size_t)desc->c * desc->f * gsz;
+    for (const void* p : {x, w_a, w_b, w_o, dy, (const void*)dx})
+        if (!aligned_to(p, esz)) return fail(FF_EINVAL, "a pointer is not aligned to its type");
+    for (const void* p : {dw_a, dw_b, dw_o})
+        if (!aligned_to(p, gsz)) return fail(FF_EINVAL, "a gradient is not aligned to its type");
+    if (!aligned_to(mask, 4)) return fail(FF_EINVAL, "mask must be 4-byte aligned");
+    const size_t need = transition_backward_workspace(*desc);
+    if ((st = check_ws(ws, ws_bytes, need)) != FF_OK) return st;
+    const Span in[] = {{x, n, "x"}, {w_a, wn, "w_a"}, {w_b, wn, "w_b"}, {w_o, wn, "w_o"}, {dy, n, "dy"}, {mask, (size_t)desc->rows * 4, "mask"}};
+    const Span out[] = {{dx, n, "dx"}, {dw_a, gn, "dw_a"}, {dw_b, gn, "dw_b"}, {dw_o, gn, "dw_o"}, {ws, need, "the workspace"}};
+    if ((st = check_spans(out, 5, in, 6)) != FF_OK) return st;
+    return transition_backward_run(*desc, x, w_a, w_b, w_o, dy, mask, dx, dw_a, dw_b, dw_o, grad_dtype, accumulate != 0, ws, (hipStream_t)hip_stream);
+}
+
+// ---- orthogonalising, the optimiser of matrices
+static bool is_finite(double v) { return v - v == 0.; }
+static ff_status check_polynomial(double a, double b, double c, double eps, int steps) {
+    if (!is_finite((float)a) || !is_finite((float)b) || !is_finite((float)c)) return fail(FF_EINVAL, "a, b and c must be finite");
+    if (!(eps >= 0.) || !is_finite(eps)) return fail(FF_EINVAL, "eps must be finite and >= 0");
+    if (steps < 1 || steps > 64) return fail(FF_EINVAL, "steps must be in 1 .. 64 (got %d)", steps);
+    return FF_OK;
+}
+static ff_status check_orthogonalise(const ff_orthogonalise_desc* d) {
+    if (!d) return fail(FF_EINVAL, "desc is NULL");
+    if (d->dtype != FF_F32 && d->dtype != FF_BF16) return fail(FF_EINVAL, "bad dtype %d", d->dtype);
+    if (d->rows < 1 || d->rows > 32768 || d->cols < 1 || d->cols > 32768) return fail(FF_EINVAL, "rows and cols must be in 1 .. 32768 (got %d, %d)", d->rows, d->cols);
+    if (d->count < 0 || (int64_t)d->count * d->rows * d->cols > (int64_t)1 << 36) return fail(FF_EINVAL, "bad number of matrices %d", d->count);
+    return check_polynomial(d->a, d->b, d->c, d->eps, d->steps);
+}
+size_t ff_orthogonalise_workspace_bytes(const ff_orthogonalise_desc* desc) {
+    return check_orthogonalise(desc) == FF_OK ? orthogonalise_workspace(*desc) : 0;
+}
+ff_status ff_orthogonalise(const ff_orthogonalise_desc* desc, const void* x, void* out, void* ws, size_t ws_bytes, void* hip_stream) {
+    ff_status st = check_orthogonalise(desc);
+    if (st != FF_OK) return st;
+    if (desc->count == 0) return FF_OK;
+    if (!x || !out) return fail(FF_EINVAL, "NULL pointer");
+    const size_t esz = desc->dtype == FF_F32 ? 4 : 2, n = (size_t)desc->count * desc->rows * desc->cols * esz;
+    if (!aligned_to(x, esz) || !aligned_to(out, esz)) return fail(FF_EINVAL, "a pointer is not aligned to its type");
+    const size_t need = orthogonalise_workspace(*desc);
+    if ((st = check_ws(ws, ws_bytes, need)) != FF_OK) return st;
+    const Span in[] = {{x, n, "x"}}, outs[] = {{out, n, "out"}, {ws, need, "the workspace"}};
+    if ((st = check_spans(outs, 2, in, 1, out, x)) != FF_OK) return st;
+    return orthogonalise_run(*desc, x, out, ws, (hipStream_t)hip_stream);
+}
+
+static ff_status check_muon(const ff_muon_desc* d) {
+    if (!d) return fail(FF_EINVAL, "desc is NULL");
+    if (d->param_dtype != FF_F32 && d->param_dtype != FF_BF16) return fail(FF_EINVAL, "bad param_dtype %d", d->param_dtype);
+    if (d->grad_dtype != FF_F32 && d->grad_dtype != FF_BF16) return fail(FF_EINVAL, "bad grad_dtype %d", d->grad_dtype);
+    if (d->n_tensors < 0) return fail(FF_EINVAL, "n_tensors must be >= 0 (got %d)", d->n_tensors);
+    return FF_OK;
+}
+static ff_status check_matrices(const ff_muon_desc* d, const ff_muon_tensor* ts) {
+    ff_status st = check_muon(d);
+    if (st != FF_OK) return st;
+    if (d->n_tensors > 0 && !ts) return fail(FF_EINVAL, "tensors is NULL");
+    int64_t total = 0;
+    for (int i = 0; i < d->n_tensors; ++i) {
+        const ff_muon_tensor& t = ts[i];
+        if (t.rows < 0 || t.cols < 0 || t.rows > 32768 || t.cols > 32768) return fail(FF_EINVAL, "tensor %d: rows and cols must be in 0 .. 32768 (got %d, %d)", i, t.rows, t.cols);
+        if (t.rows == 0 || t.cols == 0) continue;
+        if ((total += (int64_t)t.rows * t.cols) > (int64_t)1 << 40) return fail(FF_EINVAL, "too many values");
+        if (!t.p || !t.g || !t.m) return fail(FF_EINVAL, "tensor %d: p, g or m is NULL", i);
+        if (!aligned_to(t.p, d->param_dtype == FF_F32 ? 4 : 2) || !aligned_to(t.g, d->grad_dtype == FF_F32 ? 4 : 2) || !aligned_to(t.m, 4))
+            return fail(FF_EINVAL, "tensor %d: p, g or m is misaligned", i);
+        if (t.master && (d->param_dtype != FF_BF16 || !aligned_to(t.master, 4)))
+            return fail(FF_EINVAL, "tensor %d: master belongs to bfloat16 parameters and is 4-byte aligned", i);
+        if (!(t.weight_decay >= 0.f) || t.weight_decay > 1e30f) return fail(FF_EINVAL, "tensor %d: weight_decay must be finite and >= 0", i);
+    }
+    return FF_OK;
+}
+size_t ff_muon_plan_bytes(const ff_muon_desc* desc, const ff_muon_tensor* tensors) {
+    if (check_matrices(desc, tensors) != FF_OK) return 0;
+    const size_t bytes = muon_plan_size(*desc, tensors);
+    if (!bytes) fail(FF_EINVAL, "no host memory for %d matrices, or too many of them", desc->n_tensors);
+    return bytes;
+}
+ff_status ff_muon_plan(const ff_muon_desc* desc, const ff_muon_tensor* tensors, void* plan, size_t plan_bytes) {
+    ff_status st = check_matrices(desc, tensors);
+    if (st != FF_OK) return st;
+    const size_t need = muon_plan_size(*desc, tensors);
+    if (!need) return fail(FF_EINVAL, "no host memory for %d matrices, or too many of them", desc->n_tensors);
+    if (!plan || !aligned_to(plan, 8)) return fail(FF_EINVAL, "plan is NULL or misaligned");
+    if (plan_bytes != need) return fail(FF_EWORKSPACE, "the plan has %zu bytes, %zu given", need, plan_bytes);
+    const int found = muon_plan_fill(*desc, tensors, plan);
+    if (found < 0) return fail(FF_EINVAL, "no host memory for %d matrices", desc->n_tensors);
+    if (found) return fail(FF_EINVAL, "a tensor that the step writes overlaps another one of the plan");
+    return FF_OK;
+}
+static ff_status check_muon_plan(const ff_muon_desc* desc, const void* plan_host, size_t plan_bytes) {
+    ff_status st = check_muon(desc);
+    if (st != FF_OK) return st;
+    if (!plan_host || !aligned_to(plan_host, 8)) return fail(FF_EINVAL, "plan_host is NULL or misaligned");
+    if (!muon_plan_whole(*desc, plan_host, plan_bytes)) return fail(FF_EINVAL, "this is no plan of this descriptor");
+    return FF_OK;
+}
+size_t ff_muon_workspace_bytes(const ff_muon_desc* desc, const void* plan_host, size_t plan_bytes) {
+    return check_muon_plan(desc, plan_host, plan_bytes) == FF_OK ? muon_workspace(plan_host) : 0;
+}
+ff_status ff_muon_step(const ff_muon_desc* desc, const void* plan_host, const void* plan, size_t plan_bytes, const ff_muon_hyper* h, const float* norm, void* ws,
+                       size_t ws_bytes, void* hip_stream) {
+    ff_status st = check_muon_plan(desc, plan_host, plan_bytes);
+    if (st != FF_OK) return st;
+    if (!plan || !aligned16(plan)) return fail(FF_EINVAL, "plan is NULL or not 16-byte aligned");
+    if (!h) return fail(FF_EINVAL, "hyper is NULL");
+    if (!(h->lr >= 0.) || h->lr > 1e30) return fail(FF_EINVAL, "lr must be finite and >= 0");
+    if (!(h->beta >= 0.) || !(h->beta < 1.)) return fail(FF_EINVAL, "beta must be in [0, 1)");
+    if (h->nesterov != 0 && h->nesterov != 1) return fail(FF_EINVAL, "nesterov must be 0 or 1 (got %d)", h->nesterov);
+    if (h->scale != FF_MUON_SPECTRAL && h->scale != FF_MUON_RMS) return fail(FF_EINVAL, "bad scale %d", h->scale);
+    if ((st = check_polynomial(h->a, h->b, h->c, h->eps, h->steps)) != FF_OK) return st;
+    if (norm && (!(h->max_norm > 0.) || h->max_norm > 1e30)) return fail(FF_EINVAL, "max_norm must be finite and > 0");
+    if (!aligned_to(norm, 4)) return fail(FF_EINVAL, "norm is misaligned");
+    const size_t need = muon_workspace(plan_host);
+    if ((st = check_ws(ws, ws_bytes, need)) != FF_OK) return st;
+    const Span in[] = {{plan, plan_bytes, "the plan"}, {norm, 4, "norm"}}, out[] = {{ws, need, "the workspace"}};
+    if ((st = check_spans(out, 1, in, 2)) != FF_OK) return st;
+    return muon_step_run(*desc, plan_host, plan, *h, norm, ws, (hipStream_t)hip_stream);
 }
 
 size_t ff_attention_workspace_bytes(const ff_attn_desc* desc, int32_t chunk_rows) {

@@ -243,11 +243,156 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+struct Transition {
+    ff_transition_desc desc;
+    at::ScalarType dtype;
+    at::Device device;
+    at::IntArrayRef shape, rows;
+    int64_t in[2], back[2];                    // shapes of w_a and w_b, of w_o
+    Transition(const at::Tensor& x, const at::Tensor& w_a, const at::Tensor& w_b, const at::Tensor& w_o, const at::Tensor& mask, long act)
+        : dtype(x.scalar_type()), device(x.device()), shape(x.sizes()) {
+        if (shape.empty() || shape.back() < 1) value_error("no channels in shape ", shape);
+        if (!x.is_cuda()) value_error("x is on ", device, ", not on a GPU");
+        if (!x.is_contiguous()) value_error("x is not contiguous");
+        if (dtype != at::kFloat && dtype != at::kBFloat16) type_error("unsupported dtype ", dtype);
+        if (w_a.dim() != 2 || w_a.size(0) < 1) value_error("w_a has shape ", w_a.sizes(), ", not [hidden channels, channels]");
+        rows = shape.slice(0, shape.size() - 1);
+        in[0] = back[1] = w_a.size(0);
+        in[1] = back[0] = shape.back();
+        if (in[0] > INT32_MAX || in[1] > INT32_MAX) value_error("too many channels in shapes ", shape, " and ", w_a.sizes());
+        fit(w_a, "w_a", dtype, in, device);
+        fit(w_b, "w_b", dtype, in, device);
+        fit(w_o, "w_o", dtype, back, device);
+        fit_optional(mask, "mask", at::kFloat, rows, device);
+        desc = ff_transition_desc{dtype == at::kFloat ? FF_F32 : FF_BF16, (int32_t)act, (int32_t)in[1], (int32_t)in[0], x.numel() / in[1]};
+    }
+};
+// the given workspace, checked, or a new one
+void workspace(at::Tensor& ws, size_t bytes, at::Device device) {
+    if (ws.defined()) {
+        if (ws.device() != device || !ws.is_contiguous()) value_error("ws is on ", ws.device(), " or not contiguous");
+    } else
+        ws = at::empty((int64_t)bytes, at::TensorOptions().dtype(at::kByte).device(device));
+}
+
+// x, w_a, w_b, w_o, act, residual, mask, out, ws -> y
+PyObject* transition_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("transition_forward", 9, n, [&]() -> PyObject* {
+        const at::Tensor x = tensor(a[0], "x"), w_a = tensor(a[1], "w_a"), w_b = tensor(a[2], "w_b"), w_o = tensor(a[3], "w_o"), residual = optional(a[5], "residual"),
+                         mask = optional(a[6], "mask");
+        const long act = PyLong_AsLong(a[4]);
+        if (PyErr_Occurred()) return nullptr;
+        at::Tensor y = optional(a[7], "out"), ws = optional(a[8], "ws");
+        const Transition t(x, w_a, w_b, w_o, mask, act);
+        fit_optional(residual, "residual", t.dtype, t.shape, t.device);
+        ff_status status;
+        {
+            Unlocked unlocked;
+            const c10::DeviceGuard guard(t.device);
+            result(y, "out", t.dtype, t.shape, t.device);
+            workspace(ws, ff_gated_transition_forward_workspace_bytes(&t.desc), t.device);
+            status = ff_gated_transition_forward(&t.desc, in(x), in(w_a), in(w_b), in(w_o), in(residual), (const float*)in(mask), out(y), out(ws), ws.nbytes(),
+                                                 c10::hip::getCurrentHIPStream(t.device.index()).stream());
+        }
+        return status == FF_OK ? THPVariable_Wrap(y) : PyLong_FromLong(status);
+    });
+}
+
+// x, w_a, w_b, w_o, dy, act, mask, dx, dw_a, dw_b, dw_o, whether their gradients are float32 (-1: as the weights), accumulate, ws -> (dx, dw_a, dw_b, dw_o)
+PyObject* transition_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("transition_backward", 14, n, [&]() -> PyObject* {
+        const at::Tensor x = tensor(a[0], "x"), w_a = tensor(a[1], "w_a"), w_b = tensor(a[2], "w_b"), w_o = tensor(a[3], "w_o"), dy = tensor(a[4], "dy"),
+                         mask = optional(a[6], "mask");
+        const long act = PyLong_AsLong(a[5]), wide = PyLong_AsLong(a[11]);
+        const int accumulate = PyObject_IsTrue(a[12]);
+        if (PyErr_Occurred()) return nullptr;
+        at::Tensor dx = optional(a[7], "dx"), dw_a = optional(a[8], "dw_a"), dw_b = optional(a[9], "dw_b"), dw_o = optional(a[10], "dw_o"), ws = optional(a[13], "ws");
+        const Transition t(x, w_a, w_b, w_o, mask, act);
+        fit(dy, "dy", t.dtype, t.shape, t.device);
+        if (accumulate && !(dw_a.defined() && dw_b.defined() && dw_o.defined())) value_error("accumulate needs dw_a, dw_b and dw_o");
+        const at::ScalarType grad = wide < 0 ? dw_a.defined() ? dw_a.scalar_type() : t.dtype : wide ? at::kFloat : at::kBFloat16;
+        if (grad != at::kFloat && grad != at::kBFloat16) type_error("unsupported dtype ", grad, " of dw_a");
+        ff_status status;
+        {
+            Unlocked unlocked;
+            const c10::DeviceGuard guard(t.device);
+            result(dx, "dx", t.dtype, t.shape, t.device);
+            result(dw_a, "dw_a", grad, t.in, t.device);
+            result(dw_b, "dw_b", grad, t.in, t.device);
+            result(dw_o, "dw_o", grad, t.back, t.device);
+            workspace(ws, ff_gated_transition_backward_workspace_bytes(&t.desc), t.device);
+            status = ff_gated_transition_backward(&t.desc, in(x), in(w_a), in(w_b), in(w_o), in(dy), (const float*)in(mask), out(dx), out(dw_a), out(dw_b), out(dw_o),
+                                                  grad == at::kFloat ? FF_F32 : FF_BF16, accumulate, out(ws), ws.nbytes(),
+                                                  c10::hip::getCurrentHIPStream(t.device.index()).stream());
+        }
+        return status == FF_OK ? tuple_of(dx, dw_a, dw_b, dw_o) : PyLong_FromLong(status);
+    });
+}
+
+// x, steps, a, b, c, eps, out, ws -> out
+PyObject* orthogonalise(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("orthogonalise", 8, n, [&]() -> PyObject* {
+        const at::Tensor x = tensor(a[0], "x");
+        const long steps = PyLong_AsLong(a[1]);
+        const double p[4] = {PyFloat_AsDouble(a[2]), PyFloat_AsDouble(a[3]), PyFloat_AsDouble(a[4]), PyFloat_AsDouble(a[5])};
+        if (PyErr_Occurred()) return nullptr;
+        at::Tensor result_ = optional(a[6], "out"), ws = optional(a[7], "ws");
+        const at::ScalarType dtype = x.scalar_type();
+        const at::Device device = x.device();
+        if (!x.is_cuda()) value_error("x is on ", device, ", not on a GPU");
+        if (!x.is_contiguous()) value_error("x is not contiguous");
+        if (dtype != at::kFloat && dtype != at::kBFloat16) type_error("unsupported dtype ", dtype);
+        if (x.dim() < 2 || x.size(-1) < 1 || x.size(-2) < 1) value_error("no matrices in shape ", x.sizes());
+        const int64_t rows = x.size(-2), cols = x.size(-1), count = x.numel() / (rows * cols);
+        if (rows > INT32_MAX || cols > INT32_MAX || count > INT32_MAX) value_error("too many values in shape ", x.sizes());
+        const ff_orthogonalise_desc desc{dtype == at::kFloat ? FF_F32 : FF_BF16, (int32_t)count, (int32_t)rows, (int32_t)cols, (int32_t)std::min(steps, 1000l), p[0], p[1], p[2], p[3]};
+        ff_status status;
+        {
+            Unlocked unlocked;
+            const c10::DeviceGuard guard(device);
+            result(result_, "out", dtype, x.sizes(), device);
+            workspace(ws, ff_orthogonalise_workspace_bytes(&desc), device);
+            status = ff_orthogonalise(&desc, in(x), out(result_), out(ws), ws.nbytes(), c10::hip::getCurrentHIPStream(device.index()).stream());
+        }
+        return status == FF_OK ? THPVariable_Wrap(result_) : PyLong_FromLong(status);
+    });
+}
+
+// address of the plan's ff_muon_desc, of its host copy, the plan, address of ff_muon_hyper, norm, max_norm, ws, the plan's stream -> status
+PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded("muon_step", 8, n, [&]() -> PyObject* {
+        const auto* desc = (const ff_muon_desc*)PyLong_AsVoidPtr(a[0]);
+        const void* host = PyLong_AsVoidPtr(a[1]);
+        const auto* hyper = (const ff_muon_hyper*)PyLong_AsVoidPtr(a[3]);
+        void* const own = PyLong_AsVoidPtr(a[7]);
+        if (PyErr_Occurred()) return nullptr;
+        const at::Tensor plan = tensor(a[2], "plan"), norm = optional(a[4], "norm"), ws = tensor(a[6], "ws");
+        if (norm.defined() != (a[5] != Py_None)) value_error("norm and max_norm are given together");
+        const at::Device device = plan.device();
+        fit_optional(norm, "norm", at::kFloat, {1}, device);
+        if (ws.device() != device || !ws.is_contiguous()) value_error("ws is on ", ws.device(), " or not contiguous");
+        ff_status status;
+        {
+            Unlocked unlocked;
+            const c10::DeviceGuard guard(device);
+            const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(device.index());
+            status = ff_muon_step(desc, host, in(plan), plan.nbytes(), hyper, (const float*)in(norm), out(ws), ws.nbytes(), stream.stream());
+            in_use(plan, stream, own);
+            in_use(ws, stream, own);
+        }
+        return PyLong_FromLong(status);
+    });
+}
+
 PyMethodDef kMethods[] = {{"layernorm_forward", (PyCFunction)(void (*)(void))layernorm_forward, METH_FASTCALL, nullptr},
                           {"layernorm_backward", (PyCFunction)(void (*)(void))layernorm_backward, METH_FASTCALL, nullptr},
                           {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
                           {"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, nullptr},
                           {"adamw_moments", (PyCFunction)(void (*)(void))adamw_moments, METH_FASTCALL, nullptr},
+                          {"transition_forward", (PyCFunction)(void (*)(void))transition_forward, METH_FASTCALL, nullptr},
+                          {"transition_backward", (PyCFunction)(void (*)(void))transition_backward, METH_FASTCALL, nullptr},
+                          {"orthogonalise", (PyCFunction)(void (*)(void))orthogonalise, METH_FASTCALL, nullptr},
+                          {"muon_step", (PyCFunction)(void (*)(void))muon_step, METH_FASTCALL, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, kMethods};
 

@@ -103,7 +103,8 @@ enum KernelKind { KK_PREP = 0, KK_BIAS, KK_PROJ, KK_ATTN, KK_OUT, KK_LAYERNORM, 
                   KK_TM_PREP, KK_TM_PROJ, KK_TM_MUL, KK_TM_OUT, KK_GCA_KV, KK_GCA_SOFTMAX, KK_GCA_OUT,
                   KK_BWD_STATS, KK_BWD_DQ, KK_BWD_DKV, KK_BWD_DBIAS, KK_PROBE_VALU, KK_PROJ_ATTN, KK_BWD_ROWS,
                   KK_BWD_PREPARE, KK_BWD_DBIAS_REDUCE, KK_LN_FORWARD, KK_LN_BACKWARD, KK_LN_JOIN, KK_GRAD_NORM, KK_ADAMW,
-                  KK_MOMENTS, KK_COUNT };
+                  KK_MOMENTS, KK_TR_PACK, KK_TR_HIDDEN, KK_TR_OUT, KK_TR_GRAD, KK_TR_WEIGHTS, KK_TR_JOIN, KK_MUON_MOMENTUM, KK_NS_START,
+                  KK_NS_GRAM, KK_NS_POLY, KK_NS_APPLY, KK_COUNT };
 void prof_begin(int kind, hipStream_t st);
 void prof_end(int kind, hipStream_t st);
 // brackets the launches issued in its scope with HIP events when the timer is on
@@ -186,5 +187,25 @@ size_t grad_norm_workspace();
 ff_status grad_norm_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, float* norm, void* ws, hipStream_t stream);
 ff_status adamw_step_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, const ff_adamw_hyper& h, const float* norm, hipStream_t stream);
 ff_status adamw_moments_run(const ff_adamw_desc& d, const void* plan, size_t plan_bytes, float* m_out, float* v_out, hipStream_t stream);
+
+// gated transition (ff_transition.hip)
+size_t transition_forward_workspace(const ff_transition_desc& d);
+size_t transition_backward_workspace(const ff_transition_desc& d);
+ff_status transition_forward_run(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
+                                 const float* mask, void* y, void* ws, hipStream_t stream);
+ff_status transition_backward_run(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
+                                  const float* mask, void* dx, void* dw_a, void* dw_b, void* dw_o, int grad_dtype, bool accumulate, void* ws, hipStream_t stream);
+
+// Newton-Schulz products, the Muon step (ff_muon.hip)
+size_t orthogonalise_workspace(const ff_orthogonalise_desc& d);
+ff_status orthogonalise_run(const ff_orthogonalise_desc& d, const void* x, void* out, void* ws, hipStream_t stream);
+// 0 if there is no host memory, or too many matrices
+size_t muon_plan_size(const ff_muon_desc& d, const ff_muon_tensor* tensors);
+// 0: done; 1: a tensor that the step writes overlaps another one; -1: no host memory
+int muon_plan_fill(const ff_muon_desc& d, const ff_muon_tensor* tensors, void* plan);
+// whether this is a plan of this descriptor
+bool muon_plan_whole(const ff_muon_desc& d, const void* plan_host, size_t bytes);
+size_t muon_workspace(const void* plan_host);
+ff_status muon_step_run(const ff_muon_desc& d, const void* plan_host, const void* plan, const ff_muon_hyper& h, const float* norm, void* ws, hipStream_t stream);
 
 }  // namespace ff

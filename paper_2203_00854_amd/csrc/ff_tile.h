@@ -1,0 +1,260 @@
+// Products of tiles on the matrix cores, D[m][n] = sum over k of A(m, k) B(n, k): staged through LDS by loads that write it directly, two stages
+// deep.  Shared by the gated transition and the orthogonalisation.
+//
+// Three kinds of operands: bfloat16; float32 (32x32x2 float32 instructions); float16 pairs, where a value is hi + lo, each rounded to nearest
+// (24 significant bits together), and a product hi hi + hi lo + lo hi: what it leaves out, lo lo, is 2^-24 of it at most.
+// An operand lies in memory with k contiguous, [m][k], or "turned", [k][m]; the reads from LDS turn it back.
+//
+// v_mfma_f32_32x32x16: A (32 x 16): lane l holds row l % 32, columns 8 (l / 32) .. + 7; B likewise with its columns; D: lane l holds column
+// l % 32, register v holds row 8 (v / 4) + 4 (l / 32) + v % 4.  The tiles are given as A := our B, B := our A, so that a lane holds one row m
+// and four consecutive n at a time.  v_mfma_f32_32x32x2: lane l holds row l % 32, column l / 32; which k a column stands for is free as long as both
+// operands agree, so a lane's sixteen bytes feed four instructions.
+#pragma once
+
+#include "ff_common.h"
+
+namespace ff {
+namespace tile {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short i16x4;
+typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
+
+static inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+static inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {      // a -> low half
+    bf16x2 t;
+    t[0] = (__bf16)a;
+    t[1] = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, t);
+}
+
+// kStep values of k make one round of matrix instructions, 32 bytes of a row of either operand.
+struct Bf16 {
+    static constexpr int kSize = 2, kPlanes = 1, kStep = 16;
+    struct Frag { uint4 u[1]; };
+    static __device__ __forceinline__ f32x16 mma(const Frag& b, const Frag& a, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b.u[0]), __builtin_bit_cast(bf16x8, a.u[0]), c, 0, 0, 0);
+    }
+};
+struct F32 {
+    static constexpr int kSize = 4, kPlanes = 1, kStep = 8;
+    struct Frag { uint4 u[1]; };
+    static __device__ __forceinline__ f32x16 mma(const Frag& b, const Frag& a, f32x16 c) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.u[0].x), __uint_as_float(a.u[0].x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.u[0].y), __uint_as_float(a.u[0].y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.u[0].z), __uint_as_float(a.u[0].z), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(b.u[0].w), __uint_as_float(a.u[0].w), c, 0, 0, 0);
+    }
+};
+struct Pair {
+    static constexpr int kSize = 2, kPlanes = 2, kStep = 16;
+    struct Frag { uint4 u[2]; };
+    static __device__ __forceinline__ f32x16 mma(const Frag& b, const Frag& a, f32x16 c) {
+        const f16x8 bh = __builtin_bit_cast(f16x8, b.u[0]), bl = __builtin_bit_cast(f16x8, b.u[1]);
+        const f16x8 ah = __builtin_bit_cast(f16x8, a.u[0]), al = __builtin_bit_cast(f16x8, a.u[1]);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(bl, ah, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh, al, c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(bh, ah, c, 0, 0, 0);
+    }
+};
+
+// One operand in memory.  Not turned: row m at p + m pitch, `rows` of them, `bytes` of each may be read (all of its k, padded with zeros to a
+// multiple of kStep).  Turned: row k at p + k pitch, `rows` of them (all k, likewise), `bytes` of each (all m).  Bytes are a multiple of 16, p and pitch
+// 16-byte aligned.  What lies past an end is read from the last row or the last sixteen bytes: a caller stores no m or n that is not there.
+struct Operand {
+    const void* p;
+    int64_t plane;        // bytes from the hi plane to the lo plane
+    int64_t pitch;        // bytes
+    int64_t rows;
+    int32_t bytes;
+};
+
+template <class Op_, int BM_, int BN_, int BK_, int WM_, int WN_, int NA_, int NB_, bool TA_, unsigned TB_>
+struct Core {
+    typedef Op_ Op;
+    typedef typename Op::Frag Frag;
+    static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, NA = NA_, NB = NB_;
+    static constexpr bool TA = TA_;
+    static constexpr unsigned TB = TB_;                            // bit b: operand b of the B side is turned
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
+    static constexpr int kPlaneA = BM * BK * Op::kSize, kPlaneB = BN * BK * Op::kSize;
+    static constexpr int kStage = Op::kPlanes * (NA * kPlaneA + NB * kPlaneB);
+    static constexpr int kLds = 2 * kStage;
+    static_assert(MT >= 1 && NT >= 1 && BK % Op::kStep == 0, "tile");
+
+    // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that the lanes that read in one cycle
+    // (eight at sixteen bytes, sixteen at eight) meet all banks
+    template <bool T, int W> static __device__ __forceinline__ int swizzle(int row) {
+        if constexpr (T) return Op::kSize == 4 ? 0 : W >= 8 ? 2 * (row & 3) : 2 * ((row >> 1) & 1);
+        return W >= 8 ? row & 7 : W == 4 ? (row >> 1) & 3 : 0;
+    }
+
+    template <bool T, int R>
+    static __device__ __forceinline__ void load(const Operand& o, int plane, int64_t r0, int64_t k0, unsigned lds) {
+        constexpr int W = (T ? R : BK) * Op::kSize / 16, LR = T ? BK : R, kUnits = LR * W;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const int64_t first = T ? k0 : r0;
+        const char* base = (const char*)o.p + plane * o.plane + first * o.pitch;
+        const int left = (int)(o.rows - first < LR ? o.rows - first : LR) - 1;
+        const int at = (int)(T ? r0 : k0) * Op::kSize, last = o.bytes - 16;
+#pragma unroll
+        for (int j = 0; j < (kUnits + kThreads - 1) / kThreads; ++j) {
+            const int u0 = j * kThreads + wave * 64;
+            if (kUnits % kThreads != 0 && u0 >= kUnits) break;
+            const int u = u0 + lane, row = u / W, chunk = (u % W) ^ swizzle<T, W>(row);
+            const int r = row < left ? row : left, c = at + chunk * 16;
+            load16_to_lds(base, (uint32_t)(r * (int)o.pitch + (c < last ? c : last)), lds + u0 * 16);
+        }
+    }
+
+    // the lane's piece of 32 rows (from `row0`) in round s
+    template <bool T, int R>
+    static __device__ __forceinline__ uint4 piece(const unsigned char* image, int row0, int s, int lane) {
+        constexpr int W = (T ? R : BK) * Op::kSize / 16;
+        const int hf = lane >> 5;
+        if constexpr (!T) {
+            const int row = row0 + (lane & 31);
+            return *reinterpret_cast<const uint4*>(image + row * (W * 16) + (((2 * s + hf) ^ swizzle<false, W>(row)) << 4));
+        } else if constexpr (Op::kSize == 2) {
+            // of sixteen lanes, lane i asks for four columns 4 (i % 4) .. of row i / 4, and lane l receives column l of the four rows
+            const int i = lane & 15, byte = (row0 + (lane & 16) + 4 * (i & 3)) * 2;
+            uint2 h[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int k = 16 * s + 8 * hf + 4 * t + (i >> 2);
+                const unsigned char* p = image + k * (W * 16) + (((byte >> 4) ^ swizzle<true, W>(k)) << 4) + (byte & 8);
+                h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)p));
+            }
+            return make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+        } else {
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(image + (8 * s + 4 * hf + j) * (W * 16) + (row0 + (lane & 31)) * 4);
+            return make_uint4(v[0], v[1], v[2], v[3]);
+        }
+    }
+    template <bool T, int R>
+    static __device__ __forceinline__ Frag frag(const unsigned char* image, int row0, int s, int lane) {
+        Frag f;
+#pragma unroll
+        for (int p = 0; p < Op::kPlanes; ++p) f.u[p] = piece<T, R>(image + p * (R * BK * Op::kSize), row0, s, lane);
+        return f;
+    }
+
+    template <int B = 0> static __device__ __forceinline__ void load_b(const Operand* b, int64_t n0, int64_t k0, unsigned lds) {
+        if constexpr (B < NB) {
+#pragma unroll
+            for (int p = 0; p < Op::kPlanes; ++p) load<(TB >> B & 1) != 0, BN>(b[B], p, n0, k0, lds + p * kPlaneB);
+            load_b<B + 1>(b, n0, k0, lds + Op::kPlanes * kPlaneB);
+        }
+    }
+    static __device__ __forceinline__ void load_stage(const Operand* a, const Operand* b, int64_t m0, int64_t n0, int64_t k0, unsigned lds) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int p = 0; p < Op::kPlanes; ++p) load<TA, BM>(a[i], p, m0, k0, lds + (i * Op::kPlanes + p) * kPlaneA);
+        load_b(b, n0, k0, lds + NA * Op::kPlanes * kPlaneA);
+    }
+
+    template <int B = 0>
+    static __device__ __forceinline__ void products(f32x16 (&acc)[NB][MT][NT], const Frag (&fa)[NA][MT], const unsigned char* image, int wn, int s, int lane) {
+        if constexpr (B < NB) {
+            Frag fb[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) fb[n] = frag<(TB >> B & 1) != 0, BN>(image, (wn * NT + n) * 32, s, lane);
+            constexpr int A = NA == 1 || B + 1 < NB ? 0 : 1;         // a second A side belongs to the last product
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[B][m][n] = Op::mma(fb[n], fa[A][m], acc[B][m][n]);
+            products<B + 1>(acc, fa, image + Op::kPlanes * kPlaneB, wn, s, lane);
+        }
+    }
+    static __device__ __forceinline__ void round(f32x16 (&acc)[NB][MT][NT], const unsigned char* image, int wm, int wn, int s, int lane) {
+        Frag fa[NA][MT];
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) fa[i][m] = frag<TA, BM>(image + i * Op::kPlanes * kPlaneA, (wm * MT + m) * 32, s, lane);
+        products(acc, fa, image + NA * Op::kPlanes * kPlaneA, wn, s, lane);
+    }
+
+    static __device__ __forceinline__ void clear(f32x16 (&acc)[NB][MT][NT]) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[b][m][n][v] = 0.f;
+    }
+
+    // adds the products over k = from .. to (multiples of kStep) of the tile at (m0, n0); smem: kLds bytes that every thread is done with
+    static __device__ __forceinline__ void run(f32x16 (&acc)[NB][MT][NT], const Operand* a, const Operand* b, int64_t m0, int64_t n0, int64_t from, int64_t to,
+                                               unsigned char* smem) {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const int wm = wave / WN, wn = wave % WN;
+        const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+        if (from >= to) return;
+        load_stage(a, b, m0, n0, from, lds);
+        int buf = 0;
+        for (int64_t k0 = from; k0 < to; k0 += BK, buf ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();                                           // the stage is there, and nobody reads the other one any more
+            if (k0 + BK < to) load_stage(a, b, m0, n0, k0 + BK, lds + (buf ^ 1) * kStage);
+            const unsigned char* image = smem + buf * kStage;
+            if (to - k0 >= BK) {
+#pragma unroll
+                for (int s = 0; s < BK / Op::kStep; ++s) round(acc, image, wm, wn, s, lane);
+            } else {
+                const int steps = (int)(to - k0) / Op::kStep;
+                for (int s = 0; s < steps; ++s) round(acc, image, wm, wn, s, lane);
+            }
+        }
+        __syncthreads();
+    }
+
+    // body(b, m, n, v): four results v of product b in row m, columns n .. n + 3
+    template <typename F> static __device__ __forceinline__ void each(f32x16 (&acc)[NB][MT][NT], int64_t m0, int64_t n0, F body) {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const int wm = wave / WN, wn = wave % WN;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float v[NB][4];
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) v[b][q] = acc[b][i][j][4 * g + q];
+                    body(m0 + (wm * MT + i) * 32 + (lane & 31), n0 + (wn * NT + j) * 32 + 8 * g + 4 * (lane >> 5), v);
+                }
+    }
+};
+
+// Blocks of the same rows of A run one after another on one XCD (block i starts on XCD i % 8), whose L2 then holds them, while B is small enough for all.
+struct TilePlace {
+    int64_t m;
+    int n;
+};
+__device__ __forceinline__ TilePlace place_of(uint32_t block, uint32_t mtiles, uint32_t ntiles) {
+    const uint32_t full = mtiles / 8 * 8 * ntiles;
+    if (block >= full) {
+        const uint32_t rest = block - full;
+        return {(int64_t)(mtiles / 8 * 8 + rest / ntiles), (int)(rest % ntiles)};
+    }
+    const uint32_t xcd = block & 7u, local = block >> 3;
+    return {(int64_t)(local / ntiles * 8 + xcd), (int)(local % ntiles)};
+}
+
+}  // namespace tile
+}  // namespace ff

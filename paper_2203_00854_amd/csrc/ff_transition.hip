@@ -1,0 +1,463 @@
+// The gated transition, y = (act(x Wa^T) * (x Wb^T)) Wo^T, and its gradients.
+#include "ff_tile.h"
+
+#include <algorithm>
+
+namespace ff {
+
+using tile::align256;
+using tile::Bf16;
+using tile::Core;
+using tile::f32x16;
+using tile::F32;
+using tile::Operand;
+using tile::round_up;
+
+namespace {
+
+constexpr int kPad = 16;                       // rows and columns of the products' inner dimensions are padded to this with zeros
+constexpr int64_t kHiddenBytes = 64 << 20;     // of one hidden tensor of a chunk of rows
+
+template <typename T> struct OpOf;
+template <> struct OpOf<float> { typedef F32 type; };
+template <> struct OpOf<bf16_t> { typedef Bf16 type; };
+
+// ---- activations -------------------------------------------------------------------------
+// In float32 with the library's functions; for bfloat16 results the sigmoid by the machine's exponential and reciprocal (2^-22 of it, against 2^-9)
+template <bool FAST> __device__ __forceinline__ float sigmoid_of(float a) {
+    if constexpr (FAST) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * a));
+    return 1.f / (1.f + expf(-a));
+}
+template <int ACT, bool FAST> __device__ __forceinline__ float gate_of(float a) {
+    if constexpr (ACT == FF_GELU) return a * (0.5f * erfcf(-0.70710678118654752f * a));
+    const float s = sigmoid_of<FAST>(a);
+    return ACT == FF_SIGMOID ? s : a * s;
+}
+template <int ACT, bool FAST> __device__ __forceinline__ float gate_of(float a, float& slope) {
+    if constexpr (ACT == FF_GELU) {
+        const float phi = 0.5f * erfcf(-0.70710678118654752f * a);
+        slope = phi + a * (0.39894228040143268f * expf(-0.5f * a * a));
+        return a * phi;
+    }
+    const float s = sigmoid_of<FAST>(a);
+    if constexpr (ACT == FF_SIGMOID) {
+        slope = s * (1.f - s);
+        return s;
+    }
+    slope = s * (1.f + a * (1.f - s));
+    return a * s;
+}
+
+// ---- four values of a row ----------------------------------------------------------------
+struct __attribute__((packed, aligned(2))) Half4 { uint32_t w[2]; };      // (gfx950 reads and writes vectors at any alignment of their elements)
+struct __attribute__((packed, aligned(4))) Float4 { float w[4]; };
+
+__device__ __forceinline__ void store4(bf16_t* p, const float* v) { *(Half4*)p = Half4{{tile::pack2(v[0], v[1]), tile::pack2(v[2], v[3])}}; }
+__device__ __forceinline__ void store4(float* p, const float* v) { *(Float4*)p = Float4{{v[0], v[1], v[2], v[3]}}; }
+__device__ __forceinline__ void load4(const bf16_t* p, float* v) {
+    const Half4 h = *(const Half4*)p;
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(i & 1 ? h.w[i / 2] & 0xffff0000u : h.w[i / 2] << 16);
+}
+__device__ __forceinline__ void load4(const float* p, float* v) {
+    const Float4 f = *(const Float4*)p;
+    for (int i = 0; i < 4; ++i) v[i] = f.w[i];
+}
+
+// ---- packing -------------------------------------------------------------------------------
+// Copies whose rows and columns are padded with zeros, masked rows zero: what is not aligned to sixteen bytes, or has odd sizes, or rows whose values
+// must not reach sums over rows.  A thread writes sixteen bytes.
+struct PackJob {
+    const void* src;
+    void* dst;
+    const float* mask;
+    int64_t rows, rows_out;
+    int32_t cols, cols_out;
+    uint32_t blocks;
+};
+struct PackArgs { PackJob job[5]; };
+template <typename T> __global__ __launch_bounds__(256) void k_tr_pack(PackArgs a) {
+    constexpr int V = 16 / sizeof(T);
+    uint32_t block = blockIdx.x;
+    int j = 0;
+    while (j < 4 && block >= a.job[j].blocks) block -= a.job[j++].blocks;
+    const PackJob& p = a.job[j];
+    const int64_t i = (int64_t)block * 256 + threadIdx.x;
+    const int per = p.cols_out / V;
+    const int64_t r = i / per;
+    const int c = (int)(i % per) * V;
+    if (r >= p.rows_out) return;
+    const bool live = r < p.rows && !(p.mask && p.mask[r] == 0.f);
+    const T* src = (const T*)p.src + r * p.cols;
+    alignas(16) T v[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) v[q] = live && c + q < p.cols ? src[c + q] : T(0);
+    *(uint4*)((T*)p.dst + r * p.cols_out + c) = *(const uint4*)v;
+}
+
+// ---- hidden layer --------------------------------------------------------------------------
+struct HiddenArgs {
+    Operand x, w[2];
+    void* h;
+    int64_t rows, rows_out;       // of this chunk; of h
+    int32_t f, k, pitch;          // hidden channels; channels of x, padded; values of a row of h
+    uint32_t mtiles, ntiles;
+};
+// Both projections share the tile of x; their product with the activation leaves alone.  Channels and rows past the end are zeros.
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_hidden(HiddenArgs a) {
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
+    f32x16 acc[2][C::MT][C::NT];
+    C::clear(acc);
+    C::run(acc, &a.x, a.w, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
+    C::each(acc, at.m * C::BM, (int64_t)at.n * C::BN, [&](int64_t m, int64_t n, float (&v)[2][4]) {
+        if (m >= a.rows_out || n >= a.pitch) return;
+        float h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = m < a.rows && n + q < a.f ? gate_of<ACT, sizeof(T) == 2>(v[0][q]) * v[1][q] : 0.f;
+        store4((T*)a.h + m * a.pitch + n, h);
+    });
+}
+
+// ---- output --------------------------------------------------------------------------------
+struct OutArgs {
+    Operand a[2], b[2];
+    int32_t parts;                // products that are added up
+    int32_t k, cols;
+    int64_t rows;
+    const void* residual;
+    const float* mask;
+    void* out;
+    uint32_t mtiles, ntiles;
+};
+// out = (residual +) sum of the products; a masked row's sum counts as zero, whatever it is
+template <class C, typename T> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_out(OutArgs a) {
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
+    f32x16 acc[1][C::MT][C::NT];
+    C::clear(acc);
+    for (int p = 0; p < a.parts; ++p) C::run(acc, a.a + p, a.b + p, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
+    C::each(acc, at.m * C::BM, (int64_t)at.n * C::BN, [&](int64_t m, int64_t n, float (&v)[1][4]) {
+        if (m >= a.rows || n >= a.cols) return;
+        const bool live = !(a.mask && a.mask[m] == 0.f);
+        T* out = (T*)a.out + m * a.cols + n;
+        const T* residual = (const T*)a.residual + m * a.cols + n;
+        if (n + 4 <= a.cols) {
+            float r[4] = {0.f, 0.f, 0.f, 0.f};
+            if (a.residual) load4(residual, r);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) r[q] += live ? v[0][q] : 0.f;
+            store4(out, r);
+        } else
+            for (int q = 0; q < 4 && n + q < a.cols; ++q) out[q] = from_f32<T>((a.residual ? to_f32<T>(residual[q]) : 0.f) + (live ? v[0][q] : 0.f));
+    });
+}
+
+// ---- gradients of the hidden layer -----------------------------------------------------------
+struct GradArgs {
+    Operand a[2], b[3];           // x, dy; Wa, Wb, Wo
+    void *da, *db, *h;
+    int64_t rows, rows_out;
+    int32_t f, k, pitch;
+    uint32_t mtiles, ntiles;
+};
+// a, b and dh = dy Wo of a tile in one loop over the channels; da = dh b act'(a), db = dh act(a) and h, rounded to the tensors' type, are what the
+// products with the weights and with x and dy read
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_grad(GradArgs a) {
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
+    f32x16 acc[3][C::MT][C::NT];
+    C::clear(acc);
+    C::run(acc, a.a, a.b, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
+    C::each(acc, at.m * C::BM, (int64_t)at.n * C::BN, [&](int64_t m, int64_t n, float (&v)[3][4]) {
+        if (m >= a.rows_out || n >= a.pitch) return;
+        float da[4], db[4], h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const bool there = m < a.rows && n + q < a.f;
+            float slope;
+            const float gate = gate_of<ACT, sizeof(T) == 2>(v[0][q], slope);
+            da[q] = there ? v[2][q] * v[1][q] * slope : 0.f;
+            db[q] = there ? v[2][q] * gate : 0.f;
+            h[q] = there ? gate * v[1][q] : 0.f;
+        }
+        const int64_t i = m * a.pitch + n;
+        store4((T*)a.da + i, da);
+        store4((T*)a.db + i, db);
+        store4((T*)a.h + i, h);
+    });
+}
+
+// ---- gradients of the weights ------------------------------------------------------------------
+struct WeightArgs {
+    Operand a[3], b[3];           // da, db, dy; x, x, h
+    float* partial;               // [splits][3][fp cp]
+    int64_t rows;                 // padded to kPad
+    int64_t per_split;            // rows of a split
+    int32_t fp, cp;
+    uint32_t ftiles, ctiles;
+    int32_t add;                  // to what an earlier chunk left
+};
+// Sums over rows: both operands lie with the rows as k.  The rows are split over blocks, whose sums are joined in a fixed order.
+template <class C> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_weights(WeightArgs a) {
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const uint32_t tiles = a.ftiles * a.ctiles, which = blockIdx.x / tiles, t = blockIdx.x % tiles;
+    const bool last = which == 2;
+    const int64_t m0 = (int64_t)(last ? t % a.ctiles : t / a.ctiles) * C::BM, n0 = (int64_t)(last ? t / a.ctiles : t % a.ctiles) * C::BN;
+    const int64_t from = blockIdx.y * a.per_split, to = from + a.per_split < a.rows ? from + a.per_split : a.rows;
+    f32x16 acc[1][C::MT][C::NT];
+    C::clear(acc);
+    C::run(acc, a.a + which, a.b + which, m0, n0, from, to, smem);
+    float* out = a.partial + ((int64_t)blockIdx.y * 3 + which) * a.fp * a.cp;
+    const int32_t rows = last ? a.cp : a.fp, cols = last ? a.fp : a.cp;
+    C::each(acc, m0, n0, [&](int64_t m, int64_t n, float (&v)[1][4]) {
+        if (m >= rows || n >= cols) return;
+        float* p = out + m * cols + n;
+        if (a.add) {
+            float was[4];
+            load4(p, was);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[0][q] += was[q];
+        }
+        store4(p, v[0]);
+    });
+}
+
+struct JoinArgs {
+    const float* partial;
+    void* dw[3];
+    int32_t f, c, fp, cp, splits, accumulate;
+};
+template <typename G> __global__ __launch_bounds__(256) void k_tr_join(JoinArgs a) {
+    const int which = blockIdx.y;
+    const int32_t rows = which == 2 ? a.c : a.f, cols = which == 2 ? a.f : a.c, pitch = which == 2 ? a.fp : a.cp;
+    const int64_t size = (int64_t)a.fp * a.cp, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)rows * cols) return;
+    const int64_t at = which * size + i / cols * pitch + i % cols;
+    float sum = a.splits > 0 ? a.partial[at] : 0.f;
+    for (int s = 1; s < a.splits; ++s) sum += a.partial[s * 3 * size + at];
+    G* out = (G*)a.dw[which] + i;
+    *out = from_f32<G>(a.accumulate ? to_f32<G>(*out) + sum : sum);
+}
+
+// ---- the calls -------------------------------------------------------------------------------
+struct Sizes {
+    int esz;
+    int64_t cp, fp, chunk;         // padded channels; rows worked on at a time, a multiple of 128
+    int64_t chunks;
+    size_t weight;                 // bytes of a packed weight
+    size_t tokens, hidden;         // bytes of a chunk's packed x and of its hidden tensor
+    int splits;
+    int64_t per_split;
+    size_t partial;
+};
+Sizes sizes_of(const ff_transition_desc& d) {
+    Sizes s;
+    s.esz = d.dtype == FF_F32 ? 4 : 2;
+    s.cp = round_up(d.c, kPad);
+    s.fp = round_up(d.f, kPad);
+    const int64_t most = std::max<int64_t>(128, kHiddenBytes / (s.fp * s.esz) / 128 * 128);
+    s.chunk = std::min(most, round_up(std::max<int64_t>(d.rows, 1), 128));
+    s.chunks = (d.rows + s.chunk - 1) / s.chunk;
+    s.weight = align256((size_t)s.fp * s.cp * s.esz);
+    s.tokens = align256((size_t)s.chunk * s.cp * s.esz);
+    s.hidden = align256((size_t)s.chunk * s.fp * s.esz);
+    // as many splits of the rows as give two blocks for each of 256 compute units, of 256 rows at least
+    const int64_t tiles = 3 * ((d.f + 127) / 128) * ((d.c + 127) / 128);
+    const int64_t want = std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, s.chunk / 256));
+    s.per_split = round_up((s.chunk + want - 1) / want, 128);
+    s.splits = (int)((s.chunk + s.per_split - 1) / s.per_split);
+    s.partial = align256((size_t)s.splits * 3 * s.fp * s.cp * 4);
+    return s;
+}
+
+bool aligned(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+template <class C, typename Kernel, typename Args> ff_status launch(int kind, const char* what, Kernel kernel, dim3 grid, const Args& args, hipStream_t stream) {
+    Timed t(kind, stream);
+    if (C::kLds > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+    hipLaunchKernelGGL(kernel, grid, dim3(C::kThreads), C::kLds, stream, args);
+    return check_launch(what);
+}
+
+PackJob pack_job(const void* src, void* dst, const float* mask, int64_t rows, int64_t rows_out, int cols, int64_t cols_out, int esz) {
+    return {src, dst, mask, rows, rows_out, cols, (int32_t)cols_out, (uint32_t)((rows_out * (cols_out * esz / 16) + 255) / 256)};
+}
+template <typename T> ff_status pack(const PackJob* jobs, int n, hipStream_t stream) {
+    PackArgs a{};
+    uint32_t blocks = 0;
+    for (int i = 0; i < n; ++i) {
+        a.job[i] = jobs[i];
+        blocks += jobs[i].blocks;
+    }
+    for (int i = n; i < 5; ++i) a.job[i] = jobs[n - 1];             // (never reached: no block is left for them)
+    Timed t(KK_TR_PACK, stream);
+    hipLaunchKernelGGL((k_tr_pack<T>), dim3(blocks), dim3(256), 0, stream, a);
+    return check_launch("ff_gated_transition: packing");
+}
+
+Operand operand(const void* p, int64_t pitch, int64_t rows, int64_t cols, int esz) {
+    return {p, 0, pitch * esz, rows, (int32_t)(cols * esz)};
+}
+
+// the weights as the products read them: themselves, or padded copies in ws
+struct Weights {
+    Operand a, b, o;
+    ff_status status;
+};
+template <typename T> Weights weights_of(const ff_transition_desc& d, const Sizes& s, const void* w_a, const void* w_b, const void* w_o, char*& ws, hipStream_t stream) {
+    Weights w{};
+    char* copies = ws;
+    ws += 3 * s.weight;
+    const bool as_is = d.c % kPad == 0 && d.f % kPad == 0 && aligned(w_a) && aligned(w_b) && aligned(w_o);
+    const void* from[3] = {w_a, w_b, w_o};
+    if (!as_is) {
+        PackJob jobs[3];
+        for (int i = 0; i < 3; ++i) {
+            void* dst = copies + i * s.weight;
+            jobs[i] = i < 2 ? pack_job(from[i], dst, nullptr, d.f, s.fp, d.c, s.cp, s.esz) : pack_job(from[i], dst, nullptr, d.c, s.cp, d.f, s.fp, s.esz);
+            from[i] = dst;
+        }
+        w.status = pack<T>(jobs, 3, stream);
+    }
+    w.a = operand(from[0], s.cp, s.fp, s.cp, s.esz);
+    w.b = operand(from[1], s.cp, s.fp, s.cp, s.esz);
+    w.o = operand(from[2], s.fp, s.cp, s.fp, s.esz);
+    return w;
+}
+
+constexpr int bk_of(int esz) { return esz == 2 ? 64 : 16; }
+
+template <typename T> ff_status forward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
+                                        const float* mask, void* y, void* ws_, hipStream_t stream) {
+    typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 128, 64, bk_of(sizeof(T)), 2, 2, 1, 2, false, 0u> CH;
+    typedef Core<Op, 128, 128, bk_of(sizeof(T)), 2, 2, 1, 1, false, 0u> CO;
+    const Sizes s = sizes_of(d);
+    char* ws = (char*)ws_;
+    const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
+    if (w.status != FF_OK) return w.status;
+    char* const tokens = ws;
+    char* const hidden = tokens + s.tokens;
+    const bool as_is = d.c % kPad == 0 && aligned(x);
+    for (int64_t r0 = 0; r0 < d.rows; r0 += s.chunk) {
+        const int64_t rows = std::min(s.chunk, d.rows - r0);
+        const T* xr = (const T*)x + r0 * d.c;
+        if (!as_is) {
+            const PackJob job = pack_job(xr, tokens, nullptr, rows, rows, d.c, s.cp, s.esz);
+            const ff_status st = pack<T>(&job, 1, stream);
+            if (st != FF_OK) return st;
+        }
+        HiddenArgs ha{operand(as_is ? (const void*)xr : tokens, s.cp, rows, s.cp, s.esz), {w.a, w.b}, hidden, rows, rows, d.f, (int32_t)s.cp, (int32_t)s.fp,
+                      (uint32_t)((rows + CH::BM - 1) / CH::BM), (uint32_t)((s.fp + CH::BN - 1) / CH::BN)};
+        const dim3 grid(ha.mtiles * ha.ntiles);
+        ff_status st = d.act == FF_SILU   ? launch<CH>(KK_TR_HIDDEN, "ff_gated_transition_forward", k_tr_hidden<CH, T, FF_SILU>, grid, ha, stream)
+                       : d.act == FF_GELU ? launch<CH>(KK_TR_HIDDEN, "ff_gated_transition_forward", k_tr_hidden<CH, T, FF_GELU>, grid, ha, stream)
+                                          : launch<CH>(KK_TR_HIDDEN, "ff_gated_transition_forward", k_tr_hidden<CH, T, FF_SIGMOID>, grid, ha, stream);
+        if (st != FF_OK) return st;
+        OutArgs oa{};
+        oa.a[0] = operand(hidden, s.fp, rows, s.fp, s.esz);
+        oa.b[0] = w.o;
+        oa.parts = 1;
+        oa.k = (int32_t)s.fp;
+        oa.cols = d.c;
+        oa.rows = rows;
+        oa.residual = residual ? (const T*)residual + r0 * d.c : nullptr;
+        oa.mask = mask ? mask + r0 : nullptr;
+        oa.out = (T*)y + r0 * d.c;
+        oa.mtiles = (uint32_t)((rows + CO::BM - 1) / CO::BM);
+        oa.ntiles = (uint32_t)((d.c + CO::BN - 1) / CO::BN);
+        st = launch<CO>(KK_TR_OUT, "ff_gated_transition_forward", k_tr_out<CO, T>, dim3(oa.mtiles * oa.ntiles), oa, stream);
+        if (st != FF_OK) return st;
+    }
+    return FF_OK;
+}
+
+template <typename T> ff_status backward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
+                                         const float* mask, void* dx, void* const (&dw)[3], int grad_dtype, bool accumulate, void* ws_, hipStream_t stream) {
+    typedef typename OpOf<T>::type Op;
+    constexpr int BK = bk_of(sizeof(T));
+    typedef Core<Op, 128, 64, sizeof(T) == 2 ? 32 : 16, 2, 2, 2, 3, false, 4u> CG;
+    typedef Core<Op, 128, 128, BK, 2, 2, 1, 1, false, 1u> CX;
+    typedef Core<Op, 128, 128, BK, 2, 2, 1, 1, true, 1u> CW;
+    const Sizes s = sizes_of(d);
+    char* ws = (char*)ws_;
+    const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
+    if (w.status != FF_OK) return w.status;
+    char* const tokens[2] = {ws, ws + s.tokens};
+    ws += 2 * s.tokens;
+    char* const hidden[3] = {ws, ws + s.hidden, ws + 2 * s.hidden};
+    float* const partial = (float*)(ws + 3 * s.hidden);
+    const bool as_is = d.c % kPad == 0 && aligned(x) && aligned(dy) && !mask;
+    ff_status st = FF_OK;
+    for (int64_t r0 = 0; r0 < d.rows; r0 += s.chunk) {
+        const int64_t rows = std::min(s.chunk, d.rows - r0), padded = round_up(rows, kPad);
+        const void* in[2] = {(const T*)x + r0 * d.c, (const T*)dy + r0 * d.c};
+        if (!as_is) {
+            PackJob jobs[2];
+            for (int i = 0; i < 2; ++i) {
+                jobs[i] = pack_job(in[i], tokens[i], mask ? mask + r0 : nullptr, rows, rows, d.c, s.cp, s.esz);
+                in[i] = tokens[i];
+            }
+            st = pack<T>(jobs, 2, stream);
+            if (st != FF_OK) return st;
+        }
+        const Operand ox = operand(in[0], s.cp, rows, s.cp, s.esz), ody = operand(in[1], s.cp, rows, s.cp, s.esz);
+        GradArgs ga{{ox, ody}, {w.a, w.b, w.o}, hidden[0], hidden[1], hidden[2], rows, padded, d.f, (int32_t)s.cp, (int32_t)s.fp,
+                    (uint32_t)((padded + CG::BM - 1) / CG::BM), (uint32_t)((s.fp + CG::BN - 1) / CG::BN)};
+        const dim3 grid(ga.mtiles * ga.ntiles);
+        st = d.act == FF_SILU   ? launch<CG>(KK_TR_GRAD, "ff_gated_transition_backward", k_tr_grad<CG, T, FF_SILU>, grid, ga, stream)
+             : d.act == FF_GELU ? launch<CG>(KK_TR_GRAD, "ff_gated_transition_backward", k_tr_grad<CG, T, FF_GELU>, grid, ga, stream)
+                                : launch<CG>(KK_TR_GRAD, "ff_gated_transition_backward", k_tr_grad<CG, T, FF_SIGMOID>, grid, ga, stream);
+        if (st != FF_OK) return st;
+        Operand oh[3];
+        for (int i = 0; i < 3; ++i) oh[i] = operand(hidden[i], s.fp, padded, s.fp, s.esz);
+        WeightArgs wa{{oh[0], oh[1], ody}, {ox, ox, oh[2]}, partial, padded, s.per_split, (int32_t)s.fp, (int32_t)s.cp,
+                      (uint32_t)((s.fp + 127) / 128), (uint32_t)((s.cp + 127) / 128), r0 > 0};
+        st = launch<CW>(KK_TR_WEIGHTS, "ff_gated_transition_backward", k_tr_weights<CW>, dim3(3 * wa.ftiles * wa.ctiles, s.splits), wa, stream);
+        if (st != FF_OK) return st;
+        OutArgs oa{};
+        oa.a[0] = oh[0];
+        oa.a[1] = oh[1];
+        oa.b[0] = w.a;
+        oa.b[1] = w.b;
+        oa.parts = 2;
+        oa.k = (int32_t)s.fp;
+        oa.cols = d.c;
+        oa.rows = rows;
+        oa.out = (T*)dx + r0 * d.c;
+        oa.mtiles = (uint32_t)((rows + CX::BM - 1) / CX::BM);
+        oa.ntiles = (uint32_t)((d.c + CX::BN - 1) / CX::BN);
+        st = launch<CX>(KK_TR_OUT, "ff_gated_transition_backward", k_tr_out<CX, T>, dim3(oa.mtiles * oa.ntiles), oa, stream);
+        if (st != FF_OK) return st;
+    }
+    JoinArgs ja{partial, {dw[0], dw[1], dw[2]}, d.f, d.c, (int32_t)s.fp, (int32_t)s.cp, d.rows ? s.splits : 0, accumulate};
+    const dim3 grid((uint32_t)(((int64_t)d.f * d.c + 255) / 256), 3);
+    Timed t(KK_TR_JOIN, stream);
+    if (grad_dtype == FF_F32) hipLaunchKernelGGL((k_tr_join<float>), grid, dim3(256), 0, stream, ja);
+    else hipLaunchKernelGGL((k_tr_join<bf16_t>), grid, dim3(256), 0, stream, ja);
+    return check_launch("ff_gated_transition_backward");
+}
+
+}  // namespace
+
+size_t transition_forward_workspace(const ff_transition_desc& d) {
+    const Sizes s = sizes_of(d);
+    return 3 * s.weight + s.tokens + s.hidden;
+}
+size_t transition_backward_workspace(const ff_transition_desc& d) {
+    const Sizes s = sizes_of(d);
+    return 3 * s.weight + 2 * s.tokens + 3 * s.hidden + s.partial;
+}
+ff_status transition_forward_run(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
+                                 const float* mask, void* y, void* ws, hipStream_t stream) {
+    return d.dtype == FF_F32 ? forward<float>(d, x, w_a, w_b, w_o, residual, mask, y, ws, stream)
+                             : forward<bf16_t>(d, x, w_a, w_b, w_o, residual, mask, y, ws, stream);
+}
+ff_status transition_backward_run(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
+                                  const float* mask, void* dx, void* dw_a, void* dw_b, void* dw_o, int grad_dtype, bool accumulate, void* ws, hipStream_t stream) {
+    void* const dw[3] = {dw_a, dw_b, dw_o};
+    return d.dtype == FF_F32 ? backward<float>(d, x, w_a, w_b, w_o, dy, mask, dx, dw, grad_dtype, accumulate, ws, stream)
+                             : backward<bf16_t>(d, x, w_a, w_b, w_o, dy, mask, dx, dw, grad_dtype, accumulate, ws, stream);
+}
+
+}  // namespace ff
