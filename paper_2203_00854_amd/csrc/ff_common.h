@@ -103,7 +103,7 @@ enum KernelKind { KK_PREP = 0, KK_BIAS, KK_PROJ, KK_ATTN, KK_OUT, KK_LAYERNORM, 
                   KK_TM_PREP, KK_TM_PROJ, KK_TM_MUL, KK_TM_OUT, KK_GCA_KV, KK_GCA_SOFTMAX, KK_GCA_OUT,
                   KK_BWD_STATS, KK_BWD_DQ, KK_BWD_DKV, KK_BWD_DBIAS, KK_PROBE_VALU, KK_PROJ_ATTN, KK_BWD_ROWS,
                   KK_BWD_PREPARE, KK_BWD_DBIAS_REDUCE, KK_LN_FORWARD, KK_LN_BACKWARD, KK_LN_JOIN, KK_GRAD_NORM, KK_ADAMW,
-                  KK_MOMENTS, KK_TR_PACK, KK_TR_HIDDEN, KK_TR_OUT, KK_TR_GRAD, KK_TR_WEIGHTS, KK_TR_JOIN, KK_MUON_MOMENTUM, KK_NS_START,
+                  KK_MOMENTS, KK_TR_PACK, KK_TR_HIDDEN, KK_TR_OUT, KK_TR_GRAD, KK_TR_WEIGHTS, KK_TR_JOIN, KK_TR_ROWS, KK_MUON_MOMENTUM, KK_NS_START,
                   KK_NS_GRAM, KK_NS_POLY, KK_NS_APPLY, KK_COUNT };
 void prof_begin(int kind, hipStream_t st);
 void prof_end(int kind, hipStream_t st);

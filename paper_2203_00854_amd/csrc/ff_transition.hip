@@ -1,5 +1,5 @@
 // The gated transition, y = (act(x Wa^T) * (x Wb^T)) Wo^T, and its gradients.
-#include "ff_tile.h"
+#include "ff_transition_rows.h"
 
 #include <algorithm>
 
@@ -150,6 +150,76 @@ template <class C, typename T> __global__ __launch_bounds__(C::kThreads, 2) void
         } else
             for (int q = 0; q < 4 && n + q < a.cols; ++q) out[q] = from_f32<T>((a.residual ? to_f32<T>(residual[q]) : 0.f) + (live ? v[0][q] : 0.f));
     });
+}
+
+// ---- the whole forward pass with rows in registers -------------------------------------------
+struct RowsArgs {
+    const bf16_t *x, *residual;
+    const char *w_a, *w_b, *w_o;
+    const float* mask;
+    bf16_t* y;
+    int64_t rows;
+    int32_t f, c, pitch_o;        // hidden channels, padded to 32; channels; bytes of a row of Wo
+    int32_t whole;                // rows of x (residual, y) are 32 KC channels and 16-byte aligned
+};
+template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 3 : KC <= 6 ? 2 : 1) void k_tr_rows(RowsArgs a) {
+    typedef rows::Weights<KC, 4> W;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    W::load(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
+    const int64_t row = (int64_t)blockIdx.x * 128 + wave * 32 + (lane & 31);
+    const bool there = row < a.rows, live = there && !(a.mask && a.mask[row] == 0.f);
+    uint4 x[2 * KC];
+    rows::load_row<KC>(x, a.x, row, live, a.c, a.whole, lane);
+    f32x16 y[KC];
+#pragma unroll
+    for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) y[i][v] = 0.f;
+    int buf = 0;
+    for (int f0 = 0; f0 < a.f; f0 += 32, buf ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();                                       // the stage is there, and nobody reads the other one any more
+        if (f0 + 32 < a.f) W::load(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
+        const unsigned char* part = smem + buf * W::kStage;
+        f32x16 p, q;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) p[v] = q[v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2 * KC; ++s) {
+            p = rows::mma(W::in(part, s, lane), x[s], p);
+            q = rows::mma(W::in(part + W::kIn, s, lane), x[s], q);
+        }
+        uint32_t h[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) h[v] = tile::pack2(gate_of<ACT, true>(p[2 * v]) * q[2 * v], gate_of<ACT, true>(p[2 * v + 1]) * q[2 * v + 1]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < KC; ++i) y[i] = rows::mma(W::out(part + 2 * W::kIn, i, t, lane), make_uint4(h[4 * t], h[4 * t + 1], h[4 * t + 2], h[4 * t + 3]), y[i]);
+    }
+    if (!there) return;
+    const int64_t at = row * a.c + 16 * hf;
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+        if (a.whole) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float v[8];
+                uint4 r = make_uint4(0, 0, 0, 0);
+                if (a.residual) r = *reinterpret_cast<const uint4*>(a.residual + at + 32 * i + 8 * u);
+                const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (live ? y[i][8 * u + e] : 0.f) + __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+                *reinterpret_cast<uint4*>(a.y + at + 32 * i + 8 * u) = make_uint4(tile::pack2(v[0], v[1]), tile::pack2(v[2], v[3]), tile::pack2(v[4], v[5]), tile::pack2(v[6], v[7]));
+            }
+        } else
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (32 * i + 16 * hf + e < a.c)
+                    a.y[at + 32 * i + e] = f32_to_bf16((live ? y[i][e] : 0.f) + (a.residual ? bf16_to_f32(a.residual[at + 32 * i + e]) : 0.f));
+    }
 }
 
 // ---- gradients of the hidden layer -----------------------------------------------------------
@@ -327,6 +397,46 @@ template <typename T> Weights weights_of(const ff_transition_desc& d, const Size
 
 constexpr int bk_of(int esz) { return esz == 2 ? 64 : 16; }
 
+// channels / 32 that the kernels with rows in registers are built for: the next one that holds c (0: none)
+int rows_tiles(const ff_transition_desc& d) {
+    const int need = (d.c + 31) / 32;
+    return d.dtype != FF_BF16 || need > 8 ? 0 : need == 1 ? 1 : (need + 1) / 2 * 2;
+}
+
+template <int KC> ff_status launch_rows(int act, const RowsArgs& a, hipStream_t stream) {
+    typedef rows::Weights<KC, 4> W;
+    const auto kernel = act == FF_SILU ? k_tr_rows<KC, FF_SILU> : act == FF_GELU ? k_tr_rows<KC, FF_GELU> : k_tr_rows<KC, FF_SIGMOID>;
+    Timed t(KK_TR_ROWS, stream);
+    if (W::kLds > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, W::kLds);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)((a.rows + 127) / 128)), dim3(256), W::kLds, stream, a);
+    return check_launch("ff_gated_transition_forward");
+}
+ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual, const float* mask,
+                       void* y, void* ws_, hipStream_t stream) {
+    const int64_t cp = kc * 32, fp = round_up(d.f, 32);
+    const void* from[3] = {w_a, w_b, w_o};
+    if (d.c != cp || d.f != fp || !aligned(w_a) || !aligned(w_b) || !aligned(w_o)) {
+        PackJob jobs[3];
+        char* ws = (char*)ws_;
+        for (int i = 0; i < 3; ++i) {
+            jobs[i] = i < 2 ? pack_job(from[i], ws, nullptr, d.f, fp, d.c, cp, 2) : pack_job(from[i], ws, nullptr, d.c, cp, d.f, fp, 2);
+            from[i] = ws;
+            ws += align256((size_t)(fp * cp * 2));
+        }
+        const ff_status st = pack<bf16_t>(jobs, 3, stream);
+        if (st != FF_OK) return st;
+    }
+    const RowsArgs a{(const bf16_t*)x, (const bf16_t*)residual, (const char*)from[0], (const char*)from[1], (const char*)from[2], mask, (bf16_t*)y, d.rows, (int32_t)fp, d.c,
+                     (int32_t)(fp * 2), d.c == cp && aligned(x) && aligned(residual) && aligned(y)};
+    switch (kc) {
+        case 1: return launch_rows<1>(d.act, a, stream);
+        case 2: return launch_rows<2>(d.act, a, stream);
+        case 4: return launch_rows<4>(d.act, a, stream);
+        case 6: return launch_rows<6>(d.act, a, stream);
+        default: return launch_rows<8>(d.act, a, stream);
+    }
+}
+
 template <typename T> ff_status forward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                         const float* mask, void* y, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
@@ -441,6 +551,7 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
 }  // namespace
 
 size_t transition_forward_workspace(const ff_transition_desc& d) {
+    if (const int kc = rows_tiles(d)) return std::max<size_t>(256, 3 * align256((size_t)(round_up(d.f, 32) * kc * 64)));
     const Sizes s = sizes_of(d);
     return 3 * s.weight + s.tokens + s.hidden;
 }
@@ -450,6 +561,7 @@ size_t transition_backward_workspace(const ff_transition_desc& d) {
 }
 ff_status transition_forward_run(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                  const float* mask, void* y, void* ws, hipStream_t stream) {
+    if (const int kc = rows_tiles(d)) return forward_rows(d, kc, x, w_a, w_b, w_o, residual, mask, y, ws, stream);
     return d.dtype == FF_F32 ? forward<float>(d, x, w_a, w_b, w_o, residual, mask, y, ws, stream)
                              : forward<bf16_t>(d, x, w_a, w_b, w_o, residual, mask, y, ws, stream);
 }
