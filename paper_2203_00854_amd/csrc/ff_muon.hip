@@ -79,8 +79,6 @@ __device__ __forceinline__ Place place_at(const Table& t, uint32_t block) {
     return {(int32_t)(block / (uint32_t)t.each), (int32_t)(block % (uint32_t)t.each)};
 }
 
-template <typename T> __device__ __forceinline__ __attribute__((address_space(1))) T* global(T* p) { return (__attribute__((address_space(1))) T*)p; }
-
 // ---- pairs ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t half_bits(_Float16 h) { return __builtin_bit_cast(uint16_t, h); }
 __device__ __forceinline__ void split(float v, uint32_t& hi, uint32_t& lo) {
@@ -91,19 +89,19 @@ __device__ __forceinline__ void split(float v, uint32_t& hi, uint32_t& lo) {
 __device__ __forceinline__ float join(uint32_t hi, uint32_t lo) {
     return (float)__builtin_bit_cast(_Float16, (uint16_t)hi) + (float)__builtin_bit_cast(_Float16, (uint16_t)lo);
 }
-// four values of a row, at p and a plane further
-__device__ __forceinline__ void store_pairs(char* p, int64_t plane, const float* v, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+// eight values of a row, at p and a plane further
+__device__ __forceinline__ void store_pairs(char* p, int64_t plane, const float (&v)[8]) {
+    uint32_t hi[8], lo[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) split(v[q], hi[q], lo[q]);
-    *(uint2*)p = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-    *(uint2*)(p + plane) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    for (int q = 0; q < 8; ++q) split(v[q], hi[q], lo[q]);
+    *(uint4*)p = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
+    *(uint4*)(p + plane) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
 }
-__device__ __forceinline__ void load_pairs(const char* p, int64_t plane, float* v) {
-    const uint2 h = *(const uint2*)p, l = *(const uint2*)(p + plane);
-    v[0] = join(h.x & 0xffffu, l.x & 0xffffu);
-    v[1] = join(h.x >> 16, l.x >> 16);
-    v[2] = join(h.y & 0xffffu, l.y & 0xffffu);
-    v[3] = join(h.y >> 16, l.y >> 16);
+__device__ __forceinline__ void load_pairs(const char* p, int64_t plane, float (&v)[8]) {
+    const uint4 h4 = *(const uint4*)p, l4 = *(const uint4*)(p + plane);
+    const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu);
 }
 
 // ---- momentum and norm ---------------------------------------------------------------------
@@ -136,35 +134,6 @@ __device__ __forceinline__ Spot spot_of(const Matrix& x, int64_t i) {
     s.at = s.r * x.cols + s.c;
     return s;
 }
-typedef __attribute__((__vector_size__(16), aligned(2))) uint32_t Words;       // (gfx950 reads and writes vectors at any alignment of their elements)
-template <typename T> __device__ __forceinline__ void load8(const T* p, const Spot& s, float (&v)[8]) {
-    if (s.n == 8) {
-        const auto* from = (const __attribute__((address_space(1))) Words*)(p + s.at);
-        const Words w[2] = {from[0], sizeof(T) == 4 ? from[1] : from[0]};
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            if constexpr (sizeof(T) == 4) v[q] = __uint_as_float(w[q / 4][q % 4]);
-            else v[q] = __uint_as_float(q & 1 ? w[0][q / 2] & 0xffff0000u : w[0][q / 2] << 16);
-        }
-    } else
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = q < s.n ? to_f32<T>(global(p)[s.at + q]) : 0.f;
-}
-__device__ __forceinline__ void store8(float* p, const Spot& s, const float (&v)[8]) {
-    if (s.n == 8) {
-        auto* to = (__attribute__((address_space(1))) Words*)(p + s.at);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Words w;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = __float_as_uint(v[4 * h + q]);
-            to[h] = w;
-        }
-    } else
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (q < s.n) global(p)[s.at + q] = v[q];
-}
 // the update that is orthogonalised, of the new momentum and the gradient
 __device__ __forceinline__ float update_of(float m, float g, const StepArgs& a) { return a.nesterov ? a.beta * m + a.rest * g : m; }
 
@@ -179,16 +148,16 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_m
     for (int64_t i = first + threadIdx.x * 8; i < first + kPiece && i < end; i += 256 * 8) {
         const Spot s = spot_of(x, i);
         float g[8], m[8];
-        load8((const G*)x.g, s, g);
+        tile::load_some((const G*)x.g + s.at, s.n, g);
         if constexpr (MUON) {
-            load8((const float*)x.m, s, m);
+            tile::load_some((const float*)x.m + s.at, s.n, m);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 g[q] *= k;
                 m[q] = a.beta * m[q] + a.rest * g[q];
                 g[q] = update_of(m[q], g[q], a);
             }
-            if (!skip) store8(x.m, s, m);
+            if (!skip) tile::store_some(x.m + s.at, s.n, m);
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum += q < s.n ? (double)g[q] * g[q] : 0.;
@@ -225,17 +194,15 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
     for (int64_t i = first + threadIdx.x * 8; i < first + kPiece && i < end; i += 256 * 8) {
         const Spot s = spot_of(x, i);
         float g[8], m[8];
-        load8((const G*)x.g, s, g);
+        tile::load_some((const G*)x.g + s.at, s.n, g);
         if constexpr (MUON) {
-            load8((const float*)x.m, s, m);                            // (the new one)
+            tile::load_some((const float*)x.m + s.at, s.n, m);                            // (the new one)
 #pragma unroll
             for (int q = 0; q < 8; ++q) g[q] = update_of(m[q], g[q] * k, a);
         }
-        uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) split(q < s.n ? (float)(g[q] * inv) : 0.f, hi[q], lo[q]);
-        *(uint4*)(out + 2 * i) = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
-        *(uint4*)(out + 2 * i + plane) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+        for (int q = 0; q < 8; ++q) g[q] = q < s.n ? (float)(g[q] * inv) : 0.f;
+        store_pairs(out + 2 * i, plane, g);
     }
 }
 
@@ -243,6 +210,8 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
 typedef Core<Pair, kTile, kTile, 32, 2, 2, 1, 1, false, 0u> Straight;      // rows by rows
 typedef Core<Pair, kTile, kTile, 32, 2, 2, 1, 1, true, 1u> Turned;         // columns by columns
 typedef Core<Pair, kTile, kTile, 32, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
+
+constexpr size_t kTileLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
     return {ws + x.x(which), x.plane_x(), x.cp() * 2, x.rp(), (int32_t)(x.cp() * 2)};
@@ -259,20 +228,14 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
 }
 // a tile of a symmetric matrix and its mirror image; value(m, n, v) turns sums into what is held
 template <class C, typename F>
-__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[1][C::MT][C::NT], char* out, int64_t np, int64_t plane, int i, int j, F value) {
-    C::each(acc, (int64_t)i * kTile, (int64_t)j * kTile, [&](int64_t m, int64_t n, float (&v)[1][4]) {
+__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], char* out, int64_t np, int64_t plane, int i, int j, unsigned char* smem, F value) {
+    const auto store = [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= np || n >= np) return;
-        value(m, n, v[0]);
-        uint32_t hi[4], lo[4];
-        store_pairs(out + (m * np + n) * 2, plane, v[0], hi, lo);
-        if (i != j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint16_t* p = (uint16_t*)(out + ((n + q) * np + m) * 2);
-                *p = (uint16_t)hi[q];
-                *(uint16_t*)((char*)p + plane) = (uint16_t)lo[q];
-            }
-    });
+        value(m, n, v);
+        store_pairs(out + (m * np + n) * 2, plane, v);
+    };
+    C::rows(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
+    if (i != j) C::columns(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
 }
 
 __global__ __launch_bounds__(256, 2) void k_ns_gram(Table t, char* ws, int which) {
@@ -286,9 +249,9 @@ __global__ __launch_bounds__(256, 2) void k_ns_gram(Table t, char* ws, int which
     Straight::clear(acc);
     if (x.tall()) Turned::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, x.rp(), smem);
     else Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, x.cp(), smem);
-    store_symmetric<Straight>(acc, ws + x.a(0), x.np(), x.plane_a(), i, j, [&](int64_t, int64_t, float* v) {
+    store_symmetric<Straight>(acc[0], ws + x.a(0), x.np(), x.plane_a(), i, j, smem, [&](int64_t, int64_t, float (&v)[8]) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] *= kUnscale;
+        for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
     });
 }
 
@@ -305,11 +268,11 @@ __global__ __launch_bounds__(256, 2) void k_ns_poly(Table t, char* ws, float b, 
     const int64_t np = x.np(), plane = x.plane_a();
     Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
     const char* a = ws + x.a(0);
-    store_symmetric<Straight>(acc, ws + x.a(1), np, plane, i, j, [&](int64_t m, int64_t n, float* v) {
-        float was[4];
+    store_symmetric<Straight>(acc[0], ws + x.a(1), np, plane, i, j, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+        float was[8];
         load_pairs(a + (m * np + n) * 2, plane, was);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = b * was[q] + (c * kUnscale) * v[q];
+        for (int q = 0; q < 8; ++q) v[q] = b * was[q] + (c * kUnscale) * v[q];
     });
 }
 
@@ -335,30 +298,30 @@ template <int LAST, typename P> __global__ __launch_bounds__(256, 2) void k_ns_a
     char* to = ws + x.x(which ^ 1);
     const int32_t longer = x.rows > x.cols ? x.rows : x.cols;
     const float size = a.lr * (a.rms ? 0.2f * sqrtf((float)longer) : sqrtf((float)longer / (float)x.cols)), decay = a.lr * x.decay;
-    Straight::each(acc, (int64_t)i * kTile, (int64_t)j * kTile, [&](int64_t m, int64_t n, float (&v)[1][4]) {
+    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= rp || n >= cp) return;
-        float was[4];
+        float was[8];
         load_pairs(from + (m * cp + n) * 2, plane, was);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[0][q] = a.a * was[q] + kUnscale * v[0][q];
-        if constexpr (LAST == kMore) {
-            uint32_t hi[4], lo[4];
-            store_pairs(to + (m * cp + n) * 2, plane, v[0], hi, lo);
-        } else {
-            if (m >= x.rows) return;
+        for (int q = 0; q < 8; ++q) v[q] = a.a * was[q] + kUnscale * v[q];
+        if constexpr (LAST == kMore) store_pairs(to + (m * cp + n) * 2, plane, v);
+        else {
+            const int left = x.cols - (int)n;
+            if (m >= x.rows || left <= 0) return;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (n + q < x.cols) {
-                    const int64_t e = m * x.cols + n + q;
-                    auto* p = global((P*)x.p) + e;
-                    if constexpr (LAST == kOut) *p = from_f32<P>(kUnscale * v[0][q]);
-                    else {
-                        float w = x.master ? global(x.master)[e] : to_f32<P>(*p);
-                        w -= decay * w + size * (kUnscale * v[0][q]);
-                        if (x.master) global(x.master)[e] = w;
-                        *p = from_f32<P>(w);
-                    }
-                }
+            for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
+            P* p = (P*)x.p + m * x.cols + n;
+            if constexpr (LAST == kOut) tile::store_some(p, left, v);
+            else {
+                float w[8];
+                float* master = x.master + m * x.cols + n;
+                if (x.master) tile::load_some((const float*)master, left, w);
+                else tile::load_some((const P*)p, left, w);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) w[q] -= decay * w[q] + size * v[q];
+                if (x.master) tile::store_some(master, left, w);
+                tile::store_some(p, left, w);
+            }
         }
     });
 }
@@ -375,9 +338,10 @@ int tris_of(const Matrix& m) {
 }
 int apps_of(const Matrix& m) { return (int)((m.rp() + kTile - 1) / kTile * ((m.cp() + kTile - 1) / kTile)); }
 
-template <typename K, typename... A> ff_status go(int kind, K kernel, uint32_t blocks, size_t lds, hipStream_t stream, const char* what, A... args) {
+template <auto KERNEL, typename... A> ff_status go(int kind, uint32_t blocks, size_t lds, hipStream_t stream, const char* what, A... args) {
     Timed t(kind, stream);
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, stream, args...);
+    if (lds) tile::allow_lds<KERNEL>();
+    hipLaunchKernelGGL(KERNEL, dim3(blocks), dim3(256), lds, stream, args...);
     return check_launch(what);
 }
 
@@ -389,14 +353,14 @@ struct Tables {
 template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, const StepArgs& a, int steps, const float* norm, double* partial, char* ws, hipStream_t stream) {
     constexpr bool MUON = LAST == kWeights;
     const char* what = MUON ? "ff_muon_step" : "ff_orthogonalise";
-    ff_status st = go(KK_MUON_MOMENTUM, k_muon_momentum<G, MUON>, t.pieces, 0, stream, what, t.piece, a, norm, partial);
-    if (st == FF_OK) st = go(KK_NS_START, k_ns_start<G, MUON>, t.pieces, 0, stream, what, t.piece, a, norm, (const double*)partial, ws);
+    ff_status st = go<k_muon_momentum<G, MUON>>(KK_MUON_MOMENTUM, t.pieces, 0, stream, what, t.piece, a, norm, partial);
+    if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 0, stream, what, t.piece, a, norm, (const double*)partial, ws);
     for (int s = 0; s < steps && st == FF_OK; ++s) {
-        st = go(KK_NS_GRAM, k_ns_gram, t.tris, Straight::kLds, stream, what, t.tri, ws, s & 1);
-        if (st == FF_OK) st = go(KK_NS_POLY, k_ns_poly, t.tris, Straight::kLds, stream, what, t.tri, ws, a.b, a.c);
+        st = go<k_ns_gram>(KK_NS_GRAM, t.tris, kTileLds, stream, what, t.tri, ws, s & 1);
+        if (st == FF_OK) st = go<k_ns_poly>(KK_NS_POLY, t.tris, kTileLds, stream, what, t.tri, ws, a.b, a.c);
         if (st != FF_OK) return st;
-        if (s + 1 < steps) st = go(KK_NS_APPLY, k_ns_apply<kMore, float>, t.apps, Straight::kLds, stream, what, t.app, ws, s & 1, a, norm);
-        else st = go(KK_NS_APPLY, k_ns_apply<LAST, P>, t.apps, Straight::kLds, stream, what, t.app, ws, s & 1, a, norm);
+        if (s + 1 < steps) st = go<k_ns_apply<kMore, float>>(KK_NS_APPLY, t.apps, kTileLds, stream, what, t.app, ws, s & 1, a, norm);
+        else st = go<k_ns_apply<LAST, P>>(KK_NS_APPLY, t.apps, kTileLds, stream, what, t.app, ws, s & 1, a, norm);
     }
     return st;
 }

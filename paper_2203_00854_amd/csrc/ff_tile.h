@@ -33,6 +33,40 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {      // a -> low h
     return __builtin_bit_cast(uint32_t, t);
 }
 
+// ---- eight neighbours, at any alignment of their elements (gfx950 reads and writes vectors there) ----
+typedef __attribute__((__vector_size__(16), aligned(2))) uint32_t Words;
+typedef __attribute__((address_space(1))) Words GlobalWords;
+__device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
+    const Words w = *(const GlobalWords*)p;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(q & 1 ? w[q / 2] & 0xffff0000u : w[q / 2] << 16);
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const Words w[2] = {((const GlobalWords*)p)[0], ((const GlobalWords*)p)[1]};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(w[q / 4][q % 4]);
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+    *(GlobalWords*)p = Words{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        ((GlobalWords*)p)[h] = Words{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
+}
+// n of the eight (a caller's row may end inside them)
+template <typename T> __device__ __forceinline__ void load_some(const T* p, int n, float (&v)[8]) {
+    if (n >= 8) return load8(p, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = q < n ? to_f32<T>(((const __attribute__((address_space(1))) T*)p)[q]) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[8]) {
+    if (n >= 8) return store8(p, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        if (q < n) ((__attribute__((address_space(1))) T*)p)[q] = from_f32<T>(v[q]);
+}
+
 // kStep values of k make one round of matrix instructions, 32 bytes of a row of either operand.
 struct Bf16 {
     static constexpr int kSize = 2, kPlanes = 1, kStep = 16;
@@ -85,7 +119,6 @@ struct Core {
     static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
     static constexpr int kPlaneA = BM * BK * Op::kSize, kPlaneB = BN * BK * Op::kSize;
     static constexpr int kStage = Op::kPlanes * (NA * kPlaneA + NB * kPlaneB);
-    static constexpr int kLds = 2 * kStage;
     static_assert(MT >= 1 && NT >= 1 && BK % Op::kStep == 0, "tile");
 
     // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that the lanes that read in one cycle
@@ -221,25 +254,56 @@ struct Core {
         __syncthreads();
     }
 
-    // body(b, m, n, v): four results v of product b in row m, columns n .. n + 3
-    template <typename F> static __device__ __forceinline__ void each(f32x16 (&acc)[NB][MT][NT], int64_t m0, int64_t n0, F body) {
+    // Results leave through LDS, where a lane finds eight neighbours of a row: straight from the accumulators a store would reach sixteen bytes of each of 32 rows,
+    // and the stores of a tile would take longer than its products.
+    static constexpr int kPitch = BN + 4, kPitchTurned = BM + 4;        // floats; sixteen bytes more than a row, so that the rows of one cycle lie in banks of their own
+    static constexpr int kOut = 4 * BM * kPitch > 4 * BN * kPitchTurned ? 4 * BM * kPitch : 4 * BN * kPitchTurned;
+    static constexpr int kLds = 2 * kStage > kOut ? 2 * kStage : kOut;
+
+    // body(m, n, v): eight results v in row m, columns n .. n + 7.  smem: kLds bytes that every thread is done with, before and after
+    template <typename F> static __device__ __forceinline__ void rows(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, F body) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        const int wm = wave / WN, wn = wave % WN;
+        float* out = (float*)smem + ((wave / WN * MT) * 32 + (lane & 31)) * kPitch + (wave % WN * NT) * 32 + 4 * (lane >> 5);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    float v[NB][4];
+                for (int g = 0; g < 4; ++g)
+                    *(float4*)(out + i * 32 * kPitch + j * 32 + 8 * g) = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+        __syncthreads();
+        read<BM, BN, kPitch>(smem, m0, n0, body);
+        __syncthreads();
+    }
+    // the same turned: row n, columns m .. m + 7
+    template <typename F> static __device__ __forceinline__ void columns(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, F body) {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        float* out = (float*)smem + ((wave % WN * NT) * 32 + 4 * (lane >> 5)) * kPitchTurned + (wave / WN * MT) * 32 + (lane & 31);
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) v[b][q] = acc[b][i][j][4 * g + q];
-                    body(m0 + (wm * MT + i) * 32 + (lane & 31), n0 + (wn * NT + j) * 32 + 8 * g + 4 * (lane >> 5), v);
-                }
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) out[(j * 32 + 8 * (v / 4) + v % 4) * kPitchTurned + i * 32] = acc[i][j][v];
+        __syncthreads();
+        read<BN, BM, kPitchTurned>(smem, n0, m0, body);
+        __syncthreads();
+    }
+    template <int R, int C, int PITCH, typename F> static __device__ __forceinline__ void read(const unsigned char* smem, int64_t r0, int64_t c0, F body) {
+        for (int u = threadIdx.x; u < R * (C / 8); u += kThreads) {
+            const int r = u / (C / 8), c = u % (C / 8) * 8;
+            const float4 a = *(const float4*)((const float*)smem + r * PITCH + c), b = *(const float4*)((const float*)smem + r * PITCH + c + 4);
+            float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            body(r0 + r, c0 + c, v);
+        }
     }
 };
+
+// once for each kernel that needs more than 64 KiB
+template <auto KERNEL> static void allow_lds() {
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    (void)once;
+}
 
 // Blocks of the same rows of A run one after another on one XCD (block i starts on XCD i % 8), whose L2 then holds them, while B is small enough for all.
 struct TilePlace {

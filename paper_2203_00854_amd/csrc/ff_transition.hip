@@ -48,21 +48,6 @@ template <int ACT, bool FAST> __device__ __forceinline__ float gate_of(float a, 
     return a * s;
 }
 
-// ---- four values of a row ----------------------------------------------------------------
-struct __attribute__((packed, aligned(2))) Half4 { uint32_t w[2]; };      // (gfx950 reads and writes vectors at any alignment of their elements)
-struct __attribute__((packed, aligned(4))) Float4 { float w[4]; };
-
-__device__ __forceinline__ void store4(bf16_t* p, const float* v) { *(Half4*)p = Half4{{tile::pack2(v[0], v[1]), tile::pack2(v[2], v[3])}}; }
-__device__ __forceinline__ void store4(float* p, const float* v) { *(Float4*)p = Float4{{v[0], v[1], v[2], v[3]}}; }
-__device__ __forceinline__ void load4(const bf16_t* p, float* v) {
-    const Half4 h = *(const Half4*)p;
-    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(i & 1 ? h.w[i / 2] & 0xffff0000u : h.w[i / 2] << 16);
-}
-__device__ __forceinline__ void load4(const float* p, float* v) {
-    const Float4 f = *(const Float4*)p;
-    for (int i = 0; i < 4; ++i) v[i] = f.w[i];
-}
-
 // ---- packing -------------------------------------------------------------------------------
 // Copies whose rows and columns are padded with zeros, masked rows zero: what is not aligned to sixteen bytes, or has odd sizes, or rows whose values
 // must not reach sums over rows.  A thread writes sixteen bytes.
@@ -94,6 +79,13 @@ template <typename T> __global__ __launch_bounds__(256) void k_tr_pack(PackArgs 
     *(uint4*)((T*)p.dst + r * p.cols_out + c) = *(const uint4*)v;
 }
 
+// what is past the end of a row, or in a row that is none, is held as zero
+__device__ __forceinline__ void keep(float (&v)[8], int64_t n) {
+    if (n >= 8) return;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = q < n ? v[q] : 0.f;
+}
+
 // ---- hidden layer --------------------------------------------------------------------------
 struct HiddenArgs {
     Operand x, w[2];
@@ -109,12 +101,16 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
     f32x16 acc[2][C::MT][C::NT];
     C::clear(acc);
     C::run(acc, &a.x, a.w, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
-    C::each(acc, at.m * C::BM, (int64_t)at.n * C::BN, [&](int64_t m, int64_t n, float (&v)[2][4]) {
-        if (m >= a.rows_out || n >= a.pitch) return;
-        float h[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) h[q] = m < a.rows && n + q < a.f ? gate_of<ACT, sizeof(T) == 2>(v[0][q]) * v[1][q] : 0.f;
-        store4((T*)a.h + m * a.pitch + n, h);
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < C::NT; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[0][i][j][v] = gate_of<ACT, sizeof(T) == 2>(acc[0][i][j][v]) * acc[1][i][j][v];
+    C::rows(acc[0], at.m * C::BM, (int64_t)at.n * C::BN, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+        if (m >= a.rows_out || n >= a.pitch) return;
+        keep(v, m < a.rows ? a.f - n : 0);
+        tile::store8((T*)a.h + m * a.pitch + n, v);
     });
 }
 
@@ -136,19 +132,15 @@ template <class C, typename T> __global__ __launch_bounds__(C::kThreads, 2) void
     f32x16 acc[1][C::MT][C::NT];
     C::clear(acc);
     for (int p = 0; p < a.parts; ++p) C::run(acc, a.a + p, a.b + p, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
-    C::each(acc, at.m * C::BM, (int64_t)at.n * C::BN, [&](int64_t m, int64_t n, float (&v)[1][4]) {
+    C::rows(acc[0], at.m * C::BM, (int64_t)at.n * C::BN, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= a.rows || n >= a.cols) return;
         const bool live = !(a.mask && a.mask[m] == 0.f);
-        T* out = (T*)a.out + m * a.cols + n;
-        const T* residual = (const T*)a.residual + m * a.cols + n;
-        if (n + 4 <= a.cols) {
-            float r[4] = {0.f, 0.f, 0.f, 0.f};
-            if (a.residual) load4(residual, r);
+        const int left = a.cols - (int)n;
+        float r[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (a.residual) tile::load_some((const T*)a.residual + m * a.cols + n, left, r);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) r[q] += live ? v[0][q] : 0.f;
-            store4(out, r);
-        } else
-            for (int q = 0; q < 4 && n + q < a.cols; ++q) out[q] = from_f32<T>((a.residual ? to_f32<T>(residual[q]) : 0.f) + (live ? v[0][q] : 0.f));
+        for (int q = 0; q < 8; ++q) r[q] += live ? v[q] : 0.f;
+        tile::store_some((T*)a.out + m * a.cols + n, left, r);
     });
 }
 
@@ -238,23 +230,26 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
     f32x16 acc[3][C::MT][C::NT];
     C::clear(acc);
     C::run(acc, a.a, a.b, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
-    C::each(acc, at.m * C::BM, (int64_t)at.n * C::BN, [&](int64_t m, int64_t n, float (&v)[3][4]) {
-        if (m >= a.rows_out || n >= a.pitch) return;
-        float da[4], db[4], h[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const bool there = m < a.rows && n + q < a.f;
-            float slope;
-            const float gate = gate_of<ACT, sizeof(T) == 2>(v[0][q], slope);
-            da[q] = there ? v[2][q] * v[1][q] * slope : 0.f;
-            db[q] = there ? v[2][q] * gate : 0.f;
-            h[q] = there ? gate * v[1][q] : 0.f;
-        }
-        const int64_t i = m * a.pitch + n;
-        store4((T*)a.da + i, da);
-        store4((T*)a.db + i, db);
-        store4((T*)a.h + i, h);
-    });
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < C::NT; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                float slope;
+                const float gate = gate_of<ACT, sizeof(T) == 2>(acc[0][i][j][v], slope), b = acc[1][i][j][v], dh = acc[2][i][j][v];
+                acc[0][i][j][v] = dh * b * slope;
+                acc[1][i][j][v] = dh * gate;
+                acc[2][i][j][v] = gate * b;
+            }
+    void* const out[3] = {a.da, a.db, a.h};
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+        C::rows(acc[t], at.m * C::BM, (int64_t)at.n * C::BN, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+            if (m >= a.rows_out || n >= a.pitch) return;
+            keep(v, m < a.rows ? a.f - n : 0);
+            tile::store8((T*)out[t] + m * a.pitch + n, v);
+        });
 }
 
 // ---- gradients of the weights ------------------------------------------------------------------
@@ -279,16 +274,16 @@ template <class C> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_weight
     C::run(acc, a.a + which, a.b + which, m0, n0, from, to, smem);
     float* out = a.partial + ((int64_t)blockIdx.y * 3 + which) * a.fp * a.cp;
     const int32_t rows = last ? a.cp : a.fp, cols = last ? a.fp : a.cp;
-    C::each(acc, m0, n0, [&](int64_t m, int64_t n, float (&v)[1][4]) {
+    C::rows(acc[0], m0, n0, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= rows || n >= cols) return;
         float* p = out + m * cols + n;
         if (a.add) {
-            float was[4];
-            load4(p, was);
+            float was[8];
+            tile::load8(p, was);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[0][q] += was[q];
+            for (int q = 0; q < 8; ++q) v[q] += was[q];
         }
-        store4(p, v[0]);
+        tile::store8(p, v);
     });
 }
 
@@ -342,10 +337,10 @@ Sizes sizes_of(const ff_transition_desc& d) {
 
 bool aligned(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
-template <class C, typename Kernel, typename Args> ff_status launch(int kind, const char* what, Kernel kernel, dim3 grid, const Args& args, hipStream_t stream) {
+template <class C, auto KERNEL, typename Args> ff_status launch(int kind, const char* what, dim3 grid, const Args& args, hipStream_t stream) {
     Timed t(kind, stream);
-    if (C::kLds > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
-    hipLaunchKernelGGL(kernel, grid, dim3(C::kThreads), C::kLds, stream, args);
+    tile::allow_lds<KERNEL>();
+    hipLaunchKernelGGL(KERNEL, grid, dim3(C::kThreads), C::kLds, stream, args);
     return check_launch(what);
 }
 
@@ -405,11 +400,11 @@ int rows_tiles(const ff_transition_desc& d) {
 
 template <int KC> ff_status launch_rows(int act, const RowsArgs& a, hipStream_t stream) {
     typedef rows::Weights<KC, 4> W;
-    const auto kernel = act == FF_SILU ? k_tr_rows<KC, FF_SILU> : act == FF_GELU ? k_tr_rows<KC, FF_GELU> : k_tr_rows<KC, FF_SIGMOID>;
-    Timed t(KK_TR_ROWS, stream);
-    if (W::kLds > 65536) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, W::kLds);
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)((a.rows + 127) / 128)), dim3(256), W::kLds, stream, a);
-    return check_launch("ff_gated_transition_forward");
+    const dim3 grid((uint32_t)((a.rows + 127) / 128));
+    const char* what = "ff_gated_transition_forward";
+    return act == FF_SILU   ? launch<W, k_tr_rows<KC, FF_SILU>>(KK_TR_ROWS, what, grid, a, stream)
+           : act == FF_GELU ? launch<W, k_tr_rows<KC, FF_GELU>>(KK_TR_ROWS, what, grid, a, stream)
+                            : launch<W, k_tr_rows<KC, FF_SIGMOID>>(KK_TR_ROWS, what, grid, a, stream);
 }
 ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual, const float* mask,
                        void* y, void* ws_, hipStream_t stream) {
@@ -460,9 +455,9 @@ template <typename T> ff_status forward(const ff_transition_desc& d, const void*
         HiddenArgs ha{operand(as_is ? (const void*)xr : tokens, s.cp, rows, s.cp, s.esz), {w.a, w.b}, hidden, rows, rows, d.f, (int32_t)s.cp, (int32_t)s.fp,
                       (uint32_t)((rows + CH::BM - 1) / CH::BM), (uint32_t)((s.fp + CH::BN - 1) / CH::BN)};
         const dim3 grid(ha.mtiles * ha.ntiles);
-        ff_status st = d.act == FF_SILU   ? launch<CH>(KK_TR_HIDDEN, "ff_gated_transition_forward", k_tr_hidden<CH, T, FF_SILU>, grid, ha, stream)
-                       : d.act == FF_GELU ? launch<CH>(KK_TR_HIDDEN, "ff_gated_transition_forward", k_tr_hidden<CH, T, FF_GELU>, grid, ha, stream)
-                                          : launch<CH>(KK_TR_HIDDEN, "ff_gated_transition_forward", k_tr_hidden<CH, T, FF_SIGMOID>, grid, ha, stream);
+        ff_status st = d.act == FF_SILU   ? launch<CH, k_tr_hidden<CH, T, FF_SILU>>(KK_TR_HIDDEN, "ff_gated_transition_forward", grid, ha, stream)
+                       : d.act == FF_GELU ? launch<CH, k_tr_hidden<CH, T, FF_GELU>>(KK_TR_HIDDEN, "ff_gated_transition_forward", grid, ha, stream)
+                                          : launch<CH, k_tr_hidden<CH, T, FF_SIGMOID>>(KK_TR_HIDDEN, "ff_gated_transition_forward", grid, ha, stream);
         if (st != FF_OK) return st;
         OutArgs oa{};
         oa.a[0] = operand(hidden, s.fp, rows, s.fp, s.esz);
@@ -476,7 +471,7 @@ template <typename T> ff_status forward(const ff_transition_desc& d, const void*
         oa.out = (T*)y + r0 * d.c;
         oa.mtiles = (uint32_t)((rows + CO::BM - 1) / CO::BM);
         oa.ntiles = (uint32_t)((d.c + CO::BN - 1) / CO::BN);
-        st = launch<CO>(KK_TR_OUT, "ff_gated_transition_forward", k_tr_out<CO, T>, dim3(oa.mtiles * oa.ntiles), oa, stream);
+        st = launch<CO, k_tr_out<CO, T>>(KK_TR_OUT, "ff_gated_transition_forward", dim3(oa.mtiles * oa.ntiles), oa, stream);
         if (st != FF_OK) return st;
     }
     return FF_OK;
@@ -515,15 +510,15 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
         GradArgs ga{{ox, ody}, {w.a, w.b, w.o}, hidden[0], hidden[1], hidden[2], rows, padded, d.f, (int32_t)s.cp, (int32_t)s.fp,
                     (uint32_t)((padded + CG::BM - 1) / CG::BM), (uint32_t)((s.fp + CG::BN - 1) / CG::BN)};
         const dim3 grid(ga.mtiles * ga.ntiles);
-        st = d.act == FF_SILU   ? launch<CG>(KK_TR_GRAD, "ff_gated_transition_backward", k_tr_grad<CG, T, FF_SILU>, grid, ga, stream)
-             : d.act == FF_GELU ? launch<CG>(KK_TR_GRAD, "ff_gated_transition_backward", k_tr_grad<CG, T, FF_GELU>, grid, ga, stream)
-                                : launch<CG>(KK_TR_GRAD, "ff_gated_transition_backward", k_tr_grad<CG, T, FF_SIGMOID>, grid, ga, stream);
+        st = d.act == FF_SILU   ? launch<CG, k_tr_grad<CG, T, FF_SILU>>(KK_TR_GRAD, "ff_gated_transition_backward", grid, ga, stream)
+             : d.act == FF_GELU ? launch<CG, k_tr_grad<CG, T, FF_GELU>>(KK_TR_GRAD, "ff_gated_transition_backward", grid, ga, stream)
+                                : launch<CG, k_tr_grad<CG, T, FF_SIGMOID>>(KK_TR_GRAD, "ff_gated_transition_backward", grid, ga, stream);
         if (st != FF_OK) return st;
         Operand oh[3];
         for (int i = 0; i < 3; ++i) oh[i] = operand(hidden[i], s.fp, padded, s.fp, s.esz);
         WeightArgs wa{{oh[0], oh[1], ody}, {ox, ox, oh[2]}, partial, padded, s.per_split, (int32_t)s.fp, (int32_t)s.cp,
                       (uint32_t)((s.fp + 127) / 128), (uint32_t)((s.cp + 127) / 128), r0 > 0};
-        st = launch<CW>(KK_TR_WEIGHTS, "ff_gated_transition_backward", k_tr_weights<CW>, dim3(3 * wa.ftiles * wa.ctiles, s.splits), wa, stream);
+        st = launch<CW, k_tr_weights<CW>>(KK_TR_WEIGHTS, "ff_gated_transition_backward", dim3(3 * wa.ftiles * wa.ctiles, s.splits), wa, stream);
         if (st != FF_OK) return st;
         OutArgs oa{};
         oa.a[0] = oh[0];
@@ -537,7 +532,7 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
         oa.out = (T*)dx + r0 * d.c;
         oa.mtiles = (uint32_t)((rows + CX::BM - 1) / CX::BM);
         oa.ntiles = (uint32_t)((d.c + CX::BN - 1) / CX::BN);
-        st = launch<CX>(KK_TR_OUT, "ff_gated_transition_backward", k_tr_out<CX, T>, dim3(oa.mtiles * oa.ntiles), oa, stream);
+        st = launch<CX, k_tr_out<CX, T>>(KK_TR_OUT, "ff_gated_transition_backward", dim3(oa.mtiles * oa.ntiles), oa, stream);
         if (st != FF_OK) return st;
     }
     JoinArgs ja{partial, {dw[0], dw[1], dw[2]}, d.f, d.c, (int32_t)s.fp, (int32_t)s.cp, d.rows ? s.splits : 0, accumulate};

@@ -26,6 +26,7 @@ __device__ __forceinline__ f32x16 mma(uint4 a, uint4 b, f32x16 c) {
 // KC: channels / 32, 1 or even (the exchange of slots stays within eight)
 template <int KC, int WAVES> struct Weights {
     static_assert(KC == 1 || KC % 2 == 0, "slots");
+    static constexpr int kThreads = 64 * WAVES;
     static constexpr int W = KC * 4;                              // slots of sixteen bytes of a row of Wa
     static constexpr int kIn = 32 * W * 16, kOut = KC * 32 * 64;  // bytes of Wa's (Wb's) part of a stage, of Wo's
     static constexpr int kStage = 2 * kIn + kOut;
