@@ -38,7 +38,7 @@ struct Matrix {
     void* p;                                     // what the last step writes
     float* master;
     float* m;
-    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B; two planes each
+    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B, as pairs
     int32_t rows, cols;
     int32_t piece0, pieces;                      // among the batch's
     float decay;
@@ -47,11 +47,11 @@ struct Matrix {
     __host__ __device__ int64_t rp() const { return (rows + kPad - 1) / kPad * kPad; }
     __host__ __device__ int64_t cp() const { return (cols + kPad - 1) / kPad * kPad; }
     __host__ __device__ int64_t np() const { return tall() ? cp() : rp(); }
-    __host__ __device__ int64_t plane_x() const { return rp() * cp() * 2; }
-    __host__ __device__ int64_t plane_a() const { return np() * np() * 2; }
-    __host__ __device__ int64_t x(int which) const { return ws + which * 2 * plane_x(); }
-    __host__ __device__ int64_t a(int which) const { return ws + 4 * plane_x() + which * 2 * plane_a(); }
-    __host__ __device__ int64_t bytes() const { return 4 * plane_x() + 4 * plane_a(); }
+    __host__ __device__ int64_t bytes_x() const { return rp() * cp() * 4; }
+    __host__ __device__ int64_t bytes_a() const { return np() * np() * 4; }
+    __host__ __device__ int64_t x(int which) const { return ws + which * bytes_x(); }
+    __host__ __device__ int64_t a(int which) const { return ws + 2 * bytes_x() + which * bytes_a(); }
+    __host__ __device__ int64_t bytes() const { return 2 * bytes_x() + 2 * bytes_a(); }
 };
 struct Place {
     int32_t matrix, at;
@@ -89,16 +89,17 @@ __device__ __forceinline__ void split(float v, uint32_t& hi, uint32_t& lo) {
 __device__ __forceinline__ float join(uint32_t hi, uint32_t lo) {
     return (float)__builtin_bit_cast(_Float16, (uint16_t)hi) + (float)__builtin_bit_cast(_Float16, (uint16_t)lo);
 }
-// eight values of a row, at p and a plane further
-__device__ __forceinline__ void store_pairs(char* p, int64_t plane, const float (&v)[8]) {
+// eight values of a row from value i of a matrix on (rows are multiples of sixteen values): their hi parts, and 32 bytes further their lo parts
+__device__ __forceinline__ int64_t pairs_at(int64_t i) { return (i >> 4) * 64 + (i & 8) * 2; }
+__device__ __forceinline__ void store_pairs(char* p, const float (&v)[8]) {
     uint32_t hi[8], lo[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) split(v[q], hi[q], lo[q]);
     *(uint4*)p = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
-    *(uint4*)(p + plane) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+    *(uint4*)(p + 32) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
 }
-__device__ __forceinline__ void load_pairs(const char* p, int64_t plane, float (&v)[8]) {
-    const uint4 h4 = *(const uint4*)p, l4 = *(const uint4*)(p + plane);
+__device__ __forceinline__ void load_pairs(const char* p, float (&v)[8]) {
+    const uint4 h4 = *(const uint4*)p, l4 = *(const uint4*)(p + 32);
     const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] = q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu);
@@ -189,7 +190,7 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
         __syncthreads();
     }
     const double inv = (double)kScale / (sqrt(sums[0]) + a.eps);
-    const int64_t end = x.rp() * x.cp(), first = (int64_t)at.at * kPiece, plane = x.plane_x();
+    const int64_t end = x.rp() * x.cp(), first = (int64_t)at.at * kPiece;
     char* out = ws + x.x(0);
     for (int64_t i = first + threadIdx.x * 8; i < first + kPiece && i < end; i += 256 * 8) {
         const Spot s = spot_of(x, i);
@@ -202,22 +203,22 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) g[q] = q < s.n ? (float)(g[q] * inv) : 0.f;
-        store_pairs(out + 2 * i, plane, g);
+        store_pairs(out + pairs_at(i), g);
     }
 }
 
 // ---- the products --------------------------------------------------------------------------
-typedef Core<Pair, kTile, kTile, 32, 2, 2, 1, 1, false, 0u> Straight;      // rows by rows
-typedef Core<Pair, kTile, kTile, 32, 2, 2, 1, 1, true, 1u> Turned;         // columns by columns
-typedef Core<Pair, kTile, kTile, 32, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
+typedef Core<Pair, kTile, kTile, 16, 4, 2, 2, 1, 1, false, 0u> Straight;      // rows by rows
+typedef Core<Pair, kTile, kTile, 16, 4, 2, 2, 1, 1, true, 1u> Turned;         // columns by columns
+typedef Core<Pair, kTile, kTile, 16, 4, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
 
 constexpr size_t kTileLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
-    return {ws + x.x(which), x.plane_x(), x.cp() * 2, x.rp(), (int32_t)(x.cp() * 2)};
+    return {ws + x.x(which), x.cp() * 4, x.rp(), (int32_t)(x.cp() * 4)};
 }
 __device__ __forceinline__ Operand operand_a(const Matrix& x, const char* ws, int which) {
-    return {ws + x.a(which), x.plane_a(), x.np() * 2, x.np(), (int32_t)(x.np() * 2)};
+    return {ws + x.a(which), x.np() * 4, x.np(), (int32_t)(x.np() * 4)};
 }
 // tile t of the lower triangle, row by row
 __device__ __forceinline__ void triangle(int t, int& i, int& j) {
@@ -228,11 +229,11 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
 }
 // a tile of a symmetric matrix and its mirror image; value(m, n, v) turns sums into what is held
 template <class C, typename F>
-__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], char* out, int64_t np, int64_t plane, int i, int j, unsigned char* smem, F value) {
+__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], char* out, int64_t np, int i, int j, unsigned char* smem, F value) {
     const auto store = [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= np || n >= np) return;
         value(m, n, v);
-        store_pairs(out + (m * np + n) * 2, plane, v);
+        store_pairs(out + pairs_at(m * np + n), v);
     };
     C::rows(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
     if (i != j) C::columns(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void k_ns_gram(Table t, char* ws, int which
     Straight::clear(acc);
     if (x.tall()) Turned::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, x.rp(), smem);
     else Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, x.cp(), smem);
-    store_symmetric<Straight>(acc[0], ws + x.a(0), x.np(), x.plane_a(), i, j, smem, [&](int64_t, int64_t, float (&v)[8]) {
+    store_symmetric<Straight>(acc[0], ws + x.a(0), x.np(), i, j, smem, [&](int64_t, int64_t, float (&v)[8]) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
     });
@@ -265,12 +266,12 @@ __global__ __launch_bounds__(256, 2) void k_ns_poly(Table t, char* ws, float b, 
     const Operand o = operand_a(x, ws, 0);
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
-    const int64_t np = x.np(), plane = x.plane_a();
+    const int64_t np = x.np();
     Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
     const char* a = ws + x.a(0);
-    store_symmetric<Straight>(acc[0], ws + x.a(1), np, plane, i, j, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+    store_symmetric<Straight>(acc[0], ws + x.a(1), np, i, j, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
         float was[8];
-        load_pairs(a + (m * np + n) * 2, plane, was);
+        load_pairs(a + pairs_at(m * np + n), was);
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = b * was[q] + (c * kUnscale) * v[q];
     });
@@ -287,7 +288,7 @@ template <int LAST, typename P> __global__ __launch_bounds__(256, 2) void k_ns_a
         (void)clip_of(norm, a.max_norm, skip);
         if (skip) return;
     }
-    const int64_t rp = x.rp(), cp = x.cp(), plane = x.plane_x();
+    const int64_t rp = x.rp(), cp = x.cp();
     const int ntiles = (int)((cp + kTile - 1) / kTile), i = at.at / ntiles, j = at.at % ntiles;
     const Operand ox = operand_x(x, ws, which), ob = operand_a(x, ws, 1);
     f32x16 acc[1][Straight::MT][Straight::NT];
@@ -301,10 +302,10 @@ template <int LAST, typename P> __global__ __launch_bounds__(256, 2) void k_ns_a
     Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= rp || n >= cp) return;
         float was[8];
-        load_pairs(from + (m * cp + n) * 2, plane, was);
+        load_pairs(from + pairs_at(m * cp + n), was);
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = a.a * was[q] + kUnscale * v[q];
-        if constexpr (LAST == kMore) store_pairs(to + (m * cp + n) * 2, plane, v);
+        if constexpr (LAST == kMore) store_pairs(to + pairs_at(m * cp + n), v);
         else {
             const int left = x.cols - (int)n;
             if (m >= x.rows || left <= 0) return;

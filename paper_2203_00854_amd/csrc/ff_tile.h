@@ -1,8 +1,9 @@
-// Products of tiles on the matrix cores, D[m][n] = sum over k of A(m, k) B(n, k): staged through LDS by loads that write it directly, two stages
-// deep.  Shared by the gated transition and the orthogonalisation.
+// Products of tiles on the matrix cores, D[m][n] = sum over k of A(m, k) B(n, k): staged through LDS by loads that write it directly, several
+// stages deep.  Shared by the gated transition and the orthogonalisation.
 //
 // Three kinds of operands: bfloat16; float32 (32x32x2 float32 instructions); float16 pairs, where a value is hi + lo, each rounded to nearest
 // (24 significant bits together), and a product hi hi + hi lo + lo hi: what it leaves out, lo lo, is 2^-24 of it at most.
+// In memory sixteen values of a pair's hi part are followed by their lo parts, so that a row is as contiguous as one of 4-byte values.
 // An operand lies in memory with k contiguous, [m][k], or "turned", [k][m]; the reads from LDS turn it back.
 //
 // v_mfma_f32_32x32x16: A (32 x 16): lane l holds row l % 32, columns 8 (l / 32) .. + 7; B likewise with its columns; D: lane l holds column
@@ -67,9 +68,9 @@ template <typename T> __device__ __forceinline__ void store_some(T* p, int n, co
         if (q < n) ((__attribute__((address_space(1))) T*)p)[q] = from_f32<T>(v[q]);
 }
 
-// kStep values of k make one round of matrix instructions, 32 bytes of a row of either operand.
+// kStep values of k make one round of matrix instructions.
 struct Bf16 {
-    static constexpr int kSize = 2, kPlanes = 1, kStep = 16;
+    static constexpr int kSize = 2, kPlanes = 1, kStep = 16;     // bytes of a value in memory
     struct Frag { uint4 u[1]; };
     static __device__ __forceinline__ f32x16 mma(const Frag& b, const Frag& a, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b.u[0]), __builtin_bit_cast(bf16x8, a.u[0]), c, 0, 0, 0);
@@ -86,7 +87,7 @@ struct F32 {
     }
 };
 struct Pair {
-    static constexpr int kSize = 2, kPlanes = 2, kStep = 16;
+    static constexpr int kSize = 4, kPlanes = 2, kStep = 16;
     struct Frag { uint4 u[2]; };
     static __device__ __forceinline__ f32x16 mma(const Frag& b, const Frag& a, f32x16 c) {
         const f16x8 bh = __builtin_bit_cast(f16x8, b.u[0]), bl = __builtin_bit_cast(f16x8, b.u[1]);
@@ -102,67 +103,78 @@ struct Pair {
 // 16-byte aligned.  What lies past an end is read from the last row or the last sixteen bytes: a caller stores no m or n that is not there.
 struct Operand {
     const void* p;
-    int64_t plane;        // bytes from the hi plane to the lo plane
     int64_t pitch;        // bytes
     int64_t rows;
     int32_t bytes;
 };
 
-template <class Op_, int BM_, int BN_, int BK_, int WM_, int WN_, int NA_, int NB_, bool TA_, unsigned TB_>
+template <class Op_, int BM_, int BN_, int BK_, int STAGES_, int WM_, int WN_, int NA_, int NB_, bool TA_, unsigned TB_>
 struct Core {
     typedef Op_ Op;
     typedef typename Op::Frag Frag;
-    static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, NA = NA_, NB = NB_;
+    static constexpr int BM = BM_, BN = BN_, BK = BK_, STAGES = STAGES_, WM = WM_, WN = WN_, NA = NA_, NB = NB_;
     static constexpr bool TA = TA_;
     static constexpr unsigned TB = TB_;                            // bit b: operand b of the B side is turned
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
-    static constexpr int kPlaneA = BM * BK * Op::kSize, kPlaneB = BN * BK * Op::kSize;
-    static constexpr int kStage = Op::kPlanes * (NA * kPlaneA + NB * kPlaneB);
+    static constexpr int kBytesA = BM * BK * Op::kSize, kBytesB = BN * BK * Op::kSize, kStage = NA * kBytesA + NB * kBytesB;
+    static constexpr int kLoads = kStage / 16 / kThreads;          // of a wavefront, for one stage
+    static_assert(kBytesA % (16 * kThreads) == 0 && kBytesB % (16 * kThreads) == 0, "the wavefronts count the same loads");
     static_assert(MT >= 1 && NT >= 1 && BK % Op::kStep == 0, "tile");
 
     // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that the lanes that read in one cycle
     // (eight at sixteen bytes, sixteen at eight) meet all banks
     template <bool T, int W> static __device__ __forceinline__ int swizzle(int row) {
-        if constexpr (T) return Op::kSize == 4 ? 0 : W >= 8 ? 2 * (row & 3) : 2 * ((row >> 1) & 1);
+        if constexpr (T) return Op::kStep == 8 ? 0 : W >= 8 ? 2 * (row & 3) : 2 * ((row >> 1) & 1);
         return W >= 8 ? row & 7 : W == 4 ? (row >> 1) & 3 : 0;
     }
 
-    template <bool T, int R>
-    static __device__ __forceinline__ void load(const Operand& o, int plane, int64_t r0, int64_t k0, unsigned lds) {
-        constexpr int W = (T ? R : BK) * Op::kSize / 16, LR = T ? BK : R, kUnits = LR * W;
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        const int64_t first = T ? k0 : r0;
-        const char* base = (const char*)o.p + plane * o.plane + first * o.pitch;
-        const int left = (int)(o.rows - first < LR ? o.rows - first : LR) - 1;
-        const int at = (int)(T ? r0 : k0) * Op::kSize, last = o.bytes - 16;
+    // The loads of one operand's part of a stage.  A lane's address is min(x, limit) + y from a uniform base that moves with k: x, which alone can pass an end, and
+    // y are the same for all stages.
+    template <bool T, int R> struct Loader {
+        static constexpr int W = (T ? R : BK) * Op::kSize / 16, LR = T ? BK : R, N = LR * W / kThreads;
+        uint32_t x[N], y[N];
+        __device__ __forceinline__ Loader(const Operand& o, int64_t r0) {
 #pragma unroll
-        for (int j = 0; j < (kUnits + kThreads - 1) / kThreads; ++j) {
-            const int u0 = j * kThreads + wave * 64;
-            if (kUnits % kThreads != 0 && u0 >= kUnits) break;
-            const int u = u0 + lane, row = u / W, chunk = (u % W) ^ swizzle<T, W>(row);
-            const int r = row < left ? row : left, c = at + chunk * 16;
-            load16_to_lds(base, (uint32_t)(r * (int)o.pitch + (c < last ? c : last)), lds + u0 * 16);
+            for (int j = 0; j < N; ++j) {
+                const int u = j * kThreads + (int)threadIdx.x, row = u / W, chunk = ((u % W) ^ swizzle<T, W>(row)) * 16;
+                if constexpr (T) {
+                    const int c = (int)r0 * Op::kSize + chunk, last = o.bytes - 16;
+                    x[j] = (uint32_t)row * (uint32_t)o.pitch;
+                    y[j] = (uint32_t)(c < last ? c : last);
+                } else {
+                    const int left = (int)(o.rows - r0 < R ? o.rows - r0 : R) - 1;
+                    x[j] = (uint32_t)chunk;
+                    y[j] = (uint32_t)(row < left ? row : left) * (uint32_t)o.pitch;
+                }
+            }
         }
-    }
+        __device__ __forceinline__ void issue(const Operand& o, int64_t r0, int64_t k0, unsigned lds) const {
+            const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+            const char* base = (const char*)o.p + (T ? k0 * o.pitch : r0 * o.pitch + k0 * Op::kSize);
+            const uint32_t limit = T ? (uint32_t)((o.rows - k0 < LR ? o.rows - k0 : LR) - 1) * (uint32_t)o.pitch : (uint32_t)(o.bytes - 16 - (int)k0 * Op::kSize);
+#pragma unroll
+            for (int j = 0; j < N; ++j) load16_to_lds(base, (x[j] < limit ? x[j] : limit) + y[j], lds + (j * kThreads + wave * 64) * 16);
+        }
+    };
 
-    // the lane's piece of 32 rows (from `row0`) in round s
+    // the lane's piece of plane p of 32 rows (from `row0`) in round s
     template <bool T, int R>
-    static __device__ __forceinline__ uint4 piece(const unsigned char* image, int row0, int s, int lane) {
+    static __device__ __forceinline__ uint4 piece(const unsigned char* image, int p, int row0, int s, int lane) {
         constexpr int W = (T ? R : BK) * Op::kSize / 16;
         const int hf = lane >> 5;
         if constexpr (!T) {
-            const int row = row0 + (lane & 31);
-            return *reinterpret_cast<const uint4*>(image + row * (W * 16) + (((2 * s + hf) ^ swizzle<false, W>(row)) << 4));
-        } else if constexpr (Op::kSize == 2) {
+            const int row = row0 + (lane & 31), chunk = 2 * (Op::kPlanes * s + p) + hf;
+            return *reinterpret_cast<const uint4*>(image + row * (W * 16) + ((chunk ^ swizzle<false, W>(row)) << 4));
+        } else if constexpr (Op::kStep == 16) {
             // of sixteen lanes, lane i asks for four columns 4 (i % 4) .. of row i / 4, and lane l receives column l of the four rows
-            const int i = lane & 15, byte = (row0 + (lane & 16) + 4 * (i & 3)) * 2;
+            const int i = lane & 15, chunk = (row0 + (lane & 16)) / 8 * Op::kPlanes + 2 * p + (i >> 1 & 1);
             uint2 h[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int k = 16 * s + 8 * hf + 4 * t + (i >> 2);
-                const unsigned char* p = image + k * (W * 16) + (((byte >> 4) ^ swizzle<true, W>(k)) << 4) + (byte & 8);
-                h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)p));
+                const unsigned char* q = image + k * (W * 16) + ((chunk ^ swizzle<true, W>(k)) << 4) + (i & 1) * 8;
+                h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)q));
             }
             return make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
         } else {
@@ -176,46 +188,49 @@ struct Core {
     static __device__ __forceinline__ Frag frag(const unsigned char* image, int row0, int s, int lane) {
         Frag f;
 #pragma unroll
-        for (int p = 0; p < Op::kPlanes; ++p) f.u[p] = piece<T, R>(image + p * (R * BK * Op::kSize), row0, s, lane);
+        for (int p = 0; p < Op::kPlanes; ++p) f.u[p] = piece<T, R>(image, p, row0, s, lane);
         return f;
     }
 
-    template <int B = 0> static __device__ __forceinline__ void load_b(const Operand* b, int64_t n0, int64_t k0, unsigned lds) {
+    // the loads of all operands (those of one side that lie alike have pitches and sizes alike too, and differ in their bases only)
+    struct Loads {
+        Loader<TA, BM> a;
+        Loader<(TB & 1) != 0, BN> b;
+        Loader<(TB >> (NB - 1) & 1) != 0, BN> last;
+        __device__ __forceinline__ Loads(const Operand* oa, const Operand* ob, int64_t m0, int64_t n0) : a(oa[0], m0), b(ob[0], n0), last(ob[NB - 1], n0) {}
+        __device__ __forceinline__ void issue(const Operand* oa, const Operand* ob, int64_t m0, int64_t n0, int64_t k0, unsigned lds) const {
+#pragma unroll
+            for (int i = 0; i < NA; ++i) a.issue(oa[i], m0, k0, lds + i * kBytesA);
+#pragma unroll
+            for (int i = 0; i < NB - 1; ++i) b.issue(ob[i], n0, k0, lds + NA * kBytesA + i * kBytesB);
+            last.issue(ob[NB - 1], n0, k0, lds + NA * kBytesA + (NB - 1) * kBytesB);
+        }
+    };
+
+    struct Frags {
+        Frag a[NA][MT], b[NB][NT];
+    };
+    template <int B = 0> static __device__ __forceinline__ void read_b(Frags& f, const unsigned char* image, int wn, int s, int lane) {
         if constexpr (B < NB) {
 #pragma unroll
-            for (int p = 0; p < Op::kPlanes; ++p) load<(TB >> B & 1) != 0, BN>(b[B], p, n0, k0, lds + p * kPlaneB);
-            load_b<B + 1>(b, n0, k0, lds + Op::kPlanes * kPlaneB);
+            for (int n = 0; n < NT; ++n) f.b[B][n] = frag<(TB >> B & 1) != 0, BN>(image, (wn * NT + n) * 32, s, lane);
+            read_b<B + 1>(f, image + kBytesB, wn, s, lane);
         }
     }
-    static __device__ __forceinline__ void load_stage(const Operand* a, const Operand* b, int64_t m0, int64_t n0, int64_t k0, unsigned lds) {
+    static __device__ __forceinline__ void read(Frags& f, const unsigned char* image, int wm, int wn, int s, int lane) {
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
-            for (int p = 0; p < Op::kPlanes; ++p) load<TA, BM>(a[i], p, m0, k0, lds + (i * Op::kPlanes + p) * kPlaneA);
-        load_b(b, n0, k0, lds + NA * Op::kPlanes * kPlaneA);
+            for (int m = 0; m < MT; ++m) f.a[i][m] = frag<TA, BM>(image + i * kBytesA, (wm * MT + m) * 32, s, lane);
+        read_b(f, image + NA * kBytesA, wn, s, lane);
     }
-
-    template <int B = 0>
-    static __device__ __forceinline__ void products(f32x16 (&acc)[NB][MT][NT], const Frag (&fa)[NA][MT], const unsigned char* image, int wn, int s, int lane) {
-        if constexpr (B < NB) {
-            Frag fb[NT];
+    static __device__ __forceinline__ void multiply(f32x16 (&acc)[NB][MT][NT], const Frags& f) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) fb[n] = frag<(TB >> B & 1) != 0, BN>(image, (wn * NT + n) * 32, s, lane);
-            constexpr int A = NA == 1 || B + 1 < NB ? 0 : 1;         // a second A side belongs to the last product
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[B][m][n] = Op::mma(fb[n], fa[A][m], acc[B][m][n]);
-            products<B + 1>(acc, fa, image + Op::kPlanes * kPlaneB, wn, s, lane);
-        }
-    }
-    static __device__ __forceinline__ void round(f32x16 (&acc)[NB][MT][NT], const unsigned char* image, int wm, int wn, int s, int lane) {
-        Frag fa[NA][MT];
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) fa[i][m] = frag<TA, BM>(image + i * Op::kPlanes * kPlaneA, (wm * MT + m) * 32, s, lane);
-        products(acc, fa, image + NA * Op::kPlanes * kPlaneA, wn, s, lane);
+                for (int n = 0; n < NT; ++n) acc[b][m][n] = Op::mma(f.b[b][n], f.a[NA == 1 || b + 1 < NB ? 0 : 1][m], acc[b][m][n]);      // (a second A side belongs to the last product)
     }
 
     static __device__ __forceinline__ void clear(f32x16 (&acc)[NB][MT][NT]) {
@@ -236,29 +251,67 @@ struct Core {
         const int wm = wave / WN, wn = wave % WN;
         const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
         if (from >= to) return;
-        load_stage(a, b, m0, n0, from, lds);
-        int buf = 0;
-        for (int64_t k0 = from; k0 < to; k0 += BK, buf ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();                                           // the stage is there, and nobody reads the other one any more
-            if (k0 + BK < to) load_stage(a, b, m0, n0, k0 + BK, lds + (buf ^ 1) * kStage);
-            const unsigned char* image = smem + buf * kStage;
-            if (to - k0 >= BK) {
+        constexpr int R = BK / Op::kStep;
+        const int stages = (int)((to - from + BK - 1) / BK), whole = (int)((to - from) / BK);
+        const Loads loads(a, b, m0, n0);
 #pragma unroll
-                for (int s = 0; s < BK / Op::kStep; ++s) round(acc, image, wm, wn, s, lane);
-            } else {
-                const int steps = (int)(to - k0) / Op::kStep;
-                for (int s = 0; s < steps; ++s) round(acc, image, wm, wn, s, lane);
+        for (int i = 0; i < STAGES - 1; ++i)
+            if (i < stages) loads.issue(a, b, m0, n0, from + i * BK, lds + i * kStage);
+        // Operands of the next round are read while a round's products run, so a stage has to be there one turn early.
+        Frags f[2];
+        if (STAGES > 3 && stages > 2) arrive<2>();
+        else if (stages > 1) arrive<1>();
+        else arrive<0>();
+        read(f[0], smem, wm, wn, 0, lane);
+        int buf = 0, t = 0;
+        const auto turn = [&](Frags& now, Frags& then) {
+            // the next stage is there, and nobody reads the one before any more, in whose place the loads of the one STAGES - 1 ahead go
+            if (STAGES > 3 && t + 2 < stages) arrive<1>();
+            else arrive<0>();
+            if (t + STAGES - 1 < stages) loads.issue(a, b, m0, n0, from + (int64_t)(t + STAGES - 1) * BK, lds + (buf == 0 ? STAGES - 1 : buf - 1) * kStage);
+            const int next = buf + 1 == STAGES ? 0 : buf + 1;
+            const unsigned char *image = smem + buf * kStage, *image_next = smem + next * kStage;
+#pragma unroll
+            for (int s = 0; s < R; ++s) {
+                Frags &mine = s & 1 ? then : now, &other = s & 1 ? now : then;
+                if (s + 1 < R) read(other, image, wm, wn, s + 1, lane);
+                else read(other, image_next, wm, wn, 0, lane);             // (of the last stage's successor: what lies there, for no product)
+                __builtin_amdgcn_sched_barrier(0);                         // the reads before the products, or they would be waited for right behind them
+                multiply(acc, mine);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            buf = next;
+            ++t;
+        };
+        if constexpr (R & 1) {
+            while (t + 1 < whole) {
+                turn(f[0], f[1]);
+                turn(f[1], f[0]);
+            }
+            if (t < whole) {
+                turn(f[0], f[1]);
+                f[0] = f[1];
+            }
+        } else
+            while (t < whole) turn(f[0], f[1]);
+        const int rest = (int)((to - from) - (int64_t)whole * BK) / Op::kStep;
+        for (int s = 0; s < rest; ++s) {
+            multiply(acc, f[0]);
+            if (s + 1 < rest) read(f[0], smem + buf * kStage, wm, wn, s + 1, lane);
         }
         __syncthreads();
+    }
+    // waits until all but the loads of the youngest N stages have arrived, for every wavefront, and for its own reads
+    template <int N> static __device__ __forceinline__ void arrive() {
+        static_assert(STAGES >= 3 && STAGES <= 4 && 2 * kLoads < 64, "the counter");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N * kLoads) : "memory");
     }
 
     // Results leave through LDS, where a lane finds eight neighbours of a row: straight from the accumulators a store would reach sixteen bytes of each of 32 rows,
     // and the stores of a tile would take longer than its products.
     static constexpr int kPitch = BN + 4, kPitchTurned = BM + 4;        // floats; sixteen bytes more than a row, so that the rows of one cycle lie in banks of their own
     static constexpr int kOut = 4 * BM * kPitch > 4 * BN * kPitchTurned ? 4 * BM * kPitch : 4 * BN * kPitchTurned;
-    static constexpr int kLds = 2 * kStage > kOut ? 2 * kStage : kOut;
+    static constexpr int kLds = STAGES * kStage > kOut ? STAGES * kStage : kOut;
 
     // body(m, n, v): eight results v in row m, columns n .. n + 7.  smem: kLds bytes that every thread is done with, before and after
     template <typename F> static __device__ __forceinline__ void rows(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, F body) {
@@ -272,7 +325,7 @@ struct Core {
                 for (int g = 0; g < 4; ++g)
                     *(float4*)(out + i * 32 * kPitch + j * 32 + 8 * g) = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
         __syncthreads();
-        read<BM, BN, kPitch>(smem, m0, n0, body);
+        leave<BM, BN, kPitch>(smem, m0, n0, body);
         __syncthreads();
     }
     // the same turned: row n, columns m .. m + 7
@@ -286,10 +339,10 @@ struct Core {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) out[(j * 32 + 8 * (v / 4) + v % 4) * kPitchTurned + i * 32] = acc[i][j][v];
         __syncthreads();
-        read<BN, BM, kPitchTurned>(smem, n0, m0, body);
+        leave<BN, BM, kPitchTurned>(smem, n0, m0, body);
         __syncthreads();
     }
-    template <int R, int C, int PITCH, typename F> static __device__ __forceinline__ void read(const unsigned char* smem, int64_t r0, int64_t c0, F body) {
+    template <int R, int C, int PITCH, typename F> static __device__ __forceinline__ void leave(const unsigned char* smem, int64_t r0, int64_t c0, F body) {
         for (int u = threadIdx.x; u < R * (C / 8); u += kThreads) {
             const int r = u / (C / 8), c = u % (C / 8) * 8;
             const float4 a = *(const float4*)((const float*)smem + r * PITCH + c), b = *(const float4*)((const float*)smem + r * PITCH + c + 4);

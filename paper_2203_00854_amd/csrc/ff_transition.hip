@@ -361,7 +361,7 @@ template <typename T> ff_status pack(const PackJob* jobs, int n, hipStream_t str
 }
 
 Operand operand(const void* p, int64_t pitch, int64_t rows, int64_t cols, int esz) {
-    return {p, 0, pitch * esz, rows, (int32_t)(cols * esz)};
+    return {p, pitch * esz, rows, (int32_t)(cols * esz)};
 }
 
 // the weights as the products read them: themselves, or padded copies in ws
@@ -390,7 +390,7 @@ template <typename T> Weights weights_of(const ff_transition_desc& d, const Size
     return w;
 }
 
-constexpr int bk_of(int esz) { return esz == 2 ? 64 : 16; }
+constexpr int bk_of(int esz) { return 64 / esz; }              // of a row, 64 bytes a stage
 
 // channels / 32 that the kernels with rows in registers are built for: the next one that holds c (0: none)
 int rows_tiles(const ff_transition_desc& d) {
@@ -435,8 +435,8 @@ ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const
 template <typename T> ff_status forward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                         const float* mask, void* y, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
-    typedef Core<Op, 128, 64, bk_of(sizeof(T)), 2, 2, 1, 2, false, 0u> CH;
-    typedef Core<Op, 128, 128, bk_of(sizeof(T)), 2, 2, 1, 1, false, 0u> CO;
+    typedef Core<Op, 128, 64, bk_of(sizeof(T)), 4, 2, 2, 1, 2, false, 0u> CH;
+    typedef Core<Op, 128, 128, bk_of(sizeof(T)), 4, 2, 2, 1, 1, false, 0u> CO;
     const Sizes s = sizes_of(d);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
@@ -481,9 +481,9 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
                                          const float* mask, void* dx, void* const (&dw)[3], int grad_dtype, bool accumulate, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
     constexpr int BK = bk_of(sizeof(T));
-    typedef Core<Op, 128, 64, sizeof(T) == 2 ? 32 : 16, 2, 2, 2, 3, false, 4u> CG;
-    typedef Core<Op, 128, 128, BK, 2, 2, 1, 1, false, 1u> CX;
-    typedef Core<Op, 128, 128, BK, 2, 2, 1, 1, true, 1u> CW;
+    typedef Core<Op, 128, 64, BK, 3, 2, 2, 2, 3, false, 4u> CG;
+    typedef Core<Op, 128, 128, BK, 4, 2, 2, 1, 1, false, 1u> CX;
+    typedef Core<Op, 128, 128, BK, 4, 2, 2, 1, 1, true, 1u> CW;
     const Sizes s = sizes_of(d);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
