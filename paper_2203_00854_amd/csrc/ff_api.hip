@@ -25,7 +25,7 @@ static const char* kKindNames[KK_COUNT] = {"k_prep", "pair bias pass", "k_gemm<P
                                            "k_bwd_stats", "k_bwd_dq", "k_bwd_dkv", "k_bwd_dbias", "probe: vector loop",
                                            "k_proj_attn", "k_bwd_rows", "k_bwd_prepare", "k_bwd_dbias_reduce", "k_ln_forward",
                                            "k_ln_backward", "k_ln_join", "k_grad_norm", "k_adamw", "k_moments", "k_tr_pack", "k_tr_hidden", "k_tr_out",
-                                           "k_tr_grad", "k_tr_weights", "k_tr_join", "k_tr_rows", "k_muon_momentum", "k_ns_start", "k_ns_gram", "k_ns_poly", "k_ns_apply"};
+                                           "k_tr_grad", "k_tr_weights", "k_tr_join", "k_tr_rows", "k_muon_momentum", "k_ns_start", "k_ns_gram", "k_ns_poly", "k_ns_apply", "k_ns_small"};
 
 static hipEvent_t prof_event() {
     if (!g_prof_pool.empty()) {

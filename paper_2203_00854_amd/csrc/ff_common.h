@@ -104,7 +104,7 @@ enum KernelKind { KK_PREP = 0, KK_BIAS, KK_PROJ, KK_ATTN, KK_OUT, KK_LAYERNORM, 
                   KK_BWD_STATS, KK_BWD_DQ, KK_BWD_DKV, KK_BWD_DBIAS, KK_PROBE_VALU, KK_PROJ_ATTN, KK_BWD_ROWS,
                   KK_BWD_PREPARE, KK_BWD_DBIAS_REDUCE, KK_LN_FORWARD, KK_LN_BACKWARD, KK_LN_JOIN, KK_GRAD_NORM, KK_ADAMW,
                   KK_MOMENTS, KK_TR_PACK, KK_TR_HIDDEN, KK_TR_OUT, KK_TR_GRAD, KK_TR_WEIGHTS, KK_TR_JOIN, KK_TR_ROWS, KK_MUON_MOMENTUM, KK_NS_START,
-                  KK_NS_GRAM, KK_NS_POLY, KK_NS_APPLY, KK_COUNT };
+                  KK_NS_GRAM, KK_NS_POLY, KK_NS_APPLY, KK_NS_SMALL, KK_COUNT };
 void prof_begin(int kind, hipStream_t st);
 void prof_end(int kind, hipStream_t st);
 // brackets the launches issued in its scope with HIP events when the timer is on

@@ -29,6 +29,7 @@ namespace {
 constexpr float kScale = 256.f, kUnscale = 1.f / 256.f;
 constexpr int kPad = 16;
 constexpr int kTile = 128;
+constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 16384;                    // values that a block of the element-wise kernels holds
 constexpr int64_t kBatch = 256 << 20;            // workspace of the matrices that are worked on together, unless one alone needs more
 
@@ -54,7 +55,7 @@ struct Matrix {
     __host__ __device__ int64_t bytes() const { return 2 * bytes_x() + 2 * bytes_a(); }
 };
 struct Place {
-    int32_t matrix, at;
+    int32_t matrix, at;                          // matrix < 0: none
 };
 
 // Where the kernels find matrices and places: in a plan, or, for matrices of one shape that lie one after another, by counting.
@@ -63,7 +64,7 @@ struct Table {
     const Place* places;
     Matrix one;
     int64_t in_step, out_step, ws_step;
-    int32_t each;                                // places of a matrix
+    int32_t count, each;                         // matrices; places of a matrix
 };
 __device__ __forceinline__ Matrix matrix_of(const Table& t, int32_t i) {
     if (t.matrices) return t.matrices[i];
@@ -76,8 +77,12 @@ __device__ __forceinline__ Matrix matrix_of(const Table& t, int32_t i) {
 }
 __device__ __forceinline__ Place place_at(const Table& t, uint32_t block) {
     if (t.matrices) return t.places[block];
-    return {(int32_t)(block / (uint32_t)t.each), (int32_t)(block % (uint32_t)t.each)};
+    const uint32_t each = (uint32_t)t.each;
+    if (t.count < kXcds) return {(int32_t)(block / each), (int32_t)(block % each)};
+    const int32_t m = (int32_t)(block / kXcds / each * kXcds + block % kXcds);
+    return {m < t.count ? m : -1, (int32_t)(block / kXcds % each)};
 }
+uint32_t places_of(int32_t count, int32_t each) { return (uint32_t)(count < kXcds ? count : (count + kXcds - 1) / kXcds * kXcds) * (uint32_t)each; }
 
 // ---- pairs ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t half_bits(_Float16 h) { return __builtin_bit_cast(uint16_t, h); }
@@ -141,6 +146,7 @@ __device__ __forceinline__ float update_of(float m, float g, const StepArgs& a) 
 // m = beta m + (1 - beta) k g, and the sum of squares of the update, in float64: bound by HBM.  MUON false: of g itself.
 template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_momentum(Table t, StepArgs a, const float* norm, double* partial) {
     const Place at = place_at(t, blockIdx.x);
+    if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
     bool skip = false;
     const float k = MUON ? clip_of(norm, a.max_norm, skip) : 1.f;
@@ -176,6 +182,7 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_m
 // X = update / (norm + eps) as pairs, its padding zeros
 template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_start(Table t, StepArgs a, const float* norm, const double* partial, char* ws) {
     const Place at = place_at(t, blockIdx.x);
+    if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
     bool skip = false;
     const float k = MUON ? clip_of(norm, a.max_norm, skip) : 1.f;
@@ -208,11 +215,15 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
 }
 
 // ---- the products --------------------------------------------------------------------------
-typedef Core<Pair, kTile, kTile, 16, 4, 2, 2, 1, 1, false, 0u> Straight;      // rows by rows
-typedef Core<Pair, kTile, kTile, 16, 4, 2, 2, 1, 1, true, 1u> Turned;         // columns by columns
-typedef Core<Pair, kTile, kTile, 16, 4, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
-
-constexpr size_t kTileLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
+template <int STAGES> struct Cores {
+    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, false, 0u> Straight;      // rows by rows
+    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, true, 1u> Turned;         // columns by columns
+    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
+    static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
+};
+// Four stages leave room for two blocks on a compute unit, eight for one: 48 KiB under way twice, or 112 KiB once where a launch has fewer blocks than
+// there are units (a stage takes 0.18 us of matrix instructions and 0.8 us to arrive).
+constexpr int kShallow = 4, kDeep = 8;
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
     return {ws + x.x(which), x.cp() * 4, x.rp(), (int32_t)(x.cp() * 4)};
@@ -239,27 +250,75 @@ __device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], cha
     if (i != j) C::columns(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
 }
 
-__global__ __launch_bounds__(256, 2) void k_ns_gram(Table t, char* ws, int which) {
+// A.  SPLIT: sums over a part of k each, for k_ns_join
+template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, 2) void k_ns_gram(Table t, char* ws, int which, float* parts) {
+    typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
+    if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
     const Operand o = operand_x(x, ws, which);
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
-    if (x.tall()) Turned::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, x.rp(), smem);
-    else Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, x.cp(), smem);
-    store_symmetric<Straight>(acc[0], ws + x.a(0), x.np(), i, j, smem, [&](int64_t, int64_t, float (&v)[8]) {
+    const int64_t all = x.tall() ? x.rp() : x.cp(), each = SPLIT ? (all / kPad + gridDim.y - 1) / gridDim.y * kPad : all, from = SPLIT ? blockIdx.y * each : 0;
+    const int64_t to = from + each < all ? from + each : all;
+    if (x.tall()) Cores<STAGES>::Turned::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, from, to, smem);
+    else Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, from, to, smem);
+    if constexpr (SPLIT) {
+        float* out = parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kTile * kTile;
+        Straight::rows(acc[0], 0, 0, smem, [&](int64_t m, int64_t n, float (&v)[8]) { tile::store8(out + m * kTile + n, v); });
+    } else
+        store_symmetric<Straight>(acc[0], ws + x.a(0), x.np(), i, j, smem, [&](int64_t, int64_t, float (&v)[8]) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
-    });
+            for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
+        });
+}
+
+// A of its parts, added up in their order
+__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float* parts, int splits) {
+    constexpr int kPitch = kTile + 1;
+    __shared__ float tile_[kTile * kPitch];
+    const Place at = place_at(t, blockIdx.x);
+    if (at.matrix < 0) return;
+    const Matrix x = matrix_of(t, at.matrix);
+    int i, j;
+    triangle(at.at, i, j);
+    const int64_t np = x.np();
+    char* out = ws + x.a(0);
+    for (int u = threadIdx.x; u < kTile * kTile / 8; u += 256) {
+        const int r = u / (kTile / 8), c = u % (kTile / 8) * 8;
+        float v[8], more[8];
+        tile::load8(parts + (int64_t)blockIdx.x * kTile * kTile + u * 8, v);
+        for (int s = 1; s < splits; ++s) {
+            tile::load8(parts + ((int64_t)s * gridDim.x + blockIdx.x) * kTile * kTile + u * 8, more);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] += more[q];
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) tile_[r * kPitch + c + q] = v[q] *= kUnscale;
+        const int64_t m = (int64_t)i * kTile + r, n = (int64_t)j * kTile + c;
+        if (m < np && n < np) store_pairs(out + pairs_at(m * np + n), v);
+    }
+    if (i == j) return;
+    __syncthreads();
+    for (int u = threadIdx.x; u < kTile * kTile / 8; u += 256) {
+        const int r = u / (kTile / 8), c = u % (kTile / 8) * 8;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = tile_[(c + q) * kPitch + r];
+        const int64_t m = (int64_t)j * kTile + r, n = (int64_t)i * kTile + c;
+        if (m < np && n < np) store_pairs(out + pairs_at(m * np + n), v);
+    }
 }
 
 // B = b A + c A^2
-__global__ __launch_bounds__(256, 2) void k_ns_poly(Table t, char* ws, float b, float c) {
+template <int STAGES> __global__ __launch_bounds__(256, 2) void k_ns_poly(Table t, char* ws, float b, float c) {
+    typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
+    if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
@@ -278,10 +337,31 @@ __global__ __launch_bounds__(256, 2) void k_ns_poly(Table t, char* ws, float b, 
 }
 
 enum Last { kMore = 0, kOut = 1, kWeights = 2 };
+__device__ __forceinline__ float size_of(const Matrix& x, const StepArgs& a) {
+    const int32_t longer = x.rows > x.cols ? x.rows : x.cols;
+    return a.lr * (a.rms ? 0.2f * sqrtf((float)longer) : sqrtf((float)longer / (float)x.cols));
+}
+// `left` values (of eight) of the result at place `at` of the matrix
+template <int LAST, typename P> __device__ __forceinline__ void finish(const Matrix& x, const StepArgs& a, float size, int64_t at, int left, const float (&v)[8]) {
+    P* p = (P*)x.p + at;
+    if constexpr (LAST == kOut) tile::store_some(p, left, v);
+    else {
+        const float decay = a.lr * x.decay;
+        float w[8];
+        if (x.master) tile::load_some((const float*)x.master + at, left, w);
+        else tile::load_some((const P*)p, left, w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] -= decay * w[q] + size * v[q];
+        if (x.master) tile::store_some(x.master + at, left, w);
+        tile::store_some(p, left, w);
+    }
+}
 // X = a X + B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights
-template <int LAST, typename P> __global__ __launch_bounds__(256, 2) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
+template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, 2) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
+    typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
+    if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
     if (LAST == kWeights) {
         bool skip = false;
@@ -294,11 +374,10 @@ template <int LAST, typename P> __global__ __launch_bounds__(256, 2) void k_ns_a
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     if (x.tall()) Straight::run(acc, &ox, &ob, (int64_t)i * kTile, (int64_t)j * kTile, 0, cp, smem);
-    else Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
+    else Cores<STAGES>::Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
     const char* from = ws + x.x(which);
     char* to = ws + x.x(which ^ 1);
-    const int32_t longer = x.rows > x.cols ? x.rows : x.cols;
-    const float size = a.lr * (a.rms ? 0.2f * sqrtf((float)longer) : sqrtf((float)longer / (float)x.cols)), decay = a.lr * x.decay;
+    const float size = size_of(x, a);
     Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
         if (m >= rp || n >= cp) return;
         float was[8];
@@ -311,26 +390,198 @@ template <int LAST, typename P> __global__ __launch_bounds__(256, 2) void k_ns_a
             if (m >= x.rows || left <= 0) return;
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
-            P* p = (P*)x.p + m * x.cols + n;
-            if constexpr (LAST == kOut) tile::store_some(p, left, v);
-            else {
-                float w[8];
-                float* master = x.master + m * x.cols + n;
-                if (x.master) tile::load_some((const float*)master, left, w);
-                else tile::load_some((const P*)p, left, w);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) w[q] -= decay * w[q] + size * v[q];
-                if (x.master) tile::store_some(master, left, w);
-                tile::store_some(p, left, w);
-            }
+            finish<LAST, P>(x, a, size, m * x.cols + n, left, v);
         }
     });
+}
+
+// ---- small matrices: everything in one block ---------------------------------------------------
+// A matrix of at most SIZE x SIZE stays in LDS from its momentum to its weights: X and A (then B in A's place) as pairs in rows of SIZE values, a product's
+// results in registers between two barriers.  A wavefront has one 32 x 32 tile of the result (SIZE 64), or two beside each other (SIZE 128).
+// 128 x 64: one launch of 29 us where the products of the other path take 17.
+template <int SIZE> struct Small {
+    static constexpr int kWaves = SIZE == 128 ? 8 : 4, kThreads = 64 * kWaves, kUnits = SIZE == 128 ? 2 : 1;
+    static constexpr int W = SIZE / 4, kImage = SIZE * SIZE * 4, kLds = 2 * kImage;
+    // sixteen bytes of row `row`: eight values from column c, a multiple of eight, of the hi part (p = 0) or the lo part.  Rows that one cycle reads together, straight or turned, lie in banks of their own.
+    static __device__ __forceinline__ int at(int row, int c, int p) { return row * (W * 16) + (((c >> 4) * 4 + p * 2 + (c >> 3 & 1)) ^ ((row & 3) << 1 | (row >> 2 & 1))) * 16; }
+
+    // 32 rows (straight) or columns (turned) from `first`, k = 16 s ..
+    template <bool T> static __device__ __forceinline__ Pair::Frag frag(const unsigned char* image, int first, int s, int lane) {
+        Pair::Frag f;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            if constexpr (!T) f.u[p] = *(const uint4*)(image + at(first + (lane & 31), 16 * s + 8 * (lane >> 5), p));
+            else {
+                const int i = lane & 15, col = first + (lane & 16) + 4 * (i & 3);
+                uint2 h[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)(image + at(16 * s + 8 * (lane >> 5) + 4 * t + (i >> 2), col & ~7, p) + (col & 4) * 2)));
+                f.u[p] = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+            }
+        }
+        return f;
+    }
+    // the wavefront's tiles of the product of two images over k (a multiple of sixteen)
+    template <bool TA, bool TB>
+    static __device__ __forceinline__ void product(f32x16 (&acc)[kUnits], const unsigned char* a, const unsigned char* b, int m0, int n0, int tiles, int k, int lane) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[u][v] = 0.f;
+        if (tiles <= 0) return;
+        for (int s = 0; s < k / 16; ++s) {
+            const Pair::Frag fa = frag<TA>(a, m0, s, lane);
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u)
+                if (u < tiles) acc[u] = Pair::mma(frag<TB>(b, n0 + 32 * u, s, lane), fa, acc[u]);
+        }
+    }
+    // value(old, sum) of the wavefront's tiles, old being what image `from` holds there
+    template <typename F> static __device__ __forceinline__ void combine(f32x16 (&acc)[kUnits], const unsigned char* from, int m0, int n0, int tiles, int lane, F value) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (u < tiles)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int n = n0 + 32 * u + 8 * g, half = 8 * (lane >> 5);
+                    const uint2 h = *(const uint2*)(from + at(m0 + (lane & 31), n, 0) + half), l = *(const uint2*)(from + at(m0 + (lane & 31), n, 1) + half);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        acc[u][4 * g + q] = value(join((q < 2 ? h.x : h.y) >> (q & 1) * 16 & 0xffffu, (q < 2 ? l.x : l.y) >> (q & 1) * 16 & 0xffffu), acc[u][4 * g + q]);
+                }
+    }
+    // rows and columns below the given numbers
+    static __device__ __forceinline__ void store(const f32x16 (&acc)[kUnits], unsigned char* to, int m0, int n0, int tiles, int rows, int cols, int lane) {
+        if (m0 + (lane & 31) >= rows) return;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (u < tiles)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int n = n0 + 32 * u + 8 * g, half = 8 * (lane >> 5);
+                    if (n >= cols) continue;
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) split(acc[u][4 * g + q], hi[q], lo[q]);
+                    *(uint2*)(to + at(m0 + (lane & 31), n, 0) + half) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                    *(uint2*)(to + at(m0 + (lane & 31), n, 1) + half) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                }
+    }
+};
+
+template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds__(Small<SIZE>::kThreads) void k_ns_small(Table t, int first, int steps, StepArgs a, const float* norm) {
+    typedef Small<SIZE> S;
+    constexpr bool MUON = LAST == kWeights;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    unsigned char *const xs = smem, *const as = smem + S::kImage;
+    const Matrix x = matrix_of(t, first + (int)blockIdx.x);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    bool skip = false;
+    const float k = MUON ? clip_of(norm, a.max_norm, skip) : 1.f;
+    if (skip) return;
+    const int rp = (int)x.rp(), cp = (int)x.cp(), np = (int)x.np();
+    // the update, in registers, and the sum of its squares
+    constexpr int kTurns = SIZE * SIZE / 8 / S::kThreads;
+    float g[kTurns][8];
+    double sum = 0.;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int64_t place = (int64_t)(i * S::kThreads + (int)threadIdx.x) * 8;
+        if (place >= (int64_t)rp * cp) continue;
+        const Spot s = spot_of(x, place);
+        tile::load_some((const G*)x.g + s.at, s.n, g[i]);
+        if constexpr (MUON) {
+            float m[8];
+            tile::load_some((const float*)x.m + s.at, s.n, m);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                g[i][q] *= k;
+                m[q] = a.beta * m[q] + a.rest * g[i][q];
+                g[i][q] = update_of(m[q], g[i][q], a);
+            }
+            tile::store_some(x.m + s.at, s.n, m);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            g[i][q] = q < s.n ? g[i][q] : 0.f;
+            sum += (double)g[i][q] * g[i][q];
+        }
+    }
+    double* sums = (double*)smem;
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    for (int n = S::kThreads / 2; n > 0; n >>= 1) {
+        if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
+        __syncthreads();
+    }
+    const double inv = (double)kScale / (sqrt(sums[0]) + a.eps);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int place = (i * S::kThreads + (int)threadIdx.x) * 8;
+        if (place >= rp * cp) continue;
+        const int r = place / cp, c = place % cp;
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) split((float)(g[i][q] * inv), hi[q], lo[q]);
+        *(uint4*)(xs + S::at(r, c, 0)) = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
+        *(uint4*)(xs + S::at(r, c, 1)) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+    }
+    // the wavefront's tiles of A, and of X
+    const auto place = [&](int rows, int cols, int& m0, int& n0, int& tiles) {
+        const int across = (cols + 31) / 32, groups = (across + S::kUnits - 1) / S::kUnits, down = (rows + 31) / 32;
+        m0 = wave / groups * 32;
+        n0 = wave % groups * S::kUnits * 32;
+        tiles = wave < groups * down ? (across - n0 / 32 < S::kUnits ? across - n0 / 32 : S::kUnits) : 0;
+    };
+    int am, an, at, xm, xn, xt;
+    place(np, np, am, an, at);
+    place(rp, cp, xm, xn, xt);
+    f32x16 acc[S::kUnits];
+    for (int step = 0; step < steps; ++step) {
+        __syncthreads();                                       // X is whole
+        if (x.tall()) S::template product<true, true>(acc, xs, xs, am, an, at, rp, lane);
+        else S::template product<false, false>(acc, xs, xs, am, an, at, cp, lane);
+#pragma unroll
+        for (int u = 0; u < S::kUnits; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[u][v] *= kUnscale;
+        S::store(acc, as, am, an, at, np, np, lane);
+        __syncthreads();                                       // A is
+        S::template product<false, false>(acc, as, as, am, an, at, np, lane);
+        S::combine(acc, as, am, an, at, lane, [&](float was, float v) { return a.b * was + (a.c * kUnscale) * v; });
+        __syncthreads();                                       // and read
+        S::store(acc, as, am, an, at, np, np, lane);
+        __syncthreads();                                       // B is whole
+        if (x.tall()) S::template product<false, false>(acc, xs, as, xm, xn, xt, cp, lane);
+        else S::template product<false, true>(acc, as, xs, xm, xn, xt, rp, lane);
+        S::combine(acc, xs, xm, xn, xt, lane, [&](float was, float v) { return a.a * was + kUnscale * v; });
+        __syncthreads();                                       // X is read
+        S::store(acc, xs, xm, xn, xt, rp, cp, lane);
+    }
+    __syncthreads();
+    const float size = size_of(x, a);
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int place = (i * S::kThreads + (int)threadIdx.x) * 8;
+        if (place >= rp * cp) continue;
+        const Spot s = spot_of(x, place);
+        if (s.n == 0) continue;
+        const uint4 h4 = *(const uint4*)(xs + S::at((int)s.r, s.c, 0)), l4 = *(const uint4*)(xs + S::at((int)s.r, s.c, 1));
+        const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = kUnscale * (q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu));
+        finish<LAST, P>(x, a, size, s.at, s.n, v);
+    }
 }
 
 // ---- launches --------------------------------------------------------------------------------
 struct Batch {
     int64_t ws;                                   // bytes of workspace of its matrices
     int32_t piece0, pieces, tri0, tris, app0, apps;        // places of the three kinds, in the plan's lists
+    int32_t splits, pad;                          // of k in the Gram matrices, 1 = none
 };
 int pieces_of(const Matrix& m) { return (int)((m.rp() * m.cp() + kPiece - 1) / kPiece); }
 int tris_of(const Matrix& m) {
@@ -338,11 +589,18 @@ int tris_of(const Matrix& m) {
     return n * (n + 1) / 2;
 }
 int apps_of(const Matrix& m) { return (int)((m.rp() + kTile - 1) / kTile * ((m.cp() + kTile - 1) / kTile)); }
+int small_of(const Matrix& m) { return std::max(m.rows, m.cols) <= 64 ? 64 : std::max(m.rows, m.cols) <= 128 ? 128 : 0; }
+// Few Gram tiles of a long k leave most compute units without a block: k is split then, in parts of 512 and more (the join costs as much as 256 of k).
+int splits_of(int64_t tris, int64_t longest) {
+    const int64_t s = std::min<int64_t>({8, (256 + tris - 1) / tris, longest / 512});
+    return s >= 3 ? (int)s : 1;
+}
+int64_t parts_bytes(int64_t tris, int splits) { return splits > 1 ? tris * splits * kTile * kTile * 4 : 0; }
 
-template <auto KERNEL, typename... A> ff_status go(int kind, uint32_t blocks, size_t lds, hipStream_t stream, const char* what, A... args) {
+template <auto KERNEL, typename... A> ff_status go(int kind, dim3 blocks, int threads, size_t lds, hipStream_t stream, const char* what, A... args) {
     Timed t(kind, stream);
     if (lds) tile::allow_lds<KERNEL>();
-    hipLaunchKernelGGL(KERNEL, dim3(blocks), dim3(256), lds, stream, args...);
+    hipLaunchKernelGGL(KERNEL, blocks, dim3(threads), lds, stream, args...);
     return check_launch(what);
 }
 
@@ -350,29 +608,51 @@ template <auto KERNEL, typename... A> ff_status go(int kind, uint32_t blocks, si
 struct Tables {
     Table piece, tri, app;
     uint32_t pieces, tris, apps;
+    int splits;
+    double* partial;
+    float* parts;
 };
-template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, const StepArgs& a, int steps, const float* norm, double* partial, char* ws, hipStream_t stream) {
+template <int LAST> constexpr const char* kWhat = LAST == kWeights ? "ff_muon_step" : "ff_orthogonalise";
+
+template <int LAST, typename P> ff_status apply(const Tables& t, int which, const StepArgs& a, const float* norm, char* ws, hipStream_t stream, const char* what) {
+    if (t.apps > 256) return go<k_ns_apply<LAST, P, kShallow>>(KK_NS_APPLY, t.apps, 256, Cores<kShallow>::kLds, stream, what, t.app, ws, which, a, norm);
+    return go<k_ns_apply<LAST, P, kDeep>>(KK_NS_APPLY, t.apps, 256, Cores<kDeep>::kLds, stream, what, t.app, ws, which, a, norm);
+}
+template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, const StepArgs& a, int steps, const float* norm, char* ws, hipStream_t stream) {
     constexpr bool MUON = LAST == kWeights;
-    const char* what = MUON ? "ff_muon_step" : "ff_orthogonalise";
-    ff_status st = go<k_muon_momentum<G, MUON>>(KK_MUON_MOMENTUM, t.pieces, 0, stream, what, t.piece, a, norm, partial);
-    if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 0, stream, what, t.piece, a, norm, (const double*)partial, ws);
+    const char* what = kWhat<LAST>;
+    ff_status st = go<k_muon_momentum<G, MUON>>(KK_MUON_MOMENTUM, t.pieces, 256, 0, stream, what, t.piece, a, norm, t.partial);
+    if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 256, 0, stream, what, t.piece, a, norm, (const double*)t.partial, ws);
+    constexpr size_t shallow = Cores<kShallow>::kLds, deep = Cores<kDeep>::kLds;
     for (int s = 0; s < steps && st == FF_OK; ++s) {
-        st = go<k_ns_gram>(KK_NS_GRAM, t.tris, kTileLds, stream, what, t.tri, ws, s & 1);
-        if (st == FF_OK) st = go<k_ns_poly>(KK_NS_POLY, t.tris, kTileLds, stream, what, t.tri, ws, a.b, a.c);
+        const int which = s & 1;
+        if (t.splits > 1) {
+            st = go<k_ns_gram<kShallow, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, shallow, stream, what, t.tri, ws, which, t.parts);
+            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, t.tris, 256, 0, stream, what, t.tri, ws, (const float*)t.parts, t.splits);
+        } else if (t.tris > 256) st = go<k_ns_gram<kShallow, false>>(KK_NS_GRAM, t.tris, 256, shallow, stream, what, t.tri, ws, which, (float*)nullptr);
+        else st = go<k_ns_gram<kDeep, false>>(KK_NS_GRAM, t.tris, 256, deep, stream, what, t.tri, ws, which, (float*)nullptr);
         if (st != FF_OK) return st;
-        if (s + 1 < steps) st = go<k_ns_apply<kMore, float>>(KK_NS_APPLY, t.apps, kTileLds, stream, what, t.app, ws, s & 1, a, norm);
-        else st = go<k_ns_apply<LAST, P>>(KK_NS_APPLY, t.apps, kTileLds, stream, what, t.app, ws, s & 1, a, norm);
+        if (t.tris > 256) st = go<k_ns_poly<kShallow>>(KK_NS_POLY, t.tris, 256, shallow, stream, what, t.tri, ws, a.b, a.c);
+        else st = go<k_ns_poly<kDeep>>(KK_NS_POLY, t.tris, 256, deep, stream, what, t.tri, ws, a.b, a.c);
+        if (st != FF_OK) return st;
+        st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream, what) : apply<LAST, P>(t, which, a, norm, ws, stream, what);
     }
     return st;
+}
+// `count` matrices of a size from `first` on, a block each
+template <typename G, typename P, int LAST> ff_status small(const Table& t, int size, int first, int count, const StepArgs& a, int steps, const float* norm, hipStream_t stream) {
+    if (count == 0) return FF_OK;
+    if (size == 64) return go<k_ns_small<64, LAST, G, P>>(KK_NS_SMALL, count, Small<64>::kThreads, Small<64>::kLds, stream, kWhat<LAST>, t, first, steps, a, norm);
+    return go<k_ns_small<128, LAST, G, P>>(KK_NS_SMALL, count, Small<128>::kThreads, Small<128>::kLds, stream, kWhat<LAST>, t, first, steps, a, norm);
 }
 
 // ---- a plan: header, batches, matrices, places -------------------------------------------------
 struct Header {
     uint32_t tag;
     int32_t matrices, batches, pieces, tris, apps;
+    int32_t small, smaller;                       // matrices of at most 128 x 128 and, behind them, of at most 64 x 64, the last of all
     int64_t ws;                                   // the largest batch's
     int64_t bytes;                                // of the plan
-    int64_t values;
 };
 static_assert(sizeof(Header) % 16 == 0 && sizeof(Matrix) % 16 == 0 && sizeof(Batch) % 8 == 0, "the plan's records");
 uint32_t tag_of(const ff_muon_desc& d) { return 0x4d000000u | d.param_dtype << 8 | d.grad_dtype; }
@@ -403,43 +683,73 @@ Matrix matrix_from(const ff_muon_tensor& t) {
     m.pieces = pieces_of(m);
     return m;
 }
+// Places of matrices first .. last - 1 in an order that keeps a matrix (a run of its tiles, where few matrices have many) on one XCD and loads all eight alike
+template <typename Count, typename Weight>
+void spread(const std::vector<Matrix>& matrices, int first, int last, Count count, Weight weight, std::vector<Place>& out) {
+    int64_t total = 0;
+    for (int i = first; i < last; ++i) total += count(matrices[i]);
+    const int run = (int)((total + 4 * kXcds - 1) / (4 * kXcds));
+    std::vector<Place> queue[kXcds];
+    int64_t load[kXcds] = {};
+    for (int i = first; i < last; ++i) {
+        const int n = count(matrices[i]);
+        for (int at = 0; at < n; at += run) {
+            const int q = (int)(std::min_element(load, load + kXcds) - load), end = std::min(n, at + run);
+            load[q] += (end - at) * weight(matrices[i]);
+            for (int k = at; k < end; ++k) queue[q].push_back({i, k});
+        }
+    }
+    size_t longest = 0;
+    for (const auto& q : queue) longest = std::max(longest, q.size());
+    for (size_t k = 0; k < longest; ++k)
+        for (const auto& q : queue) out.push_back(k < q.size() ? q[k] : Place{-1, 0});
+}
 struct Made {
     std::vector<Matrix> matrices;
     std::vector<Batch> batches;
-    int64_t pieces = 0, tris = 0, apps = 0, ws = 0, values = 0;
+    std::vector<Place> piece, tri, app;
+    int64_t ws = 256;
+    int small = 0, smaller = 0;
 };
-// Matrices of much work first, so that small ones fill the end; a batch ends where its workspace would pass kBatch.
+// Large matrices first, so that small ones fill the end; a batch ends where its workspace would pass kBatch.
 Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
     Made r;
     for (int i = 0; i < d.n_tensors; ++i)
-        if (ts[i].rows > 0 && ts[i].cols > 0) {
-            r.matrices.push_back(matrix_from(ts[i]));
-            r.values += (int64_t)ts[i].rows * ts[i].cols;
-        }
+        if (ts[i].rows > 0 && ts[i].cols > 0) r.matrices.push_back(matrix_from(ts[i]));
     std::stable_sort(r.matrices.begin(), r.matrices.end(), [](const Matrix& a, const Matrix& b) { return std::max(a.rp(), a.cp()) > std::max(b.rp(), b.cp()); });
-    Batch b{};
-    auto close = [&] {
-        if (b.pieces) r.batches.push_back(b);
-        r.ws = std::max(r.ws, b.ws + (int64_t)align256((size_t)b.pieces * 8));
-        r.pieces += b.pieces;
-        r.tris += b.tris;
-        r.apps += b.apps;
-        b = Batch{};
-        b.piece0 = (int32_t)r.pieces;
-        b.tri0 = (int32_t)r.tris;
-        b.app0 = (int32_t)r.apps;
-    };
-    for (Matrix& m : r.matrices) {
-        if (b.pieces && b.ws + m.bytes() > kBatch) close();
-        m.ws = b.ws;
-        m.piece0 = b.pieces;
-        b.ws += (int64_t)align256((size_t)m.bytes());
-        b.pieces += m.pieces;
-        b.tris += tris_of(m);
-        b.apps += apps_of(m);
-        if (r.pieces + b.pieces > INT32_MAX / 2 || r.apps + b.apps > INT32_MAX / 2 || r.tris + b.tris > INT32_MAX / 2) throw std::bad_alloc();
+    int large = 0;
+    for (const Matrix& m : r.matrices) {
+        large += small_of(m) == 0;
+        r.small += small_of(m) == 128;
+        r.smaller += small_of(m) == 64;
     }
-    close();
+    for (int first = 0; first < large;) {
+        Batch b{};
+        b.piece0 = (int32_t)r.piece.size();
+        b.tri0 = (int32_t)r.tri.size();
+        b.app0 = (int32_t)r.app.size();
+        int last = first;
+        int64_t tris = 0, longest = 0;
+        for (; last < large && (last == first || b.ws + r.matrices[last].bytes() <= kBatch); ++last) {
+            Matrix& m = r.matrices[last];
+            m.ws = b.ws;
+            m.piece0 = b.pieces;
+            b.ws += (int64_t)align256((size_t)m.bytes());
+            b.pieces += m.pieces;
+            tris += tris_of(m);
+            longest = std::max(longest, std::max(m.rp(), m.cp()));
+            for (int32_t k = 0; k < m.pieces; ++k) r.piece.push_back({last, k});
+        }
+        spread(r.matrices, first, last, tris_of, [](const Matrix& m) { return std::max(m.rp(), m.cp()) + 128; }, r.tri);
+        spread(r.matrices, first, last, apps_of, [](const Matrix& m) { return m.np() + 128; }, r.app);
+        b.tris = (int32_t)(r.tri.size() - b.tri0);
+        b.apps = (int32_t)(r.app.size() - b.app0);
+        b.splits = splits_of(tris, longest);
+        r.ws = std::max(r.ws, b.ws + (int64_t)align256((size_t)b.pieces * 8) + parts_bytes(b.tris, b.splits));
+        if (r.piece.size() > INT32_MAX / 2 || r.tri.size() > INT32_MAX / 2 || r.app.size() > INT32_MAX / 2) throw std::bad_alloc();
+        r.batches.push_back(b);
+        first = last;
+    }
     return r;
 }
 Header header_of(const ff_muon_desc& d, const Made& r) {
@@ -447,11 +757,12 @@ Header header_of(const ff_muon_desc& d, const Made& r) {
     h.tag = tag_of(d);
     h.matrices = (int32_t)r.matrices.size();
     h.batches = (int32_t)r.batches.size();
-    h.pieces = (int32_t)r.pieces;
-    h.tris = (int32_t)r.tris;
-    h.apps = (int32_t)r.apps;
-    h.ws = std::max<int64_t>(r.ws, 256);
-    h.values = r.values;
+    h.pieces = (int32_t)r.piece.size();
+    h.tris = (int32_t)r.tri.size();
+    h.apps = (int32_t)r.app.size();
+    h.small = r.small;
+    h.smaller = r.smaller;
+    h.ws = r.ws;
     h.bytes = layout_of(h).bytes;
     return h;
 }
@@ -486,17 +797,14 @@ int muon_plan_fill(const ff_muon_desc& d, const ff_muon_tensor* ts, void* plan) 
         char* out = (char*)plan;
         memset(out, 0, (size_t)h.bytes);
         memcpy(out, &h, sizeof h);
-        if (!r.matrices.empty()) {
-            memcpy(out + l.batches, r.batches.data(), sizeof(Batch) * r.batches.size());
-            memcpy(out + l.matrices, r.matrices.data(), sizeof(Matrix) * r.matrices.size());
-        }
-        Place *piece = (Place*)(out + l.piece), *tri = (Place*)(out + l.tri), *app = (Place*)(out + l.app);
-        for (int32_t i = 0; i < h.matrices; ++i) {
-            const Matrix& m = r.matrices[i];
-            for (int32_t k = 0; k < m.pieces; ++k) *piece++ = {i, k};
-            for (int32_t k = 0; k < tris_of(m); ++k) *tri++ = {i, k};
-            for (int32_t k = 0; k < apps_of(m); ++k) *app++ = {i, k};
-        }
+        const auto put = [&](int64_t at, const void* from, size_t bytes) {
+            if (bytes) memcpy(out + at, from, bytes);
+        };
+        put(l.batches, r.batches.data(), sizeof(Batch) * r.batches.size());
+        put(l.matrices, r.matrices.data(), sizeof(Matrix) * r.matrices.size());
+        put(l.piece, r.piece.data(), sizeof(Place) * r.piece.size());
+        put(l.tri, r.tri.data(), sizeof(Place) * r.tri.size());
+        put(l.app, r.app.data(), sizeof(Place) * r.app.size());
         return 0;
     } catch (const std::bad_alloc&) {
         return -1;
@@ -510,31 +818,36 @@ bool muon_plan_whole(const ff_muon_desc& d, const void* plan_host, size_t bytes)
 }
 size_t muon_workspace(const void* plan_host) { return (size_t)((const Header*)plan_host)->ws; }
 
-ff_status muon_step_run(const ff_muon_desc& d, const void* plan_host, const void* plan, const ff_muon_hyper& h, const float* norm, void* ws, hipStream_t stream) {
-    const Header& head = *(const Header*)plan_host;
+namespace {
+template <typename G, typename P> ff_status muon_step(const Header& head, const void* plan_host, const char* dev, const StepArgs& a, int steps, const float* norm, char* ws, hipStream_t stream) {
     const Layout l = layout_of(head);
-    const StepArgs a{(float)h.lr, (float)h.beta, (float)(1. - h.beta), norm ? (float)h.max_norm : 0.f, h.eps, (float)h.a, (float)h.b, (float)h.c, h.nesterov, h.scale == FF_MUON_RMS};
-    const char* dev = (const char*)plan;
+    Table t{};
+    t.matrices = (const Matrix*)(dev + l.matrices);
     for (int i = 0; i < head.batches; ++i) {
         const Batch& b = ((const Batch*)((const char*)plan_host + l.batches))[i];
-        Table t{};
-        t.matrices = (const Matrix*)(dev + l.matrices);
-        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps};
+        char* const partial = ws + b.ws;
+        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
         ts.piece.places = (const Place*)(dev + l.piece) + b.piece0;
         ts.tri.places = (const Place*)(dev + l.tri) + b.tri0;
         ts.app.places = (const Place*)(dev + l.app) + b.app0;
-        double* partial = (double*)((char*)ws + b.ws);
-        ff_status st;
-        if (d.param_dtype == FF_F32) {
-            st = d.grad_dtype == FF_F32 ? steps_of<float, float, kWeights>(ts, a, h.steps, norm, partial, (char*)ws, stream)
-                                        : steps_of<bf16_t, float, kWeights>(ts, a, h.steps, norm, partial, (char*)ws, stream);
-        } else {
-            st = d.grad_dtype == FF_F32 ? steps_of<float, bf16_t, kWeights>(ts, a, h.steps, norm, partial, (char*)ws, stream)
-                                        : steps_of<bf16_t, bf16_t, kWeights>(ts, a, h.steps, norm, partial, (char*)ws, stream);
-        }
+        const ff_status st = steps_of<G, P, kWeights>(ts, a, steps, norm, ws, stream);
         if (st != FF_OK) return st;
     }
-    return FF_OK;
+    const int first = head.matrices - head.small - head.smaller;
+    const ff_status st = small<G, P, kWeights>(t, 128, first, head.small, a, steps, norm, stream);
+    return st != FF_OK ? st : small<G, P, kWeights>(t, 64, first + head.small, head.smaller, a, steps, norm, stream);
+}
+}  // namespace
+
+ff_status muon_step_run(const ff_muon_desc& d, const void* plan_host, const void* plan, const ff_muon_hyper& h, const float* norm, void* ws, hipStream_t stream) {
+    const Header& head = *(const Header*)plan_host;
+    const StepArgs a{(float)h.lr, (float)h.beta, (float)(1. - h.beta), norm ? (float)h.max_norm : 0.f, h.eps, (float)h.a, (float)h.b, (float)h.c, h.nesterov, h.scale == FF_MUON_RMS};
+    const char* dev = (const char*)plan;
+    if (d.param_dtype == FF_F32)
+        return d.grad_dtype == FF_F32 ? muon_step<float, float>(head, plan_host, dev, a, h.steps, norm, (char*)ws, stream)
+                                      : muon_step<bf16_t, float>(head, plan_host, dev, a, h.steps, norm, (char*)ws, stream);
+    return d.grad_dtype == FF_F32 ? muon_step<float, bf16_t>(head, plan_host, dev, a, h.steps, norm, (char*)ws, stream)
+                                  : muon_step<bf16_t, bf16_t>(head, plan_host, dev, a, h.steps, norm, (char*)ws, stream);
 }
 
 // ---- matrices of one shape -------------------------------------------------------------------
@@ -543,6 +856,8 @@ struct Uniform {
     Matrix one;
     int64_t bytes;             // of workspace a matrix
     int32_t group;             // matrices worked on together
+    int splits;
+    uint32_t tris, apps;       // places of a group
 };
 Uniform uniform_of(const ff_orthogonalise_desc& d) {
     Uniform u{};
@@ -551,39 +866,49 @@ Uniform uniform_of(const ff_orthogonalise_desc& d) {
     u.one.pieces = pieces_of(u.one);
     u.bytes = (int64_t)align256((size_t)u.one.bytes());
     u.group = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.count, kBatch / u.bytes));
+    u.splits = splits_of((int64_t)u.group * tris_of(u.one), std::max(u.one.rp(), u.one.cp()));
+    u.tris = places_of(u.group, tris_of(u.one));
+    u.apps = places_of(u.group, apps_of(u.one));
     return u;
 }
-}  // namespace
-size_t orthogonalise_workspace(const ff_orthogonalise_desc& d) {
-    const Uniform u = uniform_of(d);
-    return (size_t)u.bytes * u.group + align256((size_t)u.group * u.one.pieces * 8);
-}
-ff_status orthogonalise_run(const ff_orthogonalise_desc& d, const void* x, void* out, void* ws, hipStream_t stream) {
+template <typename T> ff_status orthogonalise(const ff_orthogonalise_desc& d, const void* x, void* out, char* ws, hipStream_t stream) {
     const Uniform u = uniform_of(d);
     StepArgs a{};
     a.eps = d.eps;
     a.a = (float)d.a;
     a.b = (float)d.b;
     a.c = (float)d.c;
-    const int64_t step = (int64_t)d.rows * d.cols * (d.dtype == FF_F32 ? 4 : 2);
+    Table t{};
+    t.one = u.one;
+    t.in_step = t.out_step = (int64_t)d.rows * d.cols * (int64_t)sizeof(T);
+    t.ws_step = u.bytes;
+    if (const int size = small_of(u.one)) {
+        t.one.g = x;
+        t.one.p = out;
+        return small<T, T, kOut>(t, size, 0, d.count, a, d.steps, nullptr, stream);
+    }
+    char* const partial = ws + u.bytes * u.group;
     for (int32_t i = 0; i < d.count; i += u.group) {
-        const int32_t n = std::min(u.group, d.count - i);
-        Table t{};
-        t.one = u.one;
-        t.one.g = (const char*)x + i * step;
-        t.one.p = (char*)out + i * step;
-        t.in_step = t.out_step = step;
-        t.ws_step = u.bytes;
-        Tables ts{t, t, t, (uint32_t)(n * u.one.pieces), (uint32_t)(n * tris_of(u.one)), (uint32_t)(n * apps_of(u.one))};
-        ts.piece.each = u.one.pieces;
-        ts.tri.each = tris_of(u.one);
-        ts.app.each = apps_of(u.one);
-        double* partial = (double*)((char*)ws + u.bytes * u.group);
-        const ff_status st = d.dtype == FF_F32 ? steps_of<float, float, kOut>(ts, a, d.steps, nullptr, partial, (char*)ws, stream)
-                                               : steps_of<bf16_t, bf16_t, kOut>(ts, a, d.steps, nullptr, partial, (char*)ws, stream);
+        t.count = std::min(u.group, d.count - i);
+        t.one.g = (const char*)x + i * t.in_step;
+        t.one.p = (char*)out + i * t.out_step;
+        Tables ts{t, t, t, 0, 0, 0, u.splits, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
+        ts.pieces = places_of(t.count, ts.piece.each = u.one.pieces);
+        ts.tris = places_of(t.count, ts.tri.each = tris_of(u.one));
+        ts.apps = places_of(t.count, ts.app.each = apps_of(u.one));
+        const ff_status st = steps_of<T, T, kOut>(ts, a, d.steps, nullptr, ws, stream);
         if (st != FF_OK) return st;
     }
     return FF_OK;
+}
+}  // namespace
+size_t orthogonalise_workspace(const ff_orthogonalise_desc& d) {
+    const Uniform u = uniform_of(d);
+    if (small_of(u.one)) return 256;
+    return (size_t)u.bytes * u.group + align256((size_t)u.group * u.one.pieces * 8) + (size_t)parts_bytes(u.tris, u.splits);
+}
+ff_status orthogonalise_run(const ff_orthogonalise_desc& d, const void* x, void* out, void* ws, hipStream_t stream) {
+    return d.dtype == FF_F32 ? orthogonalise<float>(d, x, out, (char*)ws, stream) : orthogonalise<bf16_t>(d, x, out, (char*)ws, stream);
 }
 
 }  // namespace ff

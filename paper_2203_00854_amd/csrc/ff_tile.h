@@ -259,15 +259,13 @@ struct Core {
             if (i < stages) loads.issue(a, b, m0, n0, from + i * BK, lds + i * kStage);
         // Operands of the next round are read while a round's products run, so a stage has to be there one turn early.
         Frags f[2];
-        if (STAGES > 3 && stages > 2) arrive<2>();
-        else if (stages > 1) arrive<1>();
-        else arrive<0>();
+        arrive(stages - 1 < STAGES - 2 ? stages - 1 : STAGES - 2);
         read(f[0], smem, wm, wn, 0, lane);
         int buf = 0, t = 0;
         const auto turn = [&](Frags& now, Frags& then) {
             // the next stage is there, and nobody reads the one before any more, in whose place the loads of the one STAGES - 1 ahead go
-            if (STAGES > 3 && t + 2 < stages) arrive<1>();
-            else arrive<0>();
+            if (t + STAGES - 2 < stages) arrive<STAGES - 3>();
+            else arrive(stages - t - 2);
             if (t + STAGES - 1 < stages) loads.issue(a, b, m0, n0, from + (int64_t)(t + STAGES - 1) * BK, lds + (buf == 0 ? STAGES - 1 : buf - 1) * kStage);
             const int next = buf + 1 == STAGES ? 0 : buf + 1;
             const unsigned char *image = smem + buf * kStage, *image_next = smem + next * kStage;
@@ -303,8 +301,15 @@ struct Core {
     }
     // waits until all but the loads of the youngest N stages have arrived, for every wavefront, and for its own reads
     template <int N> static __device__ __forceinline__ void arrive() {
-        static_assert(STAGES >= 3 && STAGES <= 4 && 2 * kLoads < 64, "the counter");
+        static_assert(STAGES >= 3 && (STAGES - 2) * kLoads < 64, "the counter");
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N * kLoads) : "memory");
+    }
+    template <int N = STAGES - 2> static __device__ __forceinline__ void arrive(int n) {          // at the ends, where fewer are under way
+        if constexpr (N > 0) {
+            if (n >= N) arrive<N>();
+            else arrive<N - 1>(n);
+        } else
+            arrive<0>();
     }
 
     // Results leave through LDS, where a lane finds eight neighbours of a row: straight from the accumulators a store would reach sixteen bytes of each of 32 rows,

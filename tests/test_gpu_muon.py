@@ -33,7 +33,7 @@ def check(got, g, half, **kw):
     assert np.linalg.norm(off) <= total + half * np.linalg.norm(want) and np.all(off <= most + half * (np.abs(want) + most)), (np.linalg.norm(off), total, off.max(), most)
 
 
-SHAPES = [(1, 1, 1), (3, 1, 9), (2, 9, 1), (2, 16, 16), (3, 17, 40), (3, 40, 17), (1, 128, 64), (2, 129, 130), (1, 300, 140), (1, 140, 300), (5, 64, 8)]
+SHAPES = [(1, 1, 1), (3, 1, 9), (2, 9, 1), (2, 16, 16), (3, 17, 40), (3, 40, 17), (1, 128, 64), (2, 129, 130), (1, 300, 140), (1, 140, 300), (5, 64, 8), (9, 65, 100), (2, 128, 128), (17, 150, 33), (1, 2048, 96), (1, 200, 2000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -137,7 +137,7 @@ class Model:
                 assert np.all(np.abs(n64(self.p[i]) - w) <= e_w + half * (np.abs(w) + e_w)), name
 
 
-LISTS = [[(1, 1)], [(64, 48), (48, 64), (130, 20), (0, 5), (20, 130), (1, 33), (33, 1), (7, 7)], [(256, 64), (64, 256), (128, 128)]]
+LISTS = [[(1, 1)], [(150, 40)] * 9 + [(40, 700)] * 4 + [(33, 60)] * 3, [(64, 48), (48, 64), (130, 20), (0, 5), (20, 130), (1, 33), (33, 1), (7, 7)], [(256, 64), (64, 256), (128, 128)]]
 
 
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
@@ -153,12 +153,12 @@ def test_steps(param, grad):
 
 @pytest.mark.parametrize("kw", [dict(nesterov=False), dict(scale="rms"), dict(beta=0.0), dict(steps=2, lr=0.5), dict(lr=0.0)])
 def test_step_arguments(kw):
-    model = Model(LISTS[1], "f32", "f32")
+    model = Model(LISTS[2], "f32", "f32")
     model.check(lambda: P.ff_muon_step(model.plan, **{"lr": 0.02, **kw}), **kw)
 
 
 def test_clipping_and_a_norm_that_is_not_finite():
-    model = Model(LISTS[1], "master", "bf16")
+    model = Model(LISTS[2], "master", "bf16")
     norm = P.ff_grad_norm(P.make_grad_plan([g.view(-1) for g in model.g]))
     want = np.sqrt(sum((n64(g) ** 2).sum() for g in model.g))
     assert abs(norm.item() - want) <= 2 * M.U * want
@@ -170,7 +170,7 @@ def test_clipping_and_a_norm_that_is_not_finite():
 
 
 def test_bad_gradient_stays_in_its_matrix():
-    model, other = Model(LISTS[1], "f32", "f32"), Model(LISTS[1], "f32", "f32")
+    model, other = Model(LISTS[2], "f32", "f32"), Model(LISTS[2], "f32", "f32")
     model.g[2][5, 5] = float("nan")
     for m in (model, other):
         P.ff_muon_step(m.plan, 0.02)
@@ -207,7 +207,7 @@ def test_batches_of_a_plan():
 
 
 def test_another_stream_and_a_graph():
-    model, other = Model(LISTS[1], "master", "bf16"), Model(LISTS[1], "master", "bf16")
+    model, other = Model(LISTS[2], "master", "bf16"), Model(LISTS[2], "master", "bf16")
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(stream):
