@@ -31,7 +31,7 @@ constexpr int kPad = 16;
 constexpr int kTile = 128;
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 16384;                    // values that a block of the element-wise kernels holds
-constexpr int64_t kBatch = 256 << 20;            // workspace of the matrices that are worked on together, unless one alone needs more
+constexpr int64_t kBatch = 512 << 20;            // workspace of the matrices that are worked on together, unless one alone needs more
 
 // One matrix, as the kernels see it.
 struct Matrix {
@@ -78,11 +78,17 @@ __device__ __forceinline__ Matrix matrix_of(const Table& t, int32_t i) {
 __device__ __forceinline__ Place place_at(const Table& t, uint32_t block) {
     if (t.matrices) return t.places[block];
     const uint32_t each = (uint32_t)t.each;
-    if (t.count < kXcds) return {(int32_t)(block / each), (int32_t)(block % each)};
+    if (t.count < kXcds) {                                     // few matrices: runs of tiles
+        const uint32_t all = (uint32_t)t.count * each, run = (all + kXcds - 1) / kXcds, at = block % kXcds * run + block / kXcds;
+        return {at < all ? (int32_t)(at / each) : -1, (int32_t)(at % each)};
+    }
     const int32_t m = (int32_t)(block / kXcds / each * kXcds + block % kXcds);
     return {m < t.count ? m : -1, (int32_t)(block / kXcds % each)};
 }
-uint32_t places_of(int32_t count, int32_t each) { return (uint32_t)(count < kXcds ? count : (count + kXcds - 1) / kXcds * kXcds) * (uint32_t)each; }
+uint32_t places_of(int32_t count, int32_t each) {
+    const uint32_t all = (uint32_t)count * (uint32_t)each;
+    return count < kXcds ? (all + kXcds - 1) / kXcds * kXcds : (uint32_t)((count + kXcds - 1) / kXcds * kXcds) * (uint32_t)each;
+}
 
 // ---- pairs ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t half_bits(_Float16 h) { return __builtin_bit_cast(uint16_t, h); }
@@ -103,11 +109,11 @@ __device__ __forceinline__ void store_pairs(char* p, const float (&v)[8]) {
     *(uint4*)p = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
     *(uint4*)(p + 32) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
 }
-__device__ __forceinline__ void load_pairs(const char* p, float (&v)[8]) {
-    const uint4 h4 = *(const uint4*)p, l4 = *(const uint4*)(p + 32);
-    const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu);
+struct Pairs { uint4 hi, lo; };
+__device__ __forceinline__ Pairs load_pairs(const char* p) { return {*(const uint4*)p, *(const uint4*)(p + 32)}; }
+__device__ __forceinline__ float value_of(const Pairs& p, int q) {
+    const uint32_t h[4] = {p.hi.x, p.hi.y, p.hi.z, p.hi.w}, l[4] = {p.lo.x, p.lo.y, p.lo.z, p.lo.w};
+    return q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu);
 }
 
 // ---- momentum and norm ---------------------------------------------------------------------
@@ -221,9 +227,9 @@ template <int STAGES> struct Cores {
     typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
     static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 };
-// Four stages leave room for two blocks on a compute unit, eight for one: 48 KiB under way twice, or 112 KiB once where a launch has fewer blocks than
+// Three stages leave room for three blocks on a compute unit, whose ends then overlap with the others' products; eight for one, where a launch has fewer blocks than
 // there are units (a stage takes 0.18 us of matrix instructions and 0.8 us to arrive).
-constexpr int kShallow = 4, kDeep = 8;
+constexpr int kShallow = 3, kDeep = 8;
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
     return {ws + x.x(which), x.cp() * 4, x.rp(), (int32_t)(x.cp() * 4)};
@@ -238,20 +244,21 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     j = t - i * (i + 1) / 2;
 }
-// a tile of a symmetric matrix and its mirror image; value(m, n, v) turns sums into what is held
+// a tile of a symmetric matrix and its mirror image; value(v, old) turns sums into what is held, old being what `from` (NULL: nothing) holds there
 template <class C, typename F>
-__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], char* out, int64_t np, int i, int j, unsigned char* smem, F value) {
-    const auto store = [&](int64_t m, int64_t n, float (&v)[8]) {
+__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], char* out, const char* from, int64_t np, int i, int j, unsigned char* smem, F value) {
+    const auto fetch = [&](int64_t m, int64_t n) { return from && m < np && n < np ? load_pairs(from + pairs_at(m * np + n)) : Pairs{}; };
+    const auto store = [&](int64_t m, int64_t n, float (&v)[8], const Pairs& old) {
         if (m >= np || n >= np) return;
-        value(m, n, v);
+        value(v, old);
         store_pairs(out + pairs_at(m * np + n), v);
     };
-    C::rows(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
-    if (i != j) C::columns(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, store);
+    C::rows(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
+    if (i != j) C::columns(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
 }
 
 // A.  SPLIT: sums over a part of k each, for k_ns_join
-template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, 2) void k_ns_gram(Table t, char* ws, int which, float* parts) {
+template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_gram(Table t, char* ws, int which, float* parts) {
     typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
@@ -268,9 +275,9 @@ template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, 2) void k_ns
     else Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, from, to, smem);
     if constexpr (SPLIT) {
         float* out = parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kTile * kTile;
-        Straight::rows(acc[0], 0, 0, smem, [&](int64_t m, int64_t n, float (&v)[8]) { tile::store8(out + m * kTile + n, v); });
+        Straight::rows(acc[0], 0, 0, smem, Straight::none, [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) { tile::store8(out + m * kTile + n, v); });
     } else
-        store_symmetric<Straight>(acc[0], ws + x.a(0), x.np(), i, j, smem, [&](int64_t, int64_t, float (&v)[8]) {
+        store_symmetric<Straight>(acc[0], ws + x.a(0), (const char*)nullptr, x.np(), i, j, smem, [&](float (&v)[8], const Pairs&) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
         });
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float*
 }
 
 // B = b A + c A^2
-template <int STAGES> __global__ __launch_bounds__(256, 2) void k_ns_poly(Table t, char* ws, float b, float c) {
+template <int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_poly(Table t, char* ws, float b, float c) {
     typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
@@ -327,12 +334,9 @@ template <int STAGES> __global__ __launch_bounds__(256, 2) void k_ns_poly(Table 
     Straight::clear(acc);
     const int64_t np = x.np();
     Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
-    const char* a = ws + x.a(0);
-    store_symmetric<Straight>(acc[0], ws + x.a(1), np, i, j, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
-        float was[8];
-        load_pairs(a + pairs_at(m * np + n), was);
+    store_symmetric<Straight>(acc[0], ws + x.a(1), ws + x.a(0), np, i, j, smem, [&](float (&v)[8], const Pairs& was) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = b * was[q] + (c * kUnscale) * v[q];
+        for (int q = 0; q < 8; ++q) v[q] = b * value_of(was, q) + (c * kUnscale) * v[q];
     });
 }
 
@@ -357,7 +361,7 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
     }
 }
 // X = a X + B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights
-template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, 2) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
+template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
     typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
@@ -378,12 +382,11 @@ template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, 2)
     const char* from = ws + x.x(which);
     char* to = ws + x.x(which ^ 1);
     const float size = size_of(x, a);
-    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+    const auto fetch = [&](int64_t m, int64_t n) { return m < rp && n < cp ? load_pairs(from + pairs_at(m * cp + n)) : Pairs{}; };
+    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, [&](int64_t m, int64_t n, float (&v)[8], const Pairs& was) {
         if (m >= rp || n >= cp) return;
-        float was[8];
-        load_pairs(from + pairs_at(m * cp + n), was);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = a.a * was[q] + kUnscale * v[q];
+        for (int q = 0; q < 8; ++q) v[q] = a.a * value_of(was, q) + kUnscale * v[q];
         if constexpr (LAST == kMore) store_pairs(to + pairs_at(m * cp + n), v);
         else {
             const int left = x.cols - (int)n;
@@ -403,7 +406,7 @@ template <int SIZE> struct Small {
     static constexpr int kWaves = SIZE == 128 ? 8 : 4, kThreads = 64 * kWaves, kUnits = SIZE == 128 ? 2 : 1;
     static constexpr int W = SIZE / 4, kImage = SIZE * SIZE * 4, kLds = 2 * kImage;
     // sixteen bytes of row `row`: eight values from column c, a multiple of eight, of the hi part (p = 0) or the lo part.  Rows that one cycle reads together, straight or turned, lie in banks of their own.
-    static __device__ __forceinline__ int at(int row, int c, int p) { return row * (W * 16) + (((c >> 4) * 4 + p * 2 + (c >> 3 & 1)) ^ ((row & 3) << 1 | (row >> 2 & 1))) * 16; }
+    static __device__ __forceinline__ int at(int row, int c, int p) { return row * (W * 16) + (((c >> 4) * 4 + p * 2 + (c >> 3 & 1)) ^ ((row & 1) << 1 | (row & 2) << 2 | (row >> 2 & 1) | (row & 8) >> 1)) * 16; }
 
     // 32 rows (straight) or columns (turned) from `first`, k = 16 s ..
     template <bool T> static __device__ __forceinline__ Pair::Frag frag(const unsigned char* image, int first, int s, int lane) {
@@ -430,12 +433,35 @@ template <int SIZE> struct Small {
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[u][v] = 0.f;
         if (tiles <= 0) return;
-        for (int s = 0; s < k / 16; ++s) {
-            const Pair::Frag fa = frag<TA>(a, m0, s, lane);
+        // (a second tile that is none is worked on like the first, for no result)
+        Frags f[2];
+        read<TA, TB>(f[0], a, b, m0, n0, tiles, 0, lane);
+        const int rounds = k / 16;
+        const auto turn = [&](int s, Frags& now, Frags& then) {
+            read<TA, TB>(then, a, b, m0, n0, tiles, s + 1 < rounds ? s + 1 : s, lane);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u)
-                if (u < tiles) acc[u] = Pair::mma(frag<TB>(b, n0 + 32 * u, s, lane), fa, acc[u]);
+            for (int p = 0; p < 3; ++p)                        // lo hi, hi lo, hi hi: of both tiles in turn, an instruction waits for the one before of its own
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u)
+                    acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(tile::f16x8, now.b[u].u[p == 0]), __builtin_bit_cast(tile::f16x8, now.a.u[p == 1]), acc[u], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int s = 0;
+        for (; s + 1 < rounds; s += 2) {
+            turn(s, f[0], f[1]);
+            turn(s + 1, f[1], f[0]);
         }
+        if (s < rounds) turn(s, f[0], f[1]);
+    }
+    struct Frags {
+        Pair::Frag a, b[kUnits];
+    };
+    template <bool TA, bool TB>
+    static __device__ __forceinline__ void read(Frags& f, const unsigned char* a, const unsigned char* b, int m0, int n0, int tiles, int s, int lane) {
+        f.a = frag<TA>(a, m0, s, lane);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) f.b[u] = frag<TB>(b, u < tiles ? n0 + 32 * u : n0, s, lane);
     }
     // value(old, sum) of the wavefront's tiles, old being what image `from` holds there
     template <typename F> static __device__ __forceinline__ void combine(f32x16 (&acc)[kUnits], const unsigned char* from, int m0, int n0, int tiles, int lane, F value) {
@@ -530,10 +556,10 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
     }
     // the wavefront's tiles of A, and of X
     const auto place = [&](int rows, int cols, int& m0, int& n0, int& tiles) {
-        const int across = (cols + 31) / 32, groups = (across + S::kUnits - 1) / S::kUnits, down = (rows + 31) / 32;
+        const int across = (cols + 31) / 32, down = (rows + 31) / 32, each = across * down > S::kWaves ? S::kUnits : 1, groups = (across + each - 1) / each;
         m0 = wave / groups * 32;
-        n0 = wave % groups * S::kUnits * 32;
-        tiles = wave < groups * down ? (across - n0 / 32 < S::kUnits ? across - n0 / 32 : S::kUnits) : 0;
+        n0 = wave % groups * each * 32;
+        tiles = wave < groups * down ? (across - n0 / 32 < each ? across - n0 / 32 : each) : 0;
     };
     int am, an, at, xm, xn, xt;
     place(np, np, am, an, at);
@@ -568,11 +594,10 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         if (place >= rp * cp) continue;
         const Spot s = spot_of(x, place);
         if (s.n == 0) continue;
-        const uint4 h4 = *(const uint4*)(xs + S::at((int)s.r, s.c, 0)), l4 = *(const uint4*)(xs + S::at((int)s.r, s.c, 1));
-        const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+        const Pairs p{*(const uint4*)(xs + S::at((int)s.r, s.c, 0)), *(const uint4*)(xs + S::at((int)s.r, s.c, 1))};
         float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = kUnscale * (q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu));
+        for (int q = 0; q < 8; ++q) v[q] = kUnscale * value_of(p, q);
         finish<LAST, P>(x, a, size, s.at, s.n, v);
     }
 }

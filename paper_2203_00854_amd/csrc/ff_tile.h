@@ -120,13 +120,16 @@ struct Core {
     static constexpr int kBytesA = BM * BK * Op::kSize, kBytesB = BN * BK * Op::kSize, kStage = NA * kBytesA + NB * kBytesB;
     static constexpr int kLoads = kStage / 16 / kThreads;          // of a wavefront, for one stage
     static_assert(kBytesA % (16 * kThreads) == 0 && kBytesB % (16 * kThreads) == 0, "the wavefronts count the same loads");
+    static_assert(!(TA || TB) || BM >= 64, "turned rows hold sixteen slots (bfloat16: eight)");
     static_assert(MT >= 1 && NT >= 1 && BK % Op::kStep == 0, "tile");
 
-    // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that the lanes that read in one cycle
-    // (eight at sixteen bytes, sixteen at eight) meet all banks
+    // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that what one cycle reads (256 bytes) lies in
+    // banks of its own: sixteen bytes of sixteen rows, or, turned, of 32 columns' values in four rows (of a pair's, two pieces 64 bytes apart).
     template <bool T, int W> static __device__ __forceinline__ int swizzle(int row) {
-        if constexpr (T) return Op::kStep == 8 ? 0 : W >= 8 ? 2 * (row & 3) : 2 * ((row >> 1) & 1);
-        return W >= 8 ? row & 7 : W == 4 ? (row >> 1) & 3 : 0;
+        if constexpr (!T) return W >= 16 ? row & 15 : W == 8 ? row >> 1 & 7 : W == 4 ? row >> 2 & 3 : 0;
+        else if constexpr (Op::kStep == 8) return row << 1 & 8;
+        else if constexpr (Op::kPlanes == 2) return (row & 1) << 1 | (row & 2) << 2;
+        else return W >= 16 ? 4 * (row & 3) : 4 * (row >> 1 & 1);
     }
 
     // The loads of one operand's part of a stage.  A lane's address is min(x, limit) + y from a uniform base that moves with k: x, which alone can pass an end, and
@@ -180,7 +183,10 @@ struct Core {
         } else {
             uint32_t v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(image + (8 * s + 4 * hf + j) * (W * 16) + (row0 + (lane & 31)) * 4);
+            for (int j = 0; j < 4; ++j) {
+                const int k = 8 * s + 4 * hf + j, col = row0 + (lane & 31);
+                v[j] = *reinterpret_cast<const uint32_t*>(image + k * (W * 16) + (((col >> 2) ^ swizzle<true, W>(k)) << 4) + (col & 3) * 4);
+            }
             return make_uint4(v[0], v[1], v[2], v[3]);
         }
     }
@@ -314,47 +320,68 @@ struct Core {
 
     // Results leave through LDS, where a lane finds eight neighbours of a row: straight from the accumulators a store would reach sixteen bytes of each of 32 rows,
     // and the stores of a tile would take longer than its products.
+    // A part of the tile at a time, 32 rows (columns) of each wavefront, so that it takes half the memory.
     static constexpr int kPitch = BN + 4, kPitchTurned = BM + 4;        // floats; sixteen bytes more than a row, so that the rows of one cycle lie in banks of their own
-    static constexpr int kOut = 4 * BM * kPitch > 4 * BN * kPitchTurned ? 4 * BM * kPitch : 4 * BN * kPitchTurned;
+    static constexpr int kOutRows = 128 * WM * kPitch, kOutColumns = 128 * WN * kPitchTurned;
+    static constexpr int kOut = kOutRows > kOutColumns ? kOutRows : kOutColumns;
     static constexpr int kLds = STAGES * kStage > kOut ? STAGES * kStage : kOut;
 
-    // body(m, n, v): eight results v in row m, columns n .. n + 7.  smem: kLds bytes that every thread is done with, before and after
-    template <typename F> static __device__ __forceinline__ void rows(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, F body) {
+    // body(m, n, v, old): eight results v in row m, columns n .. n + 7, and what fetch(m, n) has read for them.  The reads of four turns are under way together (a
+    // load behind another turn's store would wait for it to be issued: they may be the same memory as far as the compiler knows).  smem: kLds bytes that every
+    // thread is done with, before and after
+    template <typename Fetch, typename F> static __device__ __forceinline__ void rows(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, Fetch fetch, F body) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        float* out = (float*)smem + ((wave / WN * MT) * 32 + (lane & 31)) * kPitch + (wave % WN * NT) * 32 + 4 * (lane >> 5);
+        float* out = (float*)smem + (wave / WN * 32 + (lane & 31)) * kPitch + (wave % WN * NT) * 32 + 4 * (lane >> 5);
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i) {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    *(float4*)(out + i * 32 * kPitch + j * 32 + 8 * g) = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
-        __syncthreads();
-        leave<BM, BN, kPitch>(smem, m0, n0, body);
-        __syncthreads();
-    }
-    // the same turned: row n, columns m .. m + 7
-    template <typename F> static __device__ __forceinline__ void columns(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, F body) {
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        float* out = (float*)smem + ((wave % WN * NT) * 32 + 4 * (lane >> 5)) * kPitchTurned + (wave / WN * MT) * 32 + (lane & 31);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) out[(j * 32 + 8 * (v / 4) + v % 4) * kPitchTurned + i * 32] = acc[i][j][v];
-        __syncthreads();
-        leave<BN, BM, kPitchTurned>(smem, n0, m0, body);
-        __syncthreads();
-    }
-    template <int R, int C, int PITCH, typename F> static __device__ __forceinline__ void leave(const unsigned char* smem, int64_t r0, int64_t c0, F body) {
-        for (int u = threadIdx.x; u < R * (C / 8); u += kThreads) {
-            const int r = u / (C / 8), c = u % (C / 8) * 8;
-            const float4 a = *(const float4*)((const float*)smem + r * PITCH + c), b = *(const float4*)((const float*)smem + r * PITCH + c + 4);
-            float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            body(r0 + r, c0 + c, v);
+                    *(float4*)(out + j * 32 + 8 * g) = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+            leave<32 * WM, BM / WM, BN, kPitch>(smem, m0 + 32 * i, n0, fetch, body);
         }
     }
+    // the same turned: row n, columns m .. m + 7
+    template <typename Fetch, typename F> static __device__ __forceinline__ void columns(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, Fetch fetch, F body) {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        float* out = (float*)smem + (wave % WN * 32 + 4 * (lane >> 5)) * kPitchTurned + (wave / WN * MT) * 32 + (lane & 31);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) out[(8 * (v / 4) + v % 4) * kPitchTurned + i * 32] = acc[i][j][v];
+            leave<32 * WN, BN / WN, BM, kPitchTurned>(smem, n0 + 32 * j, m0, fetch, body);
+        }
+    }
+    // R rows of which each 32 lie APART after the 32 before
+    template <int R, int APART, int C, int PITCH, typename Fetch, typename F>
+    static __device__ __forceinline__ void leave(const unsigned char* smem, int64_t r0, int64_t c0, Fetch fetch, F body) {
+        constexpr int kTurns = R * (C / 8) / kThreads, kGroup = kTurns < 4 ? kTurns : 4;
+        static_assert(R * (C / 8) % kThreads == 0 && kTurns % kGroup == 0, "turns");
+        typedef decltype(fetch(r0, c0)) Old;
+#pragma unroll 1
+        for (int t0 = 0; t0 < kTurns; t0 += kGroup) {
+            Old old[kGroup];
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) {
+                const int u = (t0 + t) * kThreads + (int)threadIdx.x, r = u / (C / 8);
+                old[t] = fetch(r0 + r / 32 * APART + r % 32, c0 + u % (C / 8) * 8);
+            }
+            if (t0 == 0) __syncthreads();
+#pragma unroll
+            for (int t = 0; t < kGroup; ++t) {
+                const int u = (t0 + t) * kThreads + (int)threadIdx.x, r = u / (C / 8), c = u % (C / 8) * 8;
+                const float4 a = *(const float4*)((const float*)smem + r * PITCH + c), b = *(const float4*)((const float*)smem + r * PITCH + c + 4);
+                float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                body(r0 + r / 32 * APART + r % 32, c0 + c, v, old[t]);
+            }
+        }
+        __syncthreads();
+    }
+    struct Nothing {};
+    static __device__ __forceinline__ Nothing none(int64_t, int64_t) { return {}; }
 };
 
 // once for each kernel that needs more than 64 KiB

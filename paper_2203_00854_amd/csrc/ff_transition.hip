@@ -79,6 +79,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_tr_pack(PackArgs 
     *(uint4*)((T*)p.dst + r * p.cols_out + c) = *(const uint4*)v;
 }
 
+struct Eight { float v[8]; };
 // what is past the end of a row, or in a row that is none, is held as zero
 __device__ __forceinline__ void keep(float (&v)[8], int64_t n) {
     if (n >= 8) return;
@@ -107,7 +108,7 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
         for (int j = 0; j < C::NT; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[0][i][j][v] = gate_of<ACT, sizeof(T) == 2>(acc[0][i][j][v]) * acc[1][i][j][v];
-    C::rows(acc[0], at.m * C::BM, (int64_t)at.n * C::BN, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+    C::rows(acc[0], at.m * C::BM, (int64_t)at.n * C::BN, smem, C::none, [&](int64_t m, int64_t n, float (&v)[8], typename C::Nothing) {
         if (m >= a.rows_out || n >= a.pitch) return;
         keep(v, m < a.rows ? a.f - n : 0);
         tile::store8((T*)a.h + m * a.pitch + n, v);
@@ -132,15 +133,19 @@ template <class C, typename T> __global__ __launch_bounds__(C::kThreads, 2) void
     f32x16 acc[1][C::MT][C::NT];
     C::clear(acc);
     for (int p = 0; p < a.parts; ++p) C::run(acc, a.a + p, a.b + p, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
-    C::rows(acc[0], at.m * C::BM, (int64_t)at.n * C::BN, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+    const auto fetch = [&](int64_t m, int64_t n) {
+        Eight e;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) e.v[q] = 0.f;
+        if (a.residual && m < a.rows && n < a.cols) tile::load_some((const T*)a.residual + m * a.cols + n, a.cols - (int)n, e.v);
+        return e;
+    };
+    C::rows(acc[0], at.m * C::BM, (int64_t)at.n * C::BN, smem, fetch, [&](int64_t m, int64_t n, float (&v)[8], Eight r) {
         if (m >= a.rows || n >= a.cols) return;
         const bool live = !(a.mask && a.mask[m] == 0.f);
-        const int left = a.cols - (int)n;
-        float r[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (a.residual) tile::load_some((const T*)a.residual + m * a.cols + n, left, r);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) r[q] += live ? v[q] : 0.f;
-        tile::store_some((T*)a.out + m * a.cols + n, left, r);
+        for (int q = 0; q < 8; ++q) r.v[q] += live ? v[q] : 0.f;
+        tile::store_some((T*)a.out + m * a.cols + n, a.cols - (int)n, r.v);
     });
 }
 
@@ -245,7 +250,7 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
     void* const out[3] = {a.da, a.db, a.h};
 #pragma unroll
     for (int t = 0; t < 3; ++t)
-        C::rows(acc[t], at.m * C::BM, (int64_t)at.n * C::BN, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
+        C::rows(acc[t], at.m * C::BM, (int64_t)at.n * C::BN, smem, C::none, [&](int64_t m, int64_t n, float (&v)[8], typename C::Nothing) {
             if (m >= a.rows_out || n >= a.pitch) return;
             keep(v, m < a.rows ? a.f - n : 0);
             tile::store8((T*)out[t] + m * a.pitch + n, v);
@@ -274,16 +279,18 @@ template <class C> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_weight
     C::run(acc, a.a + which, a.b + which, m0, n0, from, to, smem);
     float* out = a.partial + ((int64_t)blockIdx.y * 3 + which) * a.fp * a.cp;
     const int32_t rows = last ? a.cp : a.fp, cols = last ? a.fp : a.cp;
-    C::rows(acc[0], m0, n0, smem, [&](int64_t m, int64_t n, float (&v)[8]) {
-        if (m >= rows || n >= cols) return;
-        float* p = out + m * cols + n;
-        if (a.add) {
-            float was[8];
-            tile::load8(p, was);
+    const auto fetch = [&](int64_t m, int64_t n) {
+        Eight e;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += was[q];
-        }
-        tile::store8(p, v);
+        for (int q = 0; q < 8; ++q) e.v[q] = 0.f;
+        if (a.add && m < rows && n < cols) tile::load8(out + m * cols + n, e.v);
+        return e;
+    };
+    C::rows(acc[0], m0, n0, smem, fetch, [&](int64_t m, int64_t n, float (&v)[8], const Eight& was) {
+        if (m >= rows || n >= cols) return;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] += was.v[q];
+        tile::store8(out + m * cols + n, v);
     });
 }
 

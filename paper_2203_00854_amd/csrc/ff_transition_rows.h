@@ -23,7 +23,7 @@ __device__ __forceinline__ f32x16 mma(uint4 a, uint4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// KC: channels / 32, 1 or even (the exchange of slots stays within eight)
+// KC: channels / 32, 1 or even (slots are exchanged within eight or sixteen)
 template <int KC, int WAVES> struct Weights {
     static_assert(KC == 1 || KC % 2 == 0, "slots");
     static constexpr int kThreads = 64 * WAVES;
@@ -32,12 +32,13 @@ template <int KC, int WAVES> struct Weights {
     static constexpr int kStage = 2 * kIn + kOut;
     static constexpr int kLds = 2 * kStage;
 
-    // the slot that holds piece `chunk` of a row: the eight rows that one cycle reads, and the four that a turned read takes, lie in banks of their own
+    // the slot that holds piece `chunk` of a row: the sixteen rows that one cycle reads, and four rows of 64 bytes that a turned read takes, lie in banks of their own
     static __device__ __forceinline__ int slot_in(int row, int chunk) {
-        if constexpr (W >= 8) return chunk ^ ((row & 3) << 1 | (row >> 2 & 1));
-        return chunk ^ (row >> 1 & 3);
+        if constexpr (W % 16 == 0) return chunk ^ ((row & 3) << 2 | (row >> 2 & 3));
+        if constexpr (W % 8 == 0) return chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
+        return chunk ^ (row >> 2 & 3);
     }
-    static __device__ __forceinline__ int slot_out(int row, int chunk) { return chunk ^ (row >> 1 & 3); }
+    static __device__ __forceinline__ int slot_out(int row, int chunk) { return chunk ^ (row >> 2 & 3); }
 
     // hidden channels f0 .. f0 + 31; pitches in bytes
     static __device__ __forceinline__ void load(const char* wa, const char* wb, const char* wo, int64_t f0, int pitch_o, unsigned lds) {
