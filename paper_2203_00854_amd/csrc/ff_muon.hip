@@ -2,7 +2,8 @@
 //
 //   X = G / (|G| + eps);  per step, with n the shorter side:  A = X X^T (X^T X where a matrix is tall);  X = a X + (b A + c A^2) X  (X (...))
 //
-// Three launches a step for all matrices together: the Gram matrix, the polynomial, its product with X.  Values are held as float16 pairs of kScale times
+// Three launches a step for all matrices together: A, and C = b I + c A beside it; B = a I + A C; X = B X.  So no product needs more than its operands: what else
+// it had to add would be another read, in a kernel's last microseconds.  Values are held as float16 pairs of kScale times
 // themselves: 24 significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  Magnitudes
 // to 255 have a place, and singular values are at most 1 at the start and below 1.3 after any number of steps with the usual coefficients; 2^-33 is
 // the smallest step between small values.  A tall matrix is worked on as it lies: its operands are read turned.
@@ -31,7 +32,7 @@ constexpr int kPad = 16;
 constexpr int kTile = 128;
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 16384;                    // values that a block of the element-wise kernels holds
-constexpr int64_t kBatch = 512 << 20;            // workspace of the matrices that are worked on together, unless one alone needs more
+constexpr int64_t kBatch = 1 << 30;            // workspace of the matrices that are worked on together, unless one alone needs more
 
 // One matrix, as the kernels see it.
 struct Matrix {
@@ -39,7 +40,7 @@ struct Matrix {
     void* p;                                     // what the last step writes
     float* master;
     float* m;
-    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B, as pairs
+    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B, C, as pairs
     int32_t rows, cols;
     int32_t piece0, pieces;                      // among the batch's
     float decay;
@@ -52,7 +53,7 @@ struct Matrix {
     __host__ __device__ int64_t bytes_a() const { return np() * np() * 4; }
     __host__ __device__ int64_t x(int which) const { return ws + which * bytes_x(); }
     __host__ __device__ int64_t a(int which) const { return ws + 2 * bytes_x() + which * bytes_a(); }
-    __host__ __device__ int64_t bytes() const { return 2 * bytes_x() + 2 * bytes_a(); }
+    __host__ __device__ int64_t bytes() const { return 2 * bytes_x() + 3 * bytes_a(); }
 };
 struct Place {
     int32_t matrix, at;                          // matrix < 0: none
@@ -244,21 +245,19 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     j = t - i * (i + 1) / 2;
 }
-// a tile of a symmetric matrix and its mirror image; value(v, old) turns sums into what is held, old being what `from` (NULL: nothing) holds there
-template <class C, typename F>
-__device__ __forceinline__ void store_symmetric(f32x16 (&acc)[C::MT][C::NT], char* out, const char* from, int64_t np, int i, int j, unsigned char* smem, F value) {
-    const auto fetch = [&](int64_t m, int64_t n) { return from && m < np && n < np ? load_pairs(from + pairs_at(m * np + n)) : Pairs{}; };
-    const auto store = [&](int64_t m, int64_t n, float (&v)[8], const Pairs& old) {
-        if (m >= np || n >= np) return;
-        value(v, old);
-        store_pairs(out + pairs_at(m * np + n), v);
-    };
-    C::rows(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
-    if (i != j) C::columns(acc, (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
+// eight values of A, and of C = b I + c A; row m from column n on (a multiple of eight)
+__device__ __forceinline__ void store_gram(char* a, char* c, int64_t np, int64_t m, int64_t n, const float (&v)[8], const StepArgs& p) {
+    if (m >= np || n >= np) return;
+    const int64_t at = pairs_at(m * np + n);
+    store_pairs(a + at, v);
+    float w[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) w[q] = p.c * v[q] + (n + q == m ? p.b * kScale : 0.f);
+    store_pairs(c + at, w);
 }
 
 // A.  SPLIT: sums over a part of k each, for k_ns_join
-template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_gram(Table t, char* ws, int which, float* parts) {
+template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_gram(Table t, char* ws, int which, StepArgs a, float* parts) {
     typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
@@ -276,52 +275,56 @@ template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 
     if constexpr (SPLIT) {
         float* out = parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kTile * kTile;
         Straight::rows(acc[0], 0, 0, smem, Straight::none, [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) { tile::store8(out + m * kTile + n, v); });
-    } else
-        store_symmetric<Straight>(acc[0], ws + x.a(0), (const char*)nullptr, x.np(), i, j, smem, [&](float (&v)[8], const Pairs&) {
+    } else {
+        const auto store = [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
-        });
+            store_gram(ws + x.a(0), ws + x.a(2), x.np(), m, n, v, a);
+        };
+        Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
+        if (i != j) Straight::columns(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
+    }
 }
 
-// A of its parts, added up in their order
-__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float* parts, int splits) {
-    constexpr int kPitch = kTile + 1;
-    __shared__ float tile_[kTile * kPitch];
+// A and C of A's parts, added up in their order; a block has 32 rows of a tile
+__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, const float* parts, int splits) {
+    constexpr int kBand = 32, kPitch = kBand + 1;
+    __shared__ float band[kTile * kPitch];
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
-    const int64_t np = x.np();
-    char* out = ws + x.a(0);
-    for (int u = threadIdx.x; u < kTile * kTile / 8; u += 256) {
+    const int64_t np = x.np(), m0 = (int64_t)i * kTile + blockIdx.y * kBand, n0 = (int64_t)j * kTile;
+    char *ca = ws + x.a(0), *cc = ws + x.a(2);
+    const int64_t next = (int64_t)gridDim.x * kTile * kTile;
+    const float* from = parts + ((int64_t)blockIdx.x * kTile + blockIdx.y * kBand) * kTile;
+    for (int u = threadIdx.x; u < kBand * kTile / 8; u += 256) {
         const int r = u / (kTile / 8), c = u % (kTile / 8) * 8;
-        float v[8], more[8];
-        tile::load8(parts + (int64_t)blockIdx.x * kTile * kTile + u * 8, v);
-        for (int s = 1; s < splits; ++s) {
-            tile::load8(parts + ((int64_t)s * gridDim.x + blockIdx.x) * kTile * kTile + u * 8, more);
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, more[8];
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            tile::load8(from + s * next + u * 8, more);
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] += more[q];
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q) tile_[r * kPitch + c + q] = v[q] *= kUnscale;
-        const int64_t m = (int64_t)i * kTile + r, n = (int64_t)j * kTile + c;
-        if (m < np && n < np) store_pairs(out + pairs_at(m * np + n), v);
+        for (int q = 0; q < 8; ++q) band[(c + q) * kPitch + r] = v[q] *= kUnscale;
+        store_gram(ca, cc, np, m0 + r, n0 + c, v, a);
     }
     if (i == j) return;
-    __syncthreads();
-    for (int u = threadIdx.x; u < kTile * kTile / 8; u += 256) {
-        const int r = u / (kTile / 8), c = u % (kTile / 8) * 8;
+    tile::barrier();
+    for (int u = threadIdx.x; u < kTile * kBand / 8; u += 256) {
+        const int r = u / (kBand / 8), c = u % (kBand / 8) * 8;
         float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = tile_[(c + q) * kPitch + r];
-        const int64_t m = (int64_t)j * kTile + r, n = (int64_t)i * kTile + c;
-        if (m < np && n < np) store_pairs(out + pairs_at(m * np + n), v);
+        for (int q = 0; q < 8; ++q) v[q] = band[r * kPitch + c + q];
+        store_gram(ca, cc, np, n0 + r, m0 + c, v, a);
     }
 }
 
-// B = b A + c A^2
-template <int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_poly(Table t, char* ws, float b, float c) {
+// B = a I + A C
+template <int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_poly(Table t, char* ws, StepArgs a) {
     typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
@@ -329,15 +332,20 @@ template <int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) voi
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
-    const Operand o = operand_a(x, ws, 0);
+    const Operand oa = operand_a(x, ws, 0), oc = operand_a(x, ws, 2);
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     const int64_t np = x.np();
-    Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
-    store_symmetric<Straight>(acc[0], ws + x.a(1), ws + x.a(0), np, i, j, smem, [&](float (&v)[8], const Pairs& was) {
+    Straight::run(acc, &oa, &oc, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
+    char* out = ws + x.a(1);
+    const auto store = [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
+        if (m >= np || n >= np) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = b * value_of(was, q) + (c * kUnscale) * v[q];
-    });
+        for (int q = 0; q < 8; ++q) v[q] = kUnscale * v[q] + (n + q == m ? a.a * kScale : 0.f);
+        store_pairs(out + pairs_at(m * np + n), v);
+    };
+    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
+    if (i != j) Straight::columns(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
 }
 
 enum Last { kMore = 0, kOut = 1, kWeights = 2 };
@@ -360,7 +368,7 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
         tile::store_some(p, left, w);
     }
 }
-// X = a X + B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights
+// X = B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights
 template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
     typedef typename Cores<STAGES>::Straight Straight;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -379,14 +387,12 @@ template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, ST
     Straight::clear(acc);
     if (x.tall()) Straight::run(acc, &ox, &ob, (int64_t)i * kTile, (int64_t)j * kTile, 0, cp, smem);
     else Cores<STAGES>::Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
-    const char* from = ws + x.x(which);
     char* to = ws + x.x(which ^ 1);
     const float size = size_of(x, a);
-    const auto fetch = [&](int64_t m, int64_t n) { return m < rp && n < cp ? load_pairs(from + pairs_at(m * cp + n)) : Pairs{}; };
-    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, [&](int64_t m, int64_t n, float (&v)[8], const Pairs& was) {
+    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
         if (m >= rp || n >= cp) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = a.a * value_of(was, q) + kUnscale * v[q];
+        for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
         if constexpr (LAST == kMore) store_pairs(to + pairs_at(m * cp + n), v);
         else {
             const int left = x.cols - (int)n;
@@ -652,13 +658,13 @@ template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, 
     for (int s = 0; s < steps && st == FF_OK; ++s) {
         const int which = s & 1;
         if (t.splits > 1) {
-            st = go<k_ns_gram<kShallow, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, shallow, stream, what, t.tri, ws, which, t.parts);
-            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, t.tris, 256, 0, stream, what, t.tri, ws, (const float*)t.parts, t.splits);
-        } else if (t.tris > 256) st = go<k_ns_gram<kShallow, false>>(KK_NS_GRAM, t.tris, 256, shallow, stream, what, t.tri, ws, which, (float*)nullptr);
-        else st = go<k_ns_gram<kDeep, false>>(KK_NS_GRAM, t.tris, 256, deep, stream, what, t.tri, ws, which, (float*)nullptr);
+            st = go<k_ns_gram<kShallow, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, shallow, stream, what, t.tri, ws, which, a, t.parts);
+            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, kTile / 32), 256, 0, stream, what, t.tri, ws, a, (const float*)t.parts, t.splits);
+        } else if (t.tris > 256) st = go<k_ns_gram<kShallow, false>>(KK_NS_GRAM, t.tris, 256, shallow, stream, what, t.tri, ws, which, a, (float*)nullptr);
+        else st = go<k_ns_gram<kDeep, false>>(KK_NS_GRAM, t.tris, 256, deep, stream, what, t.tri, ws, which, a, (float*)nullptr);
         if (st != FF_OK) return st;
-        if (t.tris > 256) st = go<k_ns_poly<kShallow>>(KK_NS_POLY, t.tris, 256, shallow, stream, what, t.tri, ws, a.b, a.c);
-        else st = go<k_ns_poly<kDeep>>(KK_NS_POLY, t.tris, 256, deep, stream, what, t.tri, ws, a.b, a.c);
+        if (t.tris > 256) st = go<k_ns_poly<kShallow>>(KK_NS_POLY, t.tris, 256, shallow, stream, what, t.tri, ws, a);
+        else st = go<k_ns_poly<kDeep>>(KK_NS_POLY, t.tris, 256, deep, stream, what, t.tri, ws, a);
         if (st != FF_OK) return st;
         st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream, what) : apply<LAST, P>(t, which, a, norm, ws, stream, what);
     }

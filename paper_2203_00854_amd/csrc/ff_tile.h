@@ -98,6 +98,10 @@ struct Pair {
     }
 };
 
+// All wavefronts of a block have written to LDS what they were to write, and read what they were to read.  (__syncthreads() also waits for stores to memory to be
+// acknowledged: one to two microseconds at every turn of a tile's end.)
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // One operand in memory.  Not turned: row m at p + m pitch, `rows` of them, `bytes` of each may be read (all of its k, padded with zeros to a
 // multiple of kStep).  Turned: row k at p + k pitch, `rows` of them (all k, likewise), `bytes` of each (all m).  Bytes are a multiple of 16, p and pitch
 // 16-byte aligned.  What lies past an end is read from the last row or the last sixteen bytes: a caller stores no m or n that is not there.
@@ -303,7 +307,7 @@ struct Core {
             multiply(acc, f[0]);
             if (s + 1 < rest) read(f[0], smem + buf * kStage, wm, wn, s + 1, lane);
         }
-        __syncthreads();
+        barrier();
     }
     // waits until all but the loads of the youngest N stages have arrived, for every wavefront, and for its own reads
     template <int N> static __device__ __forceinline__ void arrive() {
@@ -369,7 +373,7 @@ struct Core {
                 const int u = (t0 + t) * kThreads + (int)threadIdx.x, r = u / (C / 8);
                 old[t] = fetch(r0 + r / 32 * APART + r % 32, c0 + u % (C / 8) * 8);
             }
-            if (t0 == 0) __syncthreads();
+            if (t0 == 0) barrier();
 #pragma unroll
             for (int t = 0; t < kGroup; ++t) {
                 const int u = (t0 + t) * kThreads + (int)threadIdx.x, r = u / (C / 8), c = u % (C / 8) * 8;
@@ -378,7 +382,7 @@ struct Core {
                 body(r0 + r / 32 * APART + r % 32, c0 + c, v, old[t]);
             }
         }
-        __syncthreads();
+        barrier();
     }
     struct Nothing {};
     static __device__ __forceinline__ Nothing none(int64_t, int64_t) { return {}; }
