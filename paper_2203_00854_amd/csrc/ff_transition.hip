@@ -257,10 +257,107 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
         });
 }
 
+// The same with rows in registers (bfloat16, up to 256 channels), and dx with them: a^T, b^T and dh^T = Wo^T dy^T of 32 hidden channels leave a lane with sixteen neighbours
+// of each, from which da, db and h are stored and dx^T += Wa^T da^T + Wb^T db^T goes on.  The weights' other sides are read turned from the same stage.
+struct GradRowsArgs {
+    const bf16_t *x, *dy;
+    const char *w_a, *w_b, *w_o;
+    const float* mask;
+    bf16_t *da, *db, *h, *dx;
+    bf16_t *x_copy, *dy_copy;     // NULL, or [rows_out][32 KC]: rows and channels that are none are zeros there
+    int64_t rows, rows_out;
+    int32_t f, c, pitch_o;        // as in RowsArgs
+    int32_t whole;
+};
+template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) void k_tr_grad_rows(GradRowsArgs a) {
+    typedef rows::Weights<KC, 4> W;
+    extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    W::load(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
+    const int64_t row = (int64_t)blockIdx.x * 128 + wave * 32 + (lane & 31);
+    const bool live = row < a.rows && !(a.mask && a.mask[row] == 0.f), held = row < a.rows_out;
+    uint4 x[2 * KC], dy[2 * KC];
+    rows::load_row<KC>(x, a.x, row, live, a.c, a.whole, lane);
+    rows::load_row<KC>(dy, a.dy, row, live, a.c, a.whole, lane);
+    if (a.x_copy && held) {
+        const int64_t at = row * (32 * KC) + 8 * hf;
+#pragma unroll
+        for (int s = 0; s < 2 * KC; ++s) {
+            *(uint4*)(a.x_copy + at + 16 * s) = x[s];
+            *(uint4*)(a.dy_copy + at + 16 * s) = dy[s];
+        }
+    }
+    f32x16 dx[KC];
+#pragma unroll
+    for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dx[i][v] = 0.f;
+    int buf = 0;
+    for (int f0 = 0; f0 < a.f; f0 += 32, buf ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        tile::barrier();                                       // the stage is there, and nobody reads the other one any more
+        if (f0 + 32 < a.f) W::load(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
+        const unsigned char* part = smem + buf * W::kStage;
+        f32x16 p, q, r;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) p[v] = q[v] = r[v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2 * KC; ++s) {
+            p = rows::mma(W::in(part, s, lane), x[s], p);
+            q = rows::mma(W::in(part + W::kIn, s, lane), x[s], q);
+            r = rows::mma(W::out_turned(part + 2 * W::kIn, s, lane), dy[s], r);
+        }
+        uint32_t da[8], db[8], h[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            float w[3][2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float slope;
+                const float gate = gate_of<ACT, true>(p[2 * v + e], slope);
+                w[0][e] = r[2 * v + e] * q[2 * v + e] * slope;
+                w[1][e] = r[2 * v + e] * gate;
+                w[2][e] = gate * q[2 * v + e];
+            }
+            da[v] = tile::pack2(w[0][0], w[0][1]);
+            db[v] = tile::pack2(w[1][0], w[1][1]);
+            h[v] = tile::pack2(w[2][0], w[2][1]);
+        }
+        if (held) {
+            const int64_t at = row * a.f + f0 + 16 * hf;
+            rows::store16(a.da + at, da);
+            rows::store16(a.db + at, db);
+            rows::store16(a.h + at, h);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < KC; ++i) {
+                dx[i] = rows::mma(W::in_turned(part, i, t, lane), make_uint4(da[4 * t], da[4 * t + 1], da[4 * t + 2], da[4 * t + 3]), dx[i]);
+                dx[i] = rows::mma(W::in_turned(part + W::kIn, i, t, lane), make_uint4(db[4 * t], db[4 * t + 1], db[4 * t + 2], db[4 * t + 3]), dx[i]);
+            }
+    }
+    if (row >= a.rows) return;
+    const int64_t at = row * a.c + 16 * hf;
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+        if (a.whole) {
+            uint32_t w[8];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) w[v] = tile::pack2(dx[i][2 * v], dx[i][2 * v + 1]);
+            rows::store16(a.dx + at + 32 * i, w);
+        } else
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (32 * i + 16 * hf + e < a.c) a.dx[at + 32 * i + e] = f32_to_bf16(dx[i][e]);
+    }
+}
+
 // ---- gradients of the weights ------------------------------------------------------------------
 struct WeightArgs {
-    Operand a[3], b[3];           // da, db, dy; x, x, h
-    float* partial;               // [splits][3][fp cp]
+    Operand a[3], b[3];           // da, db, h; x, x, dy
+    float* partial;               // [splits][3][fp][cp]; the last is that of Wo turned
     int64_t rows;                 // padded to kPad
     int64_t per_split;            // rows of a split
     int32_t fp, cp;
@@ -268,17 +365,16 @@ struct WeightArgs {
     int32_t add;                  // to what an earlier chunk left
 };
 // Sums over rows: both operands lie with the rows as k.  The rows are split over blocks, whose sums are joined in a fixed order.
-template <class C> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_weights(WeightArgs a) {
+template <class C> __global__ __launch_bounds__(C::kThreads) void k_tr_weights(WeightArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const uint32_t tiles = a.ftiles * a.ctiles, which = blockIdx.x / tiles, t = blockIdx.x % tiles;
-    const bool last = which == 2;
-    const int64_t m0 = (int64_t)(last ? t % a.ctiles : t / a.ctiles) * C::BM, n0 = (int64_t)(last ? t / a.ctiles : t % a.ctiles) * C::BN;
+    const int64_t m0 = (int64_t)(t / a.ctiles) * C::BM, n0 = (int64_t)(t % a.ctiles) * C::BN;
     const int64_t from = blockIdx.y * a.per_split, to = from + a.per_split < a.rows ? from + a.per_split : a.rows;
     f32x16 acc[1][C::MT][C::NT];
     C::clear(acc);
     C::run(acc, a.a + which, a.b + which, m0, n0, from, to, smem);
     float* out = a.partial + ((int64_t)blockIdx.y * 3 + which) * a.fp * a.cp;
-    const int32_t rows = last ? a.cp : a.fp, cols = last ? a.fp : a.cp;
+    const int32_t rows = a.fp, cols = a.cp;
     const auto fetch = [&](int64_t m, int64_t n) {
         Eight e;
 #pragma unroll
@@ -299,16 +395,44 @@ struct JoinArgs {
     void* dw[3];
     int32_t f, c, fp, cp, splits, accumulate;
 };
+// The gradients of a 32 x 32 part of the weights, their parts added up in order; that of Wo is turned in LDS.
 template <typename G> __global__ __launch_bounds__(256) void k_tr_join(JoinArgs a) {
-    const int which = blockIdx.y;
-    const int32_t rows = which == 2 ? a.c : a.f, cols = which == 2 ? a.f : a.c, pitch = which == 2 ? a.fp : a.cp;
-    const int64_t size = (int64_t)a.fp * a.cp, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)rows * cols) return;
-    const int64_t at = which * size + i / cols * pitch + i % cols;
-    float sum = a.splits > 0 ? a.partial[at] : 0.f;
-    for (int s = 1; s < a.splits; ++s) sum += a.partial[s * 3 * size + at];
-    G* out = (G*)a.dw[which] + i;
-    *out = from_f32<G>(a.accumulate ? to_f32<G>(*out) + sum : sum);
+    __shared__ float turned[32][33];
+    const int which = blockIdx.z;
+    const int64_t size = (int64_t)a.fp * a.cp;
+    const int f0 = blockIdx.y * 32, c0 = blockIdx.x * 32, lane = threadIdx.x & 31;
+    G* const out = (G*)a.dw[which];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int f = f0 + ((int)threadIdx.x >> 5) + 8 * k, c = c0 + lane;
+        const bool there = f < a.f && c < a.c;
+        float sum = 0.f;
+        const float* p = a.partial + which * size + (int64_t)f * a.cp + c;
+        if (there)
+#pragma unroll 4
+            for (int s = 0; s < a.splits; ++s) sum += p[s * 3 * size];
+        if (which == 2) turned[(threadIdx.x >> 5) + 8 * k][lane] = sum;
+        else if (there) {
+            G* o = out + (int64_t)f * a.c + c;
+            *o = from_f32<G>(a.accumulate ? to_f32<G>(*o) + sum : sum);
+        }
+    }
+    if (which != 2) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int c = c0 + ((int)threadIdx.x >> 5) + 8 * k, f = f0 + lane;
+        if (f >= a.f || c >= a.c) continue;
+        const float sum = turned[lane][(threadIdx.x >> 5) + 8 * k];
+        G* o = out + (int64_t)c * a.f + f;
+        *o = from_f32<G>(a.accumulate ? to_f32<G>(*o) + sum : sum);
+    }
+}
+
+// channels / 32 that the kernels with rows in registers are built for: the next one that holds c (0: none)
+int rows_tiles(const ff_transition_desc& d) {
+    const int need = (d.c + 31) / 32;
+    return d.dtype != FF_BF16 || need > 8 ? 0 : need == 1 ? 1 : (need + 1) / 2 * 2;
 }
 
 // ---- the calls -------------------------------------------------------------------------------
@@ -318,6 +442,7 @@ struct Sizes {
     int64_t chunks;
     size_t weight;                 // bytes of a packed weight
     size_t tokens, hidden;         // bytes of a chunk's packed x and of its hidden tensor
+    bool wide;                     // tiles of 256 in the weights' gradients
     int splits;
     int64_t per_split;
     size_t partial;
@@ -325,17 +450,20 @@ struct Sizes {
 Sizes sizes_of(const ff_transition_desc& d) {
     Sizes s;
     s.esz = d.dtype == FF_F32 ? 4 : 2;
-    s.cp = round_up(d.c, kPad);
-    s.fp = round_up(d.f, kPad);
+    const int kc = rows_tiles(d);
+    s.cp = kc ? kc * 32 : round_up(d.c, kPad);
+    s.fp = round_up(d.f, kc ? 32 : kPad);
     const int64_t most = std::max<int64_t>(128, kHiddenBytes / (s.fp * s.esz) / 128 * 128);
     s.chunk = std::min(most, round_up(std::max<int64_t>(d.rows, 1), 128));
     s.chunks = (d.rows + s.chunk - 1) / s.chunk;
     s.weight = align256((size_t)s.fp * s.cp * s.esz);
     s.tokens = align256((size_t)s.chunk * s.cp * s.esz);
     s.hidden = align256((size_t)s.chunk * s.fp * s.esz);
-    // as many splits of the rows as give two blocks for each of 256 compute units, of 256 rows at least
-    const int64_t tiles = 3 * ((d.f + 127) / 128) * ((d.c + 127) / 128);
-    const int64_t want = std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, s.chunk / 256));
+    // as many splits of the rows as give a block (of small tiles two) for each of 256 compute units, of 256 rows at least
+    s.wide = d.dtype == FF_BF16 && d.f >= 256;
+    const int bm = s.wide ? 256 : 128, bn = s.wide && d.c > 128 ? 256 : 128, blocks = s.wide ? 256 : 512;
+    const int64_t tiles = 3 * ((d.f + bm - 1) / bm) * ((d.c + bn - 1) / bn);
+    const int64_t want = std::max<int64_t>(1, std::min(blocks / tiles, s.chunk / 256));
     s.per_split = round_up((s.chunk + want - 1) / want, 128);
     s.splits = (int)((s.chunk + s.per_split - 1) / s.per_split);
     s.partial = align256((size_t)s.splits * 3 * s.fp * s.cp * 4);
@@ -380,7 +508,7 @@ template <typename T> Weights weights_of(const ff_transition_desc& d, const Size
     Weights w{};
     char* copies = ws;
     ws += 3 * s.weight;
-    const bool as_is = d.c % kPad == 0 && d.f % kPad == 0 && aligned(w_a) && aligned(w_b) && aligned(w_o);
+    const bool as_is = d.c == s.cp && d.f == s.fp && aligned(w_a) && aligned(w_b) && aligned(w_o);
     const void* from[3] = {w_a, w_b, w_o};
     if (!as_is) {
         PackJob jobs[3];
@@ -398,12 +526,6 @@ template <typename T> Weights weights_of(const ff_transition_desc& d, const Size
 }
 
 constexpr int bk_of(int esz) { return 64 / esz; }              // of a row, 64 bytes a stage
-
-// channels / 32 that the kernels with rows in registers are built for: the next one that holds c (0: none)
-int rows_tiles(const ff_transition_desc& d) {
-    const int need = (d.c + 31) / 32;
-    return d.dtype != FF_BF16 || need > 8 ? 0 : need == 1 ? 1 : (need + 1) / 2 * 2;
-}
 
 template <int KC> ff_status launch_rows(int act, const RowsArgs& a, hipStream_t stream) {
     typedef rows::Weights<KC, 4> W;
@@ -484,6 +606,26 @@ template <typename T> ff_status forward(const ff_transition_desc& d, const void*
     return FF_OK;
 }
 
+template <int KC> ff_status launch_grad_rows(int act, const GradRowsArgs& a, hipStream_t stream) {
+    typedef rows::Weights<KC, 4> W;
+    const dim3 grid((uint32_t)((a.rows_out + 127) / 128));
+    const char* what = "ff_gated_transition_backward";
+    return act == FF_SILU   ? launch<W, k_tr_grad_rows<KC, FF_SILU>>(KK_TR_GRAD, what, grid, a, stream)
+           : act == FF_GELU ? launch<W, k_tr_grad_rows<KC, FF_GELU>>(KK_TR_GRAD, what, grid, a, stream)
+                            : launch<W, k_tr_grad_rows<KC, FF_SIGMOID>>(KK_TR_GRAD, what, grid, a, stream);
+}
+
+// tiles of the weights' gradients where there are enough hidden channels
+template <typename T> struct Wide {
+    typedef Core<Bf16, 256, 256, 32, 4, 2, 4, 1, 1, true, 1u> Square;
+    typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 1, true, 1u> Tall;
+};
+template <class C> ff_status weights(WeightArgs a, int splits, hipStream_t stream) {
+    a.ftiles = (uint32_t)((a.fp + C::BM - 1) / C::BM);
+    a.ctiles = (uint32_t)((a.cp + C::BN - 1) / C::BN);
+    return launch<C, k_tr_weights<C>>(KK_TR_WEIGHTS, "ff_gated_transition_backward", dim3(3 * a.ftiles * a.ctiles, splits), a, stream);
+}
+
 template <typename T> ff_status backward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
                                          const float* mask, void* dx, void* const (&dw)[3], int grad_dtype, bool accumulate, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
@@ -499,34 +641,47 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
     ws += 2 * s.tokens;
     char* const hidden[3] = {ws, ws + s.hidden, ws + 2 * s.hidden};
     float* const partial = (float*)(ws + 3 * s.hidden);
-    const bool as_is = d.c % kPad == 0 && aligned(x) && aligned(dy) && !mask;
+    const int kc = rows_tiles(d);
+    const bool as_is = (kc ? d.c == s.cp : d.c % kPad == 0) && aligned(x) && aligned(dy);
+    const char* what = "ff_gated_transition_backward";
     ff_status st = FF_OK;
     for (int64_t r0 = 0; r0 < d.rows; r0 += s.chunk) {
         const int64_t rows = std::min(s.chunk, d.rows - r0), padded = round_up(rows, kPad);
         const void* in[2] = {(const T*)x + r0 * d.c, (const T*)dy + r0 * d.c};
-        if (!as_is) {
-            PackJob jobs[2];
-            for (int i = 0; i < 2; ++i) {
-                jobs[i] = pack_job(in[i], tokens[i], mask ? mask + r0 : nullptr, rows, rows, d.c, s.cp, s.esz);
-                in[i] = tokens[i];
+        const float* const live = mask ? mask + r0 : nullptr;
+        const bool copies = !as_is || mask;
+        if (kc) {
+            if constexpr (sizeof(T) == 2) {
+                const GradRowsArgs ga{(const bf16_t*)in[0], (const bf16_t*)in[1], (const char*)w.a.p, (const char*)w.b.p, (const char*)w.o.p, live, (bf16_t*)hidden[0], (bf16_t*)hidden[1],
+                                      (bf16_t*)hidden[2], (bf16_t*)dx + r0 * d.c, copies ? (bf16_t*)tokens[0] : nullptr, (bf16_t*)tokens[1], rows, padded, (int32_t)s.fp, d.c,
+                                      (int32_t)(s.fp * 2), as_is && aligned(dx)};
+                st = kc == 1 ? launch_grad_rows<1>(d.act, ga, stream) : kc == 2 ? launch_grad_rows<2>(d.act, ga, stream) : kc == 4 ? launch_grad_rows<4>(d.act, ga, stream)
+                     : kc == 6 ? launch_grad_rows<6>(d.act, ga, stream) : launch_grad_rows<8>(d.act, ga, stream);
             }
-            st = pack<T>(jobs, 2, stream);
-            if (st != FF_OK) return st;
+        } else {
+            if (copies) {
+                PackJob jobs[2];
+                for (int i = 0; i < 2; ++i) jobs[i] = pack_job(in[i], tokens[i], live, rows, rows, d.c, s.cp, s.esz);
+                st = pack<T>(jobs, 2, stream);
+                if (st != FF_OK) return st;
+            }
+            GradArgs ga{{operand(copies ? tokens[0] : in[0], s.cp, rows, s.cp, s.esz), operand(copies ? tokens[1] : in[1], s.cp, rows, s.cp, s.esz)}, {w.a, w.b, w.o}, hidden[0],
+                        hidden[1], hidden[2], rows, padded, d.f, (int32_t)s.cp, (int32_t)s.fp, (uint32_t)((padded + CG::BM - 1) / CG::BM), (uint32_t)((s.fp + CG::BN - 1) / CG::BN)};
+            const dim3 grid(ga.mtiles * ga.ntiles);
+            st = d.act == FF_SILU   ? launch<CG, k_tr_grad<CG, T, FF_SILU>>(KK_TR_GRAD, what, grid, ga, stream)
+                 : d.act == FF_GELU ? launch<CG, k_tr_grad<CG, T, FF_GELU>>(KK_TR_GRAD, what, grid, ga, stream)
+                                    : launch<CG, k_tr_grad<CG, T, FF_SIGMOID>>(KK_TR_GRAD, what, grid, ga, stream);
         }
-        const Operand ox = operand(in[0], s.cp, rows, s.cp, s.esz), ody = operand(in[1], s.cp, rows, s.cp, s.esz);
-        GradArgs ga{{ox, ody}, {w.a, w.b, w.o}, hidden[0], hidden[1], hidden[2], rows, padded, d.f, (int32_t)s.cp, (int32_t)s.fp,
-                    (uint32_t)((padded + CG::BM - 1) / CG::BM), (uint32_t)((s.fp + CG::BN - 1) / CG::BN)};
-        const dim3 grid(ga.mtiles * ga.ntiles);
-        st = d.act == FF_SILU   ? launch<CG, k_tr_grad<CG, T, FF_SILU>>(KK_TR_GRAD, "ff_gated_transition_backward", grid, ga, stream)
-             : d.act == FF_GELU ? launch<CG, k_tr_grad<CG, T, FF_GELU>>(KK_TR_GRAD, "ff_gated_transition_backward", grid, ga, stream)
-                                : launch<CG, k_tr_grad<CG, T, FF_SIGMOID>>(KK_TR_GRAD, "ff_gated_transition_backward", grid, ga, stream);
         if (st != FF_OK) return st;
+        const Operand ox = operand(copies ? tokens[0] : in[0], s.cp, rows, s.cp, s.esz), ody = operand(copies ? tokens[1] : in[1], s.cp, rows, s.cp, s.esz);
         Operand oh[3];
         for (int i = 0; i < 3; ++i) oh[i] = operand(hidden[i], s.fp, padded, s.fp, s.esz);
-        WeightArgs wa{{oh[0], oh[1], ody}, {ox, ox, oh[2]}, partial, padded, s.per_split, (int32_t)s.fp, (int32_t)s.cp,
-                      (uint32_t)((s.fp + 127) / 128), (uint32_t)((s.cp + 127) / 128), r0 > 0};
-        st = launch<CW, k_tr_weights<CW>>(KK_TR_WEIGHTS, "ff_gated_transition_backward", dim3(3 * wa.ftiles * wa.ctiles, s.splits), wa, stream);
-        if (st != FF_OK) return st;
+        WeightArgs wa{{oh[0], oh[1], oh[2]}, {ox, ox, ody}, partial, padded, s.per_split, (int32_t)s.fp, (int32_t)s.cp, 0, 0, r0 > 0};
+        st = s.wide ? d.c > 128 ? weights<typename Wide<T>::Square>(wa, s.splits, stream) : weights<typename Wide<T>::Tall>(wa, s.splits, stream) : weights<CW>(wa, s.splits, stream);
+        if (st != FF_OK || kc) {
+            if (st != FF_OK) return st;
+            continue;
+        }
         OutArgs oa{};
         oa.a[0] = oh[0];
         oa.a[1] = oh[1];
@@ -539,11 +694,11 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
         oa.out = (T*)dx + r0 * d.c;
         oa.mtiles = (uint32_t)((rows + CX::BM - 1) / CX::BM);
         oa.ntiles = (uint32_t)((d.c + CX::BN - 1) / CX::BN);
-        st = launch<CX, k_tr_out<CX, T>>(KK_TR_OUT, "ff_gated_transition_backward", dim3(oa.mtiles * oa.ntiles), oa, stream);
+        st = launch<CX, k_tr_out<CX, T>>(KK_TR_OUT, what, dim3(oa.mtiles * oa.ntiles), oa, stream);
         if (st != FF_OK) return st;
     }
     JoinArgs ja{partial, {dw[0], dw[1], dw[2]}, d.f, d.c, (int32_t)s.fp, (int32_t)s.cp, d.rows ? s.splits : 0, accumulate};
-    const dim3 grid((uint32_t)(((int64_t)d.f * d.c + 255) / 256), 3);
+    const dim3 grid((uint32_t)((d.c + 31) / 32), (uint32_t)((d.f + 31) / 32), 3);
     Timed t(KK_TR_JOIN, stream);
     if (grad_dtype == FF_F32) hipLaunchKernelGGL((k_tr_join<float>), grid, dim3(256), 0, stream, ja);
     else hipLaunchKernelGGL((k_tr_join<bf16_t>), grid, dim3(256), 0, stream, ja);

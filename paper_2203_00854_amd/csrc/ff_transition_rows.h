@@ -69,6 +69,25 @@ template <int KC, int WAVES> struct Weights {
         const int row = 32 * ct + (lane & 31);
         return *reinterpret_cast<const uint4*>(part + row * 64 + (slot_out(row, 2 * (lane >> 5) + t) << 4));
     }
+
+    // ---- turned: four rows of 64 contiguous bytes a read, their columns in the order of place(); of sixteen lanes, lane i asks for four columns of row i / 4
+    static __device__ __forceinline__ uint4 turned(const unsigned char* p0, const unsigned char* p1) {
+        const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)p0));
+        const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)p1));
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+    // hidden channels as rows (in the order of place()), channels 16 s + 8 half .. of Wo as k
+    static __device__ __forceinline__ uint4 out_turned(const unsigned char* part, int s, int lane) {
+        const int i = lane & 15, rb = (lane >> 2 & 4) + (i & 3), chunk = 2 * (rb & 1) + (rb >> 2), row = 32 * (s >> 1) + 16 * (lane >> 5) + 4 * (s & 1) + (i >> 2);
+        const unsigned char* p = part + (rb >> 1 & 1) * 8;
+        return turned(p + row * 64 + slot_out(row, chunk) * 16, p + (row + 8) * 64 + slot_out(row + 8, chunk) * 16);
+    }
+    // channels 32 ct .. of Wa or Wb as rows (in the order of place()), hidden channels 16 half + 8 t .. as k
+    static __device__ __forceinline__ uint4 in_turned(const unsigned char* part, int ct, int t, int lane) {
+        const int i = lane & 15, rb = (lane >> 2 & 4) + (i & 3), chunk = 4 * ct + 2 * (rb & 1) + (rb >> 2), row = 16 * t + 4 * (lane >> 5) + (i >> 2);
+        const unsigned char* p = part + (rb >> 1 & 1) * 8;
+        return turned(p + row * (W * 16) + slot_in(row, chunk) * 16, p + (row + 8) * (W * 16) + slot_in(row + 8, chunk) * 16);
+    }
 };
 
 // a row's sixteen channels 16 s + 8 half .. of x as right operands, zeros past the end and in rows that are none
@@ -86,6 +105,12 @@ template <int KC> __device__ __forceinline__ void load_row(uint4 (&v)[2 * KC], c
             v[s] = *reinterpret_cast<const uint4*>(e);
         }
     }
+}
+
+// sixteen neighbours, as bfloat16, from p on (sixteen-byte aligned)
+__device__ __forceinline__ void store16(bf16_t* p, const uint32_t (&w)[8]) {
+    *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+    *(uint4*)(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
 }  // namespace rows

@@ -63,7 +63,7 @@ class Problem:
             assert np.all(off <= e), f"{name}: {(off / e).max():.2f} of the bound at {np.unravel_index(np.argmax(off / e), off.shape)}"
 
 
-SIZES = [(1, 1, 1), (1, 16, 16), (3, 7, 5), (40, 64, 128), (129, 33, 70), (300, 96, 64), (257, 128, 512), (130, 256, 160), (200, 200, 312), (64, 520, 48), (300, 300, 96), (100, 32, 33), (161, 192, 256)]
+SIZES = [(1, 1, 1), (1, 16, 16), (3, 7, 5), (40, 64, 128), (129, 33, 70), (300, 96, 64), (257, 128, 512), (130, 256, 160), (200, 200, 312), (64, 520, 48), (300, 300, 96), (100, 32, 33), (161, 192, 256), (500, 256, 300), (400, 64, 288), (300, 512, 272)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
