@@ -223,9 +223,9 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
 
 // ---- the products --------------------------------------------------------------------------
 template <int STAGES> struct Cores {
-    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, false, 0u> Straight;      // rows by rows
-    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, true, 1u> Turned;         // columns by columns
-    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, false, 1u> Mixed;         // rows by columns
+    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, 0, 0u> Straight;      // rows by rows
+    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, 1, 1u> Turned;         // columns by columns
+    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;         // rows by columns
     static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 };
 // Three stages leave room for three blocks on a compute unit, whose ends then overlap with the others' products; eight for one, where a launch has fewer blocks than

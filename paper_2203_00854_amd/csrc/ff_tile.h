@@ -105,6 +105,9 @@ __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n
 // One operand in memory.  Not turned: row m at p + m pitch, `rows` of them, `bytes` of each may be read (all of its k, padded with zeros to a
 // multiple of kStep).  Turned: row k at p + k pitch, `rows` of them (all k, likewise), `bytes` of each (all m).  Bytes are a multiple of 16, p and pitch
 // 16-byte aligned.  What lies past an end is read from the last row or the last sixteen bytes: a caller stores no m or n that is not there.
+// Blocked (the A side, bfloat16): k in blocks of 32 rows, m in blocks of 32 columns of 2 KiB each, one beside the other: four groups of eight columns, in group g
+// sixteen bytes for each of 32 rows, row r at place r ^ 4 g.  A wavefront that has 32 rows stores a kilobyte at a time, a stage is copied as it lies, and the turned
+// reads find four rows of four groups in banks of their own.  pitch: bytes from 32 rows to the next; bytes: as much; rows: a multiple of 32.
 struct Operand {
     const void* p;
     int64_t pitch;        // bytes
@@ -112,12 +115,13 @@ struct Operand {
     int32_t bytes;
 };
 
-template <class Op_, int BM_, int BN_, int BK_, int STAGES_, int WM_, int WN_, int NA_, int NB_, bool TA_, unsigned TB_>
+template <class Op_, int BM_, int BN_, int BK_, int STAGES_, int WM_, int WN_, int NA_, int NB_, int TA_, unsigned TB_>
 struct Core {
     typedef Op_ Op;
     typedef typename Op::Frag Frag;
     static constexpr int BM = BM_, BN = BN_, BK = BK_, STAGES = STAGES_, WM = WM_, WN = WN_, NA = NA_, NB = NB_;
-    static constexpr bool TA = TA_;
+    static constexpr int TA = TA_;                                 // A is turned (1) or blocked (2)
+    static_assert(TA < 2 || (Op_::kStep == 16 && Op_::kPlanes == 1 && BK_ == 32), "blocks of 32 rows");
     static constexpr unsigned TB = TB_;                            // bit b: operand b of the B side is turned
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
@@ -129,7 +133,7 @@ struct Core {
 
     // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that what one cycle reads (256 bytes) lies in
     // banks of its own: sixteen bytes of sixteen rows, or, turned, of 32 columns' values in four rows (of a pair's, two pieces 64 bytes apart).
-    template <bool T, int W> static __device__ __forceinline__ int swizzle(int row) {
+    template <int T, int W> static __device__ __forceinline__ int swizzle(int row) {
         if constexpr (!T) return W >= 16 ? row & 15 : W == 8 ? row >> 1 & 7 : W == 4 ? row >> 2 & 3 : 0;
         else if constexpr (Op::kStep == 8) return row << 1 & 8;
         else if constexpr (Op::kPlanes == 2) return (row & 1) << 1 | (row & 2) << 2;
@@ -138,14 +142,17 @@ struct Core {
 
     // The loads of one operand's part of a stage.  A lane's address is min(x, limit) + y from a uniform base that moves with k: x, which alone can pass an end, and
     // y are the same for all stages.
-    template <bool T, int R> struct Loader {
+    template <int T, int R> struct Loader {
         static constexpr int W = (T ? R : BK) * Op::kSize / 16, LR = T ? BK : R, N = LR * W / kThreads;
         uint32_t x[N], y[N];
         __device__ __forceinline__ Loader(const Operand& o, int64_t r0) {
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const int u = j * kThreads + (int)threadIdx.x, row = u / W, chunk = ((u % W) ^ swizzle<T, W>(row)) * 16;
-                if constexpr (T) {
+                if constexpr (T == 2) {
+                    x[j] = (uint32_t)u * 16u;
+                    y[j] = 0;
+                } else if constexpr (T == 1) {
                     const int c = (int)r0 * Op::kSize + chunk, last = o.bytes - 16;
                     x[j] = (uint32_t)row * (uint32_t)o.pitch;
                     y[j] = (uint32_t)(c < last ? c : last);
@@ -158,19 +165,28 @@ struct Core {
         }
         __device__ __forceinline__ void issue(const Operand& o, int64_t r0, int64_t k0, unsigned lds) const {
             const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-            const char* base = (const char*)o.p + (T ? k0 * o.pitch : r0 * o.pitch + k0 * Op::kSize);
-            const uint32_t limit = T ? (uint32_t)((o.rows - k0 < LR ? o.rows - k0 : LR) - 1) * (uint32_t)o.pitch : (uint32_t)(o.bytes - 16 - (int)k0 * Op::kSize);
+            const char* base = (const char*)o.p + (T == 2 ? k0 / 32 * o.pitch + r0 * 64 : T ? k0 * o.pitch : r0 * o.pitch + k0 * Op::kSize);
+            const uint32_t limit = T == 2 ? (uint32_t)(o.bytes - (int)r0 * 64 - 16) : T ? (uint32_t)((o.rows - k0 < LR ? o.rows - k0 : LR) - 1) * (uint32_t)o.pitch : (uint32_t)(o.bytes - 16 - (int)k0 * Op::kSize);
 #pragma unroll
             for (int j = 0; j < N; ++j) load16_to_lds(base, (x[j] < limit ? x[j] : limit) + y[j], lds + (j * kThreads + wave * 64) * 16);
         }
     };
 
     // the lane's piece of plane p of 32 rows (from `row0`) in round s
-    template <bool T, int R>
+    template <int T, int R>
     static __device__ __forceinline__ uint4 piece(const unsigned char* image, int p, int row0, int s, int lane) {
         constexpr int W = (T ? R : BK) * Op::kSize / 16;
         const int hf = lane >> 5;
-        if constexpr (!T) {
+        if constexpr (T == 2) {
+            const int i = lane & 15, group = (row0 + (lane & 16)) / 8 + (i >> 1 & 1);
+            uint2 h[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int k = 16 * s + 8 * hf + 4 * t + (i >> 2);
+                h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(image + group * 512 + ((k ^ 4 * (group & 3)) << 4) + (i & 1) * 8)));
+            }
+            return make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+        } else if constexpr (!T) {
             const int row = row0 + (lane & 31), chunk = 2 * (Op::kPlanes * s + p) + hf;
             return *reinterpret_cast<const uint4*>(image + row * (W * 16) + ((chunk ^ swizzle<false, W>(row)) << 4));
         } else if constexpr (Op::kStep == 16) {
@@ -194,7 +210,7 @@ struct Core {
             return make_uint4(v[0], v[1], v[2], v[3]);
         }
     }
-    template <bool T, int R>
+    template <int T, int R>
     static __device__ __forceinline__ Frag frag(const unsigned char* image, int row0, int s, int lane) {
         Frag f;
 #pragma unroll

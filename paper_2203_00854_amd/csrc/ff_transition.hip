@@ -263,9 +263,10 @@ struct GradRowsArgs {
     const bf16_t *x, *dy;
     const char *w_a, *w_b, *w_o;
     const float* mask;
-    bf16_t *da, *db, *h, *dx;
+    char *da, *db, *h;            // blocked, 64 f bytes for each 32 rows
+    bf16_t* dx;
     bf16_t *x_copy, *dy_copy;     // NULL, or [rows_out][32 KC]: rows and channels that are none are zeros there
-    int64_t rows, rows_out;
+    int64_t rows, rows_out;       // rows_out: a multiple of 32
     int32_t f, c, pitch_o;        // as in RowsArgs
     int32_t whole;
 };
@@ -276,7 +277,8 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) vo
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
     W::load(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
     const int64_t row = (int64_t)blockIdx.x * 128 + wave * 32 + (lane & 31);
-    const bool live = row < a.rows && !(a.mask && a.mask[row] == 0.f), held = row < a.rows_out;
+    const bool live = row < a.rows && !(a.mask && a.mask[row] == 0.f);
+    const bool held = (int64_t)blockIdx.x * 128 + wave * 32 < a.rows_out;                // the wavefront's 32 rows have a place in da, db and h
     uint4 x[2 * KC], dy[2 * KC];
     rows::load_row<KC>(x, a.x, row, live, a.c, a.whole, lane);
     rows::load_row<KC>(dy, a.dy, row, live, a.c, a.whole, lane);
@@ -295,8 +297,11 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) vo
         for (int v = 0; v < 16; ++v) dx[i][v] = 0.f;
     int buf = 0;
     for (int f0 = 0; f0 < a.f; f0 += 32, buf ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        tile::barrier();                                       // the stage is there, and nobody reads the other one any more
+        // The stage is there, and nobody reads the other one any more.  Behind its loads a wavefront has issued the six stores of the turn before, which are not waited for
+        // (operations of this kind end in their order; a wavefront without a row that is held has issued none).
+        if (f0 > 0 && held) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        tile::barrier();
         if (f0 + 32 < a.f) W::load(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
         const unsigned char* part = smem + buf * W::kStage;
         f32x16 p, q, r;
@@ -325,10 +330,10 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) vo
             h[v] = tile::pack2(w[2][0], w[2][1]);
         }
         if (held) {
-            const int64_t at = row * a.f + f0 + 16 * hf;
-            rows::store16(a.da + at, da);
-            rows::store16(a.db + at, db);
-            rows::store16(a.h + at, h);
+            const int64_t at = (row >> 5) * a.f * 64 + f0 * 64;
+            rows::store_block(a.da + at, da, lane);
+            rows::store_block(a.db + at, db, lane);
+            rows::store_block(a.h + at, h, lane);
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -564,8 +569,8 @@ ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const
 template <typename T> ff_status forward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                         const float* mask, void* y, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
-    typedef Core<Op, 128, 64, bk_of(sizeof(T)), 4, 2, 2, 1, 2, false, 0u> CH;
-    typedef Core<Op, 128, 128, bk_of(sizeof(T)), 4, 2, 2, 1, 1, false, 0u> CO;
+    typedef Core<Op, 128, 64, bk_of(sizeof(T)), 4, 2, 2, 1, 2, 0, 0u> CH;
+    typedef Core<Op, 128, 128, bk_of(sizeof(T)), 4, 2, 2, 1, 1, 0, 0u> CO;
     const Sizes s = sizes_of(d);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
@@ -615,10 +620,15 @@ template <int KC> ff_status launch_grad_rows(int act, const GradRowsArgs& a, hip
                             : launch<W, k_tr_grad_rows<KC, FF_SIGMOID>>(KK_TR_GRAD, what, grid, a, stream);
 }
 
-// tiles of the weights' gradients where there are enough hidden channels
-template <typename T> struct Wide {
-    typedef Core<Bf16, 256, 256, 32, 4, 2, 4, 1, 1, true, 1u> Square;
-    typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 1, true, 1u> Tall;
+// tiles of the weights' gradients: wide ones where there are enough hidden channels
+struct Blocked {
+    typedef Core<Bf16, 256, 256, 32, 4, 2, 4, 1, 1, 2, 1u> Square;
+    typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 1, 2, 1u> Tall;
+    typedef Core<Bf16, 128, 128, 32, 4, 2, 2, 1, 1, 2, 1u> Small;
+};
+template <typename T> struct Turned {
+    typedef Core<typename OpOf<T>::type, 128, 128, 64 / sizeof(T), 4, 2, 2, 1, 1, 1, 1u> Small;
+    typedef Core<Bf16, 256, 256, 32, 4, 2, 4, 1, 1, 1, 1u> Square;
 };
 template <class C> ff_status weights(WeightArgs a, int splits, hipStream_t stream) {
     a.ftiles = (uint32_t)((a.fp + C::BM - 1) / C::BM);
@@ -630,9 +640,8 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
                                          const float* mask, void* dx, void* const (&dw)[3], int grad_dtype, bool accumulate, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
     constexpr int BK = bk_of(sizeof(T));
-    typedef Core<Op, 128, 64, BK, 3, 2, 2, 2, 3, false, 4u> CG;
-    typedef Core<Op, 128, 128, BK, 4, 2, 2, 1, 1, false, 1u> CX;
-    typedef Core<Op, 128, 128, BK, 4, 2, 2, 1, 1, true, 1u> CW;
+    typedef Core<Op, 128, 64, BK, 3, 2, 2, 2, 3, 0, 4u> CG;
+    typedef Core<Op, 128, 128, BK, 4, 2, 2, 1, 1, 0, 1u> CX;
     const Sizes s = sizes_of(d);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
@@ -646,14 +655,14 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
     const char* what = "ff_gated_transition_backward";
     ff_status st = FF_OK;
     for (int64_t r0 = 0; r0 < d.rows; r0 += s.chunk) {
-        const int64_t rows = std::min(s.chunk, d.rows - r0), padded = round_up(rows, kPad);
+        const int64_t rows = std::min(s.chunk, d.rows - r0), padded = round_up(rows, kc ? 32 : kPad);
         const void* in[2] = {(const T*)x + r0 * d.c, (const T*)dy + r0 * d.c};
         const float* const live = mask ? mask + r0 : nullptr;
         const bool copies = !as_is || mask;
         if (kc) {
             if constexpr (sizeof(T) == 2) {
-                const GradRowsArgs ga{(const bf16_t*)in[0], (const bf16_t*)in[1], (const char*)w.a.p, (const char*)w.b.p, (const char*)w.o.p, live, (bf16_t*)hidden[0], (bf16_t*)hidden[1],
-                                      (bf16_t*)hidden[2], (bf16_t*)dx + r0 * d.c, copies ? (bf16_t*)tokens[0] : nullptr, (bf16_t*)tokens[1], rows, padded, (int32_t)s.fp, d.c,
+                const GradRowsArgs ga{(const bf16_t*)in[0], (const bf16_t*)in[1], (const char*)w.a.p, (const char*)w.b.p, (const char*)w.o.p, live, hidden[0], hidden[1],
+                                      hidden[2], (bf16_t*)dx + r0 * d.c, copies ? (bf16_t*)tokens[0] : nullptr, (bf16_t*)tokens[1], rows, padded, (int32_t)s.fp, d.c,
                                       (int32_t)(s.fp * 2), as_is && aligned(dx)};
                 st = kc == 1 ? launch_grad_rows<1>(d.act, ga, stream) : kc == 2 ? launch_grad_rows<2>(d.act, ga, stream) : kc == 4 ? launch_grad_rows<4>(d.act, ga, stream)
                      : kc == 6 ? launch_grad_rows<6>(d.act, ga, stream) : launch_grad_rows<8>(d.act, ga, stream);
@@ -675,9 +684,10 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
         if (st != FF_OK) return st;
         const Operand ox = operand(copies ? tokens[0] : in[0], s.cp, rows, s.cp, s.esz), ody = operand(copies ? tokens[1] : in[1], s.cp, rows, s.cp, s.esz);
         Operand oh[3];
-        for (int i = 0; i < 3; ++i) oh[i] = operand(hidden[i], s.fp, padded, s.fp, s.esz);
+        for (int i = 0; i < 3; ++i) oh[i] = kc ? Operand{hidden[i], s.fp * 64, padded, (int32_t)(s.fp * 64)} : operand(hidden[i], s.fp, padded, s.fp, s.esz);
         WeightArgs wa{{oh[0], oh[1], oh[2]}, {ox, ox, ody}, partial, padded, s.per_split, (int32_t)s.fp, (int32_t)s.cp, 0, 0, r0 > 0};
-        st = s.wide ? d.c > 128 ? weights<typename Wide<T>::Square>(wa, s.splits, stream) : weights<typename Wide<T>::Tall>(wa, s.splits, stream) : weights<CW>(wa, s.splits, stream);
+        if (kc) st = s.wide ? d.c > 128 ? weights<Blocked::Square>(wa, s.splits, stream) : weights<Blocked::Tall>(wa, s.splits, stream) : weights<Blocked::Small>(wa, s.splits, stream);
+        else st = s.wide ? weights<typename Turned<T>::Square>(wa, s.splits, stream) : weights<typename Turned<T>::Small>(wa, s.splits, stream);
         if (st != FF_OK || kc) {
             if (st != FF_OK) return st;
             continue;

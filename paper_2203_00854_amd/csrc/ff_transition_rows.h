@@ -49,7 +49,7 @@ template <int KC, int WAVES> struct Weights {
         for (int j = 0; j < (3 * kPieces + WAVES - 1) / WAVES; ++j) {
             const int i = j * WAVES + wave;
             if (3 * kPieces % WAVES != 0 && i >= 3 * kPieces) break;
-            const int part = i / kPieces, u = i % kPieces * 64 + lane;
+            const int part = kPieces % WAVES == 0 ? j / (kPieces / WAVES) : i / kPieces, u = i % kPieces * 64 + lane;
             if (part < 2) {
                 const int row = u / W, chunk = slot_in(row, u % W);            // (an exclusive or is its own inverse)
                 load16_to_lds(part ? b : a, (uint32_t)(place(row) * (KC * 64) + chunk * 16), lds + i * 1024);
@@ -107,6 +107,12 @@ template <int KC> __device__ __forceinline__ void load_row(uint4 (&v)[2 * KC], c
     }
 }
 
+// A wavefront's 32 x 32 values (sixteen neighbours of a row a lane) as a block of tile::Operand's third kind
+__device__ __forceinline__ void store_block(char* p, const uint32_t (&w)[8], int lane) {
+    const int r = lane & 31, g = lane >> 5 << 1;
+    *(uint4*)(p + g * 512 + (r ^ 4 * g) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+    *(uint4*)(p + (g + 1) * 512 + (r ^ 4 * (g + 1)) * 16) = make_uint4(w[4], w[5], w[6], w[7]);
+}
 // sixteen neighbours, as bfloat16, from p on (sixteen-byte aligned)
 __device__ __forceinline__ void store16(bf16_t* p, const uint32_t (&w)[8]) {
     *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
