@@ -164,8 +164,10 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 3 : KC <=
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    W::load(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
+    const typename W::Loads loads(a.pitch_o);
+    loads.issue(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
     const int64_t row = (int64_t)blockIdx.x * 128 + wave * 32 + (lane & 31);
+    const typename W::Lane at(lane);
     const bool there = row < a.rows, live = there && !(a.mask && a.mask[row] == 0.f);
     uint4 x[2 * KC];
     rows::load_row<KC>(x, a.x, row, live, a.c, a.whole, lane);
@@ -178,26 +180,27 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 3 : KC <=
     for (int f0 = 0; f0 < a.f; f0 += 32, buf ^= 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();                                       // the stage is there, and nobody reads the other one any more
-        if (f0 + 32 < a.f) W::load(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
+        if (f0 + 32 < a.f) loads.issue(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
         const unsigned char* part = smem + buf * W::kStage;
         f32x16 p, q;
 #pragma unroll
         for (int v = 0; v < 16; ++v) p[v] = q[v] = 0.f;
-#pragma unroll
-        for (int s = 0; s < 2 * KC; ++s) {
-            p = rows::mma(W::in(part, s, lane), x[s], p);
-            q = rows::mma(W::in(part + W::kIn, s, lane), x[s], q);
-        }
+        rows::ahead<2 * KC, KC <= 4 ? 2 : 3>([&](int s) { return rows::Two{W::in(part, at, s), W::in(part + W::kIn, at, s)}; },
+                                [&](int s, const rows::Two& w) {
+                                    p = rows::mma(w.a, x[s], p);
+                                    q = rows::mma(w.b, x[s], q);
+                                });
         uint32_t h[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] = tile::pack2(gate_of<ACT, true>(p[2 * v]) * q[2 * v], gate_of<ACT, true>(p[2 * v + 1]) * q[2 * v + 1]);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < KC; ++i) y[i] = rows::mma(W::out(part + 2 * W::kIn, i, t, lane), make_uint4(h[4 * t], h[4 * t + 1], h[4 * t + 2], h[4 * t + 3]), y[i]);
+        rows::ahead<2 * KC, KC <= 4 ? 4 : 5>([&](int n) { return rows::One{W::out(part + 2 * W::kIn, at, n % KC, n / KC)}; },
+                                [&](int n, const rows::One& w) {
+                                    const int t = n / KC * 4;
+                                    y[n % KC] = rows::mma(w.a, make_uint4(h[t], h[t + 1], h[t + 2], h[t + 3]), y[n % KC]);
+                                });
     }
     if (!there) return;
-    const int64_t at = row * a.c + 16 * hf;
+    const int64_t to = row * a.c + 16 * hf;
 #pragma unroll
     for (int i = 0; i < KC; ++i) {
         if (a.whole) {
@@ -205,17 +208,17 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 3 : KC <=
             for (int u = 0; u < 2; ++u) {
                 float v[8];
                 uint4 r = make_uint4(0, 0, 0, 0);
-                if (a.residual) r = *reinterpret_cast<const uint4*>(a.residual + at + 32 * i + 8 * u);
+                if (a.residual) r = *reinterpret_cast<const uint4*>(a.residual + to + 32 * i + 8 * u);
                 const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = (live ? y[i][8 * u + e] : 0.f) + __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-                *reinterpret_cast<uint4*>(a.y + at + 32 * i + 8 * u) = make_uint4(tile::pack2(v[0], v[1]), tile::pack2(v[2], v[3]), tile::pack2(v[4], v[5]), tile::pack2(v[6], v[7]));
+                *reinterpret_cast<uint4*>(a.y + to + 32 * i + 8 * u) = make_uint4(tile::pack2(v[0], v[1]), tile::pack2(v[2], v[3]), tile::pack2(v[4], v[5]), tile::pack2(v[6], v[7]));
             }
         } else
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if (32 * i + 16 * hf + e < a.c)
-                    a.y[at + 32 * i + e] = f32_to_bf16((live ? y[i][e] : 0.f) + (a.residual ? bf16_to_f32(a.residual[at + 32 * i + e]) : 0.f));
+                    a.y[to + 32 * i + e] = f32_to_bf16((live ? y[i][e] : 0.f) + (a.residual ? bf16_to_f32(a.residual[to + 32 * i + e]) : 0.f));
     }
 }
 
@@ -275,9 +278,11 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) vo
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    W::load(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
+    const typename W::Loads loads(a.pitch_o);
+    loads.issue(a.w_a, a.w_b, a.w_o, 0, a.pitch_o, lds);
     const int64_t row = (int64_t)blockIdx.x * 128 + wave * 32 + (lane & 31);
     const bool live = row < a.rows && !(a.mask && a.mask[row] == 0.f);
+    const typename W::Lane place(lane);
     const bool held = (int64_t)blockIdx.x * 128 + wave * 32 < a.rows_out;                // the wavefront's 32 rows have a place in da, db and h
     uint4 x[2 * KC], dy[2 * KC];
     rows::load_row<KC>(x, a.x, row, live, a.c, a.whole, lane);
@@ -302,17 +307,17 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) vo
         if (f0 > 0 && held) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         tile::barrier();
-        if (f0 + 32 < a.f) W::load(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
+        if (f0 + 32 < a.f) loads.issue(a.w_a, a.w_b, a.w_o, f0 + 32, a.pitch_o, lds + (buf ^ 1) * W::kStage);
         const unsigned char* part = smem + buf * W::kStage;
         f32x16 p, q, r;
 #pragma unroll
         for (int v = 0; v < 16; ++v) p[v] = q[v] = r[v] = 0.f;
-#pragma unroll
-        for (int s = 0; s < 2 * KC; ++s) {
-            p = rows::mma(W::in(part, s, lane), x[s], p);
-            q = rows::mma(W::in(part + W::kIn, s, lane), x[s], q);
-            r = rows::mma(W::out_turned(part + 2 * W::kIn, s, lane), dy[s], r);
-        }
+        rows::ahead<2 * KC, 2>([&](int s) { return rows::Three{W::in(part, place, s), W::in(part + W::kIn, place, s), W::out_turned(part + 2 * W::kIn, place, s)}; },
+                               [&](int s, const rows::Three& w) {
+                                   p = rows::mma(w.a, x[s], p);
+                                   q = rows::mma(w.b, x[s], q);
+                                   r = rows::mma(w.c, dy[s], r);
+                               });
         uint32_t da[8], db[8], h[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
@@ -335,13 +340,12 @@ template <int KC, int ACT> __global__ __launch_bounds__(256, KC <= 4 ? 2 : 1) vo
             rows::store_block(a.db + at, db, lane);
             rows::store_block(a.h + at, h, lane);
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < KC; ++i) {
-                dx[i] = rows::mma(W::in_turned(part, i, t, lane), make_uint4(da[4 * t], da[4 * t + 1], da[4 * t + 2], da[4 * t + 3]), dx[i]);
-                dx[i] = rows::mma(W::in_turned(part + W::kIn, i, t, lane), make_uint4(db[4 * t], db[4 * t + 1], db[4 * t + 2], db[4 * t + 3]), dx[i]);
-            }
+        // (channels change faster than the four parts of k: an accumulator rests between two of its own)
+        rows::ahead<4 * KC, 4>([&](int n) { return rows::One{W::in_turned(n / KC & 1 ? part + W::kIn : part, place, n % KC, n / KC >> 1)}; },
+                               [&](int n, const rows::One& w) {
+                                   const int t = (n / KC >> 1) * 4;
+                                   dx[n % KC] = rows::mma(w.a, n / KC & 1 ? make_uint4(db[t], db[t + 1], db[t + 2], db[t + 3]) : make_uint4(da[t], da[t + 1], da[t + 2], da[t + 3]), dx[n % KC]);
+                               });
     }
     if (row >= a.rows) return;
     const int64_t at = row * a.c + 16 * hf;

@@ -40,55 +40,91 @@ template <int KC, int WAVES> struct Weights {
     }
     static __device__ __forceinline__ int slot_out(int row, int chunk) { return chunk ^ (row >> 2 & 3); }
 
-    // hidden channels f0 .. f0 + 31; pitches in bytes
-    static __device__ __forceinline__ void load(const char* wa, const char* wb, const char* wo, int64_t f0, int pitch_o, unsigned lds) {
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        const char *a = wa + f0 * (KC * 64), *b = wb + f0 * (KC * 64), *o = wo + f0 * 2;
-        constexpr int kPieces = kIn / 1024;                       // wavefront-wide loads of a part (kIn == kOut)
+    // The loads of a stage.  Wa's and Wb's (Wo's) part is kPieces wavefront-wide loads, dealt to the wavefronts in turn; a lane's addresses relative to the stage's start
+    // are the same for all stages, and with rows of 256 bytes those of a wavefront's loads differ by whole rows alone.
+    static constexpr int kPieces = kIn / 1024, kEach = (kPieces + WAVES - 1) / WAVES, kKept = W == 16 ? 1 : kEach;
+    struct Loads {
+        uint32_t in[kKept], out[kKept];
+        __device__ __forceinline__ explicit Loads(int pitch_o) {
+            const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
 #pragma unroll
-        for (int j = 0; j < (3 * kPieces + WAVES - 1) / WAVES; ++j) {
-            const int i = j * WAVES + wave;
-            if (3 * kPieces % WAVES != 0 && i >= 3 * kPieces) break;
-            const int part = kPieces % WAVES == 0 ? j / (kPieces / WAVES) : i / kPieces, u = i % kPieces * 64 + lane;
-            if (part < 2) {
-                const int row = u / W, chunk = slot_in(row, u % W);            // (an exclusive or is its own inverse)
-                load16_to_lds(part ? b : a, (uint32_t)(place(row) * (KC * 64) + chunk * 16), lds + i * 1024);
-            } else {
-                const int row = u / 4, chunk = slot_out(row, u % 4);
-                load16_to_lds(o, (uint32_t)(((row & ~31) + place(row & 31)) * pitch_o + chunk * 16), lds + i * 1024);
+            for (int j = 0; j < kKept; ++j) {
+                const int u = (j * WAVES + wave) * 64 + lane, r = u / W, o = u / 4;
+                in[j] = (uint32_t)(place(r) * (KC * 64) + slot_in(r, u % W) * 16);           // (an exclusive or is its own inverse)
+                out[j] = (uint32_t)(((o & ~31) + place(o & 31)) * pitch_o + slot_out(o, u % 4) * 16);
             }
         }
-    }
+        // hidden channels f0 .. f0 + 31; pitch in bytes
+        __device__ __forceinline__ void issue(const char* wa, const char* wb, const char* wo, int64_t f0, int pitch_o, unsigned lds) const {
+            const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+            const char *a = wa + f0 * (KC * 64), *b = wb + f0 * (KC * 64), *o = wo + f0 * 2;
+            static_assert(W != 16 || WAVES == 4, "four wavefronts' loads are sixteen rows of Wa: place() of the next sixteen is eight further; of Wo 64 rows");
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (kPieces % WAVES != 0 && j * WAVES + wave >= kPieces) break;
+                const int kept = j < kKept ? j : 0, more = j - kept;
+                const unsigned to = lds + (j * WAVES + wave) * 1024;
+                load16_to_lds(a + more * 8 * (KC * 64), in[kept], to);
+                load16_to_lds(b + more * 8 * (KC * 64), in[kept], to + kIn);
+                load16_to_lds(o + (int64_t)more * 64 * pitch_o, out[kept], to + 2 * kIn);
+            }
+        }
+    };
+
+    // ---- operands: a lane's address is one of four numbers below, an exclusive or with what a step changes of the slot, and a constant
+    static constexpr int kMask = W % 16 == 0 ? 15 : W % 8 == 0 ? 7 : 3;           // of a slot, what is exchanged
+    struct Lane {
+        int in, out, in_turned, out_turned;
+        __device__ __forceinline__ explicit Lane(int lane) {
+            const int r = lane & 31, hf = lane >> 5, i = lane & 15, rb = (lane >> 2 & 4) + (i & 3), chunk = 2 * (rb & 1) + (rb >> 2), half = (rb >> 1 & 1) * 8;
+            in = r * (W * 16) + slot_in(r, hf) * 16;
+            out = r * 64 + slot_out(r, 2 * hf) * 16;
+            in_turned = (4 * hf + (i >> 2)) * (W * 16) + slot_in(4 * hf + (i >> 2), chunk) * 16 + half;
+            out_turned = (16 * hf + (i >> 2)) * 64 + chunk * 16 + half;
+        }
+    };
     // rows of Wa or Wb as left operand, channels 16 s + 8 half ..
-    static __device__ __forceinline__ uint4 in(const unsigned char* part, int s, int lane) {
-        const int row = lane & 31;
-        return *reinterpret_cast<const uint4*>(part + row * (W * 16) + (slot_in(row, 2 * s + (lane >> 5)) << 4));
+    static __device__ __forceinline__ uint4 in(const unsigned char* part, const Lane& l, int s) {
+        return *reinterpret_cast<const uint4*>(part + (l.in ^ (2 * s & kMask) << 4) + (2 * s & ~kMask) * 16);
     }
     // rows of Wo (32 ct ..), hidden channels 16 half + 8 t ..
-    static __device__ __forceinline__ uint4 out(const unsigned char* part, int ct, int t, int lane) {
-        const int row = 32 * ct + (lane & 31);
-        return *reinterpret_cast<const uint4*>(part + row * 64 + (slot_out(row, 2 * (lane >> 5) + t) << 4));
+    static __device__ __forceinline__ uint4 out(const unsigned char* part, const Lane& l, int ct, int t) {
+        return *reinterpret_cast<const uint4*>(part + (l.out ^ t << 4) + ct * 2048);
     }
-
-    // ---- turned: four rows of 64 contiguous bytes a read, their columns in the order of place(); of sixteen lanes, lane i asks for four columns of row i / 4
+    // Turned: four rows of 64 contiguous bytes a read, their columns in the order of place(); of sixteen lanes, lane i asks for four columns of row i / 4.
     static __device__ __forceinline__ uint4 turned(const unsigned char* p0, const unsigned char* p1) {
         const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)p0));
         const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)p1));
         return make_uint4(a.x, a.y, b.x, b.y);
     }
-    // hidden channels as rows (in the order of place()), channels 16 s + 8 half .. of Wo as k
-    static __device__ __forceinline__ uint4 out_turned(const unsigned char* part, int s, int lane) {
-        const int i = lane & 15, rb = (lane >> 2 & 4) + (i & 3), chunk = 2 * (rb & 1) + (rb >> 2), row = 32 * (s >> 1) + 16 * (lane >> 5) + 4 * (s & 1) + (i >> 2);
-        const unsigned char* p = part + (rb >> 1 & 1) * 8;
-        return turned(p + row * 64 + slot_out(row, chunk) * 16, p + (row + 8) * 64 + slot_out(row + 8, chunk) * 16);
+    // hidden channels as rows (in the order of place()), channels 16 s + 8 half .. of Wo as k: rows 32 (s / 2) + 16 half + 4 (s % 2) .., and eight further
+    static __device__ __forceinline__ uint4 out_turned(const unsigned char* part, const Lane& l, int s) {
+        const unsigned char* p = part + (32 * (s >> 1) + 4 * (s & 1)) * 64;
+        return turned(p + (l.out_turned ^ (s & 1) << 4), p + (l.out_turned ^ (2 + (s & 1)) << 4) + 512);
     }
-    // channels 32 ct .. of Wa or Wb as rows (in the order of place()), hidden channels 16 half + 8 t .. as k
-    static __device__ __forceinline__ uint4 in_turned(const unsigned char* part, int ct, int t, int lane) {
-        const int i = lane & 15, rb = (lane >> 2 & 4) + (i & 3), chunk = 4 * ct + 2 * (rb & 1) + (rb >> 2), row = 16 * t + 4 * (lane >> 5) + (i >> 2);
-        const unsigned char* p = part + (rb >> 1 & 1) * 8;
-        return turned(p + row * (W * 16) + slot_in(row, chunk) * 16, p + (row + 8) * (W * 16) + slot_in(row + 8, chunk) * 16);
+    // channels 32 ct .. of Wa or Wb as rows (in the order of place()), hidden channels 16 half + 8 t .. as k: rows 16 t + 4 half .., and eight further
+    static __device__ __forceinline__ uint4 in_turned(const unsigned char* part, const Lane& l, int ct, int t) {
+        const unsigned char* p = part + t * 16 * (W * 16) + (4 * ct & ~kMask) * 16;
+        return turned(p + (l.in_turned ^ (4 * ct & kMask) << 4), p + (l.in_turned ^ ((4 * ct & kMask) ^ 2) << 4) + 8 * (W * 16));
     }
 };
+
+// N steps whose operands are read AHEAD steps before they are used: left to itself the compiler reads each right in front of its product and waits
+template <int N, int AHEAD, typename Read, typename Use> __device__ __forceinline__ void ahead(Read read, Use use) {
+    decltype(read(0)) f[AHEAD + 1];
+#pragma unroll
+    for (int n = 0; n < AHEAD && n < N; ++n) f[n] = read(n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (n + AHEAD < N) f[(n + AHEAD) % (AHEAD + 1)] = read(n + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+        use(n, f[n % (AHEAD + 1)]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+struct One { uint4 a; };
+struct Two { uint4 a, b; };
+struct Three { uint4 a, b, c; };
 
 // a row's sixteen channels 16 s + 8 half .. of x as right operands, zeros past the end and in rows that are none
 template <int KC> __device__ __forceinline__ void load_row(uint4 (&v)[2 * KC], const bf16_t* x, int64_t row, bool live, int c, bool whole, int lane) {
