@@ -96,7 +96,7 @@ struct HiddenArgs {
     uint32_t mtiles, ntiles;
 };
 // Both projections share the tile of x; their product with the activation leaves alone.  Channels and rows past the end are zeros.
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_hidden(HiddenArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, sizeof(T) == 4 ? 4 : 2) void k_tr_hidden(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[2][C::MT][C::NT];
@@ -127,7 +127,7 @@ struct OutArgs {
     uint32_t mtiles, ntiles;
 };
 // out = (residual +) sum of the products; a masked row's sum counts as zero, whatever it is
-template <class C, typename T> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_out(OutArgs a) {
+template <class C, typename T> __global__ __launch_bounds__(C::kThreads, sizeof(T) == 4 ? 4 : 2) void k_tr_out(OutArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[1][C::MT][C::NT];
@@ -232,7 +232,7 @@ struct GradArgs {
 };
 // a, b and dh = dy Wo of a tile in one loop over the channels; da = dh b act'(a), db = dh act(a) and h, rounded to the tensors' type, are what the
 // products with the weights and with x and dy read
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, 2) void k_tr_grad(GradArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, sizeof(T) == 4 ? 4 : 2) void k_tr_grad(GradArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[3][C::MT][C::NT];
@@ -468,9 +468,9 @@ Sizes sizes_of(const ff_transition_desc& d) {
     s.weight = align256((size_t)s.fp * s.cp * s.esz);
     s.tokens = align256((size_t)s.chunk * s.cp * s.esz);
     s.hidden = align256((size_t)s.chunk * s.fp * s.esz);
-    // as many splits of the rows as give a block (of small tiles two) for each of 256 compute units, of 256 rows at least
+    // as many splits of the rows as give a block (of small tiles two or four) for each of 256 compute units, of 256 rows at least
     s.wide = d.dtype == FF_BF16 && d.f >= 256;
-    const int bm = s.wide ? 256 : 128, bn = s.wide && d.c > 128 ? 256 : 128, blocks = s.wide ? 256 : 512;
+    const int least = d.dtype == FF_F32 ? 64 : 128, bm = s.wide ? 256 : least, bn = s.wide && d.c > 128 ? 256 : least, blocks = s.wide ? 256 : d.dtype == FF_F32 ? 1024 : 512;
     const int64_t tiles = 3 * ((d.f + bm - 1) / bm) * ((d.c + bn - 1) / bn);
     const int64_t want = std::max<int64_t>(1, std::min(blocks / tiles, s.chunk / 256));
     s.per_split = round_up((s.chunk + want - 1) / want, 128);
@@ -534,7 +534,9 @@ template <typename T> Weights weights_of(const ff_transition_desc& d, const Size
     return w;
 }
 
-constexpr int bk_of(int esz) { return 64 / esz; }              // of a row, 64 bytes a stage
+// Tiles: float32 products are bound by their instructions (64 cycles each, a quarter of a percent of LDS's time), so small tiles cost nothing and fill the units evenly.
+template <typename T> struct Tiles { static constexpr int M = 128, N = 128; };
+template <> struct Tiles<float> { static constexpr int M = 64, N = 64; };
 
 template <int KC> ff_status launch_rows(int act, const RowsArgs& a, hipStream_t stream) {
     typedef rows::Weights<KC, 4> W;
@@ -573,8 +575,9 @@ ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const
 template <typename T> ff_status forward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                         const float* mask, void* y, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
-    typedef Core<Op, 128, 64, bk_of(sizeof(T)), 4, 2, 2, 1, 2, 0, 0u> CH;
-    typedef Core<Op, 128, 128, bk_of(sizeof(T)), 4, 2, 2, 1, 1, 0, 0u> CO;
+    constexpr int BK = 64 / sizeof(T), BM = Tiles<T>::M, BN = Tiles<T>::N;
+    typedef Core<Op, BM, 64, BK, 4, 2, 2, 1, 2, 0, 0u> CH;
+    typedef Core<Op, BM, BN, BK, 4, 2, 2, 1, 1, 0, 0u> CO;
     const Sizes s = sizes_of(d);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
@@ -631,7 +634,7 @@ struct Blocked {
     typedef Core<Bf16, 128, 128, 32, 4, 2, 2, 1, 1, 2, 1u> Small;
 };
 template <typename T> struct Turned {
-    typedef Core<typename OpOf<T>::type, 128, 128, 64 / sizeof(T), 4, 2, 2, 1, 1, 1, 1u> Small;
+    typedef Core<typename OpOf<T>::type, Tiles<T>::M, Tiles<T>::N, 64 / sizeof(T), 4, 2, 2, 1, 1, 1, 1u> Small;
     typedef Core<Bf16, 256, 256, 32, 4, 2, 4, 1, 1, 1, 1u> Square;
 };
 template <class C> ff_status weights(WeightArgs a, int splits, hipStream_t stream) {
@@ -643,9 +646,9 @@ template <class C> ff_status weights(WeightArgs a, int splits, hipStream_t strea
 template <typename T> ff_status backward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
                                          const float* mask, void* dx, void* const (&dw)[3], int grad_dtype, bool accumulate, void* ws_, hipStream_t stream) {
     typedef typename OpOf<T>::type Op;
-    constexpr int BK = bk_of(sizeof(T));
-    typedef Core<Op, 128, 64, BK, 3, 2, 2, 2, 3, 0, 4u> CG;
-    typedef Core<Op, 128, 128, BK, 4, 2, 2, 1, 1, 0, 1u> CX;
+    constexpr int BK = 64 / sizeof(T), BM = Tiles<T>::M, BN = Tiles<T>::N;
+    typedef Core<Op, BM, 64, BK, 3, 2, 2, 2, 3, 0, 4u> CG;
+    typedef Core<Op, BM, BN, BK, 4, 2, 2, 1, 1, 0, 1u> CX;
     const Sizes s = sizes_of(d);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
