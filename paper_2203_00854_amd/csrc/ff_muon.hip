@@ -29,7 +29,6 @@ namespace {
 
 constexpr float kScale = 256.f, kUnscale = 1.f / 256.f;
 constexpr int kPad = 16;
-constexpr int kTile = 128;
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 16384;                    // values that a block of the element-wise kernels holds
 constexpr int64_t kBatch = 1 << 30;            // workspace of the matrices that are worked on together, unless one alone needs more
@@ -222,15 +221,19 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
 }
 
 // ---- the products --------------------------------------------------------------------------
-template <int STAGES> struct Cores {
-    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, 0, 0u> Straight;      // rows by rows
-    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, 1, 1u> Turned;         // columns by columns
-    typedef Core<Pair, kTile, kTile, 16, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;         // rows by columns
+template <int TILE_, int STAGES> struct Cores {
+    static constexpr int TILE = TILE_;
+    typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 0, 0u> Straight;        // rows by rows
+    typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 1, 1u> Turned;          // columns by columns
+    typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;           // rows by columns
+    static constexpr int kBlocks = TILE == 128 && STAGES == 3 ? 3 : TILE == 64 ? 2 : 1;        // on a compute unit
     static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 };
 // Three stages leave room for three blocks on a compute unit, whose ends then overlap with the others' products; eight for one, where a launch has fewer blocks than
-// there are units (a stage takes 0.18 us of matrix instructions and 0.8 us to arrive).
-constexpr int kShallow = 3, kDeep = 8;
+// there are units (a stage takes 0.18 us of matrix instructions and 0.8 us to arrive).  Fewer still, and tiles of 64 fill four times the units.
+typedef Cores<128, 3> Many;
+typedef Cores<128, 8> Some;
+typedef Cores<64, 8> Few;
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
     return {ws + x.x(which), x.cp() * 4, x.rp(), (int32_t)(x.cp() * 4)};
@@ -257,8 +260,9 @@ __device__ __forceinline__ void store_gram(char* a, char* c, int64_t np, int64_t
 }
 
 // A.  SPLIT: sums over a part of k each, for k_ns_join
-template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_gram(Table t, char* ws, int which, StepArgs a, float* parts) {
-    typedef typename Cores<STAGES>::Straight Straight;
+template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int which, StepArgs a, float* parts) {
+    typedef typename C::Straight Straight;
+    constexpr int kTile = C::TILE;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -270,7 +274,7 @@ template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 
     Straight::clear(acc);
     const int64_t all = x.tall() ? x.rp() : x.cp(), each = SPLIT ? (all / kPad + gridDim.y - 1) / gridDim.y * kPad : all, from = SPLIT ? blockIdx.y * each : 0;
     const int64_t to = from + each < all ? from + each : all;
-    if (x.tall()) Cores<STAGES>::Turned::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, from, to, smem);
+    if (x.tall()) C::Turned::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, from, to, smem);
     else Straight::run(acc, &o, &o, (int64_t)i * kTile, (int64_t)j * kTile, from, to, smem);
     if constexpr (SPLIT) {
         float* out = parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kTile * kTile;
@@ -288,7 +292,7 @@ template <int STAGES, bool SPLIT> __global__ __launch_bounds__(256, STAGES <= 3 
 
 // A and C of A's parts, added up in their order; a block has 32 rows of a tile
 __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, const float* parts, int splits) {
-    constexpr int kBand = 32, kPitch = kBand + 1;
+    constexpr int kTile = Few::TILE, kBand = 32, kPitch = kBand + 1;
     __shared__ float band[kTile * kPitch];
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -324,8 +328,9 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
 }
 
 // B = a I + A C
-template <int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_poly(Table t, char* ws, StepArgs a) {
-    typedef typename Cores<STAGES>::Straight Straight;
+template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(Table t, char* ws, StepArgs a) {
+    typedef typename C::Straight Straight;
+    constexpr int kTile = C::TILE;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -369,8 +374,9 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
     }
 }
 // X = B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights
-template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, STAGES <= 3 ? 3 : 1) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
-    typedef typename Cores<STAGES>::Straight Straight;
+template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
+    typedef typename C::Straight Straight;
+    constexpr int kTile = C::TILE;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -386,7 +392,7 @@ template <int LAST, typename P, int STAGES> __global__ __launch_bounds__(256, ST
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     if (x.tall()) Straight::run(acc, &ox, &ob, (int64_t)i * kTile, (int64_t)j * kTile, 0, cp, smem);
-    else Cores<STAGES>::Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
+    else C::Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
     char* to = ws + x.x(which ^ 1);
     const float size = size_of(x, a);
     Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
@@ -612,21 +618,23 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
 struct Batch {
     int64_t ws;                                   // bytes of workspace of its matrices
     int32_t piece0, pieces, tri0, tris, app0, apps;        // places of the three kinds, in the plan's lists
-    int32_t splits, pad;                          // of k in the Gram matrices, 1 = none
+    int32_t splits, tri_tile, app_tile, pad;      // parts of k in the Gram matrices, 1 = whole; tiles of 64 or 128
 };
 int pieces_of(const Matrix& m) { return (int)((m.rp() * m.cp() + kPiece - 1) / kPiece); }
-int tris_of(const Matrix& m) {
-    const int n = (int)((m.np() + kTile - 1) / kTile);
+int tris_of(const Matrix& m, int tile) {
+    const int n = (int)((m.np() + tile - 1) / tile);
     return n * (n + 1) / 2;
 }
-int apps_of(const Matrix& m) { return (int)((m.rp() + kTile - 1) / kTile * ((m.cp() + kTile - 1) / kTile)); }
+int apps_of(const Matrix& m, int tile) { return (int)((m.rp() + tile - 1) / tile * ((m.cp() + tile - 1) / tile)); }
+// the tiles of a launch that would have this many blocks with the large ones
+int tile_for(int64_t large) { return large < 192 ? 64 : 128; }
 int small_of(const Matrix& m) { return std::max(m.rows, m.cols) <= 64 ? 64 : std::max(m.rows, m.cols) <= 128 ? 128 : 0; }
-// Few Gram tiles of a long k leave most compute units without a block: k is split then, in parts of 512 and more (the join costs as much as 256 of k).
-int splits_of(int64_t tris, int64_t longest) {
-    const int64_t s = std::min<int64_t>({8, (256 + tris - 1) / tris, longest / 512});
-    return s >= 3 ? (int)s : 1;
+// Few Gram tiles of a long k: k is split, in parts of 512 and more (the join costs as much as 512 of k).
+int splits_of(int tile, int64_t tris, int64_t longest) {
+    const int64_t s = std::min<int64_t>({8, 512 / std::max<int64_t>(tris, 1), longest / 512});
+    return tile == 64 && s >= 3 ? (int)s : 1;
 }
-int64_t parts_bytes(int64_t tris, int splits) { return splits > 1 ? tris * splits * kTile * kTile * 4 : 0; }
+int64_t parts_bytes(int64_t tris, int splits) { return splits > 1 ? tris * splits * Few::TILE * Few::TILE * 4 : 0; }
 
 template <auto KERNEL, typename... A> ff_status go(int kind, dim3 blocks, int threads, size_t lds, hipStream_t stream, const char* what, A... args) {
     Timed t(kind, stream);
@@ -639,34 +647,39 @@ template <auto KERNEL, typename... A> ff_status go(int kind, dim3 blocks, int th
 struct Tables {
     Table piece, tri, app;
     uint32_t pieces, tris, apps;
-    int splits;
+    int splits, tri_tile, app_tile;
     double* partial;
     float* parts;
 };
 template <int LAST> constexpr const char* kWhat = LAST == kWeights ? "ff_muon_step" : "ff_orthogonalise";
 
-template <int LAST, typename P> ff_status apply(const Tables& t, int which, const StepArgs& a, const float* norm, char* ws, hipStream_t stream, const char* what) {
-    if (t.apps > 256) return go<k_ns_apply<LAST, P, kShallow>>(KK_NS_APPLY, t.apps, 256, Cores<kShallow>::kLds, stream, what, t.app, ws, which, a, norm);
-    return go<k_ns_apply<LAST, P, kDeep>>(KK_NS_APPLY, t.apps, 256, Cores<kDeep>::kLds, stream, what, t.app, ws, which, a, norm);
+template <class C, int LAST, typename P> ff_status apply(const Tables& t, int which, const StepArgs& a, const float* norm, char* ws, hipStream_t stream) {
+    return go<k_ns_apply<LAST, P, C>>(KK_NS_APPLY, t.apps, 256, C::kLds, stream, kWhat<LAST>, t.app, ws, which, a, norm);
+}
+template <int LAST, typename P> ff_status apply(const Tables& t, int which, const StepArgs& a, const float* norm, char* ws, hipStream_t stream) {
+    return t.app_tile == 64 ? apply<Few, LAST, P>(t, which, a, norm, ws, stream)
+           : t.apps > 256   ? apply<Many, LAST, P>(t, which, a, norm, ws, stream)
+                            : apply<Some, LAST, P>(t, which, a, norm, ws, stream);
+}
+// A and C of X, B of both
+template <class C> ff_status gram(const Tables& t, int which, const StepArgs& a, char* ws, hipStream_t stream, const char* what) {
+    ff_status st;
+    if (C::TILE == 64 && t.splits > 1) {
+        st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, which, a, t.parts);
+        if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, a, (const float*)t.parts, t.splits);
+    } else
+        st = go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, which, a, (float*)nullptr);
+    return st != FF_OK ? st : go<k_ns_poly<C>>(KK_NS_POLY, t.tris, 256, C::kLds, stream, what, t.tri, ws, a);
 }
 template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, const StepArgs& a, int steps, const float* norm, char* ws, hipStream_t stream) {
     constexpr bool MUON = LAST == kWeights;
     const char* what = kWhat<LAST>;
     ff_status st = go<k_muon_momentum<G, MUON>>(KK_MUON_MOMENTUM, t.pieces, 256, 0, stream, what, t.piece, a, norm, t.partial);
     if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 256, 0, stream, what, t.piece, a, norm, (const double*)t.partial, ws);
-    constexpr size_t shallow = Cores<kShallow>::kLds, deep = Cores<kDeep>::kLds;
     for (int s = 0; s < steps && st == FF_OK; ++s) {
         const int which = s & 1;
-        if (t.splits > 1) {
-            st = go<k_ns_gram<kShallow, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, shallow, stream, what, t.tri, ws, which, a, t.parts);
-            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, kTile / 32), 256, 0, stream, what, t.tri, ws, a, (const float*)t.parts, t.splits);
-        } else if (t.tris > 256) st = go<k_ns_gram<kShallow, false>>(KK_NS_GRAM, t.tris, 256, shallow, stream, what, t.tri, ws, which, a, (float*)nullptr);
-        else st = go<k_ns_gram<kDeep, false>>(KK_NS_GRAM, t.tris, 256, deep, stream, what, t.tri, ws, which, a, (float*)nullptr);
-        if (st != FF_OK) return st;
-        if (t.tris > 256) st = go<k_ns_poly<kShallow>>(KK_NS_POLY, t.tris, 256, shallow, stream, what, t.tri, ws, a);
-        else st = go<k_ns_poly<kDeep>>(KK_NS_POLY, t.tris, 256, deep, stream, what, t.tri, ws, a);
-        if (st != FF_OK) return st;
-        st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream, what) : apply<LAST, P>(t, which, a, norm, ws, stream, what);
+        st = t.tri_tile == 64 ? gram<Few>(t, which, a, ws, stream, what) : t.tris > 256 ? gram<Many>(t, which, a, ws, stream, what) : gram<Some>(t, which, a, ws, stream, what);
+        if (st == FF_OK) st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream) : apply<LAST, P>(t, which, a, norm, ws, stream);
     }
     return st;
 }
@@ -760,22 +773,26 @@ Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
         b.tri0 = (int32_t)r.tri.size();
         b.app0 = (int32_t)r.app.size();
         int last = first;
-        int64_t tris = 0, longest = 0;
+        int64_t tris = 0, apps = 0, few = 0, longest = 0;
         for (; last < large && (last == first || b.ws + r.matrices[last].bytes() <= kBatch); ++last) {
             Matrix& m = r.matrices[last];
             m.ws = b.ws;
             m.piece0 = b.pieces;
             b.ws += (int64_t)align256((size_t)m.bytes());
             b.pieces += m.pieces;
-            tris += tris_of(m);
+            tris += tris_of(m, 128);
+            apps += apps_of(m, 128);
+            few += tris_of(m, 64);
             longest = std::max(longest, std::max(m.rp(), m.cp()));
             for (int32_t k = 0; k < m.pieces; ++k) r.piece.push_back({last, k});
         }
-        spread(r.matrices, first, last, tris_of, [](const Matrix& m) { return std::max(m.rp(), m.cp()) + 128; }, r.tri);
-        spread(r.matrices, first, last, apps_of, [](const Matrix& m) { return m.np() + 128; }, r.app);
+        b.tri_tile = tile_for(tris);
+        b.app_tile = tile_for(apps);
+        b.splits = splits_of(b.tri_tile, few, longest);
+        spread(r.matrices, first, last, [&](const Matrix& m) { return tris_of(m, b.tri_tile); }, [](const Matrix& m) { return std::max(m.rp(), m.cp()) + 128; }, r.tri);
+        spread(r.matrices, first, last, [&](const Matrix& m) { return apps_of(m, b.app_tile); }, [](const Matrix& m) { return m.np() + 128; }, r.app);
         b.tris = (int32_t)(r.tri.size() - b.tri0);
         b.apps = (int32_t)(r.app.size() - b.app0);
-        b.splits = splits_of(tris, longest);
         r.ws = std::max(r.ws, b.ws + (int64_t)align256((size_t)b.pieces * 8) + parts_bytes(b.tris, b.splits));
         if (r.piece.size() > INT32_MAX / 2 || r.tri.size() > INT32_MAX / 2 || r.app.size() > INT32_MAX / 2) throw std::bad_alloc();
         r.batches.push_back(b);
@@ -857,7 +874,7 @@ template <typename G, typename P> ff_status muon_step(const Header& head, const 
     for (int i = 0; i < head.batches; ++i) {
         const Batch& b = ((const Batch*)((const char*)plan_host + l.batches))[i];
         char* const partial = ws + b.ws;
-        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
+        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, b.tri_tile, b.app_tile, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
         ts.piece.places = (const Place*)(dev + l.piece) + b.piece0;
         ts.tri.places = (const Place*)(dev + l.tri) + b.tri0;
         ts.app.places = (const Place*)(dev + l.app) + b.app0;
@@ -887,8 +904,8 @@ struct Uniform {
     Matrix one;
     int64_t bytes;             // of workspace a matrix
     int32_t group;             // matrices worked on together
-    int splits;
-    uint32_t tris, apps;       // places of a group
+    int splits, tri_tile, app_tile;
+    uint32_t tris;             // places of a group
 };
 Uniform uniform_of(const ff_orthogonalise_desc& d) {
     Uniform u{};
@@ -897,9 +914,10 @@ Uniform uniform_of(const ff_orthogonalise_desc& d) {
     u.one.pieces = pieces_of(u.one);
     u.bytes = (int64_t)align256((size_t)u.one.bytes());
     u.group = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.count, kBatch / u.bytes));
-    u.splits = splits_of((int64_t)u.group * tris_of(u.one), std::max(u.one.rp(), u.one.cp()));
-    u.tris = places_of(u.group, tris_of(u.one));
-    u.apps = places_of(u.group, apps_of(u.one));
+    u.tri_tile = tile_for((int64_t)u.group * tris_of(u.one, 128));
+    u.app_tile = tile_for((int64_t)u.group * apps_of(u.one, 128));
+    u.splits = splits_of(u.tri_tile, (int64_t)u.group * tris_of(u.one, 64), std::max(u.one.rp(), u.one.cp()));
+    u.tris = places_of(u.group, tris_of(u.one, u.tri_tile));
     return u;
 }
 template <typename T> ff_status orthogonalise(const ff_orthogonalise_desc& d, const void* x, void* out, char* ws, hipStream_t stream) {
@@ -923,10 +941,10 @@ template <typename T> ff_status orthogonalise(const ff_orthogonalise_desc& d, co
         t.count = std::min(u.group, d.count - i);
         t.one.g = (const char*)x + i * t.in_step;
         t.one.p = (char*)out + i * t.out_step;
-        Tables ts{t, t, t, 0, 0, 0, u.splits, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
+        Tables ts{t, t, t, 0, 0, 0, u.splits, u.tri_tile, u.app_tile, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
         ts.pieces = places_of(t.count, ts.piece.each = u.one.pieces);
-        ts.tris = places_of(t.count, ts.tri.each = tris_of(u.one));
-        ts.apps = places_of(t.count, ts.app.each = apps_of(u.one));
+        ts.tris = places_of(t.count, ts.tri.each = tris_of(u.one, u.tri_tile));
+        ts.apps = places_of(t.count, ts.app.each = apps_of(u.one, u.app_tile));
         const ff_status st = steps_of<T, T, kOut>(ts, a, d.steps, nullptr, ws, stream);
         if (st != FF_OK) return st;
     }
