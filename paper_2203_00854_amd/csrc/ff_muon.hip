@@ -2,8 +2,9 @@
 //
 //   X = G / (|G| + eps);  per step, with n the shorter side:  A = X X^T (X^T X where a matrix is tall);  X = a X + (b A + c A^2) X  (X (...))
 //
-// Three launches a step for all matrices together: A, and C = b I + c A beside it; B = a I + A C; X = B X.  So no product needs more than its operands: what else
-// it had to add would be another read, in a kernel's last microseconds.  Values are held as float16 pairs of kScale times
+// Three launches a step for all matrices together: A; B = a I + b A + c A^2; X = B X.  With a I inside B the last product needs its operands alone; few
+// tiles hold C = b I + c A beside A, so that B = a I + A C does too: what it had to add otherwise would be another read in a short kernel's last microseconds.  Many
+// tiles do not (A is as large as X where that is square, and memory bounds them).  Values are held as float16 pairs of kScale times
 // themselves: 24 significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  Magnitudes
 // to 255 have a place, and singular values are at most 1 at the start and below 1.3 after any number of steps with the usual coefficients; 2^-33 is
 // the smallest step between small values.  A tall matrix is worked on as it lies: its operands are read turned.
@@ -30,7 +31,7 @@ namespace {
 constexpr float kScale = 256.f, kUnscale = 1.f / 256.f;
 constexpr int kPad = 16;
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
-constexpr int kPiece = 16384;                    // values that a block of the element-wise kernels holds
+constexpr int kPiece = 4096;                     // values that a block of the element-wise kernels holds
 constexpr int64_t kBatch = 1 << 30;            // workspace of the matrices that are worked on together, unless one alone needs more
 
 // One matrix, as the kernels see it.
@@ -226,6 +227,7 @@ template <int TILE_, int STAGES> struct Cores {
     typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 0, 0u> Straight;        // rows by rows
     typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 1, 1u> Turned;          // columns by columns
     typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;           // rows by columns
+    static constexpr bool kBeside = STAGES > 3;                                                 // C is held beside A
     static constexpr int kBlocks = TILE == 128 && STAGES == 3 ? 3 : TILE == 64 ? 2 : 1;        // on a compute unit
     static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 };
@@ -248,11 +250,12 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     j = t - i * (i + 1) / 2;
 }
-// eight values of A, and of C = b I + c A; row m from column n on (a multiple of eight)
-__device__ __forceinline__ void store_gram(char* a, char* c, int64_t np, int64_t m, int64_t n, const float (&v)[8], const StepArgs& p) {
+// eight values of A, and of C = b I + c A beside it; row m from column n on (a multiple of eight)
+template <bool BESIDE> __device__ __forceinline__ void store_gram(char* a, char* c, int64_t np, int64_t m, int64_t n, const float (&v)[8], const StepArgs& p) {
     if (m >= np || n >= np) return;
     const int64_t at = pairs_at(m * np + n);
     store_pairs(a + at, v);
+    if constexpr (!BESIDE) return;
     float w[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) w[q] = p.c * v[q] + (n + q == m ? p.b * kScale : 0.f);
@@ -283,7 +286,7 @@ template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) voi
         const auto store = [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
-            store_gram(ws + x.a(0), ws + x.a(2), x.np(), m, n, v, a);
+            store_gram<C::kBeside>(ws + x.a(0), ws + x.a(2), x.np(), m, n, v, a);
         };
         Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
         if (i != j) Straight::columns(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) band[(c + q) * kPitch + r] = v[q] *= kUnscale;
-        store_gram(ca, cc, np, m0 + r, n0 + c, v, a);
+        store_gram<true>(ca, cc, np, m0 + r, n0 + c, v, a);
     }
     if (i == j) return;
     tile::barrier();
@@ -323,11 +326,11 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = band[r * kPitch + c + q];
-        store_gram(ca, cc, np, n0 + r, m0 + c, v, a);
+        store_gram<true>(ca, cc, np, n0 + r, m0 + c, v, a);
     }
 }
 
-// B = a I + A C
+// B = a I + A C, or a I + b A + c A^2
 template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(Table t, char* ws, StepArgs a) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -337,20 +340,29 @@ template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
-    const Operand oa = operand_a(x, ws, 0), oc = operand_a(x, ws, 2);
+    const Operand oa = operand_a(x, ws, 0), oc = C::kBeside ? operand_a(x, ws, 2) : oa;
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     const int64_t np = x.np();
     Straight::run(acc, &oa, &oc, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
     char* out = ws + x.a(1);
-    const auto store = [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
+    const char* was = ws + x.a(0);
+    const auto fetch = [&](int64_t m, int64_t n) {
+        if constexpr (C::kBeside) return typename Straight::Nothing();
+        else return m < np && n < np ? load_pairs(was + pairs_at(m * np + n)) : Pairs{};
+    };
+    const auto store = [&](int64_t m, int64_t n, float (&v)[8], const auto& old) {
         if (m >= np || n >= np) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = kUnscale * v[q] + (n + q == m ? a.a * kScale : 0.f);
+        for (int q = 0; q < 8; ++q) {
+            if constexpr (C::kBeside) v[q] = kUnscale * v[q];
+            else v[q] = a.b * value_of(old, q) + (a.c * kUnscale) * v[q];
+            v[q] += n + q == m ? a.a * kScale : 0.f;
+        }
         store_pairs(out + pairs_at(m * np + n), v);
     };
-    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
-    if (i != j) Straight::columns(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
+    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
+    if (i != j) Straight::columns(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
 }
 
 enum Last { kMore = 0, kOut = 1, kWeights = 2 };
@@ -445,13 +457,17 @@ template <int SIZE> struct Small {
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[u][v] = 0.f;
         if (tiles <= 0) return;
-        // (a second tile that is none is worked on like the first, for no result)
         Frags f[2];
         read<TA, TB>(f[0], a, b, m0, n0, tiles, 0, lane);
         const int rounds = k / 16;
         const auto turn = [&](int s, Frags& now, Frags& then) {
             read<TA, TB>(then, a, b, m0, n0, tiles, s + 1 < rounds ? s + 1 : s, lane);
             __builtin_amdgcn_sched_barrier(0);
+            if (kUnits == 2 && tiles == 1) {                   // the other accumulator takes the cross terms
+                acc[kUnits - 1] = product_of<0>(now.b[0], now.a, acc[kUnits - 1]);
+                acc[0] = product_of<2>(now.b[0], now.a, acc[0]);
+                acc[kUnits - 1] = product_of<1>(now.b[0], now.a, acc[kUnits - 1]);
+            } else
 #pragma unroll
             for (int p = 0; p < 3; ++p)                        // lo hi, hi lo, hi hi: of both tiles in turn, an instruction waits for the one before of its own
 #pragma unroll
@@ -465,6 +481,10 @@ template <int SIZE> struct Small {
             turn(s + 1, f[1], f[0]);
         }
         if (s < rounds) turn(s, f[0], f[1]);
+        if (kUnits == 2 && tiles == 1) acc[0] += acc[kUnits - 1];
+    }
+    template <int P> static __device__ __forceinline__ f32x16 product_of(const Pair::Frag& b, const Pair::Frag& a, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(tile::f16x8, b.u[P == 0]), __builtin_bit_cast(tile::f16x8, a.u[P == 1]), c, 0, 0, 0);
     }
     struct Frags {
         Pair::Frag a, b[kUnits];
@@ -473,7 +493,8 @@ template <int SIZE> struct Small {
     static __device__ __forceinline__ void read(Frags& f, const unsigned char* a, const unsigned char* b, int m0, int n0, int tiles, int s, int lane) {
         f.a = frag<TA>(a, m0, s, lane);
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) f.b[u] = frag<TB>(b, u < tiles ? n0 + 32 * u : n0, s, lane);
+        for (int u = 0; u < kUnits; ++u)
+            if (u < tiles) f.b[u] = frag<TB>(b, n0 + 32 * u, s, lane);
     }
     // value(old, sum) of the wavefront's tiles, old being what image `from` holds there
     template <typename F> static __device__ __forceinline__ void combine(f32x16 (&acc)[kUnits], const unsigned char* from, int m0, int n0, int tiles, int lane, F value) {
