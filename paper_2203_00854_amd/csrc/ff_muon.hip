@@ -92,11 +92,13 @@ uint32_t places_of(int32_t count, int32_t each) {
 }
 
 // ---- pairs ---------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t half_bits(_Float16 h) { return __builtin_bit_cast(uint16_t, h); }
-__device__ __forceinline__ void split(float v, uint32_t& hi, uint32_t& lo) {
-    const _Float16 h = (_Float16)v;
-    hi = half_bits(h);
-    lo = half_bits((_Float16)(v - (float)h));
+typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+// two values, the first in the lower halves
+__device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& lo) {
+    const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
+    hi = __builtin_bit_cast(uint32_t, h);
+    lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a - (float)h[0], b - (float)h[1]}), f16x2));
 }
 __device__ __forceinline__ float join(uint32_t hi, uint32_t lo) {
     return (float)__builtin_bit_cast(_Float16, (uint16_t)hi) + (float)__builtin_bit_cast(_Float16, (uint16_t)lo);
@@ -104,11 +106,11 @@ __device__ __forceinline__ float join(uint32_t hi, uint32_t lo) {
 // eight values of a row from value i of a matrix on (rows are multiples of sixteen values): their hi parts, and 32 bytes further their lo parts
 __device__ __forceinline__ int64_t pairs_at(int64_t i) { return (i >> 4) * 64 + (i & 8) * 2; }
 __device__ __forceinline__ void store_pairs(char* p, const float (&v)[8]) {
-    uint32_t hi[8], lo[8];
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) split(v[q], hi[q], lo[q]);
-    *(uint4*)p = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
-    *(uint4*)(p + 32) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+    for (int q = 0; q < 4; ++q) split(v[2 * q], v[2 * q + 1], hi[q], lo[q]);
+    *(uint4*)p = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *(uint4*)(p + 32) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
 struct Pairs { uint4 hi, lo; };
 __device__ __forceinline__ Pairs load_pairs(const char* p) { return {*(const uint4*)p, *(const uint4*)(p + 32)}; }
@@ -432,99 +434,106 @@ template <int SIZE> struct Small {
     // sixteen bytes of row `row`: eight values from column c, a multiple of eight, of the hi part (p = 0) or the lo part.  Rows that one cycle reads together, straight or turned, lie in banks of their own.
     static __device__ __forceinline__ int at(int row, int c, int p) { return row * (W * 16) + (((c >> 4) * 4 + p * 2 + (c >> 3 & 1)) ^ ((row & 1) << 1 | (row & 2) << 2 | (row >> 2 & 1) | (row & 8) >> 1)) * 16; }
 
-    // 32 rows (straight) or columns (turned) from `first`, k = 16 s ..
-    template <bool T> static __device__ __forceinline__ Pair::Frag frag(const unsigned char* image, int first, int s, int lane) {
+    // 32 rows (straight) or columns (turned) from `first`, k = 16 s ..: a lane's address is a number of its own, an exclusive or with what s, the part and the half of a
+    // turned read change of the slot, and a constant.
+    template <bool T> static __device__ __forceinline__ int lane_of(int first, int lane) {
+        const int hf = lane >> 5, i = lane & 15;
+        if constexpr (!T) return at(first + (lane & 31), 8 * hf, 0);
+        return at(8 * hf + (i >> 2), first + (lane & 16) + 8 * (i >> 1 & 1), 0) + (i & 1) * 8;
+    }
+    template <bool T> static __device__ __forceinline__ Pair::Frag frag(const unsigned char* image, int of, int s) {
         Pair::Frag f;
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            if constexpr (!T) f.u[p] = *(const uint4*)(image + at(first + (lane & 31), 16 * s + 8 * (lane >> 5), p));
+            if constexpr (!T) f.u[p] = *(const uint4*)(image + (of ^ ((4 * s + 2 * p & 15) << 4)) + (4 * s & ~15) * 16);
             else {
-                const int i = lane & 15, col = first + (lane & 16) + 4 * (i & 3);
                 uint2 h[2];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)(image + at(16 * s + 8 * (lane >> 5) + 4 * t + (i >> 2), col & ~7, p) + (col & 4) * 2)));
+                for (int t = 0; t < 2; ++t) h[t] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tile::lds_i16x4)(image + (of ^ (2 * p ^ t) << 4) + (16 * s + 4 * t) * (W * 16))));
                 f.u[p] = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
             }
         }
         return f;
     }
-    // the wavefront's tiles of the product of two images over k (a multiple of sixteen)
-    template <bool TA, bool TB>
-    static __device__ __forceinline__ void product(f32x16 (&acc)[kUnits], const unsigned char* a, const unsigned char* b, int m0, int n0, int tiles, int k, int lane) {
+    // the four values that a lane holds as results 4 g .. 4 g + 3 of tile u, of the hi part (p = 0) or the lo part; of = at(m0 + lane % 32, n0, 0) + 8 (lane / 32), n0 a multiple of 32 (of 64 for two tiles)
+    static __device__ __forceinline__ int result_at(int of, int u, int g, int p) {
+        return (of ^ ((8 * u + 4 * (g >> 1) + 2 * p + (g & 1) & 15) << 4)) + (8 * u & ~15) * 16;
+    }
+    template <int TILES> struct Frags {
+        Pair::Frag a, b[TILES];
+    };
+    template <int P> static __device__ __forceinline__ f32x16 part(const Pair::Frag& b, const Pair::Frag& a, f32x16 c) {       // lo hi, hi lo, hi hi
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(tile::f16x8, b.u[P == 0]), __builtin_bit_cast(tile::f16x8, a.u[P == 1]), c, 0, 0, 0);
+    }
+    // TILES tiles of the product of two images over k (a multiple of sixteen); operands are read a round ahead.  An instruction waits for the one before on its
+    // accumulator: two tiles take turns, of one the cross terms have an accumulator of their own.
+    template <bool TA, bool TB, int TILES>
+    static __device__ __forceinline__ void product(f32x16 (&acc)[kUnits], const unsigned char* a, const unsigned char* b, int m0, int n0, int k, int lane) {
+        f32x16 c[2];
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[u][v] = 0.f;
-        if (tiles <= 0) return;
-        Frags f[2];
-        read<TA, TB>(f[0], a, b, m0, n0, tiles, 0, lane);
-        const int rounds = k / 16;
-        const auto turn = [&](int s, Frags& now, Frags& then) {
-            read<TA, TB>(then, a, b, m0, n0, tiles, s + 1 < rounds ? s + 1 : s, lane);
+            for (int v = 0; v < 16; ++v) c[u][v] = 0.f;
+        const int oa = lane_of<TA>(m0, lane), ob = lane_of<TB>(n0, lane), ob2 = TILES == 2 ? lane_of<TB>(n0 + 32, lane) : 0, rounds = k / 16;
+        Frags<TILES> f[2];
+        const auto read = [&](Frags<TILES>& f, int s) {
+            f.a = frag<TA>(a, oa, s);
+            f.b[0] = frag<TB>(b, ob, s);
+            if constexpr (TILES == 2) f.b[1] = frag<TB>(b, ob2, s);
+        };
+        const auto turn = [&](int s, Frags<TILES>& now, Frags<TILES>& then) {
+            read(then, s + 1 < rounds ? s + 1 : s);
             __builtin_amdgcn_sched_barrier(0);
-            if (kUnits == 2 && tiles == 1) {                   // the other accumulator takes the cross terms
-                acc[kUnits - 1] = product_of<0>(now.b[0], now.a, acc[kUnits - 1]);
-                acc[0] = product_of<2>(now.b[0], now.a, acc[0]);
-                acc[kUnits - 1] = product_of<1>(now.b[0], now.a, acc[kUnits - 1]);
-            } else
-#pragma unroll
-            for (int p = 0; p < 3; ++p)                        // lo hi, hi lo, hi hi: of both tiles in turn, an instruction waits for the one before of its own
-#pragma unroll
-                for (int u = 0; u < kUnits; ++u)
-                    acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(tile::f16x8, now.b[u].u[p == 0]), __builtin_bit_cast(tile::f16x8, now.a.u[p == 1]), acc[u], 0, 0, 0);
+            if constexpr (TILES == 2) {
+                c[0] = part<0>(now.b[0], now.a, c[0]);
+                c[1] = part<0>(now.b[1], now.a, c[1]);
+                c[0] = part<1>(now.b[0], now.a, c[0]);
+                c[1] = part<1>(now.b[1], now.a, c[1]);
+                c[0] = part<2>(now.b[0], now.a, c[0]);
+                c[1] = part<2>(now.b[1], now.a, c[1]);
+            } else {
+                c[1] = part<0>(now.b[0], now.a, c[1]);
+                c[0] = part<2>(now.b[0], now.a, c[0]);
+                c[1] = part<1>(now.b[0], now.a, c[1]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         };
+        read(f[0], 0);
         int s = 0;
         for (; s + 1 < rounds; s += 2) {
             turn(s, f[0], f[1]);
             turn(s + 1, f[1], f[0]);
         }
         if (s < rounds) turn(s, f[0], f[1]);
-        if (kUnits == 2 && tiles == 1) acc[0] += acc[kUnits - 1];
+        if constexpr (TILES == 1) acc[0] = c[0] + c[1];
+        else {
+            acc[0] = c[0];
+            acc[1] = c[1];
+        }
     }
-    template <int P> static __device__ __forceinline__ f32x16 product_of(const Pair::Frag& b, const Pair::Frag& a, f32x16 c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(tile::f16x8, b.u[P == 0]), __builtin_bit_cast(tile::f16x8, a.u[P == 1]), c, 0, 0, 0);
-    }
-    struct Frags {
-        Pair::Frag a, b[kUnits];
-    };
+    // the wavefront's tiles, none to kUnits
     template <bool TA, bool TB>
-    static __device__ __forceinline__ void read(Frags& f, const unsigned char* a, const unsigned char* b, int m0, int n0, int tiles, int s, int lane) {
-        f.a = frag<TA>(a, m0, s, lane);
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u)
-            if (u < tiles) f.b[u] = frag<TB>(b, n0 + 32 * u, s, lane);
-    }
-    // value(old, sum) of the wavefront's tiles, old being what image `from` holds there
-    template <typename F> static __device__ __forceinline__ void combine(f32x16 (&acc)[kUnits], const unsigned char* from, int m0, int n0, int tiles, int lane, F value) {
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u)
-            if (u < tiles)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int n = n0 + 32 * u + 8 * g, half = 8 * (lane >> 5);
-                    const uint2 h = *(const uint2*)(from + at(m0 + (lane & 31), n, 0) + half), l = *(const uint2*)(from + at(m0 + (lane & 31), n, 1) + half);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        acc[u][4 * g + q] = value(join((q < 2 ? h.x : h.y) >> (q & 1) * 16 & 0xffffu, (q < 2 ? l.x : l.y) >> (q & 1) * 16 & 0xffffu), acc[u][4 * g + q]);
-                }
+    static __device__ __forceinline__ void product(f32x16 (&acc)[kUnits], const unsigned char* a, const unsigned char* b, int m0, int n0, int tiles, int k, int lane) {
+        if constexpr (kUnits == 2) {
+            if (tiles == 2) return product<TA, TB, 2>(acc, a, b, m0, n0, k, lane);
+        }
+        if (tiles == 1) product<TA, TB, 1>(acc, a, b, m0, n0, k, lane);
     }
     // rows and columns below the given numbers
     static __device__ __forceinline__ void store(const f32x16 (&acc)[kUnits], unsigned char* to, int m0, int n0, int tiles, int rows, int cols, int lane) {
         if (m0 + (lane & 31) >= rows) return;
+        const int of = at(m0 + (lane & 31), n0, 0) + 8 * (lane >> 5);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
             if (u < tiles)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int n = n0 + 32 * u + 8 * g, half = 8 * (lane >> 5);
-                    if (n >= cols) continue;
-                    uint32_t hi[4], lo[4];
+                    if (n0 + 32 * u + 8 * g >= cols) continue;
+                    uint32_t hi[2], lo[2];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) split(acc[u][4 * g + q], hi[q], lo[q]);
-                    *(uint2*)(to + at(m0 + (lane & 31), n, 0) + half) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                    *(uint2*)(to + at(m0 + (lane & 31), n, 1) + half) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                    for (int q = 0; q < 2; ++q) split(acc[u][4 * g + 2 * q], acc[u][4 * g + 2 * q + 1], hi[q], lo[q]);
+                    *(uint2*)(to + result_at(of, u, g, 0)) = make_uint2(hi[0], hi[1]);
+                    *(uint2*)(to + result_at(of, u, g, 1)) = make_uint2(lo[0], lo[1]);
                 }
     }
 };
@@ -581,45 +590,44 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         const int place = (i * S::kThreads + (int)threadIdx.x) * 8;
         if (place >= rp * cp) continue;
         const int r = place / cp, c = place % cp;
-        uint32_t hi[8], lo[8];
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) split((float)(g[i][q] * inv), hi[q], lo[q]);
-        *(uint4*)(xs + S::at(r, c, 0)) = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
-        *(uint4*)(xs + S::at(r, c, 1)) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+        for (int q = 0; q < 4; ++q) split((float)(g[i][2 * q] * inv), (float)(g[i][2 * q + 1] * inv), hi[q], lo[q]);
+        *(uint4*)(xs + S::at(r, c, 0)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *(uint4*)(xs + S::at(r, c, 1)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
-    // the wavefront's tiles of A, and of X
-    const auto place = [&](int rows, int cols, int& m0, int& n0, int& tiles) {
+    // Three products a step, one piece of code: A of X; B = a I + b A + c A^2, into A's place; X = B X.  A wavefront has the same tiles of A and of B, and keeps its A.
+    tile::barrier();
+    f32x16 acc[S::kUnits] = {}, held[S::kUnits] = {};
+#pragma unroll 1
+    for (int phase = 0, left = 3 * steps; left > 0; --left) {
+        const bool last = phase == 2, tall = x.tall();
+        const int rows = last ? rp : np, cols = last ? cp : np;
         const int across = (cols + 31) / 32, down = (rows + 31) / 32, each = across * down > S::kWaves ? S::kUnits : 1, groups = (across + each - 1) / each;
-        m0 = wave / groups * 32;
-        n0 = wave % groups * each * 32;
-        tiles = wave < groups * down ? (across - n0 / 32 < each ? across - n0 / 32 : each) : 0;
-    };
-    int am, an, at, xm, xn, xt;
-    place(np, np, am, an, at);
-    place(rp, cp, xm, xn, xt);
-    f32x16 acc[S::kUnits];
-    for (int step = 0; step < steps; ++step) {
-        __syncthreads();                                       // X is whole
-        if (x.tall()) S::template product<true, true>(acc, xs, xs, am, an, at, rp, lane);
-        else S::template product<false, false>(acc, xs, xs, am, an, at, cp, lane);
+        const int m0 = wave / groups * 32, n0 = wave % groups * each * 32, tiles = wave < groups * down ? (across - n0 / 32 < each ? across - n0 / 32 : each) : 0;
+        if (phase == 0 && tall) S::template product<true, true>(acc, xs, xs, m0, n0, tiles, rp, lane);
+        else if (last && !tall) S::template product<false, true>(acc, as, xs, m0, n0, tiles, rp, lane);
+        else S::template product<false, false>(acc, phase == 1 ? as : xs, phase == 0 ? xs : as, m0, n0, tiles, phase == 1 ? np : cp, lane);
+        unsigned char* to = last ? xs : as;
+        if (phase == 1) {
+            const int diagonal = m0 + (lane & 31) - n0 - 4 * (lane >> 5);
 #pragma unroll
-        for (int u = 0; u < S::kUnits; ++u)
+            for (int u = 0; u < S::kUnits; ++u)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[u][v] *= kUnscale;
-        S::store(acc, as, am, an, at, np, np, lane);
-        __syncthreads();                                       // A is
-        S::template product<false, false>(acc, as, as, am, an, at, np, lane);
-        S::combine(acc, as, am, an, at, lane, [&](float was, float v) { return a.b * was + (a.c * kUnscale) * v; });
-        __syncthreads();                                       // and read
-        S::store(acc, as, am, an, at, np, np, lane);
-        __syncthreads();                                       // B is whole
-        if (x.tall()) S::template product<false, false>(acc, xs, as, xm, xn, xt, cp, lane);
-        else S::template product<false, true>(acc, as, xs, xm, xn, xt, rp, lane);
-        S::combine(acc, xs, xm, xn, xt, lane, [&](float was, float v) { return a.a * was + kUnscale * v; });
-        __syncthreads();                                       // X is read
-        S::store(acc, xs, xm, xn, xt, rp, cp, lane);
+                for (int v = 0; v < 16; ++v)
+                    acc[u][v] = a.b * held[u][v] + (a.c * kUnscale) * acc[u][v] + (diagonal == 32 * u + 8 * (v / 4) + v % 4 ? a.a * kScale : 0.f);
+        } else
+#pragma unroll
+            for (int u = 0; u < S::kUnits; ++u) acc[u] *= kUnscale;
+        if (phase == 0) {                                      // (A's place holds B, which nobody reads any more)
+#pragma unroll
+            for (int u = 0; u < S::kUnits; ++u) held[u] = acc[u];
+        } else
+            tile::barrier();                                   // all have read what is overwritten
+        S::store(acc, to, m0, n0, tiles, rows, cols, lane);
+        tile::barrier();
+        phase = last ? 0 : phase + 1;
     }
-    __syncthreads();
     const float size = size_of(x, a);
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
