@@ -154,7 +154,7 @@ def test_gradients_are_added(dtype, grad):
 def test_more_rows_than_are_worked_on_at_a_time(dtype):
     """Rows of several chunks: each row's results are those of the row among few others, the weights' gradients the sums of parts."""
     c, f = 16, 2048
-    rows = (64 << 20) // (f * (4 if dtype == "f32" else 2)) + 300
+    rows = (512 << 20) // (f * (4 if dtype == "f32" else 2)) + 300
     p = Problem(rows, c, f, dtype)
     y, (dx, *dw) = p.forward(), p.backward(grad_dtype=torch.float32)
     part = slice(rows - 400, rows)
@@ -163,8 +163,8 @@ def test_more_rows_than_are_worked_on_at_a_time(dtype):
     q.check_forward(y[part])
     assert torch.equal(q.forward(), y[part]) and torch.equal(q.backward()[0], dx[part])
     total = [torch.zeros(w.shape, dtype=torch.float64, device=DEV) for w in p.w]
-    for at in range(0, rows, 3000):
-        q.x, q.dy = p.x[at:at + 3000].contiguous(), p.dy[at:at + 3000].contiguous()
+    for at in range(0, rows, 20000):
+        q.x, q.dy = p.x[at:at + 20000].contiguous(), p.dy[at:at + 20000].contiguous()
         for t, g in zip(total, q.backward(grad_dtype=torch.float32)[1:]):
             t += g
     for t, g in zip(total, dw):
