@@ -40,7 +40,7 @@ struct Matrix {
     void* p;                                     // what the last step writes
     float* master;
     float* m;
-    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B, C, as pairs
+    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B, and C where it is held, as pairs
     int32_t rows, cols;
     int32_t piece0, pieces;                      // among the batch's
     float decay;
@@ -53,7 +53,7 @@ struct Matrix {
     __host__ __device__ int64_t bytes_a() const { return np() * np() * 4; }
     __host__ __device__ int64_t x(int which) const { return ws + which * bytes_x(); }
     __host__ __device__ int64_t a(int which) const { return ws + 2 * bytes_x() + which * bytes_a(); }
-    __host__ __device__ int64_t bytes() const { return 2 * bytes_x() + 3 * bytes_a(); }
+    __host__ __device__ int64_t bytes(bool beside) const { return 2 * bytes_x() + (beside ? 3 : 2) * bytes_a(); }
 };
 struct Place {
     int32_t matrix, at;                          // matrix < 0: none
@@ -647,7 +647,7 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
 struct Batch {
     int64_t ws;                                   // bytes of workspace of its matrices
     int32_t piece0, pieces, tri0, tris, app0, apps;        // places of the three kinds, in the plan's lists
-    int32_t splits, tri_tile, app_tile, pad;      // parts of k in the Gram matrices, 1 = whole; tiles of 64 or 128
+    int32_t splits, tri_tile, app_tile, beside;      // parts of k in the Gram matrices, 1 = whole; tiles of 64 or 128
 };
 int pieces_of(const Matrix& m) { return (int)((m.rp() * m.cp() + kPiece - 1) / kPiece); }
 int tris_of(const Matrix& m, int tile) {
@@ -655,8 +655,9 @@ int tris_of(const Matrix& m, int tile) {
     return n * (n + 1) / 2;
 }
 int apps_of(const Matrix& m, int tile) { return (int)((m.rp() + tile - 1) / tile * ((m.cp() + tile - 1) / tile)); }
-// the tiles of a launch that would have this many blocks with the large ones
+// the tiles of a launch that would have this many blocks with the large ones, and whether its Gram matrices have C beside them
 int tile_for(int64_t large) { return large < 192 ? 64 : 128; }
+bool beside_for(int64_t large) { return large <= 256; }
 int small_of(const Matrix& m) { return std::max(m.rows, m.cols) <= 64 ? 64 : std::max(m.rows, m.cols) <= 128 ? 128 : 0; }
 // Few Gram tiles of a long k: k is split, in parts of 512 and more (the join costs as much as 512 of k).
 int splits_of(int tile, int64_t tris, int64_t longest) {
@@ -677,6 +678,7 @@ struct Tables {
     Table piece, tri, app;
     uint32_t pieces, tris, apps;
     int splits, tri_tile, app_tile;
+    bool beside;
     double* partial;
     float* parts;
 };
@@ -707,7 +709,7 @@ template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, 
     if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 256, 0, stream, what, t.piece, a, norm, (const double*)t.partial, ws);
     for (int s = 0; s < steps && st == FF_OK; ++s) {
         const int which = s & 1;
-        st = t.tri_tile == 64 ? gram<Few>(t, which, a, ws, stream, what) : t.tris > 256 ? gram<Many>(t, which, a, ws, stream, what) : gram<Some>(t, which, a, ws, stream, what);
+        st = t.tri_tile == 64 ? gram<Few>(t, which, a, ws, stream, what) : t.beside ? gram<Some>(t, which, a, ws, stream, what) : gram<Many>(t, which, a, ws, stream, what);
         if (st == FF_OK) st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream) : apply<LAST, P>(t, which, a, norm, ws, stream);
     }
     return st;
@@ -802,18 +804,23 @@ Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
         b.tri0 = (int32_t)r.tri.size();
         b.app0 = (int32_t)r.app.size();
         int last = first;
-        int64_t tris = 0, apps = 0, few = 0, longest = 0;
-        for (; last < large && (last == first || b.ws + r.matrices[last].bytes() <= kBatch); ++last) {
-            Matrix& m = r.matrices[last];
-            m.ws = b.ws;
-            m.piece0 = b.pieces;
-            b.ws += (int64_t)align256((size_t)m.bytes());
-            b.pieces += m.pieces;
+        int64_t tris = 0, apps = 0, few = 0, longest = 0, room = 0;
+        for (; last < large && (last == first || room + r.matrices[last].bytes(false) <= kBatch); ++last) {
+            const Matrix& m = r.matrices[last];
+            room += (int64_t)align256((size_t)m.bytes(false));
             tris += tris_of(m, 128);
             apps += apps_of(m, 128);
             few += tris_of(m, 64);
             longest = std::max(longest, std::max(m.rp(), m.cp()));
-            for (int32_t k = 0; k < m.pieces; ++k) r.piece.push_back({last, k});
+        }
+        b.beside = beside_for(tris);
+        for (int i = first; i < last; ++i) {
+            Matrix& m = r.matrices[i];
+            m.ws = b.ws;
+            m.piece0 = b.pieces;
+            b.ws += (int64_t)align256((size_t)m.bytes(b.beside != 0));
+            b.pieces += m.pieces;
+            for (int32_t k = 0; k < m.pieces; ++k) r.piece.push_back({i, k});
         }
         b.tri_tile = tile_for(tris);
         b.app_tile = tile_for(apps);
@@ -903,7 +910,7 @@ template <typename G, typename P> ff_status muon_step(const Header& head, const 
     for (int i = 0; i < head.batches; ++i) {
         const Batch& b = ((const Batch*)((const char*)plan_host + l.batches))[i];
         char* const partial = ws + b.ws;
-        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, b.tri_tile, b.app_tile, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
+        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, b.tri_tile, b.app_tile, b.beside != 0, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
         ts.piece.places = (const Place*)(dev + l.piece) + b.piece0;
         ts.tri.places = (const Place*)(dev + l.tri) + b.tri0;
         ts.app.places = (const Place*)(dev + l.app) + b.app0;
@@ -934,6 +941,7 @@ struct Uniform {
     int64_t bytes;             // of workspace a matrix
     int32_t group;             // matrices worked on together
     int splits, tri_tile, app_tile;
+    bool beside;
     uint32_t tris;             // places of a group
 };
 Uniform uniform_of(const ff_orthogonalise_desc& d) {
@@ -941,8 +949,9 @@ Uniform uniform_of(const ff_orthogonalise_desc& d) {
     u.one.rows = d.rows;
     u.one.cols = d.cols;
     u.one.pieces = pieces_of(u.one);
-    u.bytes = (int64_t)align256((size_t)u.one.bytes());
-    u.group = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.count, kBatch / u.bytes));
+    u.group = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.count, kBatch / (int64_t)align256((size_t)u.one.bytes(false))));
+    u.beside = beside_for((int64_t)u.group * tris_of(u.one, 128));
+    u.bytes = (int64_t)align256((size_t)u.one.bytes(u.beside));
     u.tri_tile = tile_for((int64_t)u.group * tris_of(u.one, 128));
     u.app_tile = tile_for((int64_t)u.group * apps_of(u.one, 128));
     u.splits = splits_of(u.tri_tile, (int64_t)u.group * tris_of(u.one, 64), std::max(u.one.rp(), u.one.cp()));
@@ -970,7 +979,7 @@ template <typename T> ff_status orthogonalise(const ff_orthogonalise_desc& d, co
         t.count = std::min(u.group, d.count - i);
         t.one.g = (const char*)x + i * t.in_step;
         t.one.p = (char*)out + i * t.out_step;
-        Tables ts{t, t, t, 0, 0, 0, u.splits, u.tri_tile, u.app_tile, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
+        Tables ts{t, t, t, 0, 0, 0, u.splits, u.tri_tile, u.app_tile, u.beside, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
         ts.pieces = places_of(t.count, ts.piece.each = u.one.pieces);
         ts.tris = places_of(t.count, ts.tri.each = tris_of(u.one, u.tri_tile));
         ts.apps = places_of(t.count, ts.app.each = apps_of(u.one, u.app_tile));
