@@ -96,7 +96,7 @@ struct HiddenArgs {
     uint32_t mtiles, ntiles;
 };
 // Both projections share the tile of x; their product with the activation leaves alone.  Channels and rows past the end are zeros.
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, sizeof(T) == 4 ? 4 : 2) void k_tr_hidden(HiddenArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : 2) void k_tr_hidden(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[2][C::MT][C::NT];
@@ -127,7 +127,7 @@ struct OutArgs {
     uint32_t mtiles, ntiles;
 };
 // out = (residual +) sum of the products; a masked row's sum counts as zero, whatever it is
-template <class C, typename T> __global__ __launch_bounds__(C::kThreads, sizeof(T) == 4 ? 4 : 2) void k_tr_out(OutArgs a) {
+template <class C, typename T> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : 2) void k_tr_out(OutArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[1][C::MT][C::NT];
@@ -232,7 +232,7 @@ struct GradArgs {
 };
 // a, b and dh = dy Wo of a tile in one loop over the channels; da = dh b act'(a), db = dh act(a) and h, rounded to the tensors' type, are what the
 // products with the weights and with x and dy read
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, sizeof(T) == 4 ? 4 : 2) void k_tr_grad(GradArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : 2) void k_tr_grad(GradArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[3][C::MT][C::NT];
@@ -438,12 +438,14 @@ template <typename G> __global__ __launch_bounds__(256) void k_tr_join(JoinArgs 
     }
 }
 
-// channels / 32 that the kernels with rows in registers are built for: the next one that holds c (0: none)
-int rows_tiles(const ff_transition_desc& d) {
-    const int need = (d.c + 31) / 32;
-    return d.dtype != FF_BF16 || need > 8 ? 0 : need == 1 ? 1 : (need + 1) / 2 * 2;
+// Channels / 32 that the kernels with rows in registers are built for: the next one that holds c (0: none, or the tiled kernels are faster).  They
+// take a block of 128 rows a unit of its own through all hidden channels, so few rows leave units empty.  Measured, in us: rows in registers 0.18 (backward
+// 0.45) for 32 hidden channels and 32 channels, for every 256 blocks; tiled 6 (15) for the launches and 400 TFLOP/s.
+int rows_tiles(const ff_transition_desc& d, bool backward) {
+    const int need = (d.c + 31) / 32, kc = d.dtype != FF_BF16 || need > 8 ? 0 : need == 1 ? 1 : (need + 1) / 2 * 2;
+    const double turns = (double)((d.rows + 32767) / 32768) * ((d.f + 31) / 32) * kc, flop = (double)d.rows * d.c * d.f * (backward ? 10 : 6);
+    return turns * (backward ? 0.45 : 0.18) <= (backward ? 15. : 6.) + flop / 4e8 ? kc : 0;
 }
-
 // ---- the calls -------------------------------------------------------------------------------
 struct Sizes {
     int esz;
@@ -456,10 +458,10 @@ struct Sizes {
     int64_t per_split;
     size_t partial;
 };
-Sizes sizes_of(const ff_transition_desc& d) {
+Sizes sizes_of(const ff_transition_desc& d, bool backward) {
     Sizes s;
     s.esz = d.dtype == FF_F32 ? 4 : 2;
-    const int kc = rows_tiles(d);
+    const int kc = rows_tiles(d, backward);
     s.cp = kc ? kc * 32 : round_up(d.c, kPad);
     s.fp = round_up(d.f, kc ? 32 : kPad);
     const int64_t most = std::max<int64_t>(128, kHiddenBytes / (s.fp * s.esz) / 128 * 128);
@@ -534,10 +536,6 @@ template <typename T> Weights weights_of(const ff_transition_desc& d, const Size
     return w;
 }
 
-// Tiles: float32 products are bound by their instructions (64 cycles each, a quarter of a percent of LDS's time), so small tiles cost nothing and fill the units evenly.
-template <typename T> struct Tiles { static constexpr int M = 128, N = 128; };
-template <> struct Tiles<float> { static constexpr int M = 64, N = 64; };
-
 template <int KC> ff_status launch_rows(int act, const RowsArgs& a, hipStream_t stream) {
     typedef rows::Weights<KC, 4> W;
     const dim3 grid((uint32_t)((a.rows + 127) / 128));
@@ -572,13 +570,59 @@ ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const
     }
 }
 
+// ---- tiled products: the kernel of each tile size, and the choice among them -----------------------
+// Large tiles ask less of L2 (128 x 128 in bfloat16 needs 65 bytes a clock and unit, of 64 there are), small ones fill the units: the largest that gives 200 blocks.
+template <class C, auto SILU, auto GELU, auto SIGMOID, typename Args> ff_status run_act(int kind, const char* what, Args a, int64_t m, int64_t n, int act, hipStream_t stream) {
+    a.mtiles = (uint32_t)((m + C::BM - 1) / C::BM);
+    a.ntiles = (uint32_t)((n + C::BN - 1) / C::BN);
+    const dim3 grid(a.mtiles * a.ntiles);
+    return act == FF_SILU ? launch<C, SILU>(kind, what, grid, a, stream) : act == FF_GELU ? launch<C, GELU>(kind, what, grid, a, stream) : launch<C, SIGMOID>(kind, what, grid, a, stream);
+}
+template <typename T> struct Hidden {
+    typedef T Type;
+    typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 64, 64, 64 / sizeof(T), 4, 2, 2, 1, 2, 0, 0u> Small;
+    typedef Core<Bf16, 128, 64, 32, 4, 2, 2, 1, 2, 0, 0u> Medium;
+    typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 2, 0, 0u> Large;
+    template <class C> static ff_status run(const HiddenArgs& a, int64_t m, int64_t n, int act, hipStream_t stream) {
+        return run_act<C, k_tr_hidden<C, T, FF_SILU>, k_tr_hidden<C, T, FF_GELU>, k_tr_hidden<C, T, FF_SIGMOID>>(KK_TR_HIDDEN, "ff_gated_transition_forward", a, m, n, act, stream);
+    }
+};
+template <typename T, unsigned TB> struct Out {
+    typedef T Type;
+    typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 64, 64, 64 / sizeof(T), 4, 2, 2, 1, 1, 0, TB> Small;
+    typedef Core<Bf16, 128, 128, 32, 4, 2, 2, 1, 1, 0, TB> Medium;
+    typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 1, 0, TB> Large;
+    template <class C> static ff_status run(OutArgs a, int64_t m, int64_t n, int, hipStream_t stream) {
+        a.mtiles = (uint32_t)((m + C::BM - 1) / C::BM);
+        a.ntiles = (uint32_t)((n + C::BN - 1) / C::BN);
+        return launch<C, k_tr_out<C, T>>(KK_TR_OUT, "ff_gated_transition", dim3(a.mtiles * a.ntiles), a, stream);
+    }
+};
+template <typename T> struct Grad {
+    typedef T Type;
+    typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 64, 64, 64 / sizeof(T), 3, 2, 2, 2, 3, 0, 4u> Small;
+    typedef Core<Bf16, 128, 64, 32, 3, 2, 2, 2, 3, 0, 4u> Medium;
+    typedef Core<Bf16, 128, 128, 32, 3, 4, 2, 2, 3, 0, 4u> Large;
+    template <class C> static ff_status run(const GradArgs& a, int64_t m, int64_t n, int act, hipStream_t stream) {
+        return run_act<C, k_tr_grad<C, T, FF_SILU>, k_tr_grad<C, T, FF_GELU>, k_tr_grad<C, T, FF_SIGMOID>>(KK_TR_GRAD, "ff_gated_transition_backward", a, m, n, act, stream);
+    }
+};
+template <class C> bool enough(int64_t m, int64_t n) { return (m + C::BM - 1) / C::BM * ((n + C::BN - 1) / C::BN) >= 200; }
+template <class K, typename Args> ff_status tiled(int64_t m, int64_t n, const Args& a, int act, hipStream_t stream) {
+    // (float32 products are bound by their instructions, 64 cycles each: small tiles cost nothing)
+    if constexpr (sizeof(typename K::Type) == 2) {
+        if (enough<typename K::Large>(m, n)) return K::template run<typename K::Large>(a, m, n, act, stream);
+        if (enough<typename K::Medium>(m, n)) return K::template run<typename K::Medium>(a, m, n, act, stream);
+    }
+    return K::template run<typename K::Small>(a, m, n, act, stream);
+}
+
 template <typename T> ff_status forward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                         const float* mask, void* y, void* ws_, hipStream_t stream) {
-    typedef typename OpOf<T>::type Op;
-    constexpr int BK = 64 / sizeof(T), BM = Tiles<T>::M, BN = Tiles<T>::N;
-    typedef Core<Op, BM, 64, BK, 4, 2, 2, 1, 2, 0, 0u> CH;
-    typedef Core<Op, BM, BN, BK, 4, 2, 2, 1, 1, 0, 0u> CO;
-    const Sizes s = sizes_of(d);
+    const Sizes s = sizes_of(d, false);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
     if (w.status != FF_OK) return w.status;
@@ -593,12 +637,8 @@ template <typename T> ff_status forward(const ff_transition_desc& d, const void*
             const ff_status st = pack<T>(&job, 1, stream);
             if (st != FF_OK) return st;
         }
-        HiddenArgs ha{operand(as_is ? (const void*)xr : tokens, s.cp, rows, s.cp, s.esz), {w.a, w.b}, hidden, rows, rows, d.f, (int32_t)s.cp, (int32_t)s.fp,
-                      (uint32_t)((rows + CH::BM - 1) / CH::BM), (uint32_t)((s.fp + CH::BN - 1) / CH::BN)};
-        const dim3 grid(ha.mtiles * ha.ntiles);
-        ff_status st = d.act == FF_SILU   ? launch<CH, k_tr_hidden<CH, T, FF_SILU>>(KK_TR_HIDDEN, "ff_gated_transition_forward", grid, ha, stream)
-                       : d.act == FF_GELU ? launch<CH, k_tr_hidden<CH, T, FF_GELU>>(KK_TR_HIDDEN, "ff_gated_transition_forward", grid, ha, stream)
-                                          : launch<CH, k_tr_hidden<CH, T, FF_SIGMOID>>(KK_TR_HIDDEN, "ff_gated_transition_forward", grid, ha, stream);
+        const HiddenArgs ha{operand(as_is ? (const void*)xr : tokens, s.cp, rows, s.cp, s.esz), {w.a, w.b}, hidden, rows, rows, d.f, (int32_t)s.cp, (int32_t)s.fp, 0, 0};
+        ff_status st = tiled<Hidden<T>>(rows, s.fp, ha, d.act, stream);
         if (st != FF_OK) return st;
         OutArgs oa{};
         oa.a[0] = operand(hidden, s.fp, rows, s.fp, s.esz);
@@ -610,9 +650,7 @@ template <typename T> ff_status forward(const ff_transition_desc& d, const void*
         oa.residual = residual ? (const T*)residual + r0 * d.c : nullptr;
         oa.mask = mask ? mask + r0 : nullptr;
         oa.out = (T*)y + r0 * d.c;
-        oa.mtiles = (uint32_t)((rows + CO::BM - 1) / CO::BM);
-        oa.ntiles = (uint32_t)((d.c + CO::BN - 1) / CO::BN);
-        st = launch<CO, k_tr_out<CO, T>>(KK_TR_OUT, "ff_gated_transition_forward", dim3(oa.mtiles * oa.ntiles), oa, stream);
+        st = tiled<Out<T, 0u>>(rows, d.c, oa, 0, stream);
         if (st != FF_OK) return st;
     }
     return FF_OK;
@@ -634,7 +672,7 @@ struct Blocked {
     typedef Core<Bf16, 128, 128, 32, 4, 2, 2, 1, 1, 2, 1u> Small;
 };
 template <typename T> struct Turned {
-    typedef Core<typename OpOf<T>::type, Tiles<T>::M, Tiles<T>::N, 64 / sizeof(T), 4, 2, 2, 1, 1, 1, 1u> Small;
+    typedef Core<typename OpOf<T>::type, sizeof(T) == 4 ? 64 : 128, sizeof(T) == 4 ? 64 : 128, 64 / sizeof(T), 4, 2, 2, 1, 1, 1, 1u> Small;
     typedef Core<Bf16, 256, 256, 32, 4, 2, 4, 1, 1, 1, 1u> Square;
 };
 template <class C> ff_status weights(WeightArgs a, int splits, hipStream_t stream) {
@@ -645,11 +683,7 @@ template <class C> ff_status weights(WeightArgs a, int splits, hipStream_t strea
 
 template <typename T> ff_status backward(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* dy,
                                          const float* mask, void* dx, void* const (&dw)[3], int grad_dtype, bool accumulate, void* ws_, hipStream_t stream) {
-    typedef typename OpOf<T>::type Op;
-    constexpr int BK = 64 / sizeof(T), BM = Tiles<T>::M, BN = Tiles<T>::N;
-    typedef Core<Op, BM, 64, BK, 3, 2, 2, 2, 3, 0, 4u> CG;
-    typedef Core<Op, BM, BN, BK, 4, 2, 2, 1, 1, 0, 1u> CX;
-    const Sizes s = sizes_of(d);
+    const Sizes s = sizes_of(d, true);
     char* ws = (char*)ws_;
     const Weights w = weights_of<T>(d, s, w_a, w_b, w_o, ws, stream);
     if (w.status != FF_OK) return w.status;
@@ -657,9 +691,8 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
     ws += 2 * s.tokens;
     char* const hidden[3] = {ws, ws + s.hidden, ws + 2 * s.hidden};
     float* const partial = (float*)(ws + 3 * s.hidden);
-    const int kc = rows_tiles(d);
+    const int kc = rows_tiles(d, true);
     const bool as_is = (kc ? d.c == s.cp : d.c % kPad == 0) && aligned(x) && aligned(dy);
-    const char* what = "ff_gated_transition_backward";
     ff_status st = FF_OK;
     for (int64_t r0 = 0; r0 < d.rows; r0 += s.chunk) {
         const int64_t rows = std::min(s.chunk, d.rows - r0), padded = round_up(rows, kc ? 32 : kPad);
@@ -681,12 +714,9 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
                 st = pack<T>(jobs, 2, stream);
                 if (st != FF_OK) return st;
             }
-            GradArgs ga{{operand(copies ? tokens[0] : in[0], s.cp, rows, s.cp, s.esz), operand(copies ? tokens[1] : in[1], s.cp, rows, s.cp, s.esz)}, {w.a, w.b, w.o}, hidden[0],
-                        hidden[1], hidden[2], rows, padded, d.f, (int32_t)s.cp, (int32_t)s.fp, (uint32_t)((padded + CG::BM - 1) / CG::BM), (uint32_t)((s.fp + CG::BN - 1) / CG::BN)};
-            const dim3 grid(ga.mtiles * ga.ntiles);
-            st = d.act == FF_SILU   ? launch<CG, k_tr_grad<CG, T, FF_SILU>>(KK_TR_GRAD, what, grid, ga, stream)
-                 : d.act == FF_GELU ? launch<CG, k_tr_grad<CG, T, FF_GELU>>(KK_TR_GRAD, what, grid, ga, stream)
-                                    : launch<CG, k_tr_grad<CG, T, FF_SIGMOID>>(KK_TR_GRAD, what, grid, ga, stream);
+            const GradArgs ga{{operand(copies ? tokens[0] : in[0], s.cp, rows, s.cp, s.esz), operand(copies ? tokens[1] : in[1], s.cp, rows, s.cp, s.esz)}, {w.a, w.b, w.o},
+                              hidden[0], hidden[1], hidden[2], rows, padded, d.f, (int32_t)s.cp, (int32_t)s.fp, 0, 0};
+            st = tiled<Grad<T>>(padded, s.fp, ga, d.act, stream);
         }
         if (st != FF_OK) return st;
         const Operand ox = operand(copies ? tokens[0] : in[0], s.cp, rows, s.cp, s.esz), ody = operand(copies ? tokens[1] : in[1], s.cp, rows, s.cp, s.esz);
@@ -709,9 +739,7 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
         oa.cols = d.c;
         oa.rows = rows;
         oa.out = (T*)dx + r0 * d.c;
-        oa.mtiles = (uint32_t)((rows + CX::BM - 1) / CX::BM);
-        oa.ntiles = (uint32_t)((d.c + CX::BN - 1) / CX::BN);
-        st = launch<CX, k_tr_out<CX, T>>(KK_TR_OUT, what, dim3(oa.mtiles * oa.ntiles), oa, stream);
+        st = tiled<Out<T, 1u>>(rows, d.c, oa, 0, stream);
         if (st != FF_OK) return st;
     }
     JoinArgs ja{partial, {dw[0], dw[1], dw[2]}, d.f, d.c, (int32_t)s.fp, (int32_t)s.cp, d.rows ? s.splits : 0, accumulate};
@@ -725,17 +753,17 @@ template <typename T> ff_status backward(const ff_transition_desc& d, const void
 }  // namespace
 
 size_t transition_forward_workspace(const ff_transition_desc& d) {
-    if (const int kc = rows_tiles(d)) return std::max<size_t>(256, 3 * align256((size_t)(round_up(d.f, 32) * kc * 64)));
-    const Sizes s = sizes_of(d);
+    if (const int kc = rows_tiles(d, false)) return std::max<size_t>(256, 3 * align256((size_t)(round_up(d.f, 32) * kc * 64)));
+    const Sizes s = sizes_of(d, false);
     return 3 * s.weight + s.tokens + s.hidden;
 }
 size_t transition_backward_workspace(const ff_transition_desc& d) {
-    const Sizes s = sizes_of(d);
+    const Sizes s = sizes_of(d, true);
     return 3 * s.weight + 2 * s.tokens + 3 * s.hidden + s.partial;
 }
 ff_status transition_forward_run(const ff_transition_desc& d, const void* x, const void* w_a, const void* w_b, const void* w_o, const void* residual,
                                  const float* mask, void* y, void* ws, hipStream_t stream) {
-    if (const int kc = rows_tiles(d)) return forward_rows(d, kc, x, w_a, w_b, w_o, residual, mask, y, ws, stream);
+    if (const int kc = rows_tiles(d, false)) return forward_rows(d, kc, x, w_a, w_b, w_o, residual, mask, y, ws, stream);
     return d.dtype == FF_F32 ? forward<float>(d, x, w_a, w_b, w_o, residual, mask, y, ws, stream)
                              : forward<bf16_t>(d, x, w_a, w_b, w_o, residual, mask, y, ws, stream);
 }

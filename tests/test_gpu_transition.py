@@ -63,7 +63,11 @@ class Problem:
             assert np.all(off <= e), f"{name}: {(off / e).max():.2f} of the bound at {np.unravel_index(np.argmax(off / e), off.shape)}"
 
 
-SIZES = [(1, 1, 1), (1, 16, 16), (3, 7, 5), (40, 64, 128), (129, 33, 70), (300, 96, 64), (257, 128, 512), (130, 256, 160), (200, 200, 312), (64, 520, 48), (300, 300, 96), (100, 32, 33), (161, 192, 256), (500, 256, 300), (400, 64, 288), (300, 512, 272)]
+SIZES = [(1, 1, 1), (1, 16, 16), (3, 7, 5), (40, 64, 128), (129, 33, 70), (300, 96, 64), (257, 128, 512), (130, 256, 160), (200, 200, 312), (64, 520, 48), (300, 300, 96), (100, 32, 33), (161, 192, 256), (500, 256, 300), (400, 64, 288), (300, 512, 272),
+         # few hidden channels, or many rows: rows in registers
+         (2000, 250, 61), (1500, 190, 100), (700, 256, 64), (520, 192, 96), (4000, 96, 130), (9000, 128, 512),
+         # every tile of the other kernels
+         (7000, 320, 1040), (3000, 272, 544)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -152,7 +156,7 @@ def test_gradients_are_added(dtype, grad):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_more_rows_than_are_worked_on_at_a_time(dtype):
-    """Rows of several chunks: each row's results are those of the row among few others, the weights' gradients the sums of parts."""
+    """Rows of several chunks: each row's results are the oracle's, the weights' gradients the sums of parts."""
     c, f = 16, 2048
     rows = (512 << 20) // (f * (4 if dtype == "f32" else 2)) + 300
     p = Problem(rows, c, f, dtype)
@@ -161,15 +165,19 @@ def test_more_rows_than_are_worked_on_at_a_time(dtype):
     q = Problem(400, c, f, dtype)
     q.w, q.x, q.dy = p.w, p.x[part].contiguous(), p.dy[part].contiguous()
     q.check_forward(y[part])
-    assert torch.equal(q.forward(), y[part]) and torch.equal(q.backward()[0], dx[part])
+    ws, qx, qdy = [n64(w) for w in q.w], n64(q.x), n64(q.dy)
+    off, bound = np.abs(n64(dx[part]) - T.backward(qx, *ws, qdy, "silu")[0]), T.backward_bound(qx, *ws, qdy, "silu", HALF[q.x.dtype], HALF[q.x.dtype])[0]
+    assert np.all(off <= bound)
     total = [torch.zeros(w.shape, dtype=torch.float64, device=DEV) for w in p.w]
     for at in range(0, rows, 20000):
         q.x, q.dy = p.x[at:at + 20000].contiguous(), p.dy[at:at + 20000].contiguous()
         for t, g in zip(total, q.backward(grad_dtype=torch.float32)[1:]):
             t += g
+    # Float32 sums over the rows, of terms of any sign: 8 deviations.  Fewer rows may take other kernels, whose a, b and dh differ by some 18 U each, h, da and db by e = 64 U: of
+    # bfloat16 values a share 2 e / 2^-8 = 2 10^-3 then falls on the other side of a border and differs by a step, 2^-7 (2 10^-3)^(1/2) = 3.5 10^-4 of the norm.
+    other = 3.5e-4 if dtype == "bf16" else 64 * T.U
     for t, g in zip(total, dw):
-        # (the same rounded operands on both sides; float32 sums over the rows, of terms of any sign: 8 deviations)
-        assert (g - t).norm() <= 8 * T.U * rows ** 0.5 * t.norm()
+        assert (g - t).norm() <= (8 * T.U * rows ** 0.5 + other) * t.norm()
 
 
 def test_equal_calls_give_equal_bits():
