@@ -709,26 +709,30 @@ def make_muon_plan(params, grads, m, master=None, weight_decay=0.0) -> MuonPlan:
         raise ValueError("a plan needs a tensor")
     count, device = len(params), params[0].device
     dtypes = {"p": params[0].dtype, "g": grads[0].dtype, "m": torch.float32, "master": torch.float32}
-    shapes = [tuple(t.shape) for t in params]
+    shapes = [t.shape for t in params]
     for i, s in enumerate(shapes):
         if len(s) != 2:
             raise ValueError(f"tensor {i} has shape {list(s)}: it is no matrix")
-        if max(s) > 32768:
+        if s[0] > 32768 or s[1] > 32768:
             raise ValueError(f"tensor {i} has shape {list(s)}: rows and columns go up to 32768")
     table = np.zeros(count, np.dtype(MuonTensor))
     for name, ts in lists.items():
         if len(ts) != count:
             raise ValueError(f"{len(ts)} tensors of {name} for {count} parameters")
-        for t, s in zip(ts, shapes):
-            if t.dtype != dtypes[name]:
-                raise TypeError(f"{name} is {t.dtype}, not {dtypes[name]}")
-            if tuple(t.shape) != s:
-                raise ValueError(f"{name} has shape {list(t.shape)}, not {list(s)}")
-            if not t.is_cuda or t.device != device:
-                raise ValueError(f"{name} is on {t.device}, not on {device if device.type == 'cuda' else 'a GPU'}")
-            if not t.is_contiguous():
-                raise ValueError(f"{name} is not contiguous")
-        table[name] = [t.data_ptr() for t in ts]
+        other = {t.dtype for t in ts} - {dtypes[name]}
+        if other:
+            raise TypeError(f"{name} is {other.pop()}, not {dtypes[name]}")
+        # (all at once: a model has thousands of matrices)
+        if [t.shape for t in ts] != shapes:
+            t, s = next((t, s) for t, s in zip(ts, shapes) if t.shape != s)
+            raise ValueError(f"{name} has shape {list(t.shape)}, not {list(s)}")
+        table[name] = list(map(torch.Tensor.data_ptr, ts))
+    for name, ts in lists.items():
+        other = {t.device for t in ts} - ({device} if device.type == "cuda" else set())
+        if other:
+            raise ValueError(f"{name} is on {other.pop()}, not on {device if device.type == 'cuda' else 'a GPU'}")
+        if not all(map(torch.Tensor.is_contiguous, ts)):
+            raise ValueError(f"{name} is not contiguous")
     table["rows"], table["cols"] = [s[0] for s in shapes], [s[1] for s in shapes]
     if np.ndim(weight_decay) and len(weight_decay) != count:
         raise ValueError(f"{len(weight_decay)} values of weight_decay for {count} parameters")

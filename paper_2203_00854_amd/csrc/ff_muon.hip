@@ -30,6 +30,7 @@ namespace {
 
 constexpr float kScale = 256.f, kUnscale = 1.f / 256.f;
 constexpr int kPad = 16;
+constexpr int kMostBlocks = 1 << 22;             // of a launch: 2^32 threads a grid
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 4096;                     // values that a block of the element-wise kernels holds
 constexpr int64_t kBatch = 1 << 30;            // workspace of the matrices that are worked on together, unless one alone needs more
@@ -716,9 +717,13 @@ template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, 
 }
 // `count` matrices of a size from `first` on, a block each
 template <typename G, typename P, int LAST> ff_status small(const Table& t, int size, int first, int count, const StepArgs& a, int steps, const float* norm, hipStream_t stream) {
-    if (count == 0) return FF_OK;
-    if (size == 64) return go<k_ns_small<64, LAST, G, P>>(KK_NS_SMALL, count, Small<64>::kThreads, Small<64>::kLds, stream, kWhat<LAST>, t, first, steps, a, norm);
-    return go<k_ns_small<128, LAST, G, P>>(KK_NS_SMALL, count, Small<128>::kThreads, Small<128>::kLds, stream, kWhat<LAST>, t, first, steps, a, norm);
+    for (; count > 0; first += kMostBlocks, count -= kMostBlocks) {
+        const int n = std::min(count, kMostBlocks);
+        const ff_status st = size == 64 ? go<k_ns_small<64, LAST, G, P>>(KK_NS_SMALL, n, Small<64>::kThreads, Small<64>::kLds, stream, kWhat<LAST>, t, first, steps, a, norm)
+                                        : go<k_ns_small<128, LAST, G, P>>(KK_NS_SMALL, n, Small<128>::kThreads, Small<128>::kLds, stream, kWhat<LAST>, t, first, steps, a, norm);
+        if (st != FF_OK) return st;
+    }
+    return FF_OK;
 }
 
 // ---- a plan: header, batches, matrices, places -------------------------------------------------

@@ -16,7 +16,8 @@ using tile::round_up;
 namespace {
 
 constexpr int kPad = 16;                       // rows and columns of the products' inner dimensions are padded to this with zeros
-constexpr int64_t kHiddenBytes = 512 << 20;    // of one hidden tensor of a chunk of rows: more rows keep the units busier (701 x 701 x 128, f 512: 979 us in chunks of 64 MiB, 881 in one)
+constexpr int64_t kMostRows = 1 << 30;          // of a launch: two threads a row, 2^32 threads a grid
+constexpr int64_t kHiddenBytes = 512 << 20;    // of one hidden tensor (of tokens, where they are wider) of a chunk of rows: more rows keep the units busier (701 x 701 x 128, f 512: 979 us in chunks of 64 MiB, 881 in one)
 
 template <typename T> struct OpOf;
 template <> struct OpOf<float> { typedef F32 type; };
@@ -464,7 +465,7 @@ Sizes sizes_of(const ff_transition_desc& d, bool backward) {
     const int kc = rows_tiles(d, backward);
     s.cp = kc ? kc * 32 : round_up(d.c, kPad);
     s.fp = round_up(d.f, kc ? 32 : kPad);
-    const int64_t most = std::max<int64_t>(128, kHiddenBytes / (s.fp * s.esz) / 128 * 128);
+    const int64_t most = std::max<int64_t>(128, kHiddenBytes / (std::max(s.fp, s.cp) * s.esz) / 128 * 128);
     s.chunk = std::min(most, round_up(std::max<int64_t>(d.rows, 1), 128));
     s.chunks = (d.rows + s.chunk - 1) / s.chunk;
     s.weight = align256((size_t)s.fp * s.cp * s.esz);
@@ -559,15 +560,19 @@ ff_status forward_rows(const ff_transition_desc& d, int kc, const void* x, const
         const ff_status st = pack<bf16_t>(jobs, 3, stream);
         if (st != FF_OK) return st;
     }
-    const RowsArgs a{(const bf16_t*)x, (const bf16_t*)residual, (const char*)from[0], (const char*)from[1], (const char*)from[2], mask, (bf16_t*)y, d.rows, (int32_t)fp, d.c,
-                     (int32_t)(fp * 2), d.c == cp && aligned(x) && aligned(residual) && aligned(y)};
-    switch (kc) {
-        case 1: return launch_rows<1>(d.act, a, stream);
-        case 2: return launch_rows<2>(d.act, a, stream);
-        case 4: return launch_rows<4>(d.act, a, stream);
-        case 6: return launch_rows<6>(d.act, a, stream);
-        default: return launch_rows<8>(d.act, a, stream);
+    const bool whole = d.c == cp && aligned(x) && aligned(residual) && aligned(y);
+    for (int64_t r0 = 0; r0 < d.rows; r0 += kMostRows) {
+        const auto at = [&](const void* t) { return t ? (const bf16_t*)t + r0 * d.c : nullptr; };
+        const RowsArgs a{at(x), at(residual), (const char*)from[0], (const char*)from[1], (const char*)from[2], mask ? mask + r0 : nullptr, (bf16_t*)at(y), std::min(kMostRows, d.rows - r0),
+                         (int32_t)fp, d.c, (int32_t)(fp * 2), whole};
+        const ff_status st = kc == 1   ? launch_rows<1>(d.act, a, stream)
+                             : kc == 2 ? launch_rows<2>(d.act, a, stream)
+                             : kc == 4 ? launch_rows<4>(d.act, a, stream)
+                             : kc == 6 ? launch_rows<6>(d.act, a, stream)
+                                       : launch_rows<8>(d.act, a, stream);
+        if (st != FF_OK) return st;
     }
+    return FF_OK;
 }
 
 // ---- tiled products: the kernel of each tile size, and the choice among them -----------------------

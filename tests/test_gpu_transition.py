@@ -180,6 +180,34 @@ def test_more_rows_than_are_worked_on_at_a_time(dtype):
         assert (g - t).norm() <= (8 * T.U * rows ** 0.5 + other) * t.norm()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,f", [(33, 20, 17), (100, 128, 32), (70, 300, 40), (2000, 250, 61)])
+def test_memory_around_the_results_is_left_alone(rows, c, f, dtype):
+    p = Problem(rows, c, f, dtype, masked=True, residual=True)
+    around = lambda *shape: torch.full((int(np.prod(shape)) + 200,), 7.0, device=DEV, dtype=p.x.dtype)  # noqa: E731
+    inside = lambda flat, *shape: flat[100:100 + int(np.prod(shape))].view(*shape)  # noqa: E731
+    shapes = [(rows, c), (rows, c), (f, c), (f, c), (c, f)]
+    flat = [around(*s) for s in shapes]
+    y, dx, *dw = (inside(t, *s) for t, s in zip(flat, shapes))
+    p.check_forward(p.forward(out=y))
+    p.check_backward(p.backward(dx=dx, dw_a=dw[0], dw_b=dw[1], dw_o=dw[2]))
+    for t, s in zip(flat, shapes):
+        assert bool((t[:100] == 7).all()) and bool((t[100 + int(np.prod(s)):] == 7).all())
+
+
+def test_wide_tokens_and_few_hidden_channels():
+    """Rows of 16 KiB beside one hidden channel: as many at a time as 512 MiB hold."""
+    for dtype in ("bf16", "f32"):
+        p = Problem(40000, 8192, 1, dtype)
+        y, (dx, *dw) = p.forward(), p.backward()
+        q = Problem(50, 8192, 1, dtype)
+        q.w, q.x, q.dy = p.w, p.x[-50:].contiguous(), p.dy[-50:].contiguous()
+        q.check_forward(y[-50:])
+        off = np.abs(n64(dx[-50:]) - T.backward(n64(q.x), *map(n64, q.w), n64(q.dy), "silu")[0])
+        assert np.all(off <= T.backward_bound(n64(q.x), *map(n64, q.w), n64(q.dy), "silu", HALF[q.x.dtype], HALF[q.x.dtype])[0])
+        assert all(t.isfinite().all() for t in (y, dx, *dw))
+
+
 def test_equal_calls_give_equal_bits():
     p = Problem(5000, 128, 256, "bf16", masked=True, residual=True)
     y, grads = p.forward(), p.backward()
