@@ -3,7 +3,7 @@
     X = G / (|G| + eps);  A = X X^T;  X = a X + (b A + c A^2) X
     m = beta m + (1 - beta) k g;  u = m or beta m + (1 - beta) k g;  w = w - lr (decay w + s O(u))
 
-`noise` (a generator) puts into every operation what float32 sums and 24-bit values would: `roundings` of the result then tells how far off an
+`noise` (a generator) puts into every operation what float32 sums and values of 23 bits, held as pairs of float16, would: `roundings` of the result then tells how far off an
 implementation with such roundings may be, however the polynomial spreads them.
 """
 import numpy as np
@@ -22,7 +22,7 @@ def _product(p, q, noise):
 
 
 def _held(z, noise):
-    """As a pair of float16 values of 256 times z: 24 bits, or the smallest step, 2^-25 of a unit."""
+    """As a pair of float16 values of 256 times z: off by up to 2^-23 of z, 2^-24 or less in the mean, or by the smallest step, 2^-25 of a unit."""
     return z if noise is None else z + (U * np.abs(z) + 2.0 ** -33) * noise.normal(size=z.shape)
 
 

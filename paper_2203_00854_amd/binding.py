@@ -752,7 +752,7 @@ def ff_muon_step(plan: MuonPlan, lr: float, beta: float = 0.95, nesterov: bool =
     sqrt(max(rows, cols)).  norm (ff_grad_norm's result) and max_norm clip the gradients; a norm that is not finite leaves everything as it
     was.  The plan's own workspace serves one stream at a time; give ws for another.  Captured into a graph the call keeps its numbers as they are."""
     a, b, c = coefficients
-    hyper = MuonHyper(lr, beta, 0.0 if max_norm is None else max_norm, a, b, c, eps, steps, 1 if nesterov else 0, _named(SCALES, scale, "scale"))
+    hyper = MuonHyper(lr, beta, 0.0 if max_norm is None else max_norm, a, b, c, eps, min(max(steps, 0), 1000), 1 if nesterov else 0, _named(SCALES, scale, "scale"))
     _done(calls().muon_step(C.addressof(plan.desc), plan.host.ctypes.data, plan.plan, C.addressof(hyper), norm, max_norm, plan.ws if ws is None else ws, plan.stream))
 
 

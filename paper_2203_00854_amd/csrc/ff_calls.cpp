@@ -5,6 +5,8 @@
 // signatures and defaults) and return the results, or ff_status as a number where the library refuses the call.
 #include <Python.h>
 
+#include <algorithm>
+
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPCachingAllocator.h>
@@ -345,7 +347,7 @@ PyObject* orthogonalise(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (x.dim() < 2 || x.size(-1) < 1 || x.size(-2) < 1) value_error("no matrices in shape ", x.sizes());
         const int64_t rows = x.size(-2), cols = x.size(-1), count = x.numel() / (rows * cols);
         if (rows > INT32_MAX || cols > INT32_MAX || count > INT32_MAX) value_error("too many values in shape ", x.sizes());
-        const ff_orthogonalise_desc desc{dtype == at::kFloat ? FF_F32 : FF_BF16, (int32_t)count, (int32_t)rows, (int32_t)cols, (int32_t)std::min(steps, 1000l), p[0], p[1], p[2], p[3]};
+        const ff_orthogonalise_desc desc{dtype == at::kFloat ? FF_F32 : FF_BF16, (int32_t)count, (int32_t)rows, (int32_t)cols, (int32_t)std::clamp(steps, 0l, 1000l), p[0], p[1], p[2], p[3]};
         ff_status status;
         {
             Unlocked unlocked;

@@ -5,7 +5,7 @@
 // Three launches a step for all matrices together: A; B = a I + b A + c A^2; X = B X.  With a I inside B the last product needs its operands alone; few
 // tiles hold C = b I + c A beside A, so that B = a I + A C does too: what it had to add otherwise would be another read in a short kernel's last microseconds.  Many
 // tiles do not (A is as large as X where that is square, and memory bounds them).  Values are held as float16 pairs of kScale times
-// themselves: 24 significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  Magnitudes
+// themselves: 23 significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  Magnitudes
 // to 255 have a place, and singular values are at most 1 at the start and below 1.3 after any number of steps with the usual coefficients; 2^-33 is
 // the smallest step between small values.  A tall matrix is worked on as it lies: its operands are read turned.
 #include "ff_tile.h"
@@ -696,11 +696,15 @@ template <int LAST, typename P> ff_status apply(const Tables& t, int which, cons
 // A and C of X, B of both
 template <class C> ff_status gram(const Tables& t, int which, const StepArgs& a, char* ws, hipStream_t stream, const char* what) {
     ff_status st;
-    if (C::TILE == 64 && t.splits > 1) {
-        st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, which, a, t.parts);
-        if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, a, (const float*)t.parts, t.splits);
+    const auto whole = [&] { return go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, which, a, (float*)nullptr); };
+    if constexpr (C::TILE == 64) {
+        if (t.splits > 1) {
+            st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, which, a, t.parts);
+            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, a, (const float*)t.parts, t.splits);
+        } else
+            st = whole();
     } else
-        st = go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, which, a, (float*)nullptr);
+        st = whole();
     return st != FF_OK ? st : go<k_ns_poly<C>>(KK_NS_POLY, t.tris, 256, C::kLds, stream, what, t.tri, ws, a);
 }
 template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, const StepArgs& a, int steps, const float* norm, char* ws, hipStream_t stream) {

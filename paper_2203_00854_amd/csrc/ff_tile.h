@@ -2,7 +2,7 @@
 // stages deep.  Shared by the gated transition and the orthogonalisation.
 //
 // Three kinds of operands: bfloat16; float32 (32x32x2 float32 instructions); float16 pairs, where a value is hi + lo, each rounded to nearest
-// (24 significant bits together), and a product hi hi + hi lo + lo hi: what it leaves out, lo lo, is 2^-24 of it at most.
+// (an error of 2^-23 of the value at most, together), and a product hi hi + hi lo + lo hi: what it leaves out, lo lo, is 2^-22 of it at most and of either sign.
 // In memory sixteen values of a pair's hi part are followed by their lo parts, so that a row is as contiguous as one of 4-byte values.
 // An operand lies in memory with k contiguous, [m][k], or "turned", [k][m]; the reads from LDS turn it back.
 //
@@ -13,6 +13,8 @@
 #pragma once
 
 #include "ff_common.h"
+
+#include <atomic>
 
 namespace ff {
 namespace tile {
@@ -404,10 +406,15 @@ struct Core {
     static __device__ __forceinline__ Nothing none(int64_t, int64_t) { return {}; }
 };
 
-// once for each kernel that needs more than 64 KiB
+// once for each device and each kernel that needs more than 64 KiB (a device beyond 64: at each call)
 template <auto KERNEL> static void allow_lds() {
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    (void)once;
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    (void)hipGetDevice(&device);
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return;
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    done.fetch_or(bit, std::memory_order_relaxed);
 }
 
 // Blocks of the same rows of A run one after another on one XCD (block i starts on XCD i % 8), whose L2 then holds them, while B is small enough for all.

@@ -1,6 +1,6 @@
 """GPU parity of ff_orthogonalise and ff_muon_step.
 
-The tolerance of an orthogonalised matrix is what the float64 oracle shows roundings of float32 sums and 24-bit values to grow to (oracle/muon.py: eight deviations of evaluations
+The tolerance of an orthogonalised matrix is what the float64 oracle shows roundings of float32 sums and values of 23 bits grow to (oracle/muon.py: eight deviations of evaluations
 with random roundings), plus the rounding of the result; momentum counts its four operations.
 """
 import numpy as np
@@ -51,6 +51,18 @@ def test_arguments(kw):
     for rows, cols in ((48, 33), (33, 48)):
         x = matrices(1, rows, cols, "f32")[0]
         check(n64(P.ff_orthogonalise(x, **kw)), n64(x), M.U, **kw)
+
+
+def test_numbers_of_steps_that_are_none():
+    x = matrices(1, 24, 50, "f32")[0]
+    model = Model([(3, 4)], "f32", "f32")
+    before = model.all()
+    for steps in (0, -1, 65, 5 - 2 ** 32, 5 + 2 ** 32):
+        with pytest.raises(P.FFError):
+            P.ff_orthogonalise(x, steps=steps)
+        with pytest.raises(P.FFError):
+            P.ff_muon_step(model.plan, 0.02, steps=steps)
+    assert all(torch.equal(a, b) for a, b in zip(before, model.all()))
 
 
 def test_sizes_of_values():
