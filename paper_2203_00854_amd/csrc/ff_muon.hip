@@ -33,7 +33,8 @@ constexpr int kPad = 16;
 constexpr int kMostBlocks = 1 << 22;             // of a launch: 2^32 threads a grid
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 4096;                     // values that a block of the element-wise kernels holds
-constexpr int64_t kBatch = 1 << 30;            // workspace of the matrices that are worked on together, unless one alone needs more
+constexpr int kFewSmall = 64;                    // small matrices beside large ones: so few are tiles more in the large ones' launches instead of a launch of 25 us behind them
+constexpr int64_t kBatch = 1 << 30;              // workspace of the matrices that are worked on together, unless one alone needs more
 
 // One matrix, as the kernels see it.
 struct Matrix {
@@ -225,20 +226,21 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
 }
 
 // ---- the products --------------------------------------------------------------------------
-template <int TILE_, int STAGES> struct Cores {
+template <int TILE_, int BK, int STAGES, int BLOCKS, bool BESIDE> struct Cores {
     static constexpr int TILE = TILE_;
-    typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 0, 0u> Straight;        // rows by rows
-    typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 1, 1u> Turned;          // columns by columns
-    typedef Core<Pair, TILE, TILE, 16, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;           // rows by columns
-    static constexpr bool kBeside = STAGES > 3;                                                 // C is held beside A
-    static constexpr int kBlocks = TILE == 128 && STAGES == 3 ? 3 : TILE == 64 ? 2 : 1;        // on a compute unit
+    typedef Core<Pair, TILE, TILE, BK, STAGES, 2, 2, 1, 1, 0, 0u> Straight;        // rows by rows
+    typedef Core<Pair, TILE, TILE, BK, STAGES, 2, 2, 1, 1, 1, 1u> Turned;          // columns by columns
+    typedef Core<Pair, TILE, TILE, BK, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;           // rows by columns
+    static constexpr bool kBeside = BESIDE;                                        // C is held beside A
+    static constexpr int kBlocks = BLOCKS;                                         // on a compute unit
     static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 };
-// Three stages leave room for three blocks on a compute unit, whose ends then overlap with the others' products; eight for one, where a launch has fewer blocks than
-// there are units (a stage takes 0.18 us of matrix instructions and 0.8 us to arrive).  Fewer still, and tiles of 64 fill four times the units.
-typedef Cores<128, 3> Many;
-typedef Cores<128, 8> Some;
-typedef Cores<64, 8> Few;
+// Three stages of 16 k leave room for three blocks on a compute unit, whose ends then overlap with the others' products.  Where a launch has fewer blocks than there are
+// units a block stands alone with what a stage costs it, a barrier and the reads behind it, so that stages of 32 k are better (orthogonalising 4096 x 1024: eight of 16 k
+// 434 us, five of 32 383, four 374; of 64 k for the smaller tiles 390).  Fewer blocks still, and tiles of 64 fill four times the units.
+typedef Cores<128, 16, 3, 3, false> Many;
+typedef Cores<128, 32, 4, 1, true> Some;
+typedef Cores<64, 32, 4, 2, true> Few;
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
     return {ws + x.x(which), x.cp() * 4, x.rp(), (int32_t)(x.cp() * 4)};
@@ -795,7 +797,7 @@ struct Made {
     int64_t ws = 256;
     int small = 0, smaller = 0;
 };
-// Large matrices first, so that small ones fill the end; a batch ends where its workspace would pass kBatch.
+// Large matrices first, so that small ones fill the end; a batch ends where its workspace would pass kBatch (but for small ones, which are worked on with large ones where they are few).
 Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
     Made r;
     for (int i = 0; i < d.n_tensors; ++i)
@@ -807,6 +809,10 @@ Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
         r.small += small_of(m) == 128;
         r.smaller += small_of(m) == 64;
     }
+    if (large > 0 && r.small + r.smaller <= kFewSmall) {
+        large += r.small + r.smaller;
+        r.small = r.smaller = 0;
+    }
     for (int first = 0; first < large;) {
         Batch b{};
         b.piece0 = (int32_t)r.piece.size();
@@ -814,7 +820,7 @@ Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
         b.app0 = (int32_t)r.app.size();
         int last = first;
         int64_t tris = 0, apps = 0, few = 0, longest = 0, room = 0;
-        for (; last < large && (last == first || room + r.matrices[last].bytes(false) <= kBatch); ++last) {
+        for (; last < large && (last == first || room + r.matrices[last].bytes(false) <= kBatch || small_of(r.matrices[last])); ++last) {
             const Matrix& m = r.matrices[last];
             room += (int64_t)align256((size_t)m.bytes(false));
             tris += tris_of(m, 128);
