@@ -117,7 +117,8 @@ struct Operand {
     int32_t bytes;
 };
 
-template <class Op_, int BM_, int BN_, int BK_, int STAGES_, int WM_, int WN_, int NA_, int NB_, int TA_, unsigned TB_>
+// WK: wavefronts that share a tile's k, round by round; their sums are joined in LDS in a fixed order, and the first ones hold them.
+template <class Op_, int BM_, int BN_, int BK_, int STAGES_, int WM_, int WN_, int NA_, int NB_, int TA_, unsigned TB_, int WK_ = 1>
 struct Core {
     typedef Op_ Op;
     typedef typename Op::Frag Frag;
@@ -125,18 +126,20 @@ struct Core {
     static constexpr int TA = TA_;                                 // A is turned (1) or blocked (2)
     static_assert(TA < 2 || (Op_::kStep == 16 && Op_::kPlanes == 1 && BK_ == 32), "blocks of 32 rows");
     static constexpr unsigned TB = TB_;                            // bit b: operand b of the B side is turned
-    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int WK = WK_;
+    static constexpr int kWaves = WM * WN * WK, kThreads = 64 * kWaves;
     static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
     static constexpr int kBytesA = BM * BK * Op::kSize, kBytesB = BN * BK * Op::kSize, kStage = NA * kBytesA + NB * kBytesB;
     static constexpr int kLoads = kStage / 16 / kThreads;          // of a wavefront, for one stage
     static_assert(kBytesA % (16 * kThreads) == 0 && kBytesB % (16 * kThreads) == 0, "the wavefronts count the same loads");
-    static_assert(!(TA || TB) || BM >= 64, "turned rows hold sixteen slots (bfloat16: eight)");
+    static_assert(BK % (2 * WK * Op::kStep) == 0 || WK == 1, "the wavefronts of a tile have two rounds of a stage each, or more");
     static_assert(MT >= 1 && NT >= 1 && BK % Op::kStep == 0, "tile");
 
     // LDS images: rows of W slots of sixteen bytes; a row's slots are exchanged by a rule on the row, so that what one cycle reads (256 bytes) lies in
     // banks of its own: sixteen bytes of sixteen rows, or, turned, of 32 columns' values in four rows (of a pair's, two pieces 64 bytes apart).
     template <int T, int W> static __device__ __forceinline__ int swizzle(int row) {
         if constexpr (!T) return W >= 16 ? row & 15 : W == 8 ? row >> 1 & 7 : W == 4 ? row >> 2 & 3 : 0;
+        else if constexpr (W < (Op::kStep == 8 ? 16 : 8)) return 0;      // (tiles of 32: four rows of 64 bytes lie in banks of their own as they are)
         else if constexpr (Op::kStep == 8) return row << 1 & 8;
         else if constexpr (Op::kPlanes == 2) return (row & 1) << 1 | (row & 2) << 2;
         else return W >= 16 ? 4 * (row & 3) : 4 * (row >> 1 & 1);
@@ -276,10 +279,10 @@ struct Core {
     static __device__ __forceinline__ void run(f32x16 (&acc)[NB][MT][NT], const Operand* a, const Operand* b, int64_t m0, int64_t n0, int64_t from, int64_t to,
                                                unsigned char* smem) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        const int wm = wave / WN, wn = wave % WN;
+        const int wk = WK == 1 ? 0 : wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
         const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
         if (from >= to) return;
-        constexpr int R = BK / Op::kStep;
+        constexpr int R = BK / Op::kStep / WK;                   // rounds of a wavefront: WK s + wk
         const int stages = (int)((to - from + BK - 1) / BK), whole = (int)((to - from) / BK);
         const Loads loads(a, b, m0, n0);
 #pragma unroll
@@ -288,7 +291,7 @@ struct Core {
         // Operands of the next round are read while a round's products run, so a stage has to be there one turn early.
         Frags f[2];
         arrive(stages - 1 < STAGES - 2 ? stages - 1 : STAGES - 2);
-        read(f[0], smem, wm, wn, 0, lane);
+        read(f[0], smem, wm, wn, wk, lane);
         int buf = 0, t = 0;
         const auto turn = [&](Frags& now, Frags& then) {
             // the next stage is there, and nobody reads the one before any more, in whose place the loads of the one STAGES - 1 ahead go
@@ -300,8 +303,8 @@ struct Core {
 #pragma unroll
             for (int s = 0; s < R; ++s) {
                 Frags &mine = s & 1 ? then : now, &other = s & 1 ? now : then;
-                if (s + 1 < R) read(other, image, wm, wn, s + 1, lane);
-                else read(other, image_next, wm, wn, 0, lane);             // (of the last stage's successor: what lies there, for no product)
+                if (s + 1 < R) read(other, image, wm, wn, WK * (s + 1) + wk, lane);
+                else read(other, image_next, wm, wn, wk, lane);            // (of the last stage's successor: what lies there, for no product)
                 __builtin_amdgcn_sched_barrier(0);                         // the reads before the products, or they would be waited for right behind them
                 multiply(acc, mine);
                 __builtin_amdgcn_sched_barrier(0);
@@ -321,11 +324,47 @@ struct Core {
         } else
             while (t < whole) turn(f[0], f[1]);
         const int rest = (int)((to - from) - (int64_t)whole * BK) / Op::kStep;
-        for (int s = 0; s < rest; ++s) {
+        for (int s = wk; s < rest; s += WK) {
             multiply(acc, f[0]);
-            if (s + 1 < rest) read(f[0], smem + buf * kStage, wm, wn, s + 1, lane);
+            if (s + WK < rest) read(f[0], smem + buf * kStage, wm, wn, s + WK, lane);
         }
         barrier();
+    }
+    // the sums of the wavefronts that share k, in the first of them; smem as for run
+    static __device__ __forceinline__ void join(f32x16 (&acc)[NB][MT][NT], unsigned char* smem) {
+        if constexpr (WK > 1) {
+            static_assert((WK - 1) * WM * WN * NB * MT * NT * 4096 <= STAGES * kStage, "room");
+            const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, wk = wave / (WM * WN), tile = wave % (WM * WN);
+            const auto at = [&](int k, int b, int m, int n, int g) { return (float4*)smem + ((((((k - 1) * WM * WN + tile) * NB + b) * MT + m) * NT + n) * 4 + g) * 64 + lane; };
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            if (wk > 0) *at(wk, b, m, n, g) = make_float4(acc[b][m][n][4 * g], acc[b][m][n][4 * g + 1], acc[b][m][n][4 * g + 2], acc[b][m][n][4 * g + 3]);
+            barrier();
+            if (wk == 0)
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                                for (int k = 1; k < WK; ++k) {
+                                    const float4 v = *at(k, b, m, n, g);
+                                    acc[b][m][n][4 * g] += v.x;
+                                    acc[b][m][n][4 * g + 1] += v.y;
+                                    acc[b][m][n][4 * g + 2] += v.z;
+                                    acc[b][m][n][4 * g + 3] += v.w;
+                                }
+            barrier();
+        }
     }
     // waits until all but the loads of the youngest N stages have arrived, for every wavefront, and for its own reads
     template <int N> static __device__ __forceinline__ void arrive() {
@@ -353,20 +392,22 @@ struct Core {
     // thread is done with, before and after
     template <typename Fetch, typename F> static __device__ __forceinline__ void rows(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, Fetch fetch, F body) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-        float* out = (float*)smem + (wave / WN * 32 + (lane & 31)) * kPitch + (wave % WN * NT) * 32 + 4 * (lane >> 5);
+        float* out = (float*)smem + (wave / WN % WM * 32 + (lane & 31)) * kPitch + (wave % WN * NT) * 32 + 4 * (lane >> 5);
+        const bool mine = WK == 1 || wave < WM * WN;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    *(float4*)(out + j * 32 + 8 * g) = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+                    if (mine) *(float4*)(out + j * 32 + 8 * g) = make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
             leave<32 * WM, BM / WM, BN, kPitch>(smem, m0 + 32 * i, n0, fetch, body);
         }
     }
     // the same turned: row n, columns m .. m + 7
     template <typename Fetch, typename F> static __device__ __forceinline__ void columns(const f32x16 (&acc)[MT][NT], int64_t m0, int64_t n0, unsigned char* smem, Fetch fetch, F body) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        static_assert(WK == 1, "whole tiles");
         float* out = (float*)smem + (wave % WN * 32 + 4 * (lane >> 5)) * kPitchTurned + (wave / WN * MT) * 32 + (lane & 31);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -380,8 +421,8 @@ struct Core {
     // R rows of which each 32 lie APART after the 32 before
     template <int R, int APART, int C, int PITCH, typename Fetch, typename F>
     static __device__ __forceinline__ void leave(const unsigned char* smem, int64_t r0, int64_t c0, Fetch fetch, F body) {
-        constexpr int kTurns = R * (C / 8) / kThreads, kGroup = kTurns < 4 ? kTurns : 4;
-        static_assert(R * (C / 8) % kThreads == 0 && kTurns % kGroup == 0, "turns");
+        constexpr int kPieces = R * (C / 8), kTurns = (kPieces + kThreads - 1) / kThreads, kGroup = kTurns < 4 ? kTurns : 4;
+        static_assert((kPieces % kThreads == 0 || kTurns == 1) && kTurns % kGroup == 0, "turns");
         typedef decltype(fetch(r0, c0)) Old;
 #pragma unroll 1
         for (int t0 = 0; t0 < kTurns; t0 += kGroup) {
@@ -389,12 +430,14 @@ struct Core {
 #pragma unroll
             for (int t = 0; t < kGroup; ++t) {
                 const int u = (t0 + t) * kThreads + (int)threadIdx.x, r = u / (C / 8);
+                if (kPieces < kThreads && u >= kPieces) break;
                 old[t] = fetch(r0 + r / 32 * APART + r % 32, c0 + u % (C / 8) * 8);
             }
             if (t0 == 0) barrier();
 #pragma unroll
             for (int t = 0; t < kGroup; ++t) {
                 const int u = (t0 + t) * kThreads + (int)threadIdx.x, r = u / (C / 8), c = u % (C / 8) * 8;
+                if (kPieces < kThreads && u >= kPieces) break;
                 const float4 a = *(const float4*)((const float*)smem + r * PITCH + c), b = *(const float4*)((const float*)smem + r * PITCH + c + 4);
                 float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
                 body(r0 + r / 32 * APART + r % 32, c0 + c, v, old[t]);

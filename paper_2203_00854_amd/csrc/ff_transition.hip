@@ -97,12 +97,13 @@ struct HiddenArgs {
     uint32_t mtiles, ntiles;
 };
 // Both projections share the tile of x; their product with the activation leaves alone.  Channels and rows past the end are zeros.
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : 2) void k_tr_hidden(HiddenArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : C::BM == 32 ? 1 : 2) void k_tr_hidden(HiddenArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[2][C::MT][C::NT];
     C::clear(acc);
     C::run(acc, &a.x, a.w, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
+    C::join(acc, smem);
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)
 #pragma unroll
@@ -128,12 +129,13 @@ struct OutArgs {
     uint32_t mtiles, ntiles;
 };
 // out = (residual +) sum of the products; a masked row's sum counts as zero, whatever it is
-template <class C, typename T> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : 2) void k_tr_out(OutArgs a) {
+template <class C, typename T> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : C::BM == 32 ? 1 : 2) void k_tr_out(OutArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[1][C::MT][C::NT];
     C::clear(acc);
     for (int p = 0; p < a.parts; ++p) C::run(acc, a.a + p, a.b + p, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
+    C::join(acc, smem);
     const auto fetch = [&](int64_t m, int64_t n) {
         Eight e;
 #pragma unroll
@@ -233,12 +235,13 @@ struct GradArgs {
 };
 // a, b and dh = dy Wo of a tile in one loop over the channels; da = dh b act'(a), db = dh act(a) and h, rounded to the tensors' type, are what the
 // products with the weights and with x and dy read
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : 2) void k_tr_grad(GradArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : C::BM == 32 ? 1 : 2) void k_tr_grad(GradArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[3][C::MT][C::NT];
     C::clear(acc);
     C::run(acc, a.a, a.b, at.m * C::BM, (int64_t)at.n * C::BN, 0, a.k, smem);
+    C::join(acc, smem);
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)
 #pragma unroll
@@ -586,6 +589,7 @@ template <class C, auto SILU, auto GELU, auto SIGMOID, typename Args> ff_status 
 template <typename T> struct Hidden {
     typedef T Type;
     typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 32, 32, 256 / sizeof(T), 4, 1, 1, 1, 2, 0, 0u, 4> Least;
     typedef Core<Op, 64, 64, 64 / sizeof(T), 4, 2, 2, 1, 2, 0, 0u> Small;
     typedef Core<Bf16, 128, 64, 32, 4, 2, 2, 1, 2, 0, 0u> Medium;
     typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 2, 0, 0u> Large;
@@ -596,6 +600,7 @@ template <typename T> struct Hidden {
 template <typename T, unsigned TB> struct Out {
     typedef T Type;
     typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 32, 32, 256 / sizeof(T), 4, 1, 1, 1, 1, 0, TB, 4> Least;
     typedef Core<Op, 64, 64, 64 / sizeof(T), 4, 2, 2, 1, 1, 0, TB> Small;
     typedef Core<Bf16, 128, 128, 32, 4, 2, 2, 1, 1, 0, TB> Medium;
     typedef Core<Bf16, 256, 128, 32, 4, 4, 2, 1, 1, 0, TB> Large;
@@ -608,6 +613,7 @@ template <typename T, unsigned TB> struct Out {
 template <typename T> struct Grad {
     typedef T Type;
     typedef typename OpOf<T>::type Op;
+    typedef Core<Op, 32, 32, 256 / sizeof(T), 3, 1, 1, 2, 3, 0, 4u, 4> Least;
     typedef Core<Op, 64, 64, 64 / sizeof(T), 3, 2, 2, 2, 3, 0, 4u> Small;
     typedef Core<Bf16, 128, 64, 32, 3, 2, 2, 2, 3, 0, 4u> Medium;
     typedef Core<Bf16, 128, 128, 32, 3, 4, 2, 2, 3, 0, 4u> Large;
@@ -615,6 +621,9 @@ template <typename T> struct Grad {
         return run_act<C, k_tr_grad<C, T, FF_SILU>, k_tr_grad<C, T, FF_GELU>, k_tr_grad<C, T, FF_SIGMOID>>(KK_TR_GRAD, "ff_gated_transition_backward", a, m, n, act, stream);
     }
 };
+// Tiles of 64 by 64 that are few leave most units empty: four times as many of 32 by 32, k shared by four wavefronts, up to this many.  Float32, 16 rows of 384 channels with 1536
+// hidden ones 55 -> 19 us, 400 rows 60 -> 32, with more of them 36; bfloat16, 16 rows of 1024 with 4096 37 -> 15, 100 rows 40 -> 20, 400 rows 46 -> 31.
+constexpr int64_t kFewTiles = 128;
 template <class C> bool enough(int64_t m, int64_t n) { return (m + C::BM - 1) / C::BM * ((n + C::BN - 1) / C::BN) >= 200; }
 template <class K, typename Args> ff_status tiled(int64_t m, int64_t n, const Args& a, int act, hipStream_t stream) {
     // (float32 products are bound by their instructions, 64 cycles each: small tiles cost nothing)
@@ -622,6 +631,7 @@ template <class K, typename Args> ff_status tiled(int64_t m, int64_t n, const Ar
         if (enough<typename K::Large>(m, n)) return K::template run<typename K::Large>(a, m, n, act, stream);
         if (enough<typename K::Medium>(m, n)) return K::template run<typename K::Medium>(a, m, n, act, stream);
     }
+    if ((m + 63) / 64 * ((n + 63) / 64) <= kFewTiles) return K::template run<typename K::Least>(a, m, n, act, stream);
     return K::template run<typename K::Small>(a, m, n, act, stream);
 }
 
