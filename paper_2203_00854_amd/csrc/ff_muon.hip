@@ -154,7 +154,8 @@ __device__ __forceinline__ Spot spot_of(const Matrix& x, int64_t i) {
 // the update that is orthogonalised, of the new momentum and the gradient
 __device__ __forceinline__ float update_of(float m, float g, const StepArgs& a) { return a.nesterov ? a.beta * m + a.rest * g : m; }
 
-// m = beta m + (1 - beta) k g, and the sum of squares of the update, in float64: bound by HBM.  MUON false: of g itself.
+// m = beta m + (1 - beta) k g, and the sum of squares of the update, in float64.  MUON false: of g itself.  Bound by HBM: 48 blocks' 79 M values
+// in matrices beyond 128 x 128, bfloat16 gradients, 137 us for 770 MB, 5.6 TB/s.
 template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_momentum(Table t, StepArgs a, const float* norm, double* partial) {
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -190,7 +191,7 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_m
     if (threadIdx.x == 0) partial[x.piece0 + at.at] = sums[0];
 }
 
-// X = update / (norm + eps) as pairs, its padding zeros
+// X = update / (norm + eps) as pairs, its padding zeros.  Bound by HBM likewise: 158 us for 770 MB.  (The update is formed again: it would be another 4 bytes a value.)
 template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_start(Table t, StepArgs a, const float* norm, const double* partial, char* ws) {
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -267,7 +268,8 @@ template <bool BESIDE> __device__ __forceinline__ void store_gram(char* a, char*
     store_pairs(c + at, w);
 }
 
-// A.  SPLIT: sums over a part of k each, for k_ns_join
+// A.  SPLIT: sums over a part of k each, for k_ns_join.  48 blocks: 127 us for 2016 tiles, the matrix units 0.38 busy, 480 MB through HBM at 3.7 TB/s: k is 256 long for most tiles, so a third is
+// the way in and out.  4096 x 1024: 136 tiles of 64 in three parts each 26 us and 6 for the join.
 template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int which, StepArgs a, float* parts) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
     }
 }
 
-// B = a I + A C, or a I + b A + c A^2
+// B = a I + A C, or a I + b A + c A^2.  48 blocks 109 us for 490 MB; 4096 x 1024 15 us, 32 stages of 32 k in a row by half the units.
 template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(Table t, char* ws, StepArgs a) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -390,7 +392,8 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
         tile::store_some(p, left, w);
     }
 }
-// X = B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights
+// X = B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights.  48 blocks 200 us for 785 MB (the last, with weights and masters, 283 for 1.25 GB);
+// 4096 x 1024 36 us, 256 tiles, one a unit, 23 of them matrix instructions at the rate of a large product.
 template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -430,7 +433,8 @@ template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kB
 // ---- small matrices: everything in one block ---------------------------------------------------
 // A matrix of at most SIZE x SIZE stays in LDS from its momentum to its weights: X and A (then B in A's place) as pairs in rows of SIZE values, a product's
 // results in registers between two barriers.  A wavefront has one 32 x 32 tile of the result (SIZE 64), or two beside each other (SIZE 128).
-// 128 x 64: one launch of 29 us where the products of the other path take 17.
+// Bound by the chain of 3 steps dependent products, each a barrier, reads from LDS, 3 k / 16 matrix instructions in a row and the rounding into pairs: one 128 x 64 29 us (1.9 a product),
+// where the other path needs seventeen launches; 1200 matrices of up to 128 x 128 on 256 units 400 us, the matrix units 0.30 busy.
 template <int SIZE> struct Small {
     static constexpr int kWaves = SIZE == 128 ? 8 : 4, kThreads = 64 * kWaves, kUnits = SIZE == 128 ? 2 : 1;
     static constexpr int W = SIZE / 4, kImage = SIZE * SIZE * 4, kLds = 2 * kImage;
@@ -671,7 +675,10 @@ int64_t parts_bytes(int64_t tris, int splits) { return splits > 1 ? tris * split
 
 template <auto KERNEL, typename... A> ff_status go(int kind, dim3 blocks, int threads, size_t lds, hipStream_t stream, const char* what, A... args) {
     Timed t(kind, stream);
-    if (lds) tile::allow_lds<KERNEL>();
+    if (lds) {
+        const ff_status st = tile::allow_lds<KERNEL>(what);
+        if (st != FF_OK) return st;
+    }
     hipLaunchKernelGGL(KERNEL, blocks, dim3(threads), lds, stream, args...);
     return check_launch(what);
 }

@@ -450,14 +450,16 @@ struct Core {
 };
 
 // once for each device and each kernel that needs more than 64 KiB (a device beyond 64: at each call)
-template <auto KERNEL> static void allow_lds() {
+template <auto KERNEL> static ff_status allow_lds(const char* what) {
     static std::atomic<uint64_t> done{0};
     int device = 0;
     (void)hipGetDevice(&device);
     const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
-    if (done.load(std::memory_order_relaxed) & bit) return;
-    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (done.load(std::memory_order_relaxed) & bit) return FF_OK;
+    const hipError_t error = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (error != hipSuccess) return fail(FF_EHIP, "%s: dynamic LDS limit: %s", what, hipGetErrorString(error));
     done.fetch_or(bit, std::memory_order_relaxed);
+    return FF_OK;
 }
 
 // Blocks of the same rows of A run one after another on one XCD (block i starts on XCD i % 8), whose L2 then holds them, while B is small enough for all.

@@ -157,32 +157,35 @@ def test_muon_plan_sizes():
         assert P.lib().ff_muon_workspace_bytes(C.byref(muon(n=count)), host.ctypes.data, host.size) > 0
 
 
-def test_muon_plan_has_every_place_once():
-    """Tiles of large matrices, each once (places that are none fill up), small ones behind them in the order of their sizes."""
-    shapes = [(64, 64), (300, 700), (128, 100), (2000, 130), (1, 5), (700, 300), (129, 1), (260, 260)]
+@pytest.mark.parametrize("more", [0, 61, 62])
+def test_muon_plan_has_every_place_once(more):
+    """Tiles of large matrices, each once (places that are none fill up), small ones behind them in the order of their sizes; up to 64 small ones have tiles too."""
+    shapes = [(64, 64), (300, 700), (128, 100), (2000, 130), (1, 5), (700, 300), (129, 1), (260, 260)] + [(20, 30)] * more
+    count, small, smaller = len(shapes), *((0, 0) if 3 + more <= 64 else (1, 2 + more))
+    large = count - small - smaller
     rows = [{**GOOD, "rows": r, "cols": c, "p": (3 * i + 1) << 24, "g": (3 * i + 2) << 24, "m": (3 * i + 3) << 24} for i, (r, c) in enumerate(shapes)]
     host = plan_of(muon(n=len(rows)), matrices(*rows))
     head = host[:48].view(np.dtype([("tag", "<u4"), ("matrices", "<i4"), ("batches", "<i4"), ("pieces", "<i4"), ("tris", "<i4"), ("apps", "<i4"), ("small", "<i4"), ("smaller", "<i4"),
                                     ("ws", "<i8"), ("bytes", "<i8")]))[0]
-    assert (head["matrices"], head["batches"], head["small"], head["smaller"]) == (8, 1, 1, 2) and head["bytes"] == host.size
+    assert (head["matrices"], head["batches"], head["small"], head["smaller"]) == (count, 1, small, smaller) and head["bytes"] == host.size
     batch = host[48:96].view(np.dtype([("ws", "<i8")] + [(n, "<i4") for n in ("piece0", "pieces", "tri0", "tris", "app0", "apps", "splits", "tri_tile", "app_tile", "beside")]))[0]
     at = 96
-    found = host[at:at + 64 * 8].view(np.dtype([("p", "<u8"), ("g", "<u8"), ("master", "<u8"), ("m", "<u8"), ("ws", "<i8"), ("rows", "<i4"), ("cols", "<i4"), ("piece0", "<i4"),
+    found = host[at:at + 64 * count].view(np.dtype([("p", "<u8"), ("g", "<u8"), ("master", "<u8"), ("m", "<u8"), ("ws", "<i8"), ("rows", "<i4"), ("cols", "<i4"), ("piece0", "<i4"),
                                                 ("pieces", "<i4"), ("decay", "<f4"), ("pad", "<i4")]))
     assert sorted((int(f["rows"]), int(f["cols"])) for f in found) == sorted(shapes)
-    assert [max(int(f["rows"]), int(f["cols"])) for f in found[-3:]] == [128, 64, 5]
-    places = host[at + 64 * 8:].view("<i4").reshape(-1, 2)
+    assert [max(int(f["rows"]), int(f["cols"])) for f in found[5:]] == [128, 64] + [30] * more + [5]
+    places = host[at + 64 * count:].view("<i4").reshape(-1, 2)
     tile = lambda n, t: -(-n // t)  # noqa: E731
     pad = lambda n: -(-n // 16) * 16  # noqa: E731
     kinds = (("pieces", lambda r, c: tile(pad(r) * pad(c), 4096)), ("tris", lambda r, c: tile(pad(min(r, c)), int(batch["tri_tile"])) * (tile(pad(min(r, c)), int(batch["tri_tile"])) + 1) // 2),
              ("apps", lambda r, c: tile(pad(r), int(batch["app_tile"])) * tile(pad(c), int(batch["app_tile"]))))
     first = 0
-    for kind, count in kinds:
+    for kind, tiles in kinds:
         got = places[first:first + head[kind]]
         got = [tuple(g) for g in got.tolist() if g[0] >= 0]
-        assert sorted(got) == [(i, k) for i in range(5) for k in range(count(int(found[i]["rows"]), int(found[i]["cols"])))], kind
+        assert sorted(got) == [(i, k) for i in range(large) for k in range(tiles(int(found[i]["rows"]), int(found[i]["cols"])))], kind
         first += head[kind]
-    spans = sorted((int(f["ws"]), int(f["ws"]) + 4 * (2 * pad(int(f["rows"])) * pad(int(f["cols"])) + 2 * pad(min(int(f["rows"]), int(f["cols"]))) ** 2)) for f in found[:5])
+    spans = sorted((int(f["ws"]), int(f["ws"]) + 4 * (2 * pad(int(f["rows"])) * pad(int(f["cols"])) + 2 * pad(min(int(f["rows"]), int(f["cols"]))) ** 2)) for f in found[:large])
     assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])) and spans[-1][1] <= head["ws"]
 
 
