@@ -241,7 +241,7 @@ struct GradArgs {
 };
 // a, b and dh = dy Wo of a tile in one loop over the channels; da = dh b act'(a), db = dh act(a) and h, rounded to the tensors' type, are what the
 // products with the weights and with x and dy read.  Three accumulators a tile: 18000 x 173 with 692 hidden channels in float32 161 us, the matrix units 0.66 busy.
-template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 ? 2 : C::BM == 64 ? 4 : C::BM == 32 ? 1 : 2) void k_tr_grad(GradArgs a) {
+template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads, C::kThreads == 512 || C::BM == 64 ? 2 : C::BM == 32 ? 1 : 2) void k_tr_grad(GradArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
     const tile::TilePlace at = tile::place_of(blockIdx.x, a.mtiles, a.ntiles);
     f32x16 acc[3][C::MT][C::NT];
@@ -386,17 +386,20 @@ struct WeightArgs {
     int32_t add;                  // to what an earlier chunk left
 };
 // Sums over rows: both operands lie with the rows as k.  The rows are split over blocks, whose sums are joined in a fixed order.  Bound by HBM where rows are many: 701 x 701 x 128
-// with 512 hidden channels 416 us for the 2.2 GB that da, db, h, x and dy are, each read once by tiles of 256 x 128; 128 x 256 x 256 with 1024 69 us and 18 for the join of 20 parts, 61 MB of
+// with 512 hidden channels 407 us for 1.7 GB, da, db and h read once by tiles of 256 x 128; 128 x 256 x 256 with 1024 67 us and 16 for the join of 20 parts, 61 MB of
 // sums that the 240 blocks' accumulators are.  Float32, 18000 x 173: 163 us, the matrix units 0.71 busy.
 template <class C> __global__ __launch_bounds__(C::kThreads) void k_tr_weights(WeightArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
-    const uint32_t tiles = a.ftiles * a.ctiles, which = blockIdx.x / tiles, t = blockIdx.x % tiles;
+    // each XCD (block i starts on XCD i % 8) has a run of neighbouring items: tiles of the same rows, which its L2 then holds
+    // (18000 x 173 in float32 196 MB from HBM instead of 675, 128 x 256 x 256 233 instead of 393: the latter's whole backward pass 198 -> 192 us, 701 x 701 x 128 887 -> 873)
+    const uint32_t tiles = a.ftiles * a.ctiles, block = blockIdx.y * gridDim.x + blockIdx.x, all = gridDim.x * gridDim.y, xcd = block & 7u;
+    const uint32_t item = xcd * (all >> 3) + (xcd < (all & 7u) ? xcd : all & 7u) + (block >> 3), split = item / gridDim.x, rest = item % gridDim.x, which = rest / tiles, t = rest % tiles;
     const int64_t m0 = (int64_t)(t / a.ctiles) * C::BM, n0 = (int64_t)(t % a.ctiles) * C::BN;
-    const int64_t from = blockIdx.y * a.per_split, to = from + a.per_split < a.rows ? from + a.per_split : a.rows;
+    const int64_t from = split * a.per_split, to = from + a.per_split < a.rows ? from + a.per_split : a.rows;
     f32x16 acc[1][C::MT][C::NT];
     C::clear(acc);
     C::run(acc, a.a + which, a.b + which, m0, n0, from, to, smem);
-    float* out = a.partial + ((int64_t)blockIdx.y * 3 + which) * a.fp * a.cp;
+    float* out = a.partial + ((int64_t)split * 3 + which) * a.fp * a.cp;
     const int32_t rows = a.fp, cols = a.cp;
     const auto fetch = [&](int64_t m, int64_t n) {
         Eight e;
