@@ -157,7 +157,7 @@ template <class C, typename T> __global__ __launch_bounds__(C::kThreads, C::kThr
 // ---- the whole forward pass with rows in registers -------------------------------------------
 // The hidden layer would be 4 times the bytes of x (f = 4 c, and twice that, written and read): it stays in registers.  A block has 128 rows, four wavefronts, and streams the weights, which
 // L2 holds, through LDS; 32 hidden channels are 3 c / 16 matrix instructions a wavefront between two barriers, three blocks a unit at up to 128 channels fill each other's
-// gaps.  Bound by the matrix units and the exponentials between them: 2048 x 2048 x 128 with 512 hidden channels and residual 1.77 ms, 935 TFLOP/s (through memory 4.9 ms), of 3.2 GB that
+// gaps.  Bound by the matrix units and the exponentials between them: 2048 x 2048 x 128 with 512 hidden channels and residual 1.73 ms, 950 TFLOP/s (through memory 4.9 ms), of 3.2 GB that
 // take 0.63; 128 x 256 x 256 with 1024 60 us, 853 TFLOP/s: 256 blocks, one a unit, whose last turns nothing fills.
 struct RowsArgs {
     const bf16_t *x, *residual;
@@ -272,7 +272,7 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
 
 // The same with rows in registers (bfloat16, up to 256 channels), and dx with them: a^T, b^T and dh^T = Wo^T dy^T of 32 hidden channels leave a lane with sixteen neighbours
 // of each, from which da, db and h are stored and dx^T += Wa^T da^T + Wb^T db^T goes on.  The weights' other sides are read turned from the same stage.
-// Bound by its stores, 6 f bytes a row (701 x 701 x 128 with 512 hidden channels 600 us, 2.1 GB), and by two wavefronts a SIMD, which the registers of x, dy and dx allow: the matrix units are 0.36 busy.
+// Bound by its stores, 6 f bytes a row (701 x 701 x 128 with 512 hidden channels 585 us, 2.1 GB), and by two wavefronts a SIMD, which the registers of x, dy and dx allow: the matrix units are 0.36 busy.
 // Without the stores the weights' gradients would need a, b and dh once more, 6 of 16 parts of the work.
 struct GradRowsArgs {
     const bf16_t *x, *dy;
