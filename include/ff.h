@@ -405,7 +405,7 @@ typedef struct {
     int64_t rows;       /* >= 0 */
 } ff_transition_desc;
 
-/* Bytes of device workspace (padded copies of weights and tokens, hidden tensors of some thousand rows, partial sums); 0 if desc is invalid. */
+/* Bytes of device workspace (padded copies of weights and tokens, hidden tensors of up to 512 MiB each, one forward and three backward, partial sums); 0 if desc is invalid. */
 size_t ff_gated_transition_forward_workspace_bytes(const ff_transition_desc* desc);
 size_t ff_gated_transition_backward_workspace_bytes(const ff_transition_desc* desc);
 
