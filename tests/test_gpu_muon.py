@@ -154,7 +154,8 @@ class Model:
                 assert np.all(np.abs(n64(self.p[i]) - w) <= e_w + half * (np.abs(w) + e_w)), name
 
 
-LISTS = [[(1, 1)], [(150, 40)] * 9 + [(40, 700)] * 4 + [(33, 60)] * 3, [(64, 48), (48, 64), (130, 20), (0, 5), (20, 130), (1, 33), (33, 1), (7, 7)], [(256, 64), (64, 256), (128, 128)], [(150, 40)] + [(33, 60)] * 40 + [(100, 20)] * 25]
+LISTS = [[(1, 1)], [(150, 40)] * 9 + [(40, 700)] * 4 + [(33, 60)] * 3, [(64, 48), (48, 64), (130, 20), (0, 5), (20, 130), (1, 33), (33, 1), (7, 7)], [(256, 64), (64, 256), (128, 128)], [(150, 40)] + [(33, 60)] * 40 + [(100, 20)] * 25,
+         [(1700, 150), (30, 20), (130, 40), (5, 5), (140, 2100)]]          # a k that is split, beside ones that are not
 
 
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
