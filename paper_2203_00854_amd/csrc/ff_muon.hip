@@ -2,9 +2,9 @@
 //
 //   X = G / (|G| + eps);  per step, with n the shorter side:  A = X X^T (X^T X where a matrix is tall);  X = a X + (b A + c A^2) X  (X (...))
 //
-// Three launches a step for all matrices together: A; B = a I + b A + c A^2; X = B X.  With a I inside B the last product needs its operands alone; few
-// tiles hold C = b I + c A beside A, so that B = a I + A C does too: what it had to add otherwise would be another read in a short kernel's last microseconds.  Many
-// tiles do not (A is as large as X where that is square, and memory bounds them).  Values are held as float16 pairs of kScale times
+// Three launches a step for all matrices together: A; B = b A + c A^2; X = a X + B X.  What is added behind a product is added in float32: with a I inside B the rounding of B's
+// diagonal, another one in each row, would carry the large singular directions into the small ones, which the next steps make larger (2048 x 2048: an
+// error of 3.2e-6 in norm instead of 1.3e-6; b I inside an operand of B's product likewise, 256 x 256 2.1e-6 instead of 2.0e-6).  Values are held as float16 pairs of kScale times
 // themselves: 23 significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  Magnitudes
 // to 255 have a place, and singular values are at most 1 at the start and below 1.3 after any number of steps with the usual coefficients; 2^-33 is
 // the smallest step between small values.  A tall matrix is worked on as it lies: its operands are read turned.
@@ -42,7 +42,7 @@ struct Matrix {
     void* p;                                     // what the last step writes
     float* master;
     float* m;
-    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A, B, and C where it is held, as pairs
+    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A and B as pairs
     int32_t rows, cols;
     int32_t piece0, pieces;                      // among the batch's
     float decay;
@@ -55,7 +55,7 @@ struct Matrix {
     __host__ __device__ int64_t bytes_a() const { return np() * np() * 4; }
     __host__ __device__ int64_t x(int which) const { return ws + which * bytes_x(); }
     __host__ __device__ int64_t a(int which) const { return ws + 2 * bytes_x() + which * bytes_a(); }
-    __host__ __device__ int64_t bytes(bool beside) const { return 2 * bytes_x() + (beside ? 3 : 2) * bytes_a(); }
+    __host__ __device__ int64_t bytes() const { return 2 * (bytes_x() + bytes_a()); }
 };
 struct Place {
     int32_t matrix, at;                          // matrix < 0: none
@@ -227,21 +227,20 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
 }
 
 // ---- the products --------------------------------------------------------------------------
-template <int TILE_, int BK, int STAGES, int BLOCKS, bool BESIDE> struct Cores {
+template <int TILE_, int BK, int STAGES, int BLOCKS> struct Cores {
     static constexpr int TILE = TILE_;
     typedef Core<Pair, TILE, TILE, BK, STAGES, 2, 2, 1, 1, 0, 0u> Straight;        // rows by rows
     typedef Core<Pair, TILE, TILE, BK, STAGES, 2, 2, 1, 1, 1, 1u> Turned;          // columns by columns
     typedef Core<Pair, TILE, TILE, BK, STAGES, 2, 2, 1, 1, 0, 1u> Mixed;           // rows by columns
-    static constexpr bool kBeside = BESIDE;                                        // C is held beside A
     static constexpr int kBlocks = BLOCKS;                                         // on a compute unit
     static constexpr size_t kLds = std::max({Straight::kLds, Turned::kLds, Mixed::kLds});
 };
 // Three stages of 16 k leave room for three blocks on a compute unit, whose ends then overlap with the others' products.  Where a launch has fewer blocks than there are
 // units a block stands alone with what a stage costs it, a barrier and the reads behind it, so that stages of 32 k are better (orthogonalising 4096 x 1024: eight of 16 k
 // 434 us, five of 32 383, four 374; of 64 k for the smaller tiles 390).  Fewer blocks still, and tiles of 64 fill four times the units.
-typedef Cores<128, 16, 3, 3, false> Many;
-typedef Cores<128, 32, 4, 1, true> Some;
-typedef Cores<64, 32, 4, 2, true> Few;
+typedef Cores<128, 16, 3, 3> Many;
+typedef Cores<128, 32, 4, 1> Some;
+typedef Cores<64, 32, 4, 2> Few;
 
 __device__ __forceinline__ Operand operand_x(const Matrix& x, const char* ws, int which) {
     return {ws + x.x(which), x.cp() * 4, x.rp(), (int32_t)(x.cp() * 4)};
@@ -256,21 +255,14 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     j = t - i * (i + 1) / 2;
 }
-// eight values of A, and of C = b I + c A beside it; row m from column n on (a multiple of eight)
-template <bool BESIDE> __device__ __forceinline__ void store_gram(char* a, char* c, int64_t np, int64_t m, int64_t n, const float (&v)[8], const StepArgs& p) {
-    if (m >= np || n >= np) return;
-    const int64_t at = pairs_at(m * np + n);
-    store_pairs(a + at, v);
-    if constexpr (!BESIDE) return;
-    float w[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q) w[q] = p.c * v[q] + (n + q == m ? p.b * kScale : 0.f);
-    store_pairs(c + at, w);
+// eight values of A, row m from column n on (a multiple of eight)
+__device__ __forceinline__ void store_gram(char* a, int64_t np, int64_t m, int64_t n, const float (&v)[8]) {
+    if (m < np && n < np) store_pairs(a + pairs_at(m * np + n), v);
 }
 
 // A.  SPLIT: sums over a part of k each, for k_ns_join.  48 blocks: 127 us for 2016 tiles, the matrix units 0.38 busy, 480 MB through HBM at 3.7 TB/s: k is 256 long for most tiles, so a third is
 // the way in and out.  4096 x 1024: 136 tiles of 64 in three parts each 26 us and 6 for the join.
-template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int which, StepArgs a, float* parts) {
+template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int which, float* parts) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -293,15 +285,15 @@ template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) voi
         const auto store = [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
-            store_gram<C::kBeside>(ws + x.a(0), ws + x.a(2), x.np(), m, n, v, a);
+            store_gram(ws + x.a(0), x.np(), m, n, v);
         };
         Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
         if (i != j) Straight::columns(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
     }
 }
 
-// A and C of A's parts, added up in their order; a block has 32 rows of a tile
-__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, const float* parts, int splits) {
+// A of its parts, added up in their order; a block has 32 rows of a tile
+__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float* parts, int splits) {
     constexpr int kTile = Few::TILE, kBand = 32, kPitch = kBand + 1;
     __shared__ float band[kTile * kPitch];
     const Place at = place_at(t, blockIdx.x);
@@ -310,7 +302,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
     int i, j;
     triangle(at.at, i, j);
     const int64_t np = x.np(), m0 = (int64_t)i * kTile + blockIdx.y * kBand, n0 = (int64_t)j * kTile;
-    char *ca = ws + x.a(0), *cc = ws + x.a(2);
+    char* to = ws + x.a(0);
     const int64_t next = (int64_t)gridDim.x * kTile * kTile;
     const float* from = parts + ((int64_t)blockIdx.x * kTile + blockIdx.y * kBand) * kTile;
     for (int u = threadIdx.x; u < kBand * kTile / 8; u += 256) {
@@ -324,7 +316,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) band[(c + q) * kPitch + r] = v[q] *= kUnscale;
-        store_gram<true>(ca, cc, np, m0 + r, n0 + c, v, a);
+        store_gram(to, np, m0 + r, n0 + c, v);
     }
     if (i == j) return;
     tile::barrier();
@@ -333,11 +325,11 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, StepArgs a, 
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = band[r * kPitch + c + q];
-        store_gram<true>(ca, cc, np, n0 + r, m0 + c, v, a);
+        store_gram(to, np, n0 + r, m0 + c, v);
     }
 }
 
-// B = a I + A C, or a I + b A + c A^2.  48 blocks 109 us for 490 MB; 4096 x 1024 15 us, 32 stages of 32 k in a row by half the units.
+// B = b A + c A^2.  48 blocks 109 us for 490 MB; 4096 x 1024 15 us, 32 stages of 32 k in a row by half the units.
 template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(Table t, char* ws, StepArgs a) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -347,25 +339,18 @@ template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
-    const Operand oa = operand_a(x, ws, 0), oc = C::kBeside ? operand_a(x, ws, 2) : oa;
+    const Operand oa = operand_a(x, ws, 0);
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     const int64_t np = x.np();
-    Straight::run(acc, &oa, &oc, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
+    Straight::run(acc, &oa, &oa, (int64_t)i * kTile, (int64_t)j * kTile, 0, np, smem);
     char* out = ws + x.a(1);
     const char* was = ws + x.a(0);
-    const auto fetch = [&](int64_t m, int64_t n) {
-        if constexpr (C::kBeside) return typename Straight::Nothing();
-        else return m < np && n < np ? load_pairs(was + pairs_at(m * np + n)) : Pairs{};
-    };
-    const auto store = [&](int64_t m, int64_t n, float (&v)[8], const auto& old) {
+    const auto fetch = [&](int64_t m, int64_t n) { return m < np && n < np ? load_pairs(was + pairs_at(m * np + n)) : Pairs{}; };
+    const auto store = [&](int64_t m, int64_t n, float (&v)[8], const Pairs& old) {
         if (m >= np || n >= np) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            if constexpr (C::kBeside) v[q] = kUnscale * v[q];
-            else v[q] = a.b * value_of(old, q) + (a.c * kUnscale) * v[q];
-            v[q] += n + q == m ? a.a * kScale : 0.f;
-        }
+        for (int q = 0; q < 8; ++q) v[q] = a.b * value_of(old, q) + (a.c * kUnscale) * v[q];
         store_pairs(out + pairs_at(m * np + n), v);
     };
     Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, store);
@@ -392,7 +377,7 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
         tile::store_some(p, left, w);
     }
 }
-// X = B X (X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights.  48 blocks 200 us for 785 MB (the last, with weights and masters, 283 for 1.25 GB);
+// X = a X + B X (a X + X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights.  48 blocks 200 us for 785 MB (the last, with weights and masters, 283 for 1.25 GB);
 // 4096 x 1024 36 us, 256 tiles, one a unit, 23 of them matrix instructions at the rate of a large product.
 template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
     typedef typename C::Straight Straight;
@@ -415,10 +400,12 @@ template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kB
     else C::Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
     char* to = ws + x.x(which ^ 1);
     const float size = size_of(x, a);
-    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
+    const char* was = ws + x.x(which);
+    const auto fetch = [&](int64_t m, int64_t n) { return m < rp && n < cp ? load_pairs(was + pairs_at(m * cp + n)) : Pairs{}; };
+    Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, [&](int64_t m, int64_t n, float (&v)[8], const Pairs& old) {
         if (m >= rp || n >= cp) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
+        for (int q = 0; q < 8; ++q) v[q] = a.a * value_of(old, q) + kUnscale * v[q];
         if constexpr (LAST == kMore) store_pairs(to + pairs_at(m * cp + n), v);
         else {
             const int left = x.cols - (int)n;
@@ -526,6 +513,22 @@ template <int SIZE> struct Small {
         }
         if (tiles == 1) product<TA, TB, 1>(acc, a, b, m0, n0, k, lane);
     }
+    // what store() has written there
+    static __device__ __forceinline__ void load(f32x16 (&acc)[kUnits], const unsigned char* from, int m0, int n0, int tiles, int rows, int cols, int lane) {
+        if (m0 + (lane & 31) >= rows) return;
+        const int of = at(m0 + (lane & 31), n0, 0) + 8 * (lane >> 5);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (u < tiles)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    if (n0 + 32 * u + 8 * g >= cols) continue;
+                    const uint2 hi = *(const uint2*)(from + result_at(of, u, g, 0)), lo = *(const uint2*)(from + result_at(of, u, g, 1));
+                    const uint32_t h[2] = {hi.x, hi.y}, l[2] = {lo.x, lo.y};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[u][4 * g + q] = q & 1 ? join(h[q / 2] >> 16, l[q / 2] >> 16) : join(h[q / 2] & 0xffffu, l[q / 2] & 0xffffu);
+                }
+    }
     // rows and columns below the given numbers
     static __device__ __forceinline__ void store(const f32x16 (&acc)[kUnits], unsigned char* to, int m0, int n0, int tiles, int rows, int cols, int lane) {
         if (m0 + (lane & 31) >= rows) return;
@@ -603,35 +606,35 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         *(uint4*)(xs + S::at(r, c, 0)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *(uint4*)(xs + S::at(r, c, 1)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
-    // Three products a step, one piece of code: A of X; B = a I + b A + c A^2, into A's place; X = B X.  A wavefront has the same tiles of A and of B, and keeps its A.
+    // Three products a step, one piece of code: A of X; B = b A + c A^2, into A's place; X = a X + B X.  A wavefront has the same tiles of A and of B, and keeps
+    // its A; and its tiles of X.
     tile::barrier();
-    f32x16 acc[S::kUnits] = {}, held[S::kUnits] = {};
+    struct Tiles {
+        int rows, cols, m0, n0, count;
+    };
+    const auto tiles_of = [&](int rows, int cols) {
+        const int across = (cols + 31) / 32, down = (rows + 31) / 32, each = across * down > S::kWaves ? S::kUnits : 1, groups = (across + each - 1) / each;
+        const int m0 = wave / groups * 32, n0 = wave % groups * each * 32;
+        return Tiles{rows, cols, m0, n0, wave < groups * down ? (across - n0 / 32 < each ? across - n0 / 32 : each) : 0};
+    };
+    const Tiles square = tiles_of(np, np), whole = tiles_of(rp, cp);
+    f32x16 acc[S::kUnits] = {}, held[S::kUnits] = {}, kept[S::kUnits] = {};          // kept: X before it is rounded
+    S::load(kept, xs, whole.m0, whole.n0, whole.count, rp, cp, lane);
 #pragma unroll 1
     for (int phase = 0, left = 3 * steps; left > 0; --left) {
         const bool last = phase == 2, tall = x.tall();
-        const int rows = last ? rp : np, cols = last ? cp : np;
-        const int across = (cols + 31) / 32, down = (rows + 31) / 32, each = across * down > S::kWaves ? S::kUnits : 1, groups = (across + each - 1) / each;
-        const int m0 = wave / groups * 32, n0 = wave % groups * each * 32, tiles = wave < groups * down ? (across - n0 / 32 < each ? across - n0 / 32 : each) : 0;
-        if (phase == 0 && tall) S::template product<true, true>(acc, xs, xs, m0, n0, tiles, rp, lane);
-        else if (last && !tall) S::template product<false, true>(acc, as, xs, m0, n0, tiles, rp, lane);
-        else S::template product<false, false>(acc, phase == 1 ? as : xs, phase == 0 ? xs : as, m0, n0, tiles, phase == 1 ? np : cp, lane);
-        unsigned char* to = last ? xs : as;
-        if (phase == 1) {
-            const int diagonal = m0 + (lane & 31) - n0 - 4 * (lane >> 5);
+        const Tiles mine = last ? whole : square;
+        if (phase == 0 && tall) S::template product<true, true>(acc, xs, xs, mine.m0, mine.n0, mine.count, rp, lane);
+        else if (last && !tall) S::template product<false, true>(acc, as, xs, mine.m0, mine.n0, mine.count, rp, lane);
+        else S::template product<false, false>(acc, phase == 1 ? as : xs, phase == 0 ? xs : as, mine.m0, mine.n0, mine.count, phase == 1 ? np : cp, lane);
 #pragma unroll
-            for (int u = 0; u < S::kUnits; ++u)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    acc[u][v] = a.b * held[u][v] + (a.c * kUnscale) * acc[u][v] + (diagonal == 32 * u + 8 * (v / 4) + v % 4 ? a.a * kScale : 0.f);
-        } else
-#pragma unroll
-            for (int u = 0; u < S::kUnits; ++u) acc[u] *= kUnscale;
-        if (phase == 0) {                                      // (A's place holds B, which nobody reads any more)
-#pragma unroll
-            for (int u = 0; u < S::kUnits; ++u) held[u] = acc[u];
-        } else
-            tile::barrier();                                   // all have read what is overwritten
-        S::store(acc, to, m0, n0, tiles, rows, cols, lane);
+        for (int u = 0; u < S::kUnits; ++u) {
+            if (phase == 1) acc[u] = a.b * held[u] + (a.c * kUnscale) * acc[u];
+            else if (last) kept[u] = acc[u] = a.a * kept[u] + kUnscale * acc[u];
+            else held[u] = acc[u] = kUnscale * acc[u];
+        }
+        if (phase > 0) tile::barrier();                        // all have read what is overwritten (A's place holds B at first, which nobody reads any more)
+        S::store(acc, last ? xs : as, mine.m0, mine.n0, mine.count, mine.rows, mine.cols, lane);
         tile::barrier();
         phase = last ? 0 : phase + 1;
     }
@@ -654,7 +657,7 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
 struct Batch {
     int64_t ws;                                   // bytes of workspace of its matrices
     int32_t piece0, pieces, tri0, tris, app0, apps;        // places of the three kinds, in the plan's lists
-    int32_t splits, tri_tile, app_tile, beside;      // parts of k in the Gram matrices, 1 = whole; tiles of 64 or 128
+    int32_t splits, tri_tile, app_tile, pad;         // parts of k in the Gram matrices, 1 = whole; tiles of 64 or 128
 };
 int pieces_of(const Matrix& m) { return (int)((m.rp() * m.cp() + kPiece - 1) / kPiece); }
 int tris_of(const Matrix& m, int tile) {
@@ -662,9 +665,8 @@ int tris_of(const Matrix& m, int tile) {
     return n * (n + 1) / 2;
 }
 int apps_of(const Matrix& m, int tile) { return (int)((m.rp() + tile - 1) / tile * ((m.cp() + tile - 1) / tile)); }
-// the tiles of a launch that would have this many blocks with the large ones, and whether its Gram matrices have C beside them
+// the tiles of a launch that would have this many blocks with the large ones
 int tile_for(int64_t large) { return large < 192 ? 64 : 128; }
-bool beside_for(int64_t large) { return large <= 256; }
 int small_of(const Matrix& m) { return std::max(m.rows, m.cols) <= 64 ? 64 : std::max(m.rows, m.cols) <= 128 ? 128 : 0; }
 // Few Gram tiles of a long k: k is split, in parts of 512 and more (the join costs as much as 512 of k).
 int splits_of(int tile, int64_t tris, int64_t longest) {
@@ -688,7 +690,6 @@ struct Tables {
     Table piece, tri, app;
     uint32_t pieces, tris, apps;
     int splits, tri_tile, app_tile;
-    bool beside;
     double* partial;
     float* parts;
 };
@@ -702,14 +703,14 @@ template <int LAST, typename P> ff_status apply(const Tables& t, int which, cons
            : t.apps > 256   ? apply<Many, LAST, P>(t, which, a, norm, ws, stream)
                             : apply<Some, LAST, P>(t, which, a, norm, ws, stream);
 }
-// A and C of X, B of both
+// A of X, B of A
 template <class C> ff_status gram(const Tables& t, int which, const StepArgs& a, char* ws, hipStream_t stream, const char* what) {
     ff_status st;
-    const auto whole = [&] { return go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, which, a, (float*)nullptr); };
+    const auto whole = [&] { return go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, which, (float*)nullptr); };
     if constexpr (C::TILE == 64) {
         if (t.splits > 1) {
-            st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, which, a, t.parts);
-            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, a, (const float*)t.parts, t.splits);
+            st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, which, t.parts);
+            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, (const float*)t.parts, t.splits);
         } else
             st = whole();
     } else
@@ -723,7 +724,7 @@ template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, 
     if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 256, 0, stream, what, t.piece, a, norm, (const double*)t.partial, ws);
     for (int s = 0; s < steps && st == FF_OK; ++s) {
         const int which = s & 1;
-        st = t.tri_tile == 64 ? gram<Few>(t, which, a, ws, stream, what) : t.beside ? gram<Some>(t, which, a, ws, stream, what) : gram<Many>(t, which, a, ws, stream, what);
+        st = t.tri_tile == 64 ? gram<Few>(t, which, a, ws, stream, what) : t.tris > 256 ? gram<Many>(t, which, a, ws, stream, what) : gram<Some>(t, which, a, ws, stream, what);
         if (st == FF_OK) st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream) : apply<LAST, P>(t, which, a, norm, ws, stream);
     }
     return st;
@@ -827,20 +828,19 @@ Made make(const ff_muon_desc& d, const ff_muon_tensor* ts) {
         b.app0 = (int32_t)r.app.size();
         int last = first;
         int64_t tris = 0, apps = 0, few = 0, longest = 0, room = 0;
-        for (; last < large && (last == first || room + r.matrices[last].bytes(false) <= kBatch || small_of(r.matrices[last])); ++last) {
+        for (; last < large && (last == first || room + r.matrices[last].bytes() <= kBatch || small_of(r.matrices[last])); ++last) {
             const Matrix& m = r.matrices[last];
-            room += (int64_t)align256((size_t)m.bytes(false));
+            room += (int64_t)align256((size_t)m.bytes());
             tris += tris_of(m, 128);
             apps += apps_of(m, 128);
             few += tris_of(m, 64);
             longest = std::max(longest, std::max(m.rp(), m.cp()));
         }
-        b.beside = beside_for(tris);
         for (int i = first; i < last; ++i) {
             Matrix& m = r.matrices[i];
             m.ws = b.ws;
             m.piece0 = b.pieces;
-            b.ws += (int64_t)align256((size_t)m.bytes(b.beside != 0));
+            b.ws += (int64_t)align256((size_t)m.bytes());
             b.pieces += m.pieces;
             for (int32_t k = 0; k < m.pieces; ++k) r.piece.push_back({i, k});
         }
@@ -932,7 +932,7 @@ template <typename G, typename P> ff_status muon_step(const Header& head, const 
     for (int i = 0; i < head.batches; ++i) {
         const Batch& b = ((const Batch*)((const char*)plan_host + l.batches))[i];
         char* const partial = ws + b.ws;
-        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, b.tri_tile, b.app_tile, b.beside != 0, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
+        Tables ts{t, t, t, (uint32_t)b.pieces, (uint32_t)b.tris, (uint32_t)b.apps, b.splits, b.tri_tile, b.app_tile, (double*)partial, (float*)(partial + align256((size_t)b.pieces * 8))};
         ts.piece.places = (const Place*)(dev + l.piece) + b.piece0;
         ts.tri.places = (const Place*)(dev + l.tri) + b.tri0;
         ts.app.places = (const Place*)(dev + l.app) + b.app0;
@@ -963,7 +963,6 @@ struct Uniform {
     int64_t bytes;             // of workspace a matrix
     int32_t group;             // matrices worked on together
     int splits, tri_tile, app_tile;
-    bool beside;
     uint32_t tris;             // places of a group
 };
 Uniform uniform_of(const ff_orthogonalise_desc& d) {
@@ -971,9 +970,8 @@ Uniform uniform_of(const ff_orthogonalise_desc& d) {
     u.one.rows = d.rows;
     u.one.cols = d.cols;
     u.one.pieces = pieces_of(u.one);
-    u.group = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.count, kBatch / (int64_t)align256((size_t)u.one.bytes(false))));
-    u.beside = beside_for((int64_t)u.group * tris_of(u.one, 128));
-    u.bytes = (int64_t)align256((size_t)u.one.bytes(u.beside));
+    u.bytes = (int64_t)align256((size_t)u.one.bytes());
+    u.group = (int32_t)std::max<int64_t>(1, std::min<int64_t>(d.count, kBatch / u.bytes));
     u.tri_tile = tile_for((int64_t)u.group * tris_of(u.one, 128));
     u.app_tile = tile_for((int64_t)u.group * apps_of(u.one, 128));
     u.splits = splits_of(u.tri_tile, (int64_t)u.group * tris_of(u.one, 64), std::max(u.one.rp(), u.one.cp()));
@@ -1001,7 +999,7 @@ template <typename T> ff_status orthogonalise(const ff_orthogonalise_desc& d, co
         t.count = std::min(u.group, d.count - i);
         t.one.g = (const char*)x + i * t.in_step;
         t.one.p = (char*)out + i * t.out_step;
-        Tables ts{t, t, t, 0, 0, 0, u.splits, u.tri_tile, u.app_tile, u.beside, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
+        Tables ts{t, t, t, 0, 0, 0, u.splits, u.tri_tile, u.app_tile, (double*)partial, (float*)(partial + align256((size_t)u.group * u.one.pieces * 8))};
         ts.pieces = places_of(t.count, ts.piece.each = u.one.pieces);
         ts.tris = places_of(t.count, ts.tri.each = tris_of(u.one, u.tri_tile));
         ts.apps = places_of(t.count, ts.app.each = apps_of(u.one, u.app_tile));

@@ -1,0 +1,74 @@
+"""GPU precision of the Newton-Schulz products (ff_orthogonalise): a step whose every number is exact, and errors beside those of float32.
+"""
+import pytest
+import torch
+
+import paper_2203_00854_amd as P
+from oracle import muon as M
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def powers(lowest, copies):
+    """Three each of 1/2, 1/4 .. 2^-lowest and one 2^-lowest more, whose squares have the sum 1, `copies` times."""
+    return torch.tensor([2.0 ** -j for j in range(1, lowest + 1) for _ in range(3)] + [2.0 ** -lowest], device=DEV).repeat(copies)
+
+
+# Rows whose squares' sum is 4 or 16, beside a power of four of columns: 124 x 64 is a small matrix.  Of 448 x 1024 one has 10 tiles of 128 in A and B and 32 in X: one takes tiles
+# of 64, 7 of them tiles of 128 in X, 224 of them, 22 tiles of 128 in A, 220 of them, and 30 more than 256 in all three.  448 x 4096 splits k.
+EXACT = [(10, 4, 64, 1), (10, 4, 64, 300), (9, 16, 1024, 1), (9, 16, 4096, 1), (9, 16, 1024, 7), (9, 16, 1024, 22), (9, 16, 1024, 30)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tall", [False, True])
+@pytest.mark.parametrize("lowest,copies,cols,count", EXACT)
+def test_one_step_of_powers_of_two_is_exact(lowest, copies, cols, count, tall, dtype):
+    """G = u v^T with powers of two in u and +-1 in v has a power of two as norm; X, A and A^2 are powers of two, and with a = 4.125, b = -3.125, c = 2.125 so is B, for b + c = -1.  The sums
+    over u_k^2 are multiples of 2^-22 of their largest: no sum has more than 23 bits, and X = a X + B X = 3.125 X without any rounding.  Where a is added to B's diagonal first, that
+    would need 4.125 - 2^-22, which is no float32 value: 4.125 in its place is a last place of the result."""
+    u = powers(lowest, copies)
+    gen = torch.Generator(DEV).manual_seed(lowest + count)
+    u = u[torch.randperm(u.numel(), generator=gen, device=DEV)]
+    v = (torch.rand(count, 1, cols, generator=gen, device=DEV) < 0.5).float() * 2 - 1
+    g = u[None, :, None] * v
+    norm = (copies * cols) ** 0.5
+    assert norm == 2.0 ** round(torch.tensor(norm).log2().item())
+    if tall:
+        g = g.mT.contiguous()
+    out = P.ff_orthogonalise(g.to(DTYPES[dtype]), steps=1, coefficients=(4.125, -3.125, 2.125), eps=0.0)
+    assert torch.equal(out, (3.125 / norm * g).to(DTYPES[dtype]))
+
+
+def gradients(rows, cols, seed):
+    """Few large singular values above noise."""
+    gen = torch.Generator(DEV).manual_seed(seed)
+    randn = lambda *s: torch.randn(*s, generator=gen, device=DEV)  # noqa: E731
+    k = min(8, rows, cols)
+    return randn(rows, k) @ (randn(k, cols) * torch.exp(-torch.arange(k, device=DEV) / 2)[:, None]) + 0.2 * randn(rows, cols)
+
+
+def newton_schulz(g, dtype, eps=1e-7):
+    tall = g.shape[0] > g.shape[1]
+    x = (g.double() / (g.double().norm() + eps)).to(dtype)
+    a, b, c = M.COEFFICIENTS
+    for _ in range(5):
+        gram = x.mT.contiguous() @ x if tall else x @ x.mT.contiguous()
+        poly = b * gram + c * (gram @ gram)
+        x = a * x + (x @ poly if tall else poly @ x)
+    return x
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 128), (128, 128), (100, 64), (512, 512), (700, 1100), (1100, 700), (1024, 2048), (2048, 2048), (4096, 1024)])
+def test_errors_beside_those_of_float32(rows, cols):
+    """A pair of float16 is off by up to 2^-23 of its value where its lower part is of the upper half of its range, and 2^-24, 2^-25 .. below: a deviation of 0.87 2^-24, 1.5 times
+    that of a float32 value (2^-24 / sqrt 3).  Sums are float32 on both sides.  So the error in norm, a sum over all values, is 1.5 times that of the same formulas in float32 at most; twice leaves room for
+    how sums are ordered."""
+    for seed in range(3):
+        g = gradients(rows, cols, seed)
+        want = newton_schulz(g, torch.float64)
+        plain = (newton_schulz(g, torch.float32).double() - want).norm()
+        got = (P.ff_orthogonalise(g).double() - want).norm()
+        print(f"{rows} x {cols}: {got / want.norm():.2e}, float32 {plain / want.norm():.2e}", flush=True)
+        assert got <= 2 * plain
