@@ -428,9 +428,10 @@ ff_status ff_gated_transition_backward(const ff_transition_desc* desc, const voi
 /* Orthogonalising a matrix by Newton-Schulz products: X = G / (|G| + eps) with the root of the sum of squares as norm, then `steps` times, with n the
  * shorter side and A = X X^T [n, n] (X^T X for a matrix with more rows than columns):
  *   X = a X + (b A + c A^2) X      (X (b A + c A^2))
- * which brings all singular values near 1.  Norms are float64, sums float32; X, A and the polynomial are held as pairs of float16 values, 23
- * significant bits together, with places for magnitudes below 255 (the usual coefficients 3.4445, -4.7750, 2.0315 keep singular values below 1.3; coefficients that let them
- * grow past that give infinities). */
+ * which brings all singular values near 1.  Norms are float64, sums float32; X, A and b A + c A^2 are held as pairs of float16 values, 23
+ * significant bits together.  A and b A + c A^2 have places for magnitudes below 255, 2^-32 apart; X is held times a power of two that a bound of its norm sets in every step, so that
+ * it keeps its digits where |G| is far below eps, and has places for magnitudes below 255 too.  (The usual coefficients 3.4445, -4.7750, 2.0315 keep singular values below 1.3;
+ * coefficients that let values grow past those places give infinities and NaN.) */
 typedef struct {
     int32_t dtype;              /* ff_dtype of x and out */
     int32_t count;              /* matrices, one after another, >= 0 */

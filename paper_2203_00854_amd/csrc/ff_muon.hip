@@ -4,12 +4,14 @@
 //
 // Three launches a step for all matrices together: A; B = b A + c A^2; X = a X + B X.  What is added behind a product is added in float32: with a I inside B the rounding of B's
 // diagonal, another one in each row, would carry the large singular directions into the small ones, which the next steps make larger (2048 x 2048: an
-// error of 3.2e-6 in norm instead of 1.3e-6; b I inside an operand of B's product likewise, 256 x 256 2.1e-6 instead of 2.0e-6).  Values are held as float16 pairs of kScale times
-// themselves: 23 significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  Magnitudes
-// to 255 have a place, and singular values are at most 1 at the start and below 1.3 after any number of steps with the usual coefficients; 2^-33 is
-// the smallest step between small values.  A tall matrix is worked on as it lies: its operands are read turned.
+// error of 3.2e-6 in norm instead of 1.3e-6; b I inside an operand of B's product likewise, 256 x 256 2.1e-6 instead of 2.0e-6).  Values are held as float16 pairs: 23
+// significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  A and B are held times kScale, so that magnitudes to
+// 255 have a place and the smallest are 2^-32 apart.  X is held times a power of two of its own in each step, from a bound of its norm: an update far below eps is a
+// small X, of which a fixed factor would leave few bits or none (at 10^-5 eps, times 256: an error of 2e-3), and large matrices have small values.  With the usual coefficients singular
+// values are at most 1 at the start and below 1.3 after any number of steps.  A tall matrix is worked on as it lies: its operands are read turned.
 #include "ff_tile.h"
 
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 
@@ -28,8 +30,9 @@ using tile::round_up;
 
 namespace {
 
-constexpr float kScale = 256.f, kUnscale = 1.f / 256.f;
+constexpr float kRoot = 16.f, kScale = kRoot * kRoot, kUnscale = 1.f / kScale;
 constexpr int kPad = 16;
+constexpr int64_t kHead = 256;                   // bytes in front of a matrix's workspace: the factor of X in each step, 64 floats
 constexpr int kMostBlocks = 1 << 22;             // of a launch: 2^32 threads a grid
 constexpr int kXcds = 8;                         // block i starts on XCD i % 8: places are laid out so that a matrix stays with one, whose L2 its tiles share
 constexpr int kPiece = 4096;                     // values that a block of the element-wise kernels holds
@@ -42,7 +45,7 @@ struct Matrix {
     void* p;                                     // what the last step writes
     float* master;
     float* m;
-    int64_t ws;                                  // bytes into the workspace: X, X of the next step, A and B as pairs
+    int64_t ws;                                  // bytes into the workspace: the factors of X; X, X of the next step, A and B as pairs
     int32_t rows, cols;
     int32_t piece0, pieces;                      // among the batch's
     float decay;
@@ -53,9 +56,9 @@ struct Matrix {
     __host__ __device__ int64_t np() const { return tall() ? cp() : rp(); }
     __host__ __device__ int64_t bytes_x() const { return rp() * cp() * 4; }
     __host__ __device__ int64_t bytes_a() const { return np() * np() * 4; }
-    __host__ __device__ int64_t x(int which) const { return ws + which * bytes_x(); }
-    __host__ __device__ int64_t a(int which) const { return ws + 2 * bytes_x() + which * bytes_a(); }
-    __host__ __device__ int64_t bytes() const { return 2 * (bytes_x() + bytes_a()); }
+    __host__ __device__ int64_t x(int which) const { return ws + kHead + which * bytes_x(); }
+    __host__ __device__ int64_t a(int which) const { return ws + kHead + 2 * bytes_x() + which * bytes_a(); }
+    __host__ __device__ int64_t bytes() const { return kHead + 2 * (bytes_x() + bytes_a()); }
 };
 struct Place {
     int32_t matrix, at;                          // matrix < 0: none
@@ -126,8 +129,23 @@ struct StepArgs {
     float lr, beta, rest, max_norm;
     double eps;
     float a, b, c;
+    float top_at[2], top[2];                     // where |a t + b t^3 + c t^5| has its maxima, and how high they are
     int32_t nesterov, rms;
 };
+// X has a norm, and values, of at most `bound`: the power of two that brings them below 2^14, of float16's 2^16.  (256 at least: a bound passes 255 with coefficients that let X
+// grow, perhaps without X.  2^120 at most, so that its inverse and what is multiplied with it are float32 values of full precision.)
+__device__ __forceinline__ float factor_of(float bound) {
+    const int e = 140 - (int)(__float_as_uint(bound) >> 23 & 255u);
+    return __uint_as_float((uint32_t)(127 + (e < 8 ? 8 : e > 120 ? 120 : e)) << 23);
+}
+constexpr float kRoom = 1.f + 1.f / 256.f;       // for roundings of the bound and of X
+__device__ __forceinline__ float next_bound(float bound, const StepArgs& a) {
+    const float q = bound * bound;
+    float v = fabsf(bound * (a.a + q * (a.b + q * a.c)));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v = a.top_at[i] < bound && v < a.top[i] ? a.top[i] : v;
+    return v * kRoom;
+}
 __device__ __forceinline__ float clip_of(const float* norm, float max_norm, bool& skip) {
     if (!norm) return 1.f;
     const float n = *norm;
@@ -191,8 +209,10 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_m
     if (threadIdx.x == 0) partial[x.piece0 + at.at] = sums[0];
 }
 
-// X = update / (norm + eps) as pairs, its padding zeros.  Bound by HBM likewise: 158 us for 770 MB.  (The update is formed again: it would be another 4 bytes a value.)
-template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_start(Table t, StepArgs a, const float* norm, const double* partial, char* ws) {
+__device__ __forceinline__ float* factors_of(const Matrix& x, char* ws) { return (float*)(ws + x.ws); }
+
+// X = update / (norm + eps) as pairs, its padding zeros, and its factors.  Bound by HBM likewise: 158 us for 770 MB.  (The update is formed again: it would be another 4 bytes a value.)
+template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_start(Table t, StepArgs a, const float* norm, const double* partial, char* ws, int steps) {
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
     const Matrix x = matrix_of(t, at.matrix);
@@ -208,7 +228,11 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
         if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
         __syncthreads();
     }
-    const double inv = (double)kScale / (sqrt(sums[0]) + a.eps);
+    const double length = sqrt(sums[0]);
+    float bound = (float)(length / (length + a.eps)) * kRoom;
+    const double inv = (double)factor_of(bound) / (length + a.eps);
+    if (at.at == 0 && threadIdx.x == 0)
+        for (int s = 0; s < steps; ++s, bound = next_bound(bound, a)) factors_of(x, ws)[s] = factor_of(bound);
     const int64_t end = x.rp() * x.cp(), first = (int64_t)at.at * kPiece;
     char* out = ws + x.x(0);
     for (int64_t i = first + threadIdx.x * 8; i < first + kPiece && i < end; i += 256 * 8) {
@@ -262,7 +286,7 @@ __device__ __forceinline__ void store_gram(char* a, int64_t np, int64_t m, int64
 
 // A.  SPLIT: sums over a part of k each, for k_ns_join.  48 blocks: 127 us for 2016 tiles, the matrix units 0.38 busy, 480 MB through HBM at 3.7 TB/s: k is 256 long for most tiles, so a third is
 // the way in and out.  4096 x 1024: 136 tiles of 64 in three parts each 26 us and 6 for the join.
-template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int which, float* parts) {
+template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int step, float* parts) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -271,7 +295,8 @@ template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) voi
     const Matrix x = matrix_of(t, at.matrix);
     int i, j;
     triangle(at.at, i, j);
-    const Operand o = operand_x(x, ws, which);
+    const Operand o = operand_x(x, ws, step & 1);
+    const float factor = factors_of(x, ws)[step];
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     const int64_t all = x.tall() ? x.rp() : x.cp(), each = SPLIT ? (all / kPad + gridDim.y - 1) / gridDim.y * kPad : all, from = SPLIT ? blockIdx.y * each : 0;
@@ -282,9 +307,10 @@ template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) voi
         float* out = parts + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kTile * kTile;
         Straight::rows(acc[0], 0, 0, smem, Straight::none, [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) { tile::store8(out + m * kTile + n, v); });
     } else {
+        const float by = kRoot / factor;                           // its square is kScale over that of X's factor (and no float32 value where that is large)
         const auto store = [&](int64_t m, int64_t n, float (&v)[8], typename Straight::Nothing) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
+            for (int q = 0; q < 8; ++q) v[q] = v[q] * by * by;
             store_gram(ws + x.a(0), x.np(), m, n, v);
         };
         Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, Straight::none, store);
@@ -293,7 +319,7 @@ template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) voi
 }
 
 // A of its parts, added up in their order; a block has 32 rows of a tile
-__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float* parts, int splits) {
+__global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, int step, const float* parts, int splits) {
     constexpr int kTile = Few::TILE, kBand = 32, kPitch = kBand + 1;
     __shared__ float band[kTile * kPitch];
     const Place at = place_at(t, blockIdx.x);
@@ -304,6 +330,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float*
     const int64_t np = x.np(), m0 = (int64_t)i * kTile + blockIdx.y * kBand, n0 = (int64_t)j * kTile;
     char* to = ws + x.a(0);
     const int64_t next = (int64_t)gridDim.x * kTile * kTile;
+    const float by = kRoot / factors_of(x, ws)[step];
     const float* from = parts + ((int64_t)blockIdx.x * kTile + blockIdx.y * kBand) * kTile;
     for (int u = threadIdx.x; u < kBand * kTile / 8; u += 256) {
         const int r = u / (kTile / 8), c = u % (kTile / 8) * 8;
@@ -315,7 +342,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, const float*
             for (int q = 0; q < 8; ++q) v[q] += more[q];
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q) band[(c + q) * kPitch + r] = v[q] *= kUnscale;
+        for (int q = 0; q < 8; ++q) band[(c + q) * kPitch + r] = v[q] = v[q] * by * by;
         store_gram(to, np, m0 + r, n0 + c, v);
     }
     if (i == j) return;
@@ -379,7 +406,7 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
 }
 // X = a X + B X (a X + X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights.  48 blocks 200 us for 785 MB (the last, with weights and masters, 283 for 1.25 GB);
 // 4096 x 1024 36 us, 256 tiles, one a unit, 23 of them matrix instructions at the rate of a large product.
-template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_apply(Table t, char* ws, int which, StepArgs a, const float* norm) {
+template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_apply(Table t, char* ws, int step, StepArgs a, const float* norm) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -393,25 +420,24 @@ template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kB
     }
     const int64_t rp = x.rp(), cp = x.cp();
     const int ntiles = (int)((cp + kTile - 1) / kTile), i = at.at / ntiles, j = at.at % ntiles;
-    const Operand ox = operand_x(x, ws, which), ob = operand_a(x, ws, 1);
+    const Operand ox = operand_x(x, ws, step & 1), ob = operand_a(x, ws, 1);
+    const float factor = factors_of(x, ws)[step], next = LAST == kMore ? factors_of(x, ws)[step + 1] : 1.f;
     f32x16 acc[1][Straight::MT][Straight::NT];
     Straight::clear(acc);
     if (x.tall()) Straight::run(acc, &ox, &ob, (int64_t)i * kTile, (int64_t)j * kTile, 0, cp, smem);
     else C::Mixed::run(acc, &ob, &ox, (int64_t)i * kTile, (int64_t)j * kTile, 0, rp, smem);
-    char* to = ws + x.x(which ^ 1);
-    const float size = size_of(x, a);
-    const char* was = ws + x.x(which);
+    char* to = ws + x.x(~step & 1);
+    const float size = size_of(x, a), by = next / factor;
+    const char* was = ws + x.x(step & 1);
     const auto fetch = [&](int64_t m, int64_t n) { return m < rp && n < cp ? load_pairs(was + pairs_at(m * cp + n)) : Pairs{}; };
     Straight::rows(acc[0], (int64_t)i * kTile, (int64_t)j * kTile, smem, fetch, [&](int64_t m, int64_t n, float (&v)[8], const Pairs& old) {
         if (m >= rp || n >= cp) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = a.a * value_of(old, q) + kUnscale * v[q];
+        for (int q = 0; q < 8; ++q) v[q] = (a.a * value_of(old, q) + kUnscale * v[q]) * by;
         if constexpr (LAST == kMore) store_pairs(to + pairs_at(m * cp + n), v);
         else {
             const int left = x.cols - (int)n;
             if (m >= x.rows || left <= 0) return;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] *= kUnscale;
             finish<LAST, P>(x, a, size, m * x.cols + n, left, v);
         }
     });
@@ -593,7 +619,9 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
         __syncthreads();
     }
-    const double inv = (double)kScale / (sqrt(sums[0]) + a.eps);
+    const double length = sqrt(sums[0]);
+    float bound = (float)(length / (length + a.eps)) * kRoom, factor = factor_of(bound);
+    const double inv = (double)factor / (length + a.eps);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
@@ -627,18 +655,25 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         if (phase == 0 && tall) S::template product<true, true>(acc, xs, xs, mine.m0, mine.n0, mine.count, rp, lane);
         else if (last && !tall) S::template product<false, true>(acc, as, xs, mine.m0, mine.n0, mine.count, rp, lane);
         else S::template product<false, false>(acc, phase == 1 ? as : xs, phase == 0 ? xs : as, mine.m0, mine.n0, mine.count, phase == 1 ? np : cp, lane);
+        float by = kRoot / factor;                              // as in k_ns_gram
+        if (last) {
+            bound = next_bound(bound, a);
+            const float next = factor_of(bound);
+            by = next / factor;
+            factor = next;
+        }
 #pragma unroll
         for (int u = 0; u < S::kUnits; ++u) {
             if (phase == 1) acc[u] = a.b * held[u] + (a.c * kUnscale) * acc[u];
-            else if (last) kept[u] = acc[u] = a.a * kept[u] + kUnscale * acc[u];
-            else held[u] = acc[u] = kUnscale * acc[u];
+            else if (last) kept[u] = acc[u] = (a.a * kept[u] + kUnscale * acc[u]) * by;
+            else held[u] = acc[u] = acc[u] * by * by;
         }
         if (phase > 0) tile::barrier();                        // all have read what is overwritten (A's place holds B at first, which nobody reads any more)
         S::store(acc, last ? xs : as, mine.m0, mine.n0, mine.count, mine.rows, mine.cols, lane);
         tile::barrier();
         phase = last ? 0 : phase + 1;
     }
-    const float size = size_of(x, a);
+    const float size = size_of(x, a), by = 1.f / factor;
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int place = (i * S::kThreads + (int)threadIdx.x) * 8;
@@ -648,7 +683,7 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         const Pairs p{*(const uint4*)(xs + S::at((int)s.r, s.c, 0)), *(const uint4*)(xs + S::at((int)s.r, s.c, 1))};
         float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = kUnscale * value_of(p, q);
+        for (int q = 0; q < 8; ++q) v[q] = by * value_of(p, q);
         finish<LAST, P>(x, a, size, s.at, s.n, v);
     }
 }
@@ -693,24 +728,37 @@ struct Tables {
     double* partial;
     float* parts;
 };
+// the polynomial and its maxima: the roots t^2 of a + 3 b t^2 + 5 c t^4
+void polynomial(StepArgs& s, double a, double b, double c) {
+    s.a = (float)a;
+    s.b = (float)b;
+    s.c = (float)c;
+    const double half = 3 * b / 2, disc = half * half - 5 * c * a, root = half < 0 ? half - sqrt(std::max(disc, 0.)) : half + sqrt(std::max(disc, 0.));
+    const double q[2] = {root != 0 ? -a / root : 0, c != 0 ? -root / (5 * c) : 0};
+    for (int i = 0; i < 2; ++i) {
+        const bool there = disc >= 0 && q[i] > 0;
+        s.top_at[i] = there ? (float)sqrt(q[i]) : INFINITY;
+        s.top[i] = there ? (float)fabs(sqrt(q[i]) * (a + q[i] * (b + q[i] * c))) : 0.f;
+    }
+}
 template <int LAST> constexpr const char* kWhat = LAST == kWeights ? "ff_muon_step" : "ff_orthogonalise";
 
-template <class C, int LAST, typename P> ff_status apply(const Tables& t, int which, const StepArgs& a, const float* norm, char* ws, hipStream_t stream) {
-    return go<k_ns_apply<LAST, P, C>>(KK_NS_APPLY, t.apps, 256, C::kLds, stream, kWhat<LAST>, t.app, ws, which, a, norm);
+template <class C, int LAST, typename P> ff_status apply(const Tables& t, int step, const StepArgs& a, const float* norm, char* ws, hipStream_t stream) {
+    return go<k_ns_apply<LAST, P, C>>(KK_NS_APPLY, t.apps, 256, C::kLds, stream, kWhat<LAST>, t.app, ws, step, a, norm);
 }
-template <int LAST, typename P> ff_status apply(const Tables& t, int which, const StepArgs& a, const float* norm, char* ws, hipStream_t stream) {
-    return t.app_tile == 64 ? apply<Few, LAST, P>(t, which, a, norm, ws, stream)
-           : t.apps > 256   ? apply<Many, LAST, P>(t, which, a, norm, ws, stream)
-                            : apply<Some, LAST, P>(t, which, a, norm, ws, stream);
+template <int LAST, typename P> ff_status apply(const Tables& t, int step, const StepArgs& a, const float* norm, char* ws, hipStream_t stream) {
+    return t.app_tile == 64 ? apply<Few, LAST, P>(t, step, a, norm, ws, stream)
+           : t.apps > 256   ? apply<Many, LAST, P>(t, step, a, norm, ws, stream)
+                            : apply<Some, LAST, P>(t, step, a, norm, ws, stream);
 }
 // A of X, B of A
-template <class C> ff_status gram(const Tables& t, int which, const StepArgs& a, char* ws, hipStream_t stream, const char* what) {
+template <class C> ff_status gram(const Tables& t, int step, const StepArgs& a, char* ws, hipStream_t stream, const char* what) {
     ff_status st;
-    const auto whole = [&] { return go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, which, (float*)nullptr); };
+    const auto whole = [&] { return go<k_ns_gram<C, false>>(KK_NS_GRAM, t.tris, 256, C::kLds, stream, what, t.tri, ws, step, (float*)nullptr); };
     if constexpr (C::TILE == 64) {
         if (t.splits > 1) {
-            st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, which, t.parts);
-            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, (const float*)t.parts, t.splits);
+            st = go<k_ns_gram<C, true>>(KK_NS_GRAM, dim3(t.tris, t.splits), 256, C::kLds, stream, what, t.tri, ws, step, t.parts);
+            if (st == FF_OK) st = go<k_ns_join>(KK_NS_GRAM, dim3(t.tris, 2), 256, 0, stream, what, t.tri, ws, step, (const float*)t.parts, t.splits);
         } else
             st = whole();
     } else
@@ -721,11 +769,10 @@ template <typename G, typename P, int LAST> ff_status steps_of(const Tables& t, 
     constexpr bool MUON = LAST == kWeights;
     const char* what = kWhat<LAST>;
     ff_status st = go<k_muon_momentum<G, MUON>>(KK_MUON_MOMENTUM, t.pieces, 256, 0, stream, what, t.piece, a, norm, t.partial);
-    if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 256, 0, stream, what, t.piece, a, norm, (const double*)t.partial, ws);
+    if (st == FF_OK) st = go<k_ns_start<G, MUON>>(KK_NS_START, t.pieces, 256, 0, stream, what, t.piece, a, norm, (const double*)t.partial, ws, steps);
     for (int s = 0; s < steps && st == FF_OK; ++s) {
-        const int which = s & 1;
-        st = t.tri_tile == 64 ? gram<Few>(t, which, a, ws, stream, what) : t.tris > 256 ? gram<Many>(t, which, a, ws, stream, what) : gram<Some>(t, which, a, ws, stream, what);
-        if (st == FF_OK) st = s + 1 < steps ? apply<kMore, float>(t, which, a, norm, ws, stream) : apply<LAST, P>(t, which, a, norm, ws, stream);
+        st = t.tri_tile == 64 ? gram<Few>(t, s, a, ws, stream, what) : t.tris > 256 ? gram<Many>(t, s, a, ws, stream, what) : gram<Some>(t, s, a, ws, stream, what);
+        if (st == FF_OK) st = s + 1 < steps ? apply<kMore, float>(t, s, a, norm, ws, stream) : apply<LAST, P>(t, s, a, norm, ws, stream);
     }
     return st;
 }
@@ -947,7 +994,15 @@ template <typename G, typename P> ff_status muon_step(const Header& head, const 
 
 ff_status muon_step_run(const ff_muon_desc& d, const void* plan_host, const void* plan, const ff_muon_hyper& h, const float* norm, void* ws, hipStream_t stream) {
     const Header& head = *(const Header*)plan_host;
-    const StepArgs a{(float)h.lr, (float)h.beta, (float)(1. - h.beta), norm ? (float)h.max_norm : 0.f, h.eps, (float)h.a, (float)h.b, (float)h.c, h.nesterov, h.scale == FF_MUON_RMS};
+    StepArgs a{};
+    a.lr = (float)h.lr;
+    a.beta = (float)h.beta;
+    a.rest = (float)(1. - h.beta);
+    a.max_norm = norm ? (float)h.max_norm : 0.f;
+    a.eps = h.eps;
+    polynomial(a, h.a, h.b, h.c);
+    a.nesterov = h.nesterov;
+    a.rms = h.scale == FF_MUON_RMS;
     const char* dev = (const char*)plan;
     if (d.param_dtype == FF_F32)
         return d.grad_dtype == FF_F32 ? muon_step<float, float>(head, plan_host, dev, a, h.steps, norm, (char*)ws, stream)
@@ -982,9 +1037,7 @@ template <typename T> ff_status orthogonalise(const ff_orthogonalise_desc& d, co
     const Uniform u = uniform_of(d);
     StepArgs a{};
     a.eps = d.eps;
-    a.a = (float)d.a;
-    a.b = (float)d.b;
-    a.c = (float)d.c;
+    polynomial(a, d.a, d.b, d.c);
     Table t{};
     t.one = u.one;
     t.in_step = t.out_step = (int64_t)d.rows * d.cols * (int64_t)sizeof(T);

@@ -72,3 +72,52 @@ def test_errors_beside_those_of_float32(rows, cols):
         got = (P.ff_orthogonalise(g).double() - want).norm()
         print(f"{rows} x {cols}: {got / want.norm():.2e}, float32 {plain / want.norm():.2e}", flush=True)
         assert got <= 2 * plain
+
+
+# a small matrix of either kind, tiles of 64, a k that is split, and tiles of 128: some, and many
+SMALL_UPDATES = [(1, 24, 50), (2, 128, 100), (1, 300, 700), (1, 700, 300), (1, 150, 2000), (7, 448, 1024), (30, 1024, 448)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count,rows,cols", SMALL_UPDATES)
+def test_updates_far_below_eps_keep_their_digits(count, rows, cols, dtype):
+    """With |G| = r eps and r of 10^-5 and less X stays below 5 10^-3 in five steps, and a step is X = a X but for 5 X^3 (of the oracle too).  A value is rounded to a pair, 2^-23 at most, and by
+    one product, one sum and one coefficient, 2^-24 each; once more at the start: 36 units of 2^-24 in six.  (X^3, a few 10^-5 of X, brings its own 23 bits: less than a unit.)  Values
+    below 2^-15 of the largest lose digits to float16's smallest step, of 2^-38 of it: counted as a unit of the mean value."""
+    g = torch.stack([gradients(rows, cols, i) for i in range(count)])
+    g /= g.norm(dim=(1, 2), keepdim=True)
+    half = M.U if dtype == "f32" else 2.0 ** -8
+    for length, eps in ((1e-12, 1e-7), (1e-20, 1e-7), (1e-7, 1e-2), (1e-30, 1.0)):
+        x = (length * g).to(DTYPES[dtype])
+        got = P.ff_orthogonalise(x, eps=eps)
+        for i in {0, count - 1}:
+            want = newton_schulz(x[i], torch.float64, eps)
+            bound = 36 * M.U * (want.abs() + want.square().mean().sqrt())
+            off = (got[i].double() - want).abs()
+            print(f"{rows} x {cols} {dtype}, |G| {length}, eps {eps}: {(off / (bound + half * want.abs() + 1e-300)).max():.2f} of the bound", flush=True)
+            assert bool((off <= bound + half * (want.abs() + bound)).all())
+
+
+def test_a_step_of_updates_far_below_eps():
+    """The same in the Muon step: weights that are zero move by the update alone."""
+    shapes = [(24, 50), (50, 100), (300, 200)]
+    for more in ([], [(40, 30)] * 70):                       # with so many the small ones are launched by themselves
+        each = [1e-10 * gradients(*s, i) / gradients(*s, i).norm() for i, s in enumerate(shapes + more)]
+        p, m = [torch.zeros_like(g) for g in each], [torch.zeros_like(g) for g in each]
+        P.ff_muon_step(P.make_muon_plan(p, each, m), 0.5, beta=0.0, nesterov=False, eps=1e-2)
+        for w, g in zip(p, each):
+            want = -0.5 * M.step_size("spectral", *g.shape) * newton_schulz(g, torch.float64, 1e-2)
+            # as above, and the factor, the product with it and the sum
+            assert bool(((w.double() - want).abs() <= 42 * M.U * (want.abs() + want.square().mean().sqrt())).all())
+
+
+@pytest.mark.parametrize("coefficients", [(2.0, -1.5, 0.5), (1.5, -0.5, 0.0), (-1.0, 0.0, 0.0), (0.0, 0.0, 3.0), (4.0, -8.0, 4.5), (5.0, 0.0, 0.0), (0.5, 1.0, 1.0)])
+def test_coefficients(coefficients):
+    """Polynomials with two, one and no maxima, that shrink X and let it grow, within the places that values have; against the oracle's bound."""
+    for rows, cols in ((24, 50), (100, 128), (200, 150)):
+        x = gradients(rows, cols, 1)
+        g = x.cpu().double().numpy()
+        for steps in (1, 3):
+            total, most = M.roundings(g, steps, coefficients)
+            off = abs(P.ff_orthogonalise(x, steps=steps, coefficients=coefficients).cpu().double().numpy() - M.orthogonalise(g, steps, coefficients))
+            assert off.max() <= most + 2 * M.U, (rows, steps, off.max(), most)
