@@ -425,7 +425,7 @@ ff_status ff_gated_transition_backward(const ff_transition_desc* desc, const voi
                                        const void* dy, const float* mask, void* dx, void* dw_a, void* dw_b, void* dw_o, int32_t grad_dtype,
                                        int32_t accumulate, void* ws, size_t ws_bytes, void* hip_stream);
 
-/* Orthogonalising a matrix by Newton-Schulz products: X = G / (|G| + eps) with the root of the sum of squares as norm, then `steps` times, with n the
+/* Orthogonalising a matrix by Newton-Schulz products: X = G / (|G| + eps) with the root of the sum of squares as norm (0 for a matrix of zeros, with eps = 0 too), then `steps` times, with n the
  * shorter side and A = X X^T [n, n] (X^T X for a matrix with more rows than columns):
  *   X = a X + (b A + c A^2) X      (X (b A + c A^2))
  * which brings all singular values near 1.  Norms are float64, sums float32; X, A and b A + c A^2 are held as pairs of float16 values, 23

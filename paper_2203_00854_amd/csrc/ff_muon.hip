@@ -139,6 +139,11 @@ __device__ __forceinline__ float factor_of(float bound) {
     return __uint_as_float((uint32_t)(127 + (e < 8 ? 8 : e > 120 ? 120 : e)) << 23);
 }
 constexpr float kRoom = 1.f + 1.f / 256.f;       // for roundings of the bound and of X
+// of X = G by, by = 1 / (norm + eps).  Where both are 0 so is G, and its X is 0 as with any other eps: 0 / 0 would turn the weights of a matrix that has no gradient yet into NaN.
+__device__ __forceinline__ float first_bound(double norm, double eps, double& by) {
+    by = norm + eps == 0. ? 0. : 1. / (norm + eps);
+    return (float)(norm * by) * kRoom;
+}
 __device__ __forceinline__ float next_bound(float bound, const StepArgs& a) {
     const float q = bound * bound;
     float v = fabsf(bound * (a.a + q * (a.b + q * a.c)));
@@ -228,9 +233,9 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_sta
         if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
         __syncthreads();
     }
-    const double length = sqrt(sums[0]);
-    float bound = (float)(length / (length + a.eps)) * kRoom;
-    const double inv = (double)factor_of(bound) / (length + a.eps);
+    double by;
+    float bound = first_bound(sqrt(sums[0]), a.eps, by);
+    const double inv = by * factor_of(bound);
     if (at.at == 0 && threadIdx.x == 0)
         for (int s = 0; s < steps; ++s, bound = next_bound(bound, a)) factors_of(x, ws)[s] = factor_of(bound);
     const int64_t end = x.rp() * x.cp(), first = (int64_t)at.at * kPiece;
@@ -619,9 +624,9 @@ template <int SIZE, int LAST, typename G, typename P> __global__ __launch_bounds
         if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
         __syncthreads();
     }
-    const double length = sqrt(sums[0]);
-    float bound = (float)(length / (length + a.eps)) * kRoom, factor = factor_of(bound);
-    const double inv = (double)factor / (length + a.eps);
+    double per;
+    float bound = first_bound(sqrt(sums[0]), a.eps, per), factor = factor_of(bound);
+    const double inv = per * factor;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {

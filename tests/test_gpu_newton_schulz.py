@@ -121,3 +121,30 @@ def test_coefficients(coefficients):
             total, most = M.roundings(g, steps, coefficients)
             off = abs(P.ff_orthogonalise(x, steps=steps, coefficients=coefficients).cpu().double().numpy() - M.orthogonalise(g, steps, coefficients))
             assert off.max() <= most + 2 * M.U, (rows, steps, off.max(), most)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_zeros_without_eps(dtype):
+    """A matrix of zeros stays one, beside others."""
+    for rows, cols in ((20, 10), (128, 90), (200, 300)):
+        x = torch.stack([gradients(rows, cols, i) for i in range(3)]).to(DTYPES[dtype])
+        want = P.ff_orthogonalise(x, eps=0.0)
+        x[1] = 0
+        got = P.ff_orthogonalise(x, eps=0.0)
+        assert not got[1].any() and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("param", ["f32", "master", "bf16"])
+def test_a_step_without_a_gradient_and_without_eps(param):
+    """No gradient and no momentum: the weight decay alone."""
+    for shapes in ([(20, 10), (300, 200)], [(20, 10), (128, 90), (300, 200)] * 25):
+        kind = torch.float32 if param == "f32" else torch.bfloat16
+        p = [gradients(*s, i).to(kind) for i, s in enumerate(shapes)]
+        master = [t.float() for t in p] if param == "master" else None
+        g, m = [torch.zeros_like(t) for t in p], P.muon_states(p)["m"]
+        before = [t.clone() for t in (master or p)]
+        P.ff_muon_step(P.make_muon_plan(p, g, m, master=master, weight_decay=0.5), 0.25, eps=0.0)
+        for after, was in zip(master or p, before):
+            # 0.125 w is exact, and the difference has one rounding
+            assert torch.equal(after, (was.double() * 0.875).to(after.dtype))
+        assert not any(t.any() for t in m)
