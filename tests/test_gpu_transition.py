@@ -66,6 +66,7 @@ class Problem:
 SIZES = [(1, 1, 1), (1, 16, 16), (3, 7, 5), (40, 64, 128), (129, 33, 70), (300, 96, 64), (257, 128, 512), (130, 256, 160), (200, 200, 312), (64, 520, 48), (300, 300, 96), (100, 32, 33), (161, 192, 256), (500, 256, 300), (400, 64, 288), (300, 512, 272),
          # few hidden channels, or many rows: rows in registers
          (2000, 250, 61), (1500, 190, 100), (700, 256, 64), (520, 192, 96), (4000, 96, 130), (9000, 128, 512),
+         # with the sizes of test_gpu_transition_routes.py:
          # every tile of the other kernels
          (7000, 320, 1040), (3000, 272, 544)]
 
