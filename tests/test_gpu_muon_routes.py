@@ -68,3 +68,28 @@ def test_steps(name, param, grad):
         else:
             bound = bound + HALF[kind] * want.norm()
         assert (after - want).norm() <= bound, (s, (after - want).norm(), bound)
+
+
+@pytest.mark.parametrize("rows,cols", [(32768, 32768), (32768, 1), (1, 32768), (130, 32768), (32768, 130)])
+def test_largest_matrices(rows, cols):
+    """One step of the largest sides, whose X and A reach 4 GiB each: some rows of it in float64, from X alone."""
+    g = gradients(rows, cols, rows + cols)                # (large singular values, or the products would be small beside a X)
+    some = sorted({0, 1, rows // 3, rows - 2, rows - 1} & set(range(rows)))
+    out = P.ff_orthogonalise(g, steps=1)
+    a, b, c = M.COEFFICIENTS
+
+    def product(left, turned):                              # by parts of the rows of g, in float64
+        parts = [g[at:at + 4096].double() for at in range(0, rows, 4096)]
+        if turned:
+            return torch.cat([left @ p.mT.contiguous() for p in parts], 1)
+        return sum(left[:, 4096 * i:4096 * i + p.shape[0]] @ p for i, p in enumerate(parts))
+
+    length = sum(g[at:at + 4096].double().square().sum() for at in range(0, rows, 4096)).sqrt() + 1e-7
+    x = g[some].double() / length
+    once = product(product(x, True), False) / length ** 2             # X X^T X
+    want = a * x + b * once + c * product(product(once, True), False) / length ** 2
+    off = (out[some].double() - want).norm() / want.norm()
+    # a value of X, A, B: 2^-23 at most, in a sum of terms of any sign no more of it in norm; float32 sums of n terms of one sign (A's diagonal) or any: 8 deviations of 2^-24 (n / 2)^(1/2)
+    bound = (4 * 2 + 8 * (max(rows, cols) / 2) ** 0.5) * M.U * (a - b + c) * x.norm() / want.norm()
+    print(f"{rows} x {cols}: {off:.2e} of {bound:.2e}", flush=True)
+    assert off <= bound

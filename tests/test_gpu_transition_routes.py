@@ -96,3 +96,25 @@ def test_weights_of_wide_tokens(dtype):
         q = Problem(40, 8192, 1, dtype)
         q.w, q.x = p.w, p.x[part]
         q.check_forward(y[part])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_most_channels(dtype):
+    """8192 channels with 32768 hidden ones, weights of up to 1 GiB; unaligned tensors are copied."""
+    for gap in (0, 1):
+        p = Problem(3, 8192, 32768, dtype, gap=gap)
+        dx, *dw = p.backward(grad_dtype=torch.float32)
+        check_weights(p, dw)
+        del dw
+        w_a, w_b, w_o = (w.double() for w in p.w)
+        x, dy = p.x.double(), p.dy.double()
+        a, b, dh = x @ w_a.T, x @ w_b.T, dy @ w_o
+        s = torch.sigmoid(a)
+        want = (a * s * b) @ w_o.T, (dh * b * (s * (1 + a * (1 - s)))) @ w_a + (dh * (a * s)) @ w_b
+        # as in check_weights, for sums of 32768 terms behind sums of 8192, and the results' own rounding
+        bound = (8 * 32768 ** 0.5 + 64) * T.U + (2 * HALF[p.x.dtype] if dtype == "bf16" else 0.0)
+        for name, got, exact in zip(("y", "dx"), (p.forward(), dx), want):
+            off = (got.double() - exact).norm() / exact.norm()
+            print(f"{name} {dtype} gap {gap}: {off:.2e} of {bound:.2e}", flush=True)
+            assert off <= bound, name
+        del w_a, w_b, w_o
