@@ -409,7 +409,8 @@ typedef struct {
 size_t ff_gated_transition_forward_workspace_bytes(const ff_transition_desc* desc);
 size_t ff_gated_transition_backward_workspace_bytes(const ff_transition_desc* desc);
 
-/*   x            [rows, c];  w_a, w_b [f, c];  w_o [c, f]: aligned to their type (fastest 16-byte aligned, c and f multiples of 16)
+/*   x            [rows, c];  w_a, w_b [f, c];  w_o [c, f]: aligned to their type.  Fastest 16-byte aligned: bfloat16 with c = 32, 64, 128, 192 or 256 and f a multiple
+ *                of 32, anything else with c and f multiples of 16.  Other sizes are padded in copies; bfloat16 with other c up to 256 also reads and writes its rows two bytes at a time
  *   residual     [rows, c] or NULL;  mask float32 [rows], 0 = masked, or NULL
  *   y            [rows, c]; may be residual itself, must not overlap x, a weight or the mask
  *   ws, ws_bytes device scratch, 256-byte aligned, at least the size above, that overlaps none of them

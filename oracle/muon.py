@@ -22,7 +22,7 @@ def _product(p, q, noise):
 
 
 def _held(z, noise):
-    """As a pair of float16 values of 256 times z: off by up to 2^-23 of z, 2^-24 or less in the mean, or by the smallest step, 2^-25 of a unit."""
+    """As a pair of float16 values of 256 times z (or more: X): off by up to 2^-23 of z, 2^-24 or less in the mean, or by half their smallest step, 2^-33."""
     return z if noise is None else z + (U * np.abs(z) + 2.0 ** -33) * noise.normal(size=z.shape)
 
 

@@ -4,7 +4,7 @@
 //
 // Three launches a step for all matrices together: A; B = b A + c A^2; X = a X + B X.  What is added behind a product is added in float32: with a I inside B the rounding of B's
 // diagonal, another one in each row, would carry the large singular directions into the small ones, which the next steps make larger (2048 x 2048: an
-// error of 3.2e-6 in norm instead of 1.3e-6; b I inside an operand of B's product likewise, 256 x 256 2.1e-6 instead of 2.0e-6).  Values are held as float16 pairs: 23
+// error of 3.5e-6 in norm instead of 2.3e-6, and more beside more exact sums; b I inside an operand of B's product does the same).  Values are held as float16 pairs: 23
 // significant bits, and three matrix instructions for a product where float32 ones would take sixteen times the time of one.  A and B are held times kScale, so that magnitudes to
 // 255 have a place and the smallest are 2^-32 apart.  X is held times a power of two of its own in each step, from a bound of its norm: an update far below eps is a
 // small X, of which a fixed factor would leave few bits or none (at 10^-5 eps, times 256: an error of 2e-3), and large matrices have small values.  With the usual coefficients singular
@@ -178,7 +178,7 @@ __device__ __forceinline__ Spot spot_of(const Matrix& x, int64_t i) {
 __device__ __forceinline__ float update_of(float m, float g, const StepArgs& a) { return a.nesterov ? a.beta * m + a.rest * g : m; }
 
 // m = beta m + (1 - beta) k g, and the sum of squares of the update, in float64.  MUON false: of g itself.  Bound by HBM: 48 blocks' 79 M values
-// in matrices beyond 128 x 128, bfloat16 gradients, 137 us for 770 MB, 5.6 TB/s.
+// in matrices beyond 128 x 128, bfloat16 gradients, 135 us for 770 MB, 5.7 TB/s.
 template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_momentum(Table t, StepArgs a, const float* norm, double* partial) {
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -216,7 +216,7 @@ template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_muon_m
 
 __device__ __forceinline__ float* factors_of(const Matrix& x, char* ws) { return (float*)(ws + x.ws); }
 
-// X = update / (norm + eps) as pairs, its padding zeros, and its factors.  Bound by HBM likewise: 158 us for 770 MB.  (The update is formed again: it would be another 4 bytes a value.)
+// X = update / (norm + eps) as pairs, its padding zeros, and its factors.  Bound by HBM likewise: 159 us for 770 MB.  (The update is formed again: it would be another 4 bytes a value.)
 template <typename G, bool MUON> __global__ __launch_bounds__(256) void k_ns_start(Table t, StepArgs a, const float* norm, const double* partial, char* ws, int steps) {
     const Place at = place_at(t, blockIdx.x);
     if (at.matrix < 0) return;
@@ -266,7 +266,7 @@ template <int TILE_, int BK, int STAGES, int BLOCKS> struct Cores {
 };
 // Three stages of 16 k leave room for three blocks on a compute unit, whose ends then overlap with the others' products.  Where a launch has fewer blocks than there are
 // units a block stands alone with what a stage costs it, a barrier and the reads behind it, so that stages of 32 k are better (orthogonalising 4096 x 1024: eight of 16 k
-// 434 us, five of 32 383, four 374; of 64 k for the smaller tiles 390).  Fewer blocks still, and tiles of 64 fill four times the units.
+// 434 us, five of 32 383, four 374; of 64 k for the smaller tiles 390: all while the ends read no A and no X; 391 now).  Fewer blocks still, and tiles of 64 fill four times the units.
 typedef Cores<128, 16, 3, 3> Many;
 typedef Cores<128, 32, 4, 1> Some;
 typedef Cores<64, 32, 4, 2> Few;
@@ -289,8 +289,8 @@ __device__ __forceinline__ void store_gram(char* a, int64_t np, int64_t m, int64
     if (m < np && n < np) store_pairs(a + pairs_at(m * np + n), v);
 }
 
-// A.  SPLIT: sums over a part of k each, for k_ns_join.  48 blocks: 127 us for 2016 tiles, the matrix units 0.38 busy, 480 MB through HBM at 3.7 TB/s: k is 256 long for most tiles, so a third is
-// the way in and out.  4096 x 1024: 136 tiles of 64 in three parts each 26 us and 6 for the join.
+// A.  SPLIT: sums over a part of k each, for k_ns_join.  48 blocks: 126 us for 2016 tiles, the matrix units 0.38 busy, 480 MB through HBM at 3.7 TB/s: k is 256 long for most tiles, so a third is
+// the way in and out.  4096 x 1024: 136 tiles of 64 in three parts each 25 us and 5 for the join.
 template <class C, bool SPLIT> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_gram(Table t, char* ws, int step, float* parts) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256) void k_ns_join(Table t, char* ws, int step, co
     }
 }
 
-// B = b A + c A^2.  48 blocks 109 us for 490 MB; 4096 x 1024 15 us, 32 stages of 32 k in a row by half the units.
+// B = b A + c A^2.  48 blocks 107 us for 490 MB; 4096 x 1024 15 us, 32 stages of 32 k in a row by half the units.
 template <class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_poly(Table t, char* ws, StepArgs a) {
     typedef typename C::Straight Straight;
     constexpr int kTile = C::TILE;
@@ -409,7 +409,8 @@ template <int LAST, typename P> __device__ __forceinline__ void finish(const Mat
         tile::store_some(p, left, w);
     }
 }
-// X = a X + B X (a X + X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights.  48 blocks 200 us for 785 MB (the last, with weights and masters, 283 for 1.25 GB);
+// X = a X + B X (a X + X B where a matrix is tall); the last step's goes to the caller: as it is, or into the weights.  48 blocks 223 us for 1.05 GB, of which 270 MB are X once more for the end (the last, with
+// weights and masters, 299 for 1.51 GB);
 // 4096 x 1024 36 us, 256 tiles, one a unit, 23 of them matrix instructions at the rate of a large product.
 template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kBlocks) void k_ns_apply(Table t, char* ws, int step, StepArgs a, const float* norm) {
     typedef typename C::Straight Straight;
@@ -451,8 +452,8 @@ template <int LAST, typename P, class C> __global__ __launch_bounds__(256, C::kB
 // ---- small matrices: everything in one block ---------------------------------------------------
 // A matrix of at most SIZE x SIZE stays in LDS from its momentum to its weights: X and A (then B in A's place) as pairs in rows of SIZE values, a product's
 // results in registers between two barriers.  A wavefront has one 32 x 32 tile of the result (SIZE 64), or two beside each other (SIZE 128).
-// Bound by the chain of 3 steps dependent products, each a barrier, reads from LDS, 3 k / 16 matrix instructions in a row and the rounding into pairs: one 128 x 64 29 us (1.9 a product),
-// where the other path needs seventeen launches; 1200 matrices of up to 128 x 128 on 256 units 400 us, the matrix units 0.30 busy.
+// Bound by the chain of 3 steps dependent products, each a barrier, reads from LDS, 3 k / 16 matrix instructions in a row and the rounding into pairs: one 128 x 64 31 us (2.0 a product),
+// where the other path needs seventeen launches; 1200 matrices of up to 128 x 128 on 256 units 420 us, the matrix units 0.29 busy.
 template <int SIZE> struct Small {
     static constexpr int kWaves = SIZE == 128 ? 8 : 4, kThreads = 64 * kWaves, kUnits = SIZE == 128 ? 2 : 1;
     static constexpr int W = SIZE / 4, kImage = SIZE * SIZE * 4, kLds = 2 * kImage;

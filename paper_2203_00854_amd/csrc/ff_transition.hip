@@ -24,7 +24,8 @@ template <> struct OpOf<float> { typedef F32 type; };
 template <> struct OpOf<bf16_t> { typedef Bf16 type; };
 
 // ---- activations -------------------------------------------------------------------------
-// In float32 with the library's functions; for bfloat16 results the sigmoid by the machine's exponential and reciprocal (2^-22 of it, against 2^-9)
+// In float32 with the library's functions; for bfloat16 results the sigmoid by the machine's exponential and reciprocal: off by (1.5 |a| + 5) 2^-24 of it (log2 e and the product with
+// it are rounded, which the exponential multiplies by |a|; a step for it, half a one for the sum, a step for the reciprocal), against the results' 2^-8
 template <bool FAST> __device__ __forceinline__ float sigmoid_of(float a) {
     if constexpr (FAST) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * a));
     return 1.f / (1.f + expf(-a));
@@ -272,8 +273,8 @@ template <class C, typename T, int ACT> __global__ __launch_bounds__(C::kThreads
 
 // The same with rows in registers (bfloat16, up to 256 channels), and dx with them: a^T, b^T and dh^T = Wo^T dy^T of 32 hidden channels leave a lane with sixteen neighbours
 // of each, from which da, db and h are stored and dx^T += Wa^T da^T + Wb^T db^T goes on.  The weights' other sides are read turned from the same stage.
-// Bound by its stores, 6 f bytes a row (701 x 701 x 128 with 512 hidden channels 585 us, 2.1 GB), and by two wavefronts a SIMD, which the registers of x, dy and dx allow: the matrix units are 0.36 busy.
-// Without the stores the weights' gradients would need a, b and dh once more, 6 of 16 parts of the work.
+// Its stores, 6 f bytes a row, and two wavefronts a SIMD, which the registers of x, dy and dx allow: 701 x 701 x 128 with 512 hidden channels 585 us, 2.1 GB at 3.6 TB/s of the 5.0 that a
+// copy reaches and the matrix units 0.36 busy, so neither is full.  Without the stores the weights' gradients would need a, b and dh once more, 6 of 16 parts of the work.
 struct GradRowsArgs {
     const bf16_t *x, *dy;
     const char *w_a, *w_b, *w_o;
@@ -385,8 +386,8 @@ struct WeightArgs {
     uint32_t ftiles, ctiles;
     int32_t add;                  // to what an earlier chunk left
 };
-// Sums over rows: both operands lie with the rows as k.  The rows are split over blocks, whose sums are joined in a fixed order.  Bound by HBM where rows are many: 701 x 701 x 128
-// with 512 hidden channels 407 us for 1.7 GB, da, db and h read once by tiles of 256 x 128; 128 x 256 x 256 with 1024 67 us and 16 for the join of 20 parts, 61 MB of
+// Sums over rows: both operands lie with the rows as k.  The rows are split over blocks, whose sums are joined in a fixed order.  Where rows are many da, db and h
+// are read once by tiles of 256 x 128: 701 x 701 x 128 with 512 hidden channels 407 us for 1.7 GB, 4.3 TB/s, the matrix units 0.27 busy; 128 x 256 x 256 with 1024 67 us and 16 for the join of 20 parts, 61 MB of
 // sums that the 240 blocks' accumulators are.  Float32, 18000 x 173: 163 us, the matrix units 0.71 busy.
 template <class C> __global__ __launch_bounds__(C::kThreads) void k_tr_weights(WeightArgs a) {
     extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
@@ -467,7 +468,6 @@ int rows_tiles(const ff_transition_desc& d, bool backward) {
 struct Sizes {
     int esz;
     int64_t cp, fp, chunk;         // padded channels; rows worked on at a time, a multiple of 128
-    int64_t chunks;
     size_t weight;                 // bytes of a packed weight
     size_t tokens, hidden;         // bytes of a chunk's packed x and of its hidden tensor
     bool wide;                     // tiles of 256 in the weights' gradients
@@ -483,7 +483,6 @@ Sizes sizes_of(const ff_transition_desc& d, bool backward) {
     s.fp = round_up(d.f, kc ? 32 : kPad);
     const int64_t most = std::max<int64_t>(128, kHiddenBytes / (std::max(s.fp, s.cp) * s.esz) / 128 * 128);
     s.chunk = std::min(most, round_up(std::max<int64_t>(d.rows, 1), 128));
-    s.chunks = (d.rows + s.chunk - 1) / s.chunk;
     s.weight = align256((size_t)s.fp * s.cp * s.esz);
     s.tokens = align256((size_t)s.chunk * s.cp * s.esz);
     s.hidden = align256((size_t)s.chunk * s.fp * s.esz);
