@@ -139,9 +139,10 @@ __device__ __forceinline__ float factor_of(float bound) {
     return __uint_as_float((uint32_t)(127 + (e < 8 ? 8 : e > 120 ? 120 : e)) << 23);
 }
 constexpr float kRoom = 1.f + 1.f / 256.f;       // for roundings of the bound and of X
-// of X = G by, by = 1 / (norm + eps).  Where both are 0 so is G, and its X is 0 as with any other eps: 0 / 0 would turn the weights of a matrix that has no gradient yet into NaN.
+// of X = G by, by = 1 / (norm + eps).  A matrix of zeros is its own X, whatever eps is: 1 / 0, or the inverse of an eps below 2^-1024, is infinite and 0 times it NaN, which would reach
+// the weights of a matrix that has no gradient yet.
 __device__ __forceinline__ float first_bound(double norm, double eps, double& by) {
-    by = norm + eps == 0. ? 0. : 1. / (norm + eps);
+    by = norm == 0. ? 0. : 1. / (norm + eps);
     return (float)(norm * by) * kRoom;
 }
 __device__ __forceinline__ float next_bound(float bound, const StepArgs& a) {

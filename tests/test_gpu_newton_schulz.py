@@ -148,3 +148,10 @@ def test_a_step_without_a_gradient_and_without_eps(param):
             # 0.125 w is exact, and the difference has one rounding
             assert torch.equal(after, (was.double() * 0.875).to(after.dtype))
         assert not any(t.any() for t in m)
+
+
+@pytest.mark.parametrize("eps", [0.0, 5e-324, 1e-310, 1e-300, 1e300])
+def test_zeros_beside_any_eps(eps):
+    """Also one whose inverse is no number."""
+    for rows, cols in ((20, 10), (128, 90), (200, 300)):
+        assert not P.ff_orthogonalise(torch.zeros(2, rows, cols, device=DEV), eps=eps).any()
